@@ -489,6 +489,112 @@ int kkm_peak_read_rows(kkm_ctx *ctx, const void *buf, int64_t nrows, int64_t ld,
                        int32_t nchunks, int32_t seg, float *sums, int32_t reps, float *ms_out);
 int kkm_peak_mfma(kkm_ctx *ctx, int32_t iters, float *out, int32_t reps, float *ms_out, double *flops_out);
 
+/* ---- A model that learns from a clustering ----------------------------------
+ *
+ * Exact kernel K-means gives ids to the points it was run on; a new point's
+ * distances would need K against all of them.  These operators train a model
+ * that answers for new points, and are what such a model ends in: layer norm
+ * of its features, a linear head with a logit per class, and two losses on it,
+ * cross entropy with the ids and distillation from a teacher's top logits (of
+ * another model, or -D/tau of a point's nearest clusters).
+ *
+ * All of them are asynchronous on the context's stream, need no build, and do
+ * not touch a built K.  Their scratch belongs to the context: it is allocated
+ * when a call needs more than an earlier one did (that call waits for the
+ * device), counts against the budget, and is given back by the next build and
+ * by kkm_destroy.  Matrices are row-major with a row stride (ld, in elements)
+ * of at least their width; ids and fp32 vectors are contiguous.  Every sum,
+ * statistic and softmax is held in fp32, and results are rounded once, to
+ * nearest even, to the type of the matrix they are written to.  Calls give the
+ * same bits for the same inputs.  Errors: KKM_ERR_ARG, KKM_ERR_OOM (scratch),
+ * KKM_ERR_HIP. */
+typedef enum kkm_type { KKM_F32 = 0, KKM_F16 = 1, KKM_BF16 = 2 } kkm_type;
+#define KKM_MAX_TOP 256        /* pairs of a distillation target's row */
+#define KKM_MAX_FEATURES (1 << 20) /* d of these operators */
+#define KKM_MAX_ROWS (1 << 21) /* n and classes of the head, n * m below 2^31 */
+
+/* Layer norm of the n rows of x, d wide:
+ *   mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), y = (x - mu) r weight + bias.
+ * weight and bias hold d values of type wtype (KKM_F32 or x's type); NULL
+ * stands for ones and for zeros.  mean and rstd (fp32[n]) take mu and r for the
+ * gradient; each may be NULL.  y may be x (with ldy = ldx).  n = 0 does nothing. */
+int kkm_layer_norm(kkm_ctx *ctx, int32_t type, int64_t n, int32_t d, const void *x, int64_t ldx, int32_t wtype,
+                   const void *weight, const void *bias, float eps, void *y, int64_t ldy, float *mean, float *rstd);
+
+/* Its gradient from dy, with mean and rstd of the forward call: with
+ * xh = (x - mu) r and g = dy weight,
+ *   dx = r (g - mean g - xh mean(g xh)), dweight = sum_i dy xh, dbias = sum_i dy.
+ * dx, dweight and dbias may each be NULL; dx may be dy or x (same stride).
+ * n = 0 writes zeros to dweight and dbias. */
+int kkm_layer_norm_grad(kkm_ctx *ctx, int32_t type, int64_t n, int32_t d, const void *x, int64_t ldx, int32_t wtype,
+                        const void *weight, const float *mean, const float *rstd, const void *dy, int64_t lddy,
+                        void *dx, int64_t lddx, void *dweight, void *dbias);
+
+/* The head: logits z(i, v) = scale h_i . w_v + offset_v of n rows of h and
+ * `classes` rows of w, d wide, both of one type.  offset (fp32[classes], may be
+ * NULL) is a constant, e.g. the log of the clusters' sizes; -inf leaves a class
+ * out: it has no probability, its row of w is not looked at (it may hold NaN)
+ * and its gradient is zero.  The logits are never stored.  fp32 operands are
+ * taken as three bfloat16 parts, 24 bits together; an infinite entry of theirs
+ * gives NaN. */
+typedef struct kkm_head {
+  int32_t type; /* kkm_type of h, w and their gradients */
+  int32_t d;
+  int64_t n, classes;
+  const void *h;
+  int64_t ldh;
+  const void *w;
+  int64_t ldw;
+  const float *offset;
+  float scale;
+} kkm_head;
+
+/* Softmax cross entropy with ids (int32[n]):
+ *   lse_i = log sum_v exp z(i, v),  loss_i = lse_i - z(i, ids_i)
+ * into loss and lse (fp32[n]).  A negative id is a row without a label: its
+ * loss is 0.  An id >= classes gives NaN.  An id that is left out gives +inf. */
+int kkm_head_loss(kkm_ctx *ctx, const kkm_head *head, const int32_t *ids, float *loss, float *lse);
+
+/* The loss as above and the gradient of sum_i dloss_i loss_i (dloss: fp32[n],
+ * e.g. 1/n) by h and w:
+ *   G(i, v) = dloss_i scale (exp(z(i, v) - lse_i) - [v = ids_i]),  dh = G w,  dw = G^T h
+ * into dh (n x d) and dw (classes x d); each may be NULL.  G is held in 16 bits
+ * (fp32 operands: in three parts) for pieces of the classes.  Rows without a
+ * label or with dloss_i = 0 take no part: whatever they hold, their row of dh
+ * is zero.  In a row whose target is left out G is zero there. */
+int kkm_head_grad(kkm_ctx *ctx, const kkm_head *head, const int32_t *ids, const float *dloss, float *loss, float *lse,
+                  void *dh, int64_t lddh, void *dw, int64_t lddw);
+
+/* A teacher's top m logits per row: classes ids (int32[n x m]) and their logits
+ * (fp32[n x m]), of which the target is q = softmax(scale logits) over the
+ * row's pairs; a pair of a negative id or a logit of -inf is none.  A class
+ * named twice counts with both. */
+typedef struct kkm_teacher {
+  const int32_t *ids;
+  const float *logits;
+  int32_t m;
+  float scale; /* 1 / temperature */
+} kkm_teacher;
+
+/* Distillation: loss_i = sum_j q_j (log q_j - z(i, id_j) + lse_i), the
+ * divergence of the head's distribution from q; a row without a pair has loss
+ * 0.  Ids as for kkm_head_loss.  With the temperature 1/s on both sides set the
+ * scale of the head too; the usual factor T^2 goes into dloss. */
+int kkm_distill_loss(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teacher, float *loss, float *lse);
+
+/* The loss as above and, as kkm_head_grad, the gradient:
+ *   G(i, v) = dloss_i scale (exp(z(i, v) - lse_i) - sum_{j: id_j = v} q_j). */
+int kkm_distill_grad(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teacher, const float *dloss, float *loss,
+                     float *lse, void *dh, int64_t lddh, void *dw, int64_t lddw);
+
+/* The checks of these calls that need no context: KKM_OK or KKM_ERR_ARG (the
+ * message from kkm_last_error(NULL)).  teacher may be NULL. */
+int kkm_check_norm_args(int32_t type, int64_t n, int32_t d, int64_t ldx, int32_t wtype, float eps);
+int kkm_check_head_args(const kkm_head *head, const kkm_teacher *teacher);
+
+/* The stream of kkm_create. */
+int kkm_get_stream(kkm_ctx *ctx, void **out);
+
 int kkm_abi_version(void);
 
 #ifdef __cplusplus

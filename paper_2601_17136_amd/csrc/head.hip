@@ -1,0 +1,772 @@
+// A class head's losses and their gradients, the logits never stored.
+//
+//   z(i, v) = scale h_i . w_v + offset_v,   lse_i = log sum_v exp z(i, v)
+//   loss_i = sum_j q_j (log q_j - z(i, id_j) + lse_i)      over the row's pairs (id_j, q_j)
+//   G(i, v) = dloss_i scale (exp(z(i, v) - lse_i) - sum_{j: id_j = v} q_j)
+//   dH = G W,   dW = G^T H
+//
+// Forward: scores_kernel multiplies 16-bit tiles on the matrix cores and keeps
+// of a tile each row's largest logit and sum of exponentials; targets_kernel
+// joins them to lse, takes the few logits of the row's targets as plain dot
+// products, and writes the loss.  Gradient: pieces of the classes, as many as
+// keep G below kPieceBytes; of a piece the scores are computed again and G is
+// written in both orders, fix_kernel puts the targets' entries in place, and
+// two products give the piece's rows of dW and its part of dH.
+//
+// Operands are 16 bits with the contraction index contiguous.  Rows of binary16
+// and bfloat16 that are aligned to 16 bytes serve in place; others are copied.
+// fp32 is split into three bfloat16 planes (head_tile.h).  The gradient's
+// products take copies of W and H with the other index contiguous, in which
+// classes left out and rows without a target are zero, so that nothing that
+// stands there (an infinity, a NaN) reaches a sum.
+#include <algorithm>
+
+#include "head_tile.h"
+#include "model_ops.h"
+
+namespace kkm {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr size_t kPieceBytes = (size_t)256 << 20;
+constexpr int kMaxParts = 64;          // workgroups of max_dloss_kernel
+constexpr float kHalfScale = 16384.f;  // binary16 G: probabilities to 4e-9 keep all their bits
+
+__device__ inline float pow2_at_least(float v) {  // v >= 0, or infinite or NaN
+  if (!(v > 0.f) || isinf(v)) return v;
+  int e;
+  const float m = frexpf(v, &e);
+  return ldexpf(1.f, m == 0.5f ? e - 1 : e);
+}
+
+// ------------------------------------------------------------------ operands
+
+template <typename E, int P>
+__device__ inline void split_planes(float x, E (&out)[P]) {
+  out[0] = (E)x;
+  if constexpr (P == 3) {
+    const bool fin = isfinite((float)out[0]);
+    const float r = fin ? x - (float)out[0] : 0.f;
+    out[1] = (E)r;
+    out[2] = (E)(r - (float)out[1]);
+  }
+}
+
+// Rows in place of src's, kp wide (zero from d on), as P planes.  A thread
+// writes 8 values.
+template <typename XT, typename E, int P>
+__global__ __launch_bounds__(256) void stage_rows_kernel(const XT* __restrict__ src, int64_t ld, int64_t rows, int d,
+                                                         int kp, E* __restrict__ dst, int64_t plane) {
+  const int64_t per = kp / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * per) return;
+  const int64_t row = i / per;
+  const int c = (int)(i - row * per) * 8;
+  float v[8];
+  if constexpr (sizeof(XT) == 2) {
+    load_part(src + row * ld, c, d, v);
+  } else {
+    float a[4], b[4];
+    load_part(src + row * ld, c, d, a);
+    load_part(src + row * ld, c + 4, d, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+  }
+  frag<E> o[P];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    E pl[P];
+    split_planes<E, P>(v[e], pl);
+#pragma unroll
+    for (int p = 0; p < P; ++p) o[p][e] = pl[p];
+  }
+#pragma unroll
+  for (int p = 0; p < P; ++p) *(frag<E>*)(dst + p * plane + row * kp + c) = o[p];
+}
+
+// The transposed copy: dst[c][row], rp rows wide (zero from `rows` on).  A row
+// counts as zero where weight[row] is 0, or, LEFT_OUT, -inf.  A workgroup turns
+// a 64 x 64 block through LDS.
+template <typename XT, typename E, int P, bool LEFT_OUT>
+__global__ __launch_bounds__(256) void stage_cols_kernel(const XT* __restrict__ src, int64_t ld, int64_t rows, int d,
+                                                         const float* __restrict__ weight, int64_t rp,
+                                                         E* __restrict__ dst, int64_t plane) {
+  __shared__ float tile[64][65];
+  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  const int c0 = blockIdx.y * 64, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int k = wave; k < 64; k += 4) {
+    const int64_t row = r0 + k;
+    bool use = row < rows && c0 + lane < d;
+    if (use && weight) use = weight[row] != (LEFT_OUT ? -INFINITY : 0.f);
+    tile[k][lane] = use ? (float)src[row * ld + c0 + lane] : 0.f;
+  }
+  __syncthreads();
+  const int part = (threadIdx.x & 7) * 8;
+  for (int c = threadIdx.x >> 3; c < 64; c += 32) {
+    if (c0 + c >= d || r0 + part >= rp) continue;
+    frag<E> o[P];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      E pl[P];
+      split_planes<E, P>(tile[part + e][c], pl);
+#pragma unroll
+      for (int p = 0; p < P; ++p) o[p][e] = pl[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) *(frag<E>*)(dst + p * plane + (int64_t)(c0 + c) * rp + r0 + part) = o[p];
+  }
+}
+
+// ------------------------------------------------------------------ scores
+
+template <typename E>
+struct ScoreArgs {
+  Side w, h;
+  int64_t n;
+  int classes, v0;  // v0: first class of the piece
+  int K, nkc, nseg, mt, nt;
+  float zscale;         // scale log2 e
+  const float* offset;  // may be null
+  float2* part;         // forward: (largest, sum) in base 2 of each class tile and row, [tile][n]
+  // gradient: rows' lse in base 2 and factors, G [row][class of the piece] and its transpose
+  const float *lse2, *coef;
+  E *G, *Gt;
+  int64_t ldg, planeg, ldt, planet;
+};
+
+// Tile of classes (the matrix rows) by rows of H (the columns): a lane holds 16
+// classes a block of one row of H, so a row's largest and sum stay in a lane
+// up to one exchange and the wavefronts' sums in LDS.
+template <typename E, class S, int P, bool GRAD>
+__global__ __launch_bounds__(S::threads, 1) void scores_kernel(ScoreArgs<E> a) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  int mi, ni;
+  tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
+  const int64_t c0 = a.v0 + (int64_t)mi * S::BM, t0 = (int64_t)ni * S::BN;
+  floatx16 acc[S::WM][S::WN];
+  tile_product<E, S>(a.w, a.h, c0, t0, a.K, a.nkc, a.nseg, 0, a.nseg * a.nkc, lds, acc);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
+  // z in base 2; -inf where a class is left out, whatever its product
+#pragma unroll
+  for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t v = c0 + (wm * S::WM + bi) * 32 + 8 * q + 4 * h + e;
+        const float off = v >= a.classes ? -INFINITY : a.offset ? a.offset[v] * kLog2e : 0.f;
+#pragma unroll
+        for (int bj = 0; bj < S::WN; ++bj) {
+          const float z = fmaf(acc[bi][bj][4 * q + e], a.zscale, off);
+          acc[bi][bj][4 * q + e] = off == -INFINITY ? -INFINITY : z;
+        }
+      }
+  if constexpr (!GRAD) {
+    float2* red = (float2*)lds;  // [wm][column of the tile]
+#pragma unroll
+    for (int bj = 0; bj < S::WN; ++bj) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, acc[bi][bj][r]);
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      const float m0 = m == -INFINITY ? 0.f : m;
+      float s = 0.f;
+#pragma unroll
+      for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(acc[bi][bj][r] - m0);
+      s += __shfl_xor(s, 32, 64);
+      if (h == 0) red[wm * S::BN + (wn * S::WN + bj) * 32 + l32] = make_float2(m, s);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < S::BN; c += S::threads) {
+      if (t0 + c >= a.n) break;
+      float m = -INFINITY, s = 0.f;
+#pragma unroll
+      for (int g = 0; g < S::GM; ++g) m = fmaxf(m, red[g * S::BN + c].x);
+      const float m0 = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int g = 0; g < S::GM; ++g) {
+        const float2 v = red[g * S::BN + c];
+        s += v.y * __builtin_amdgcn_exp2f(v.x - m0);
+      }
+      a.part[(c0 / S::BM) * a.n + t0 + c] = make_float2(m, s);
+    }
+  } else {
+    const int64_t cl = c0 - a.v0;
+#pragma unroll
+    for (int bj = 0; bj < S::WN; ++bj) {
+      const int64_t t = t0 + (wn * S::WN + bj) * 32 + l32;
+      const float lse2 = t < a.n ? a.lse2[t] : 0.f, cf = t < a.n ? a.coef[t] : 0.f;
+#pragma unroll
+      for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t v = cl + (wm * S::WM + bi) * 32 + 8 * q + 4 * h;
+          typedef E e4 __attribute__((ext_vector_type(4)));
+          e4 o[P];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            // (a row without a target has no gradient, whatever its logits)
+            const float g = cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(acc[bi][bj][4 * q + e] - lse2);
+            E pl[P];
+            split_planes<E, P>(g, pl);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+              o[p][e] = pl[p];
+              a.Gt[p * a.planet + (v + e) * a.ldt + t] = pl[p];
+            }
+          }
+#pragma unroll
+          for (int p = 0; p < P; ++p) *(e4*)(a.G + p * a.planeg + t * a.ldg + v) = o[p];
+        }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ targets
+
+// Largest |dloss| of each workgroup's rows (binary16: G is kept in its range).
+__global__ __launch_bounds__(256) void max_dloss_kernel(const float* __restrict__ dloss, int64_t n,
+                                                        unsigned* __restrict__ parts) {
+  unsigned m = 0u;  // ordered as the floats are, NaN above all
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    m = max(m, __float_as_uint(dloss[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o, 64));
+  __shared__ unsigned red[4];
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) parts[blockIdx.x] = max(max(red[0], red[1]), max(red[2], red[3]));
+}
+
+struct TargetArgs {
+  const void *h, *w;
+  int64_t ldh, ldw, n;
+  int d, classes, m, ntiles;
+  float scale, tscale;
+  const float* offset;
+  const int32_t* ids;
+  const float* tlogits;
+  const float2* part;
+  float *loss, *lse;
+  // gradient
+  const float* dloss;
+  const unsigned* dparts;  // null: G holds dloss as it is
+  float *lse2, *coef, *alpha;
+  int32_t* fix_id;  // n x m
+  float* fix_val;
+};
+
+// One wavefront per row: joins the tiles' sums, takes the targets' logits, and
+// writes loss and lse; for the gradient also the row's factor and its entries
+// of G at the targets.
+template <typename XT, int NQ>
+__global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (i >= a.n) return;
+  float m = -INFINITY, s = 0.f;
+  for (int t = lane; t < a.ntiles; t += 64) {
+    const float2 v = a.part[(int64_t)t * a.n + i];
+    const float nm = fmaxf(m, v.x), n0 = nm == -INFINITY ? 0.f : nm;
+    s = s * __builtin_amdgcn_exp2f(m - n0) + v.y * __builtin_amdgcn_exp2f(v.x - n0);
+    m = nm;
+  }
+  float top = m;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const float top0 = top == -INFINITY ? 0.f : top;
+  s = wave_sum(s * __builtin_amdgcn_exp2f(m - top0));
+  const float lse2 = top + log2f(s);  // -inf where every class is left out
+
+  // the row's pairs, lane l holding l, l + 64, ..: id (-1: none), q
+  int id[NQ];
+  float q[NQ], z[NQ], tm = -INFINITY, ts = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    const int j = k * 64 + lane;
+    id[k] = j < a.m ? a.ids[i * a.m + j] : -1;
+    q[k] = id[k] < 0 ? -INFINITY : a.tlogits ? a.tscale * a.tlogits[i * a.m + j] : 0.f;
+    if (q[k] == -INFINITY) id[k] = -1;
+    if (id[k] >= a.classes) {
+      id[k] = -1;
+      bad = true;
+    }
+    tm = fmaxf(tm, q[k]);
+    z[k] = 0.f;
+  }
+  bad = __ballot(bad) != 0;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) tm = fmaxf(tm, __shfl_xor(tm, o, 64));
+  if (tm == -INFINITY) tm = 0.f;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    q[k] = id[k] < 0 ? 0.f : expf(q[k] - tm);
+    ts += q[k];
+  }
+  ts = wave_sum(ts);
+  const bool some = ts != 0.f;  // (a NaN among the teacher's logits stays one)
+  const float inv = some ? 1.f / ts : 0.f;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) q[k] *= inv;
+
+  // the targets' logits, four dot products at a time
+  const XT* hr = (const XT*)a.h + i * a.ldh;
+  for (int j0 = 0; j0 < a.m; j0 += 4) {
+    const XT* wr[4];
+    int idj[4];
+    bool any = false;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      idj[u] = -1;
+#pragma unroll
+      for (int k = 0; k < NQ; ++k)
+        if (j0 / 64 == k) idj[u] = __shfl(id[k], (j0 + u) & 63, 64);  // (4 divides 64: one k for all four)
+      any |= idj[u] >= 0;
+      wr[u] = (const XT*)a.w + (int64_t)max(idj[u], 0) * a.ldw;
+    }
+    if (!any) continue;
+    float dot[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int c = lane * kVec<XT>; c < a.d; c += 64 * kVec<XT>) {
+      float hv[kVec<XT>];
+      load_part(hr, c, a.d, hv);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (idj[u] < 0) continue;  // (uniform)
+        float wv[kVec<XT>];
+        load_part(wr[u], c, a.d, wv);
+#pragma unroll
+        for (int e = 0; e < kVec<XT>; ++e) dot[u] = fmaf(hv[e], wv[e], dot[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (idj[u] < 0) continue;
+      const float off = a.offset ? a.offset[idj[u]] * kLog2e : 0.f;
+      const float zz = off == -INFINITY ? -INFINITY : fmaf(wave_sum(dot[u]), a.scale * kLog2e, off);
+#pragma unroll
+      for (int k = 0; k < NQ; ++k)
+        if (j0 / 64 == k && lane == ((j0 + u) & 63)) z[k] = zz;
+    }
+  }
+  float l = 0.f;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k)
+    if (q[k] != 0.f) {  // lse2 - z is +inf at a target that is left out, where every class is too
+      const float gap = z[k] == -INFINITY ? INFINITY : lse2 - z[k];
+      l += q[k] * (logf(q[k]) + gap * kLn2);
+    }
+  l = wave_sum(l);
+  if (lane == 0) {
+    a.loss[i] = bad ? __builtin_nanf("") : some ? l : 0.f;
+    a.lse[i] = lse2 * kLn2;
+  }
+  if (!a.coef) return;
+  float cf = a.dloss[i] * a.scale;
+  if (a.dparts) {
+    unsigned mx = a.dparts[lane];
+#pragma unroll
+    for (int o = 32; o; o >>= 1) mx = max(mx, (unsigned)__shfl_xor((int)mx, o, 64));
+    const float D = pow2_at_least(__uint_as_float(mx));
+    cf = D == 0.f ? 0.f : a.dloss[i] / D * kHalfScale;
+    if (i == 0 && lane == 0) *a.alpha = D / kHalfScale * a.scale;
+  }
+  if (!some || lse2 == -INFINITY) cf = 0.f;
+  if (bad) cf = __builtin_nanf("");
+  if (lane == 0) {
+    a.lse2[i] = lse2 == -INFINITY ? 0.f : lse2;
+    a.coef[i] = cf;
+  }
+  // the entries of G at the targets, a class named twice once
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    const int j = k * 64 + lane;
+    float qs = 0.f;
+    bool first = true;
+    for (int jj = 0; jj < a.m; ++jj) {
+      int ij = -1;
+      float qj = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < NQ; ++kk)
+        if (jj / 64 == kk) {
+          ij = __shfl(id[kk], jj & 63, 64);
+          qj = __shfl(q[kk], jj & 63, 64);
+        }
+      if (ij == id[k]) {
+        qs += qj;
+        if (jj < j) first = false;
+      }
+    }
+    if (j < a.m) {
+      a.fix_id[i * a.m + j] = first && cf != 0.f ? id[k] : -1;
+      a.fix_val[i * a.m + j] = z[k] == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z[k] - lse2) - qs);
+    }
+  }
+}
+
+template <typename E, int P>
+__global__ __launch_bounds__(256) void fix_kernel(const int32_t* __restrict__ id, const float* __restrict__ val,
+                                                  int64_t n, int m, int v0, int v1, E* __restrict__ G, int64_t ldg,
+                                                  int64_t planeg, E* __restrict__ Gt, int64_t ldt, int64_t planet) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x >= n * m) return;
+  const int v = id[x];
+  if (v < v0 || v >= v1) return;
+  const int64_t i = x / m;
+  E pl[P];
+  split_planes<E, P>(val[x], pl);
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    G[p * planeg + i * ldg + (v - v0)] = pl[p];
+    Gt[p * planet + (v - v0) * ldt + i] = pl[p];
+  }
+}
+
+// ------------------------------------------------------------------ products
+
+struct ProductArgs {
+  Side a, b;
+  int64_t M, N;
+  int K, nkc, nseg, mt, nt;
+  int per;              // chunks of a slab
+  float* slabs;         // fp32 sums, M x N each, or null: straight to out
+  int add;              // to what the slabs hold
+  void* out;
+  int64_t ldo;
+  const float* alpha;   // null: 1
+  const float* coef;    // rows of weight 0 are 0, whatever stands in b; null: none
+};
+
+template <typename E, typename OT, class S>
+__global__ __launch_bounds__(S::threads, 1) void product_kernel(ProductArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  int mi, ni;
+  tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
+  const int64_t r0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+  const int c0 = blockIdx.y * a.per, c1 = min(c0 + a.per, a.nseg * a.nkc);
+  floatx16 acc[S::WM][S::WN];
+  tile_product<E, S>(a.a, a.b, r0, n0, a.K, a.nkc, a.nseg, c0, c1, lds, acc);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
+  const float alpha = a.alpha ? *a.alpha : 1.f;
+  float* slab = a.slabs ? a.slabs + (int64_t)blockIdx.y * a.M * a.N : nullptr;
+#pragma unroll
+  for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int64_t row = r0 + (wm * S::WM + bi) * 32 + acc_row(r, h);
+      if (row >= a.M) continue;
+      const bool none = !slab && a.coef && a.coef[row] == 0.f;
+#pragma unroll
+      for (int bj = 0; bj < S::WN; ++bj) {
+        const int64_t col = n0 + (wn * S::WN + bj) * 32 + l32;
+        if (col >= a.N) continue;
+        if (slab) {
+          float* p = slab + row * a.N + col;
+          *p = a.add ? *p + acc[bi][bj][r] : acc[bi][bj][r];
+        } else {
+          ((OT*)a.out)[row * a.ldo + col] = (OT)(none ? 0.f : acc[bi][bj][r] * alpha);
+        }
+      }
+    }
+}
+
+template <typename OT>
+__global__ __launch_bounds__(256) void slabs_kernel(const float* __restrict__ slabs, int count, int64_t M, int64_t N,
+                                                    const float* __restrict__ alpha,
+                                                    const float* __restrict__ coef, OT* __restrict__ out,
+                                                    int64_t ldo) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x >= M * N) return;
+  float s = 0.f;
+  for (int k = 0; k < count; ++k) s += slabs[k * M * N + x];
+  const int64_t row = x / N;
+  out[row * ldo + (x - row * N)] = (OT)(coef && coef[row] == 0.f ? 0.f : s * (alpha ? *alpha : 1.f));
+}
+
+template <typename OT>
+__global__ __launch_bounds__(256) void zero_rows_kernel(OT* __restrict__ out, int64_t M, int64_t N, int64_t ldo) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x < M * N) out[x / N * ldo + x % N] = (OT)0.f;
+}
+
+// ------------------------------------------------------------------ plan
+
+int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int kPad = 256;  // G's rows and classes: whole tiles of any shape
+
+// (a tile's rows are reached by 32-bit offsets: kMaxStride)
+constexpr int64_t kMaxStride = (int64_t)1 << 21;
+bool in_place(const HeadArgs& a, const void* p, int64_t ld) {
+  return a.type != TYPE_F32 && a.d % 8 == 0 && ld % 8 == 0 && ld <= kMaxStride && (uintptr_t)p % 16 == 0;
+}
+
+// A product's slabs: enough workgroups for the chip where its tiles are few.
+int slab_count(int64_t tiles, int64_t chunks) {
+  const int64_t want = cdiv(256, tiles);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, chunks / 8, 32}));
+}
+
+struct HeadPlan {
+  int planes, nseg, kp;
+  int64_t n_pad, v_pad;
+  bool big;             // scores in 256 x 256 tiles
+  int bm, ntiles;
+  int piece;            // classes of a piece (a multiple of kPad)
+  int sh, sw;           // slabs of dH and dW (0: none)
+  bool bigh, bigw;
+  // workspace offsets
+  size_t h, w, part, ht, wt, lse2, coef, dparts, alpha, fix_id, fix_val, G, Gt, slabs_h, slabs_w, bytes;
+};
+
+HeadPlan plan_of(const HeadArgs& a, bool grad) {
+  HeadPlan p{};
+  p.planes = a.type == TYPE_F32 ? 3 : 1;
+  p.nseg = a.type == TYPE_F32 ? kSegs : 1;
+  p.kp = (int)up(a.d, kChunkK);
+  p.n_pad = up(a.n, kPad);
+  p.v_pad = up(a.classes, kPad);
+  p.big = cdiv(a.n, 256) * cdiv(a.classes, 256) >= 192;
+  p.bm = p.big ? 256 : 128;
+  p.ntiles = (int)cdiv(a.classes, p.bm);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t r = at;
+    at += up(bytes, 1024);
+    return r;
+  };
+  if (!in_place(a, a.h, a.ldh)) p.h = take((size_t)p.planes * a.n * p.kp * 2);
+  if (!in_place(a, a.w, a.ldw)) p.w = take((size_t)p.planes * a.classes * p.kp * 2);
+  p.part = take((size_t)p.ntiles * a.n * 8);
+  if (grad) {
+    p.piece = (int)std::min<int64_t>(p.v_pad, std::max<int64_t>(kPad, kPieceBytes / ((size_t)p.planes * p.n_pad * 2) /
+                                                                          kPad * kPad));
+    p.ht = take((size_t)p.planes * a.d * p.n_pad * 2);
+    p.wt = take((size_t)p.planes * a.d * p.v_pad * 2);
+    p.lse2 = take((size_t)a.n * 4);
+    p.coef = take((size_t)a.n * 4);
+    p.dparts = take(kMaxParts * 4);
+    p.alpha = take(4);
+    p.fix_id = take((size_t)a.n * a.m * 4);
+    p.fix_val = take((size_t)a.n * a.m * 4);
+    p.G = take((size_t)p.planes * p.n_pad * p.piece * 2);
+    p.Gt = take((size_t)p.planes * p.n_pad * p.piece * 2);
+    const int64_t pieces = cdiv(a.classes, p.piece);
+    auto shape = [&](int64_t M, int64_t N, int64_t chunks, bool& big) {
+      big = cdiv(M, 256) * cdiv(N, 256) >= 192;
+      const int b = big ? 256 : 128;
+      return slab_count(cdiv(M, b) * cdiv(N, b), chunks);
+    };
+    p.sh = shape(a.n, a.d, p.nseg * cdiv(std::min<int64_t>(p.piece, a.classes), kChunkK), p.bigh);
+    p.sw = shape(std::min<int64_t>(p.piece, a.classes), a.d, p.nseg * cdiv(a.n, kChunkK), p.bigw);
+    if (p.sh == 1 && pieces == 1) p.sh = 0;
+    if (p.sw == 1) p.sw = 0;
+    p.slabs_h = take((size_t)p.sh * a.n * a.d * 4);
+    p.slabs_w = take((size_t)p.sw * std::min<int64_t>(p.piece, a.classes) * a.d * 4);
+  }
+  p.bytes = at;
+  return p;
+}
+
+#define KKM_TRY(expr)                        \
+  do {                                       \
+    hipError_t e_ = (expr);                  \
+    if (e_ != hipSuccess) return e_;         \
+  } while (0)
+
+inline dim3 grid1(int64_t items) { return dim3((unsigned)cdiv(items, 256)); }
+
+template <typename XT, typename E, int P>
+struct Head {
+  const HeadArgs& a;
+  const HeadPlan& p;
+  char* ws;
+  hipStream_t s;
+
+  template <typename T>
+  T* at(size_t off) const { return (T*)(ws + off); }
+
+  hipError_t side(const void* src, int64_t ld, int64_t rows, size_t off, Side& out) const {
+    if (in_place(a, src, ld)) {
+      out = {src, ld, 0, rows};
+      return hipSuccess;
+    }
+    const int64_t plane = rows * p.kp;
+    hipLaunchKernelGGL((stage_rows_kernel<XT, E, P>), grid1(rows * (p.kp / 8)), dim3(256), 0, s, (const XT*)src, ld,
+                       rows, a.d, p.kp, at<E>(off), plane);
+    out = {at<E>(off), p.kp, plane, rows};
+    return hipGetLastError();
+  }
+
+  template <bool GRAD>
+  hipError_t scores(ScoreArgs<E> sa, int64_t classes) const {
+    sa.mt = (int)cdiv(classes, p.bm);
+    sa.nt = (int)cdiv(a.n, p.bm);
+    const dim3 grid((unsigned)((int64_t)sa.mt * sa.nt));
+    if (p.big)
+      hipLaunchKernelGGL((scores_kernel<E, BigTile, P, GRAD>), grid, dim3(BigTile::threads), 0, s, sa);
+    else
+      hipLaunchKernelGGL((scores_kernel<E, SmallTile, P, GRAD>), grid, dim3(SmallTile::threads), 0, s, sa);
+    return hipGetLastError();
+  }
+
+  // out (M x N) = A B^T over K, or its slabs where there are any
+  // (K0: the first piece's K, from which the slabs' shares are)
+  hipError_t product(Side x, Side y, int64_t M, int64_t N, int K, int K0, bool big, int slabs, float* slab, int add,
+                     void* out, int64_t ldo, const float* alpha, const float* coef) const {
+    ProductArgs pa{};
+    pa.a = x;
+    pa.b = y;
+    pa.M = M;
+    pa.N = N;
+    pa.K = K;
+    pa.nkc = (int)cdiv(K, kChunkK);
+    pa.nseg = p.nseg;
+    const int b = big ? 256 : 128;
+    pa.mt = (int)cdiv(M, b);
+    pa.nt = (int)cdiv(N, b);
+    pa.per = share(K0, slabs);
+    pa.slabs = slabs ? slab : nullptr;
+    pa.add = add;
+    pa.out = out;
+    pa.ldo = ldo;
+    pa.alpha = alpha;
+    pa.coef = coef;
+    const dim3 grid((unsigned)((int64_t)pa.mt * pa.nt), (unsigned)cdiv(pa.nkc * pa.nseg, pa.per));
+    if (big)
+      hipLaunchKernelGGL((product_kernel<E, XT, BigTile>), grid, dim3(BigTile::threads), 0, s, pa);
+    else
+      hipLaunchKernelGGL((product_kernel<E, XT, SmallTile>), grid, dim3(SmallTile::threads), 0, s, pa);
+    return hipGetLastError();
+  }
+
+  // chunks of a slab, and the slabs that a product of K wrote
+  int share(int K, int slabs) const { return (int)cdiv(cdiv(K, kChunkK) * p.nseg, std::max(slabs, 1)); }
+  int written(int K, int slabs) const { return (int)cdiv(cdiv(K, kChunkK) * p.nseg, share(K, slabs)); }
+
+  hipError_t sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, const float* coef,
+                 void* out, int64_t ldo) const {
+    hipLaunchKernelGGL((slabs_kernel<XT>), grid1(M * N), dim3(256), 0, s, slabs, count, M, N, alpha, coef,
+                       (XT*)out, ldo);
+    return hipGetLastError();
+  }
+
+  hipError_t run(bool grad) const {
+    ScoreArgs<E> sa{};
+    KKM_TRY(side(a.h, a.ldh, a.n, p.h, sa.h));
+    KKM_TRY(side(a.w, a.ldw, a.classes, p.w, sa.w));
+    sa.n = a.n;
+    sa.classes = a.classes;
+    sa.K = in_place(a, a.h, a.ldh) || in_place(a, a.w, a.ldw) ? a.d : p.kp;
+    sa.nkc = p.kp / kChunkK;
+    sa.nseg = p.nseg;
+    sa.zscale = a.scale * kLog2e;
+    sa.offset = a.offset;
+    sa.part = at<float2>(p.part);
+    KKM_TRY(scores<false>(sa, a.classes));
+
+    TargetArgs ta{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, p.ntiles, a.scale, a.tscale, a.offset,
+                  a.ids, a.tlogits, sa.part, a.loss, a.lse, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+    const float* alpha = nullptr;
+    if (grad) {
+      ta.dloss = a.dloss;
+      ta.lse2 = at<float>(p.lse2);
+      ta.coef = at<float>(p.coef);
+      ta.fix_id = at<int32_t>(p.fix_id);
+      ta.fix_val = at<float>(p.fix_val);
+      if (a.type == TYPE_F16) {
+        ta.dparts = at<unsigned>(p.dparts);
+        ta.alpha = at<float>(p.alpha);
+        alpha = ta.alpha;
+        hipLaunchKernelGGL(max_dloss_kernel, dim3(kMaxParts), dim3(256), 0, s, a.dloss, a.n, at<unsigned>(p.dparts));
+        KKM_TRY(hipGetLastError());
+      }
+    }
+    const dim3 tg((unsigned)cdiv(a.n, 4));
+    if (a.m <= 64)
+      hipLaunchKernelGGL((targets_kernel<XT, 1>), tg, dim3(256), 0, s, ta);
+    else
+      hipLaunchKernelGGL((targets_kernel<XT, 4>), tg, dim3(256), 0, s, ta);
+    KKM_TRY(hipGetLastError());
+    if (!grad) return hipSuccess;
+
+    Side ht{at<E>(p.ht), p.n_pad, (int64_t)a.d * p.n_pad, a.d}, wt{at<E>(p.wt), p.v_pad, (int64_t)a.d * p.v_pad, a.d};
+    if (a.dw) {
+      hipLaunchKernelGGL((stage_cols_kernel<XT, E, P, false>),
+                         dim3((unsigned)cdiv(a.n, 64), (unsigned)cdiv(a.d, 64)), dim3(256), 0, s, (const XT*)a.h, a.ldh,
+                         a.n, a.d, ta.coef, p.n_pad, at<E>(p.ht), ht.plane);
+      KKM_TRY(hipGetLastError());
+    }
+    if (a.dh) {
+      hipLaunchKernelGGL((stage_cols_kernel<XT, E, P, true>),
+                         dim3((unsigned)cdiv(a.classes, 64), (unsigned)cdiv(a.d, 64)), dim3(256), 0, s,
+                         (const XT*)a.w, a.ldw, a.classes, a.d, a.offset, p.v_pad, at<E>(p.wt), wt.plane);
+      KKM_TRY(hipGetLastError());
+    }
+    sa.lse2 = ta.lse2;
+    sa.coef = ta.coef;
+    sa.G = at<E>(p.G);
+    sa.Gt = at<E>(p.Gt);
+    sa.ldg = p.piece;
+    sa.planeg = sa.planet = p.n_pad * p.piece;
+    sa.ldt = p.n_pad;
+    const int kn = (int)up(a.n, kChunkK);
+    const int kv0 = (int)up(std::min(p.piece, a.classes), kChunkK);
+    for (int v0 = 0; v0 < a.classes; v0 += p.piece) {
+      const int cnt = std::min(p.piece, a.classes - v0), kv = (int)up(cnt, kChunkK);
+      sa.v0 = v0;
+      KKM_TRY(scores<true>(sa, cnt));
+      hipLaunchKernelGGL((fix_kernel<E, P>), grid1(a.n * a.m), dim3(256), 0, s, ta.fix_id, ta.fix_val, a.n, a.m, v0,
+                         v0 + cnt, sa.G, sa.ldg, sa.planeg, sa.Gt, sa.ldt, sa.planet);
+      KKM_TRY(hipGetLastError());
+      if (a.dh) {
+        Side wv = wt;
+        wv.p = at<E>(p.wt) + v0;
+        KKM_TRY(product({sa.G, sa.ldg, sa.planeg, p.n_pad}, wv, a.n, a.d, kv, kv0, p.bigh, p.sh, at<float>(p.slabs_h),
+                        v0 > 0, a.dh, a.lddh, alpha, ta.coef));
+      }
+      if (a.dw) {
+        XT* dw = (XT*)a.dw + (int64_t)v0 * a.lddw;
+        KKM_TRY(product({sa.Gt, sa.ldt, sa.planet, p.piece}, ht, cnt, a.d, kn, kn, p.bigw, p.sw, at<float>(p.slabs_w), 0,
+                        dw, a.lddw, alpha, nullptr));
+        if (p.sw) KKM_TRY(sum(at<float>(p.slabs_w), written(kn, p.sw), cnt, a.d, alpha, nullptr, dw, a.lddw));
+      }
+    }
+    if (a.dh && p.sh) KKM_TRY(sum(at<float>(p.slabs_h), written(kv0, p.sh), a.n, a.d, alpha, ta.coef, a.dh, a.lddh));
+    return hipSuccess;
+  }
+};
+
+template <typename XT, typename E, int P>
+hipError_t launch_typed(const HeadArgs& a, bool grad, void* scratch, hipStream_t s) {
+  if (a.n == 0) {
+    if (grad && a.dw) {
+      hipLaunchKernelGGL((zero_rows_kernel<XT>), grid1((int64_t)a.classes * a.d), dim3(256), 0, s, (XT*)a.dw,
+                         a.classes, a.d, a.lddw);
+      return hipGetLastError();
+    }
+    return hipSuccess;
+  }
+  const HeadPlan p = plan_of(a, grad);
+  return Head<XT, E, P>{a, p, (char*)scratch, s}.run(grad);
+}
+
+}  // namespace
+
+size_t head_scratch(const HeadArgs& a, bool grad) { return a.n == 0 ? 0 : plan_of(a, grad).bytes; }
+
+hipError_t launch_head(const HeadArgs& a, bool grad, void* scratch, hipStream_t s) {
+  switch (a.type) {
+    case TYPE_F32: return launch_typed<float, bf16_t, 3>(a, grad, scratch, s);
+    case TYPE_F16: return launch_typed<half_t, half_t, 1>(a, grad, scratch, s);
+    default: return launch_typed<bf16_t, bf16_t, 1>(a, grad, scratch, s);
+  }
+}
+
+}  // namespace kkm

@@ -18,6 +18,7 @@
 
 #include "kkm.h"
 #include "kkm_internal.h"
+#include "model_ops.h"
 
 using namespace kkm;
 
@@ -209,6 +210,8 @@ struct kkm_ctx {
   int *sd_bestc = nullptr, *sd_centers = nullptr;
   double* sd_bsum[2] = {nullptr, nullptr};
 
+  std::vector<Alloc> model_allocs;  // workspace of the model operators (model_capi.cpp); builds give it back
+
   HostReport* report = nullptr;  // pinned host memory, from the first kkm_iterate or kkm_step on (may stay null)
   void* scratch = nullptr;  // this device's static scratch (kkm_iterate_noalloc)
 
@@ -369,7 +372,14 @@ void free_hist(kkm_ctx* c) {
   c->obj = nullptr;
 }
 
+void free_model(kkm_ctx* c) {
+  if (c->model_allocs.empty()) return;
+  (void)hipStreamSynchronize(c->stream);
+  release(c, c->model_allocs);
+}
+
 void free_build(kkm_ctx* c) {
+  free_model(c);
   free_ws(c);
   free_hist(c);
   free_seed(c);
@@ -730,6 +740,32 @@ int plan_impl(int64_t n, int32_t d, int32_t k, bool k_known, int32_t kind, size_
 }
 
 }  // namespace
+
+namespace kkm {
+
+hipStream_t ctx_stream(const kkm_ctx* c) { return c->stream; }
+
+int ctx_fail(kkm_ctx* c, int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(c, code, "%s", buf);
+}
+
+int ctx_workspace(kkm_ctx* c, size_t bytes, void** out) {
+  if (c->model_allocs.empty() || c->model_allocs[0].bytes < bytes) {
+    free_model(c);
+    void* p = nullptr;
+    int rc = dalloc(c, &p, bytes, c->model_allocs, "operator workspace");
+    if (rc) return rc;
+  }
+  *out = c->model_allocs[0].p;
+  return KKM_OK;
+}
+
+}  // namespace kkm
 
 extern "C" {
 

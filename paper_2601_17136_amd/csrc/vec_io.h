@@ -1,0 +1,68 @@
+// Element types of the model operators (fp32, binary16, bfloat16) and 16-byte
+// accesses to their rows at any element alignment.
+#pragma once
+#include "kkm_internal.h"
+
+namespace kkm {
+
+typedef __bf16 bf16_t;
+
+// Vector of 16 bytes of T whose address need only suit T: gfx950 takes global
+// loads and stores of any width at any address.
+template <typename T>
+constexpr int kVec = 16 / (int)sizeof(T);
+
+template <typename T>
+using raw_vec = T __attribute__((ext_vector_type(kVec<T>)));
+template <typename T>
+using any_vec = raw_vec<T> __attribute__((aligned(alignof(T))));
+
+template <typename T>
+__device__ inline void to_floats(const raw_vec<T>& r, float (&v)[kVec<T>]) {
+#pragma unroll
+  for (int e = 0; e < kVec<T>; ++e) v[e] = (float)r[e];
+}
+
+// Elements i .. i + kVec - 1 of a row of d, zero from d on.
+template <typename T>
+__device__ inline raw_vec<T> load_raw(const T* row, int i, int d) {
+  if (i + kVec<T> <= d) return *(const any_vec<T>*)(row + i);
+  raw_vec<T> r;
+#pragma unroll
+  for (int e = 0; e < kVec<T>; ++e) r[e] = i + e < d ? row[i + e] : (T)0.f;
+  return r;
+}
+template <typename T>
+__device__ inline void load_part(const T* row, int i, int d, float (&v)[kVec<T>]) {
+  to_floats<T>(load_raw(row, i, d), v);
+}
+
+// One rounding to T, to nearest even.
+template <typename T>
+__device__ inline void store_part(T* row, int i, int d, const float (&v)[kVec<T>]) {
+  if (i + kVec<T> <= d) {
+    raw_vec<T> r;
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e) r[e] = (T)v[e];
+    *(any_vec<T>*)(row + i) = r;
+  } else {
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e)
+      if (i + e < d) row[i + e] = (T)v[e];
+  }
+}
+
+// Elements i .. i + N - 1 of a vector of WT beside a vector of another type.
+template <int N, typename WT>
+__device__ inline void load_beside(const WT* w, int i, int d, float none, float (&v)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = w && i + e < d ? (float)w[i + e] : none;
+}
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+}  // namespace kkm

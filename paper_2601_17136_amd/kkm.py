@@ -19,6 +19,8 @@ KKM_OK, KKM_ERR_ARG, KKM_ERR_OOM, KKM_ERR_HIP, KKM_ERR_STATE, KKM_ERR_DEVICE_DAT
 KKM_LINEAR, KKM_POLY, KKM_GAUSS = 0, 1, 2
 KKM_MODE_AUTO, KKM_MODE_RESIDENT, KKM_MODE_ONTHEFLY, KKM_MODE_PACKED = 0, 1, 2, 3
 KKM_STORE_F32, KKM_STORE_F16 = 0, 1
+KKM_F32, KKM_F16, KKM_BF16 = 0, 1, 2
+KKM_MAX_TOP, KKM_MAX_FEATURES, KKM_MAX_ROWS = 256, 1 << 20, 1 << 21
 STORAGES = {"f32": KKM_STORE_F32, "f16": KKM_STORE_F16}
 KKM_MAX_K = 1024
 KKM_PACKED_MAX_K = 64
@@ -57,8 +59,21 @@ class kkm_info(ctypes.Structure):
                 ("r0", ctypes.c_int64), ("r1", ctypes.c_int64), ("c0", ctypes.c_int64), ("c1", ctypes.c_int64)]
 
 
+class kkm_head(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("d", ctypes.c_int32), ("n", ctypes.c_int64),
+                ("classes", ctypes.c_int64), ("h", ctypes.c_void_p), ("ldh", ctypes.c_int64),
+                ("w", ctypes.c_void_p), ("ldw", ctypes.c_int64), ("offset", ctypes.c_void_p),
+                ("scale", ctypes.c_float)]
+
+
+class kkm_teacher(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("logits", ctypes.c_void_p), ("m", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
 _lib = None
 _vp, _i32, _i64, _f64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
+_f32, _headp, _teacherp = ctypes.c_float, ctypes.POINTER(kkm_head), ctypes.POINTER(kkm_teacher)
 _SIGS = {
     "kkm_abi_version": ([], _i32),
     "kkm_last_error": ([_vp], ctypes.c_char_p),
@@ -91,6 +106,16 @@ _SIGS = {
     "kkm_peak_mfma": ([_vp, _i32, _vp, _i32, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(_f64)], _i32),
     "kkm_get_timing": ([_vp, ctypes.POINTER(kkm_timing)], _i32),
     "kkm_get_info": ([_vp, ctypes.POINTER(kkm_info)], _i32),
+    "kkm_layer_norm": ([_vp, _i32, _i64, _i32, _vp, _i64, _i32, _vp, _vp, _f32, _vp, _i64, _vp, _vp], _i32),
+    "kkm_layer_norm_grad": ([_vp, _i32, _i64, _i32, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp],
+                            _i32),
+    "kkm_head_loss": ([_vp, _headp, _vp, _vp, _vp], _i32),
+    "kkm_head_grad": ([_vp, _headp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64], _i32),
+    "kkm_distill_loss": ([_vp, _headp, _teacherp, _vp, _vp], _i32),
+    "kkm_distill_grad": ([_vp, _headp, _teacherp, _vp, _vp, _vp, _vp, _i64, _vp, _i64], _i32),
+    "kkm_check_norm_args": ([_i32, _i64, _i32, _i64, _i32, _f32], _i32),
+    "kkm_check_head_args": ([_headp, _teacherp], _i32),
+    "kkm_get_stream": ([_vp, ctypes.POINTER(_vp)], _i32),
 }
 
 
@@ -441,3 +466,185 @@ def kkm_get_info(ctx) -> dict:
     i = kkm_info()
     _check(lib().kkm_get_info(ctx, ctypes.byref(i)), ctx)
     return {f: getattr(i, f) for f, _ in kkm_info._fields_}
+
+
+# ------------------------------------------------------------------ a model that learns from a clustering
+
+def _type_code(dtype, name):
+    import torch
+    codes = {torch.float32: KKM_F32, torch.float16: KKM_F16, torch.bfloat16: KKM_BF16}
+    if dtype not in codes:
+        raise TypeError(f"{name} must have dtype float32, float16 or bfloat16, got {dtype}")
+    return codes[dtype]
+
+
+def _rows(t, name, dtype=None, shape=None):
+    """(address, row stride in elements) of a device matrix whose rows are contiguous."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix, got {t.dim()} dimensions")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    n, d = t.shape
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    ld = t.stride(0) if n > 1 else max(d, t.stride(0))
+    if ld < d:
+        raise ValueError(f"{name}'s rows overlap (stride {ld}, width {d})")
+    return t.data_ptr(), ld
+
+
+class _ordered:
+    """The context's stream as the place of the call's work: where torch's
+    current stream is another, the work waits for what that stream has enqueued,
+    that stream waits for the work, and the tensors' memory is held until then."""
+
+    def __init__(self, ctx, *tensors):
+        import torch
+        h = _vp()
+        _check(lib().kkm_get_stream(ctx, ctypes.byref(h)), ctx)
+        self.here = torch.cuda.current_stream()
+        self.there = None
+        if (h.value or 0) != self.here.cuda_stream:
+            self.there = torch.cuda.ExternalStream(h.value or 0) if h.value else torch.cuda.default_stream()
+            self.tensors = [t for t in tensors if t is not None]
+
+    def __enter__(self):
+        if self.there is not None:
+            self.there.wait_stream(self.here)
+
+    def __exit__(self, *exc):
+        if self.there is not None:
+            self.here.wait_stream(self.there)
+            for t in self.tensors:
+                t.record_stream(self.there)
+
+
+def kkm_layer_norm(ctx, x, weight, bias, eps: float, y, mean=None, rstd=None) -> None:
+    """Layer norm of the rows of x (n x d) into y; weight and bias (fp32 or x's
+    dtype) may be None.  mean and rstd (fp32[n]) take the statistics that the
+    gradient needs.  y may be x."""
+    import torch
+    px, ldx = _rows(x, "x")
+    n, d = x.shape
+    py, ldy = _rows(y, "y", x.dtype, (n, d))
+    wdt = _weight_dtype(x, weight, bias)
+    with _ordered(ctx, x, weight, bias, y, mean, rstd):
+        _check(lib().kkm_layer_norm(ctx, _type_code(x.dtype, "x"), n, d, px, ldx, _type_code(wdt, "weight"),
+                                    _dev_ptr(weight, wdt, "weight", d), _dev_ptr(bias, wdt, "bias", d), float(eps),
+                                    py, ldy, _dev_ptr(mean, torch.float32, "mean", n),
+                                    _dev_ptr(rstd, torch.float32, "rstd", n)), ctx)
+
+
+def _weight_dtype(x, *vectors):
+    import torch
+    for v in vectors:
+        if v is not None:
+            return v.dtype
+    return torch.float32
+
+
+def kkm_layer_norm_grad(ctx, x, weight, dy, mean, rstd, dx=None, dweight=None, dbias=None) -> None:
+    """The gradient of kkm_layer_norm from dy into dx, dweight and dbias (each
+    may be None; the last two have weight's dtype)."""
+    import torch
+    px, ldx = _rows(x, "x")
+    n, d = x.shape
+    pdy, lddy = _rows(dy, "dy", x.dtype, (n, d))
+    pdx, lddx = _rows(dx, "dx", x.dtype, (n, d)) if dx is not None else (None, d)
+    wdt = _weight_dtype(x, weight, dweight, dbias)
+    with _ordered(ctx, x, weight, dy, mean, rstd, dx, dweight, dbias):
+        _check(lib().kkm_layer_norm_grad(ctx, _type_code(x.dtype, "x"), n, d, px, ldx, _type_code(wdt, "weight"),
+                                         _dev_ptr(weight, wdt, "weight", d), _dev_ptr(mean, torch.float32, "mean", n),
+                                         _dev_ptr(rstd, torch.float32, "rstd", n), pdy, lddy, pdx, lddx,
+                                         _dev_ptr(dweight, wdt, "dweight", d), _dev_ptr(dbias, wdt, "dbias", d)), ctx)
+
+
+def _head_args(h, w, scale, offset):
+    import torch
+    ph, ldh = _rows(h, "h")
+    pw, ldw = _rows(w, "w", h.dtype)
+    n, d = h.shape
+    if w.shape[1] != d:
+        raise ValueError(f"w must be as wide as h ({d}), got {w.shape[1]}")
+    return kkm_head(_type_code(h.dtype, "h"), d, n, w.shape[0], ph, ldh, pw, ldw,
+                    _dev_ptr(offset, torch.float32, "offset", w.shape[0]), float(scale))
+
+
+def _teacher_args(n, top_ids, top_logits, teacher_scale):
+    import torch
+    if top_ids.dim() != 2 or top_ids.shape[0] != n:
+        raise ValueError(f"top_ids must be a matrix of {n} rows, got shape {tuple(top_ids.shape)}")
+    m = top_ids.shape[1]
+    return kkm_teacher(_dev_ptr(top_ids, torch.int32, "top_ids"),
+                       _dev_ptr(top_logits, torch.float32, "top_logits", n * m), m, float(teacher_scale))
+
+
+def _head_grads(h, w, dh, dw):
+    pdh, lddh = _rows(dh, "dh", h.dtype, h.shape) if dh is not None else (None, 0)
+    pdw, lddw = _rows(dw, "dw", h.dtype, w.shape) if dw is not None else (None, 0)
+    return pdh, lddh, pdw, lddw
+
+
+def kkm_head_loss(ctx, h, w, ids, loss, lse, scale: float = 1.0, offset=None) -> None:
+    """Softmax cross entropy of the logits scale * h w^T + offset with ids
+    (int32[n]; negative: no label) into loss and lse (fp32[n])."""
+    import torch
+    a, n, f32 = _head_args(h, w, scale, offset), h.shape[0], torch.float32
+    with _ordered(ctx, h, w, offset, ids, loss, lse):
+        _check(lib().kkm_head_loss(ctx, ctypes.byref(a), _dev_ptr(ids, torch.int32, "ids", n),
+                                   _dev_ptr(loss, f32, "loss", n), _dev_ptr(lse, f32, "lse", n)), ctx)
+
+
+def kkm_head_grad(ctx, h, w, ids, dloss, loss, lse, dh=None, dw=None, scale: float = 1.0, offset=None) -> None:
+    """kkm_head_loss, and the gradient of sum(dloss * loss) by h and w into dh and dw (each may be None)."""
+    import torch
+    a, n, f32 = _head_args(h, w, scale, offset), h.shape[0], torch.float32
+    g = _head_grads(h, w, dh, dw)
+    with _ordered(ctx, h, w, offset, ids, dloss, loss, lse, dh, dw):
+        _check(lib().kkm_head_grad(ctx, ctypes.byref(a), _dev_ptr(ids, torch.int32, "ids", n),
+                                   _dev_ptr(dloss, f32, "dloss", n), _dev_ptr(loss, f32, "loss", n),
+                                   _dev_ptr(lse, f32, "lse", n), *g), ctx)
+
+
+def kkm_distill_loss(ctx, h, w, top_ids, top_logits, loss, lse, scale: float = 1.0, offset=None,
+                     teacher_scale: float = 1.0) -> None:
+    """Divergence of softmax(scale * h w^T + offset) from the teacher's
+    softmax(teacher_scale * top_logits) over the classes top_ids (int32, n x m)."""
+    import torch
+    a, n, f32 = _head_args(h, w, scale, offset), h.shape[0], torch.float32
+    t = _teacher_args(n, top_ids, top_logits, teacher_scale)
+    with _ordered(ctx, h, w, offset, top_ids, top_logits, loss, lse):
+        _check(lib().kkm_distill_loss(ctx, ctypes.byref(a), ctypes.byref(t), _dev_ptr(loss, f32, "loss", n),
+                                      _dev_ptr(lse, f32, "lse", n)), ctx)
+
+
+def kkm_distill_grad(ctx, h, w, top_ids, top_logits, dloss, loss, lse, dh=None, dw=None, scale: float = 1.0,
+                     offset=None, teacher_scale: float = 1.0) -> None:
+    """kkm_distill_loss, and the gradient of sum(dloss * loss) by h and w into dh and dw (each may be None)."""
+    import torch
+    a, n, f32 = _head_args(h, w, scale, offset), h.shape[0], torch.float32
+    t = _teacher_args(n, top_ids, top_logits, teacher_scale)
+    g = _head_grads(h, w, dh, dw)
+    with _ordered(ctx, h, w, offset, top_ids, top_logits, dloss, loss, lse, dh, dw):
+        _check(lib().kkm_distill_grad(ctx, ctypes.byref(a), ctypes.byref(t), _dev_ptr(dloss, f32, "dloss", n),
+                                      _dev_ptr(loss, f32, "loss", n), _dev_ptr(lse, f32, "lse", n), *g), ctx)
+
+
+def kkm_check_norm_args(type_: int, n: int, d: int, ldx: int, wtype: int, eps: float) -> int:
+    return lib().kkm_check_norm_args(int(type_), int(n), int(d), int(ldx), int(wtype), float(eps))
+
+
+def kkm_check_head_args(head: kkm_head, teacher=None) -> int:
+    return lib().kkm_check_head_args(ctypes.byref(head), ctypes.byref(teacher) if teacher is not None else None)
+
+
+def kkm_get_stream(ctx) -> int:
+    """hipStream_t of the context (0: the default stream)."""
+    h = _vp()
+    _check(lib().kkm_get_stream(ctx, ctypes.byref(h)), ctx)
+    return h.value or 0
