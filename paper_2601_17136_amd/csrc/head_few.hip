@@ -1,0 +1,619 @@
+// The class head where one side of it is short: at most kFew classes, or at
+// most kFew rows of h.  The scores are then a matrix of S <= kFew columns, and
+// the work is to read h (or w) and write its gradient once, so no operand is
+// copied or padded: lanes load 16 bytes of a row each, in the shape the 16 x 16
+// matrix instructions take them, and every sum and G stay in fp32.
+//
+//   few classes:  scores_few (G = softmax less targets, [n][S])
+//                 dH = G W       rows_few    reads G and W, writes dH
+//                 dW = G^T H     cols_few    reads H once more
+//   few rows:     scores_few (the scores Z, [classes][S]), targets_few (lse, loss),
+//                 grad_few (Z becomes G^T)
+//                 dW = G^T H     rows_few    writes dW
+//                 dH = G W       cols_few    reads W once more
+//
+// (Z is S scores per class beside the d values of its row of w.)
+#include <algorithm>
+#include <type_traits>
+
+#include "model_ops.h"
+#include "vec_io.h"
+
+namespace kkm {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+// The products of 16 bytes of each row: a lane's elements of row lane % 16 at
+// k = kVec * (lane / 16) + e.  fp32: four instructions of 4 k each, one per e.
+__device__ inline floatx4 mfma_few(raw_vec<float> a, raw_vec<float> b, floatx4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+__device__ inline floatx4 mfma_few(raw_vec<half_t> a, raw_vec<half_t> b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ inline floatx4 mfma_few(raw_vec<bf16_t> a, raw_vec<bf16_t> b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+struct FewArgs {
+  const void *h, *w;
+  int64_t ldh, ldw, n;
+  int d, classes, m;
+  float zscale, scale, tscale;  // zscale: scale log2 e
+  const float* offset;
+  const int32_t* ids;
+  const float *tlogits, *dloss;
+  float *loss, *lse, *lse2, *coef;
+  float* C;       // G [n][S], or Z and G^T [classes][S]
+  float2* part;   // few rows: [class tile][n]
+  int32_t* fix_id;
+  float* fix_val;
+};
+
+// z in base 2 of CT x NT blocks of 16 classes by 16 rows of h into zs[row][class],
+// the workgroup's four wavefronts taking every fourth step of the features.
+// -inf where a class is left out or past the last.
+template <typename XT, int CT, int NT>
+__device__ inline void scores_block(const FewArgs& a, int64_t v0, int64_t t0, float (*zs)[NT * 16][CT * 16 + 1]) {
+  constexpr int VEC = kVec<XT>, KS = 4 * VEC, UN = CT * NT > 8 ? 1 : CT + NT > 4 ? 2 : 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const XT *pa[CT], *pb[NT];
+#pragma unroll
+  for (int i = 0; i < CT; ++i)
+    pa[i] = (const XT*)a.w + min(v0 + i * 16 + l16, (int64_t)a.classes - 1) * a.ldw;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) pb[i] = (const XT*)a.h + min(t0 + i * 16 + l16, a.n - 1) * a.ldh;
+  floatx4 acc[CT][NT];
+#pragma unroll
+  for (int i = 0; i < CT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  auto steps = [&](int s, auto whole) {
+    raw_vec<XT> fa[UN][CT], fb[UN][NT];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int k = (s + 4 * u) * KS + g * VEC;
+#pragma unroll
+      for (int i = 0; i < CT; ++i)
+        fa[u][i] = whole ? *(const any_vec<XT>*)(pa[i] + k) : load_raw(pa[i], k, a.d);
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        fb[u][i] = whole ? *(const any_vec<XT>*)(pb[i] + k) : load_raw(pb[i], k, a.d);
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+#pragma unroll
+      for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = mfma_few(fa[u][i], fb[u][j], acc[i][j]);
+  };
+  const int full = a.d / KS;
+  int s = wave;
+  for (; s + 4 * (UN - 1) < full; s += 4 * UN) steps(s, std::true_type{});
+  for (; s * KS < a.d; s += 4 * UN) steps(s, std::false_type{});
+#pragma unroll
+  for (int i = 0; i < CT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) zs[wave][j * 16 + l16][i * 16 + 4 * g + r] = acc[i][j][r];
+  __syncthreads();
+  for (int x = threadIdx.x; x < CT * NT * 256; x += 256) {
+    const int c = x % (CT * 16), t = x / (CT * 16);
+    const int64_t v = v0 + c;
+    const float off = v >= a.classes ? -INFINITY : a.offset ? a.offset[v] * kLog2e : 0.f;
+    const float z = (zs[0][t][c] + zs[1][t][c]) + (zs[2][t][c] + zs[3][t][c]);
+    zs[0][t][c] = off == -INFINITY ? -INFINITY : fmaf(z, a.zscale, off);
+  }
+  __syncthreads();
+}
+
+// sums and maxima over P neighbouring lanes
+template <int P>
+__device__ inline float near_sum(float v) {
+#pragma unroll
+  for (int o = P / 2; o; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+template <int P>
+__device__ inline float near_max(float v) {
+#pragma unroll
+  for (int o = P / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ inline float safe(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ inline float pair_logit(const FewArgs& a, int64_t at, int& id, bool& bad) {
+  id = a.ids[at];
+  const float t = id < 0 ? -INFINITY : a.tlogits ? a.tscale * a.tlogits[at] : 0.f;
+  if (t == -INFINITY) id = -1;
+  if (id >= a.classes) {
+    id = -1;
+    bad = true;
+  }
+  return id < 0 ? -INFINITY : t;
+}
+
+// Few classes: 32 rows of h by all classes; eight lanes finish a row, lane p
+// owning the classes c % 8 = p, so that no two add to one target.
+template <typename XT, int CT>
+__global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a) {
+  constexpr int NT = 2, S = CT * 16;
+  __shared__ float zs[4][NT * 16][S + 1];
+  const int64_t t0 = (int64_t)blockIdx.x * (NT * 16);
+  scores_block<XT, CT, NT>(a, 0, t0, zs);
+  const int row = threadIdx.x >> 3, p = threadIdx.x & 7;
+  const int64_t i = t0 + row;
+  float* z = zs[0][row];
+  float* q = zs[1][row];
+  float m = -INFINITY, s = 0.f;
+#pragma unroll
+  for (int c = p; c < S; c += 8) {
+    m = fmaxf(m, z[c]);
+    q[c] = 0.f;
+  }
+  m = near_max<8>(m);
+  const float m0 = safe(m);
+#pragma unroll
+  for (int c = p; c < S; c += 8) s += __builtin_amdgcn_exp2f(z[c] - m0);
+  const float lse2 = m + log2f(near_sum<8>(s));
+  // the target: its largest logit, then its sum, then each pair
+  const bool here = i < a.n;
+  const int pairs = here ? a.m : 0;
+  float tm = -INFINITY, ts = 0.f, loss = 0.f;
+  bool bad = false;
+  int id;
+  for (int j = p; j < pairs; j += 8) tm = fmaxf(tm, pair_logit(a, i * a.m + j, id, bad));
+  tm = safe(near_max<8>(tm));
+  for (int j = p; j < pairs; j += 8) {
+    const float t = pair_logit(a, i * a.m + j, id, bad);
+    ts += id < 0 ? 0.f : expf(t - tm);
+  }
+  ts = near_sum<8>(ts);
+  bad = near_sum<8>(bad ? 1.f : 0.f) != 0.f;
+  const bool some = ts != 0.f;
+  const float inv = some ? 1.f / ts : 0.f;
+  for (int j = 0; j < pairs; ++j) {
+    bool b;
+    const float t = pair_logit(a, i * a.m + j, id, b);
+    if (id < 0 || (id & 7) != p) continue;
+    const float qj = expf(t - tm) * inv;
+    if (qj != 0.f) loss += qj * (logf(qj) + (z[id] == -INFINITY ? INFINITY : lse2 - z[id]) * kLn2);
+    q[id] += qj;
+  }
+  loss = near_sum<8>(loss);
+  if (!here) return;
+  if (p == 0) {
+    a.loss[i] = bad ? __builtin_nanf("") : some ? loss : 0.f;
+    a.lse[i] = lse2 * kLn2;
+  }
+  if (!a.C) return;
+  float cf = a.dloss[i] * a.scale;
+  if (!some || lse2 == -INFINITY) cf = 0.f;
+  if (bad) cf = __builtin_nanf("");
+  if (p == 0) a.coef[i] = cf;
+  const float l2 = safe(lse2);
+#pragma unroll
+  for (int c = p; c < S; c += 8)
+    a.C[i * S + c] =
+        cf == 0.f || z[c] == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z[c] - l2) - q[c]);
+}
+
+// Few rows: CT x 16 classes by all rows of h; the rows' (largest, sum) of the
+// tile, and Z.
+template <typename XT, int CT, int NT>
+__global__ __launch_bounds__(256) void scores_few_rows_kernel(FewArgs a) {
+  constexpr int S = NT * 16, P = 256 / S;
+  __shared__ float zs[4][S][CT * 16 + 1];
+  const int64_t v0 = (int64_t)blockIdx.x * (CT * 16);
+  scores_block<XT, CT, NT>(a, v0, 0, zs);
+  const int row = threadIdx.x / P, p = threadIdx.x % P;
+  const float* z = zs[0][row];
+  float m = -INFINITY, s = 0.f;
+  for (int c = p; c < CT * 16; c += P) m = fmaxf(m, z[c]);
+  m = near_max<P>(m);
+  for (int c = p; c < CT * 16; c += P) s += __builtin_amdgcn_exp2f(z[c] - safe(m));
+  s = near_sum<P>(s);
+  if (p == 0 && row < a.n) a.part[(int64_t)blockIdx.x * a.n + row] = make_float2(m, s);
+  for (int x = threadIdx.x; x < CT * 16 * S; x += 256) {
+    const int c = x / S, t = x % S;
+    if (v0 + c < a.classes) a.C[(v0 + c) * S + t] = zs[0][t][c];
+  }
+}
+
+// Few rows: a workgroup joins a row's tiles and takes its targets from Z, a
+// thread per pair.
+template <int S>
+__global__ __launch_bounds__(256) void targets_few_kernel(FewArgs a, int ntiles) {
+  __shared__ float red[3][4];
+  __shared__ int sid[kMaxTop];
+  __shared__ float sq[kMaxTop];
+  const int64_t i = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto all_sum = [&](float v, int slot) {
+    v = wave_sum(v);
+    __syncthreads();
+    if (lane == 0) red[slot][wave] = v;
+    __syncthreads();
+    return (red[slot][0] + red[slot][1]) + (red[slot][2] + red[slot][3]);
+  };
+  auto all_max = [&](float v, int slot) {
+    v = near_max<64>(v);
+    __syncthreads();
+    if (lane == 0) red[slot][wave] = v;
+    __syncthreads();
+    return fmaxf(fmaxf(red[slot][0], red[slot][1]), fmaxf(red[slot][2], red[slot][3]));
+  };
+  float m = -INFINITY, s = 0.f;
+  for (int t = tid; t < ntiles; t += 256) {
+    const float2 v = a.part[(int64_t)t * a.n + i];
+    const float nm = fmaxf(m, v.x);
+    s = s * __builtin_amdgcn_exp2f(m - safe(nm)) + v.y * __builtin_amdgcn_exp2f(v.x - safe(nm));
+    m = nm;
+  }
+  const float top = all_max(m, 0);
+  const float lse2 = top + log2f(all_sum(s * __builtin_amdgcn_exp2f(m - safe(top)), 1));
+  int id = -1;
+  bool bad = false;
+  float t = -INFINITY;
+  if (tid < a.m) t = pair_logit(a, i * a.m + tid, id, bad);
+  const float tm = safe(all_max(t, 2));
+  const float e = id < 0 ? 0.f : expf(t - tm);
+  const float ts = all_sum(e, 0);
+  bad = all_sum(bad ? 1.f : 0.f, 1) != 0.f;
+  const bool some = ts != 0.f;
+  const float q = some ? e / ts : 0.f, z = id < 0 ? 0.f : a.C[(int64_t)id * S + i];
+  const float l = q != 0.f ? q * (logf(q) + (z == -INFINITY ? INFINITY : lse2 - z) * kLn2) : 0.f;
+  const float loss = all_sum(l, 2);
+  if (tid == 0) {
+    a.loss[i] = bad ? __builtin_nanf("") : some ? loss : 0.f;
+    a.lse[i] = lse2 * kLn2;
+  }
+  if (!a.coef) return;
+  float cf = a.dloss[i] * a.scale;
+  if (!some || lse2 == -INFINITY) cf = 0.f;
+  if (bad) cf = __builtin_nanf("");
+  if (tid == 0) {
+    a.lse2[i] = safe(lse2);
+    a.coef[i] = cf;
+  }
+  if (tid < a.m) {
+    sid[tid] = id;
+    sq[tid] = q;
+  }
+  __syncthreads();
+  if (tid >= a.m) return;
+  float qs = 0.f;  // a class named twice: once, with both
+  bool first = true;
+  for (int j = 0; j < a.m; ++j)
+    if (sid[j] == id) {
+      qs += sq[j];
+      first &= j >= tid;
+    }
+  a.fix_id[i * a.m + tid] = first && cf != 0.f ? id : -1;
+  a.fix_val[i * a.m + tid] = z == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z - safe(lse2)) - qs);
+}
+
+// Few rows: Z becomes G^T, without the targets, which fix_few_kernel puts in.
+__global__ __launch_bounds__(256) void grad_few_kernel(float* __restrict__ C, int64_t count, int S, int64_t n,
+                                                       const float* __restrict__ lse2,
+                                                       const float* __restrict__ coef) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x >= count) return;
+  const int64_t t = x % S;
+  const float cf = t < n ? coef[t] : 0.f;
+  C[x] = cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(C[x] - lse2[t]);
+}
+__global__ __launch_bounds__(256) void fix_few_kernel(float* __restrict__ C, int S, const int32_t* __restrict__ id,
+                                                      const float* __restrict__ val, int64_t pairs, int m) {
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x < pairs && id[x] >= 0) C[(int64_t)id[x] * S + x / m] = val[x];
+}
+
+// A row that takes no part: weight[row] is `none` (0, or -inf).
+__device__ inline bool takes_part(const float* weight, float none, int64_t row) {
+  return !weight || weight[row] != none;
+}
+
+// out (R x d) = C (R x S) B (S x d), rows of B that take no part left out, rows
+// of out that take none 0.  The matrix instructions have the features as rows:
+// one of a lane's kVec features each, so that a lane ends with 16 or 32
+// neighbouring features of a row of out.  A wavefront: 16 kVec features by
+// 16 RT rows; four of them side by side.
+template <typename XT, int S>
+__global__ __launch_bounds__(256) void rows_few_kernel(const float* __restrict__ C, const XT* __restrict__ B,
+                                                       int64_t ldb, int rows_b, const float* __restrict__ weight_b,
+                                                       float none_b, int64_t R, int d,
+                                                       const float* __restrict__ weight_r, XT* __restrict__ out,
+                                                       int64_t ldo) {
+  constexpr int VEC = kVec<XT>, RT = VEC == 4 ? 4 : 2;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  const int c0 = (blockIdx.y * 4 + wave) * (16 * VEC);
+  const int64_t r0 = (int64_t)blockIdx.x * (RT * 16);
+  if (c0 >= d) return;
+  floatx4 acc[VEC][RT];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k0 = 0; k0 < S; k0 += 16) {
+    if (k0 >= rows_b) break;  // (uniform)
+    floatx4 c[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int64_t row = r0 + t * 16 + l16;
+      c[t] = row < R ? *(const floatx4*)(C + row * S + k0 + 4 * g) : floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    raw_vec<XT> b[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = k0 + 4 * g + e;
+      const bool use = k < rows_b && takes_part(weight_b, none_b, k);
+      b[e] = load_raw(B + (int64_t)(use ? k : 0) * ldb, c0 + l16 * VEC, use ? d : 0);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+          acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[e][j], c[t][e], acc[j][t], 0, 0, 0);
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int64_t row = r0 + t * 16 + l16;
+    if (row >= R) continue;
+    const bool part = takes_part(weight_r, 0.f, row);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float v[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[j] = part ? acc[j][t][r] : 0.f;
+      store_part(out + row * ldo, c0 + VEC * (4 * g + r), d, v);
+    }
+  }
+}
+
+// slab (S x d) = C^T X over this workgroup's rows of X (R x d), rows that take
+// no part left out.  A step is four rows: a lane loads kVec features of row
+// lane / 16 and S / 16 of the row's entries of C.  The four wavefronts take
+// every fourth step and join in LDS.
+template <typename XT, int S>
+__global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__ C, const XT* __restrict__ X,
+                                                       int64_t ldx, int64_t R, int d,
+                                                       const float* __restrict__ weight, float none, int64_t per,
+                                                       float* __restrict__ slabs) {
+  constexpr int VEC = kVec<XT>, CT = S / 16, UN = 4;
+  typedef float cvec __attribute__((ext_vector_type(CT)));
+  __shared__ float red[S][16 * VEC + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  const int c0 = blockIdx.x * (16 * VEC), col = c0 + l16 * VEC;
+  const int64_t lo = (int64_t)blockIdx.y * per, hi = min(lo + per, R);
+  floatx4 acc[VEC][CT];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j)
+#pragma unroll
+    for (int t = 0; t < CT; ++t) acc[j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int64_t s = lo + wave * (4 * UN); s < hi; s += 16 * UN) {
+    raw_vec<XT> x[UN];
+    cvec c[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int64_t row = s + u * 4 + g;
+      const bool use = row < hi && takes_part(weight, none, row);
+      x[u] = load_raw(X + (use ? row : lo) * ldx, col, use ? d : 0);
+      if (row < hi) {
+        c[u] = *(const cvec*)(C + row * S + CT * l16);
+      } else {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) ((float*)&c[u])[t] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const float ct = ((const float*)&c[u])[t];
+          acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(ct, (float)x[u][j], acc[j][t], 0, 0, 0);
+        }
+  }
+  // entry r of block (j, t): row CT (4 g + r) + t of the slab, feature VEC l16 + j
+  for (int o = 0; o < 4; ++o) {
+    if (wave == o)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float* p = &red[CT * (4 * g + r) + t][VEC * l16 + j];
+            *p = o ? *p + acc[j][t][r] : acc[j][t][r];
+          }
+    __syncthreads();
+  }
+  float* slab = slabs + (int64_t)blockIdx.y * S * d;
+  for (int x = threadIdx.x; x < S * 16 * VEC; x += 256) {
+    const int sr = x / (16 * VEC), cc = x % (16 * VEC);
+    if (c0 + cc < d) slab[(int64_t)sr * d + c0 + cc] = red[sr][cc];
+  }
+}
+
+// out (M x d, M <= S) from the slabs, in order; rows of weight 0 are 0.
+template <typename OT>
+__global__ __launch_bounds__(256) void slabs_few_kernel(const float* __restrict__ slabs, int count, int S, int M,
+                                                        int d, const float* __restrict__ weight,
+                                                        OT* __restrict__ out, int64_t ldo) {
+  const int64_t x = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int wave = threadIdx.x >> 6;
+  __shared__ float red[4][64];
+  float s = 0.f;
+  if (x < (int64_t)M * d)
+    for (int k = wave; k < count; k += 4) s += slabs[(int64_t)k * S * d + x];
+  red[wave][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (wave || x >= (int64_t)M * d) return;
+  const int lane = threadIdx.x;
+  s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+  const int64_t row = x / d;
+  out[row * ldo + (x - row * d)] = (OT)(takes_part(weight, 0.f, row) ? s : 0.f);
+}
+
+// ------------------------------------------------------------------ plan
+
+int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct FewPlan {
+  bool classes;  // few classes, or few rows
+  int S;         // the short side, padded to 16, 32 or 64
+  int64_t R;     // the long side
+  int ct;        // few rows: class blocks of a tile
+  int ntiles;
+  int splits;
+  int64_t per;
+  size_t C, part, lse2, coef, fix_id, fix_val, slabs, bytes;
+};
+
+FewPlan few_plan(const HeadArgs& a, bool grad) {
+  FewPlan p{};
+  p.classes = a.classes <= kFew;
+  const int64_t s = p.classes ? a.classes : a.n;
+  p.S = s <= 16 ? 16 : s <= 32 ? 32 : 64;
+  p.R = p.classes ? a.n : a.classes;
+  p.ct = a.classes >= 16384 ? 4 : a.classes >= 4096 ? 2 : 1;
+  if (p.S == 64) p.ct = std::min(p.ct, 2);
+  p.ntiles = (int)cdiv(a.classes, 16 * p.ct);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t r = at;
+    at += up(bytes, 1024);
+    return r;
+  };
+  if (grad || !p.classes) p.C = take((size_t)p.R * p.S * 4);
+  if (!p.classes) p.part = take((size_t)p.ntiles * a.n * 8);
+  if (grad) {
+    p.lse2 = take((size_t)a.n * 4);
+    p.coef = take((size_t)a.n * 4);
+    if (!p.classes) {
+      p.fix_id = take((size_t)a.n * a.m * 4);
+      p.fix_val = take((size_t)a.n * a.m * 4);
+    }
+    // rows of a slab: enough workgroups for the chip, no more slabs than their sum is worth
+    const int vec = 16 / (int)elem_bytes(a.type);
+    const int64_t chunks = cdiv(a.d, 16 * vec);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(1024, chunks), cdiv(p.R, 64)));
+    p.per = up(cdiv(p.R, p.splits), 64);
+    p.splits = (int)cdiv(p.R, p.per);
+    p.slabs = take((size_t)p.splits * p.S * a.d * 4);
+  }
+  p.bytes = at;
+  return p;
+}
+
+#define KKM_TRY(expr)                        \
+  do {                                       \
+    hipError_t e_ = (expr);                  \
+    if (e_ != hipSuccess) return e_;         \
+  } while (0)
+
+template <int N>
+using num = std::integral_constant<int, N>;
+template <typename F>
+void by_short(int S, F&& f) {
+  if (S == 16) f(num<16>{});
+  else if (S == 32) f(num<32>{});
+  else f(num<64>{});
+}
+
+template <typename XT>
+hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
+  const FewPlan p = few_plan(a, grad);
+  FewArgs f{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, a.scale * kLog2e, a.scale, a.tscale, a.offset,
+            a.ids, a.tlogits, a.dloss, a.loss, a.lse, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+  if (grad || !p.classes) f.C = (float*)(ws + p.C);
+  if (grad) {
+    f.lse2 = (float*)(ws + p.lse2);
+    f.coef = (float*)(ws + p.coef);
+  }
+  if (p.classes) {
+    by_short(p.S, [&](auto S) {
+      hipLaunchKernelGGL((scores_few_classes_kernel<XT, decltype(S)::value / 16>), dim3((unsigned)cdiv(a.n, 32)),
+                         dim3(256), 0, s, f);
+    });
+    KKM_TRY(hipGetLastError());
+  } else {
+    f.part = (float2*)(ws + p.part);
+    f.fix_id = (int32_t*)(ws + p.fix_id);
+    f.fix_val = (float*)(ws + p.fix_val);
+    by_short(p.S, [&](auto S) {
+      constexpr int NT = decltype(S)::value / 16;
+      const dim3 grid((unsigned)p.ntiles);
+      if (p.ct == 1)
+        hipLaunchKernelGGL((scores_few_rows_kernel<XT, 1, NT>), grid, dim3(256), 0, s, f);
+      else if (p.ct == 2)
+        hipLaunchKernelGGL((scores_few_rows_kernel<XT, 2, NT>), grid, dim3(256), 0, s, f);
+      else if constexpr (NT < 4)
+        hipLaunchKernelGGL((scores_few_rows_kernel<XT, 4, NT>), grid, dim3(256), 0, s, f);
+      hipLaunchKernelGGL((targets_few_kernel<decltype(S)::value>), dim3((unsigned)a.n), dim3(256), 0, s, f, p.ntiles);
+    });
+    KKM_TRY(hipGetLastError());
+    if (grad) {
+      const int64_t count = p.R * p.S, pairs = a.n * a.m;
+      hipLaunchKernelGGL(grad_few_kernel, dim3((unsigned)cdiv(count, 256)), dim3(256), 0, s, f.C, count, p.S, a.n,
+                         f.lse2, f.coef);
+      hipLaunchKernelGGL(fix_few_kernel, dim3((unsigned)cdiv(pairs, 256)), dim3(256), 0, s, f.C, p.S, f.fix_id,
+                         f.fix_val, pairs, a.m);
+      KKM_TRY(hipGetLastError());
+    }
+  }
+  if (!grad) return hipSuccess;
+  // the long side's gradient, then the short side's
+  const float none = -INFINITY;
+  void* long_out = p.classes ? a.dh : a.dw;
+  void* short_out = p.classes ? a.dw : a.dh;
+  const int rows_b = p.classes ? a.classes : (int)a.n;
+  constexpr int VEC = kVec<XT>, RT = VEC == 4 ? 4 : 2;
+  by_short(p.S, [&](auto S_) {
+    constexpr int S = decltype(S_)::value;
+    if (long_out) {
+      const dim3 grid((unsigned)cdiv(p.R, RT * 16), (unsigned)cdiv(a.d, 64 * VEC));
+      hipLaunchKernelGGL((rows_few_kernel<XT, S>), grid, dim3(256), 0, s, f.C, (const XT*)(p.classes ? a.w : a.h),
+                         p.classes ? a.ldw : a.ldh, rows_b, p.classes ? a.offset : f.coef, p.classes ? none : 0.f,
+                         p.R, a.d, p.classes ? f.coef : nullptr, (XT*)long_out, p.classes ? a.lddh : a.lddw);
+    }
+    if (short_out) {
+      float* slabs = (float*)(ws + p.slabs);
+      hipLaunchKernelGGL((cols_few_kernel<XT, S>), dim3((unsigned)cdiv(a.d, 16 * VEC), (unsigned)p.splits), dim3(256),
+                         0, s, f.C, (const XT*)(p.classes ? a.h : a.w), p.classes ? a.ldh : a.ldw, p.R, a.d,
+                         p.classes ? f.coef : a.offset, p.classes ? 0.f : none, p.per, slabs);
+      hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3((unsigned)cdiv((int64_t)rows_b * a.d, 64)), dim3(256), 0, s,
+                         slabs, p.splits, S, rows_b, a.d, p.classes ? nullptr : f.coef, (XT*)short_out,
+                         p.classes ? a.lddw : a.lddh);
+    }
+  });
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool head_is_few(const HeadArgs& a) { return a.classes <= kFew || a.n <= kFew; }
+
+size_t head_few_scratch(const HeadArgs& a, bool grad) { return few_plan(a, grad).bytes; }
+
+hipError_t launch_head_few(const HeadArgs& a, bool grad, void* scratch, hipStream_t s) {
+  switch (a.type) {
+    case TYPE_F32: return few_typed<float>(a, grad, (char*)scratch, s);
+    case TYPE_F16: return few_typed<half_t>(a, grad, (char*)scratch, s);
+    default: return few_typed<bf16_t>(a, grad, (char*)scratch, s);
+  }
+}
+
+}  // namespace kkm

@@ -53,6 +53,12 @@ struct HeadArgs {
 };
 constexpr int kMaxTop = 256;
 
+// A head with a short side (head_few.hip): at most kFew classes, or rows.
+constexpr int kFew = 64;
+bool head_is_few(const HeadArgs& a);
+size_t head_few_scratch(const HeadArgs& a, bool grad);
+hipError_t launch_head_few(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);
+
 size_t head_scratch(const HeadArgs& a, bool grad);
 hipError_t launch_head(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);
 

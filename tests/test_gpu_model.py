@@ -134,7 +134,8 @@ def _check_head(r, loss, lse, dh, dw):
 
 
 HEAD = [(1, 1, 1), (1, 5, 3), (2, 8, 2), (3, 64, 130), (5, 7, 1000), (33, 100, 17), (64, 54, 7), (127, 65, 129),
-        (128, 128, 128), (130, 16, 257), (257, 784, 10), (300, 301, 64), (700, 72, 300), (1030, 24, 65)]
+        (128, 128, 128), (130, 16, 257), (257, 784, 10), (300, 301, 64), (700, 72, 300), (1030, 24, 65),
+        (2000, 19, 32), (999, 130, 16), (16, 300, 4100), (17, 64, 5000), (64, 40, 16400), (65, 65, 65), (1, 2048, 700)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
