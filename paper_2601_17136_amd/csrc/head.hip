@@ -91,24 +91,30 @@ template <typename XT, typename E, int P, bool LEFT_OUT>
 __global__ __launch_bounds__(256) void stage_cols_kernel(const XT* __restrict__ src, int64_t ld, int64_t rows, int d,
                                                          const float* __restrict__ weight, int64_t rp,
                                                          E* __restrict__ dst, int64_t plane) {
-  __shared__ float tile[64][65];
+  constexpr int VEC = kVec<XT>, LANES = 64 / VEC, PASS = 256 / LANES;  // lanes of a row, rows of a pass
+  __shared__ XT tile[64][64 + 4 / sizeof(XT)];
   const int64_t r0 = (int64_t)blockIdx.x * 64;
-  const int c0 = blockIdx.y * 64, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int k = wave; k < 64; k += 4) {
-    const int64_t row = r0 + k;
-    bool use = row < rows && c0 + lane < d;
+  const int c0 = blockIdx.y * 64, col = (threadIdx.x % LANES) * VEC;
+#pragma unroll
+  for (int k = 0; k < 64 / PASS; ++k) {
+    const int rr = k * PASS + threadIdx.x / LANES;
+    const int64_t row = r0 + rr;
+    bool use = row < rows;
     if (use && weight) use = weight[row] != (LEFT_OUT ? -INFINITY : 0.f);
-    tile[k][lane] = use ? (float)src[row * ld + c0 + lane] : 0.f;
+    const raw_vec<XT> v = load_raw(src + (use ? row : 0) * ld, c0 + col, use ? d : 0);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) tile[rr][col + e] = v[e];
   }
   __syncthreads();
   const int part = (threadIdx.x & 7) * 8;
+#pragma unroll
   for (int c = threadIdx.x >> 3; c < 64; c += 32) {
     if (c0 + c >= d || r0 + part >= rp) continue;
     frag<E> o[P];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       E pl[P];
-      split_planes<E, P>(tile[part + e][c], pl);
+      split_planes<E, P>((float)tile[part + e][c], pl);
 #pragma unroll
       for (int p = 0; p < P; ++p) o[p][e] = pl[p];
     }
@@ -118,6 +124,36 @@ __global__ __launch_bounds__(256) void stage_cols_kernel(const XT* __restrict__ 
 }
 
 // ------------------------------------------------------------------ scores
+
+template <typename E>
+__device__ inline unsigned pack2(E lo, E hi) {
+  typedef E e2 __attribute__((ext_vector_type(2)));
+  const e2 v = {lo, hi};
+  return __builtin_bit_cast(unsigned, v);
+}
+
+// (x, y) holds entries 0 .. 3 of this lane's column, two to a word; afterwards
+// entry lane % 4 of the four neighbouring lanes' columns.
+__device__ inline void turn4(unsigned& x, unsigned& y) {
+  const int lane = threadIdx.x;
+  const unsigned xn = __builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, true);  // lane ^ 1
+  const unsigned yn = __builtin_amdgcn_mov_dpp((int)y, 0xb1, 0xf, 0xf, true);
+  const bool odd = lane & 1;
+  const unsigned a = odd ? (xn >> 16) | (x & 0xffff0000u) : (x & 0xffffu) | (xn << 16);
+  const unsigned b = odd ? (yn >> 16) | (y & 0xffff0000u) : (y & 0xffffu) | (yn << 16);
+  const bool upper = lane & 2;  // entries 2 and 3 are wanted there
+  const unsigned send = upper ? a : b;
+  const unsigned got = __builtin_amdgcn_mov_dpp((int)send, 0x4e, 0xf, 0xf, true);  // lane ^ 2
+  x = upper ? got : a;
+  y = upper ? b : got;
+}
+
+// lo: a of the lower half of the wavefront, b's lower half in the upper; hi: a's upper half, b's upper half.
+__device__ inline void swap_halves(unsigned a, unsigned b, unsigned& lo, unsigned& hi) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  lo = r[0];
+  hi = r[1];
+}
 
 template <typename E>
 struct ScoreArgs {
@@ -138,7 +174,7 @@ struct ScoreArgs {
 // classes a block of one row of H, so a row's largest and sum stay in a lane
 // up to one exchange and the wavefronts' sums in LDS.
 template <typename E, class S, int P, bool GRAD>
-__global__ __launch_bounds__(S::threads, 1) void scores_kernel(ScoreArgs<E> a) {
+__global__ __launch_bounds__(S::threads, S::per_cu) void scores_kernel(ScoreArgs<E> a) {
   __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
   int mi, ni;
   tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
@@ -202,27 +238,45 @@ __global__ __launch_bounds__(S::threads, 1) void scores_kernel(ScoreArgs<E> a) {
       const int64_t t = t0 + (wn * S::WN + bj) * 32 + l32;
       const float lse2 = t < a.n ? a.lse2[t] : 0.f, cf = t < a.n ? a.coef[t] : 0.f;
 #pragma unroll
-      for (int bi = 0; bi < S::WM; ++bi)
+      for (int bi = 0; bi < S::WM; ++bi) {
+        const int64_t v = cl + (wm * S::WM + bi) * 32;
+        unsigned o[P][4][2];  // classes 8 q + 4 h + 0 .. 3 of row t, two to a word
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int64_t v = cl + (wm * S::WM + bi) * 32 + 8 * q + 4 * h;
-          typedef E e4 __attribute__((ext_vector_type(4)));
-          e4 o[P];
+          E pl[4][P];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < 4; ++e)
             // (a row without a target has no gradient, whatever its logits)
-            const float g = cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(acc[bi][bj][4 * q + e] - lse2);
-            E pl[P];
-            split_planes<E, P>(g, pl);
+            split_planes<E, P>(cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(acc[bi][bj][4 * q + e] - lse2), pl[e]);
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-              o[p][e] = pl[p];
-              a.Gt[p * a.planet + (v + e) * a.ldt + t] = pl[p];
-            }
+          for (int p = 0; p < P; ++p) {
+            o[p][q][0] = pack2(pl[0][p], pl[1][p]);
+            o[p][q][1] = pack2(pl[2][p], pl[3][p]);
           }
-#pragma unroll
-          for (int p = 0; p < P; ++p) *(e4*)(a.G + p * a.planeg + t * a.ldg + v) = o[p];
         }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          // G^T: four neighbouring lanes turn their 4 x 4 entries, so that a lane
+          // has four rows of h of one class
+          E* gt = a.Gt + p * a.planet + (v + 4 * h + (l32 & 3)) * a.ldt + (t & ~(int64_t)3);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            unsigned x = o[p][q][0], y = o[p][q][1];
+            turn4(x, y);
+            *(uint2*)(gt + (int64_t)(8 * q) * a.ldt) = make_uint2(x, y);
+          }
+          // G: the halves of the wavefront exchange, so that a lane has 16
+          // neighbouring classes, the lower half 0 .. 15, the upper 16 .. 31
+          E* g = a.G + p * a.planeg + t * a.ldg + v + 16 * h;
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            uint4 w;
+            swap_halves(o[p][q][0], o[p][q + 2][0], w.x, w.z);
+            swap_halves(o[p][q][1], o[p][q + 2][1], w.y, w.w);
+            *(uint4*)(g + 8 * q) = w;
+          }
+        }
+      }
     }
   }
 }
@@ -443,7 +497,7 @@ struct ProductArgs {
 };
 
 template <typename E, typename OT, class S>
-__global__ __launch_bounds__(S::threads, 1) void product_kernel(ProductArgs a) {
+__global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
   int mi, ni;
   tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
@@ -476,17 +530,38 @@ __global__ __launch_bounds__(S::threads, 1) void product_kernel(ProductArgs a) {
     }
 }
 
+// out from the slabs, in order; a thread takes four neighbouring entries of a row.
 template <typename OT>
 __global__ __launch_bounds__(256) void slabs_kernel(const float* __restrict__ slabs, int count, int64_t M, int64_t N,
                                                     const float* __restrict__ alpha,
                                                     const float* __restrict__ coef, OT* __restrict__ out,
                                                     int64_t ldo) {
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (x >= M * N) return;
-  float s = 0.f;
-  for (int k = 0; k < count; ++k) s += slabs[k * M * N + x];
-  const int64_t row = x / N;
-  out[row * ldo + (x - row * N)] = (OT)(coef && coef[row] == 0.f ? 0.f : s * (alpha ? *alpha : 1.f));
+  const int64_t per = (N + 3) / 4, x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (x >= M * per) return;
+  const int64_t row = x / per, c = (x - row * per) * 4;
+  const int m = (int)min((int64_t)4, N - c);
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < count; ++k) {
+    const float* p = slabs + (k * M + row) * N + c;
+    if (m == 4) {
+      const raw_vec<float> v = *(const any_vec<float>*)p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    } else {
+      for (int e = 0; e < m; ++e) s[e] += p[e];
+    }
+  }
+  const float f = alpha ? *alpha : 1.f;
+  const bool none = coef && coef[row] == 0.f;
+  typedef OT o4 __attribute__((ext_vector_type(4)));
+  typedef o4 any4 __attribute__((aligned(alignof(OT))));
+  o4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (OT)(none ? 0.f : s[e] * f);
+  if (m == 4)
+    *(any4*)(out + row * ldo + c) = o;
+  else
+    for (int e = 0; e < m; ++e) out[row * ldo + c + e] = o[e];
 }
 
 template <typename OT>
@@ -503,6 +578,7 @@ constexpr int kPad = 256;  // G's rows and classes: whole tiles of any shape
 
 // (a tile's rows are reached by 32-bit offsets: kMaxStride)
 constexpr int64_t kMaxStride = (int64_t)1 << 21;
+constexpr int64_t kBigTiles = 192 * 65536 / (BigTile::BM * BigTile::BN);
 bool in_place(const HeadArgs& a, const void* p, int64_t ld) {
   return a.type != TYPE_F32 && a.d % 8 == 0 && ld % 8 == 0 && ld <= kMaxStride && (uintptr_t)p % 16 == 0;
 }
@@ -516,8 +592,8 @@ int slab_count(int64_t tiles, int64_t chunks) {
 struct HeadPlan {
   int planes, nseg, kp;
   int64_t n_pad, v_pad;
-  bool big;             // scores in 256 x 256 tiles
-  int bm, ntiles;
+  bool big;             // scores in BigTile
+  int ntiles;
   int piece;            // classes of a piece (a multiple of kPad)
   int sh, sw;           // slabs of dH and dW (0: none)
   bool bigh, bigw;
@@ -532,9 +608,8 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
   p.kp = (int)up(a.d, kChunkK);
   p.n_pad = up(a.n, kPad);
   p.v_pad = up(a.classes, kPad);
-  p.big = cdiv(a.n, 256) * cdiv(a.classes, 256) >= 192;
-  p.bm = p.big ? 256 : 128;
-  p.ntiles = (int)cdiv(a.classes, p.bm);
+  p.big = cdiv(a.classes, BigTile::BM) * cdiv(a.n, BigTile::BN) >= kBigTiles;
+  p.ntiles = (int)cdiv(a.classes, p.big ? BigTile::BM : SmallTile::BM);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t r = at;
@@ -559,9 +634,10 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
     p.Gt = take((size_t)p.planes * p.n_pad * p.piece * 2);
     const int64_t pieces = cdiv(a.classes, p.piece);
     auto shape = [&](int64_t M, int64_t N, int64_t chunks, bool& big) {
-      big = cdiv(M, 256) * cdiv(N, 256) >= 192;
-      const int b = big ? 256 : 128;
-      return slab_count(cdiv(M, b) * cdiv(N, b), chunks);
+      big = cdiv(M, BigTile::BM) * cdiv(N, BigTile::BN) >= kBigTiles;
+      const int64_t tiles = big ? cdiv(M, BigTile::BM) * cdiv(N, BigTile::BN)
+                                : cdiv(M, SmallTile::BM) * cdiv(N, SmallTile::BN);
+      return slab_count(tiles, chunks);
     };
     p.sh = shape(a.n, a.d, p.nseg * cdiv(std::min<int64_t>(p.piece, a.classes), kChunkK), p.bigh);
     p.sw = shape(std::min<int64_t>(p.piece, a.classes), a.d, p.nseg * cdiv(a.n, kChunkK), p.bigw);
@@ -606,8 +682,9 @@ struct Head {
 
   template <bool GRAD>
   hipError_t scores(ScoreArgs<E> sa, int64_t classes) const {
-    sa.mt = (int)cdiv(classes, p.bm);
-    sa.nt = (int)cdiv(a.n, p.bm);
+    sa.nkc = p.kp / (p.big ? BigTile::BK : SmallTile::BK);
+    sa.mt = (int)cdiv(classes, p.big ? BigTile::BM : SmallTile::BM);
+    sa.nt = (int)cdiv(a.n, p.big ? BigTile::BN : SmallTile::BN);
     const dim3 grid((unsigned)((int64_t)sa.mt * sa.nt));
     if (p.big)
       hipLaunchKernelGGL((scores_kernel<E, BigTile, P, GRAD>), grid, dim3(BigTile::threads), 0, s, sa);
@@ -626,12 +703,11 @@ struct Head {
     pa.M = M;
     pa.N = N;
     pa.K = K;
-    pa.nkc = (int)cdiv(K, kChunkK);
+    pa.nkc = (int)cdiv(K, chunk_of(big));
     pa.nseg = p.nseg;
-    const int b = big ? 256 : 128;
-    pa.mt = (int)cdiv(M, b);
-    pa.nt = (int)cdiv(N, b);
-    pa.per = share(K0, slabs);
+    pa.mt = (int)cdiv(M, big ? BigTile::BM : SmallTile::BM);
+    pa.nt = (int)cdiv(N, big ? BigTile::BN : SmallTile::BN);
+    pa.per = share(K0, big, slabs);
     pa.slabs = slabs ? slab : nullptr;
     pa.add = add;
     pa.out = out;
@@ -647,12 +723,17 @@ struct Head {
   }
 
   // chunks of a slab, and the slabs that a product of K wrote
-  int share(int K, int slabs) const { return (int)cdiv(cdiv(K, kChunkK) * p.nseg, std::max(slabs, 1)); }
-  int written(int K, int slabs) const { return (int)cdiv(cdiv(K, kChunkK) * p.nseg, share(K, slabs)); }
+  static int chunk_of(bool big) { return big ? BigTile::BK : SmallTile::BK; }
+  int share(int K, bool big, int slabs) const {
+    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, std::max(slabs, 1));
+  }
+  int written(int K, bool big, int slabs) const {
+    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, share(K, big, slabs));
+  }
 
   hipError_t sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, const float* coef,
                  void* out, int64_t ldo) const {
-    hipLaunchKernelGGL((slabs_kernel<XT>), grid1(M * N), dim3(256), 0, s, slabs, count, M, N, alpha, coef,
+    hipLaunchKernelGGL((slabs_kernel<XT>), grid1(M * cdiv(N, 4)), dim3(256), 0, s, slabs, count, M, N, alpha, coef,
                        (XT*)out, ldo);
     return hipGetLastError();
   }
@@ -664,7 +745,6 @@ struct Head {
     sa.n = a.n;
     sa.classes = a.classes;
     sa.K = in_place(a, a.h, a.ldh) || in_place(a, a.w, a.ldw) ? a.d : p.kp;
-    sa.nkc = p.kp / kChunkK;
     sa.nseg = p.nseg;
     sa.zscale = a.scale * kLog2e;
     sa.offset = a.offset;
@@ -735,10 +815,10 @@ struct Head {
         XT* dw = (XT*)a.dw + (int64_t)v0 * a.lddw;
         KKM_TRY(product({sa.Gt, sa.ldt, sa.planet, p.piece}, ht, cnt, a.d, kn, kn, p.bigw, p.sw, at<float>(p.slabs_w), 0,
                         dw, a.lddw, alpha, nullptr));
-        if (p.sw) KKM_TRY(sum(at<float>(p.slabs_w), written(kn, p.sw), cnt, a.d, alpha, nullptr, dw, a.lddw));
+        if (p.sw) KKM_TRY(sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha, nullptr, dw, a.lddw));
       }
     }
-    if (a.dh && p.sh) KKM_TRY(sum(at<float>(p.slabs_h), written(kv0, p.sh), a.n, a.d, alpha, ta.coef, a.dh, a.lddh));
+    if (a.dh && p.sh) KKM_TRY(sum(at<float>(p.slabs_h), written(kv0, p.bigh, p.sh), a.n, a.d, alpha, ta.coef, a.dh, a.lddh));
     return hipSuccess;
   }
 };

@@ -60,7 +60,7 @@ struct FewArgs {
 // -inf where a class is left out or past the last.
 template <typename XT, int CT, int NT>
 __device__ inline void scores_block(const FewArgs& a, int64_t v0, int64_t t0, float (*zs)[NT * 16][CT * 16 + 1]) {
-  constexpr int VEC = kVec<XT>, KS = 4 * VEC, UN = CT * NT > 8 ? 1 : CT + NT > 4 ? 2 : 4;
+  constexpr int VEC = kVec<XT>, KS = 4 * VEC, UN = CT + NT > 4 ? 2 : 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const XT *pa[CT], *pb[NT];
@@ -146,9 +146,16 @@ __global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a) {
   constexpr int NT = 2, S = CT * 16;
   __shared__ float zs[4][NT * 16][S + 1];
   const int64_t t0 = (int64_t)blockIdx.x * (NT * 16);
-  scores_block<XT, CT, NT>(a, 0, t0, zs);
   const int row = threadIdx.x >> 3, p = threadIdx.x & 7;
   const int64_t i = t0 + row;
+  // the first eight pairs and the row's factor, loaded ahead
+  const bool here = i < a.n;
+  const int pairs = here ? a.m : 0;
+  int id0 = -1;
+  bool bad = false;
+  const float p0 = p < pairs ? pair_logit(a, i * a.m + p, id0, bad) : -INFINITY;
+  const float dl = here && a.C ? a.dloss[i] : 0.f;
+  scores_block<XT, CT, NT>(a, 0, t0, zs);
   float* z = zs[0][row];
   float* q = zs[1][row];
   float m = -INFINITY, s = 0.f;
@@ -163,14 +170,12 @@ __global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a) {
   for (int c = p; c < S; c += 8) s += __builtin_amdgcn_exp2f(z[c] - m0);
   const float lse2 = m + log2f(near_sum<8>(s));
   // the target: its largest logit, then its sum, then each pair
-  const bool here = i < a.n;
-  const int pairs = here ? a.m : 0;
-  float tm = -INFINITY, ts = 0.f, loss = 0.f;
-  bool bad = false;
+  float tm = p0, ts = 0.f, loss = 0.f;
   int id;
-  for (int j = p; j < pairs; j += 8) tm = fmaxf(tm, pair_logit(a, i * a.m + j, id, bad));
+  for (int j = p + 8; j < pairs; j += 8) tm = fmaxf(tm, pair_logit(a, i * a.m + j, id, bad));
   tm = safe(near_max<8>(tm));
-  for (int j = p; j < pairs; j += 8) {
+  ts = id0 < 0 ? 0.f : expf(p0 - tm);
+  for (int j = p + 8; j < pairs; j += 8) {
     const float t = pair_logit(a, i * a.m + j, id, bad);
     ts += id < 0 ? 0.f : expf(t - tm);
   }
@@ -178,13 +183,19 @@ __global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a) {
   bad = near_sum<8>(bad ? 1.f : 0.f) != 0.f;
   const bool some = ts != 0.f;
   const float inv = some ? 1.f / ts : 0.f;
-  for (int j = 0; j < pairs; ++j) {
+  for (int j0 = 0; j0 < a.m; j0 += 8) {
     bool b;
-    const float t = pair_logit(a, i * a.m + j, id, b);
-    if (id < 0 || (id & 7) != p) continue;
-    const float qj = expf(t - tm) * inv;
-    if (qj != 0.f) loss += qj * (logf(qj) + (z[id] == -INFINITY ? INFINITY : lse2 - z[id]) * kLn2);
-    q[id] += qj;
+    id = j0 ? -1 : id0;
+    float t = p0;
+    if (j0 && j0 + p < pairs) t = pair_logit(a, i * a.m + j0 + p, id, b);
+    const float mine = id < 0 ? 0.f : expf(t - tm) * inv;
+    for (int o = 0; o < min(8, a.m - j0); ++o) {
+      const int v = __shfl(id, o, 8);
+      const float qj = __shfl(mine, o, 8);
+      if (v < 0 || (v & 7) != p) continue;
+      if (qj != 0.f) loss += qj * (logf(qj) + (z[v] == -INFINITY ? INFINITY : lse2 - z[v]) * kLn2);
+      q[v] += qj;
+    }
   }
   loss = near_sum<8>(loss);
   if (!here) return;
@@ -193,7 +204,7 @@ __global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a) {
     a.lse[i] = lse2 * kLn2;
   }
   if (!a.C) return;
-  float cf = a.dloss[i] * a.scale;
+  float cf = dl * a.scale;
   if (!some || lse2 == -INFINITY) cf = 0.f;
   if (bad) cf = __builtin_nanf("");
   if (p == 0) a.coef[i] = cf;
@@ -323,126 +334,170 @@ __device__ inline bool takes_part(const float* weight, float none, int64_t row) 
 // out (R x d) = C (R x S) B (S x d), rows of B that take no part left out, rows
 // of out that take none 0.  The matrix instructions have the features as rows:
 // one of a lane's kVec features each, so that a lane ends with 16 or 32
-// neighbouring features of a row of out.  A wavefront: 16 kVec features by
-// 16 RT rows; four of them side by side.
+// neighbouring features of a row of out, the four lanes of a row 64 bytes at a
+// time.  A wavefront keeps its 16 kVec features of B in registers and goes over
+// blocks of 16 rows a grid apart, the next one's C on its way.
 template <typename XT, int S>
 __global__ __launch_bounds__(256) void rows_few_kernel(const float* __restrict__ C, const XT* __restrict__ B,
                                                        int64_t ldb, int rows_b, const float* __restrict__ weight_b,
                                                        float none_b, int64_t R, int d,
                                                        const float* __restrict__ weight_r, XT* __restrict__ out,
                                                        int64_t ldo) {
-  constexpr int VEC = kVec<XT>, RT = VEC == 4 ? 4 : 2;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  constexpr int VEC = kVec<XT>, KB = S / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
   const int c0 = (blockIdx.y * 4 + wave) * (16 * VEC);
-  const int64_t r0 = (int64_t)blockIdx.x * (RT * 16);
   if (c0 >= d) return;
-  floatx4 acc[VEC][RT];
+  const int place = (l16 >> 2) + 4 * (l16 & 3);  // matrix row 4 g + r holds the features from kVec (g + 4 r)
+  raw_vec<XT> b[KB][4];
 #pragma unroll
-  for (int j = 0; j < VEC; ++j)
-#pragma unroll
-    for (int t = 0; t < RT; ++t) acc[j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int k0 = 0; k0 < S; k0 += 16) {
-    if (k0 >= rows_b) break;  // (uniform)
-    floatx4 c[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int64_t row = r0 + t * 16 + l16;
-      c[t] = row < R ? *(const floatx4*)(C + row * S + k0 + 4 * g) : floatx4{0.f, 0.f, 0.f, 0.f};
-    }
-    raw_vec<XT> b[4];
+  for (int k0 = 0; k0 < KB; ++k0)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int k = k0 + 4 * g + e;
+      const int k = 16 * k0 + 4 * g + e;
       const bool use = k < rows_b && takes_part(weight_b, none_b, k);
-      b[e] = load_raw(B + (int64_t)(use ? k : 0) * ldb, c0 + l16 * VEC, use ? d : 0);
+      b[k0][e] = load_raw(B + (int64_t)(use ? k : 0) * ldb, c0 + place * VEC, use ? d : 0);
     }
+  floatx4 c[KB], cn[KB];
+  float wn = 1.f;
+  auto fetch = [&](int64_t r0) {
+    const int64_t row = min(r0 + l16, R - 1);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int k0 = 0; k0 < KB; ++k0) cn[k0] = *(const floatx4*)(C + row * S + 16 * k0 + 4 * g);
+    if (weight_r) wn = weight_r[row];
+  };
+  const int64_t step = (int64_t)gridDim.x * 16;
+  int64_t r0 = (int64_t)blockIdx.x * 16;
+  fetch(r0);
+  for (; r0 < R; r0 += step) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j)
+    for (int k0 = 0; k0 < KB; ++k0) c[k0] = cn[k0];
+    const bool part = wn != 0.f;
+    fetch(r0 + step);
+    floatx4 acc[VEC];
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-          acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[e][j], c[t][e], acc[j][t], 0, 0, 0);
-  }
+    for (int j = 0; j < VEC; ++j) acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int64_t row = r0 + t * 16 + l16;
+    for (int k0 = 0; k0 < KB; ++k0)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[k0][e][j], c[k0][e], acc[j], 0, 0, 0);
+    const int64_t row = r0 + l16;
     if (row >= R) continue;
-    const bool part = takes_part(weight_r, 0.f, row);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float v[VEC];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) v[j] = part ? acc[j][t][r] : 0.f;
-      store_part(out + row * ldo, c0 + VEC * (4 * g + r), d, v);
+      for (int j = 0; j < VEC; ++j) v[j] = part ? acc[j][r] : 0.f;
+      store_part(out + row * ldo, c0 + VEC * (g + 4 * r), d, v);
     }
   }
 }
 
 // slab (S x d) = C^T X over this workgroup's rows of X (R x d), rows that take
-// no part left out.  A step is four rows: a lane loads kVec features of row
-// lane / 16 and S / 16 of the row's entries of C.  The four wavefronts take
-// every fourth step and join in LDS.
+// no part left out.  A step is 4 UN rows: a lane loads kVec features of row
+// lane / 16 in each of CH blocks of 16 kVec features, and S / 16 of the row's
+// entries of C.  The four wavefronts take every fourth step and join in LDS.
+template <typename XT, int S>
+struct ColsShape {
+  static constexpr int VEC = kVec<XT>, CT = S / 16;
+  static constexpr int CH = 16 / (VEC * CT) > 0 ? 16 / (VEC * CT) : 1;  // 64 sums a lane (128: 16 bits, S = 64)
+  static constexpr int UN = CH >= 4 ? 1 : CH == 2 ? 2 : 4;
+  static constexpr int width = CH * 16 * VEC;
+};
 template <typename XT, int S>
 __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__ C, const XT* __restrict__ X,
                                                        int64_t ldx, int64_t R, int d,
                                                        const float* __restrict__ weight, float none, int64_t per,
                                                        float* __restrict__ slabs) {
-  constexpr int VEC = kVec<XT>, CT = S / 16, UN = 4;
+  using Sh = ColsShape<XT, S>;
+  constexpr int VEC = Sh::VEC, CT = Sh::CT, CH = Sh::CH, UN = Sh::UN;
   typedef float cvec __attribute__((ext_vector_type(CT)));
   __shared__ float red[S][16 * VEC + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * (16 * VEC), col = c0 + l16 * VEC;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int c0 = blockIdx.x * Sh::width;
   const int64_t lo = (int64_t)blockIdx.y * per, hi = min(lo + per, R);
-  floatx4 acc[VEC][CT];
+  floatx4 acc[CH][VEC][CT];
 #pragma unroll
-  for (int j = 0; j < VEC; ++j)
+  for (int h = 0; h < CH; ++h)
 #pragma unroll
-    for (int t = 0; t < CT; ++t) acc[j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  for (int64_t s = lo + wave * (4 * UN); s < hi; s += 16 * UN) {
-    raw_vec<XT> x[UN];
-    cvec c[UN];
+    for (int j = 0; j < VEC; ++j)
+#pragma unroll
+      for (int t = 0; t < CT; ++t) acc[h][j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  raw_vec<XT> x[UN][CH], xn[UN][CH];  // this step's, and the next one's on their way
+  float c[UN][CT], cn[UN][CT];
+  bool un[UN];
+  const bool inside = c0 + Sh::width <= d;
+  auto fetch = [&](int64_t s) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int64_t row = s + u * 4 + g;
       const bool use = row < hi && takes_part(weight, none, row);
-      x[u] = load_raw(X + (use ? row : lo) * ldx, col, use ? d : 0);
-      if (row < hi) {
-        c[u] = *(const cvec*)(C + row * S + CT * l16);
-      } else {
+      const XT* xr = X + (use ? row : lo) * ldx;
 #pragma unroll
-        for (int t = 0; t < CT; ++t) ((float*)&c[u])[t] = 0.f;
+      for (int h = 0; h < CH; ++h) {
+        const int col = c0 + (h * 16 + l16) * VEC;
+        if (inside) {
+          xn[u][h] = *(const any_vec<XT>*)(xr + col);
+        } else {
+          xn[u][h] = load_raw(xr, col, d);
+        }
       }
+      const cvec cv = *(const cvec*)(C + (row < hi ? row : lo) * S + CT * l16);
+#pragma unroll
+      for (int t = 0; t < CT; ++t) cn[u][t] = ((const float*)&cv)[t];
+      un[u] = use;
     }
+  };
+  constexpr int step = 16 * UN;  // rows of the four wavefronts' steps
+  int64_t s = lo + wave * (4 * UN);
+  if (s < hi) fetch(s);
+  for (; s < hi; s += step) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+#pragma unroll
+      for (int h = 0; h < CH; ++h)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][h][e] = un[u] ? xn[u][h][e] : (XT)0.f;
+#pragma unroll
+      for (int t = 0; t < CT; ++t) c[u][t] = un[u] ? cn[u][t] : 0.f;
+    }
+    if (s + step < hi) fetch(s + step);
 #pragma unroll
     for (int u = 0; u < UN; ++u)
 #pragma unroll
-      for (int j = 0; j < VEC; ++j)
+      for (int h = 0; h < CH; ++h)
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          const float ct = ((const float*)&c[u])[t];
-          acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(ct, (float)x[u][j], acc[j][t], 0, 0, 0);
-        }
+        for (int j = 0; j < VEC; ++j)
+#pragma unroll
+          for (int t = 0; t < CT; ++t)
+            acc[h][j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(c[u][t], (float)x[u][h][j], acc[h][j][t], 0, 0, 0);
   }
   // entry r of block (j, t): row CT (4 g + r) + t of the slab, feature VEC l16 + j
-  for (int o = 0; o < 4; ++o) {
-    if (wave == o)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j)
-#pragma unroll
-        for (int t = 0; t < CT; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float* p = &red[CT * (4 * g + r) + t][VEC * l16 + j];
-            *p = o ? *p + acc[j][t][r] : acc[j][t][r];
-          }
-    __syncthreads();
-  }
   float* slab = slabs + (int64_t)blockIdx.y * S * d;
-  for (int x = threadIdx.x; x < S * 16 * VEC; x += 256) {
-    const int sr = x / (16 * VEC), cc = x % (16 * VEC);
-    if (c0 + cc < d) slab[(int64_t)sr * d + c0 + cc] = red[sr][cc];
+#pragma unroll
+  for (int h = 0; h < CH; ++h) {
+    for (int o = 0; o < 4; ++o) {
+      if (wave == o)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+#pragma unroll
+          for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float* p = &red[CT * (4 * g + r) + t][VEC * l16 + j];
+              *p = o ? *p + acc[h][j][t][r] : acc[h][j][t][r];
+            }
+      __syncthreads();
+    }
+    for (int y = threadIdx.x; y < S * 16 * VEC; y += 256) {
+      const int sr = y / (16 * VEC), cc = c0 + h * 16 * VEC + y % (16 * VEC);
+      if (cc < d) slab[(int64_t)sr * d + cc] = red[sr][y % (16 * VEC)];
+    }
+    __syncthreads();
   }
 }
 
@@ -456,6 +511,7 @@ __global__ __launch_bounds__(256) void slabs_few_kernel(const float* __restrict_
   __shared__ float red[4][64];
   float s = 0.f;
   if (x < (int64_t)M * d)
+#pragma unroll 8
     for (int k = wave; k < count; k += 4) s += slabs[(int64_t)k * S * d + x];
   red[wave][threadIdx.x & 63] = s;
   __syncthreads();
@@ -507,9 +563,9 @@ FewPlan few_plan(const HeadArgs& a, bool grad) {
       p.fix_val = take((size_t)a.n * a.m * 4);
     }
     // rows of a slab: enough workgroups for the chip, no more slabs than their sum is worth
-    const int vec = 16 / (int)elem_bytes(a.type);
-    const int64_t chunks = cdiv(a.d, 16 * vec);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(1024, chunks), cdiv(p.R, 64)));
+    const int vec = 16 / (int)elem_bytes(a.type), ch = std::max(1, 256 / (vec * p.S));  // ColsShape::width
+    const int64_t chunks = cdiv(a.d, ch * 16 * vec);
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(512, chunks), cdiv(p.R, 64)));
     p.per = up(cdiv(p.R, p.splits), 64);
     p.splits = (int)cdiv(p.R, p.per);
     p.slabs = take((size_t)p.splits * p.S * a.d * 4);
@@ -580,23 +636,25 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   void* long_out = p.classes ? a.dh : a.dw;
   void* short_out = p.classes ? a.dw : a.dh;
   const int rows_b = p.classes ? a.classes : (int)a.n;
-  constexpr int VEC = kVec<XT>, RT = VEC == 4 ? 4 : 2;
+  constexpr int VEC = kVec<XT>;
   by_short(p.S, [&](auto S_) {
     constexpr int S = decltype(S_)::value;
-    if (long_out) {
-      const dim3 grid((unsigned)cdiv(p.R, RT * 16), (unsigned)cdiv(a.d, 64 * VEC));
-      hipLaunchKernelGGL((rows_few_kernel<XT, S>), grid, dim3(256), 0, s, f.C, (const XT*)(p.classes ? a.w : a.h),
-                         p.classes ? a.ldw : a.ldh, rows_b, p.classes ? a.offset : f.coef, p.classes ? none : 0.f,
-                         p.R, a.d, p.classes ? f.coef : nullptr, (XT*)long_out, p.classes ? a.lddh : a.lddw);
-    }
+    // (the sums first: the long side's rows may still be in the last-level cache)
     if (short_out) {
       float* slabs = (float*)(ws + p.slabs);
-      hipLaunchKernelGGL((cols_few_kernel<XT, S>), dim3((unsigned)cdiv(a.d, 16 * VEC), (unsigned)p.splits), dim3(256),
+      hipLaunchKernelGGL((cols_few_kernel<XT, S>), dim3((unsigned)cdiv(a.d, ColsShape<XT, S>::width), (unsigned)p.splits), dim3(256),
                          0, s, f.C, (const XT*)(p.classes ? a.h : a.w), p.classes ? a.ldh : a.ldw, p.R, a.d,
                          p.classes ? f.coef : a.offset, p.classes ? 0.f : none, p.per, slabs);
       hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3((unsigned)cdiv((int64_t)rows_b * a.d, 64)), dim3(256), 0, s,
                          slabs, p.splits, S, rows_b, a.d, p.classes ? nullptr : f.coef, (XT*)short_out,
                          p.classes ? a.lddw : a.lddh);
+    }
+    if (long_out) {
+      const int64_t cols = cdiv(a.d, 64 * VEC);
+      const dim3 grid((unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max<int64_t>(1, 1536 / cols)), (unsigned)cols);
+      hipLaunchKernelGGL((rows_few_kernel<XT, S>), grid, dim3(256), 0, s, f.C, (const XT*)(p.classes ? a.w : a.h),
+                         p.classes ? a.ldw : a.ldh, rows_b, p.classes ? a.offset : f.coef, p.classes ? none : 0.f,
+                         p.R, a.d, p.classes ? f.coef : nullptr, (XT*)long_out, p.classes ? a.lddh : a.lddw);
     }
   });
   return hipGetLastError();

@@ -34,47 +34,62 @@ __device__ inline floatx16 mfma16(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+constexpr int lds_of(int bm, int bn, int bk, int stages) { return (bm + bn) * bk * 2 * stages; }
 // A workgroup of GM x GN wavefronts, each WM x WN blocks of 32 x 32; chunks of
-// kChunkK contraction indices, STAGES of them in LDS.
-constexpr int kChunkK = 64;
-template <int WM_, int WN_, int GM_, int GN_, int STAGES_>
+// BK contraction indices, STAGES of them in LDS.
+template <int WM_, int WN_, int GM_, int GN_, int BK_, int STAGES_>
 struct TileShape {
-  static constexpr int WM = WM_, WN = WN_, GM = GM_, GN = GN_, STAGES = STAGES_;
+  static constexpr int WM = WM_, WN = WN_, GM = GM_, GN = GN_, BK = BK_, STAGES = STAGES_;
   static constexpr int BM = WM * GM * 32, BN = WN * GN * 32, waves = GM * GN, threads = waves * 64;
-  static constexpr int stage_bytes = (BM + BN) * kChunkK * 2, lds_bytes = stage_bytes * STAGES;
-  static constexpr int loads = (BM + BN) / 8 / waves;  // 1 KB loads (8 rows) per wavefront and chunk
-  static_assert((BM / 8) % waves == 0 && (BN / 8) % waves == 0, "");
+  static constexpr int per_cu = lds_of(BM, BN, BK, STAGES) <= 80 * 1024 ? 2 : 1;  // workgroups
+  static constexpr int row_bytes = BK * 2, slots = row_bytes / 16, group = 64 / slots;  // rows of a 1 KB load
+  static constexpr int stage_bytes = (BM + BN) * row_bytes, lds_bytes = stage_bytes * STAGES;
+  static constexpr int LA = BM / group / waves, LB = BN / group / waves;  // loads per wavefront and chunk
+  static_assert(BM % (group * waves) == 0 && BN % (group * waves) == 0, "");
+  static_assert(LA * group % 16 == 0 && LB * group % 16 == 0, "turn() of a wavefront's rows goes by its own");
+  // 16-byte slot s of a row lies at s ^ turn(row): sixteen rows at one s meet in
+  // none of LDS's 64 banks
+  __device__ static int turn(int row) { return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
 };
-using BigTile = TileShape<4, 2, 2, 4, 2>;    // 256 x 256, 128 KB
-using SmallTile = TileShape<2, 2, 2, 2, 2>;  // 128 x 128, 64 KB
+using BigTile = TileShape<4, 2, 2, 4, 64, 2>;    // 256 x 256, 128 KB
+using SmallTile = TileShape<2, 2, 2, 2, 64, 2>;  // 128 x 128, 64 KB
+constexpr int kChunkK = 64;  // what operands are padded to
 
 typedef __attribute__((address_space(3))) void lds_void;
 
+template <int VM>
+__device__ inline void wait_loads() {  // at most VM loads outstanding, every LDS read done
+  __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | ((VM >> 4) << 14));
+}
+
 // acc = the tile at rows row0 of a and col0 of b, over chunks [c0, c1) of the
-// nseg x nkc (segment, chunk) pairs.  A row in LDS is 128 bytes, its 16-byte
-// slots at slot ^ (row % 8), so that neither the loads nor the operand reads
-// meet in a bank; the loads permute their source instead of their target, which
-// is a wavefront's 1 KB in order.  Rows past the operand's end read its last
-// one (what they give is not stored), contraction indices past K read zero.
+// nseg x nkc (segment, chunk) pairs.  Loads go straight to LDS and permute
+// their source instead of their target, which is a wavefront's 1 KB in order.
+// Rows past the operand's end read its last one (what they give is not stored),
+// contraction indices past K read zero.  Chunk c + STAGES - 1 is requested
+// while chunk c is multiplied; a step's operands are read from LDS while the
+// step before is multiplied, across the chunk's one barrier too.
 template <typename E, class S>
 __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, int64_t col0, int K, int nkc, int nseg,
                                     int c0, int c1, char* lds, floatx16 (&acc)[S::WM][S::WN]) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host pass knows no buffer resources)
-  constexpr int LA = S::BM / 8 / S::waves, LB = S::BN / 8 / S::waves;
   constexpr unsigned kBound = 0x7ffffff0u, kOut = 0x80000000u;
+  constexpr int NS = S::BK / 16, D = S::STAGES, L = S::LA + S::LB;
+  constexpr int SP = D == 2 ? NS / 2 : NS, LP = L / SP;  // a chunk's loads go out in its first SP steps
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
-  const int slot = (lane & 7) ^ (lane >> 3);  // of the source row lane / 8
-  unsigned va[LA], vb[LB];
+  const int lrow = lane / S::slots;
+  auto slot = [&](int j) { return (lane % S::slots) ^ S::turn(j * S::group + lrow); };  // what this lane loads
+  unsigned va[S::LA], vb[S::LB];
 #pragma unroll
-  for (int j = 0; j < LA; ++j) {
-    const int64_t r = row0 + (wave * LA + j) * 8 + (lane >> 3);
-    va[j] = (unsigned)((min(r, a.rows - 1) - row0) * a.ld * 2) + slot * 16;
+  for (int j = 0; j < S::LA; ++j) {
+    const int64_t r = row0 + (wave * S::LA + j) * S::group + lrow;
+    va[j] = (unsigned)((min(r, a.rows - 1) - row0) * a.ld * 2) + slot(j) * 16;
   }
 #pragma unroll
-  for (int j = 0; j < LB; ++j) {
-    const int64_t r = col0 + (wave * LB + j) * 8 + (lane >> 3);
-    vb[j] = (unsigned)((min(r, b.rows - 1) - col0) * b.ld * 2) + slot * 16;
+  for (int j = 0; j < S::LB; ++j) {
+    const int64_t r = col0 + (wave * S::LB + j) * S::group + lrow;
+    vb[j] = (unsigned)((min(r, b.rows - 1) - col0) * b.ld * 2) + slot(j) * 16;
   }
 #pragma unroll
   for (int bi = 0; bi < S::WM; ++bi)
@@ -83,51 +98,92 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[bi][bj][r] = 0.f;
 
-  int fs = c0 / nkc, fk = c0 % nkc;  // the next chunk to fetch
-  auto fetch = [&](int c) {
-    const int sa = nseg > 1 ? seg_a(fs) : 0, sb = nseg > 1 ? seg_b(fs) : 0;
-    auto ra = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.p + (sa * a.plane + row0 * a.ld) * 2), 0,
-                                                kBound, 0x00027000);
-    auto rb = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)b.p + (sb * b.plane + col0 * b.ld) * 2), 0,
-                                                kBound, 0x00027000);
-    char* st = lds + ((c - c0) % S::STAGES) * S::stage_bytes;
-    const int so = fk * (kChunkK * 2);
-    const bool out = fk * kChunkK + slot * 8 >= K;
-#pragma unroll
-    for (int j = 0; j < LA; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(st + (wave * LA + j) * 1024), 16, out ? kOut : va[j],
-                                               so, 0, 0);
-#pragma unroll
-    for (int j = 0; j < LB; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(st + S::BM * 128 + (wave * LB + j) * 1024), 16,
-                                               out ? kOut : vb[j], so, 0, 0);
-    if (++fk == nkc) {
+  // The chunk being fetched: its resources, place along k, and stage.  Past the
+  // last chunk it is that one again, so that the count of loads stays.
+  int fc = c0, fs = c0 / nkc, fk = c0 % nkc, fst = 0;
+  auto base = [&](const Side& x, int plane, int64_t row) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)x.p + (plane * x.plane + row * x.ld) * 2), 0, kBound,
+                                             0x00027000);
+  };
+  auto issue = [&](int j) {  // load j of the chunk's L
+    const int left = K - fk * S::BK;  // slots from left / 8 on lie past K
+    char* st = lds + fst * S::stage_bytes;
+    const int so = fk * S::row_bytes;
+    if (j < S::LA) {
+      auto r = base(a, nseg > 1 ? seg_a(fs) : 0, row0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(st + (wave * S::LA + j) * 1024), 16,
+                                               slot(j) * 8 < left ? va[j] : kOut, so, 0, 0);
+    } else {
+      const int i = j - S::LA;
+      auto r = base(b, nseg > 1 ? seg_b(fs) : 0, col0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(st + S::BM * S::row_bytes + (wave * S::LB + i) * 1024),
+                                               16, slot(i) * 8 < left ? vb[i] : kOut, so, 0, 0);
+    }
+  };
+  auto advance = [&]() {
+    fst = fst + 1 == D ? 0 : fst + 1;
+    if (++fc < c1 && ++fk == nkc) {
       fk = 0;
       ++fs;
     }
   };
-  fetch(c0);
-  for (int c = c0; c < c1; ++c) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wavefront's part of chunk c; the barrier: everyone's
-    __syncthreads();                     // and everyone has read chunk c - 1, whose buffer c + 1 takes
-    if (c + 1 < c1) fetch(c + 1);
-    const char* st = lds + ((c - c0) % S::STAGES) * S::stage_bytes;
+  frag<E> fa[2][S::WM], fb[2][S::WN];
+  // operand i of step k (the columns' first: the products start with them)
+  auto read = [&](int set, const char* st, int k, int i) {
+    const int sl = ((2 * k + h) ^ S::turn(l32)) * 16;
+    if (i < S::WN)
+      fb[set][i] = *(const frag<E>*)(st + S::BM * S::row_bytes + ((wn * S::WN + i) * 32 + l32) * S::row_bytes + sl);
+    else
+      fa[set][i - S::WN] = *(const frag<E>*)(st + ((wm * S::WM + i - S::WN) * 32 + l32) * S::row_bytes + sl);
+  };
+  // The products of step k.  Among them, one at a time, so that the wavefronts
+  // do not queue up for LDS or the loads with the matrix cores idle: the reads of
+  // the next step's operands (step kn of stage st) and the step's share of the
+  // next chunk's loads.
+  auto multiply = [&](int k, const char* st, int kn) {
+    constexpr int per = S::WM * S::WN, gap = per / LP;
+    static_assert(L % SP == 0 && per % LP == 0, "");
 #pragma unroll
-    for (int k = 0; k < kChunkK / 16; ++k) {
-      const int sl = ((2 * k + h) ^ (l32 & 7)) * 16;
-      frag<E> fa[S::WM], fb[S::WN];
+    for (int i = 0; i < per; ++i) {
+      const int bi = i / S::WN, bj = i % S::WN;
+      acc[bi][bj] = mfma16(fa[k & 1][bi], fb[k & 1][bj], acc[bi][bj]);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int bi = 0; bi < S::WM; ++bi)
-        fa[bi] = *(const frag<E>*)(st + ((wm * S::WM + bi) * 32 + l32) * 128 + sl);
-#pragma unroll
-      for (int bj = 0; bj < S::WN; ++bj)
-        fb[bj] = *(const frag<E>*)(st + S::BM * 128 + ((wn * S::WN + bj) * 32 + l32) * 128 + sl);
-#pragma unroll
-      for (int bi = 0; bi < S::WM; ++bi)
-#pragma unroll
-        for (int bj = 0; bj < S::WN; ++bj) acc[bi][bj] = mfma16(fa[bi], fb[bj], acc[bi][bj]);
+      for (int j = i * (S::WM + S::WN) / per; j < (i + 1) * (S::WM + S::WN) / per; ++j) read((k + 1) & 1, st, kn, j);
+      if (i % gap == 0 && k < SP) issue(k * LP + i / gap);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  };
+  auto arrive = [&](auto vm) {  // this wavefront's part of the next chunk is in LDS; the barrier: everyone's
+    __builtin_amdgcn_sched_barrier(0);
+    wait_loads<decltype(vm)::value>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+#pragma unroll
+  for (int i = 0; i < D - 1; ++i) {
+#pragma unroll
+    for (int j = 0; j < L; ++j) issue(j);
+    advance();
   }
+  arrive(std::integral_constant<int, (D - 2) * L>{});
+#pragma unroll
+  for (int i = 0; i < S::WM + S::WN; ++i) read(0, lds, 0, i);
+  int cst = 0;
+  for (int c = c0; c < c1; ++c) {
+    // (the chunk fetched goes into the stage of chunk c - 1, which everyone has read)
+    const char* st = lds + cst * S::stage_bytes;
+    cst = cst + 1 == D ? 0 : cst + 1;
+#pragma unroll
+    for (int k = 0; k < NS - 1; ++k) multiply(k, st, k + 1);
+    // in flight may be: the chunks after the next, and of the last of them what has been requested
+    arrive(std::integral_constant<int, D == 2 ? 0 : (D - 3) * L + (NS - 1) * LP>{});
+    multiply(NS - 1, lds + cst * S::stage_bytes, 0);
+    advance();
+  }
+  wait_loads<0>();
   __syncthreads();
 #endif
 }
