@@ -840,11 +840,11 @@ hipError_t launch_typed(const HeadArgs& a, bool grad, void* scratch, hipStream_t
 }  // namespace
 
 size_t head_scratch(const HeadArgs& a, bool grad) {
-  return a.n == 0 ? 0 : head_is_few(a) ? head_few_scratch(a, grad) : plan_of(a, grad).bytes;
+  return a.n == 0 ? 0 : head_form(a) != HEAD_TILED ? head_short_scratch(a, grad) : plan_of(a, grad).bytes;
 }
 
 hipError_t launch_head(const HeadArgs& a, bool grad, void* scratch, hipStream_t s) {
-  if (a.n > 0 && head_is_few(a)) return launch_head_few(a, grad, scratch, s);
+  if (a.n > 0 && head_form(a) != HEAD_TILED) return launch_head_short(a, grad, scratch, s);
   switch (a.type) {
     case TYPE_F32: return launch_typed<float, bf16_t, 3>(a, grad, scratch, s);
     case TYPE_F16: return launch_typed<half_t, half_t, 1>(a, grad, scratch, s);

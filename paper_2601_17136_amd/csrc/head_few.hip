@@ -310,20 +310,21 @@ __global__ __launch_bounds__(256) void targets_few_kernel(FewArgs a, int ntiles)
   a.fix_val[i * a.m + tid] = z == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z - safe(lse2)) - qs);
 }
 
-// Few rows: Z becomes G^T, without the targets, which fix_few_kernel puts in.
-__global__ __launch_bounds__(256) void grad_few_kernel(float* __restrict__ C, int64_t count, int S, int64_t n,
-                                                       const float* __restrict__ lse2,
-                                                       const float* __restrict__ coef) {
+// Few rows: Z becomes G^T; the targets' entries come from the rows' lists.
+__global__ __launch_bounds__(256) void grad_few_kernel(float* __restrict__ C, int64_t count, int S, int64_t n, int m,
+                                                       const float* __restrict__ lse2, const float* __restrict__ coef,
+                                                       const int32_t* __restrict__ id, const float* __restrict__ val) {
   const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (x >= count) return;
-  const int64_t t = x % S;
+  const int64_t v = x / S, t = x - v * S;
   const float cf = t < n ? coef[t] : 0.f;
-  C[x] = cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(C[x] - lse2[t]);
-}
-__global__ __launch_bounds__(256) void fix_few_kernel(float* __restrict__ C, int S, const int32_t* __restrict__ id,
-                                                      const float* __restrict__ val, int64_t pairs, int m) {
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (x < pairs && id[x] >= 0) C[(int64_t)id[x] * S + x / m] = val[x];
+  float g = 0.f;
+  if (cf != 0.f) {
+    g = cf * __builtin_amdgcn_exp2f(C[x] - lse2[t]);
+    for (int j = 0; j < m; ++j)
+      if (id[t * m + j] == v) g = val[t * m + j];
+  }
+  C[x] = g;
 }
 
 // A row that takes no part: weight[row] is `none` (0, or -inf).
@@ -396,8 +397,9 @@ __global__ __launch_bounds__(256) void rows_few_kernel(const float* __restrict__
   }
 }
 
-// slab (S x d) = C^T X over this workgroup's rows of X (R x d), rows that take
-// no part left out.  A step is 4 UN rows: a lane loads kVec features of row
+// out (M x d) = C^T X, rows of X (R x d) that take no part left out and rows of
+// out that take none 0: S columns of C a workgroup, and where blockIdx.y splits
+// the rows of X, their sums into that slab.  A step is 4 UN rows: a lane loads kVec features of row
 // lane / 16 in each of CH blocks of 16 kVec features, and S / 16 of the row's
 // entries of C.  The four wavefronts take every fourth step and join in LDS.
 template <typename XT, int S>
@@ -408,17 +410,20 @@ struct ColsShape {
   static constexpr int width = CH * 16 * VEC;
 };
 template <typename XT, int S>
-__global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__ C, const XT* __restrict__ X,
-                                                       int64_t ldx, int64_t R, int d,
+__global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__ C, int64_t ldc,
+                                                       const XT* __restrict__ X, int64_t ldx, int64_t R, int d,
                                                        const float* __restrict__ weight, float none, int64_t per,
-                                                       float* __restrict__ slabs) {
+                                                       float* __restrict__ slabs, int M,
+                                                       const float* __restrict__ weight_m, XT* __restrict__ out,
+                                                       int64_t ldo) {
   using Sh = ColsShape<XT, S>;
   constexpr int VEC = Sh::VEC, CT = Sh::CT, CH = Sh::CH, UN = Sh::UN;
   typedef float cvec __attribute__((ext_vector_type(CT)));
   __shared__ float red[S][16 * VEC + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * Sh::width;
+  const int c0 = blockIdx.x * Sh::width, s0 = blockIdx.z * S;
+  C += s0;
   const int64_t lo = (int64_t)blockIdx.y * per, hi = min(lo + per, R);
   floatx4 acc[CH][VEC][CT];
 #pragma unroll
@@ -446,7 +451,7 @@ __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__
           xn[u][h] = load_raw(xr, col, d);
         }
       }
-      const cvec cv = *(const cvec*)(C + (row < hi ? row : lo) * S + CT * l16);
+      const cvec cv = *(const cvec*)(C + (row < hi ? row : lo) * ldc + CT * l16);
 #pragma unroll
       for (int t = 0; t < CT; ++t) cn[u][t] = ((const float*)&cv)[t];
       un[u] = use;
@@ -477,7 +482,7 @@ __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__
             acc[h][j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(c[u][t], (float)x[u][h][j], acc[h][j][t], 0, 0, 0);
   }
   // entry r of block (j, t): row CT (4 g + r) + t of the slab, feature VEC l16 + j
-  float* slab = slabs + (int64_t)blockIdx.y * S * d;
+  float* slab = slabs + ((int64_t)blockIdx.y * M + s0) * d;
 #pragma unroll
   for (int h = 0; h < CH; ++h) {
     for (int o = 0; o < 4; ++o) {
@@ -495,16 +500,20 @@ __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__
     }
     for (int y = threadIdx.x; y < S * 16 * VEC; y += 256) {
       const int sr = y / (16 * VEC), cc = c0 + h * 16 * VEC + y % (16 * VEC);
-      if (cc < d) slab[(int64_t)sr * d + cc] = red[sr][y % (16 * VEC)];
+      if (cc >= d || s0 + sr >= M) continue;
+      const float v = red[sr][y % (16 * VEC)];
+      if (out)
+        out[(s0 + sr) * ldo + cc] = (XT)(takes_part(weight_m, 0.f, s0 + sr) ? v : 0.f);
+      else
+        slab[(int64_t)sr * d + cc] = v;
     }
     __syncthreads();
   }
 }
 
-// out (M x d, M <= S) from the slabs, in order; rows of weight 0 are 0.
+// out (M x d) from the slabs, in order; rows of weight 0 are 0.
 template <typename OT>
-__global__ __launch_bounds__(256) void slabs_few_kernel(const float* __restrict__ slabs, int count, int S, int M,
-                                                        int d, const float* __restrict__ weight,
+__global__ __launch_bounds__(256) void slabs_few_kernel(const float* __restrict__ slabs, int count, int M, int d, const float* __restrict__ weight,
                                                         OT* __restrict__ out, int64_t ldo) {
   const int64_t x = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
   const int wave = threadIdx.x >> 6;
@@ -512,7 +521,7 @@ __global__ __launch_bounds__(256) void slabs_few_kernel(const float* __restrict_
   float s = 0.f;
   if (x < (int64_t)M * d)
 #pragma unroll 8
-    for (int k = wave; k < count; k += 4) s += slabs[(int64_t)k * S * d + x];
+    for (int k = wave; k < count; k += 4) s += slabs[(int64_t)k * M * d + x];
   red[wave][threadIdx.x & 63] = s;
   __syncthreads();
   if (wave || x >= (int64_t)M * d) return;
@@ -520,6 +529,214 @@ __global__ __launch_bounds__(256) void slabs_few_kernel(const float* __restrict_
   s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
   const int64_t row = x / d;
   out[row * ldo + (x - row * d)] = (OT)(takes_part(weight, 0.f, row) ? s : 0.f);
+}
+
+// ------------------------------------------------------------------ both sides longer, little work
+
+// 32 rows of h by 64 classes: Z in base 2, [n][ldz].
+template <typename XT>
+__global__ __launch_bounds__(256) void scores_direct_kernel(FewArgs a, int64_t ldz) {
+  __shared__ float zs[4][32][65];
+  const int64_t v0 = (int64_t)blockIdx.x * 64, t0 = (int64_t)blockIdx.y * 32;
+  scores_block<XT, 4, 2>(a, v0, t0, zs);
+#pragma unroll
+  for (int x = threadIdx.x; x < 32 * 64; x += 256)
+    if (t0 + x / 64 < a.n) a.C[(t0 + x / 64) * ldz + v0 + x % 64] = zs[0][x / 64][x % 64];
+}
+
+// lse, the loss, and Z becomes G: a row by WR wavefronts (1, or 4 where it is
+// long), which all hold its pairs, lane l the pairs l, l + 64, ...
+template <int NQ, int WR>
+__global__ __launch_bounds__(256) void row_direct_kernel(FewArgs a, int64_t ldz, bool grad) {
+  __shared__ float red[2][4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t i = WR == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
+  if (i >= a.n) return;
+  float* zr = a.C + i * ldz;
+  int id[NQ];
+  float q[NQ], z[NQ], tm = -INFINITY, ts = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    const int j = k * 64 + lane;
+    id[k] = -1;
+    q[k] = j < a.m ? pair_logit(a, i * a.m + j, id[k], bad) : -INFINITY;
+    z[k] = id[k] >= 0 ? zr[id[k]] : 0.f;
+    tm = fmaxf(tm, q[k]);
+  }
+  const float dl = grad ? a.dloss[i] : 0.f;
+  float m = -INFINITY, s = 0.f;
+  const int64_t c0 = (WR == 1 ? lane : threadIdx.x) * 4;
+#pragma unroll 4
+  for (int64_t c = c0; c < ldz; c += 256 * WR) {
+    const floatx4 v = *(const floatx4*)(zr + c);
+    const float nm = fmaxf(fmaxf(m, fmaxf(v[0], v[1])), fmaxf(v[2], v[3])), n0 = safe(nm);
+    s *= __builtin_amdgcn_exp2f(m - n0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(v[e] - n0);
+    m = nm;
+  }
+  float top = near_max<64>(m);
+  s = wave_sum(s * __builtin_amdgcn_exp2f(m - safe(top)));
+  if (WR > 1) {
+    if (lane == 0) {
+      red[0][wave] = top;
+      red[1][wave] = s;
+    }
+    __syncthreads();  // (also: every target's z is read before any G is written)
+    top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s += red[1][w] * __builtin_amdgcn_exp2f(red[0][w] - safe(top));
+  }
+  const float lse2 = top + log2f(s);
+  tm = safe(near_max<64>(tm));
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    q[k] = id[k] < 0 ? 0.f : expf(q[k] - tm);
+    ts += q[k];
+  }
+  ts = wave_sum(ts);
+  bad = __ballot(bad) != 0;
+  const bool some = ts != 0.f, writer = lane == 0 && (WR == 1 || wave == 0);
+  float l = 0.f;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    q[k] = some ? q[k] / ts : 0.f;
+    if (q[k] != 0.f) l += q[k] * (logf(q[k]) + (z[k] == -INFINITY ? INFINITY : lse2 - z[k]) * kLn2);
+  }
+  l = wave_sum(l);
+  if (writer) {
+    a.loss[i] = bad ? __builtin_nanf("") : some ? l : 0.f;
+    a.lse[i] = lse2 * kLn2;
+  }
+  if (!grad) return;
+  float cf = dl * a.scale;
+  if (!some || lse2 == -INFINITY) cf = 0.f;
+  if (bad) cf = __builtin_nanf("");
+  if (writer) a.coef[i] = cf;
+  const float l2 = safe(lse2);
+#pragma unroll 4
+  for (int64_t c = c0; c < ldz; c += 256 * WR) {
+    floatx4 v = *(const floatx4*)(zr + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(v[e] - l2);
+    *(floatx4*)(zr + c) = v;
+  }
+  // the targets' entries, a class named twice once, after the row's own stores
+  float g[NQ];
+  bool first[NQ];
+#pragma unroll
+  for (int k = 0; k < NQ; ++k) {
+    float qs = 0.f;
+    first[k] = true;
+    for (int jj = 0; jj < a.m; ++jj) {
+      int ij = -1;
+      float qj = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < NQ; ++kk)
+        if (jj / 64 == kk) {
+          ij = __shfl(id[kk], jj & 63, 64);
+          qj = __shfl(q[kk], jj & 63, 64);
+        }
+      if (ij == id[k]) {
+        qs += qj;
+        if (jj < k * 64 + lane) first[k] = false;
+      }
+    }
+    g[k] = z[k] == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z[k] - l2) - qs);
+  }
+  if (WR > 1) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the row is written
+  }
+  if (cf == 0.f || (WR > 1 && wave)) return;
+#pragma unroll
+  for (int k = 0; k < NQ; ++k)
+    if (id[k] >= 0 && first[k]) zr[id[k]] = g[k];
+}
+
+// out (R x d) = C (R x K) B (K x d) for any K (C padded with zeros to 16): as
+// rows_few_kernel, 32 rows by 16 kVec features a workgroup, whose wavefronts
+// take every fourth 16 of K and join in LDS.  blockIdx.z splits K into slabs.
+template <typename XT>
+__global__ __launch_bounds__(256) void rows_direct_kernel(const float* __restrict__ C, int64_t ldc,
+                                                          const XT* __restrict__ B, int64_t ldb, int K,
+                                                          const float* __restrict__ weight_b, float none_b, int64_t R,
+                                                          int d, const float* __restrict__ weight_r, int per,
+                                                          float* __restrict__ slabs, XT* __restrict__ out,
+                                                          int64_t ldo) {
+  constexpr int VEC = kVec<XT>, W = 16 * VEC;
+  __shared__ float red[4][32][W + 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int c0 = blockIdx.x * W, place = (l16 >> 2) + 4 * (l16 & 3);
+  const int64_t r0 = (int64_t)blockIdx.y * 32;
+  const float* cr[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) cr[t] = C + min(r0 + t * 16 + l16, R - 1) * ldc + 4 * g;
+  floatx4 acc[VEC][2];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) acc[j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  raw_vec<XT> b[4], bn[4];
+  floatx4 c[2], cn[2];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) cn[t] = *(const floatx4*)(cr[t] + k0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = k0 + 4 * g + e;
+      const bool use = k < K && takes_part(weight_b, none_b, k);
+      bn[e] = load_raw(B + (int64_t)(use ? k : 0) * ldb, c0 + place * VEC, use ? d : 0);
+    }
+  };
+  const int end = min(K, ((int)blockIdx.z + 1) * per);
+  int k0 = blockIdx.z * per + wave * 16;
+  if (k0 < end) fetch(k0);
+  for (; k0 < end; k0 += 64) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = bn[e];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) c[t] = cn[t];
+    if (k0 + 64 < end) fetch(k0 + 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[e][j], c[t][e], acc[j][t], 0, 0, 0);
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) red[wave][t * 16 + l16][VEC * (g + 4 * r) + j] = acc[j][t][r];
+  __syncthreads();
+#pragma unroll
+  for (int x = threadIdx.x; x < 32 * 16; x += 256) {
+    const int rr = x / 16, cc = (x % 16) * VEC;
+    const int64_t row = r0 + rr;
+    if (row >= R || c0 + cc >= d) continue;
+    const bool part = takes_part(weight_r, 0.f, row);
+    float v[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      v[e] = part ? (red[0][rr][cc + e] + red[1][rr][cc + e]) + (red[2][rr][cc + e] + red[3][rr][cc + e]) : 0.f;
+    if (out) {
+      store_part(out + row * ldo, c0 + cc, d, v);
+    } else {
+      float* p = slabs + ((int64_t)blockIdx.z * R + row) * d + c0 + cc;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (c0 + cc + e < d) p[e] = v[e];
+    }
+  }
 }
 
 // ------------------------------------------------------------------ plan
@@ -568,7 +785,7 @@ FewPlan few_plan(const HeadArgs& a, bool grad) {
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(512, chunks), cdiv(p.R, 64)));
     p.per = up(cdiv(p.R, p.splits), 64);
     p.splits = (int)cdiv(p.R, p.per);
-    p.slabs = take((size_t)p.splits * p.S * a.d * 4);
+    if (p.splits > 1) p.slabs = take((size_t)p.splits * s * a.d * 4);
   }
   p.bytes = at;
   return p;
@@ -587,6 +804,18 @@ void by_short(int S, F&& f) {
   if (S == 16) f(num<16>{});
   else if (S == 32) f(num<32>{});
   else f(num<64>{});
+}
+
+// out (M x d) = C^T X, C [R][ldc], over `splits` slabs
+template <typename XT, int S>
+void cols(const float* weight, float none, const float* C, int64_t ldc, const void* X, int64_t ldx, int64_t R, int d,
+          int splits, int64_t per, float* slabs, int M, const float* weight_m, void* out, int64_t ldo, hipStream_t s) {
+  const dim3 grid((unsigned)cdiv(d, ColsShape<XT, S>::width), (unsigned)splits, (unsigned)cdiv(M, S));
+  hipLaunchKernelGGL((cols_few_kernel<XT, S>), grid, dim3(256), 0, s, C, ldc, (const XT*)X, ldx, R, d, weight, none,
+                     per, slabs, M, weight_m, splits > 1 ? nullptr : (XT*)out, ldo);
+  if (splits > 1)
+    hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3((unsigned)cdiv((int64_t)M * d, 64)), dim3(256), 0, s, slabs,
+                       splits, M, d, weight_m, (XT*)out, ldo);
 }
 
 template <typename XT>
@@ -622,11 +851,9 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
     });
     KKM_TRY(hipGetLastError());
     if (grad) {
-      const int64_t count = p.R * p.S, pairs = a.n * a.m;
-      hipLaunchKernelGGL(grad_few_kernel, dim3((unsigned)cdiv(count, 256)), dim3(256), 0, s, f.C, count, p.S, a.n,
-                         f.lse2, f.coef);
-      hipLaunchKernelGGL(fix_few_kernel, dim3((unsigned)cdiv(pairs, 256)), dim3(256), 0, s, f.C, p.S, f.fix_id,
-                         f.fix_val, pairs, a.m);
+      const int64_t count = p.R * p.S;
+      hipLaunchKernelGGL(grad_few_kernel, dim3((unsigned)cdiv(count, 256)), dim3(256), 0, s, f.C, count, p.S, a.n, a.m,
+                         f.lse2, f.coef, f.fix_id, f.fix_val);
       KKM_TRY(hipGetLastError());
     }
   }
@@ -640,15 +867,10 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   by_short(p.S, [&](auto S_) {
     constexpr int S = decltype(S_)::value;
     // (the sums first: the long side's rows may still be in the last-level cache)
-    if (short_out) {
-      float* slabs = (float*)(ws + p.slabs);
-      hipLaunchKernelGGL((cols_few_kernel<XT, S>), dim3((unsigned)cdiv(a.d, ColsShape<XT, S>::width), (unsigned)p.splits), dim3(256),
-                         0, s, f.C, (const XT*)(p.classes ? a.h : a.w), p.classes ? a.ldh : a.ldw, p.R, a.d,
-                         p.classes ? f.coef : a.offset, p.classes ? 0.f : none, p.per, slabs);
-      hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3((unsigned)cdiv((int64_t)rows_b * a.d, 64)), dim3(256), 0, s,
-                         slabs, p.splits, S, rows_b, a.d, p.classes ? nullptr : f.coef, (XT*)short_out,
-                         p.classes ? a.lddw : a.lddh);
-    }
+    if (short_out)
+      cols<XT, S>(p.classes ? f.coef : a.offset, p.classes ? 0.f : none, f.C, p.S, p.classes ? a.h : a.w,
+                  p.classes ? a.ldh : a.ldw, p.R, a.d, p.splits, p.per, (float*)(ws + p.slabs), rows_b,
+                  p.classes ? nullptr : f.coef, short_out, p.classes ? a.lddw : a.lddh, s);
     if (long_out) {
       const int64_t cols = cdiv(a.d, 64 * VEC);
       const dim3 grid((unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max<int64_t>(1, 1536 / cols)), (unsigned)cols);
@@ -660,17 +882,104 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
+struct DirectPlan {
+  int64_t ldz, per;  // per: rows of h of a slab of dW
+  int splits;
+  int perh, splitsh;  // classes of a slab of dH
+  size_t C, coef, slabs, bytes;
+};
+
+DirectPlan direct_plan(const HeadArgs& a, bool grad) {
+  DirectPlan p{};
+  p.ldz = up(a.classes, 64);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t r = at;
+    at += up(bytes, 1024);
+    return r;
+  };
+  p.C = take((size_t)a.n * p.ldz * 4);
+  if (grad) {
+    p.coef = take((size_t)a.n * 4);
+    const int64_t chunks = cdiv(a.d, 256 / (int)elem_bytes(a.type));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(512, chunks * (p.ldz / 64)), cdiv(a.n, 128)));
+    p.per = up(cdiv(a.n, p.splits), 64);
+    p.splits = (int)cdiv(a.n, p.per);
+    p.splitsh = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(256, chunks * cdiv(a.n, 32)), p.ldz / 256));
+    p.perh = (int)up(cdiv(a.classes, p.splitsh), 64);
+    p.splitsh = (int)cdiv(a.classes, p.perh);
+    const size_t w = p.splits > 1 ? (size_t)p.splits * a.classes * a.d : 0,
+                 h = p.splitsh > 1 ? (size_t)p.splitsh * a.n * a.d : 0;
+    if (std::max(w, h)) p.slabs = take(std::max(w, h) * 4);  // of one, then of the other
+  }
+  p.bytes = at;
+  return p;
+}
+
+template <typename XT>
+hipError_t direct_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
+  const DirectPlan p = direct_plan(a, grad);
+  FewArgs f{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, a.scale * kLog2e, a.scale, a.tscale, a.offset,
+            a.ids, a.tlogits, a.dloss, a.loss, a.lse, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+  f.C = (float*)(ws + p.C);
+  f.coef = (float*)(ws + p.coef);
+  float* slabs = (float*)(ws + p.slabs);
+  hipLaunchKernelGGL((scores_direct_kernel<XT>), dim3((unsigned)(p.ldz / 64), (unsigned)cdiv(a.n, 32)), dim3(256), 0, s,
+                     f, p.ldz);
+  auto rows = [&](auto nq, auto wr) {
+    hipLaunchKernelGGL((row_direct_kernel<decltype(nq)::value, decltype(wr)::value>),
+                       dim3((unsigned)(wr == 1 ? cdiv(a.n, 4) : a.n)), dim3(256), 0, s, f, p.ldz, grad);
+  };
+  const bool longer = a.classes > 1024;
+  if (a.m <= 64) longer ? rows(num<1>{}, num<4>{}) : rows(num<1>{}, num<1>{});
+  else longer ? rows(num<4>{}, num<4>{}) : rows(num<4>{}, num<1>{});
+  KKM_TRY(hipGetLastError());
+  if (grad && a.dw)
+    cols<XT, 64>(f.coef, 0.f, f.C, p.ldz, a.h, a.ldh, a.n, a.d, p.splits, p.per, slabs, a.classes, nullptr, a.dw,
+                 a.lddw, s);
+  if (grad && a.dh) {
+    const dim3 grid((unsigned)cdiv(a.d, 16 * kVec<XT>), (unsigned)cdiv(a.n, 32), (unsigned)p.splitsh);
+    hipLaunchKernelGGL((rows_direct_kernel<XT>), grid, dim3(256), 0, s, f.C, p.ldz, (const XT*)a.w, a.ldw, a.classes,
+                       a.offset, -INFINITY, a.n, a.d, f.coef, p.perh, slabs, p.splitsh > 1 ? nullptr : (XT*)a.dh,
+                       a.lddh);
+    if (p.splitsh > 1)
+      hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3((unsigned)cdiv(a.n * a.d, 64)), dim3(256), 0, s, slabs,
+                         p.splitsh, (int)a.n, a.d, f.coef, (XT*)a.dh, a.lddh);
+  }
+  return hipGetLastError();
+}
+
 }  // namespace
 
-bool head_is_few(const HeadArgs& a) { return a.classes <= kFew || a.n <= kFew; }
+// DIRECT up to so much work (n times classes times d): it needs four launches in
+// place of eight or more and no copies, but multiplies in fp32 on the way to the
+// gradients, and holds n times classes scores.  Microseconds with gradient, TILED
+// / DIRECT: fp32, 400 classes of 300 features 119 / 46 at n = 100, 136 / 70 at
+// 2000, 185 / 156 at 8000; 100 of 1000 225 / 59 at 2000, 610 / 426 at 30000; 1000 of
+// 1000 203 / 50 at 100, 308 / 216 at 2000; 1000 of 300 256 / 340 at 8000.  bfloat16,
+// 400 of 300 77 / 61 at 100, 89 / 87 at 2000; 1000 of 300 83 / 64 at 500, 90 / 139
+// at 2000; 400 of 64 83 / 102 at 8000.
+HeadForm head_form(const HeadArgs& a) {
+  if (a.classes <= kFew || a.n <= kFew) return HEAD_FEW;
+  const double work = (double)a.n * a.classes * a.d;
+  const double most = a.type != TYPE_F32 ? 1.5e8 : a.classes <= 128 ? 3e9 : a.d >= 600 ? 2e9 : 8e8;
+  return a.n * (int64_t)a.classes <= kDirectScores && work <= most ? HEAD_DIRECT : HEAD_TILED;
+}
 
-size_t head_few_scratch(const HeadArgs& a, bool grad) { return few_plan(a, grad).bytes; }
+size_t head_short_scratch(const HeadArgs& a, bool grad) {
+  return head_form(a) == HEAD_FEW ? few_plan(a, grad).bytes : direct_plan(a, grad).bytes;
+}
 
-hipError_t launch_head_few(const HeadArgs& a, bool grad, void* scratch, hipStream_t s) {
+hipError_t launch_head_short(const HeadArgs& a, bool grad, void* scratch, hipStream_t s) {
+  const bool few = head_form(a) == HEAD_FEW;
+  auto run = [&](auto x) {
+    using XT = decltype(x);
+    return few ? few_typed<XT>(a, grad, (char*)scratch, s) : direct_typed<XT>(a, grad, (char*)scratch, s);
+  };
   switch (a.type) {
-    case TYPE_F32: return few_typed<float>(a, grad, (char*)scratch, s);
-    case TYPE_F16: return few_typed<half_t>(a, grad, (char*)scratch, s);
-    default: return few_typed<bf16_t>(a, grad, (char*)scratch, s);
+    case TYPE_F32: return run(float{});
+    case TYPE_F16: return run(half_t{});
+    default: return run(bf16_t{});
   }
 }
 

@@ -53,11 +53,15 @@ struct HeadArgs {
 };
 constexpr int kMaxTop = 256;
 
-// A head with a short side (head_few.hip): at most kFew classes, or rows.
+// How a head runs: FEW, at most kFew classes or rows, and DIRECT, little work on
+// more of both, straight from the rows (head_few.hip); TILED, matrix products of
+// copies in tiles, the logits never stored (head.hip).
+enum HeadForm { HEAD_FEW, HEAD_DIRECT, HEAD_TILED };
 constexpr int kFew = 64;
-bool head_is_few(const HeadArgs& a);
-size_t head_few_scratch(const HeadArgs& a, bool grad);
-hipError_t launch_head_few(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);
+constexpr int64_t kDirectScores = (int64_t)16 << 20;  // n times classes: 64 MB of scores
+HeadForm head_form(const HeadArgs& a);
+size_t head_short_scratch(const HeadArgs& a, bool grad);
+hipError_t launch_head_short(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);
 
 size_t head_scratch(const HeadArgs& a, bool grad);
 hipError_t launch_head(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);

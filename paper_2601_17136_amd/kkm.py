@@ -8,6 +8,7 @@ library has not been built, loading it fails loudly; there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -498,30 +499,38 @@ def _rows(t, name, dtype=None, shape=None):
     return t.data_ptr(), ld
 
 
-class _ordered:
-    """The context's stream as the place of the call's work: where torch's
-    current stream is another, the work waits for what that stream has enqueued,
-    that stream waits for the work, and the tensors' memory is held until then."""
+class _Elsewhere:
+    """Work on the context's stream while torch's current stream is another: it
+    waits for what that stream has enqueued, that stream waits for it, and the
+    tensors' memory is held until then."""
 
-    def __init__(self, ctx, *tensors):
+    def __init__(self, handle, tensors):
         import torch
-        h = _vp()
-        _check(lib().kkm_get_stream(ctx, ctypes.byref(h)), ctx)
         self.here = torch.cuda.current_stream()
-        self.there = None
-        if (h.value or 0) != self.here.cuda_stream:
-            self.there = torch.cuda.ExternalStream(h.value or 0) if h.value else torch.cuda.default_stream()
-            self.tensors = [t for t in tensors if t is not None]
+        self.there = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+        self.tensors = [t for t in tensors if t is not None]
 
     def __enter__(self):
-        if self.there is not None:
-            self.there.wait_stream(self.here)
+        self.there.wait_stream(self.here)
 
     def __exit__(self, *exc):
-        if self.there is not None:
-            self.here.wait_stream(self.there)
-            for t in self.tensors:
-                t.record_stream(self.there)
+        self.here.wait_stream(self.there)
+        for t in self.tensors:
+            t.record_stream(self.there)
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _ordered(ctx, *tensors):
+    """The context's stream as the place of the call's work."""
+    import torch
+    h = _vp()
+    _check(lib().kkm_get_stream(ctx, ctypes.byref(h)), ctx)
+    handle = h.value or 0
+    if handle == torch._C._cuda_getCurrentRawStream(tensors[0].device.index):
+        return _HERE
+    return _Elsewhere(handle, tensors)
 
 
 def kkm_layer_norm(ctx, x, weight, bias, eps: float, y, mean=None, rstd=None) -> None:

@@ -135,7 +135,8 @@ def _check_head(r, loss, lse, dh, dw):
 
 HEAD = [(1, 1, 1), (1, 5, 3), (2, 8, 2), (3, 64, 130), (5, 7, 1000), (33, 100, 17), (64, 54, 7), (127, 65, 129),
         (128, 128, 128), (130, 16, 257), (257, 784, 10), (300, 301, 64), (700, 72, 300), (1030, 24, 65),
-        (2000, 19, 32), (999, 130, 16), (16, 300, 4100), (17, 64, 5000), (64, 40, 16400), (65, 65, 65), (1, 2048, 700)]
+        (2000, 19, 32), (999, 130, 16), (16, 300, 4100), (17, 64, 5000), (64, 40, 16400), (65, 65, 65), (1, 2048, 700),
+        (1500, 2100, 1030), (777, 4000, 1100), (5000, 56, 4000)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -292,7 +293,7 @@ def _teacher(n, V, m, g, kept):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n,d,V,m", [(1, 1, 1, 1), (1, 6, 5, 3), (4, 17, 9, 12), (50, 54, 7, 7), (130, 33, 257, 64),
-                                     (65, 120, 1000, 65), (40, 8, 300, 256), (600, 784, 64, 8), (300, 100, 513, 20)])
+                                     (65, 120, 1000, 65), (40, 8, 300, 256), (600, 784, 64, 8), (300, 100, 513, 20), (100, 60, 2050, 200), (1200, 2050, 1001, 70)])
 def test_distill(ctx, n, d, V, m, dtype):
     from paper_2601_17136_amd import kkm
     pad = (0, 8, 1)[(n + d) % 3]
@@ -405,8 +406,8 @@ def test_workspace_counts_against_the_budget_and_goes_with_a_build():
         h, w, _, ids, dloss, _, _ = _head_case(2000, 64, 100, "f32", 51)
         out = _outputs(h, w)
         kkm.kkm_head_grad(c, h, w, ids, dloss, *out)
-        big = torch.randn(40000, 64, device="cuda")
-        bigids = torch.zeros(40000, dtype=torch.int32, device="cuda")
+        big = torch.randn(200000, 64, device="cuda")
+        bigids = torch.zeros(200000, dtype=torch.int32, device="cuda")
         with pytest.raises(kkm.KKMError) as e:
             kkm.kkm_head_grad(c, big, w, bigids, big[:, 0].contiguous(), *_outputs(big, w))
         assert e.value.code == kkm.KKM_ERR_OOM
