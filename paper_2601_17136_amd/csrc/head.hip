@@ -53,22 +53,40 @@ __device__ inline void split_planes(float x, E (&out)[P]) {
   }
 }
 
+// A copy of h and one of w run in one launch: the first `split` workgroups are
+// the first job's.
+struct StageJob {
+  const void* src;
+  int64_t ld, rows;
+  void* dst;
+  int64_t plane;
+  const float* weight;  // transposed copies: rows of weight `none` are zero; may be null
+  float none;
+  int64_t rp;           // their width
+};
+struct StageJobs {
+  StageJob j[2];
+  unsigned split;
+};
+
 // Rows in place of src's, kp wide (zero from d on), as P planes.  A thread
 // writes 8 values.
 template <typename XT, typename E, int P>
-__global__ __launch_bounds__(256) void stage_rows_kernel(const XT* __restrict__ src, int64_t ld, int64_t rows, int d,
-                                                         int kp, E* __restrict__ dst, int64_t plane) {
-  const int64_t per = kp / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * per) return;
+__global__ __launch_bounds__(256) void stage_rows_kernel(StageJobs jobs, int d, int kp) {
+  const bool second = blockIdx.x >= jobs.split;
+  const StageJob& j = jobs.j[second];
+  const int64_t per = kp / 8, i = (int64_t)(blockIdx.x - (second ? jobs.split : 0u)) * 256 + threadIdx.x;
+  if (i >= j.rows * per) return;
   const int64_t row = i / per;
   const int c = (int)(i - row * per) * 8;
+  const XT* src = (const XT*)j.src + row * j.ld;
   float v[8];
   if constexpr (sizeof(XT) == 2) {
-    load_part(src + row * ld, c, d, v);
+    load_part(src, c, d, v);
   } else {
     float a[4], b[4];
-    load_part(src + row * ld, c, d, a);
-    load_part(src + row * ld, c + 4, d, b);
+    load_part(src, c, d, a);
+    load_part(src, c + 4, d, b);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
   }
@@ -81,26 +99,27 @@ __global__ __launch_bounds__(256) void stage_rows_kernel(const XT* __restrict__ 
     for (int p = 0; p < P; ++p) o[p][e] = pl[p];
   }
 #pragma unroll
-  for (int p = 0; p < P; ++p) *(frag<E>*)(dst + p * plane + row * kp + c) = o[p];
+  for (int p = 0; p < P; ++p) *(frag<E>*)((E*)j.dst + p * j.plane + row * kp + c) = o[p];
 }
 
-// The transposed copy: dst[c][row], rp rows wide (zero from `rows` on).  A row
-// counts as zero where weight[row] is 0, or, LEFT_OUT, -inf.  A workgroup turns
-// a 64 x 64 block through LDS.
-template <typename XT, typename E, int P, bool LEFT_OUT>
-__global__ __launch_bounds__(256) void stage_cols_kernel(const XT* __restrict__ src, int64_t ld, int64_t rows, int d,
-                                                         const float* __restrict__ weight, int64_t rp,
-                                                         E* __restrict__ dst, int64_t plane) {
+// The transposed copies: dst[c][row], rp rows wide (zero from `rows` on).  A
+// workgroup turns a 64 x 64 block through LDS.
+template <typename XT, typename E, int P>
+__global__ __launch_bounds__(256) void stage_cols_kernel(StageJobs jobs, int d) {
   constexpr int VEC = kVec<XT>, LANES = 64 / VEC, PASS = 256 / LANES;  // lanes of a row, rows of a pass
   __shared__ XT tile[64][64 + 4 / sizeof(XT)];
-  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  const bool second = blockIdx.x >= jobs.split;
+  const StageJob& j = jobs.j[second];
+  const XT* src = (const XT*)j.src;
+  E* dst = (E*)j.dst;
+  const int64_t r0 = (int64_t)(blockIdx.x - (second ? jobs.split : 0u)) * 64, rows = j.rows, ld = j.ld, rp = j.rp,
+                plane = j.plane;
   const int c0 = blockIdx.y * 64, col = (threadIdx.x % LANES) * VEC;
 #pragma unroll
   for (int k = 0; k < 64 / PASS; ++k) {
     const int rr = k * PASS + threadIdx.x / LANES;
     const int64_t row = r0 + rr;
-    bool use = row < rows;
-    if (use && weight) use = weight[row] != (LEFT_OUT ? -INFINITY : 0.f);
+    const bool use = row < rows && !(j.weight && j.weight[row] == j.none);
     const raw_vec<XT> v = load_raw(src + (use ? row : 0) * ld, c0 + col, use ? d : 0);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) tile[rr][col + e] = v[e];
@@ -166,6 +185,8 @@ struct ScoreArgs {
   float2* part;         // forward: (largest, sum) in base 2 of each class tile and row, [tile][n]
   // gradient: rows' lse in base 2 and factors, G [row][class of the piece] and its transpose
   const float *lse2, *coef;
+  const int32_t* fix_id;  // one target per row: its entry of G (else fix_kernel's work), or null
+  const float* fix_val;
   E *G, *Gt;
   int64_t ldg, planeg, ldt, planet;
 };
@@ -237,6 +258,9 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void scores_kernel(ScoreArgs
     for (int bj = 0; bj < S::WN; ++bj) {
       const int64_t t = t0 + (wn * S::WN + bj) * 32 + l32;
       const float lse2 = t < a.n ? a.lse2[t] : 0.f, cf = t < a.n ? a.coef[t] : 0.f;
+      const bool one = a.fix_id && t < a.n;
+      const int at = one ? a.fix_id[t] - (int)a.v0 : -1;  // (no class is at -1 - v0)
+      const float val = one ? a.fix_val[t] : 0.f;
 #pragma unroll
       for (int bi = 0; bi < S::WM; ++bi) {
         const int64_t v = cl + (wm * S::WM + bi) * 32;
@@ -245,9 +269,11 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void scores_kernel(ScoreArgs
         for (int q = 0; q < 4; ++q) {
           E pl[4][P];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int e = 0; e < 4; ++e) {
             // (a row without a target has no gradient, whatever its logits)
-            split_planes<E, P>(cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(acc[bi][bj][4 * q + e] - lse2), pl[e]);
+            const float g = cf == 0.f ? 0.f : cf * __builtin_amdgcn_exp2f(acc[bi][bj][4 * q + e] - lse2);
+            split_planes<E, P>((int)v + 8 * q + 4 * h + e == at ? val : g, pl[e]);
+          }
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             o[p][q][0] = pack2(pl[0][p], pl[1][p]);
@@ -488,6 +514,7 @@ struct ProductArgs {
   int64_t M, N;
   int K, nkc, nseg, mt, nt;
   int per;              // chunks of a slab
+  unsigned blocks;      // tiles times slabs
   float* slabs;         // fp32 sums, M x N each, or null: straight to out
   int add;              // to what the slabs hold
   void* out;
@@ -495,20 +522,28 @@ struct ProductArgs {
   const float* alpha;   // null: 1
   const float* coef;    // rows of weight 0 are 0, whatever stands in b; null: none
 };
+// The two products of a piece run in one launch where their tiles are alike.
+struct ProductJobs {
+  ProductArgs j[2];
+};
 
 template <typename E, typename OT, class S>
-__global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductArgs a) {
+__global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductJobs jobs) {
   __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  const bool second = blockIdx.x >= jobs.j[0].blocks;
+  const ProductArgs& a = jobs.j[second];
+  const unsigned g = blockIdx.x - (second ? jobs.j[0].blocks : 0u), tiles = (unsigned)(a.mt * a.nt);
+  const int sl = __builtin_amdgcn_readfirstlane((int)(g / tiles));
   int mi, ni;
-  tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
+  tile_of(g - sl * tiles, tiles, a.mt, a.nt, mi, ni);
   const int64_t r0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
-  const int c0 = blockIdx.y * a.per, c1 = min(c0 + a.per, a.nseg * a.nkc);
+  const int c0 = sl * a.per, c1 = min(c0 + a.per, a.nseg * a.nkc);
   floatx16 acc[S::WM][S::WN];
   tile_product<E, S>(a.a, a.b, r0, n0, a.K, a.nkc, a.nseg, c0, c1, lds, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
   const float alpha = a.alpha ? *a.alpha : 1.f;
-  float* slab = a.slabs ? a.slabs + (int64_t)blockIdx.y * a.M * a.N : nullptr;
+  float* slab = a.slabs ? a.slabs + (int64_t)sl * a.M * a.N : nullptr;
 #pragma unroll
   for (int bi = 0; bi < S::WM; ++bi)
 #pragma unroll
@@ -531,12 +566,27 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductA
 }
 
 // out from the slabs, in order; a thread takes four neighbouring entries of a row.
+struct SlabJob {
+  const float* slabs;
+  int count;
+  int64_t M, N;
+  const float *alpha, *coef;
+  void* out;
+  int64_t ldo;
+  unsigned blocks;
+};
+struct SlabJobs {
+  SlabJob j[2];
+};
 template <typename OT>
-__global__ __launch_bounds__(256) void slabs_kernel(const float* __restrict__ slabs, int count, int64_t M, int64_t N,
-                                                    const float* __restrict__ alpha,
-                                                    const float* __restrict__ coef, OT* __restrict__ out,
-                                                    int64_t ldo) {
-  const int64_t per = (N + 3) / 4, x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void slabs_kernel(SlabJobs jobs) {
+  const bool second = blockIdx.x >= jobs.j[0].blocks;
+  const SlabJob& j = jobs.j[second];
+  const float *slabs = j.slabs, *alpha = j.alpha, *coef = j.coef;
+  OT* out = (OT*)j.out;
+  const int count = j.count;
+  const int64_t M = j.M, N = j.N, ldo = j.ldo;
+  const int64_t per = (N + 3) / 4, x = (int64_t)(blockIdx.x - (second ? jobs.j[0].blocks : 0u)) * 256 + threadIdx.x;
   if (x >= M * per) return;
   const int64_t row = x / per, c = (x - row * per) * 4;
   const int m = (int)min((int64_t)4, N - c);
@@ -668,16 +718,14 @@ struct Head {
   template <typename T>
   T* at(size_t off) const { return (T*)(ws + off); }
 
-  hipError_t side(const void* src, int64_t ld, int64_t rows, size_t off, Side& out) const {
-    if (in_place(a, src, ld)) {
-      out = {src, ld, 0, rows};
-      return hipSuccess;
-    }
+  // The operands as they are multiplied: in place, or a copy at `off`, whose job joins `jobs`.
+  Side side(const void* src, int64_t ld, int64_t rows, size_t off, StageJobs& jobs, int& count) const {
+    if (in_place(a, src, ld)) return {src, ld, 0, rows};
     const int64_t plane = rows * p.kp;
-    hipLaunchKernelGGL((stage_rows_kernel<XT, E, P>), grid1(rows * (p.kp / 8)), dim3(256), 0, s, (const XT*)src, ld,
-                       rows, a.d, p.kp, at<E>(off), plane);
-    out = {at<E>(off), p.kp, plane, rows};
-    return hipGetLastError();
+    jobs.j[count] = {src, ld, rows, at<E>(off), plane, nullptr, 0.f, 0};
+    const unsigned blocks = (unsigned)cdiv(rows * (p.kp / 8), 256);
+    if (count++ == 0) jobs.split = blocks;
+    return {at<E>(off), p.kp, plane, rows};
   }
 
   template <bool GRAD>
@@ -693,10 +741,19 @@ struct Head {
     return hipGetLastError();
   }
 
-  // out (M x N) = A B^T over K, or its slabs where there are any
-  // (K0: the first piece's K, from which the slabs' shares are)
-  hipError_t product(Side x, Side y, int64_t M, int64_t N, int K, int K0, bool big, int slabs, float* slab, int add,
-                     void* out, int64_t ldo, const float* alpha, const float* coef) const {
+  static int chunk_of(bool big) { return big ? BigTile::BK : SmallTile::BK; }
+  // chunks of a slab, and the slabs that a product of K writes
+  int share(int K, bool big, int slabs) const {
+    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, std::max(slabs, 1));
+  }
+  int written(int K, bool big, int slabs) const {
+    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, share(K, big, slabs));
+  }
+
+  // out (M x N) = A B^T over K, or its slabs where there are any (K0: the first
+  // piece's K, from which the slabs' shares are)
+  ProductArgs product(Side x, Side y, int64_t M, int64_t N, int K, int K0, bool big, int slabs, float* slab, int add,
+                      void* out, int64_t ldo, const float* alpha, const float* coef) const {
     ProductArgs pa{};
     pa.a = x;
     pa.b = y;
@@ -708,40 +765,39 @@ struct Head {
     pa.mt = (int)cdiv(M, big ? BigTile::BM : SmallTile::BM);
     pa.nt = (int)cdiv(N, big ? BigTile::BN : SmallTile::BN);
     pa.per = share(K0, big, slabs);
+    pa.blocks = (unsigned)((int64_t)pa.mt * pa.nt * cdiv(pa.nkc * pa.nseg, pa.per));
     pa.slabs = slabs ? slab : nullptr;
     pa.add = add;
     pa.out = out;
     pa.ldo = ldo;
     pa.alpha = alpha;
     pa.coef = coef;
-    const dim3 grid((unsigned)((int64_t)pa.mt * pa.nt), (unsigned)cdiv(pa.nkc * pa.nseg, pa.per));
+    return pa;
+  }
+  hipError_t multiply(const ProductJobs& jobs, bool big) const {
+    const dim3 grid(jobs.j[0].blocks + jobs.j[1].blocks);
     if (big)
-      hipLaunchKernelGGL((product_kernel<E, XT, BigTile>), grid, dim3(BigTile::threads), 0, s, pa);
+      hipLaunchKernelGGL((product_kernel<E, XT, BigTile>), grid, dim3(BigTile::threads), 0, s, jobs);
     else
-      hipLaunchKernelGGL((product_kernel<E, XT, SmallTile>), grid, dim3(SmallTile::threads), 0, s, pa);
+      hipLaunchKernelGGL((product_kernel<E, XT, SmallTile>), grid, dim3(SmallTile::threads), 0, s, jobs);
     return hipGetLastError();
   }
-
-  // chunks of a slab, and the slabs that a product of K wrote
-  static int chunk_of(bool big) { return big ? BigTile::BK : SmallTile::BK; }
-  int share(int K, bool big, int slabs) const {
-    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, std::max(slabs, 1));
-  }
-  int written(int K, bool big, int slabs) const {
-    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, share(K, big, slabs));
-  }
-
-  hipError_t sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, const float* coef,
-                 void* out, int64_t ldo) const {
-    hipLaunchKernelGGL((slabs_kernel<XT>), grid1(M * cdiv(N, 4)), dim3(256), 0, s, slabs, count, M, N, alpha, coef,
-                       (XT*)out, ldo);
-    return hipGetLastError();
+  SlabJob sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, const float* coef, void* out,
+              int64_t ldo) const {
+    return {slabs, count, M, N, alpha, coef, out, ldo, (unsigned)cdiv(M * cdiv(N, 4), 256)};
   }
 
   hipError_t run(bool grad) const {
     ScoreArgs<E> sa{};
-    KKM_TRY(side(a.h, a.ldh, a.n, p.h, sa.h));
-    KKM_TRY(side(a.w, a.ldw, a.classes, p.w, sa.w));
+    StageJobs copies{};
+    int count = 0;
+    sa.h = side(a.h, a.ldh, a.n, p.h, copies, count);
+    sa.w = side(a.w, a.ldw, a.classes, p.w, copies, count);
+    if (count) {
+      const unsigned rest = count > 1 ? (unsigned)cdiv(copies.j[1].rows * (p.kp / 8), 256) : 0u;
+      hipLaunchKernelGGL((stage_rows_kernel<XT, E, P>), dim3(copies.split + rest), dim3(256), 0, s, copies, a.d, p.kp);
+      KKM_TRY(hipGetLastError());
+    }
     sa.n = a.n;
     sa.classes = a.classes;
     sa.K = in_place(a, a.h, a.ldh) || in_place(a, a.w, a.ldw) ? a.d : p.kp;
@@ -777,20 +833,22 @@ struct Head {
     if (!grad) return hipSuccess;
 
     Side ht{at<E>(p.ht), p.n_pad, (int64_t)a.d * p.n_pad, a.d}, wt{at<E>(p.wt), p.v_pad, (int64_t)a.d * p.v_pad, a.d};
+    StageJobs turned{};
     if (a.dw) {
-      hipLaunchKernelGGL((stage_cols_kernel<XT, E, P, false>),
-                         dim3((unsigned)cdiv(a.n, 64), (unsigned)cdiv(a.d, 64)), dim3(256), 0, s, (const XT*)a.h, a.ldh,
-                         a.n, a.d, ta.coef, p.n_pad, at<E>(p.ht), ht.plane);
-      KKM_TRY(hipGetLastError());
+      turned.j[0] = {a.h, a.ldh, a.n, at<E>(p.ht), ht.plane, ta.coef, 0.f, p.n_pad};
+      turned.split = (unsigned)cdiv(a.n, 64);
     }
-    if (a.dh) {
-      hipLaunchKernelGGL((stage_cols_kernel<XT, E, P, true>),
-                         dim3((unsigned)cdiv(a.classes, 64), (unsigned)cdiv(a.d, 64)), dim3(256), 0, s,
-                         (const XT*)a.w, a.ldw, a.classes, a.d, a.offset, p.v_pad, at<E>(p.wt), wt.plane);
-      KKM_TRY(hipGetLastError());
-    }
+    if (a.dh) turned.j[1] = {a.w, a.ldw, a.classes, at<E>(p.wt), wt.plane, a.offset, -INFINITY, p.v_pad};
+    hipLaunchKernelGGL((stage_cols_kernel<XT, E, P>),
+                       dim3(turned.split + (a.dh ? (unsigned)cdiv(a.classes, 64) : 0u), (unsigned)cdiv(a.d, 64)),
+                       dim3(256), 0, s, turned, a.d);
+    KKM_TRY(hipGetLastError());
     sa.lse2 = ta.lse2;
     sa.coef = ta.coef;
+    if (a.m == 1) {
+      sa.fix_id = ta.fix_id;
+      sa.fix_val = ta.fix_val;
+    }
     sa.G = at<E>(p.G);
     sa.Gt = at<E>(p.Gt);
     sa.ldg = p.piece;
@@ -802,23 +860,41 @@ struct Head {
       const int cnt = std::min(p.piece, a.classes - v0), kv = (int)up(cnt, kChunkK);
       sa.v0 = v0;
       KKM_TRY(scores<true>(sa, cnt));
-      hipLaunchKernelGGL((fix_kernel<E, P>), grid1(a.n * a.m), dim3(256), 0, s, ta.fix_id, ta.fix_val, a.n, a.m, v0,
-                         v0 + cnt, sa.G, sa.ldg, sa.planeg, sa.Gt, sa.ldt, sa.planet);
-      KKM_TRY(hipGetLastError());
+      if (a.m > 1) {
+        hipLaunchKernelGGL((fix_kernel<E, P>), grid1(a.n * a.m), dim3(256), 0, s, ta.fix_id, ta.fix_val, a.n, a.m, v0,
+                           v0 + cnt, sa.G, sa.ldg, sa.planeg, sa.Gt, sa.ldt, sa.planet);
+        KKM_TRY(hipGetLastError());
+      }
+      ProductArgs ph{}, pw{};
+      SlabJobs sums{};
+      int n_sums = 0;
       if (a.dh) {
         Side wv = wt;
         wv.p = at<E>(p.wt) + v0;
-        KKM_TRY(product({sa.G, sa.ldg, sa.planeg, p.n_pad}, wv, a.n, a.d, kv, kv0, p.bigh, p.sh, at<float>(p.slabs_h),
-                        v0 > 0, a.dh, a.lddh, alpha, ta.coef));
+        ph = product({sa.G, sa.ldg, sa.planeg, p.n_pad}, wv, a.n, a.d, kv, kv0, p.bigh, p.sh, at<float>(p.slabs_h),
+                     v0 > 0, a.dh, a.lddh, alpha, ta.coef);
+        if (p.sh && v0 + p.piece >= a.classes)
+          sums.j[n_sums++] = sum(at<float>(p.slabs_h), written(kv0, p.bigh, p.sh), a.n, a.d, alpha, ta.coef, a.dh,
+                                 a.lddh);
       }
       if (a.dw) {
         XT* dw = (XT*)a.dw + (int64_t)v0 * a.lddw;
-        KKM_TRY(product({sa.Gt, sa.ldt, sa.planet, p.piece}, ht, cnt, a.d, kn, kn, p.bigw, p.sw, at<float>(p.slabs_w), 0,
-                        dw, a.lddw, alpha, nullptr));
-        if (p.sw) KKM_TRY(sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha, nullptr, dw, a.lddw));
+        pw = product({sa.Gt, sa.ldt, sa.planet, p.piece}, ht, cnt, a.d, kn, kn, p.bigw, p.sw, at<float>(p.slabs_w), 0,
+                     dw, a.lddw, alpha, nullptr);
+        if (p.sw)
+          sums.j[n_sums++] = sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha, nullptr, dw, a.lddw);
+      }
+      if (a.dh && a.dw && p.bigh == p.bigw) {
+        KKM_TRY(multiply({{ph, pw}}, p.bigh));
+      } else {
+        if (a.dh) KKM_TRY(multiply({{ph, {}}}, p.bigh));
+        if (a.dw) KKM_TRY(multiply({{pw, {}}}, p.bigw));
+      }
+      if (n_sums) {
+        hipLaunchKernelGGL((slabs_kernel<XT>), dim3(sums.j[0].blocks + sums.j[1].blocks), dim3(256), 0, s, sums);
+        KKM_TRY(hipGetLastError());
       }
     }
-    if (a.dh && p.sh) KKM_TRY(sum(at<float>(p.slabs_h), written(kv0, p.bigh, p.sh), a.n, a.d, alpha, ta.coef, a.dh, a.lddh));
     return hipSuccess;
   }
 };

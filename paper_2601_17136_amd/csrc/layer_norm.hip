@@ -22,8 +22,14 @@ namespace kkm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kLines = 512;   // workgroups of the gradient, a line of sums each
-constexpr int kWgsFwd = 2048;
+
+// Workgroups, at most: a narrow row needs many for the bytes in flight, wider
+// ones gain from w and b loaded once, and in the gradient from fewer lines of
+// sums, one a workgroup.  Microseconds at 2048 / 1024 workgroups, forward: 40001
+// binary16 rows of 301 17 / 22; 8231 bfloat16 rows of 744 12 / 10; 3961 fp32 rows
+// of 7880 52 / 47.  At 1024 / 512, the gradient: 29 / 45, 20 / 17, 115 / 99.
+int wgs_fwd(int d) { return d <= 512 ? 2048 : 1024; }
+int wgs_grad(int d) { return d <= 512 ? 1024 : 512; }
 
 // v and w summed over the T threads of a row; T = 256: through red, one of two
 // halves used in turn, so that one barrier suffices.
@@ -207,28 +213,32 @@ __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(
   }
 }
 
-// dw and db from the lines: a workgroup takes 64 of the 2 d columns, its four
-// wavefronts a quarter of the lines each.
+// dw and db from the lines: a workgroup takes 64 of the 2 d columns, its
+// sixteen wavefronts every sixteenth line.
 template <typename WT>
-__global__ __launch_bounds__(kThreads) void norm_lines_kernel(const float* __restrict__ lines, int nlines, int d,
-                                                              WT* __restrict__ dw, WT* __restrict__ db) {
-  __shared__ float part[4][64];
+__global__ __launch_bounds__(1024) void norm_lines_kernel(const float* __restrict__ lines, int nlines, int d,
+                                                          WT* __restrict__ dw, WT* __restrict__ db) {
+  __shared__ float part[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.x * 64 + lane;
   float s = 0.f;
   if (c < 2 * (int64_t)d) {
     float a[8] = {};
     int l = wave;
-    for (; l + 28 < nlines; l += 32)
+    for (; l + 112 < nlines; l += 128)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) a[u] += lines[(int64_t)(l + 4 * u) * 2 * d + c];
-    for (; l < nlines; l += 4) a[0] += lines[(int64_t)l * 2 * d + c];
+      for (int u = 0; u < 8; ++u) a[u] += lines[(int64_t)(l + 16 * u) * 2 * d + c];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (l + 16 * u < nlines) a[u] += lines[(int64_t)(l + 16 * u) * 2 * d + c];
     s = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
   }
   part[wave][lane] = s;
   __syncthreads();
   if (wave || c >= 2 * (int64_t)d) return;
-  s = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) s += part[w][lane];
   if (c < d) {
     if (dw) dw[c] = (WT)s;
   } else if (db) {
@@ -365,12 +375,12 @@ hipError_t norm_typed(const NormArgs& a, hipStream_t s) {
   by_width<kVec<XT>>(a.d, [&](auto t_, auto nv_) {
     constexpr int T = decltype(t_)::value, NV = decltype(nv_)::value;
     if constexpr (T == 0) {
-      hipLaunchKernelGGL((layer_norm_wide_kernel<XT, WT>), dim3((unsigned)std::min<int64_t>(a.n, kWgsFwd)),
+      hipLaunchKernelGGL((layer_norm_wide_kernel<XT, WT>), dim3((unsigned)std::min<int64_t>(a.n, wgs_fwd(a.d))),
                          dim3(kThreads), 0, s, (const XT*)a.x, a.ldx, (const WT*)a.w, (const WT*)a.b, a.eps, a.n, a.d,
                          (XT*)a.y, a.ldy, a.mean, a.rstd);
     } else {
       const int64_t wgs = (a.n + kThreads / T - 1) / (kThreads / T);
-      hipLaunchKernelGGL((layer_norm_kernel<XT, WT, T, NV>), dim3((unsigned)std::min<int64_t>(wgs, kWgsFwd)),
+      hipLaunchKernelGGL((layer_norm_kernel<XT, WT, T, NV>), dim3((unsigned)std::min<int64_t>(wgs, wgs_fwd(a.d))),
                          dim3(kThreads), 0, s, (const XT*)a.x, a.ldx, (const WT*)a.w, (const WT*)a.b, a.eps, a.n, a.d,
                          (XT*)a.y, a.ldy, a.mean, a.rstd);
     }
@@ -381,7 +391,7 @@ hipError_t norm_typed(const NormArgs& a, hipStream_t s) {
 template <typename XT, typename WT>
 hipError_t norm_grad_typed(const NormArgs& a, float* lines, hipStream_t s) {
   const bool sums = a.dw || a.db;
-  int nlines = norm_lines(a.n);
+  int nlines = norm_lines(a.n, a.d);
   if (a.n > 0) by_width<kVec<XT>>(a.d, [&](auto t_, auto nv_) {
     constexpr int T = decltype(t_)::value, NV = decltype(nv_)::value;
     if constexpr (T == 0) {
@@ -391,7 +401,7 @@ hipError_t norm_grad_typed(const NormArgs& a, float* lines, hipStream_t s) {
                            dim3((unsigned)((a.d + kThreads - 1) / kThreads), (unsigned)nlines), dim3(kThreads), 0, s,
                            (const XT*)a.x, a.ldx, a.mean, a.rstd, (const XT*)a.dy, a.lddy, a.n, a.d, lines);
       if (a.dx)
-        hipLaunchKernelGGL((layer_norm_grad_wide_kernel<XT, WT>), dim3((unsigned)std::min<int64_t>(a.n, kWgsFwd)),
+        hipLaunchKernelGGL((layer_norm_grad_wide_kernel<XT, WT>), dim3((unsigned)std::min<int64_t>(a.n, wgs_fwd(a.d))),
                            dim3(kThreads), 0, s, (const XT*)a.x, a.ldx, (const WT*)a.w, a.mean, a.rstd,
                            (const XT*)a.dy, a.lddy, a.n, a.d, (XT*)a.dx, a.lddx);
     } else {
@@ -403,7 +413,7 @@ hipError_t norm_grad_typed(const NormArgs& a, float* lines, hipStream_t s) {
   });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !sums) return e;
-  hipLaunchKernelGGL((norm_lines_kernel<WT>), dim3((unsigned)((2 * (int64_t)a.d + 63) / 64)), dim3(kThreads), 0, s,
+  hipLaunchKernelGGL((norm_lines_kernel<WT>), dim3((unsigned)((2 * (int64_t)a.d + 63) / 64)), dim3(1024), 0, s,
                      lines, nlines, a.d, (WT*)a.dw, (WT*)a.db);
   return hipGetLastError();
 }
@@ -419,8 +429,8 @@ hipError_t by_types(const NormArgs& a, F&& f) {
 
 }  // namespace
 
-int norm_lines(int64_t n) { return (int)std::min<int64_t>(n, kLines); }
-size_t norm_scratch(int64_t n, int d) { return (size_t)norm_lines(n) * 2 * (size_t)d * sizeof(float); }
+int norm_lines(int64_t n, int d) { return (int)std::min<int64_t>(n, wgs_grad(d)); }
+size_t norm_scratch(int64_t n, int d) { return (size_t)norm_lines(n, d) * 2 * (size_t)d * sizeof(float); }
 
 hipError_t launch_layer_norm(const NormArgs& a, hipStream_t s) {
   if (a.n == 0) return hipSuccess;

@@ -30,7 +30,7 @@ struct NormArgs {
   void *dx, *dw, *db;  // each may be null
 };
 size_t norm_scratch(int64_t n, int d);
-int norm_lines(int64_t n);
+int norm_lines(int64_t n, int d);
 hipError_t launch_layer_norm(const NormArgs& a, hipStream_t s);
 hipError_t launch_layer_norm_grad(const NormArgs& a, float* lines, hipStream_t s);
 

@@ -52,11 +52,20 @@ __device__ inline void store_part(T* row, int i, int d, const float (&v)[kVec<T>
   }
 }
 
-// Elements i .. i + N - 1 of a vector of WT beside a vector of another type.
+// Elements i .. i + N - 1 of a vector of WT beside a vector of another type;
+// `none` past d and where there is no vector.
 template <int N, typename WT>
 __device__ inline void load_beside(const WT* w, int i, int d, float none, float (&v)[N]) {
+  typedef WT raw __attribute__((ext_vector_type(N)));
+  typedef raw any __attribute__((aligned(alignof(WT))));
+  if (w && i + N <= d) {
+    const raw r = *(const any*)(w + i);
 #pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = w && i + e < d ? (float)w[i + e] : none;
+    for (int e = 0; e < N; ++e) v[e] = (float)r[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = w && i + e < d ? (float)w[i + e] : none;
+  }
 }
 
 __device__ inline float wave_sum(float v) {
