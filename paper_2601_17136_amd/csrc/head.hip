@@ -628,21 +628,114 @@ constexpr int kPad = 256;  // G's rows and classes: whole tiles of any shape
 
 // (a tile's rows are reached by 32-bit offsets: kMaxStride)
 constexpr int64_t kMaxStride = (int64_t)1 << 21;
-constexpr int64_t kBigTiles = 192 * 65536 / (BigTile::BM * BigTile::BN);
 bool in_place(const HeadArgs& a, const void* p, int64_t ld) {
   return a.type != TYPE_F32 && a.d % 8 == 0 && ld % 8 == 0 && ld <= kMaxStride && (uintptr_t)p % 16 == 0;
 }
 
-// A product's slabs: enough workgroups for the chip where its tiles are few.
-int slab_count(int64_t tiles, int64_t chunks) {
-  const int64_t want = cdiv(256, tiles);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, chunks / 8, 32}));
+// What a launch of tiles takes, in microseconds, by which tiles and slabs are
+// chosen.  A workgroup's chunk of 64 and its epilogue, as measured on full
+// launches: 256 x 256 tiles 1.7 and 6 (scores 9, with G's stores 19), one on a
+// CU; 128 x 128 tiles 1.2 and 4 (4, 9), two on a CU.
+struct TileCost {
+  double chunk, end;
+  int slots;
+};
+TileCost tile_cost(bool big) { return big ? TileCost{1.7, 6, 256} : TileCost{1.2, 4, 512}; }
+int64_t tile_count(int64_t M, int64_t N, bool big) {
+  return big ? cdiv(M, BigTile::BM) * cdiv(N, BigTile::BN) : cdiv(M, SmallTile::BM) * cdiv(N, SmallTile::BN);
+}
+bool big_scores(int64_t classes, int64_t n, int64_t chunks, int planes, bool grad) {
+  double t[2];
+  for (int big = 0; big < 2; ++big) {
+    const TileCost c = tile_cost(big);
+    const double end = planes * (grad ? (big ? 19 : 9) : (big ? 9 : 4));
+    t[big] = cdiv(tile_count(classes, n, big), c.slots) * (chunks * c.chunk + (grad ? end : end / planes));
+  }
+  return t[1] < t[0];
+}
+
+// When the last of n0 workgroups of d0 and then n1 of d1 ends, dealt to `slots`
+// places in order as these fall free.
+double makespan(int64_t n0, double d0, int64_t n1, double d1, int slots) {
+  if (n0 + n1 > 6 * (int64_t)slots) return (n0 * d0 + n1 * d1) / slots + 0.5 * std::max(d0, d1);
+  struct Places {
+    double at;
+    int64_t count;
+  } q[32] = {{0, slots}};  // ordered by time
+  int len = 1;
+  const int64_t n[2] = {n0, n1};
+  const double d[2] = {d0, d1};
+  double last = 0;
+  for (int j = 0; j < 2; ++j)
+    for (int64_t left = n[j]; left > 0;) {
+      const int64_t take = std::min(left, q[0].count);
+      const double end = q[0].at + d[j];
+      last = std::max(last, end);
+      left -= take;
+      if (!(q[0].count -= take)) {
+        for (int i = 1; i < len; ++i) q[i - 1] = q[i];
+        --len;
+      }
+      int at = len;
+      while (at > 0 && q[at - 1].at > end) --at;
+      if (len == 32) return (n0 * d0 + n1 * d1) / slots + 0.5 * std::max(d0, d1);
+      for (int i = len; i > at; --i) q[i] = q[i - 1];
+      q[at] = {end, take};
+      ++len;
+    }
+  return last;
+}
+
+// The two products of a piece, dH (of n x d over the piece's classes) and dW:
+// tiles and slabs of each.  Tiles alike run in one launch, whose workgroups share
+// the CUs; slabs are written and read once.  A
+// gradient has the same bits whether or not the other one is asked for.
+struct ProductChoice {
+  bool big[2];
+  int slabs[2];
+};
+ProductChoice choose_products(const int64_t (&M)[2], int64_t N, const int64_t (&chunks)[2]) {
+  static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  ProductChoice best{};
+  double least = 1e300;
+  struct Side1 {
+    int64_t wgs;
+    double one, extra;
+    bool big;
+    int slabs;
+  };
+  Side1 opt[2][20];
+  int num[2] = {0, 0};
+  for (int j = 0; j < 2; ++j)
+    for (int big = 0; big < 2; ++big)
+      for (int s : counts) {
+        if (s > 1 && chunks[j] / s < 4) break;
+        const TileCost c = tile_cost(big);
+        const int64_t wgs = tile_count(M[j], N, big) * s;
+        if (s > 1 && wgs > 4 * c.slots) break;
+        const double one = cdiv(chunks[j], s) * c.chunk + c.end;
+        const double extra = s > 1 ? s * (double)M[j] * N * 8 / 4.5e6 : 0;
+        opt[j][num[j]++] = {wgs, one, extra, big != 0, s};
+      }
+  for (int i = 0; i < num[0]; ++i)
+    for (int k = 0; k < num[1]; ++k) {
+      const Side1 &x = opt[0][i], &y = opt[1][k];
+      const int sx = tile_cost(x.big).slots, sy = tile_cost(y.big).slots;
+      double t = x.big == y.big ? makespan(x.wgs, x.one, y.wgs, y.one, sx)
+                                : makespan(x.wgs, x.one, 0, 0, sx) + makespan(y.wgs, y.one, 0, 0, sy) + 5;
+      t += x.extra + y.extra + (x.slabs > 1 || y.slabs > 1 ? 5 : 0);
+      if (t < least) {
+        least = t;
+        best = {{x.big, y.big}, {x.slabs, y.slabs}};
+      }
+    }
+  return best;
 }
 
 struct HeadPlan {
   int planes, nseg, kp;
   int64_t n_pad, v_pad;
-  bool big;             // scores in BigTile
+  bool big, bigg;       // scores in BigTile: the forward pass, and for G
   int ntiles;
   int piece;            // classes of a piece (a multiple of kPad)
   int sh, sw;           // slabs of dH and dW (0: none)
@@ -658,7 +751,7 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
   p.kp = (int)up(a.d, kChunkK);
   p.n_pad = up(a.n, kPad);
   p.v_pad = up(a.classes, kPad);
-  p.big = cdiv(a.classes, BigTile::BM) * cdiv(a.n, BigTile::BN) >= kBigTiles;
+  p.big = big_scores(a.classes, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, false);
   p.ntiles = (int)cdiv(a.classes, p.big ? BigTile::BM : SmallTile::BM);
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -682,17 +775,14 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
     p.fix_val = take((size_t)a.n * a.m * 4);
     p.G = take((size_t)p.planes * p.n_pad * p.piece * 2);
     p.Gt = take((size_t)p.planes * p.n_pad * p.piece * 2);
-    const int64_t pieces = cdiv(a.classes, p.piece);
-    auto shape = [&](int64_t M, int64_t N, int64_t chunks, bool& big) {
-      big = cdiv(M, BigTile::BM) * cdiv(N, BigTile::BN) >= kBigTiles;
-      const int64_t tiles = big ? cdiv(M, BigTile::BM) * cdiv(N, BigTile::BN)
-                                : cdiv(M, SmallTile::BM) * cdiv(N, SmallTile::BN);
-      return slab_count(tiles, chunks);
-    };
-    p.sh = shape(a.n, a.d, p.nseg * cdiv(std::min<int64_t>(p.piece, a.classes), kChunkK), p.bigh);
-    p.sw = shape(std::min<int64_t>(p.piece, a.classes), a.d, p.nseg * cdiv(a.n, kChunkK), p.bigw);
-    if (p.sh == 1 && pieces == 1) p.sh = 0;
-    if (p.sw == 1) p.sw = 0;
+    const int64_t pieces = cdiv(a.classes, p.piece), of_piece = std::min<int64_t>(p.piece, a.classes);
+    p.bigg = big_scores(of_piece, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, true);
+    const ProductChoice c = choose_products({a.n, of_piece}, a.d, {p.nseg * cdiv(of_piece, kChunkK),
+                                                                   p.nseg * cdiv(a.n, kChunkK)});
+    p.bigh = c.big[0];
+    p.bigw = c.big[1];
+    p.sh = c.slabs[0] > 1 || pieces > 1 ? c.slabs[0] : 0;
+    p.sw = c.slabs[1] > 1 ? c.slabs[1] : 0;
     p.slabs_h = take((size_t)p.sh * a.n * a.d * 4);
     p.slabs_w = take((size_t)p.sw * std::min<int64_t>(p.piece, a.classes) * a.d * 4);
   }
@@ -730,11 +820,12 @@ struct Head {
 
   template <bool GRAD>
   hipError_t scores(ScoreArgs<E> sa, int64_t classes) const {
-    sa.nkc = p.kp / (p.big ? BigTile::BK : SmallTile::BK);
-    sa.mt = (int)cdiv(classes, p.big ? BigTile::BM : SmallTile::BM);
-    sa.nt = (int)cdiv(a.n, p.big ? BigTile::BN : SmallTile::BN);
+    const bool big = GRAD ? p.bigg : p.big;
+    sa.nkc = p.kp / chunk_of(big);
+    sa.mt = (int)cdiv(classes, big ? BigTile::BM : SmallTile::BM);
+    sa.nt = (int)cdiv(a.n, big ? BigTile::BN : SmallTile::BN);
     const dim3 grid((unsigned)((int64_t)sa.mt * sa.nt));
-    if (p.big)
+    if (big)
       hipLaunchKernelGGL((scores_kernel<E, BigTile, P, GRAD>), grid, dim3(BigTile::threads), 0, s, sa);
     else
       hipLaunchKernelGGL((scores_kernel<E, SmallTile, P, GRAD>), grid, dim3(SmallTile::threads), 0, s, sa);
