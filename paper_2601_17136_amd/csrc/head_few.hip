@@ -56,7 +56,8 @@ struct FewArgs {
 };
 
 // z in base 2 of CT x NT blocks of 16 classes by 16 rows of h into zs[row][class],
-// the workgroup's four wavefronts taking every fourth step of the features.
+// the workgroup's four wavefronts taking every fourth run of UN steps of the
+// features, so that one reads 256 neighbouring bytes of a row at a time.
 // -inf where a class is left out or past the last.
 template <typename XT, int CT, int NT>
 __device__ inline void scores_block(const FewArgs& a, int64_t v0, int64_t t0, float (*zs)[NT * 16][CT * 16 + 1]) {
@@ -78,7 +79,7 @@ __device__ inline void scores_block(const FewArgs& a, int64_t v0, int64_t t0, fl
     raw_vec<XT> fa[UN][CT], fb[UN][NT];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      const int k = (s + 4 * u) * KS + g * VEC;
+      const int k = (s + u) * KS + g * VEC;
 #pragma unroll
       for (int i = 0; i < CT; ++i)
         fa[u][i] = whole ? *(const any_vec<XT>*)(pa[i] + k) : load_raw(pa[i], k, a.d);
@@ -94,8 +95,8 @@ __device__ inline void scores_block(const FewArgs& a, int64_t v0, int64_t t0, fl
         for (int j = 0; j < NT; ++j) acc[i][j] = mfma_few(fa[u][i], fb[u][j], acc[i][j]);
   };
   const int full = a.d / KS;
-  int s = wave;
-  for (; s + 4 * (UN - 1) < full; s += 4 * UN) steps(s, std::true_type{});
+  int s = wave * UN;
+  for (; s + UN <= full; s += 4 * UN) steps(s, std::true_type{});
   for (; s * KS < a.d; s += 4 * UN) steps(s, std::false_type{});
 #pragma unroll
   for (int i = 0; i < CT; ++i)
@@ -140,11 +141,14 @@ __device__ inline float pair_logit(const FewArgs& a, int64_t at, int& id, bool& 
 }
 
 // Few classes: 32 rows of h by all classes; eight lanes finish a row, lane p
-// owning the classes c % 8 = p, so that no two add to one target.
+// owning the classes c % 8 = p, so that no two add to one target.  With dh the
+// workgroup goes on to its rows of dH = G W: the matrix instructions have the
+// features as rows, as in rows_few_kernel, and the wavefronts take every fourth
+// 16 kVec features.
 template <typename XT, int CT>
-__global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a) {
+__global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a, XT* __restrict__ dh, int64_t lddh) {
   constexpr int NT = 2, S = CT * 16;
-  __shared__ float zs[4][NT * 16][S + 1];
+  __shared__ __attribute__((aligned(16))) float zs[4][NT * 16][S + 1];
   const int64_t t0 = (int64_t)blockIdx.x * (NT * 16);
   const int row = threadIdx.x >> 3, p = threadIdx.x & 7;
   const int64_t i = t0 + row;
@@ -198,21 +202,79 @@ __global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a) {
     }
   }
   loss = near_sum<8>(loss);
-  if (!here) return;
-  if (p == 0) {
+  if (here && p == 0) {
     a.loss[i] = bad ? __builtin_nanf("") : some ? loss : 0.f;
     a.lse[i] = lse2 * kLn2;
   }
   if (!a.C) return;
   float cf = dl * a.scale;
-  if (!some || lse2 == -INFINITY) cf = 0.f;
-  if (bad) cf = __builtin_nanf("");
-  if (p == 0) a.coef[i] = cf;
+  if (!here || !some || lse2 == -INFINITY) cf = 0.f;
+  if (here && bad) cf = __builtin_nanf("");
+  if (here && p == 0) a.coef[i] = cf;
   const float l2 = safe(lse2);
+  float* gs = &zs[2][0][0] + row * (S + 4);  // G once more, for dH: rows of 16-byte words
 #pragma unroll
-  for (int c = p; c < S; c += 8)
-    a.C[i * S + c] =
-        cf == 0.f || z[c] == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z[c] - l2) - q[c]);
+  for (int c = p; c < S; c += 8) {
+    const float g = cf == 0.f || z[c] == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z[c] - l2) - q[c]);
+    if (here) a.C[i * S + c] = g;
+    gs[c] = g;
+  }
+  if (!dh) return;
+  __syncthreads();
+  constexpr int VEC = kVec<XT>, KB = CT;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4, place = (l16 >> 2) + 4 * (l16 & 3);
+  floatx4 gr[KB][NT];
+  bool part[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    float any = 0.f;  // (a row of weight 0 has no G, and dH = 0 whatever stands in w)
+#pragma unroll
+    for (int k0 = 0; k0 < KB; ++k0) {
+      gr[k0][t] = *(const floatx4*)(&zs[2][0][0] + (t * 16 + l16) * (S + 4) + 16 * k0 + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any = gr[k0][t][e] != 0.f ? 1.f : any;
+    }
+    any += __shfl_xor(any, 16, 64);
+    any += __shfl_xor(any, 32, 64);
+    part[t] = any != 0.f;
+  }
+  for (int c0 = wave * (16 * VEC); c0 < a.d; c0 += 64 * VEC) {
+    floatx4 acc[VEC][NT];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k0 = 0; k0 < KB; ++k0) {
+      raw_vec<XT> b[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int k = 16 * k0 + 4 * g + e;
+        const bool use = k < a.classes && !(a.offset && a.offset[k] == -INFINITY);
+        b[e] = load_raw((const XT*)a.w + (int64_t)(use ? k : 0) * a.ldw, c0 + place * VEC, use ? a.d : 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[e][j], gr[k0][t][e], acc[j][t], 0, 0, 0);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int64_t r = t0 + t * 16 + l16;
+      if (r >= a.n) continue;
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        float v[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[j] = part[t] ? acc[j][t][q4] : 0.f;
+        store_part(dh + r * lddh, c0 + VEC * (g + 4 * q4), a.d, v);
+      }
+    }
+  }
 }
 
 // Few rows: CT x 16 classes by all rows of h; the rows' (largest, sum) of the
@@ -399,15 +461,15 @@ __global__ __launch_bounds__(256) void rows_few_kernel(const float* __restrict__
 
 // out (M x d) = C^T X, rows of X (R x d) that take no part left out and rows of
 // out that take none 0: S columns of C a workgroup, and where blockIdx.y splits
-// the rows of X, their sums into that slab.  A step is 4 UN rows: a lane loads kVec features of row
-// lane / 16 in each of CH blocks of 16 kVec features, and S / 16 of the row's
+// the rows of X, their sums into that slab.  A step is 4 UN rows: a lane loads VEC features of row
+// lane / 16 in each of CH blocks of 16 VEC features, and S / 16 of the row's
 // entries of C.  The four wavefronts take every fourth step and join in LDS.
 template <typename XT, int S>
 struct ColsShape {
-  static constexpr int VEC = kVec<XT>, CT = S / 16;
-  static constexpr int CH = 16 / (VEC * CT) > 0 ? 16 / (VEC * CT) : 1;  // 64 sums a lane (128: 16 bits, S = 64)
+  static constexpr int CT = S / 16, VEC = kVec<XT> * CT > 16 ? 16 / CT : kVec<XT>;  // features of a load
+  static constexpr int CH = 16 / (VEC * CT);                                        // 64 sums a lane
   static constexpr int UN = CH >= 4 ? 1 : CH == 2 ? 2 : 4;
-  static constexpr int width = CH * 16 * VEC;
+  static constexpr int width = CH * 16 * VEC;  // 256, 128 or 64
 };
 template <typename XT, int S>
 __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__ C, int64_t ldc,
@@ -432,7 +494,7 @@ __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__
     for (int j = 0; j < VEC; ++j)
 #pragma unroll
       for (int t = 0; t < CT; ++t) acc[h][j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  raw_vec<XT> x[UN][CH], xn[UN][CH];  // this step's, and the next one's on their way
+  raw_n<VEC, XT> x[UN][CH], xn[UN][CH];  // this step's, and the next one's on their way
   float c[UN][CT], cn[UN][CT];
   bool un[UN];
   const bool inside = c0 + Sh::width <= d;
@@ -446,9 +508,9 @@ __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__
       for (int h = 0; h < CH; ++h) {
         const int col = c0 + (h * 16 + l16) * VEC;
         if (inside) {
-          xn[u][h] = *(const any_vec<XT>*)(xr + col);
+          xn[u][h] = *(const any_n<VEC, XT>*)(xr + col);
         } else {
-          xn[u][h] = load_raw(xr, col, d);
+          xn[u][h] = load_n<VEC>(xr, col, d);
         }
       }
       const cvec cv = *(const cvec*)(C + (row < hi ? row : lo) * ldc + CT * l16);
@@ -746,6 +808,7 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct FewPlan {
   bool classes;  // few classes, or few rows
+  bool joined;   // few classes: dH in the scores' launch
   int S;         // the short side, padded to 16, 32 or 64
   int64_t R;     // the long side
   int ct;        // few rows: class blocks of a tile
@@ -758,6 +821,9 @@ struct FewPlan {
 FewPlan few_plan(const HeadArgs& a, bool grad) {
   FewPlan p{};
   p.classes = a.classes <= kFew;
+  // (many rows of 16 bits: a launch of its own fits more wavefronts on a CU; 20000
+  // bfloat16 rows of 784, 64 classes 139 / 132 us, where 200 fp32 rows of 64 take 24 / 27)
+  p.joined = p.classes && (a.type == TYPE_F32 || a.n <= 4096);
   const int64_t s = p.classes ? a.classes : a.n;
   p.S = s <= 16 ? 16 : s <= 32 ? 32 : 64;
   p.R = p.classes ? a.n : a.classes;
@@ -780,8 +846,7 @@ FewPlan few_plan(const HeadArgs& a, bool grad) {
       p.fix_val = take((size_t)a.n * a.m * 4);
     }
     // rows of a slab: enough workgroups for the chip, no more slabs than their sum is worth
-    const int vec = 16 / (int)elem_bytes(a.type), ch = std::max(1, 256 / (vec * p.S));  // ColsShape::width
-    const int64_t chunks = cdiv(a.d, ch * 16 * vec);
+    const int64_t chunks = cdiv(a.d, p.S == 16 ? 256 : p.S == 32 ? 128 : 64);  // ColsShape::width
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(512, chunks), cdiv(p.R, 64)));
     p.per = up(cdiv(p.R, p.splits), 64);
     p.splits = (int)cdiv(p.R, p.per);
@@ -831,7 +896,7 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   if (p.classes) {
     by_short(p.S, [&](auto S) {
       hipLaunchKernelGGL((scores_few_classes_kernel<XT, decltype(S)::value / 16>), dim3((unsigned)cdiv(a.n, 32)),
-                         dim3(256), 0, s, f);
+                         dim3(256), 0, s, f, (XT*)(p.joined && grad ? a.dh : nullptr), a.lddh);
     });
     KKM_TRY(hipGetLastError());
   } else {
@@ -871,9 +936,9 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
       cols<XT, S>(p.classes ? f.coef : a.offset, p.classes ? 0.f : none, f.C, p.S, p.classes ? a.h : a.w,
                   p.classes ? a.ldh : a.ldw, p.R, a.d, p.splits, p.per, (float*)(ws + p.slabs), rows_b,
                   p.classes ? nullptr : f.coef, short_out, p.classes ? a.lddw : a.lddh, s);
-    if (long_out) {
+    if (long_out && !p.joined) {
       const int64_t cols = cdiv(a.d, 64 * VEC);
-      const dim3 grid((unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max<int64_t>(1, 1536 / cols)), (unsigned)cols);
+      const dim3 grid((unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max<int64_t>(1, (S == 64 ? 512 : 1536) / cols)), (unsigned)cols);
       hipLaunchKernelGGL((rows_few_kernel<XT, S>), grid, dim3(256), 0, s, f.C, (const XT*)(p.classes ? a.w : a.h),
                          p.classes ? a.ldw : a.ldh, rows_b, p.classes ? a.offset : f.coef, p.classes ? none : 0.f,
                          p.R, a.d, p.classes ? f.coef : nullptr, (XT*)long_out, p.classes ? a.lddh : a.lddw);
@@ -901,11 +966,11 @@ DirectPlan direct_plan(const HeadArgs& a, bool grad) {
   p.C = take((size_t)a.n * p.ldz * 4);
   if (grad) {
     p.coef = take((size_t)a.n * 4);
-    const int64_t chunks = cdiv(a.d, 256 / (int)elem_bytes(a.type));
+    const int64_t chunks = cdiv(a.d, 64);
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(512, chunks * (p.ldz / 64)), cdiv(a.n, 128)));
     p.per = up(cdiv(a.n, p.splits), 64);
     p.splits = (int)cdiv(a.n, p.per);
-    p.splitsh = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(256, chunks * cdiv(a.n, 32)), p.ldz / 256));
+    p.splitsh = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(256, cdiv(a.d, 256 / (int)elem_bytes(a.type)) * cdiv(a.n, 32)), p.ldz / 256));
     p.perh = (int)up(cdiv(a.classes, p.splitsh), 64);
     p.splitsh = (int)cdiv(a.classes, p.perh);
     const size_t w = p.splits > 1 ? (size_t)p.splits * a.classes * a.d : 0,

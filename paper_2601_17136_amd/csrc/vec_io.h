@@ -17,20 +17,29 @@ using raw_vec = T __attribute__((ext_vector_type(kVec<T>)));
 template <typename T>
 using any_vec = raw_vec<T> __attribute__((aligned(alignof(T))));
 
+// N elements from element i of a row of d, zero from d on.
+template <int N, typename T>
+using raw_n = T __attribute__((ext_vector_type(N)));
+template <int N, typename T>
+using any_n = raw_n<N, T> __attribute__((aligned(alignof(T))));
+template <int N, typename T>
+__device__ inline raw_n<N, T> load_n(const T* row, int i, int d) {
+  if (i + N <= d) return *(const any_n<N, T>*)(row + i);
+  raw_n<N, T> r;
+#pragma unroll
+  for (int e = 0; e < N; ++e) r[e] = i + e < d ? row[i + e] : (T)0.f;
+  return r;
+}
+
 template <typename T>
 __device__ inline void to_floats(const raw_vec<T>& r, float (&v)[kVec<T>]) {
 #pragma unroll
   for (int e = 0; e < kVec<T>; ++e) v[e] = (float)r[e];
 }
 
-// Elements i .. i + kVec - 1 of a row of d, zero from d on.
 template <typename T>
 __device__ inline raw_vec<T> load_raw(const T* row, int i, int d) {
-  if (i + kVec<T> <= d) return *(const any_vec<T>*)(row + i);
-  raw_vec<T> r;
-#pragma unroll
-  for (int e = 0; e < kVec<T>; ++e) r[e] = i + e < d ? row[i + e] : (T)0.f;
-  return r;
+  return load_n<kVec<T>>(row, i, d);
 }
 template <typename T>
 __device__ inline void load_part(const T* row, int i, int d, float (&v)[kVec<T>]) {

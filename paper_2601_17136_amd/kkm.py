@@ -471,12 +471,17 @@ def kkm_get_info(ctx) -> dict:
 
 # ------------------------------------------------------------------ a model that learns from a clustering
 
+_TYPE_CODES = {}
+
+
 def _type_code(dtype, name):
-    import torch
-    codes = {torch.float32: KKM_F32, torch.float16: KKM_F16, torch.bfloat16: KKM_BF16}
-    if dtype not in codes:
+    if not _TYPE_CODES:
+        import torch
+        _TYPE_CODES.update({torch.float32: KKM_F32, torch.float16: KKM_F16, torch.bfloat16: KKM_BF16})
+    code = _TYPE_CODES.get(dtype)
+    if code is None:
         raise TypeError(f"{name} must have dtype float32, float16 or bfloat16, got {dtype}")
-    return codes[dtype]
+    return code
 
 
 def _rows(t, name, dtype=None, shape=None):
@@ -486,16 +491,19 @@ def _rows(t, name, dtype=None, shape=None):
         raise TypeError(f"{name} must be a device tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if t.dim() != 2:
-        raise ValueError(f"{name} must be a matrix, got {t.dim()} dimensions")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    n, d = t.shape
-    if d > 1 and t.stride(1) != 1:
+    size = t.shape
+    if len(size) != 2:
+        raise ValueError(f"{name} must be a matrix, got {len(size)} dimensions")
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(size)}")
+    n, d = size
+    ld, step = t.stride()
+    if d > 1 and step != 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    ld = t.stride(0) if n > 1 else max(d, t.stride(0))
     if ld < d:
-        raise ValueError(f"{name}'s rows overlap (stride {ld}, width {d})")
+        if n > 1:
+            raise ValueError(f"{name}'s rows overlap (stride {ld}, width {d})")
+        ld = d
     return t.data_ptr(), ld
 
 
@@ -525,9 +533,7 @@ _HERE = contextlib.nullcontext()
 def _ordered(ctx, *tensors):
     """The context's stream as the place of the call's work."""
     import torch
-    h = _vp()
-    _check(lib().kkm_get_stream(ctx, ctypes.byref(h)), ctx)
-    handle = h.value or 0
+    handle = kkm_get_stream(ctx)
     if handle == torch._C._cuda_getCurrentRawStream(tensors[0].device.index):
         return _HERE
     return _Elsewhere(handle, tensors)
