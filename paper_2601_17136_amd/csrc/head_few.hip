@@ -400,16 +400,37 @@ __device__ inline bool takes_part(const float* weight, float none, int64_t row) 
 // neighbouring features of a row of out, the four lanes of a row 64 bytes at a
 // time.  A wavefront keeps its 16 kVec features of B in registers and goes over
 // blocks of 16 rows a grid apart, the next one's C on its way.
+struct RowsJob {
+  const float* C;
+  int64_t ldc;  // rows_direct only: C's width
+  const void* B;
+  int64_t ldb;
+  int rows_b;
+  const float* weight_b;  // rows of B that take no part have `none_b` here
+  float none_b;
+  int64_t R;
+  int d;
+  const float* weight_r;  // rows of out that take no part have 0 here
+  void* out;
+  int64_t ldo;
+  int per;       // rows_direct: classes of a slab
+  float* slabs;  // rows_direct: where out is null
+  unsigned gx, gy;  // the workgroups
+};
+
 template <typename XT, int S>
-__global__ __launch_bounds__(256) void rows_few_kernel(const float* __restrict__ C, const XT* __restrict__ B,
-                                                       int64_t ldb, int rows_b, const float* __restrict__ weight_b,
-                                                       float none_b, int64_t R, int d,
-                                                       const float* __restrict__ weight_r, XT* __restrict__ out,
-                                                       int64_t ldo) {
+__device__ inline void rows_few(const RowsJob& q, unsigned bx, unsigned by) {
+  const float* __restrict__ C = q.C;
+  const XT* __restrict__ B = (const XT*)q.B;
+  XT* __restrict__ out = (XT*)q.out;
+  const float *weight_b = q.weight_b, *weight_r = q.weight_r;
+  const float none_b = q.none_b;
+  const int64_t ldb = q.ldb, R = q.R, ldo = q.ldo;
+  const int rows_b = q.rows_b, d = q.d;
   constexpr int VEC = kVec<XT>, KB = S / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int c0 = (blockIdx.y * 4 + wave) * (16 * VEC);
+  const int c0 = (by * 4 + wave) * (16 * VEC);
   if (c0 >= d) return;
   const int place = (l16 >> 2) + 4 * (l16 & 3);  // matrix row 4 g + r holds the features from kVec (g + 4 r)
   raw_vec<XT> b[KB][4];
@@ -429,8 +450,8 @@ __global__ __launch_bounds__(256) void rows_few_kernel(const float* __restrict__
     for (int k0 = 0; k0 < KB; ++k0) cn[k0] = *(const floatx4*)(C + row * S + 16 * k0 + 4 * g);
     if (weight_r) wn = weight_r[row];
   };
-  const int64_t step = (int64_t)gridDim.x * 16;
-  int64_t r0 = (int64_t)blockIdx.x * 16;
+  const int64_t step = (int64_t)q.gx * 16;
+  int64_t r0 = (int64_t)bx * 16;
   fetch(r0);
   for (; r0 < R; r0 += step) {
 #pragma unroll
@@ -460,8 +481,8 @@ __global__ __launch_bounds__(256) void rows_few_kernel(const float* __restrict__
 }
 
 // out (M x d) = C^T X, rows of X (R x d) that take no part left out and rows of
-// out that take none 0: S columns of C a workgroup, and where blockIdx.y splits
-// the rows of X, their sums into that slab.  A step is 4 UN rows: a lane loads VEC features of row
+// out that take none 0: S columns of C a workgroup, and where by splits the rows
+// of X, their sums into that slab.  A step is 4 UN rows: a lane loads VEC features of row
 // lane / 16 in each of CH blocks of 16 VEC features, and S / 16 of the row's
 // entries of C.  The four wavefronts take every fourth step and join in LDS.
 template <typename XT, int S>
@@ -469,24 +490,42 @@ struct ColsShape {
   static constexpr int CT = S / 16, VEC = kVec<XT> * CT > 16 ? 16 / CT : kVec<XT>;  // features of a load
   static constexpr int CH = 16 / (VEC * CT);                                        // 64 sums a lane
   static constexpr int UN = CH >= 4 ? 1 : CH == 2 ? 2 : 4;
+  static constexpr int lds = S * (16 * VEC + 1);  // floats
   static constexpr int width = CH * 16 * VEC;  // 256, 128 or 64
 };
+struct ColsJob {
+  const float* C;
+  int64_t ldc;
+  const void* X;
+  int64_t ldx, R;
+  int d;
+  const float* weight;  // rows of X that take no part have `none` here
+  float none;
+  int64_t per;
+  float* slabs;
+  int M;
+  const float* weight_m;  // rows of out that take no part have 0 here
+  void* out;              // null: slabs
+  int64_t ldo;
+  unsigned gx, gy, gz;  // the workgroups: features, splits, columns of C
+};
+
 template <typename XT, int S>
-__global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__ C, int64_t ldc,
-                                                       const XT* __restrict__ X, int64_t ldx, int64_t R, int d,
-                                                       const float* __restrict__ weight, float none, int64_t per,
-                                                       float* __restrict__ slabs, int M,
-                                                       const float* __restrict__ weight_m, XT* __restrict__ out,
-                                                       int64_t ldo) {
+__device__ inline void cols_few(const ColsJob& q, unsigned bx, unsigned by, unsigned bz, float* lds) {
   using Sh = ColsShape<XT, S>;
   constexpr int VEC = Sh::VEC, CT = Sh::CT, CH = Sh::CH, UN = Sh::UN;
   typedef float cvec __attribute__((ext_vector_type(CT)));
-  __shared__ float red[S][16 * VEC + 1];
+  float (*red)[16 * VEC + 1] = (float (*)[16 * VEC + 1])lds;  // [S]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * Sh::width, s0 = blockIdx.z * S;
-  C += s0;
-  const int64_t lo = (int64_t)blockIdx.y * per, hi = min(lo + per, R);
+  const int c0 = bx * Sh::width, s0 = bz * S, M = q.M, d = q.d;
+  const float* __restrict__ C = q.C + s0;
+  const XT* __restrict__ X = (const XT*)q.X;
+  XT* __restrict__ out = (XT*)q.out;
+  const float *weight = q.weight, *weight_m = q.weight_m;
+  const float none = q.none;
+  const int64_t ldc = q.ldc, ldx = q.ldx, ldo = q.ldo;
+  const int64_t lo = (int64_t)by * q.per, hi = min(lo + q.per, q.R);
   floatx4 acc[CH][VEC][CT];
 #pragma unroll
   for (int h = 0; h < CH; ++h)
@@ -544,7 +583,7 @@ __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__
             acc[h][j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(c[u][t], (float)x[u][h][j], acc[h][j][t], 0, 0, 0);
   }
   // entry r of block (j, t): row CT (4 g + r) + t of the slab, feature VEC l16 + j
-  float* slab = slabs + ((int64_t)blockIdx.y * M + s0) * d;
+  float* slab = q.slabs + ((int64_t)by * M + s0) * d;
 #pragma unroll
   for (int h = 0; h < CH; ++h) {
     for (int o = 0; o < 4; ++o) {
@@ -574,23 +613,37 @@ __global__ __launch_bounds__(256) void cols_few_kernel(const float* __restrict__
 }
 
 // out (M x d) from the slabs, in order; rows of weight 0 are 0.
+struct SlabsJob {
+  const float* slabs;
+  int count, M, d;
+  const float* weight;
+  void* out;
+  int64_t ldo;
+  unsigned blocks;
+};
+struct SlabsJobs {
+  SlabsJob j[2];
+};
 template <typename OT>
-__global__ __launch_bounds__(256) void slabs_few_kernel(const float* __restrict__ slabs, int count, int M, int d, const float* __restrict__ weight,
-                                                        OT* __restrict__ out, int64_t ldo) {
-  const int64_t x = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+__global__ __launch_bounds__(256) void slabs_few_kernel(SlabsJobs jobs) {
+  const bool second = blockIdx.x >= jobs.j[0].blocks;
+  const SlabsJob& q = jobs.j[second];
+  const int d = q.d, count = q.count;
+  const int64_t x = (int64_t)(blockIdx.x - (second ? jobs.j[0].blocks : 0u)) * 64 + (threadIdx.x & 63);
   const int wave = threadIdx.x >> 6;
+  const int64_t entries = (int64_t)q.M * d;
   __shared__ float red[4][64];
   float s = 0.f;
-  if (x < (int64_t)M * d)
+  if (x < entries)
 #pragma unroll 8
-    for (int k = wave; k < count; k += 4) s += slabs[(int64_t)k * M * d + x];
+    for (int k = wave; k < count; k += 4) s += q.slabs[(int64_t)k * entries + x];
   red[wave][threadIdx.x & 63] = s;
   __syncthreads();
-  if (wave || x >= (int64_t)M * d) return;
+  if (wave || x >= entries) return;
   const int lane = threadIdx.x;
   s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
   const int64_t row = x / d;
-  out[row * ldo + (x - row * d)] = (OT)(takes_part(weight, 0.f, row) ? s : 0.f);
+  ((OT*)q.out)[row * q.ldo + (x - row * d)] = (OT)(takes_part(q.weight, 0.f, row) ? s : 0.f);
 }
 
 // ------------------------------------------------------------------ both sides longer, little work
@@ -722,20 +775,24 @@ __global__ __launch_bounds__(256) void row_direct_kernel(FewArgs a, int64_t ldz,
 
 // out (R x d) = C (R x K) B (K x d) for any K (C padded with zeros to 16): as
 // rows_few_kernel, 32 rows by 16 kVec features a workgroup, whose wavefronts
-// take every fourth 16 of K and join in LDS.  blockIdx.z splits K into slabs.
+// take every fourth 16 of K and join in LDS.  bz splits K into slabs.
 template <typename XT>
-__global__ __launch_bounds__(256) void rows_direct_kernel(const float* __restrict__ C, int64_t ldc,
-                                                          const XT* __restrict__ B, int64_t ldb, int K,
-                                                          const float* __restrict__ weight_b, float none_b, int64_t R,
-                                                          int d, const float* __restrict__ weight_r, int per,
-                                                          float* __restrict__ slabs, XT* __restrict__ out,
-                                                          int64_t ldo) {
+constexpr int kDirectLds = 4 * 32 * (16 * kVec<XT> + 4);  // floats
+template <typename XT>
+__device__ inline void rows_direct(const RowsJob& q, unsigned bx, unsigned by, unsigned bz, float* lds) {
   constexpr int VEC = kVec<XT>, W = 16 * VEC;
-  __shared__ float red[4][32][W + 4];
+  float (*red)[32][W + 4] = (float (*)[32][W + 4])lds;  // [4]
+  const float* __restrict__ C = q.C;
+  const XT* __restrict__ B = (const XT*)q.B;
+  XT* __restrict__ out = (XT*)q.out;
+  const float *weight_b = q.weight_b, *weight_r = q.weight_r;
+  const float none_b = q.none_b;
+  const int64_t ldc = q.ldc, ldb = q.ldb, R = q.R, ldo = q.ldo;
+  const int K = q.rows_b, d = q.d, per = q.per;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int c0 = blockIdx.x * W, place = (l16 >> 2) + 4 * (l16 & 3);
-  const int64_t r0 = (int64_t)blockIdx.y * 32;
+  const int c0 = bx * W, place = (l16 >> 2) + 4 * (l16 & 3);
+  const int64_t r0 = (int64_t)by * 32;
   const float* cr[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) cr[t] = C + min(r0 + t * 16 + l16, R - 1) * ldc + 4 * g;
@@ -756,8 +813,8 @@ __global__ __launch_bounds__(256) void rows_direct_kernel(const float* __restric
       bn[e] = load_raw(B + (int64_t)(use ? k : 0) * ldb, c0 + place * VEC, use ? d : 0);
     }
   };
-  const int end = min(K, ((int)blockIdx.z + 1) * per);
-  int k0 = blockIdx.z * per + wave * 16;
+  const int end = min(K, ((int)bz + 1) * per);
+  int k0 = bz * per + wave * 16;
   if (k0 < end) fetch(k0);
   for (; k0 < end; k0 += 64) {
 #pragma unroll
@@ -793,11 +850,33 @@ __global__ __launch_bounds__(256) void rows_direct_kernel(const float* __restric
     if (out) {
       store_part(out + row * ldo, c0 + cc, d, v);
     } else {
-      float* p = slabs + ((int64_t)blockIdx.z * R + row) * d + c0 + cc;
+      float* p = q.slabs + ((int64_t)bz * R + row) * d + c0 + cc;
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
         if (c0 + cc + e < d) p[e] = v[e];
     }
+  }
+}
+
+// Both gradients in one launch, the sums' workgroups first (what they read may
+// still be in the last-level cache).  ROWS: rows_few, rows_direct or neither.
+enum { ROWS_NONE, ROWS_FEW, ROWS_DIRECT };
+template <typename XT, int S, int ROWS>
+__global__ __launch_bounds__(256, 2) void grads_few_kernel(ColsJob c, RowsJob r) {
+  constexpr int kLds = ROWS == ROWS_DIRECT && kDirectLds<XT> > ColsShape<XT, S>::lds ? kDirectLds<XT>
+                                                                                      : ColsShape<XT, S>::lds;
+  __shared__ __attribute__((aligned(16))) float lds[kLds];
+  unsigned b = blockIdx.x;
+  const unsigned nc = c.gx * c.gy * c.gz;
+  auto uniform = [](unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); };
+  if (b < nc) {
+    const unsigned x = uniform(b % c.gx), yz = uniform(b / c.gx);
+    cols_few<XT, S>(c, x, uniform(yz % c.gy), uniform(yz / c.gy), lds);
+  } else if constexpr (ROWS != ROWS_NONE) {
+    b -= nc;
+    const unsigned x = uniform(b % r.gx), yz = uniform(b / r.gx), y = uniform(yz % r.gy);
+    if constexpr (ROWS == ROWS_FEW) rows_few<XT, S>(r, x, y);
+    else rows_direct<XT>(r, x, y, uniform(yz / r.gy), lds);
   }
 }
 
@@ -871,16 +950,23 @@ void by_short(int S, F&& f) {
   else f(num<64>{});
 }
 
-// out (M x d) = C^T X, C [R][ldc], over `splits` slabs
 template <typename XT, int S>
-void cols(const float* weight, float none, const float* C, int64_t ldc, const void* X, int64_t ldx, int64_t R, int d,
-          int splits, int64_t per, float* slabs, int M, const float* weight_m, void* out, int64_t ldo, hipStream_t s) {
-  const dim3 grid((unsigned)cdiv(d, ColsShape<XT, S>::width), (unsigned)splits, (unsigned)cdiv(M, S));
-  hipLaunchKernelGGL((cols_few_kernel<XT, S>), grid, dim3(256), 0, s, C, ldc, (const XT*)X, ldx, R, d, weight, none,
-                     per, slabs, M, weight_m, splits > 1 ? nullptr : (XT*)out, ldo);
-  if (splits > 1)
-    hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3((unsigned)cdiv((int64_t)M * d, 64)), dim3(256), 0, s, slabs,
-                       splits, M, d, weight_m, (XT*)out, ldo);
+ColsJob cols_job(const float* weight, float none, const float* C, int64_t ldc, const void* X, int64_t ldx, int64_t R,
+                 int d, int splits, int64_t per, float* slabs, int M, const float* weight_m, void* out, int64_t ldo) {
+  return {C, ldc, X, ldx, R, d, weight, none, per, slabs, M, weight_m, splits > 1 ? nullptr : out, ldo,
+          (unsigned)cdiv(d, ColsShape<XT, S>::width), (unsigned)splits, (unsigned)cdiv(M, S)};
+}
+SlabsJob sum_job(const float* slabs, int count, int M, int d, const float* weight, void* out, int64_t ldo) {
+  return {slabs, count, M, d, weight, out, ldo, (unsigned)cdiv((int64_t)M * d, 64)};
+}
+template <typename XT, int S, int ROWS>
+void launch_grads(const ColsJob& c, const RowsJob& r, unsigned blocks_r, hipStream_t s) {
+  hipLaunchKernelGGL((grads_few_kernel<XT, S, ROWS>), dim3(c.gx * c.gy * c.gz + blocks_r), dim3(256), 0, s, c, r);
+}
+template <typename XT>
+void launch_sums(const SlabsJobs& jobs, hipStream_t s) {
+  if (const unsigned blocks = jobs.j[0].blocks + jobs.j[1].blocks)
+    hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3(blocks), dim3(256), 0, s, jobs);
 }
 
 template <typename XT>
@@ -931,18 +1017,28 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   constexpr int VEC = kVec<XT>;
   by_short(p.S, [&](auto S_) {
     constexpr int S = decltype(S_)::value;
-    // (the sums first: the long side's rows may still be in the last-level cache)
-    if (short_out)
-      cols<XT, S>(p.classes ? f.coef : a.offset, p.classes ? 0.f : none, f.C, p.S, p.classes ? a.h : a.w,
-                  p.classes ? a.ldh : a.ldw, p.R, a.d, p.splits, p.per, (float*)(ws + p.slabs), rows_b,
-                  p.classes ? nullptr : f.coef, short_out, p.classes ? a.lddw : a.lddh, s);
-    if (long_out && !p.joined) {
-      const int64_t cols = cdiv(a.d, 64 * VEC);
-      const dim3 grid((unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max<int64_t>(1, (S == 64 ? 512 : 1536) / cols)), (unsigned)cols);
-      hipLaunchKernelGGL((rows_few_kernel<XT, S>), grid, dim3(256), 0, s, f.C, (const XT*)(p.classes ? a.w : a.h),
-                         p.classes ? a.ldw : a.ldh, rows_b, p.classes ? a.offset : f.coef, p.classes ? none : 0.f,
-                         p.R, a.d, p.classes ? f.coef : nullptr, (XT*)long_out, p.classes ? a.lddh : a.lddw);
+    ColsJob c{};
+    RowsJob r{};
+    SlabsJobs sums{};
+    float* slabs = (float*)(ws + p.slabs);
+    if (short_out) {
+      c = cols_job<XT, S>(p.classes ? f.coef : a.offset, p.classes ? 0.f : none, f.C, p.S, p.classes ? a.h : a.w,
+                          p.classes ? a.ldh : a.ldw, p.R, a.d, p.splits, p.per, slabs, rows_b,
+                          p.classes ? nullptr : f.coef, short_out, p.classes ? a.lddw : a.lddh);
+      if (p.splits > 1)
+        sums.j[0] = sum_job(slabs, p.splits, rows_b, a.d, p.classes ? nullptr : f.coef, short_out,
+                            p.classes ? a.lddw : a.lddh);
     }
+    if (long_out && !p.joined) {
+      const unsigned cols = (unsigned)cdiv(a.d, 64 * VEC);
+      r = {f.C, p.S, p.classes ? a.w : a.h, p.classes ? a.ldw : a.ldh, rows_b, p.classes ? a.offset : f.coef,
+           p.classes ? none : 0.f, p.R, a.d, p.classes ? f.coef : nullptr, long_out, p.classes ? a.lddh : a.lddw, 0,
+           nullptr, (unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max(1u, (S == 64 ? 512u : 1536u) / cols)), cols};
+      launch_grads<XT, S, ROWS_FEW>(c, r, r.gx * r.gy, s);
+    } else if (short_out) {
+      launch_grads<XT, S, ROWS_NONE>(c, r, 0, s);
+    }
+    launch_sums<XT>(sums, s);
   });
   return hipGetLastError();
 }
@@ -951,7 +1047,7 @@ struct DirectPlan {
   int64_t ldz, per;  // per: rows of h of a slab of dW
   int splits;
   int perh, splitsh;  // classes of a slab of dH
-  size_t C, coef, slabs, bytes;
+  size_t C, coef, slabs_w, slabs_h, bytes;
 };
 
 DirectPlan direct_plan(const HeadArgs& a, bool grad) {
@@ -973,9 +1069,8 @@ DirectPlan direct_plan(const HeadArgs& a, bool grad) {
     p.splitsh = (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(256, cdiv(a.d, 256 / (int)elem_bytes(a.type)) * cdiv(a.n, 32)), p.ldz / 256));
     p.perh = (int)up(cdiv(a.classes, p.splitsh), 64);
     p.splitsh = (int)cdiv(a.classes, p.perh);
-    const size_t w = p.splits > 1 ? (size_t)p.splits * a.classes * a.d : 0,
-                 h = p.splitsh > 1 ? (size_t)p.splitsh * a.n * a.d : 0;
-    if (std::max(w, h)) p.slabs = take(std::max(w, h) * 4);  // of one, then of the other
+    if (p.splits > 1) p.slabs_w = take((size_t)p.splits * a.classes * a.d * 4);
+    if (p.splitsh > 1) p.slabs_h = take((size_t)p.splitsh * a.n * a.d * 4);
   }
   p.bytes = at;
   return p;
@@ -988,7 +1083,6 @@ hipError_t direct_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
             a.ids, a.tlogits, a.dloss, a.loss, a.lse, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   f.C = (float*)(ws + p.C);
   f.coef = (float*)(ws + p.coef);
-  float* slabs = (float*)(ws + p.slabs);
   hipLaunchKernelGGL((scores_direct_kernel<XT>), dim3((unsigned)(p.ldz / 64), (unsigned)cdiv(a.n, 32)), dim3(256), 0, s,
                      f, p.ldz);
   auto rows = [&](auto nq, auto wr) {
@@ -999,18 +1093,25 @@ hipError_t direct_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   if (a.m <= 64) longer ? rows(num<1>{}, num<4>{}) : rows(num<1>{}, num<1>{});
   else longer ? rows(num<4>{}, num<4>{}) : rows(num<4>{}, num<1>{});
   KKM_TRY(hipGetLastError());
-  if (grad && a.dw)
-    cols<XT, 64>(f.coef, 0.f, f.C, p.ldz, a.h, a.ldh, a.n, a.d, p.splits, p.per, slabs, a.classes, nullptr, a.dw,
-                 a.lddw, s);
-  if (grad && a.dh) {
-    const dim3 grid((unsigned)cdiv(a.d, 16 * kVec<XT>), (unsigned)cdiv(a.n, 32), (unsigned)p.splitsh);
-    hipLaunchKernelGGL((rows_direct_kernel<XT>), grid, dim3(256), 0, s, f.C, p.ldz, (const XT*)a.w, a.ldw, a.classes,
-                       a.offset, -INFINITY, a.n, a.d, f.coef, p.perh, slabs, p.splitsh > 1 ? nullptr : (XT*)a.dh,
-                       a.lddh);
-    if (p.splitsh > 1)
-      hipLaunchKernelGGL((slabs_few_kernel<XT>), dim3((unsigned)cdiv(a.n * a.d, 64)), dim3(256), 0, s, slabs,
-                         p.splitsh, (int)a.n, a.d, f.coef, (XT*)a.dh, a.lddh);
+  if (!grad) return hipSuccess;
+  ColsJob c{};
+  RowsJob r{};
+  SlabsJobs sums{};
+  float *sw = (float*)(ws + p.slabs_w), *sh = (float*)(ws + p.slabs_h);
+  if (a.dw) {
+    c = cols_job<XT, 64>(f.coef, 0.f, f.C, p.ldz, a.h, a.ldh, a.n, a.d, p.splits, p.per, sw, a.classes, nullptr, a.dw,
+                         a.lddw);
+    if (p.splits > 1) sums.j[0] = sum_job(sw, p.splits, a.classes, a.d, nullptr, a.dw, a.lddw);
   }
+  if (a.dh) {
+    r = {f.C, p.ldz, a.w, a.ldw, a.classes, a.offset, -INFINITY, a.n, a.d, f.coef, p.splitsh > 1 ? nullptr : a.dh,
+         a.lddh, p.perh, sh, (unsigned)cdiv(a.d, 16 * kVec<XT>), (unsigned)cdiv(a.n, 32)};
+    launch_grads<XT, 64, ROWS_DIRECT>(c, r, r.gx * r.gy * p.splitsh, s);
+    if (p.splitsh > 1) sums.j[1] = sum_job(sh, p.splitsh, (int)a.n, a.d, f.coef, a.dh, a.lddh);
+  } else {
+    launch_grads<XT, 64, ROWS_NONE>(c, r, 0, s);
+  }
+  launch_sums<XT>(sums, s);
   return hipGetLastError();
 }
 
