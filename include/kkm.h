@@ -501,13 +501,15 @@ int kkm_peak_mfma(kkm_ctx *ctx, int32_t iters, float *out, int32_t reps, float *
  * All of them are asynchronous on the context's stream, need no build, and do
  * not touch a built K.  Their scratch belongs to the context: it is allocated
  * when a call needs more than an earlier one did (that call waits for the
- * device), counts against the budget, and is given back by the next build and
- * by kkm_destroy.  Matrices are row-major with a row stride (ld, in elements)
- * of at least their width; ids and fp32 vectors are contiguous.  Every sum,
- * statistic and softmax is held in fp32, and results are rounded once, to
- * nearest even, to the type of the matrix they are written to.  Calls give the
- * same bits for the same inputs.  Errors: KKM_ERR_ARG, KKM_ERR_OOM (scratch),
- * KKM_ERR_HIP. */
+ * device, so a call to be captured into a graph follows one of its sizes),
+ * counts against the budget, and is given back by the next build and by
+ * kkm_destroy.  Matrices are row-major with a row stride (ld, in elements) of at
+ * least their width, at any alignment of their type; ids and fp32 vectors are
+ * contiguous.  Outputs do not overlap inputs or each other except where said.
+ * Every sum, statistic and softmax is held in fp32, and results are rounded
+ * once, to nearest even, to the type of the matrix they are written to.  Calls
+ * give the same bits for the same inputs.  Errors: KKM_ERR_ARG, KKM_ERR_OOM
+ * (scratch), KKM_ERR_HIP. */
 typedef enum kkm_type { KKM_F32 = 0, KKM_F16 = 1, KKM_BF16 = 2 } kkm_type;
 #define KKM_MAX_TOP 256        /* pairs of a distillation target's row */
 #define KKM_MAX_FEATURES (1 << 20) /* d of these operators */
@@ -534,9 +536,15 @@ int kkm_layer_norm_grad(kkm_ctx *ctx, int32_t type, int64_t n, int32_t d, const 
  * `classes` rows of w, d wide, both of one type.  offset (fp32[classes], may be
  * NULL) is a constant, e.g. the log of the clusters' sizes; -inf leaves a class
  * out: it has no probability, its row of w is not looked at (it may hold NaN)
- * and its gradient is zero.  The logits are never stored.  fp32 operands are
- * taken as three bfloat16 parts, 24 bits together; an infinite entry of theirs
- * gives NaN. */
+ * and its gradient is zero.
+ *
+ * The logits of a large head are never stored: 256 x 256 of them at a time
+ * leave their rows' largest and sum, and for the gradient they are computed
+ * again, a piece of the classes at a time (G of a piece: at most 256 MB, or 256
+ * classes).  fp32 operands are then taken as three bfloat16 parts, 24 bits
+ * together, and an infinite entry of theirs gives NaN.  A head of at most 64
+ * classes or 64 rows, or of little work (at most 64 MB of logits), holds its
+ * scores as fp32 scratch and multiplies fp32 as fp32. */
 typedef struct kkm_head {
   int32_t type; /* kkm_type of h, w and their gradients */
   int32_t d;
@@ -558,9 +566,9 @@ int kkm_head_loss(kkm_ctx *ctx, const kkm_head *head, const int32_t *ids, float 
 /* The loss as above and the gradient of sum_i dloss_i loss_i (dloss: fp32[n],
  * e.g. 1/n) by h and w:
  *   G(i, v) = dloss_i scale (exp(z(i, v) - lse_i) - [v = ids_i]),  dh = G w,  dw = G^T h
- * into dh (n x d) and dw (classes x d); each may be NULL.  G is held in 16 bits
- * (fp32 operands: in three parts) for pieces of the classes.  Rows without a
- * label or with dloss_i = 0 take no part: whatever they hold, their row of dh
+ * into dh (n x d) and dw (classes x d); each may be NULL.  Of a large head G is
+ * rounded to the operands' 16 bits (fp32: three parts) before its products, of
+ * others it stays in fp32.  Rows without a label or with dloss_i = 0 take no part: whatever they hold, their row of dh
  * is zero.  In a row whose target is left out G is zero there. */
 int kkm_head_grad(kkm_ctx *ctx, const kkm_head *head, const int32_t *ids, const float *dloss, float *loss, float *lse,
                   void *dh, int64_t lddh, void *dw, int64_t lddw);

@@ -30,7 +30,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;
-constexpr int kMaxParts = 64;          // workgroups of max_dloss_kernel
+constexpr int kMaxParts = 64;          // workgroups that look for the largest dloss
 constexpr float kHalfScale = 16384.f;  // binary16 G: probabilities to 4e-9 keep all their bits
 
 __device__ inline float pow2_at_least(float v) {  // v >= 0, or infinite or NaN
@@ -174,6 +174,23 @@ __device__ inline void swap_halves(unsigned a, unsigned b, unsigned& lo, unsigne
   hi = r[1];
 }
 
+// Largest |dloss| of a workgroup's share of the rows (binary16: G is kept in its range).
+__device__ inline void max_dloss(const float* __restrict__ dloss, int64_t n, unsigned* __restrict__ parts,
+                                 unsigned count, unsigned* red) {
+  unsigned m = 0u;  // ordered as the floats are, NaN above all
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)count * blockDim.x)
+    m = max(m, __float_as_uint(dloss[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o, 64));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (unsigned w = 1; w < blockDim.x / 64; ++w) m = max(m, red[w]);
+    parts[blockIdx.x] = m;
+  }
+  __syncthreads();
+}
+
 template <typename E>
 struct ScoreArgs {
   Side w, h;
@@ -182,6 +199,9 @@ struct ScoreArgs {
   int K, nkc, nseg, mt, nt;
   float zscale;         // scale log2 e
   const float* offset;  // may be null
+  const float* dloss;   // forward: the first nparts workgroups leave their rows' largest here; may be null
+  unsigned* dparts;
+  unsigned nparts;
   float2* part;         // forward: (largest, sum) in base 2 of each class tile and row, [tile][n]
   // gradient: rows' lse in base 2 and factors, G [row][class of the piece] and its transpose
   const float *lse2, *coef;
@@ -197,6 +217,7 @@ struct ScoreArgs {
 template <typename E, class S, int P, bool GRAD>
 __global__ __launch_bounds__(S::threads, S::per_cu) void scores_kernel(ScoreArgs<E> a) {
   __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  if (!GRAD && a.dloss && blockIdx.x < a.nparts) max_dloss(a.dloss, a.n, a.dparts, a.nparts, (unsigned*)lds);
   int mi, ni;
   tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
   const int64_t c0 = a.v0 + (int64_t)mi * S::BM, t0 = (int64_t)ni * S::BN;
@@ -309,20 +330,6 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void scores_kernel(ScoreArgs
 
 // ------------------------------------------------------------------ targets
 
-// Largest |dloss| of each workgroup's rows (binary16: G is kept in its range).
-__global__ __launch_bounds__(256) void max_dloss_kernel(const float* __restrict__ dloss, int64_t n,
-                                                        unsigned* __restrict__ parts) {
-  unsigned m = 0u;  // ordered as the floats are, NaN above all
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
-    m = max(m, __float_as_uint(dloss[i]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o, 64));
-  __shared__ unsigned red[4];
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  if (threadIdx.x == 0) parts[blockIdx.x] = max(max(red[0], red[1]), max(red[2], red[3]));
-}
-
 struct TargetArgs {
   const void *h, *w;
   int64_t ldh, ldw, n;
@@ -336,6 +343,7 @@ struct TargetArgs {
   // gradient
   const float* dloss;
   const unsigned* dparts;  // null: G holds dloss as it is
+  unsigned nparts;
   float *lse2, *coef, *alpha;
   int32_t* fix_id;  // n x m
   float* fix_val;
@@ -449,7 +457,7 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
   if (!a.coef) return;
   float cf = a.dloss[i] * a.scale;
   if (a.dparts) {
-    unsigned mx = a.dparts[lane];
+    unsigned mx = lane < (int)a.nparts ? a.dparts[lane] : 0u;
 #pragma unroll
     for (int o = 32; o; o >>= 1) mx = max(mx, (unsigned)__shfl_xor((int)mx, o, 64));
     const float D = pow2_at_least(__uint_as_float(mx));
@@ -825,6 +833,7 @@ struct Head {
     sa.mt = (int)cdiv(classes, big ? BigTile::BM : SmallTile::BM);
     sa.nt = (int)cdiv(a.n, big ? BigTile::BN : SmallTile::BN);
     const dim3 grid((unsigned)((int64_t)sa.mt * sa.nt));
+    sa.nparts = std::min((unsigned)kMaxParts, grid.x);
     if (big)
       hipLaunchKernelGGL((scores_kernel<E, BigTile, P, GRAD>), grid, dim3(BigTile::threads), 0, s, sa);
     else
@@ -896,10 +905,14 @@ struct Head {
     sa.zscale = a.scale * kLog2e;
     sa.offset = a.offset;
     sa.part = at<float2>(p.part);
+    if (grad && a.type == TYPE_F16) {
+      sa.dloss = a.dloss;
+      sa.dparts = at<unsigned>(p.dparts);
+    }
     KKM_TRY(scores<false>(sa, a.classes));
 
     TargetArgs ta{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, p.ntiles, a.scale, a.tscale, a.offset,
-                  a.ids, a.tlogits, sa.part, a.loss, a.lse, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+                  a.ids, a.tlogits, sa.part, a.loss, a.lse, nullptr, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr};
     const float* alpha = nullptr;
     if (grad) {
       ta.dloss = a.dloss;
@@ -911,8 +924,7 @@ struct Head {
         ta.dparts = at<unsigned>(p.dparts);
         ta.alpha = at<float>(p.alpha);
         alpha = ta.alpha;
-        hipLaunchKernelGGL(max_dloss_kernel, dim3(kMaxParts), dim3(256), 0, s, a.dloss, a.n, at<unsigned>(p.dparts));
-        KKM_TRY(hipGetLastError());
+        ta.nparts = (unsigned)std::min<int64_t>(kMaxParts, tile_count(a.classes, a.n, p.big));
       }
     }
     const dim3 tg((unsigned)cdiv(a.n, 4));

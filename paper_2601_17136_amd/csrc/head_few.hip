@@ -146,7 +146,7 @@ __device__ inline float pair_logit(const FewArgs& a, int64_t at, int& id, bool& 
 // features as rows, as in rows_few_kernel, and the wavefronts take every fourth
 // 16 kVec features.
 template <typename XT, int CT>
-__global__ __launch_bounds__(256) void scores_few_classes_kernel(FewArgs a, XT* __restrict__ dh, int64_t lddh) {
+__global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void scores_few_classes_kernel(FewArgs a, XT* __restrict__ dh, int64_t lddh) {
   constexpr int NT = 2, S = CT * 16;
   __shared__ __attribute__((aligned(16))) float zs[4][NT * 16][S + 1];
   const int64_t t0 = (int64_t)blockIdx.x * (NT * 16);

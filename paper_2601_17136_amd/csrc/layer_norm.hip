@@ -123,7 +123,7 @@ template <typename XT, typename WT, int T, int NV>
 __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(
     const XT* __restrict__ x, int64_t ldx, const WT* __restrict__ w, const float* __restrict__ mean,
     const float* __restrict__ rstd, const XT* __restrict__ dy, int64_t lddy, int64_t n, int d, XT* __restrict__ dx,
-    int64_t lddx, float* __restrict__ lines) {
+    int64_t lddx, float* __restrict__ lines, WT* __restrict__ dw, WT* __restrict__ db) {
   constexpr int VEC = kVec<XT>, G = kThreads / T;
   __shared__ float red[2][2][4];
   __shared__ float part[G > 1 ? T * NV * VEC : 1];
@@ -183,7 +183,8 @@ __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(
     }
   }
   if (!lines) return;
-  // the workgroup's line: dw in the first d, db in the next; its groups add up in order
+  // the workgroup's line, dw in the first d, db in the next (or, of the only one,
+  // dw and db); its groups add up in order
   float* line = lines + (int64_t)blockIdx.x * 2 * d;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -208,7 +209,11 @@ __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           const int i = (j * T + t) * VEC + e;
-          if (i < d) line[(int64_t)k * d + i] = G > 1 ? part[(j * VEC + e) * T + t] : mine(j, e);
+          if (i >= d) continue;
+          const float v = G > 1 ? part[(j * VEC + e) * T + t] : mine(j, e);
+          WT* out = k ? db : dw;
+          if (gridDim.x > 1) line[(int64_t)k * d + i] = v;
+          else if (out) out[i] = (WT)v;
         }
   }
 }
@@ -405,14 +410,16 @@ hipError_t norm_grad_typed(const NormArgs& a, float* lines, hipStream_t s) {
                            dim3(kThreads), 0, s, (const XT*)a.x, a.ldx, (const WT*)a.w, a.mean, a.rstd,
                            (const XT*)a.dy, a.lddy, a.n, a.d, (XT*)a.dx, a.lddx);
     } else {
-      nlines = (int)std::min<int64_t>(nlines, (a.n + kThreads / T - 1) / (kThreads / T));
+      const int64_t groups = kThreads / T;
+      nlines = (int)std::min<int64_t>(nlines, (a.n + groups - 1) / groups);
       hipLaunchKernelGGL((layer_norm_grad_kernel<XT, WT, T, NV>), dim3((unsigned)nlines), dim3(kThreads), 0, s,
                          (const XT*)a.x, a.ldx, (const WT*)a.w, a.mean, a.rstd, (const XT*)a.dy, a.lddy, a.n, a.d,
-                         (XT*)a.dx, a.lddx, sums ? lines : nullptr);
+                         (XT*)a.dx, a.lddx, sums ? lines : nullptr, (WT*)a.dw, (WT*)a.db);
+      if (nlines == 1) nlines = -1;  // one workgroup needs no second launch
     }
   });
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !sums) return e;
+  if (e != hipSuccess || !sums || nlines < 0) return e;
   hipLaunchKernelGGL((norm_lines_kernel<WT>), dim3((unsigned)((2 * (int64_t)a.d + 63) / 64)), dim3(1024), 0, s,
                      lines, nlines, a.d, (WT*)a.dw, (WT*)a.db);
   return hipGetLastError();

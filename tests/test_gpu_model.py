@@ -165,9 +165,9 @@ def test_head(ctx, n, d, V, dtype):
 def test_head_of_many_rows_and_classes(ctx, n, d, V, dtype):
     from paper_2601_17136_amd import kkm
     print(f"[gpu] head n={n} d={d} V={V} {dtype}", flush=True)
-    h, w, off, ids, dloss, _, _ = _head_case(n, d, V, dtype, 11, drop=0.1)
+    h, w, off, ids, dloss, _, _ = _head_case(n, d, V, dtype, 11, drop=0.1, offset=V == 1600)
     loss, lse, dh, dw = _outputs(h, w)
-    kkm.kkm_head_grad(ctx, h, w, ids, dloss, loss, lse, dh, dw)
+    kkm.kkm_head_grad(ctx, h, w, ids, dloss, loss, lse, dh, dw, offset=off)
     _check_head(ref.head(h, w, ref.one_hot(ids, V), dloss, 1.0, off), loss, lse, dh, dw)
 
 
@@ -183,12 +183,14 @@ def test_head_in_pieces_of_the_classes(ctx, n, d, V, dtype):
     _check_head(ref.head(h, w, ref.one_hot(ids, V), dloss, 1.0, off), loss, lse, dh, dw)
 
 
+# (each form the head runs in: few classes, few rows, little work, tiles)
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_head_masks(ctx, dtype):
+@pytest.mark.parametrize("n,d,V", [(150, 40, 90), (150, 40, 50), (40, 40, 90), (2600, 640, 1300)])
+def test_head_masks(ctx, n, d, V, dtype):
     """What a mask covers may hold anything: classes left out with NaN rows of w,
     rows without a label or of weight 0 with NaN in h, rows that see no class."""
     from paper_2601_17136_amd import kkm
-    n, d, V = 150, 40, 90
+    print(f"[gpu] head masks n={n} d={d} V={V} {dtype}", flush=True)
     h, w, _, ids, dloss, _, _ = _head_case(n, d, V, dtype, 13)
     off = torch.zeros(V, device="cuda")
     off[10:30] = -float("inf")
