@@ -419,18 +419,28 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
       wr[u] = (const XT*)a.w + (int64_t)max(idj[u], 0) * a.ldw;
     }
     if (!any) continue;
+    // (a pair that is none reads row 0 of w, and its sum is not used)
+    constexpr int VEC = kVec<XT>, W = 64 * VEC;
     float dot[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int c = lane * kVec<XT>; c < a.d; c += 64 * kVec<XT>) {
-      float hv[kVec<XT>];
-      load_part(hr, c, a.d, hv);
+    auto add = [&](const raw_vec<XT>& hv, const raw_vec<XT> (&wv)[4]) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (idj[u] < 0) continue;  // (uniform)
-        float wv[kVec<XT>];
-        load_part(wr[u], c, a.d, wv);
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int e = 0; e < kVec<XT>; ++e) dot[u] = fmaf(hv[e], wv[e], dot[u]);
-      }
+        for (int e = 0; e < VEC; ++e) dot[u] = fmaf((float)hv[e], (float)wv[u][e], dot[u]);
+    };
+    int c = lane * VEC;
+#pragma unroll 4
+    for (int c0 = 0; c0 + W <= a.d; c0 += W, c += W) {
+      raw_vec<XT> wv[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) wv[u] = *(const any_vec<XT>*)(wr[u] + c);
+      add(*(const any_vec<XT>*)(hr + c), wv);
+    }
+    if (c < a.d) {
+      raw_vec<XT> wv[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) wv[u] = load_raw(wr[u], c, a.d);
+      add(load_raw(hr, c, a.d), wv);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
