@@ -423,3 +423,59 @@ def test_workspace_counts_against_the_budget_and_goes_with_a_build():
         assert kkm.kkm_objective(c, torch.zeros(2600, dtype=torch.int32, device="cuda"), 1) == J
     finally:
         kkm.kkm_destroy(c)
+
+
+# ------------------------------------------------------------------ few classes of many rows
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,V,m", [(4096, 1, 1, 0), (4111, 33, 5, 3), (5000, 780, 10, 0), (4200, 513, 31, 40),
+                                     (9001, 1000, 16, 0), (6002, 900, 3, 7), (4999, 512, 32, 0), (4500, 257, 17, 5),
+                                     (4100, 1024, 12, 2), (4101, 1025, 12, 2)])
+def test_few_classes_of_many_rows(ctx, n, d, V, m, dtype):
+    """The same loss from each call, rows without a label that hold infinities, a label past the classes."""
+    from paper_2601_17136_amd import kkm
+    pad = (0, 3, 8)[(n + d + V) % 3]
+    print(f"[gpu] few classes n={n} d={d} V={V} m={m} {dtype} pad={pad}", flush=True)
+    h, w, off, ids, dloss, g, kept = _head_case(n, d, V, dtype, n + 5 * d + V, pad, offset=V > 2 and d % 2 == 1,
+                                                drop=0.15)
+    more = dict(scale=0.6, offset=off)
+    if m:
+        top, logits = _teacher(n, V, m, g, kept)
+        more["teacher_scale"] = 0.9
+        fwd, bwd, said = kkm.kkm_distill_loss, kkm.kkm_distill_grad, (top, logits)
+        q = ref.teacher(top, logits, 0.9, V)
+        none = 2
+    else:
+        ids[7] = -1
+        fwd, bwd, said = kkm.kkm_head_loss, kkm.kkm_head_grad, (ids,)
+        q = ref.one_hot(ids, V)
+        none = 7
+    loss, lse, dh, dw = _outputs(h, w, pad)
+    bwd(ctx, h, w, *said, dloss, loss, lse, dh, dw, **more)
+    r = ref.head(h, w, q, dloss, 0.6, off)
+    if m:  # each pair's own terms: a class named twice has q log q of its parts
+        parts = torch.softmax(torch.where(top >= 0, logits.double() * 0.9, -torch.inf), 1).nan_to_num(0.0).cpu()
+        r["loss"] = r["loss"] + (torch.special.entr(q).sum(1) - torch.special.entr(parts).sum(1))
+    _check_head(r, loss, lse, dh, dw)
+    assert loss[none] == 0 and not dh[none].any()
+    # the loss alone, one gradient alone: the same bits
+    a = _outputs(h, w)
+    fwd(ctx, h, w, *said, *a[:2], **more)
+    assert torch.equal(a[0], loss) and torch.equal(a[1], lse)
+    bwd(ctx, h, w, *said, dloss, *a[:2], a[2], None, **more)
+    bwd(ctx, h, w, *said, dloss, *a[:2], None, a[3], **more)
+    assert torch.equal(a[2], dh) and torch.equal(a[3], dw)
+    # an infinity in a row that takes no part reaches no other row's results
+    h2 = h.clone()
+    h2[none] = float("inf")
+    b = _outputs(h, w)
+    bwd(ctx, h2, w, *said, dloss, *b, **more)
+    assert torch.equal(b[3], dw) and not b[2][none].any()
+    # a label past the classes: NaN for its row, and in dW
+    first = said[0].clone()
+    first.view(n, -1)[11, 0] = V
+    if m:
+        logits[11, 0] = 0.5
+    bwd(ctx, h, w, first, *said[1:], dloss, *b, **more)
+    assert torch.isnan(b[0][11]) and torch.isnan(b[3]).any()
+    assert torch.equal(b[0][:11], loss[:11]) and torch.equal(b[2][12:], dh[12:])
