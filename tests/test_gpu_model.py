@@ -479,3 +479,58 @@ def test_few_classes_of_many_rows(ctx, n, d, V, m, dtype):
     bwd(ctx, h, w, first, *said[1:], dloss, *b, **more)
     assert torch.isnan(b[0][11]) and torch.isnan(b[3]).any()
     assert torch.equal(b[0][:11], loss[:11]) and torch.equal(b[2][12:], dh[12:])
+
+
+# ------------------------------------------------------------------ rows far apart
+
+def _far(values, ld):
+    """The rows `ld` elements apart: past 32 bits for the last."""
+    n, d = values.shape
+    t = torch.empty((n - 1) * ld + d, device="cuda", dtype=values.dtype).as_strided((n, d), (ld, 1))
+    assert (n - 1) * ld > 2 ** 31
+    return t.copy_(values)
+
+
+@pytest.mark.parametrize("n,d,V,dtype,ld", [(2100, 48, 10, "bf16", 2 ** 20 + 8), (2100, 64, 100, "f16", 2 ** 20 + 8),
+                                            (1300, 64, 90, "f32", 2 ** 21 - 5), (2100, 264, 2000, "bf16", 2 ** 20 + 8),
+                                            (1100, 264, 2000, "bf16", 2 ** 21 + 8), (1100, 250, 2000, "f32", 2 ** 21)])
+def test_rows_of_h_far_apart(ctx, n, d, V, dtype, ld):
+    from paper_2601_17136_amd import kkm
+    print(f"[gpu] far h n={n} d={d} V={V} {dtype} ld={ld}", flush=True)
+    h, w, off, ids, dloss, _, _ = _head_case(n, d, V, dtype, n + d, offset=True, drop=0.1)
+    want, got = _outputs(h, w), list(_outputs(h, w))
+    kkm.kkm_head_grad(ctx, h, w, ids, dloss, *want, offset=off)
+    got[2] = _far(torch.zeros_like(h), ld)
+    kkm.kkm_head_grad(ctx, _far(h, ld), w, ids, dloss, *got, offset=off)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("n,V,d,dtype", [(16, 2100, 72, "bf16"), (200, 2100, 72, "f16"), (2000, 2100, 264, "bf16")])
+def test_rows_of_w_far_apart(ctx, n, V, d, dtype):
+    from paper_2601_17136_amd import kkm
+    print(f"[gpu] far w n={n} d={d} V={V} {dtype}", flush=True)
+    h, w, _, _, dloss, g, kept = _head_case(n, d, V, dtype, n + d)
+    ids, logits = _teacher(n, V, 5, g, kept)
+    want, got = _outputs(h, w), list(_outputs(h, w))
+    kkm.kkm_distill_grad(ctx, h, w, ids, logits, dloss, *want)
+    got[3] = _far(torch.zeros_like(w), 2 ** 20 + 8)
+    kkm.kkm_distill_grad(ctx, h, _far(w, 2 ** 20 + 8), ids, logits, dloss, *got)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("n,d,dtype", [(2100, 300, "bf16"), (2100, 3001, "f16"), (2100, 20000, "bf16")])
+def test_layer_norm_of_rows_far_apart(ctx, n, d, dtype):
+    from paper_2601_17136_amd import kkm
+    print(f"[gpu] far norm n={n} d={d} {dtype}", flush=True)
+    ld, dev = 2 ** 20 + 8, {"device": "cuda"}
+    x, dy = (torch.randn(n, d, generator=_gen(d + k), **dev).to(DTYPES[dtype]) for k in (0, 1))
+    w, b = torch.randn(d, generator=_gen(5), **dev), torch.randn(d, generator=_gen(6), **dev)
+    outs = []
+    for far in (False, True):
+        place = (lambda t: _far(t, ld)) if far else (lambda t: t)
+        y, dx = place(torch.zeros_like(x)), place(torch.zeros_like(x))
+        mean, rstd, dw, db = (torch.empty(k, **dev) for k in (n, n, d, d))
+        kkm.kkm_layer_norm(ctx, place(x), w, b, 1e-5, y, mean, rstd)
+        kkm.kkm_layer_norm_grad(ctx, place(x), w, place(dy), mean, rstd, dx, dw, db)
+        outs.append([t.clone() for t in (y, mean, rstd, dx, dw, db)])
+    assert all(torch.equal(x, y) for x, y in zip(*outs))
