@@ -14,8 +14,9 @@
 // targets by fix_kernel), and two products, in one launch where their tiles are
 // alike, give the piece's rows of dW and its part of dH.
 //
-// The gradient so multiplies four times where a caller that kept the logits
-// would three times, and holds 256 MB of G in place of all logits (1.07 GB as fp32
+// Logits of at most 256 MB are kept for G where that takes less (keep_logits).
+// Others are multiplied again: four products where a caller that kept them would
+// take three, with 256 MB of G in place of all logits (1.07 GB as fp32
 // for 8192 rows of 32768 classes).  Bound by the matrix cores, whose clock falls
 // to 1.75 - 1.97 GHz under this load.
 //
@@ -35,6 +36,7 @@ namespace kkm {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 constexpr int kMaxParts = 64;          // workgroups that look for the largest dloss
 constexpr float kHalfScale = 16384.f;  // binary16 G: probabilities to 4e-9 keep all their bits
@@ -211,6 +213,7 @@ struct ScoreArgs {
   unsigned* dparts;
   unsigned nparts;
   float2* part;         // forward: (largest, sum) in base 2 of each class tile and row, [tile][n]
+  floatx4* z;           // logits in base 2 in the order of the tiles' lanes, written forward, read for G; may be null
   // gradient: rows' lse in base 2 and factors, G [row][class of the piece] and its transpose
   const float *lse2, *coef;
   const int32_t* fix_id;  // one target per row: its entry of G (else fix_kernel's work), or null
@@ -226,33 +229,64 @@ struct ScoreArgs {
 // both orders at 3.4 TB/s.  bfloat16, 8192 rows of 4096: 32768 classes 1.83 ms, 1.20
 // PFLOP/s, matrix cores busy 62 % of the cycles (a library product of that shape
 // 1.41 PFLOP/s); with G, 16384 classes 1.07 ms, 1.02 PFLOP/s, 56 %.  fp32, 4000 rows
-// of 1000, 4000 classes: 158 us, 1.2 PFLOP/s of plane products; with G 196 us.
-template <typename E, class S, int P, bool GRAD>
-__global__ __launch_bounds__(S::threads, S::per_cu) void scores_kernel(ScoreArgs<E> a) {
-  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+// of 1000, 4000 classes: 158 us, 1.2 PFLOP/s of plane products; with G 196 us.  G of
+// kept logits is bound by memory and needs no LDS: 20011 binary16 classes of 1777
+// rows 82 us, 3.5 TB/s, where multiplying again takes 141.
+enum ScoresMode { SCORES_LOSS, SCORES_G, SCORES_G_OF_Z };
+template <typename E, class S, int P, int MODE>
+__global__ __launch_bounds__(S::threads, MODE == SCORES_G_OF_Z ? 2 : S::per_cu) void scores_kernel(ScoreArgs<E> a) {
+  constexpr bool GRAD = MODE != SCORES_LOSS;
+  __shared__ __attribute__((aligned(1024))) char lds[MODE == SCORES_G_OF_Z ? 16 : S::lds_bytes];
   if (!GRAD && a.dloss && blockIdx.x < a.nparts) max_dloss(a.dloss, a.n, a.dparts, a.nparts, (unsigned*)lds);
   int mi, ni;
   tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
   const int64_t c0 = a.v0 + (int64_t)mi * S::BM, t0 = (int64_t)ni * S::BN;
-  floatx16 acc[S::WM][S::WN];
-  tile_product<E, S>(a.w, a.h, c0, t0, a.K, a.nkc, a.nseg, 0, a.nseg * a.nkc, lds, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
-  // z in base 2; -inf where a class is left out, whatever its product
+  floatx16 acc[S::WM][S::WN];
+  floatx4* kept = a.z + (((int64_t)ni * a.mt + mi) * S::waves + wave) * (S::WM * S::WN * 4 * 64) + lane;
+  if constexpr (MODE == SCORES_G_OF_Z) {
 #pragma unroll
-  for (int bi = 0; bi < S::WM; ++bi)
+    for (int bi = 0; bi < S::WM; ++bi)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+      for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int64_t v = c0 + (wm * S::WM + bi) * 32 + 8 * q + 4 * h + e;
-        const float off = v >= a.classes ? -INFINITY : a.offset ? a.offset[v] * kLog2e : 0.f;
+        for (int q = 0; q < 4; ++q) {
+          const floatx4 z = kept[((bi * S::WN + bj) * 4 + q) * 64];
 #pragma unroll
-        for (int bj = 0; bj < S::WN; ++bj) {
-          const float z = fmaf(acc[bi][bj][4 * q + e], a.zscale, off);
-          acc[bi][bj][4 * q + e] = off == -INFINITY ? -INFINITY : z;
+          for (int e = 0; e < 4; ++e) acc[bi][bj][4 * q + e] = z[e];
         }
-      }
+  } else {
+    tile_product<E, S>(a.w, a.h, c0, t0, a.K, a.nkc, a.nseg, 0, a.nseg * a.nkc, lds, acc);
+    // z in base 2; -inf where a class is left out, whatever its product
+#pragma unroll
+    for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int64_t v = c0 + (wm * S::WM + bi) * 32 + 8 * q + 4 * h + e;
+          const float off = v >= a.classes ? -INFINITY : a.offset ? a.offset[v] * kLog2e : 0.f;
+#pragma unroll
+          for (int bj = 0; bj < S::WN; ++bj) {
+            const float z = fmaf(acc[bi][bj][4 * q + e], a.zscale, off);
+            acc[bi][bj][4 * q + e] = off == -INFINITY ? -INFINITY : z;
+          }
+        }
+    if (MODE == SCORES_LOSS && a.z) {
+#pragma unroll
+      for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+        for (int bj = 0; bj < S::WN; ++bj)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            floatx4 z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = acc[bi][bj][4 * q + e];
+            kept[((bi * S::WN + bj) * 4 + q) * 64] = z;
+          }
+    }
+  }
   if constexpr (!GRAD) {
     float2* red = (float2*)lds;  // [wm][column of the tile]
 #pragma unroll
@@ -683,14 +717,35 @@ TileCost tile_cost(bool big) { return big ? TileCost{1.7, 6, 256} : TileCost{1.2
 int64_t tile_count(int64_t M, int64_t N, bool big) {
   return big ? cdiv(M, BigTile::BM) * cdiv(N, BigTile::BN) : cdiv(M, SmallTile::BM) * cdiv(N, SmallTile::BN);
 }
-bool big_scores(int64_t classes, int64_t n, int64_t chunks, int planes, bool grad) {
+// A launch of scores; *big: in which tiles it takes less.
+double scores_time(int64_t classes, int64_t n, int64_t chunks, int planes, bool grad, bool* big) {
   double t[2];
-  for (int big = 0; big < 2; ++big) {
-    const TileCost c = tile_cost(big);
-    const double end = planes * (grad ? (big ? 19 : 9) : (big ? 9 : 4));
-    t[big] = cdiv(tile_count(classes, n, big), c.slots) * (chunks * c.chunk + (grad ? end : end / planes));
+  for (int b = 0; b < 2; ++b) {
+    const TileCost c = tile_cost(b);
+    const double end = planes * (grad ? (b ? 19 : 9) : (b ? 9 : 4));
+    t[b] = cdiv(tile_count(classes, n, b), c.slots) * (chunks * c.chunk + (grad ? end : end / planes));
   }
-  return t[1] < t[0];
+  *big = t[1] < t[0];
+  return t[*big];
+}
+bool big_scores(int64_t classes, int64_t n, int64_t chunks, int planes, bool grad) {
+  bool big;
+  scores_time(classes, n, chunks, planes, grad, &big);
+  return big;
+}
+
+// Whether logits that fit a piece's bytes stay for G rather than be multiplied
+// again: 4 bytes of each written and read, beside G's, at 4.5 TB/s.  Microseconds
+// with gradient, multiplied again / kept: fp32, 4553 rows of 3268, 834 classes 988 /
+// 731, 8000 of 300, 1500 classes 305 / 282; bfloat16, 8000 classes of 8000 rows of 100
+// 250 / 346, of 512 427 / 476, of 2048 1081 / 950; 984 classes of 2020 rows of 752
+// 72 / 65; binary16, 2000 of 30000 of 256 343 / 406, 3000 of 18979 of 1979 1205 / 1077.
+bool keep_logits(int64_t classes, int64_t n, int64_t chunks, int planes, bool big) {
+  bool again_big;
+  const double again = scores_time(classes, n, chunks, planes, true, &again_big);
+  const int side = big ? BigTile::BM : SmallTile::BM;
+  const double scores = (double)tile_count(classes, n, big) * side * side;
+  return 1.15 * (8 + scores * (8 + 4 * planes) / 4.5e6) < again;
 }
 
 // When the last of n0 workgroups of d0 and then n1 of d1 ends, dealt to `slots`
@@ -775,12 +830,13 @@ struct HeadPlan {
   int planes, nseg, kp;
   int64_t n_pad, v_pad;
   bool big, bigg;       // scores in BigTile: the forward pass, and for G
+  bool keep;            // the forward pass's logits stay for G
   int ntiles;
   int piece;            // classes of a piece (a multiple of kPad)
   int sh, sw;           // slabs of dH and dW (0: none)
   bool bigh, bigw;
   // workspace offsets
-  size_t h, w, part, ht, wt, lse2, coef, dparts, alpha, fix_id, fix_val, G, Gt, slabs_h, slabs_w, bytes;
+  size_t h, w, part, z, ht, wt, lse2, coef, dparts, alpha, fix_id, fix_val, G, Gt, slabs_h, slabs_w, bytes;
 };
 
 HeadPlan plan_of(const HeadArgs& a, bool grad) {
@@ -814,8 +870,13 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
     p.fix_val = take((size_t)a.n * a.m * 4);
     p.G = take((size_t)p.planes * p.n_pad * p.piece * 2);
     p.Gt = take((size_t)p.planes * p.n_pad * p.piece * 2);
+    const size_t z_bytes = (size_t)tile_count(a.classes, a.n, p.big) *
+                           (p.big ? BigTile::BM * BigTile::BN : SmallTile::BM * SmallTile::BN) * 4;
+    p.keep = a.classes <= p.piece && z_bytes <= kPieceBytes &&
+             keep_logits(a.classes, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, p.big);
+    if (p.keep) p.z = take(z_bytes);
     const int64_t pieces = cdiv(a.classes, p.piece), of_piece = std::min<int64_t>(p.piece, a.classes);
-    p.bigg = big_scores(of_piece, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, true);
+    p.bigg = p.keep ? p.big : big_scores(of_piece, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, true);
     const ProductChoice c = choose_products({a.n, of_piece}, a.d, {p.nseg * cdiv(of_piece, kChunkK),
                                                                    p.nseg * cdiv(a.n, kChunkK)});
     p.bigh = c.big[0];
@@ -857,18 +918,18 @@ struct Head {
     return {at<E>(off), p.kp, plane, rows};
   }
 
-  template <bool GRAD>
+  template <int MODE>
   hipError_t scores(ScoreArgs<E> sa, int64_t classes) const {
-    const bool big = GRAD ? p.bigg : p.big;
+    const bool big = MODE == SCORES_LOSS ? p.big : p.bigg;
     sa.nkc = p.kp / chunk_of(big);
     sa.mt = (int)cdiv(classes, big ? BigTile::BM : SmallTile::BM);
     sa.nt = (int)cdiv(a.n, big ? BigTile::BN : SmallTile::BN);
     const dim3 grid((unsigned)((int64_t)sa.mt * sa.nt));
     sa.nparts = std::min((unsigned)kMaxParts, grid.x);
     if (big)
-      hipLaunchKernelGGL((scores_kernel<E, BigTile, P, GRAD>), grid, dim3(BigTile::threads), 0, s, sa);
+      hipLaunchKernelGGL((scores_kernel<E, BigTile, P, MODE>), grid, dim3(BigTile::threads), 0, s, sa);
     else
-      hipLaunchKernelGGL((scores_kernel<E, SmallTile, P, GRAD>), grid, dim3(SmallTile::threads), 0, s, sa);
+      hipLaunchKernelGGL((scores_kernel<E, SmallTile, P, MODE>), grid, dim3(SmallTile::threads), 0, s, sa);
     return hipGetLastError();
   }
 
@@ -940,7 +1001,8 @@ struct Head {
       sa.dloss = a.dloss;
       sa.dparts = at<unsigned>(p.dparts);
     }
-    KKM_TRY(scores<false>(sa, a.classes));
+    if (p.keep) sa.z = at<floatx4>(p.z);
+    KKM_TRY(scores<SCORES_LOSS>(sa, a.classes));
 
     TargetArgs ta{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, p.ntiles, a.scale, a.tscale, a.offset,
                   a.ids, a.tlogits, sa.part, a.loss, a.lse, nullptr, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr};
@@ -993,7 +1055,7 @@ struct Head {
     for (int v0 = 0; v0 < a.classes; v0 += p.piece) {
       const int cnt = std::min(p.piece, a.classes - v0), kv = (int)up(cnt, kChunkK);
       sa.v0 = v0;
-      KKM_TRY(scores<true>(sa, cnt));
+      KKM_TRY(p.keep ? scores<SCORES_G_OF_Z>(sa, cnt) : scores<SCORES_G>(sa, cnt));
       if (a.m > 1) {
         hipLaunchKernelGGL((fix_kernel<E, P>), grid1(a.n * a.m), dim3(256), 0, s, ta.fix_id, ta.fix_val, a.n, a.m, v0,
                            v0 + cnt, sa.G, sa.ldg, sa.planeg, sa.Gt, sa.ldt, sa.planet);
