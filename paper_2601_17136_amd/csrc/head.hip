@@ -14,9 +14,9 @@
 // targets by fix_kernel), and two products, in one launch where their tiles are
 // alike, give the piece's rows of dW and its part of dH.
 //
-// Logits of at most 256 MB are kept for G where that takes less (keep_logits).
-// Others are multiplied again: four products where a caller that kept them would
-// take three, with 256 MB of G in place of all logits (1.07 GB as fp32
+// The first classes' logits, at most 256 MB of them, stay for G where that takes
+// less (kept_tiles).  The others are multiplied again: four products where a caller
+// that kept all would take three, with those 256 MB of G in place of 1.07 GB (fp32
 // for 8192 rows of 32768 classes).  Bound by the matrix cores, whose clock falls
 // to 1.75 - 1.97 GHz under this load.
 //
@@ -213,7 +213,8 @@ struct ScoreArgs {
   unsigned* dparts;
   unsigned nparts;
   float2* part;         // forward: (largest, sum) in base 2 of each class tile and row, [tile][n]
-  floatx4* z;           // logits in base 2 in the order of the tiles' lanes, written forward, read for G; may be null
+  floatx4* z;           // logits in base 2 of the first `kept` class tiles, in the order of the tiles' lanes,
+  int kept;             // written forward, read for G
   // gradient: rows' lse in base 2 and factors, G [row][class of the piece] and its transpose
   const float *lse2, *coef;
   const int32_t* fix_id;  // one target per row: its entry of G (else fix_kernel's work), or null
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(S::threads, MODE == SCORES_G_OF_Z ? 2 : S::per_cu) 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
   floatx16 acc[S::WM][S::WN];
-  floatx4* kept = a.z + (((int64_t)ni * a.mt + mi) * S::waves + wave) * (S::WM * S::WN * 4 * 64) + lane;
+  floatx4* kept = a.z + (((int64_t)ni * a.kept + mi) * S::waves + wave) * (S::WM * S::WN * 4 * 64) + lane;
   if constexpr (MODE == SCORES_G_OF_Z) {
 #pragma unroll
     for (int bi = 0; bi < S::WM; ++bi)
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(S::threads, MODE == SCORES_G_OF_Z ? 2 : S::per_cu) 
             acc[bi][bj][4 * q + e] = off == -INFINITY ? -INFINITY : z;
           }
         }
-    if (MODE == SCORES_LOSS && a.z) {
+    if (MODE == SCORES_LOSS && mi < a.kept) {
 #pragma unroll
       for (int bi = 0; bi < S::WM; ++bi)
 #pragma unroll
@@ -734,18 +735,28 @@ bool big_scores(int64_t classes, int64_t n, int64_t chunks, int planes, bool gra
   return big;
 }
 
-// Whether logits that fit a piece's bytes stay for G rather than be multiplied
-// again: 4 bytes of each written and read, beside G's, at 4.5 TB/s.  Microseconds
-// with gradient, multiplied again / kept: fp32, 4553 rows of 3268, 834 classes 988 /
-// 731, 8000 of 300, 1500 classes 305 / 282; bfloat16, 8000 classes of 8000 rows of 100
-// 250 / 346, of 512 427 / 476, of 2048 1081 / 950; 984 classes of 2020 rows of 752
-// 72 / 65; binary16, 2000 of 30000 of 256 343 / 406, 3000 of 18979 of 1979 1205 / 1077.
-bool keep_logits(int64_t classes, int64_t n, int64_t chunks, int planes, bool big) {
-  bool again_big;
-  const double again = scores_time(classes, n, chunks, planes, true, &again_big);
+// Class tiles whose logits stay for G rather than be multiplied again: those of
+// the first piece that fit a piece's bytes, where that takes less.  4 bytes of each
+// are written and read, beside G's, at 4.5 TB/s.  Microseconds with gradient,
+// multiplied again / kept: fp32, 4553 rows of 3268, 834 classes 988 / 731, 8000 of
+// 300, 1500 classes 305 / 282; bfloat16, 8000 classes of 8000 rows of 100 250 / 346,
+// of 512 427 / 476, of 2048 1081 / 950; 984 classes of 2020 rows of 752 72 / 65;
+// binary16, 2000 of 30000 of 256 343 / 406, 3000 of 18979 of 1979 1205 / 1077.  A part
+// of the classes: bfloat16, 32768 of 8192 rows of 4096 8262 / 7969, fp32, 9001 of 9000
+// of 1500 6080 / 5518.
+int kept_tiles(int64_t classes, int64_t n, int64_t chunks, int planes, bool big, int piece) {
   const int side = big ? BigTile::BM : SmallTile::BM;
-  const double scores = (double)tile_count(classes, n, big) * side * side;
-  return 1.15 * (8 + scores * (8 + 4 * planes) / 4.5e6) < again;
+  const int64_t row_tiles = cdiv(n, side), bytes = row_tiles * side * side * 4;
+  int64_t fit = std::min((int64_t)piece / side, (int64_t)(kPieceBytes / bytes));
+  // (the other classes' tiles, of either shape, begin at a multiple of kPad and so end in the piece)
+  fit = fit * side >= classes ? cdiv(classes, side) : fit * side / kPad * kPad / side;
+  if (fit <= 0) return 0;
+  bool again_big;
+  const int64_t first = std::min<int64_t>(piece, classes), rest = first - std::min(first, fit * side);
+  const double again = scores_time(first, n, chunks, planes, true, &again_big);
+  const double left = rest ? 5 + scores_time(rest, n, chunks, planes, true, &again_big) : 0;
+  const double keep = 8 + (double)(fit * bytes / 4) * (8 + 4 * planes) / 4.5e6;
+  return 1.15 * keep + left < again ? (int)fit : 0;
 }
 
 // When the last of n0 workgroups of d0 and then n1 of d1 ends, dealt to `slots`
@@ -830,7 +841,7 @@ struct HeadPlan {
   int planes, nseg, kp;
   int64_t n_pad, v_pad;
   bool big, bigg;       // scores in BigTile: the forward pass, and for G
-  bool keep;            // the forward pass's logits stay for G
+  int kept;             // class tiles whose logits stay for G
   int ntiles;
   int piece;            // classes of a piece (a multiple of kPad)
   int sh, sw;           // slabs of dH and dW (0: none)
@@ -870,13 +881,11 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
     p.fix_val = take((size_t)a.n * a.m * 4);
     p.G = take((size_t)p.planes * p.n_pad * p.piece * 2);
     p.Gt = take((size_t)p.planes * p.n_pad * p.piece * 2);
-    const size_t z_bytes = (size_t)tile_count(a.classes, a.n, p.big) *
-                           (p.big ? BigTile::BM * BigTile::BN : SmallTile::BM * SmallTile::BN) * 4;
-    p.keep = a.classes <= p.piece && z_bytes <= kPieceBytes &&
-             keep_logits(a.classes, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, p.big);
-    if (p.keep) p.z = take(z_bytes);
+    p.kept = kept_tiles(a.classes, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, p.big, p.piece);
+    const int64_t side = p.big ? BigTile::BM : SmallTile::BM;
+    p.z = take((size_t)(p.kept * cdiv(a.n, side) * side * side * 4));
     const int64_t pieces = cdiv(a.classes, p.piece), of_piece = std::min<int64_t>(p.piece, a.classes);
-    p.bigg = p.keep ? p.big : big_scores(of_piece, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, true);
+    p.bigg = big_scores(of_piece, a.n, (int64_t)p.nseg * p.kp / kChunkK, p.planes, true);
     const ProductChoice c = choose_products({a.n, of_piece}, a.d, {p.nseg * cdiv(of_piece, kChunkK),
                                                                    p.nseg * cdiv(a.n, kChunkK)});
     p.bigh = c.big[0];
@@ -920,7 +929,7 @@ struct Head {
 
   template <int MODE>
   hipError_t scores(ScoreArgs<E> sa, int64_t classes) const {
-    const bool big = MODE == SCORES_LOSS ? p.big : p.bigg;
+    const bool big = MODE == SCORES_G ? p.bigg : p.big;
     sa.nkc = p.kp / chunk_of(big);
     sa.mt = (int)cdiv(classes, big ? BigTile::BM : SmallTile::BM);
     sa.nt = (int)cdiv(a.n, big ? BigTile::BN : SmallTile::BN);
@@ -1001,7 +1010,10 @@ struct Head {
       sa.dloss = a.dloss;
       sa.dparts = at<unsigned>(p.dparts);
     }
-    if (p.keep) sa.z = at<floatx4>(p.z);
+    if (grad) {
+      sa.z = at<floatx4>(p.z);
+      sa.kept = p.kept;
+    }
     KKM_TRY(scores<SCORES_LOSS>(sa, a.classes));
 
     TargetArgs ta{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, p.ntiles, a.scale, a.tscale, a.offset,
@@ -1055,7 +1067,15 @@ struct Head {
     for (int v0 = 0; v0 < a.classes; v0 += p.piece) {
       const int cnt = std::min(p.piece, a.classes - v0), kv = (int)up(cnt, kChunkK);
       sa.v0 = v0;
-      KKM_TRY(p.keep ? scores<SCORES_G_OF_Z>(sa, cnt) : scores<SCORES_G>(sa, cnt));
+      const int kept = v0 ? 0 : (int)std::min<int64_t>(cnt, (int64_t)p.kept * (p.big ? BigTile::BM : SmallTile::BM));
+      if (kept) KKM_TRY(scores<SCORES_G_OF_Z>(sa, kept));
+      if (kept < cnt) {
+        ScoreArgs<E> rest = sa;
+        rest.v0 += kept;
+        rest.G += kept;
+        rest.Gt += (int64_t)kept * sa.ldt;
+        KKM_TRY(scores<SCORES_G>(rest, cnt - kept));
+      }
       if (a.m > 1) {
         hipLaunchKernelGGL((fix_kernel<E, P>), grid1(a.n * a.m), dim3(256), 0, s, ta.fix_id, ta.fix_val, a.n, a.m, v0,
                            v0 + cnt, sa.G, sa.ldg, sa.planeg, sa.Gt, sa.ldt, sa.planet);

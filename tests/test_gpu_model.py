@@ -534,3 +534,65 @@ def test_layer_norm_of_rows_far_apart(ctx, n, d, dtype):
         kkm.kkm_layer_norm_grad(ctx, place(x), w, place(dy), mean, rstd, dx, dw, db)
         outs.append([t.clone() for t in (y, mean, rstd, dx, dw, db)])
     assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+# ------------------------------------------------------------------ logits kept for a part of the classes
+
+@pytest.mark.parametrize("n,d,V,m,dtype", [(4096, 2056, 20000, 0, "bf16"), (5001, 1111, 40007, 3, "f16"),
+                                           (9000, 320, 9001, 0, "f32"), (66000, 1100, 1300, 2, "bf16")])
+def test_head_of_more_logits_than_are_kept(ctx, n, d, V, m, dtype):
+    """Rows and classes on both sides of what is kept, against the formulas on a part of each."""
+    from paper_2601_17136_amd import kkm
+    print(f"[gpu] kept in part n={n} d={d} V={V} m={m} {dtype}", flush=True)
+    h, w, off, ids, dloss, g, kept = _head_case(n, d, V, dtype, n + V, offset=True, drop=0.1)
+    more, out = dict(scale=0.7, offset=off), _outputs(h, w)
+    if m:
+        ids, logits = _teacher(n, V, m, g, kept)
+        kkm.kkm_distill_grad(ctx, h, w, ids, logits, dloss, *out, teacher_scale=0.9, **more)
+        t = torch.where(ids >= 0, logits.double() * 0.9, -torch.inf)
+        q = torch.softmax(t, 1).nan_to_num(0.0)
+    else:
+        kkm.kkm_head_grad(ctx, h, w, ids, dloss, *out, **more)
+        q = (ids >= 0).double()[:, None]
+        ids = ids[:, None]
+    loss, lse, dh, dw = out
+    # G in blocks of rows, in 64 bits on the GPU (plain products of two matrices)
+    wd = torch.where((off > -torch.inf)[:, None], w.double(), 0.0)
+    want_dw = torch.zeros(V, d, device="cuda", dtype=torch.float64)
+    size_dw = torch.zeros(V, d, device="cuda", dtype=torch.float64)
+    unit = ref.UNIT[h.dtype] if h.dtype != torch.float32 else 2 * ref.U
+    for i in range(0, n, 2048):
+        r = slice(i, min(i + 2048, n))
+        hd = h[r].double()
+        z = 0.7 * (hd @ wd.t().contiguous()) + off.double()
+        L = torch.logsumexp(z, 1)
+        has = q[r].sum(1) > 0
+        # an entry's error: a logit's, the sum's, one rounding to the operands' type
+        dz = (0.7 * (hd.abs() @ wd.abs().t().contiguous())).amax(1) * ref.sum_error(d, h.dtype) + 1e-5
+        assert bool(((lse[r].double() - L).abs() <= dz + (16 + V / 64) * 2 * ref.U * (1 + L.abs())).all())
+        c = torch.where(has, dloss[r].double(), 0.0)[:, None] * 0.7
+        G = torch.exp(z - L[:, None])
+        dG = G * (4 * dz[:, None] + (V / 64 + 32) * 2 * ref.U)
+        at = ids[r].long().clamp(min=0)
+        G.scatter_add_(1, at, -q[r])
+        dG.scatter_add_(1, at, 8 * ref.U * q[r])
+        G, dG = G * c, dG * c.abs() + (G * c).abs() * unit
+        dG = dG + ref.STEP[h.dtype] * dloss.abs().max() * 2.0 ** -12 * (c != 0)
+        G, dG = torch.where(c != 0, G, 0.0), torch.where(c != 0, dG, 0.0)
+        want, size = G @ wd, (dG + G.abs() * (ref.sum_error(V, h.dtype) + 40 * ref.U)) @ wd.abs()
+        assert bool(((dh[r].double() - want).abs() <= size + ref.UNIT[h.dtype] * want.abs() + ref.STEP[h.dtype]).all())
+        want_dw += G.t().contiguous() @ hd
+        size_dw += (dG + G.abs() * (ref.sum_error(n, h.dtype) + 40 * ref.U)).t().contiguous() @ hd.abs()
+    assert bool(((dw.double() - want_dw).abs() <= size_dw + ref.UNIT[h.dtype] * want_dw.abs() + ref.STEP[h.dtype]).all())
+    # one gradient alone, and the loss alone, have the same bits
+    b = _outputs(h, w)
+    if m:
+        kkm.kkm_distill_loss(ctx, h, w, ids, logits, *b[:2], teacher_scale=0.9, **more)
+        assert torch.equal(b[0], loss) and torch.equal(b[1], lse)
+        kkm.kkm_distill_grad(ctx, h, w, ids, logits, dloss, *b[:2], None, b[3], teacher_scale=0.9, **more)
+    else:
+        one = ids[:, 0].contiguous()
+        kkm.kkm_head_loss(ctx, h, w, one, *b[:2], **more)
+        assert torch.equal(b[0], loss) and torch.equal(b[1], lse)
+        kkm.kkm_head_grad(ctx, h, w, one, dloss, *b[:2], None, b[3], **more)
+    assert torch.equal(b[3], dw)
