@@ -538,10 +538,10 @@ int kkm_layer_norm_grad(kkm_ctx *ctx, int32_t type, int64_t n, int32_t d, const 
  * out: it has no probability, its row of w is not looked at (it may hold NaN)
  * and its gradient is zero.
  *
- * The logits of a large head are never stored: 256 x 256 of them at a time
- * leave their rows' largest and sum, and for the gradient they are computed
- * again, a piece of the classes at a time (G of a piece: at most 256 MB, or 256
- * classes).  fp32 operands are then taken as three bfloat16 parts, 24 bits
+ * Of a large head's logits at most 256 MB are stored: 256 x 256 of them at a
+ * time leave their rows' largest and sum, and for the gradient what was not kept
+ * is computed again, a piece of the classes at a time (G of a piece: at most 256
+ * MB, or 256 classes).  fp32 operands are then taken as three bfloat16 parts, 24 bits
  * together, and an infinite entry of theirs gives NaN.  A head of at most 64
  * classes or 64 rows, or of little work (at most 64 MB of logits), holds its
  * scores as fp32 scratch and multiplies fp32 as fp32. */

@@ -1,4 +1,5 @@
-// A class head's losses and their gradients, the logits never stored.
+// A class head's losses and their gradients, with at most 256 MB of the logits in
+// memory.
 //
 //   z(i, v) = scale h_i . w_v + offset_v,   lse_i = log sum_v exp z(i, v)
 //   loss_i = sum_j q_j (log q_j - z(i, id_j) + lse_i)      over the row's pairs (id_j, q_j)
@@ -230,9 +231,9 @@ struct ScoreArgs {
 // both orders at 3.4 TB/s.  bfloat16, 8192 rows of 4096: 32768 classes 1.83 ms, 1.20
 // PFLOP/s, matrix cores busy 62 % of the cycles (a library product of that shape
 // 1.41 PFLOP/s); with G, 16384 classes 1.07 ms, 1.02 PFLOP/s, 56 %.  fp32, 4000 rows
-// of 1000, 4000 classes: 158 us, 1.2 PFLOP/s of plane products; with G 196 us.  G of
-// kept logits is bound by memory and needs no LDS: 20011 binary16 classes of 1777
-// rows 82 us, 3.5 TB/s, where multiplying again takes 141.
+// of 1000, 4000 classes: 158 us, 1.2 PFLOP/s of plane products; with G 196 us, or 60
+// of kept logits.  G of kept logits is bound by memory and needs no LDS: 20011 binary16 classes of 1777
+// rows 79 to 82 us, 3.5 TB/s, where multiplying again takes 141.
 enum ScoresMode { SCORES_LOSS, SCORES_G, SCORES_G_OF_Z };
 template <typename E, class S, int P, int MODE>
 __global__ __launch_bounds__(S::threads, MODE == SCORES_G_OF_Z ? 2 : S::per_cu) void scores_kernel(ScoreArgs<E> a) {

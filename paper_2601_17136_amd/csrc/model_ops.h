@@ -55,7 +55,7 @@ constexpr int kMaxTop = 256;
 
 // How a head runs: FEW, at most kFew classes or rows, and DIRECT, little work on
 // more of both, straight from the rows (head_few.hip); TILED, matrix products of
-// copies in tiles, the logits never stored (head.hip).
+// copies in tiles, at most 256 MB of the logits stored (head.hip).
 enum HeadForm { HEAD_FEW, HEAD_DIRECT, HEAD_TILED };
 constexpr int kFew = 64;
 constexpr int64_t kDirectScores = (int64_t)16 << 20;  // n times classes: 64 MB of scores
