@@ -401,8 +401,14 @@ struct TargetArgs {
 // One wavefront per row: joins the tiles' sums, takes the targets' logits, and
 // writes loss and lse; for the gradient also the row's factor and its entries
 // of G at the targets.  Bound by gathering the targets' rows of w: 4096 rows of 2048
-// with 32 bfloat16 targets each (537 MB) 99 us, 5.4 TB/s.
-template <typename XT, int NQ>
+// with 32 bfloat16 targets each (537 MB) 99 us, 5.4 TB/s.  Every P lanes take four
+// targets at a time.  Of up to four targets a row's 64 lanes: the loss with ids at
+// P = 64 / 16, 20000 rows of 784, 1000 bfloat16 classes 74 / 87 us, 8192 of 4096, 4000
+// classes 238 / 263 (short rows differ by 3 %: 43373 of 35, 137 classes, 4 pairs 63 /
+// 61).  Of more, 16, or 8 for short rows: at 64 / 16, the 20000 rows with 16 pairs
+// 108 / 93, 49190 of 304, 217 classes, 10 pairs 98 / 75; at 64 / 8, 43373 of 35, 137
+// classes, 47 pairs 310 / 85.
+template <typename XT, int NQ, int P>
 __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -453,9 +459,11 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
 #pragma unroll
   for (int k = 0; k < NQ; ++k) q[k] *= inv;
 
-  // the targets' logits, four dot products at a time
+  // the targets' logits, four dot products at a time by each P lanes
+  constexpr int VEC = kVec<XT>, W = P * VEC, STEP = 4 * (64 / P);
+  const int part = lane % P, group = lane / P;
   const XT* hr = (const XT*)a.h + i * a.ldh;
-  for (int j0 = 0; j0 < a.m; j0 += 4) {
+  for (int j0 = 0; j0 < a.m; j0 += STEP) {
     const XT* wr[4];
     int idj[4];
     bool any = false;
@@ -464,13 +472,12 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
       idj[u] = -1;
 #pragma unroll
       for (int k = 0; k < NQ; ++k)
-        if (j0 / 64 == k) idj[u] = __shfl(id[k], (j0 + u) & 63, 64);  // (4 divides 64: one k for all four)
+        if (j0 / 64 == k) idj[u] = __shfl(id[k], (j0 + 4 * group + u) & 63, 64);  // (STEP divides 64: one k for all)
       any |= idj[u] >= 0;
       wr[u] = (const XT*)a.w + (int64_t)max(idj[u], 0) * a.ldw;
     }
-    if (!any) continue;
+    if (!__any(any)) continue;
     // (a pair that is none reads row 0 of w, and its sum is not used)
-    constexpr int VEC = kVec<XT>, W = 64 * VEC;
     float dot[4] = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](const raw_vec<XT>& hv, const raw_vec<XT> (&wv)[4]) {
 #pragma unroll
@@ -478,7 +485,7 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) dot[u] = fmaf((float)hv[e], (float)wv[u][e], dot[u]);
     };
-    int c = lane * VEC;
+    int c = part * VEC;
 #pragma unroll 4
     for (int c0 = 0; c0 + W <= a.d; c0 += W, c += W) {
       raw_vec<XT> wv[4];
@@ -492,14 +499,23 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
       for (int u = 0; u < 4; ++u) wv[u] = load_raw(wr[u], c, a.d);
       add(load_raw(hr, c, a.d), wv);
     }
+    const int mine = (lane - j0) & 63;  // this lane's pair among the STEP
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      if (idj[u] < 0) continue;
-      const float off = a.offset ? a.offset[idj[u]] * kLog2e : 0.f;
-      const float zz = off == -INFINITY ? -INFINITY : fmaf(wave_sum(dot[u]), a.scale * kLog2e, off);
+      if (!__any(idj[u] >= 0)) continue;
+      float sum = dot[u];
+      if constexpr (P == 64) {
+        sum = wave_sum(sum);
+      } else {
+#pragma unroll
+        for (int o = P / 2; o; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      }
+      const float off = a.offset && idj[u] >= 0 ? a.offset[idj[u]] * kLog2e : 0.f;
+      float zz = off == -INFINITY ? -INFINITY : fmaf(sum, a.scale * kLog2e, off);
+      if constexpr (P < 64) zz = __shfl(zz, (mine / 4 * P) & 63, 64);
 #pragma unroll
       for (int k = 0; k < NQ; ++k)
-        if (j0 / 64 == k && lane == ((j0 + u) & 63)) z[k] = zz;
+        if (j0 / 64 == k && mine < STEP && mine % 4 == u) z[k] = zz;
     }
   }
   float l = 0.f;
@@ -1034,10 +1050,16 @@ struct Head {
       }
     }
     const dim3 tg((unsigned)cdiv(a.n, 4));
-    if (a.m <= 64)
-      hipLaunchKernelGGL((targets_kernel<XT, 1>), tg, dim3(256), 0, s, ta);
-    else
-      hipLaunchKernelGGL((targets_kernel<XT, 4>), tg, dim3(256), 0, s, ta);
+    auto targets = [&](auto P_) {
+      constexpr int TP = decltype(P_)::value;
+      if (a.m <= 64)
+        hipLaunchKernelGGL((targets_kernel<XT, 1, TP>), tg, dim3(256), 0, s, ta);
+      else
+        hipLaunchKernelGGL((targets_kernel<XT, 4, TP>), tg, dim3(256), 0, s, ta);
+    };
+    if (a.m <= 4) targets(std::integral_constant<int, 64>{});
+    else if (a.d <= 8 * kVec<XT>) targets(std::integral_constant<int, 8>{});
+    else targets(std::integral_constant<int, 16>{});
     KKM_TRY(hipGetLastError());
     if (!grad) return hipSuccess;
 

@@ -596,3 +596,11 @@ def test_head_of_more_logits_than_are_kept(ctx, n, d, V, m, dtype):
         assert torch.equal(b[0], loss) and torch.equal(b[1], lse)
         kkm.kkm_head_grad(ctx, h, w, one, dloss, *b[:2], None, b[3], **more)
     assert torch.equal(b[3], dw)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,V,m", [(2500, 8, 9000, 4), (2500, 33, 3000, 5), (2100, 64, 2100, 33), (2100, 65, 2100, 64),
+                                     (1500, 127, 2000, 65), (1400, 300, 1400, 17), (900, 1025, 1500, 100),
+                                     (2500, 20, 9001, 256)])
+def test_distill_of_many_pairs_of_short_and_long_rows(ctx, n, d, V, m, dtype):
+    test_distill(ctx, n, d, V, m, dtype)
