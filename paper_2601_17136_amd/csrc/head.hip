@@ -401,7 +401,7 @@ struct TargetArgs {
 // One wavefront per row: joins the tiles' sums, takes the targets' logits, and
 // writes loss and lse; for the gradient also the row's factor and its entries
 // of G at the targets.  Bound by gathering the targets' rows of w: 4096 rows of 2048
-// with 32 bfloat16 targets each (537 MB) 99 us, 5.4 TB/s.  Every P lanes take four
+// with 32 bfloat16 targets each (537 MB) 85 us, 6.3 TB/s.  Every P lanes take four
 // targets at a time.  Of up to four targets a row's 64 lanes: the loss with ids at
 // P = 64 / 16, 20000 rows of 784, 1000 bfloat16 classes 74 / 87 us, 8192 of 4096, 4000
 // classes 238 / 263 (short rows differ by 3 %: 43373 of 35, 137 classes, 4 pairs 63 /
