@@ -39,14 +39,32 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr size_t kPieceBytes = (size_t)256 << 20;
-constexpr int kMaxParts = 64;          // workgroups that look for the largest dloss
-constexpr float kHalfScale = 16384.f;  // binary16 G: probabilities to 4e-9 keep all their bits
 
-__device__ inline float pow2_at_least(float v) {  // v >= 0, or infinite or NaN
-  if (!(v > 0.f) || isinf(v)) return v;
+// Binary16 has no room for weights (dloss) of every size, so each row has its own
+// power of two: G is held for a weight of 2^13 to 2^14 whatever the row's is (a
+// probability to 4e-9 keeps all its bits), and dH's rows are put right as they
+// are stored.  dW sums over the rows: its copy of h takes the row's power, with
+// the largest entry of all rows (weight times largest feature, the row's level)
+// just below 2^15.  A row's features then keep their bits down to 2^-29 of that entry.
+constexpr int kHalfG = 14, kHalfH = 15;
+// Words that share the search for the highest level, each in a cache line of its
+// own: an atomic a row on one line took 40000 rows of 256 with 1000 classes 150 us.
+constexpr int kLevels = 64, kLevelStep = 32, kLevelBias = 1024;
+
+typedef unsigned short shorts8 __attribute__((ext_vector_type(8)));
+
+__device__ inline int exponent_of(float v) {  // |v| in [1/2, 1) 2^e; 0 of 0, infinities and NaN
+  if (v == 0.f || !isfinite(v)) return 0;
   int e;
-  const float m = frexpf(v, &e);
-  return ldexpf(1.f, m == 0.5f ? e - 1 : e);
+  (void)frexpf(v, &e);
+  return e;
+}
+// The words' highest, for a whole wavefront; 0 where no row has one.
+__device__ inline int top_level(const unsigned* __restrict__ level) {
+  unsigned m = level[(threadIdx.x & (kLevels - 1)) * kLevelStep];
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o, 64));
+  return m ? (int)m - kLevelBias : 0;
 }
 
 // ------------------------------------------------------------------ operands
@@ -72,10 +90,14 @@ struct StageJob {
   const float* weight;  // transposed copies: rows of weight `none` are zero; may be null
   float none;
   int64_t rp;           // their width
+  const float* dloss;   // binary16's h: rows take their weights' powers of two; null: none
 };
 struct StageJobs {
   StageJob j[2];
   unsigned split;
+  const unsigned* level;  // with dloss: the words of top_level
+  float scale;
+  float* alpha;           // takes what dW's sums are multiplied by
 };
 
 // Rows in place of src's, kp wide (zero from d on), as P planes.  A thread
@@ -126,12 +148,25 @@ __global__ __launch_bounds__(256) void stage_cols_kernel(StageJobs jobs, int d) 
   const int64_t r0 = (int64_t)(blockIdx.x - (second ? jobs.split : 0u)) * 64, rows = j.rows, ld = j.ld, rp = j.rp,
                 plane = j.plane;
   const int c0 = blockIdx.y * 64, col = (threadIdx.x % LANES) * VEC;
+  int top = 0;
+  if (std::is_same<XT, half_t>::value && j.dloss) {
+    top = top_level(jobs.level);
+    if (blockIdx.x == 0 && c0 == 0 && threadIdx.x == 0) *jobs.alpha = ldexpf(jobs.scale, top - kHalfG - kHalfH);
+  }
 #pragma unroll
   for (int k = 0; k < 64 / PASS; ++k) {
     const int rr = k * PASS + threadIdx.x / LANES;
     const int64_t row = r0 + rr;
     const bool use = row < rows && !(j.weight && j.weight[row] == j.none);
-    const raw_vec<XT> v = load_raw(src + (use ? row : 0) * ld, c0 + col, use ? d : 0);
+    raw_vec<XT> v = load_raw(src + (use ? row : 0) * ld, c0 + col, use ? d : 0);
+    if constexpr (std::is_same<XT, half_t>::value) {
+      if (j.dloss && use) {
+        // (a row that set no level has zeros, or is NaN in any case)
+        const float f = ldexpf(1.f, min(exponent_of(j.dloss[row]) + kHalfH - top, 64));
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = (XT)((float)v[e] * f);
+      }
+    }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) tile[rr][col + e] = v[e];
   }
@@ -185,23 +220,6 @@ __device__ inline void swap_halves(unsigned a, unsigned b, unsigned& lo, unsigne
   hi = r[1];
 }
 
-// Largest |dloss| of a workgroup's share of the rows (binary16: G is kept in its range).
-__device__ inline void max_dloss(const float* __restrict__ dloss, int64_t n, unsigned* __restrict__ parts,
-                                 unsigned count, unsigned* red) {
-  unsigned m = 0u;  // ordered as the floats are, NaN above all
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)count * blockDim.x)
-    m = max(m, __float_as_uint(dloss[i]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o, 64));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (unsigned w = 1; w < blockDim.x / 64; ++w) m = max(m, red[w]);
-    parts[blockIdx.x] = m;
-  }
-  __syncthreads();
-}
-
 template <typename E>
 struct ScoreArgs {
   Side w, h;
@@ -210,9 +228,7 @@ struct ScoreArgs {
   int K, nkc, nseg, mt, nt;
   float zscale;         // scale log2 e
   const float* offset;  // may be null
-  const float* dloss;   // forward: the first nparts workgroups leave their rows' largest here; may be null
-  unsigned* dparts;
-  unsigned nparts;
+  unsigned* level;      // forward: cleared for targets_kernel; may be null
   float2* part;         // forward: (largest, sum) in base 2 of each class tile and row, [tile][n]
   floatx4* z;           // logits in base 2 of the first `kept` class tiles, in the order of the tiles' lanes,
   int kept;             // written forward, read for G
@@ -239,7 +255,7 @@ template <typename E, class S, int P, int MODE>
 __global__ __launch_bounds__(S::threads, MODE == SCORES_G_OF_Z ? 2 : S::per_cu) void scores_kernel(ScoreArgs<E> a) {
   constexpr bool GRAD = MODE != SCORES_LOSS;
   __shared__ __attribute__((aligned(1024))) char lds[MODE == SCORES_G_OF_Z ? 16 : S::lds_bytes];
-  if (!GRAD && a.dloss && blockIdx.x < a.nparts) max_dloss(a.dloss, a.n, a.dparts, a.nparts, (unsigned*)lds);
+  if (!GRAD && a.level && blockIdx.x == 0 && threadIdx.x < kLevels) a.level[threadIdx.x * kLevelStep] = 0u;
   int mi, ni;
   tile_of(blockIdx.x, gridDim.x, a.mt, a.nt, mi, ni);
   const int64_t c0 = a.v0 + (int64_t)mi * S::BM, t0 = (int64_t)ni * S::BN;
@@ -391,9 +407,8 @@ struct TargetArgs {
   float *loss, *lse;
   // gradient
   const float* dloss;
-  const unsigned* dparts;  // null: G holds dloss as it is
-  unsigned nparts;
-  float *lse2, *coef, *alpha;
+  unsigned* level;  // the words of top_level; null: G holds dloss as it is
+  float *lse2, *coef, *alpha;  // alpha: what a row of dH's sums is multiplied by, beside level
   int32_t* fix_id;  // n x m
   float* fix_val;
 };
@@ -463,6 +478,7 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
   constexpr int VEC = kVec<XT>, W = P * VEC, STEP = 4 * (64 / P);
   const int part = lane % P, group = lane / P;
   const XT* hr = (const XT*)a.h + i * a.ldh;
+  shorts8 largest = {};  // of the row's binary16 features
   for (int j0 = 0; j0 < a.m; j0 += STEP) {
     const XT* wr[4];
     int idj[4];
@@ -480,6 +496,8 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
     // (a pair that is none reads row 0 of w, and its sum is not used)
     float dot[4] = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](const raw_vec<XT>& hv, const raw_vec<XT> (&wv)[4]) {
+      if constexpr (std::is_same<XT, half_t>::value)  // (without their signs halves are ordered as their bits)
+        largest = __builtin_elementwise_max(largest, __builtin_bit_cast(shorts8, hv) & (unsigned short)0x7fff);
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -531,14 +549,22 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
     a.lse[i] = lse2 * kLn2;
   }
   if (!a.coef) return;
-  float cf = a.dloss[i] * a.scale;
-  if (a.dparts) {
-    unsigned mx = lane < (int)a.nparts ? a.dparts[lane] : 0u;
+  const float dl = a.dloss[i];
+  float cf = dl * a.scale;
+  if (a.level) {
+    const int e = exponent_of(dl);
+    if (cf != 0.f) cf = ldexpf(dl, kHalfG - e);
+    int bits = __builtin_reduce_max(largest);
 #pragma unroll
-    for (int o = 32; o; o >>= 1) mx = max(mx, (unsigned)__shfl_xor((int)mx, o, 64));
-    const float D = pow2_at_least(__uint_as_float(mx));
-    cf = D == 0.f ? 0.f : a.dloss[i] / D * kHalfScale;
-    if (i == 0 && lane == 0) *a.alpha = D / kHalfScale * a.scale;
+    for (int o = 32; o; o >>= 1) bits = max(bits, __shfl_xor(bits, o, 64));
+    if (lane == 0) {
+      const float most = (float)__builtin_bit_cast(half_t, (unsigned short)bits);
+      a.alpha[i] = ldexpf(a.scale, e - kHalfG);
+      // (a row of none of these is 0 or NaN, whatever its level)
+      if (some && !bad && cf != 0.f && isfinite(cf) && isfinite(lse2) && most > 0.f && isfinite(most))
+        atomicMax(&a.level[(blockIdx.x & (kLevels - 1)) * kLevelStep],
+                  (unsigned)(e + exponent_of(most) + kLevelBias));
+    }
   }
   if (!some || lse2 == -INFINITY) cf = 0.f;
   if (bad) cf = __builtin_nanf("");
@@ -606,6 +632,7 @@ struct ProductArgs {
   void* out;
   int64_t ldo;
   const float* alpha;   // null: 1
+  int each;             // alpha holds one for each row
   const float* coef;    // rows of weight 0 are 0, whatever stands in b; null: none
 };
 // The two products of a piece run in one launch where their tiles are alike.
@@ -632,7 +659,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductJ
   tile_product<E, S>(a.a, a.b, r0, n0, a.K, a.nkc, a.nseg, c0, c1, lds, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
-  const float alpha = a.alpha ? *a.alpha : 1.f;
+  float alpha = a.alpha && !a.each ? *a.alpha : 1.f;
   float* slab = a.slabs ? a.slabs + (int64_t)sl * a.M * a.N : nullptr;
 #pragma unroll
   for (int bi = 0; bi < S::WM; ++bi)
@@ -641,6 +668,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductJ
       const int64_t row = r0 + (wm * S::WM + bi) * 32 + acc_row(r, h);
       if (row >= a.M) continue;
       const bool none = !slab && a.coef && a.coef[row] == 0.f;
+      if (!slab && a.each) alpha = a.alpha[row];
 #pragma unroll
       for (int bj = 0; bj < S::WN; ++bj) {
         const int64_t col = n0 + (wn * S::WN + bj) * 32 + l32;
@@ -661,7 +689,9 @@ struct SlabJob {
   const float* slabs;
   int count;
   int64_t M, N;
-  const float *alpha, *coef;
+  const float* alpha;  // as ProductArgs'
+  int each;
+  const float* coef;
   void* out;
   int64_t ldo;
   unsigned blocks;
@@ -692,7 +722,7 @@ __global__ __launch_bounds__(256) void slabs_kernel(SlabJobs jobs) {
       for (int e = 0; e < m; ++e) s[e] += p[e];
     }
   }
-  const float f = alpha ? *alpha : 1.f;
+  const float f = alpha ? alpha[j.each ? row : 0] : 1.f;
   const bool none = coef && coef[row] == 0.f;
   typedef OT o4 __attribute__((ext_vector_type(4)));
   typedef o4 any4 __attribute__((aligned(alignof(OT))));
@@ -864,7 +894,7 @@ struct HeadPlan {
   int sh, sw;           // slabs of dH and dW (0: none)
   bool bigh, bigw;
   // workspace offsets
-  size_t h, w, part, z, ht, wt, lse2, coef, dparts, alpha, fix_id, fix_val, G, Gt, slabs_h, slabs_w, bytes;
+  size_t h, w, part, z, ht, wt, lse2, coef, level, alpha, alpha_w, fix_id, fix_val, G, Gt, slabs_h, slabs_w, bytes;
 };
 
 HeadPlan plan_of(const HeadArgs& a, bool grad) {
@@ -892,8 +922,11 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
     p.wt = take((size_t)p.planes * a.d * p.v_pad * 2);
     p.lse2 = take((size_t)a.n * 4);
     p.coef = take((size_t)a.n * 4);
-    p.dparts = take(kMaxParts * 4);
-    p.alpha = take(4);
+    if (a.type == TYPE_F16) {
+      p.level = take(kLevels * kLevelStep * 4);
+      p.alpha = take((size_t)a.n * 4);
+      p.alpha_w = take(4);
+    }
     p.fix_id = take((size_t)a.n * a.m * 4);
     p.fix_val = take((size_t)a.n * a.m * 4);
     p.G = take((size_t)p.planes * p.n_pad * p.piece * 2);
@@ -938,7 +971,7 @@ struct Head {
   Side side(const void* src, int64_t ld, int64_t rows, size_t off, StageJobs& jobs, int& count) const {
     if (in_place(a, src, ld)) return {src, ld, 0, rows};
     const int64_t plane = rows * p.kp;
-    jobs.j[count] = {src, ld, rows, at<E>(off), plane, nullptr, 0.f, 0};
+    jobs.j[count] = {src, ld, rows, at<E>(off), plane, nullptr, 0.f, 0, nullptr};
     const unsigned blocks = (unsigned)cdiv(rows * (p.kp / 8), 256);
     if (count++ == 0) jobs.split = blocks;
     return {at<E>(off), p.kp, plane, rows};
@@ -951,7 +984,6 @@ struct Head {
     sa.mt = (int)cdiv(classes, big ? BigTile::BM : SmallTile::BM);
     sa.nt = (int)cdiv(a.n, big ? BigTile::BN : SmallTile::BN);
     const dim3 grid((unsigned)((int64_t)sa.mt * sa.nt));
-    sa.nparts = std::min((unsigned)kMaxParts, grid.x);
     if (big)
       hipLaunchKernelGGL((scores_kernel<E, BigTile, P, MODE>), grid, dim3(BigTile::threads), 0, s, sa);
     else
@@ -971,7 +1003,7 @@ struct Head {
   // out (M x N) = A B^T over K, or its slabs where there are any (K0: the first
   // piece's K, from which the slabs' shares are)
   ProductArgs product(Side x, Side y, int64_t M, int64_t N, int K, int K0, bool big, int slabs, float* slab, int add,
-                      void* out, int64_t ldo, const float* alpha, const float* coef) const {
+                      void* out, int64_t ldo, const float* alpha, int each, const float* coef) const {
     ProductArgs pa{};
     pa.a = x;
     pa.b = y;
@@ -989,6 +1021,7 @@ struct Head {
     pa.out = out;
     pa.ldo = ldo;
     pa.alpha = alpha;
+    pa.each = alpha && each;
     pa.coef = coef;
     return pa;
   }
@@ -1000,9 +1033,9 @@ struct Head {
       hipLaunchKernelGGL((product_kernel<E, XT, SmallTile>), grid, dim3(SmallTile::threads), 0, s, jobs);
     return hipGetLastError();
   }
-  SlabJob sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, const float* coef, void* out,
-              int64_t ldo) const {
-    return {slabs, count, M, N, alpha, coef, out, ldo, (unsigned)cdiv(M * cdiv(N, 4), 256)};
+  SlabJob sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, int each, const float* coef,
+              void* out, int64_t ldo) const {
+    return {slabs, count, M, N, alpha, each, coef, out, ldo, (unsigned)cdiv(M * cdiv(N, 4), 256)};
   }
 
   hipError_t run(bool grad) const {
@@ -1023,10 +1056,8 @@ struct Head {
     sa.zscale = a.scale * kLog2e;
     sa.offset = a.offset;
     sa.part = at<float2>(p.part);
-    if (grad && a.type == TYPE_F16) {
-      sa.dloss = a.dloss;
-      sa.dparts = at<unsigned>(p.dparts);
-    }
+    const bool half = grad && a.type == TYPE_F16;
+    if (half) sa.level = at<unsigned>(p.level);
     if (grad) {
       sa.z = at<floatx4>(p.z);
       sa.kept = p.kept;
@@ -1034,19 +1065,16 @@ struct Head {
     KKM_TRY(scores<SCORES_LOSS>(sa, a.classes));
 
     TargetArgs ta{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, p.ntiles, a.scale, a.tscale, a.offset,
-                  a.ids, a.tlogits, sa.part, a.loss, a.lse, nullptr, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr};
-    const float* alpha = nullptr;
+                  a.ids, a.tlogits, sa.part, a.loss, a.lse, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
     if (grad) {
       ta.dloss = a.dloss;
       ta.lse2 = at<float>(p.lse2);
       ta.coef = at<float>(p.coef);
       ta.fix_id = at<int32_t>(p.fix_id);
       ta.fix_val = at<float>(p.fix_val);
-      if (a.type == TYPE_F16) {
-        ta.dparts = at<unsigned>(p.dparts);
+      if (half) {
+        ta.level = sa.level;
         ta.alpha = at<float>(p.alpha);
-        alpha = ta.alpha;
-        ta.nparts = (unsigned)std::min<int64_t>(kMaxParts, tile_count(a.classes, a.n, p.big));
       }
     }
     const dim3 tg((unsigned)cdiv(a.n, 4));
@@ -1065,11 +1093,17 @@ struct Head {
 
     Side ht{at<E>(p.ht), p.n_pad, (int64_t)a.d * p.n_pad, a.d}, wt{at<E>(p.wt), p.v_pad, (int64_t)a.d * p.v_pad, a.d};
     StageJobs turned{};
+    const float* alpha_w = half ? at<float>(p.alpha_w) : nullptr;
     if (a.dw) {
-      turned.j[0] = {a.h, a.ldh, a.n, at<E>(p.ht), ht.plane, ta.coef, 0.f, p.n_pad};
+      if (half) {
+        turned.level = ta.level;
+        turned.scale = a.scale;
+        turned.alpha = at<float>(p.alpha_w);
+      }
+      turned.j[0] = {a.h, a.ldh, a.n, at<E>(p.ht), ht.plane, ta.coef, 0.f, p.n_pad, half ? a.dloss : nullptr};
       turned.split = (unsigned)cdiv(a.n, 64);
     }
-    if (a.dh) turned.j[1] = {a.w, a.ldw, a.classes, at<E>(p.wt), wt.plane, a.offset, -INFINITY, p.v_pad};
+    if (a.dh) turned.j[1] = {a.w, a.ldw, a.classes, at<E>(p.wt), wt.plane, a.offset, -INFINITY, p.v_pad, nullptr};
     hipLaunchKernelGGL((stage_cols_kernel<XT, E, P>),
                        dim3(turned.split + (a.dh ? (unsigned)cdiv(a.classes, 64) : 0u), (unsigned)cdiv(a.d, 64)),
                        dim3(256), 0, s, turned, a.d);
@@ -1111,17 +1145,18 @@ struct Head {
         Side wv = wt;
         wv.p = at<E>(p.wt) + v0;
         ph = product({sa.G, sa.ldg, sa.planeg, p.n_pad}, wv, a.n, a.d, kv, kv0, p.bigh, p.sh, at<float>(p.slabs_h),
-                     v0 > 0, a.dh, a.lddh, alpha, ta.coef);
+                     v0 > 0, a.dh, a.lddh, ta.alpha, 1, ta.coef);
         if (p.sh && v0 + p.piece >= a.classes)
-          sums.j[n_sums++] = sum(at<float>(p.slabs_h), written(kv0, p.bigh, p.sh), a.n, a.d, alpha, ta.coef, a.dh,
-                                 a.lddh);
+          sums.j[n_sums++] = sum(at<float>(p.slabs_h), written(kv0, p.bigh, p.sh), a.n, a.d, ta.alpha, 1, ta.coef,
+                                 a.dh, a.lddh);
       }
       if (a.dw) {
         XT* dw = (XT*)a.dw + (int64_t)v0 * a.lddw;
         pw = product({sa.Gt, sa.ldt, sa.planet, p.piece}, ht, cnt, a.d, kn, kn, p.bigw, p.sw, at<float>(p.slabs_w), 0,
-                     dw, a.lddw, alpha, nullptr);
+                     dw, a.lddw, alpha_w, 0, nullptr);
         if (p.sw)
-          sums.j[n_sums++] = sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha, nullptr, dw, a.lddw);
+          sums.j[n_sums++] = sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha_w, 0, nullptr,
+                                 dw, a.lddw);
       }
       if (a.dh && a.dw && p.bigh == p.bigw) {
         KKM_TRY(multiply({{ph, pw}}, p.bigh));
