@@ -584,7 +584,7 @@ typedef struct kkm_teacher {
   const int32_t *ids;
   const float *logits;
   int32_t m;
-  float scale; /* 1 / temperature */
+  float scale; /* 1 / temperature; 0: every pair alike */
 } kkm_teacher;
 
 /* Distillation: loss_i = sum_j q_j (log q_j - z(i, id_j) + lse_i), the

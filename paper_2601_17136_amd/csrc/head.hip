@@ -29,6 +29,7 @@
 // stands there (an infinity, a NaN) reaches a sum.
 #include <algorithm>
 
+#include "head_pairs.h"
 #include "head_tile.h"
 #include "model_ops.h"
 
@@ -449,13 +450,8 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
 #pragma unroll
   for (int k = 0; k < NQ; ++k) {
     const int j = k * 64 + lane;
-    id[k] = j < a.m ? a.ids[i * a.m + j] : -1;
-    q[k] = id[k] < 0 ? -INFINITY : a.tlogits ? a.tscale * a.tlogits[i * a.m + j] : 0.f;
-    if (q[k] == -INFINITY) id[k] = -1;
-    if (id[k] >= a.classes) {
-      id[k] = -1;
-      bad = true;
-    }
+    id[k] = -1;
+    q[k] = j < a.m ? pair_key(a.ids, a.tlogits, i * a.m + j, a.tscale, a.classes, id[k], bad) : -INFINITY;
     tm = fmaxf(tm, q[k]);
     z[k] = 0.f;
   }
@@ -465,7 +461,7 @@ __global__ __launch_bounds__(256) void targets_kernel(TargetArgs a) {
   if (tm == -INFINITY) tm = 0.f;
 #pragma unroll
   for (int k = 0; k < NQ; ++k) {
-    q[k] = id[k] < 0 ? 0.f : expf(q[k] - tm);
+    q[k] = id[k] < 0 ? 0.f : pair_weight(q[k], tm, a.tscale);
     ts += q[k];
   }
   ts = wave_sum(ts);

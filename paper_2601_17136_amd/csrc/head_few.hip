@@ -19,6 +19,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "head_pairs.h"
 #include "model_ops.h"
 #include "vec_io.h"
 
@@ -132,15 +133,8 @@ __device__ inline float near_max(float v) {
   return v;
 }
 __device__ inline float safe(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ inline float pair_logit(const FewArgs& a, int64_t at, int& id, bool& bad) {
-  id = a.ids[at];
-  const float t = id < 0 ? -INFINITY : a.tlogits ? a.tscale * a.tlogits[at] : 0.f;
-  if (t == -INFINITY) id = -1;
-  if (id >= a.classes) {
-    id = -1;
-    bad = true;
-  }
-  return id < 0 ? -INFINITY : t;
+__device__ inline float pair_key(const FewArgs& a, int64_t at, int& id, bool& bad) {
+  return kkm::pair_key(a.ids, a.tlogits, at, a.tscale, a.classes, id, bad);
 }
 
 // Few classes: 32 rows of h by all classes; eight lanes finish a row, lane p
@@ -163,7 +157,7 @@ __global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void score
   const int pairs = here ? a.m : 0;
   int id0 = -1;
   bool bad = false;
-  const float p0 = p < pairs ? pair_logit(a, i * a.m + p, id0, bad) : -INFINITY;
+  const float p0 = p < pairs ? pair_key(a, i * a.m + p, id0, bad) : -INFINITY;
   const float dl = here && a.C ? a.dloss[i] : 0.f;
   scores_block<XT, CT, NT>(a, 0, t0, zs);
   float* z = zs[0][row];
@@ -182,12 +176,12 @@ __global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void score
   // the target: its largest logit, then its sum, then each pair
   float tm = p0, ts = 0.f, loss = 0.f;
   int id;
-  for (int j = p + 8; j < pairs; j += 8) tm = fmaxf(tm, pair_logit(a, i * a.m + j, id, bad));
+  for (int j = p + 8; j < pairs; j += 8) tm = fmaxf(tm, pair_key(a, i * a.m + j, id, bad));
   tm = safe(near_max<8>(tm));
-  ts = id0 < 0 ? 0.f : expf(p0 - tm);
+  ts = id0 < 0 ? 0.f : pair_weight(p0, tm, a.tscale);
   for (int j = p + 8; j < pairs; j += 8) {
-    const float t = pair_logit(a, i * a.m + j, id, bad);
-    ts += id < 0 ? 0.f : expf(t - tm);
+    const float t = pair_key(a, i * a.m + j, id, bad);
+    ts += id < 0 ? 0.f : pair_weight(t, tm, a.tscale);
   }
   ts = near_sum<8>(ts);
   bad = near_sum<8>(bad ? 1.f : 0.f) != 0.f;
@@ -197,8 +191,8 @@ __global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void score
     bool b;
     id = j0 ? -1 : id0;
     float t = p0;
-    if (j0 && j0 + p < pairs) t = pair_logit(a, i * a.m + j0 + p, id, b);
-    const float mine = id < 0 ? 0.f : expf(t - tm) * inv;
+    if (j0 && j0 + p < pairs) t = pair_key(a, i * a.m + j0 + p, id, b);
+    const float mine = id < 0 ? 0.f : pair_weight(t, tm, a.tscale) * inv;
     for (int o = 0; o < min(8, a.m - j0); ++o) {
       const int v = __shfl(id, o, 8);
       const float qj = __shfl(mine, o, 8);
@@ -341,9 +335,9 @@ __global__ __launch_bounds__(256) void targets_few_kernel(FewArgs a, int ntiles)
   int id = -1;
   bool bad = false;
   float t = -INFINITY;
-  if (tid < a.m) t = pair_logit(a, i * a.m + tid, id, bad);
+  if (tid < a.m) t = pair_key(a, i * a.m + tid, id, bad);
   const float tm = safe(all_max(t, 2));
-  const float e = id < 0 ? 0.f : expf(t - tm);
+  const float e = id < 0 ? 0.f : pair_weight(t, tm, a.tscale);
   const float ts = all_sum(e, 0);
   bad = all_sum(bad ? 1.f : 0.f, 1) != 0.f;
   const bool some = ts != 0.f;
@@ -687,7 +681,7 @@ __global__ __launch_bounds__(256) void row_direct_kernel(FewArgs a, int64_t ldz,
   for (int k = 0; k < NQ; ++k) {
     const int j = k * 64 + lane;
     id[k] = -1;
-    q[k] = j < a.m ? pair_logit(a, i * a.m + j, id[k], bad) : -INFINITY;
+    q[k] = j < a.m ? pair_key(a, i * a.m + j, id[k], bad) : -INFINITY;
     z[k] = id[k] >= 0 ? zr[id[k]] : 0.f;
     tm = fmaxf(tm, q[k]);
   }
@@ -720,7 +714,7 @@ __global__ __launch_bounds__(256) void row_direct_kernel(FewArgs a, int64_t ldz,
   tm = safe(near_max<64>(tm));
 #pragma unroll
   for (int k = 0; k < NQ; ++k) {
-    q[k] = id[k] < 0 ? 0.f : expf(q[k] - tm);
+    q[k] = id[k] < 0 ? 0.f : pair_weight(q[k], tm, a.tscale);
     ts += q[k];
   }
   ts = wave_sum(ts);
