@@ -5,8 +5,10 @@
 //
 // Both are bound by memory: x in and y out; x and dy in and dx out.  A row
 // lives in the registers of its T threads (a wavefront up to 4 vectors a lane,
-// then a workgroup of 256), so it is read once, and the variance is taken about
-// the mean.  A group goes over rows a grid apart and keeps its columns' w and b,
+// then a workgroup of 256), so it is read once.  The mean is taken twice: what the
+// first sum's rounding left of it is the mean of x - mu, summed beside the squares,
+// and both it and its square are taken off.  Rows of one value so have xh = 0;
+// with the first mean alone 1000 values of 30000 gave xh = -0.5.  A group goes over rows a grid apart and keeps its columns' w and b,
 // and in the gradient the fp32 sums of dw and db, in registers; a workgroup's
 // sums go to its line of the scratch, and a second launch adds the lines in
 // order, so the gradient's bits do not depend on timing.  Rows wider than the
@@ -61,6 +63,12 @@ __device__ inline float row_sum(float v, float (*red)[2][4], int& turn) {
   return v;
 }
 
+// 1 / sqrt(variance + eps) of squares about a mean that is off by `left`.
+__device__ inline float inverse_deviation(float squares, float left, float eps) {
+  const float var = squares - left * left;
+  return 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);  // (a NaN stays one)
+}
+
 // Forward, x read once: 20000 fp32 rows of 784 21 us, 5.9 TB/s of what it must read
 // and write; 16384 bfloat16 rows of 4096 44 us, 6.0 TB/s; 40001 binary16 rows of
 // 301 18 us, 2.6 TB/s (38 of a wavefront's 64 lanes have features there).
@@ -99,24 +107,27 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(const XT* __restri
     }
     if (row + step < n) fetch(row + step);
     const float mu = row_sum<T>(s, red, turn) * inv_d;
-    float q = 0.f;
+    float q = 0.f, left = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         v[j][e] = (j * T + t) * VEC + e < d ? v[j][e] - mu : 0.f;
         q = fmaf(v[j][e], v[j][e], q);
+        left += v[j][e];
       }
-    const float r = 1.f / sqrtf(row_sum<T>(q, red, turn) * inv_d + eps);
+    row_sums<T>(q, left, red, turn);
+    left *= inv_d;
+    const float r = inverse_deviation(q * inv_d, left, eps);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float o[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) o[e] = fmaf(v[j][e] * r, wv[j][e], bv[j][e]);
+      for (int e = 0; e < VEC; ++e) o[e] = fmaf((v[j][e] - left) * r, wv[j][e], bv[j][e]);
       store_part(y + row * ldy, (j * T + t) * VEC, d, o);
     }
     if (t == 0) {
-      if (mean) mean[row] = mu;
+      if (mean) mean[row] = mu + left;
       if (rstd) rstd[row] = r;
     }
   }
@@ -274,7 +285,7 @@ __global__ __launch_bounds__(kThreads) void layer_norm_wide_kernel(const XT* __r
   const float inv_d = 1.f / (float)d;
   for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
     const XT* xr = x + row * ldx;
-    float s = 0.f, q = 0.f, v[VEC];
+    float s = 0.f, q = 0.f, left = 0.f, v[VEC];
     for (int i = threadIdx.x * VEC; i < d; i += kThreads * VEC) {
       load_part(xr, i, d, v);
 #pragma unroll
@@ -287,20 +298,23 @@ __global__ __launch_bounds__(kThreads) void layer_norm_wide_kernel(const XT* __r
       for (int e = 0; e < VEC; ++e) {
         const float c = i + e < d ? v[e] - mu : 0.f;
         q = fmaf(c, c, q);
+        left += c;
       }
     }
-    const float r = 1.f / sqrtf(row_sum<256>(q, red, turn) * inv_d + eps);
+    row_sums<256>(q, left, red, turn);
+    left *= inv_d;
+    const float r = inverse_deviation(q * inv_d, left, eps);
     for (int i = threadIdx.x * VEC; i < d; i += kThreads * VEC) {
       float wv[VEC], bv[VEC];
       load_part(xr, i, d, v);
       load_beside<VEC>(w, i, d, 1.f, wv);
       load_beside<VEC>(b, i, d, 0.f, bv);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v[e] = fmaf((v[e] - mu) * r, wv[e], bv[e]);
+      for (int e = 0; e < VEC; ++e) v[e] = fmaf((v[e] - mu - left) * r, wv[e], bv[e]);
       store_part(y + row * ldy, i, d, v);
     }
     if (threadIdx.x == 0) {
-      if (mean) mean[row] = mu;
+      if (mean) mean[row] = mu + left;
       if (rstd) rstd[row] = r;
     }
   }
