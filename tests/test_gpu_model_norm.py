@@ -1,4 +1,5 @@
-"""Layer norm: rows of one value, whose differences from the mean are all rounding."""
+"""Layer norm: rows of one value, whose differences from the mean are all
+rounding, and more rows than a launch has groups for."""
 import pytest
 
 import model_reference as ref
@@ -47,3 +48,22 @@ def test_rows_of_one_value_in_16_bits(ctx, d, dtype):
     assert torch.equal(mean, values.float())
     left = (L * ref.U) ** 2 * values.abs().double() / eps ** 0.5
     assert bool((y.abs().double() <= (left * 1.01 + ref.STEP[t])[:, None]).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d", [(9001, 301), (5001, 784), (2500, 4096), (1100, 20000)])
+def test_more_rows_than_groups(ctx, n, d, dtype):
+    """Each group of lanes goes over several rows, the next on its way while one is summed."""
+    from paper_2601_17136_amd import kkm
+    t, g = DTYPES[dtype], _gen(n + d)
+    print(f"[gpu] layer norm n={n} d={d} {dtype}", flush=True)
+    x = (torch.randn(n, d, device="cuda", generator=g) * 2 + torch.randn(n, 1, device="cuda", generator=g) * 3).to(t)
+    dy = torch.randn(n, d, device="cuda", generator=g).to(t)
+    w, b = 1 + 0.3 * torch.randn(d, device="cuda", generator=g), torch.randn(d, device="cuda", generator=g)
+    y, dx, dw, db = torch.empty_like(x), torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    kkm.kkm_layer_norm(ctx, x, w, b, 1e-3, y, mean, rstd)
+    kkm.kkm_layer_norm_grad(ctx, x, w, dy, mean, rstd, dx, dw, db)
+    r = ref.layer_norm(x, w, b, 1e-3, dy)
+    for name, got in (("y", y), ("mean", mean), ("rstd", rstd), ("dx", dx), ("dw", dw), ("db", db)):
+        ref.check(name, got, r[name], r["tol_" + name])
