@@ -897,7 +897,8 @@ int build_impl(kkm_ctx* c, const float* X, int64_t n, int32_t d, int32_t kind, c
   const bool reuse = c->built && c->sz.n == n && c->d == d && c->mode == mode && c->kind == kind &&
                      c->storage == storage && (c->pc1 > 0) == panel && c->pr1 - c->pr0 == pr1 - pr0 &&
                      c->pc1 - c->pc0 == pc1 - pc0;
-  if (!reuse) free_build(c);
+  if (reuse) free_model(c);  // (every build gives that back)
+  else free_build(c);
 
   c->sz = sizes_for(n, d, mode);
   if (panel) {  // the block's columns: a multiple of kTile, so its tiles store whole
