@@ -502,8 +502,9 @@ int kkm_peak_mfma(kkm_ctx *ctx, int32_t iters, float *out, int32_t reps, float *
  * not touch a built K.  Their scratch belongs to the context: it is allocated
  * when a call needs more than an earlier one did (that call waits for the
  * device, so a call to be captured into a graph follows one of its sizes),
- * counts against the budget, and is given back by the next build and by
- * kkm_destroy.  Matrices are row-major with a row stride (ld, in elements) of at
+ * counts against the budget, and is given back by the next build, by
+ * kkm_destroy, and when an update or a seeding needs its room.  It takes nothing
+ * that a build holds: a call that finds no room fails.  Matrices are row-major with a row stride (ld, in elements) of at
  * least their width, at any alignment of their type; ids and fp32 vectors are
  * contiguous.  Outputs do not overlap inputs or each other except where said.
  * Every sum, statistic and softmax is held in fp32, and results are rounded

@@ -210,7 +210,9 @@ struct kkm_ctx {
   int *sd_bestc = nullptr, *sd_centers = nullptr;
   double* sd_bsum[2] = {nullptr, nullptr};
 
-  std::vector<Alloc> model_allocs;  // workspace of the model operators (model_capi.cpp); builds give it back
+  // Workspace of the model operators (model_capi.cpp); given back to builds, and
+  // when something of the engine's needs the room.
+  std::vector<Alloc> model_allocs;
 
   HostReport* report = nullptr;  // pinned host memory, from the first kkm_iterate or kkm_step on (may stay null)
   void* scratch = nullptr;  // this device's static scratch (kkm_iterate_noalloc)
@@ -274,6 +276,12 @@ void free_seed(kkm_ctx* c) {
   c->sd_bsum[0] = c->sd_bsum[1] = nullptr;
 }
 
+void free_model(kkm_ctx* c) {
+  if (c->model_allocs.empty()) return;
+  (void)hipStreamSynchronize(c->stream);
+  release(c, c->model_allocs);
+}
+
 size_t bytes_of(const std::vector<Alloc>& v) {
   size_t b = 0;
   for (const Alloc& a : v) b += a.bytes;
@@ -281,12 +289,18 @@ size_t bytes_of(const std::vector<Alloc>& v) {
 }
 
 // Gives back what the budget cannot hold beside so many more bytes, if that
-// makes the room: the seeding scratch (the next seeding makes it again), else
-// the split points, else both.
+// makes the room: the model operators' scratch (their next call makes it
+// again), then the seeding scratch (the next seeding does), else the split
+// points, else both.  For the operators' own scratch, only the seeding scratch:
+// on the fly an update without the split points is slower and has other bits.
 void make_room(kkm_ctx* c, size_t bytes, const std::vector<Alloc>& owner) {
   if (c->held + bytes <= c->budget) return;
+  const bool model = &owner == &c->model_allocs;
+  const size_t seed = &owner == &c->seed_allocs ? 0 : bytes_of(c->seed_allocs);
+  const size_t split = model ? 0 : bytes_of(c->split_allocs);
+  if (!model && c->held + bytes - bytes_of(c->model_allocs) <= c->budget + seed + split) free_model(c);
+  if (c->held + bytes <= c->budget) return;
   const size_t need = c->held + bytes - c->budget;
-  const size_t seed = &owner == &c->seed_allocs ? 0 : bytes_of(c->seed_allocs), split = bytes_of(c->split_allocs);
   if (seed + split < need) return;
   if (seed >= need || split < need) free_seed(c);
   if (seed < need) release_split(c);
@@ -299,7 +313,13 @@ int dalloc(kkm_ctx* c, void** p, size_t bytes, std::vector<Alloc>& owner, const 
     return fail(c, KKM_ERR_OOM, "%s needs %zu bytes; %zu of the %zu-byte budget already held", what,
                 bytes, c->held, c->budget);
   hipError_t e = hipMalloc(p, bytes);
-  if (e != hipSuccess && c->Xf) {  // once more without the split points
+  const bool model = &owner == &c->model_allocs;
+  if (e != hipSuccess && !model && !c->model_allocs.empty()) {  // once more without the operators' scratch
+    (void)hipGetLastError();
+    free_model(c);
+    e = hipMalloc(p, bytes);
+  }
+  if (e != hipSuccess && !model && c->Xf) {  // and without the split points
     (void)hipGetLastError();
     release_split(c);
     e = hipMalloc(p, bytes);
@@ -370,12 +390,6 @@ void free_hist(kkm_ctx* c) {
   c->iter_ws = 0;
   c->changed = nullptr;
   c->obj = nullptr;
-}
-
-void free_model(kkm_ctx* c) {
-  if (c->model_allocs.empty()) return;
-  (void)hipStreamSynchronize(c->stream);
-  release(c, c->model_allocs);
 }
 
 void free_build(kkm_ctx* c) {
@@ -557,6 +571,7 @@ int ensure_ws(kkm_ctx* c, int k, int iters) {
   if (c->k_ws != k) {
     free_ws(c);
     const size_t need = ws_bytes(c->wsz, k, c->mode) + (size_t)std::max(iters, 64) * 12 + 512;
+    if (c->held + need > c->budget) free_model(c);
     if (c->held + need > c->budget) {
       int rc = release_fix_list(c);
       if (rc) return rc;
