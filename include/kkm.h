@@ -501,16 +501,23 @@ int kkm_peak_mfma(kkm_ctx *ctx, int32_t iters, float *out, int32_t reps, float *
  * All of them are asynchronous on the context's stream, need no build, and do
  * not touch a built K.  Their scratch belongs to the context: it is allocated
  * when a call needs more than an earlier one did (that call waits for the
- * device, so a call to be captured into a graph follows one of its sizes),
- * counts against the budget, and is given back by the next build, by
+ * device), counts against the budget, and is given back by the next build, by
  * kkm_destroy, and when an update or a seeding needs its room.  It takes nothing
- * that a build holds: a call that finds no room fails.  Matrices are row-major with a row stride (ld, in elements) of at
+ * that a build holds: a call that finds no room fails.
+ *
+ * A graph holds the scratch's address.  A call to be captured follows one of its
+ * sizes (else KKM_ERR_STATE), and the graph may be replayed until the scratch
+ * goes or grows: until the context's next build, seeding, update of another k or
+ * of more iterations, larger operator, or kkm_destroy.  After any of these it
+ * writes to freed memory; capture it again.
+ *
+ * Matrices are row-major with a row stride (ld, in elements) of at
  * least their width, at any alignment of their type; ids and fp32 vectors are
  * contiguous.  Outputs do not overlap inputs or each other except where said.
  * Every sum, statistic and softmax is held in fp32, and results are rounded
  * once, to nearest even, to the type of the matrix they are written to.  Calls
  * give the same bits for the same inputs.  Errors: KKM_ERR_ARG, KKM_ERR_OOM
- * (scratch), KKM_ERR_HIP. */
+ * (scratch), KKM_ERR_STATE (capture), KKM_ERR_HIP. */
 typedef enum kkm_type { KKM_F32 = 0, KKM_F16 = 1, KKM_BF16 = 2 } kkm_type;
 #define KKM_MAX_TOP 256        /* pairs of a distillation target's row */
 #define KKM_MAX_FEATURES (1 << 20) /* d of these operators */

@@ -771,6 +771,11 @@ int ctx_fail(kkm_ctx* c, int code, const char* fmt, ...) {
 
 int ctx_workspace(kkm_ctx* c, size_t bytes, void** out) {
   if (c->model_allocs.empty() || c->model_allocs[0].bytes < bytes) {
+    // (memory cannot be freed or made while the stream is captured)
+    hipStreamCaptureStatus state = hipStreamCaptureStatusNone;
+    HIP_TRY(c, hipStreamIsCapturing(c->stream, &state), "capture status");
+    if (state != hipStreamCaptureStatusNone)
+      return fail(c, KKM_ERR_STATE, "the captured call needs %zu bytes of scratch: call it once before the capture", bytes);
     free_model(c);
     void* p = nullptr;
     int rc = dalloc(c, &p, bytes, c->model_allocs, "operator workspace");
