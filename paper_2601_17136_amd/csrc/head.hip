@@ -81,6 +81,11 @@ __device__ inline void split_planes(float x, E (&out)[P]) {
   }
 }
 
+// A launch's work-items are a 32-bit count: a job of more than so many workgroups
+// of 256 goes over its items with what it has.
+constexpr int64_t kMaxBlocks = (int64_t)1 << 22;
+constexpr int64_t kMaxItems = (int64_t)1 << 31;
+
 // A copy of h and one of w run in one launch: the first `split` workgroups are
 // the first job's.
 struct StageJob {
@@ -108,31 +113,33 @@ template <typename XT, typename E, int P>
 __global__ __launch_bounds__(256) void stage_rows_kernel(StageJobs jobs, int d, int kp) {
   const bool second = blockIdx.x >= jobs.split;
   const StageJob& j = jobs.j[second];
-  const int64_t per = kp / 8, i = (int64_t)(blockIdx.x - (second ? jobs.split : 0u)) * 256 + threadIdx.x;
-  if (i >= j.rows * per) return;
-  const int64_t row = i / per;
-  const int c = (int)(i - row * per) * 8;
-  const XT* src = (const XT*)j.src + row * j.ld;
-  float v[8];
-  if constexpr (sizeof(XT) == 2) {
-    load_part(src, c, d, v);
-  } else {
-    float a[4], b[4];
-    load_part(src, c, d, a);
-    load_part(src, c + 4, d, b);
+  const unsigned first = second ? jobs.split : 0u, blocks = second ? gridDim.x - first : min(jobs.split, gridDim.x);
+  const int64_t per = kp / 8, step = (int64_t)blocks * 256;
+  for (int64_t i = (int64_t)(blockIdx.x - first) * 256 + threadIdx.x; i < j.rows * per; i += step) {
+    const int64_t row = i / per;
+    const int c = (int)(i - row * per) * 8;
+    const XT* src = (const XT*)j.src + row * j.ld;
+    float v[8];
+    if constexpr (sizeof(XT) == 2) {
+      load_part(src, c, d, v);
+    } else {
+      float a[4], b[4];
+      load_part(src, c, d, a);
+      load_part(src, c + 4, d, b);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+      for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+    }
+    frag<E> o[P];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      E pl[P];
+      split_planes<E, P>(v[e], pl);
+#pragma unroll
+      for (int p = 0; p < P; ++p) o[p][e] = pl[p];
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) *(frag<E>*)((E*)j.dst + p * j.plane + row * kp + c) = o[p];
   }
-  frag<E> o[P];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    E pl[P];
-    split_planes<E, P>(v[e], pl);
-#pragma unroll
-    for (int p = 0; p < P; ++p) o[p][e] = pl[p];
-  }
-#pragma unroll
-  for (int p = 0; p < P; ++p) *(frag<E>*)((E*)j.dst + p * j.plane + row * kp + c) = o[p];
 }
 
 // The transposed copies: dst[c][row], rp rows wide (zero from `rows` on).  A
@@ -703,38 +710,41 @@ __global__ __launch_bounds__(256) void slabs_kernel(SlabJobs jobs) {
   OT* out = (OT*)j.out;
   const int count = j.count;
   const int64_t M = j.M, N = j.N, ldo = j.ldo;
-  const int64_t per = (N + 3) / 4, x = (int64_t)(blockIdx.x - (second ? jobs.j[0].blocks : 0u)) * 256 + threadIdx.x;
-  if (x >= M * per) return;
-  const int64_t row = x / per, c = (x - row * per) * 4;
-  const int m = (int)min((int64_t)4, N - c);
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < count; ++k) {
-    const float* p = slabs + (k * M + row) * N + c;
-    if (m == 4) {
-      const raw_vec<float> v = *(const any_vec<float>*)p;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += v[e];
-    } else {
-      for (int e = 0; e < m; ++e) s[e] += p[e];
-    }
-  }
-  const float f = alpha ? alpha[j.each ? row : 0] : 1.f;
-  const bool none = coef && coef[row] == 0.f;
+  const int64_t per = (N + 3) / 4, step = (int64_t)j.blocks * 256;
+  const float f = alpha && !j.each ? *alpha : 1.f;
   typedef OT o4 __attribute__((ext_vector_type(4)));
   typedef o4 any4 __attribute__((aligned(alignof(OT))));
-  o4 o;
+  const unsigned first = second ? jobs.j[0].blocks : 0u;
+  for (int64_t x = (int64_t)(blockIdx.x - first) * 256 + threadIdx.x; x < M * per; x += step) {
+    const int64_t row = x / per, c = (x - row * per) * 4;
+    const int m = (int)min((int64_t)4, N - c);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < count; ++k) {
+      const float* p = slabs + (k * M + row) * N + c;
+      if (m == 4) {
+        const raw_vec<float> v = *(const any_vec<float>*)p;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = (OT)(none ? 0.f : s[e] * f);
-  if (m == 4)
-    *(any4*)(out + row * ldo + c) = o;
-  else
-    for (int e = 0; e < m; ++e) out[row * ldo + c + e] = o[e];
+        for (int e = 0; e < 4; ++e) s[e] += v[e];
+      } else {
+        for (int e = 0; e < m; ++e) s[e] += p[e];
+      }
+    }
+    const float fr = j.each ? alpha[row] : f;
+    const bool none = coef && coef[row] == 0.f;
+    o4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (OT)(none ? 0.f : s[e] * fr);
+    if (m == 4)
+      *(any4*)(out + row * ldo + c) = o;
+    else
+      for (int e = 0; e < m; ++e) out[row * ldo + c + e] = o[e];
+  }
 }
 
 template <typename OT>
 __global__ __launch_bounds__(256) void zero_rows_kernel(OT* __restrict__ out, int64_t M, int64_t N, int64_t ldo) {
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (x < M * N) out[x / N * ldo + x % N] = (OT)0.f;
+  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < M * N; x += (int64_t)gridDim.x * 256)
+    out[x / N * ldo + x % N] = (OT)0.f;
 }
 
 // ------------------------------------------------------------------ plan
@@ -951,7 +961,7 @@ HeadPlan plan_of(const HeadArgs& a, bool grad) {
     if (e_ != hipSuccess) return e_;         \
   } while (0)
 
-inline dim3 grid1(int64_t items) { return dim3((unsigned)cdiv(items, 256)); }
+unsigned blocks_of(int64_t items) { return (unsigned)std::min(cdiv(items, 256), kMaxBlocks); }
 
 template <typename XT, typename E, int P>
 struct Head {
@@ -968,7 +978,7 @@ struct Head {
     if (in_place(a, src, ld)) return {src, ld, 0, rows};
     const int64_t plane = rows * p.kp;
     jobs.j[count] = {src, ld, rows, at<E>(off), plane, nullptr, 0.f, 0, nullptr};
-    const unsigned blocks = (unsigned)cdiv(rows * (p.kp / 8), 256);
+    const unsigned blocks = blocks_of(rows * (p.kp / 8));
     if (count++ == 0) jobs.split = blocks;
     return {at<E>(off), p.kp, plane, rows};
   }
@@ -1031,7 +1041,7 @@ struct Head {
   }
   SlabJob sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, int each, const float* coef,
               void* out, int64_t ldo) const {
-    return {slabs, count, M, N, alpha, each, coef, out, ldo, (unsigned)cdiv(M * cdiv(N, 4), 256)};
+    return {slabs, count, M, N, alpha, alpha && each, coef, out, ldo, blocks_of(M * cdiv(N, 4))};
   }
 
   hipError_t run(bool grad) const {
@@ -1041,7 +1051,7 @@ struct Head {
     sa.h = side(a.h, a.ldh, a.n, p.h, copies, count);
     sa.w = side(a.w, a.ldw, a.classes, p.w, copies, count);
     if (count) {
-      const unsigned rest = count > 1 ? (unsigned)cdiv(copies.j[1].rows * (p.kp / 8), 256) : 0u;
+      const unsigned rest = count > 1 ? blocks_of(copies.j[1].rows * (p.kp / 8)) : 0u;
       hipLaunchKernelGGL((stage_rows_kernel<XT, E, P>), dim3(copies.split + rest), dim3(256), 0, s, copies, a.d, p.kp);
       KKM_TRY(hipGetLastError());
     }
@@ -1058,7 +1068,15 @@ struct Head {
       sa.z = at<floatx4>(p.z);
       sa.kept = p.kept;
     }
-    KKM_TRY(scores<SCORES_LOSS>(sa, a.classes));
+    // (the classes whose logits are kept, 256 MB of them, lie in the first launch)
+    const int64_t side = p.big ? BigTile::BM : SmallTile::BM, threads = p.big ? BigTile::threads : SmallTile::threads;
+    const int64_t most = std::max<int64_t>(kMaxItems / (cdiv(a.n, side) * threads), 1) * side;
+    for (int64_t v0 = 0; v0 < a.classes; v0 += most) {
+      ScoreArgs<E> some = sa;
+      some.v0 = (int)v0;
+      if (v0) some.kept = 0;
+      KKM_TRY(scores<SCORES_LOSS>(some, std::min(most, a.classes - v0)));
+    }
 
     TargetArgs ta{a.h, a.w, a.ldh, a.ldw, a.n, a.d, a.classes, a.m, p.ntiles, a.scale, a.tscale, a.offset,
                   a.ids, a.tlogits, sa.part, a.loss, a.lse, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
@@ -1130,8 +1148,8 @@ struct Head {
         KKM_TRY(scores<SCORES_G>(rest, cnt - kept));
       }
       if (a.m > 1) {
-        hipLaunchKernelGGL((fix_kernel<E, P>), grid1(a.n * a.m), dim3(256), 0, s, ta.fix_id, ta.fix_val, a.n, a.m, v0,
-                           v0 + cnt, sa.G, sa.ldg, sa.planeg, sa.Gt, sa.ldt, sa.planet);
+        hipLaunchKernelGGL((fix_kernel<E, P>), dim3((unsigned)cdiv(a.n * a.m, 256)), dim3(256), 0, s, ta.fix_id,
+                           ta.fix_val, a.n, a.m, v0, v0 + cnt, sa.G, sa.ldg, sa.planeg, sa.Gt, sa.ldt, sa.planet);
         KKM_TRY(hipGetLastError());
       }
       ProductArgs ph{}, pw{};
@@ -1173,8 +1191,8 @@ template <typename XT, typename E, int P>
 hipError_t launch_typed(const HeadArgs& a, bool grad, void* scratch, hipStream_t s) {
   if (a.n == 0) {
     if (grad && a.dw) {
-      hipLaunchKernelGGL((zero_rows_kernel<XT>), grid1((int64_t)a.classes * a.d), dim3(256), 0, s, (XT*)a.dw,
-                         a.classes, a.d, a.lddw);
+      hipLaunchKernelGGL((zero_rows_kernel<XT>), dim3(blocks_of((int64_t)a.classes * a.d)), dim3(256), 0, s,
+                         (XT*)a.dw, a.classes, a.d, a.lddw);
       return hipGetLastError();
     }
     return hipSuccess;
