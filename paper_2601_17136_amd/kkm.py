@@ -508,15 +508,18 @@ def _rows(t, name, dtype=None, shape=None):
 
 
 class _Elsewhere:
-    """Work on the context's stream while torch's current stream is another: it
-    waits for what that stream has enqueued, that stream waits for it, and the
-    tensors' memory is held until then."""
+    """Work on the context's stream while torch's current stream of the tensors'
+    device is another: it waits for what that stream has enqueued, that stream
+    waits for it, and the tensors' memory is held until then (memory given as an
+    address is the caller's to keep)."""
 
     def __init__(self, handle, tensors):
         import torch
-        self.here = torch.cuda.current_stream()
-        self.there = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
-        self.tensors = [t for t in tensors if t is not None]
+        device = tensors[0].device
+        self.here = torch.cuda.current_stream(device)
+        self.there = (torch.cuda.ExternalStream(handle, device=device) if handle
+                      else torch.cuda.default_stream(device))
+        self.tensors = [t for t in tensors if t is not None and not isinstance(t, int)]
 
     def __enter__(self):
         self.there.wait_stream(self.here)
