@@ -544,7 +544,9 @@ int kkm_layer_norm_grad(kkm_ctx *ctx, int32_t type, int64_t n, int32_t d, const 
  * `classes` rows of w, d wide, both of one type.  offset (fp32[classes], may be
  * NULL) is a constant, e.g. the log of the clusters' sizes; -inf leaves a class
  * out: it has no probability, its row of w is not looked at (it may hold NaN)
- * and its gradient is zero.
+ * and its gradient is zero, whatever the rows of h hold.  A value below -2.3e38,
+ * such as the type's lowest, gives a class no probability either, but its row of
+ * w and the rows of h are to be finite then.
  *
  * Of a large head's logits at most 256 MB are stored: 256 x 256 of them at a
  * time leave their rows' largest and sum, and for the gradient what was not kept

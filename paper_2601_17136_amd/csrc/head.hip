@@ -636,7 +636,8 @@ struct ProductArgs {
   int64_t ldo;
   const float* alpha;   // null: 1
   int each;             // alpha holds one for each row
-  const float* coef;    // rows of weight 0 are 0, whatever stands in b; null: none
+  const float* weight;  // rows whose weight is `none` are 0, whatever stands in a and b; may be null
+  float none;
 };
 // The two products of a piece run in one launch where their tiles are alike.
 // Bound by the matrix cores: both products of 8192 rows of 4096 and 16384 classes
@@ -662,16 +663,26 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductJ
   tile_product<E, S>(a.a, a.b, r0, n0, a.K, a.nkc, a.nseg, c0, c1, lds, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
-  float alpha = a.alpha && !a.each ? *a.alpha : 1.f;
+  const float alpha = a.alpha && !a.each ? *a.alpha : 1.f;
   float* slab = a.slabs ? a.slabs + (int64_t)sl * a.M * a.N : nullptr;
 #pragma unroll
-  for (int bi = 0; bi < S::WM; ++bi)
+  for (int bi = 0; bi < S::WM; ++bi) {
+    const int64_t b0 = r0 + (wm * S::WM + bi) * 32;
+    // what the rows are multiplied by, and which of them are 0, before any store
+    float f[16];
+    unsigned none = 0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) f[r] = alpha;
+    if (std::is_same<E, half_t>::value && !slab && a.each)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) f[r] = a.alpha[min(b0 + acc_row(r, h), a.M - 1)];
+    if (!slab && a.weight)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) none |= a.weight[min(b0 + acc_row(r, h), a.M - 1)] == a.none ? 1u << r : 0u;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int64_t row = r0 + (wm * S::WM + bi) * 32 + acc_row(r, h);
+      const int64_t row = b0 + acc_row(r, h);
       if (row >= a.M) continue;
-      const bool none = !slab && a.coef && a.coef[row] == 0.f;
-      if (!slab && a.each) alpha = a.alpha[row];
 #pragma unroll
       for (int bj = 0; bj < S::WN; ++bj) {
         const int64_t col = n0 + (wn * S::WN + bj) * 32 + l32;
@@ -680,10 +691,11 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductJ
           float* p = slab + row * a.N + col;
           *p = a.add ? *p + acc[bi][bj][r] : acc[bi][bj][r];
         } else {
-          ((OT*)a.out)[row * a.ldo + col] = (OT)(none ? 0.f : acc[bi][bj][r] * alpha);
+          ((OT*)a.out)[row * a.ldo + col] = (OT)(none >> r & 1 ? 0.f : acc[bi][bj][r] * f[r]);
         }
       }
     }
+  }
 }
 
 // out from the slabs, in order, so that the bits do not depend on timing; a thread
@@ -694,7 +706,8 @@ struct SlabJob {
   int64_t M, N;
   const float* alpha;  // as ProductArgs'
   int each;
-  const float* coef;
+  const float* weight;
+  float none;
   void* out;
   int64_t ldo;
   unsigned blocks;
@@ -706,7 +719,7 @@ template <typename OT>
 __global__ __launch_bounds__(256) void slabs_kernel(SlabJobs jobs) {
   const bool second = blockIdx.x >= jobs.j[0].blocks;
   const SlabJob& j = jobs.j[second];
-  const float *slabs = j.slabs, *alpha = j.alpha, *coef = j.coef;
+  const float *slabs = j.slabs, *alpha = j.alpha, *weight = j.weight;
   OT* out = (OT*)j.out;
   const int count = j.count;
   const int64_t M = j.M, N = j.N, ldo = j.ldo;
@@ -730,7 +743,7 @@ __global__ __launch_bounds__(256) void slabs_kernel(SlabJobs jobs) {
       }
     }
     const float fr = j.each ? alpha[row] : f;
-    const bool none = coef && coef[row] == 0.f;
+    const bool none = weight && weight[row] == j.none;
     o4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (OT)(none ? 0.f : s[e] * fr);
@@ -1009,7 +1022,8 @@ struct Head {
   // out (M x N) = A B^T over K, or its slabs where there are any (K0: the first
   // piece's K, from which the slabs' shares are)
   ProductArgs product(Side x, Side y, int64_t M, int64_t N, int K, int K0, bool big, int slabs, float* slab, int add,
-                      void* out, int64_t ldo, const float* alpha, int each, const float* coef) const {
+                      void* out, int64_t ldo, const float* alpha, int each, const float* weight,
+                      float none) const {
     ProductArgs pa{};
     pa.a = x;
     pa.b = y;
@@ -1028,7 +1042,8 @@ struct Head {
     pa.ldo = ldo;
     pa.alpha = alpha;
     pa.each = alpha && each;
-    pa.coef = coef;
+    pa.weight = weight;
+    pa.none = none;
     return pa;
   }
   hipError_t multiply(const ProductJobs& jobs, bool big) const {
@@ -1039,9 +1054,9 @@ struct Head {
       hipLaunchKernelGGL((product_kernel<E, XT, SmallTile>), grid, dim3(SmallTile::threads), 0, s, jobs);
     return hipGetLastError();
   }
-  SlabJob sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, int each, const float* coef,
-              void* out, int64_t ldo) const {
-    return {slabs, count, M, N, alpha, alpha && each, coef, out, ldo, blocks_of(M * cdiv(N, 4))};
+  SlabJob sum(const float* slabs, int count, int64_t M, int64_t N, const float* alpha, int each, const float* weight,
+              float none, void* out, int64_t ldo) const {
+    return {slabs, count, M, N, alpha, alpha && each, weight, none, out, ldo, blocks_of(M * cdiv(N, 4))};
   }
 
   hipError_t run(bool grad) const {
@@ -1159,18 +1174,20 @@ struct Head {
         Side wv = wt;
         wv.p = at<E>(p.wt) + v0;
         ph = product({sa.G, sa.ldg, sa.planeg, p.n_pad}, wv, a.n, a.d, kv, kv0, p.bigh, p.sh, at<float>(p.slabs_h),
-                     v0 > 0, a.dh, a.lddh, ta.alpha, 1, ta.coef);
+                     v0 > 0, a.dh, a.lddh, ta.alpha, 1, ta.coef, 0.f);
         if (p.sh && v0 + p.piece >= a.classes)
           sums.j[n_sums++] = sum(at<float>(p.slabs_h), written(kv0, p.bigh, p.sh), a.n, a.d, ta.alpha, 1, ta.coef,
-                                 a.dh, a.lddh);
+                                 0.f, a.dh, a.lddh);
       }
       if (a.dw) {
         XT* dw = (XT*)a.dw + (int64_t)v0 * a.lddw;
+        // (a NaN in G or in h is in every class's sum, but not in the gradient of one left out)
+        const float* off = a.offset ? a.offset + v0 : nullptr;
         pw = product({sa.Gt, sa.ldt, sa.planet, p.piece}, ht, cnt, a.d, kn, kn, p.bigw, p.sw, at<float>(p.slabs_w), 0,
-                     dw, a.lddw, alpha_w, 0, nullptr);
+                     dw, a.lddw, alpha_w, 0, off, -INFINITY);
         if (p.sw)
-          sums.j[n_sums++] = sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha_w, 0, nullptr,
-                                 dw, a.lddw);
+          sums.j[n_sums++] = sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha_w, 0, off,
+                                 -INFINITY, dw, a.lddw);
       }
       if (a.dh && a.dw && p.bigh == p.bigw) {
         KKM_TRY(multiply({{ph, pw}}, p.bigh));

@@ -412,7 +412,8 @@ struct RowsJob {
   float none_b;
   int64_t R;
   int d;
-  const float* weight_r;  // rows of out that take no part have 0 here
+  const float* weight_r;  // rows of out that take no part have `none_r` here
+  float none_r;
   void* out;
   int64_t ldo;
   int per;       // rows_direct: classes of a slab
@@ -445,7 +446,7 @@ __device__ inline void rows_few(const RowsJob& q, unsigned bx, unsigned by) {
       b[k0][e] = load_raw(B + (int64_t)(use ? k : 0) * ldb, c0 + place * VEC, use ? d : 0);
     }
   floatx4 c[KB], cn[KB];
-  float wn = 1.f;
+  float wn = 1.f;  // (compared where it is used: the row is on its way)
   auto fetch = [&](int64_t r0) {
     const int64_t row = min(r0 + l16, R - 1);
 #pragma unroll
@@ -458,7 +459,7 @@ __device__ inline void rows_few(const RowsJob& q, unsigned bx, unsigned by) {
   for (; r0 < R; r0 += step) {
 #pragma unroll
     for (int k0 = 0; k0 < KB; ++k0) c[k0] = cn[k0];
-    const bool part = wn != 0.f;
+    const bool part = wn != q.none_r;
     fetch(r0 + step);
     floatx4 acc[VEC];
 #pragma unroll
@@ -508,7 +509,8 @@ struct ColsJob {
   int64_t per;
   float* slabs;
   int M;
-  const float* weight_m;  // rows of out that take no part have 0 here
+  const float* weight_m;  // rows of out that take no part have `none_m` here
+  float none_m;
   void* out;              // null: slabs
   int64_t ldo;
   unsigned gx, gy, gz;  // the workgroups: features, splits, columns of C
@@ -608,7 +610,7 @@ __device__ inline void cols_few(const ColsJob& q, unsigned bx, unsigned by, unsi
       if (cc >= d || s0 + sr >= M) continue;
       const float v = red[sr][y % (16 * VEC)];
       if (out)
-        out[(s0 + sr) * ldo + cc] = (XT)(takes_part(weight_m, 0.f, s0 + sr) ? v : 0.f);
+        out[(s0 + sr) * ldo + cc] = (XT)(takes_part(weight_m, q.none_m, s0 + sr) ? v : 0.f);
       else
         slab[(int64_t)sr * d + cc] = v;
     }
@@ -617,11 +619,12 @@ __device__ inline void cols_few(const ColsJob& q, unsigned bx, unsigned by, unsi
 }
 
 // out (M x d) from the slabs, in order, so that the bits do not depend on timing;
-// rows of weight 0 are 0.  4 to 5 us, of which most is the launch.
+// rows whose weight is `none` are 0.  4 to 5 us, of which most is the launch.
 struct SlabsJob {
   const float* slabs;
   int count, M, d;
   const float* weight;
+  float none;
   void* out;
   int64_t ldo;
   unsigned blocks;
@@ -648,7 +651,7 @@ __global__ __launch_bounds__(256) void slabs_few_kernel(SlabsJobs jobs) {
   const int lane = threadIdx.x;
   s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
   const int64_t row = x / d;
-  ((OT*)q.out)[row * q.ldo + (x - row * d)] = (OT)(takes_part(q.weight, 0.f, row) ? s : 0.f);
+  ((OT*)q.out)[row * q.ldo + (x - row * d)] = (OT)(takes_part(q.weight, q.none, row) ? s : 0.f);
 }
 
 // ------------------------------------------------------------------ both sides longer, little work
@@ -848,7 +851,7 @@ __device__ inline void rows_direct(const RowsJob& q, unsigned bx, unsigned by, u
     const int rr = x / 16, cc = (x % 16) * VEC;
     const int64_t row = r0 + rr;
     if (row >= R || c0 + cc >= d) continue;
-    const bool part = takes_part(weight_r, 0.f, row);
+    const bool part = takes_part(weight_r, q.none_r, row);
     float v[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
@@ -962,12 +965,13 @@ void by_short(int S, F&& f) {
 
 template <typename XT, int S>
 ColsJob cols_job(const float* weight, float none, const float* C, int64_t ldc, const void* X, int64_t ldx, int64_t R,
-                 int d, int splits, int64_t per, float* slabs, int M, const float* weight_m, void* out, int64_t ldo) {
-  return {C, ldc, X, ldx, R, d, weight, none, per, slabs, M, weight_m, splits > 1 ? nullptr : out, ldo,
+                 int d, int splits, int64_t per, float* slabs, int M, const float* weight_m, float none_m, void* out,
+                 int64_t ldo) {
+  return {C, ldc, X, ldx, R, d, weight, none, per, slabs, M, weight_m, none_m, splits > 1 ? nullptr : out, ldo,
           (unsigned)cdiv(d, ColsShape<XT, S>::width), (unsigned)splits, (unsigned)cdiv(M, S)};
 }
-SlabsJob sum_job(const float* slabs, int count, int M, int d, const float* weight, void* out, int64_t ldo) {
-  return {slabs, count, M, d, weight, out, ldo, (unsigned)cdiv((int64_t)M * d, 64)};
+SlabsJob sum_job(const float* slabs, int count, int M, int d, const float* weight, float none, void* out, int64_t ldo) {
+  return {slabs, count, M, d, weight, none, out, ldo, (unsigned)cdiv((int64_t)M * d, 64)};
 }
 template <typename XT, int S, int ROWS>
 void launch_grads(const ColsJob& c, const RowsJob& r, unsigned blocks_r, hipStream_t s) {
@@ -1031,19 +1035,22 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
     RowsJob r{};
     SlabsJobs sums{};
     float* slabs = (float*)(ws + p.slabs);
+    // who takes part: of the long side and of the short one
+    const float *in_long = p.classes ? f.coef : a.offset, *in_short = p.classes ? a.offset : f.coef;
+    const float none_long = p.classes ? 0.f : none, none_short = p.classes ? none : 0.f;
     if (short_out) {
-      c = cols_job<XT, S>(p.classes ? f.coef : a.offset, p.classes ? 0.f : none, f.C, p.S, p.classes ? a.h : a.w,
-                          p.classes ? a.ldh : a.ldw, p.R, a.d, p.splits, p.per, slabs, rows_b,
-                          p.classes ? nullptr : f.coef, short_out, p.classes ? a.lddw : a.lddh);
+      c = cols_job<XT, S>(in_long, none_long, f.C, p.S, p.classes ? a.h : a.w, p.classes ? a.ldh : a.ldw, p.R, a.d,
+                          p.splits, p.per, slabs, rows_b, in_short, none_short, short_out,
+                          p.classes ? a.lddw : a.lddh);
       if (p.splits > 1)
-        sums.j[0] = sum_job(slabs, p.splits, rows_b, a.d, p.classes ? nullptr : f.coef, short_out,
+        sums.j[0] = sum_job(slabs, p.splits, rows_b, a.d, in_short, none_short, short_out,
                             p.classes ? a.lddw : a.lddh);
     }
     if (long_out && !p.joined) {
       const unsigned cols = (unsigned)cdiv(a.d, 64 * VEC);
-      r = {f.C, p.S, p.classes ? a.w : a.h, p.classes ? a.ldw : a.ldh, rows_b, p.classes ? a.offset : f.coef,
-           p.classes ? none : 0.f, p.R, a.d, p.classes ? f.coef : nullptr, long_out, p.classes ? a.lddh : a.lddw, 0,
-           nullptr, (unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max(1u, (S == 64 ? 512u : 1536u) / cols)), cols};
+      r = {f.C, p.S, p.classes ? a.w : a.h, p.classes ? a.ldw : a.ldh, rows_b, in_short, none_short, p.R, a.d,
+           in_long, none_long, long_out, p.classes ? a.lddh : a.lddw, 0, nullptr,
+           (unsigned)std::min<int64_t>(cdiv(p.R, 16), std::max(1u, (S == 64 ? 512u : 1536u) / cols)), cols};
       launch_grads<XT, S, ROWS_FEW>(c, r, r.gx * r.gy, s);
     } else if (short_out) {
       launch_grads<XT, S, ROWS_NONE>(c, r, 0, s);
@@ -1109,15 +1116,15 @@ hipError_t direct_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   SlabsJobs sums{};
   float *sw = (float*)(ws + p.slabs_w), *sh = (float*)(ws + p.slabs_h);
   if (a.dw) {
-    c = cols_job<XT, 64>(f.coef, 0.f, f.C, p.ldz, a.h, a.ldh, a.n, a.d, p.splits, p.per, sw, a.classes, nullptr, a.dw,
-                         a.lddw);
-    if (p.splits > 1) sums.j[0] = sum_job(sw, p.splits, a.classes, a.d, nullptr, a.dw, a.lddw);
+    c = cols_job<XT, 64>(f.coef, 0.f, f.C, p.ldz, a.h, a.ldh, a.n, a.d, p.splits, p.per, sw, a.classes, a.offset,
+                         -INFINITY, a.dw, a.lddw);
+    if (p.splits > 1) sums.j[0] = sum_job(sw, p.splits, a.classes, a.d, a.offset, -INFINITY, a.dw, a.lddw);
   }
   if (a.dh) {
-    r = {f.C, p.ldz, a.w, a.ldw, a.classes, a.offset, -INFINITY, a.n, a.d, f.coef, p.splitsh > 1 ? nullptr : a.dh,
+    r = {f.C, p.ldz, a.w, a.ldw, a.classes, a.offset, -INFINITY, a.n, a.d, f.coef, 0.f, p.splitsh > 1 ? nullptr : a.dh,
          a.lddh, p.perh, sh, (unsigned)cdiv(a.d, 16 * kVec<XT>), (unsigned)cdiv(a.n, 32)};
     launch_grads<XT, 64, ROWS_DIRECT>(c, r, r.gx * r.gy * p.splitsh, s);
-    if (p.splitsh > 1) sums.j[1] = sum_job(sh, p.splitsh, (int)a.n, a.d, f.coef, a.dh, a.lddh);
+    if (p.splitsh > 1) sums.j[1] = sum_job(sh, p.splitsh, (int)a.n, a.d, f.coef, 0.f, a.dh, a.lddh);
   } else {
     launch_grads<XT, 64, ROWS_NONE>(c, r, 0, s);
   }
