@@ -1002,7 +1002,7 @@ struct Head {
   template <int MODE>
   hipError_t scores(ScoreArgs<E> sa, int64_t classes) const {
     const bool big = MODE == SCORES_G ? p.bigg : p.big;
-    sa.nkc = p.kp / chunk_of(big);
+    sa.nkc = p.kp / kChunkK;
     sa.mt = (int)cdiv(classes, big ? BigTile::BM : SmallTile::BM);
     sa.nt = (int)cdiv(a.n, big ? BigTile::BN : SmallTile::BN);
     const dim3 grid((unsigned)((int64_t)sa.mt * sa.nt));
@@ -1013,13 +1013,12 @@ struct Head {
     return hipGetLastError();
   }
 
-  static int chunk_of(bool big) { return big ? BigTile::BK : SmallTile::BK; }
   // chunks of a slab, and the slabs that a product of K writes
-  int share(int K, bool big, int slabs) const {
-    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, std::max(slabs, 1));
+  int share(int K, int slabs) const {
+    return (int)cdiv(cdiv(K, kChunkK) * p.nseg, std::max(slabs, 1));
   }
-  int written(int K, bool big, int slabs) const {
-    return (int)cdiv(cdiv(K, chunk_of(big)) * p.nseg, share(K, big, slabs));
+  int written(int K, int slabs) const {
+    return (int)cdiv(cdiv(K, kChunkK) * p.nseg, share(K, slabs));
   }
 
   // out (M x N) = A B^T over K, or its slabs where there are any (K0: the first
@@ -1033,11 +1032,11 @@ struct Head {
     pa.M = M;
     pa.N = N;
     pa.K = K;
-    pa.nkc = (int)cdiv(K, chunk_of(big));
+    pa.nkc = (int)cdiv(K, kChunkK);
     pa.nseg = p.nseg;
     pa.mt = (int)cdiv(M, big ? BigTile::BM : SmallTile::BM);
     pa.nt = (int)cdiv(N, big ? BigTile::BN : SmallTile::BN);
-    pa.per = share(K0, big, slabs);
+    pa.per = share(K0, slabs);
     pa.blocks = (unsigned)((int64_t)pa.mt * pa.nt * cdiv(pa.nkc * pa.nseg, pa.per));
     pa.slabs = slabs ? slab : nullptr;
     pa.add = add;
@@ -1179,7 +1178,7 @@ struct Head {
         ph = product({sa.G, sa.ldg, sa.planeg, p.n_pad}, wv, a.n, a.d, kv, kv0, p.bigh, p.sh, at<float>(p.slabs_h),
                      v0 > 0, a.dh, a.lddh, ta.alpha, 1, ta.coef, 0.f);
         if (p.sh && v0 + p.piece >= a.classes)
-          sums.j[n_sums++] = sum(at<float>(p.slabs_h), written(kv0, p.bigh, p.sh), a.n, a.d, ta.alpha, 1, ta.coef,
+          sums.j[n_sums++] = sum(at<float>(p.slabs_h), written(kv0, p.sh), a.n, a.d, ta.alpha, 1, ta.coef,
                                  0.f, a.dh, a.lddh);
       }
       if (a.dw) {
@@ -1189,7 +1188,7 @@ struct Head {
         pw = product({sa.Gt, sa.ldt, sa.planet, p.piece}, ht, cnt, a.d, kn, kn, p.bigw, p.sw, at<float>(p.slabs_w), 0,
                      dw, a.lddw, alpha_w, 0, off, -INFINITY);
         if (p.sw)
-          sums.j[n_sums++] = sum(at<float>(p.slabs_w), written(kn, p.bigw, p.sw), cnt, a.d, alpha_w, 0, off,
+          sums.j[n_sums++] = sum(at<float>(p.slabs_w), written(kn, p.sw), cnt, a.d, alpha_w, 0, off,
                                  -INFINITY, dw, a.lddw);
       }
       if (a.dh && a.dw && p.bigh == p.bigw) {

@@ -34,39 +34,36 @@ __device__ inline floatx16 mfma16(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-constexpr int lds_of(int bm, int bn, int bk, int stages) { return (bm + bn) * bk * 2 * stages; }
-// A workgroup of GM x GN wavefronts, each WM x WN blocks of 32 x 32; chunks of
-// BK contraction indices, STAGES of them in LDS.
-template <int WM_, int WN_, int GM_, int GN_, int BK_, int STAGES_>
+constexpr int kChunkK = 64;  // contraction indices of a chunk, to which operands are padded
+
+// A workgroup of GM x GN wavefronts, each WM x WN blocks of 32 x 32; two chunks
+// lie in LDS.
+template <int WM_, int WN_, int GM_, int GN_>
 struct TileShape {
-  static constexpr int WM = WM_, WN = WN_, GM = GM_, GN = GN_, BK = BK_, STAGES = STAGES_;
+  static constexpr int WM = WM_, WN = WN_, GM = GM_, GN = GN_;
   static constexpr int BM = WM * GM * 32, BN = WN * GN * 32, waves = GM * GN, threads = waves * 64;
-  static constexpr int per_cu = lds_of(BM, BN, BK, STAGES) <= 80 * 1024 ? 2 : 1;  // workgroups
-  static constexpr int row_bytes = BK * 2, slots = row_bytes / 16, group = 64 / slots;  // rows of a 1 KB load
-  static constexpr int stage_bytes = (BM + BN) * row_bytes, lds_bytes = stage_bytes * STAGES;
+  static constexpr int row_bytes = kChunkK * 2, slots = row_bytes / 16, group = 64 / slots;  // rows of a 1 KB load
+  static constexpr int stage_bytes = (BM + BN) * row_bytes, lds_bytes = stage_bytes * 2;
+  static constexpr int per_cu = lds_bytes <= 80 * 1024 ? 2 : 1;  // workgroups
   static constexpr int LA = BM / group / waves, LB = BN / group / waves;  // loads per wavefront and chunk
   static_assert(BM % (group * waves) == 0 && BN % (group * waves) == 0, "");
   static_assert(LA * group % 16 == 0 && LB * group % 16 == 0, "turn() of a wavefront's rows goes by its own");
   // 16-byte slot s of a row lies at s ^ turn(row): sixteen rows at one s meet in
   // none of LDS's 64 banks
-  __device__ static int turn(int row) { return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3; }
+  __device__ static int turn(int row) { return (row >> 1) & 7; }
 };
-using BigTile = TileShape<4, 2, 2, 4, 64, 2>;    // 256 x 256, 128 KB
-using SmallTile = TileShape<2, 2, 2, 2, 64, 2>;  // 128 x 128, 64 KB
-constexpr int kChunkK = 64;  // what operands are padded to
+using BigTile = TileShape<4, 2, 2, 4>;    // 256 x 256, 128 KB
+using SmallTile = TileShape<2, 2, 2, 2>;  // 128 x 128, 64 KB
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-template <int VM>
-__device__ inline void wait_loads() {  // at most VM loads outstanding, every LDS read done
-  __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | ((VM >> 4) << 14));
-}
+__device__ inline void wait_loads() { __builtin_amdgcn_s_waitcnt(7 << 4); }  // every load and LDS read done
 
 // acc = the tile at rows row0 of a and col0 of b, over chunks [c0, c1) of the
 // nseg x nkc (segment, chunk) pairs.  Loads go straight to LDS and permute
 // their source instead of their target, which is a wavefront's 1 KB in order.
 // Rows past the operand's end read its last one (what they give is not stored),
-// contraction indices past K read zero.  Chunk c + STAGES - 1 is requested
+// contraction indices past K read zero.  Chunk c + 1 is requested
 // while chunk c is multiplied; a step's operands are read from LDS while the
 // step before is multiplied, across the chunk's one barrier too.
 template <typename E, class S>
@@ -74,8 +71,8 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
                                     int c0, int c1, char* lds, floatx16 (&acc)[S::WM][S::WN]) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host pass knows no buffer resources)
   constexpr unsigned kBound = 0x7ffffff0u, kOut = 0x80000000u;
-  constexpr int NS = S::BK / 16, D = S::STAGES, L = S::LA + S::LB;
-  constexpr int SP = D == 2 ? NS / 2 : NS, LP = L / SP;  // a chunk's loads go out in its first SP steps
+  constexpr int NS = kChunkK / 16, L = S::LA + S::LB;
+  constexpr int SP = NS / 2, LP = L / SP;  // a chunk's loads go out in its first SP steps
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
   const int lrow = lane / S::slots;
@@ -106,7 +103,7 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
                                              0x00027000);
   };
   auto issue = [&](int j) {  // load j of the chunk's L
-    const int left = K - fk * S::BK;  // slots from left / 8 on lie past K
+    const int left = K - fk * kChunkK;  // slots from left / 8 on lie past K
     char* st = lds + fst * S::stage_bytes;
     const int so = fk * S::row_bytes;
     if (j < S::LA) {
@@ -121,7 +118,7 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
     }
   };
   auto advance = [&]() {
-    fst = fst + 1 == D ? 0 : fst + 1;
+    fst ^= 1;
     if (++fc < c1 && ++fk == nkc) {
       fk = 0;
       ++fs;
@@ -154,36 +151,32 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto arrive = [&](auto vm) {  // this wavefront's part of the next chunk is in LDS; the barrier: everyone's
+  auto arrive = [&]() {  // this wavefront's part of the next chunk is in LDS; the barrier: everyone's
     __builtin_amdgcn_sched_barrier(0);
-    wait_loads<decltype(vm)::value>();
+    wait_loads();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll
-  for (int i = 0; i < D - 1; ++i) {
-#pragma unroll
-    for (int j = 0; j < L; ++j) issue(j);
-    advance();
-  }
-  arrive(std::integral_constant<int, (D - 2) * L>{});
+  for (int j = 0; j < L; ++j) issue(j);
+  advance();
+  arrive();
 #pragma unroll
   for (int i = 0; i < S::WM + S::WN; ++i) read(0, lds, 0, i);
   int cst = 0;
   for (int c = c0; c < c1; ++c) {
     // (the chunk fetched goes into the stage of chunk c - 1, which everyone has read)
     const char* st = lds + cst * S::stage_bytes;
-    cst = cst + 1 == D ? 0 : cst + 1;
+    cst ^= 1;
 #pragma unroll
     for (int k = 0; k < NS - 1; ++k) multiply(k, st, k + 1);
-    // in flight may be: the chunks after the next, and of the last of them what has been requested
-    arrive(std::integral_constant<int, D == 2 ? 0 : (D - 3) * L + (NS - 1) * LP>{});
+    arrive();
     multiply(NS - 1, lds + cst * S::stage_bytes, 0);
     advance();
   }
-  wait_loads<0>();
+  wait_loads();
   __syncthreads();
 #endif
 }
