@@ -5,9 +5,8 @@
 // the scores are a matrix of S <= kFew columns, and the work is to read h (or w)
 // and write its gradient once.
 //
-//   few classes:  scores_few (G = softmax less targets, [n][S]; of fp32 or of few rows
-//                 also dH = G W), then dW = G^T H (cols_few, reads H once more) and
-//                 what is left of dH (rows_few)
+//   few classes:  scores_few (G = softmax less targets, [n][S]), then dW = G^T H
+//                 (cols_few, reads H once more) and dH = G W (rows_few)
 //   few rows:     scores_few (the scores Z, [classes][S]), targets_few (lse, loss),
 //                 grad_few (Z becomes G^T), then dW = G^T H (rows_few) and
 //                 dH = G W (cols_few, reads W once more)
@@ -138,17 +137,17 @@ __device__ inline float pair_key(const FewArgs& a, int64_t at, int& id, bool& ba
 }
 
 // Few classes: 32 rows of h by all classes; eight lanes finish a row, lane p
-// owning the classes c % 8 = p, so that no two add to one target.  With dh the
-// workgroup goes on to its rows of dH = G W: the matrix instructions have the
-// features as rows, as in rows_few, and the wavefronts take every fourth
-// 16 kVec features.  Few classes are bound by reading h (and writing dH): 60000 fp32
-// rows of 780, 10 classes, with dH 107 us, 3.5 TB/s of h, dH and G.  64 of them by
-// the fp32 matrix instructions: 20000 rows of 784 79 us, 51 TFLOP/s.
+// owning the classes c % 8 = p, so that no two add to one target.  Few
+// are bound by reading h: 60000 fp32 rows of 780, 10 classes, 57 us with G, 3.3
+// TB/s, the loss alone 37, 5.1 TB/s.  64 of them by the fp32 matrix instructions:
+// 20000 rows of 784 35 us, 57 TFLOP/s (39 held to three wavefronts a SIMD, which the
+// others may be).  dH in this launch as well, from G in LDS, read w again for every
+// 32 rows and was slower wherever it was timed: those cases with gradient 158 / 148
+// and 121 / 111, 200 rows of 64 and 20 classes 22.6 / 19.0.
 template <typename XT, int CT>
-__global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void scores_few_classes_kernel(
-    FewArgs a, XT* __restrict__ dh, int64_t lddh) {
+__global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void scores_few_classes_kernel(FewArgs a) {
   constexpr int NT = 2, S = CT * 16;
-  __shared__ __attribute__((aligned(16))) float zs[4][NT * 16][S + 1];
+  __shared__ float zs[4][NT * 16][S + 1];
   const int64_t t0 = (int64_t)blockIdx.x * (NT * 16);
   const int row = threadIdx.x >> 3, p = threadIdx.x & 7;
   const int64_t i = t0 + row;
@@ -208,73 +207,14 @@ __global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void score
   }
   if (!a.C) return;
   float cf = dl * a.scale;
-  if (!here || !some || lse2 == -INFINITY) cf = 0.f;
-  if (here && bad) cf = __builtin_nanf("");
+  if (!some || lse2 == -INFINITY) cf = 0.f;
+  if (bad) cf = __builtin_nanf("");
   if (here && p == 0) a.coef[i] = cf;
   const float l2 = safe(lse2);
-  float* gs = &zs[2][0][0] + row * (S + 4);  // G once more, for dH: rows of 16-byte words
+  if (!here) return;
 #pragma unroll
-  for (int c = p; c < S; c += 8) {
-    const float g = cf == 0.f || z[c] == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z[c] - l2) - q[c]);
-    if (here) a.C[i * S + c] = g;
-    gs[c] = g;
-  }
-  if (!dh) return;
-  __syncthreads();
-  constexpr int VEC = kVec<XT>, KB = CT;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l16 = lane & 15, g = lane >> 4, place = (l16 >> 2) + 4 * (l16 & 3);
-  floatx4 gr[KB][NT];
-  bool part[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    float any = 0.f;  // (a row of weight 0 has no G, and dH = 0 whatever stands in w)
-#pragma unroll
-    for (int k0 = 0; k0 < KB; ++k0) {
-      gr[k0][t] = *(const floatx4*)(&zs[2][0][0] + (t * 16 + l16) * (S + 4) + 16 * k0 + 4 * g);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) any = gr[k0][t][e] != 0.f ? 1.f : any;
-    }
-    any += __shfl_xor(any, 16, 64);
-    any += __shfl_xor(any, 32, 64);
-    part[t] = any != 0.f;
-  }
-  for (int c0 = wave * (16 * VEC); c0 < a.d; c0 += 64 * VEC) {
-    floatx4 acc[VEC][NT];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[j][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k0 = 0; k0 < KB; ++k0) {
-      raw_vec<XT> b[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int k = 16 * k0 + 4 * g + e;
-        const bool use = k < a.classes && !(a.offset && a.offset[k] == -INFINITY);
-        b[e] = load_raw((const XT*)a.w + (int64_t)(use ? k : 0) * a.ldw, c0 + place * VEC, use ? a.d : 0);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)b[e][j], gr[k0][t][e], acc[j][t], 0, 0, 0);
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int64_t r = t0 + t * 16 + l16;
-      if (r >= a.n) continue;
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        float v[VEC];
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v[j] = part[t] ? acc[j][t][q4] : 0.f;
-        store_part(dh + r * lddh, c0 + VEC * (g + 4 * q4), a.d, v);
-      }
-    }
-  }
+  for (int c = p; c < S; c += 8)
+    a.C[i * S + c] = cf == 0.f || z[c] == -INFINITY ? 0.f : cf * (__builtin_amdgcn_exp2f(z[c] - l2) - q[c]);
 }
 
 // Few rows: CT x 16 classes by all rows of h; the rows' (largest, sum) of the
@@ -869,10 +809,10 @@ __device__ inline void rows_direct(const RowsJob& q, unsigned bx, unsigned by, u
 
 // Both gradients in one launch, the sums' workgroups first (what they read may
 // still be in the last-level cache).  ROWS: rows_few, rows_direct or neither.
-// Bound by reading the long side: dW of 60000 fp32 rows of 780, 10 classes 46 us, 4.2
-// TB/s; both of 16 rows, 32000 bfloat16 classes of 2000 74 us, 3.5 TB/s of w and
-// dW.  64 classes by the fp32 matrix instructions: dW of 20000 rows of 784 44 us,
-// 46 TFLOP/s.
+// Bound by reading the long side: both of 60000 fp32 rows of 780, 10 classes 78 us, 4.8
+// TB/s of h and dH; of 16 rows, 32000 bfloat16 classes of 2000 74 us, 3.5 TB/s of w
+// and dW.  64 classes by the fp32 matrix instructions: both of 20000 rows of 784 63
+// us, 63 TFLOP/s.
 enum { ROWS_NONE, ROWS_FEW, ROWS_DIRECT };
 template <typename XT, int S, int ROWS>
 __global__ __launch_bounds__(256, 2) void grads_few_kernel(ColsJob c, RowsJob r) {
@@ -900,7 +840,6 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct FewPlan {
   bool classes;  // few classes, or few rows
-  bool joined;   // few classes: dH in the scores' launch
   int S;         // the short side, padded to 16, 32 or 64
   int64_t R;     // the long side
   int ct;        // few rows: class blocks of a tile
@@ -913,9 +852,6 @@ struct FewPlan {
 FewPlan few_plan(const HeadArgs& a, bool grad) {
   FewPlan p{};
   p.classes = a.classes <= kFew;
-  // (many rows of 16 bits: a launch of its own fits more wavefronts on a CU; 20000
-  // bfloat16 rows of 784, 64 classes 139 / 132 us, where 200 fp32 rows of 64 take 24 / 27)
-  p.joined = p.classes && (a.type == TYPE_F32 || a.n <= 4096);
   const int64_t s = p.classes ? a.classes : a.n;
   p.S = s <= 16 ? 16 : s <= 32 ? 32 : 64;
   p.R = p.classes ? a.n : a.classes;
@@ -996,7 +932,7 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
   if (p.classes) {
     by_short(p.S, [&](auto S) {
       hipLaunchKernelGGL((scores_few_classes_kernel<XT, decltype(S)::value / 16>), dim3((unsigned)cdiv(a.n, 32)),
-                         dim3(256), 0, s, f, (XT*)(p.joined && grad ? a.dh : nullptr), a.lddh);
+                         dim3(256), 0, s, f);
     });
     KKM_TRY(hipGetLastError());
   } else {
@@ -1046,7 +982,7 @@ hipError_t few_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
         sums.j[0] = sum_job(slabs, p.splits, rows_b, a.d, in_short, none_short, short_out,
                             p.classes ? a.lddw : a.lddh);
     }
-    if (long_out && !p.joined) {
+    if (long_out) {
       const unsigned cols = (unsigned)cdiv(a.d, 64 * VEC);
       r = {f.C, p.S, p.classes ? a.w : a.h, p.classes ? a.ldw : a.ldh, rows_b, in_short, none_short, p.R, a.d,
            in_long, none_long, long_out, p.classes ? a.lddh : a.lddw, 0, nullptr,
