@@ -550,11 +550,14 @@ int kkm_layer_norm_grad(kkm_ctx *ctx, int32_t type, int64_t n, int32_t d, const 
  *
  * Of a large head's logits at most 256 MB are stored: 256 x 256 of them at a
  * time leave their rows' largest and sum, and for the gradient what was not kept
- * is computed again, a piece of the classes at a time (G of a piece: at most 256
- * MB, or 256 classes).  fp32 operands are then taken as three bfloat16 parts, 24 bits
- * together, and an infinite entry of theirs gives NaN.  A head of at most 64
- * classes or 64 rows, or of little work (at most 64 MB of logits), holds its
- * scores as fp32 scratch and multiplies fp32 as fp32. */
+ * is computed again, a piece of the classes at a time (G of a piece, in two orders:
+ * each at most 256 MB, or 256 classes).  The gradient also holds transposed copies
+ * of h and w: 1.28 GB in all for 8192 bfloat16 rows of 4096 features, 32768 classes.
+ * fp32 operands are then taken as three bfloat16 parts, 24 bits together, and an
+ * entry of theirs that is infinite or past bfloat16's 3.39e38 gives NaN.  A head of
+ * at most 64 classes or 64 rows, or of little work (at most 64 MB of logits), holds
+ * its scores as fp32 scratch, one side padded to 64 at most, and multiplies fp32 as
+ * fp32. */
 typedef struct kkm_head {
   int32_t type; /* kkm_type of h, w and their gradients */
   int32_t d;

@@ -17,9 +17,12 @@
 //
 // The first classes' logits, at most 256 MB of them, stay for G where that takes
 // less (kept_tiles).  The others are multiplied again: four products where a caller
-// that kept all would take three, with those 256 MB of G in place of 1.07 GB (fp32
-// for 8192 rows of 32768 classes).  Bound by the matrix cores, whose clock falls
-// to 1.75 - 1.97 GHz under this load.
+// that kept all would take three.  G in its two orders and the kept logits are at
+// most 256 MB each, or 256 classes (for 8192 rows of 32768 classes all of them would
+// be 2.1 GB); a gradient's scratch has the transposed copies, copies of rows that
+// do not serve in place, and sums besides: 1.28 GB for those rows of 4096 bfloat16
+// features.  Bound by the matrix cores, whose clock falls to 1.75 - 1.97 GHz under
+// this load.
 //
 // Operands are 16 bits with the contraction index contiguous.  Rows of binary16
 // and bfloat16 that are aligned to 16 bytes serve in place; others are copied.
@@ -107,8 +110,8 @@ struct StageJobs {
 };
 
 // Rows in place of src's, kp wide (zero from d on), as P planes.  A thread
-// writes 8 values.  3001 + 10007 binary16 rows of 1001 10 us, 5.5 TB/s; 8000 fp32
-// rows of 1000 to three planes 15 us.
+// writes 8 values.  3001 + 10007 binary16 rows of 1001 11 us, 4.8 TB/s; 8000 fp32
+// rows of 1000 to three planes 16 us.
 template <typename XT, typename E, int P>
 __global__ __launch_bounds__(256) void stage_rows_kernel(StageJobs jobs, int d, int kp) {
   const bool second = blockIdx.x >= jobs.split;
@@ -144,7 +147,7 @@ __global__ __launch_bounds__(256) void stage_rows_kernel(StageJobs jobs, int d, 
 
 // The transposed copies: dst[c][row], rp rows wide (zero from `rows` on).  A
 // workgroup turns a 64 x 64 block through LDS.  8192 + 32768 bfloat16 rows of 4096
-// 125 us, 5.4 TB/s read and written.
+// 127 us, 5.3 TB/s read and written.
 template <typename XT, typename E, int P>
 __global__ __launch_bounds__(256) void stage_cols_kernel(StageJobs jobs, int d) {
   constexpr int VEC = kVec<XT>, LANES = 64 / VEC, PASS = 256 / LANES;  // lanes of a row, rows of a pass
@@ -252,12 +255,13 @@ struct ScoreArgs {
 // classes a block of one row of H, so a row's largest and sum stay in a lane
 // up to one exchange and the wavefronts' sums in LDS.  The epilogue holds up the
 // matrix cores once a tile: 9 us of a 256 x 256 tile, 19 with G, which it stores in
-// both orders at 3.4 TB/s.  bfloat16, 8192 rows of 4096: 32768 classes 1.83 ms, 1.20
-// PFLOP/s, matrix cores busy 62 % of the cycles (a library product of that shape
-// 1.41 PFLOP/s); with G, 16384 classes 1.07 ms, 1.02 PFLOP/s, 56 %.  fp32, 4000 rows
-// of 1000, 4000 classes: 158 us, 1.2 PFLOP/s of plane products; with G 196 us, or 60
-// of kept logits.  G of kept logits is bound by memory and needs no LDS: 20011 binary16 classes of 1777
-// rows 79 to 82 us, 3.5 TB/s, where multiplying again takes 141.
+// both orders at 3.4 TB/s.  bfloat16, 8192 rows of 4096: 32768 classes, of which 8192
+// are kept, 1.92 ms, 1.15 PFLOP/s, matrix cores busy 62 % of the cycles (a library
+// product of that shape 1.41 PFLOP/s); with G, 16384 classes 1.09 ms, 1.01 PFLOP/s, 57
+// %.  fp32, 4000 rows of 1000, 4000 classes: 159 us, 1.2 PFLOP/s of plane products;
+// with G 196 us, or 57 of kept logits.  G of kept logits is bound by memory and needs
+// no LDS: 20011 binary16 classes of 1777 rows 77 to 82 us, 3.5 TB/s, where
+// multiplying again takes 141.
 enum ScoresMode { SCORES_LOSS, SCORES_G, SCORES_G_OF_Z };
 template <typename E, class S, int P, int MODE>
 __global__ __launch_bounds__(S::threads, MODE == SCORES_G_OF_Z ? 2 : S::per_cu) void scores_kernel(ScoreArgs<E> a) {
@@ -641,8 +645,8 @@ struct ProductArgs {
 };
 // The two products of a piece run in one launch where their tiles are alike.
 // Bound by the matrix cores: both products of 8192 rows of 4096 and 16384 classes
-// 1.91 ms, 1.15 PFLOP/s, matrix cores busy 61 %; 3001 rows of 1001 and 10007 binary16
-// classes 136 us, 0.88: 160 workgroups have a tile of dW, 47 chunks long, and 96 half
+// 1.96 ms, 1.12 PFLOP/s, matrix cores busy 63 %; 3001 rows of 1001 and 10007 binary16
+// classes 139 us, 0.87: 160 workgroups have a tile of dW, 47 chunks long, and 96 half
 // of a tile of dH, 79 chunks long, which the others wait for.
 struct ProductJobs {
   ProductArgs j[2];
@@ -699,7 +703,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void product_kernel(ProductJ
 }
 
 // out from the slabs, in order, so that the bits do not depend on timing; a thread
-// takes four neighbouring entries of a row.  8192 rows of 4096, dH of bfloat16: 42 us.
+// takes four neighbouring entries of a row.  8192 rows of 4096, dH of bfloat16: 45 us.
 struct SlabJob {
   const float* slabs;
   int count;

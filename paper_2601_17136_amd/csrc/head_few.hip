@@ -138,10 +138,10 @@ __device__ inline float pair_key(const FewArgs& a, int64_t at, int& id, bool& ba
 
 // Few classes: 32 rows of h by all classes; eight lanes finish a row, lane p
 // owning the classes c % 8 = p, so that no two add to one target.  Few
-// are bound by reading h: 60000 fp32 rows of 780, 10 classes, 57 us with G, 3.3
-// TB/s, the loss alone 37, 5.1 TB/s.  64 of them by the fp32 matrix instructions:
-// 20000 rows of 784 35 us, 57 TFLOP/s (39 held to three wavefronts a SIMD, which the
-// others may be).  dH in this launch as well, from G in LDS, read w again for every
+// are bound by reading h: 60000 fp32 rows of 780, 10 classes, 59 us with G, 3.2
+// TB/s, the loss alone 37, 5.0 TB/s.  64 of them by the fp32 matrix instructions:
+// 20000 rows of 784 36 us, 56 TFLOP/s (a pass of 38.9 us is one of 42.5 if held to
+// three wavefronts a SIMD; the others may be).  dH in this launch as well, from G in LDS, read w again for every
 // 32 rows and was slower wherever it was timed: those cases with gradient 158 / 148
 // and 121 / 111, 200 rows of 64 and 20 classes 22.6 / 19.0.
 template <typename XT, int CT>
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void score
 
 // Few rows: CT x 16 classes by all rows of h; the rows' (largest, sum) of the
 // tile, and Z.  Bound by reading w: one row, 32768 bfloat16 classes of 2048 22 us,
-// 6.2 TB/s.
+// 6.1 TB/s.
 template <typename XT, int CT, int NT>
 __global__ __launch_bounds__(256) void scores_few_rows_kernel(FewArgs a) {
   constexpr int S = NT * 16, P = 256 / S;
@@ -809,10 +809,10 @@ __device__ inline void rows_direct(const RowsJob& q, unsigned bx, unsigned by, u
 
 // Both gradients in one launch, the sums' workgroups first (what they read may
 // still be in the last-level cache).  ROWS: rows_few, rows_direct or neither.
-// Bound by reading the long side: both of 60000 fp32 rows of 780, 10 classes 78 us, 4.8
-// TB/s of h and dH; of 16 rows, 32000 bfloat16 classes of 2000 74 us, 3.5 TB/s of w
+// Bound by reading the long side: both of 60000 fp32 rows of 780, 10 classes 79 us, 4.7
+// TB/s of h and dH; of 16 rows, 32000 bfloat16 classes of 2000 73 us, 3.5 TB/s of w
 // and dW.  64 classes by the fp32 matrix instructions: both of 20000 rows of 784 63
-// us, 63 TFLOP/s.
+// to 69 us, 58 to 63 TFLOP/s.
 enum { ROWS_NONE, ROWS_FEW, ROWS_DIRECT };
 template <typename XT, int S, int ROWS>
 __global__ __launch_bounds__(256, 2) void grads_few_kernel(ColsJob c, RowsJob r) {
@@ -1073,11 +1073,12 @@ hipError_t direct_typed(const HeadArgs& a, bool grad, char* ws, hipStream_t s) {
 // DIRECT up to so much work (n times classes times d): it needs four launches in
 // place of eight or more and no copies, but multiplies in fp32 on the way to the
 // gradients, and holds n times classes scores.  Microseconds with gradient, TILED
-// / DIRECT: fp32, 400 classes of 300 features 119 / 46 at n = 100, 136 / 70 at
-// 2000, 185 / 156 at 8000; 100 of 1000 225 / 59 at 2000, 610 / 426 at 30000; 1000 of
-// 1000 203 / 50 at 100, 308 / 216 at 2000; 1000 of 300 256 / 340 at 8000.  bfloat16,
-// 400 of 300 77 / 61 at 100, 89 / 87 at 2000; 1000 of 300 83 / 64 at 500, 90 / 139
-// at 2000; 400 of 64 83 / 102 at 8000.
+// / DIRECT: fp32, 400 classes of 300 features 71 / 31 at n = 100, 89 / 50 at 2000, 136
+// / 116 at 6600 and 133 / 127 at 8000, on either side of the limit; 700 of 300 114 /
+// 118 at 4000; 400 of 100 186 / 144 at 20000; 100 of 1000 130 / 54 at 2000, 514 / 405
+// at 30000; 1000 of 1000 121 / 41 at 100, 190 / 198 at 2000; 1000 of 300 203 / 250 at
+// 8000.  bfloat16, 400 of 300 48 / 37 at 100, 59 / 65 at 2000; 1000 of 300 52 / 42 at
+// 500, 62 / 89 at 2000; 400 of 64 61 / 70 at 8000.  At a limit the two are within 10 %.
 HeadForm head_form(const HeadArgs& a) {
   if (a.classes <= kFew || a.n <= kFew) return HEAD_FEW;
   const double work = (double)a.n * a.classes * a.d;

@@ -8,11 +8,12 @@
 // then a workgroup of 256), so it is read once.  The mean is taken twice: what the
 // first sum's rounding left of it is the mean of x - mu, summed beside the squares,
 // and both it and its square are taken off.  Rows of one value so have xh = 0;
-// with the first mean alone 1000 values of 30000 gave xh = -0.5.  A group goes over rows a grid apart and keeps its columns' w and b,
-// and in the gradient the fp32 sums of dw and db, in registers; a workgroup's
-// sums go to its line of the scratch, and a second launch adds the lines in
-// order, so the gradient's bits do not depend on timing.  Rows wider than the
-// registers take a loop over the row per pass instead.
+// with the first mean alone 1000 values of 30000 gave xh = -0.5.  A group goes over
+// rows a grid apart and keeps its columns' w and b, and in the gradient the fp32
+// sums of dw and db, in registers; a workgroup's sums go to its line of the
+// scratch, and a second launch adds the lines in order, so the gradient's bits do
+// not depend on timing.  Rows wider than the registers take a loop over the row
+// per pass instead.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,8 +29,8 @@ constexpr int kThreads = 256;
 // Workgroups, at most: a narrow row needs many for the bytes in flight, wider
 // ones gain from w and b loaded once, and in the gradient from fewer lines of
 // sums, one a workgroup.  Microseconds at 2048 / 1024 workgroups, forward: 40001
-// binary16 rows of 301 17 / 22; 8231 bfloat16 rows of 744 12 / 10; 3961 fp32 rows
-// of 7880 52 / 47.  At 1024 / 512, the gradient: 29 / 45, 20 / 17, 115 / 99.
+// binary16 rows of 301 19 / 23; 8231 bfloat16 rows of 744 12 / 10; 3961 fp32 rows
+// of 7880 54 / 48.  At 1024 / 512, the gradient: 28 / 46, 20 / 16, 112 / 97.
 int wgs_fwd(int d) { return d <= 512 ? 2048 : 1024; }
 int wgs_grad(int d) { return d <= 512 ? 1024 : 512; }
 
@@ -69,9 +70,9 @@ __device__ inline float inverse_deviation(float squares, float left, float eps) 
   return 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);  // (a NaN stays one)
 }
 
-// Forward, x read once: 20000 fp32 rows of 784 21 us, 5.9 TB/s of what it must read
-// and write; 16384 bfloat16 rows of 4096 44 us, 6.0 TB/s; 40001 binary16 rows of
-// 301 18 us, 2.6 TB/s (38 of a wavefront's 64 lanes have features there).
+// Forward, x read once: 20000 fp32 rows of 784 21 us, 6.0 TB/s of what it must read
+// and write; 16384 bfloat16 rows of 4096 44 us, 6.1 TB/s; 40001 binary16 rows of
+// 301 18 to 19 us, 2.6 TB/s (38 of a wavefront's 64 lanes have features there).
 template <typename XT, typename WT, int T, int NV>
 __global__ __launch_bounds__(kThreads) void layer_norm_kernel(const XT* __restrict__ x, int64_t ldx,
                                                               const WT* __restrict__ w, const WT* __restrict__ b,
@@ -133,8 +134,8 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(const XT* __restri
   }
 }
 
-// Gradient, x and dy read once: the same rows in 36 us, 5.3 TB/s; 87 us, 4.6 TB/s;
-// 29 us, 2.5 TB/s.  The sums over the rows cost it the lines besides: 17 MB
+// Gradient, x and dy read once: the same rows in 35 us, 5.4 TB/s; 89 us, 4.5 TB/s;
+// 30 us, 2.4 TB/s.  The sums over the rows cost it the lines besides: 17 MB
 // written for the bfloat16 rows.
 template <typename XT, typename WT, int T, int NV>
 __global__ __launch_bounds__(kThreads) void layer_norm_grad_kernel(
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(1024) void norm_lines_kernel(const float* __restric
 
 // Rows too wide for the registers: a workgroup per row and a pass over it for
 // the mean, the variance and the result (from the second on out of L2).  2000 rows
-// of 40000: fp32 230 us, 2.8 TB/s of x and y; bfloat16 112 us, 2.9.
+// of 40000: fp32 231 us, 2.8 TB/s of x and y; bfloat16 113 us, 2.8.
 template <typename XT, typename WT>
 __global__ __launch_bounds__(kThreads) void layer_norm_wide_kernel(const XT* __restrict__ x, int64_t ldx,
                                                                    const WT* __restrict__ w,

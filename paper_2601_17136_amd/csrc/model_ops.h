@@ -58,7 +58,8 @@ constexpr int kMaxTop = 256;
 // copies in tiles, at most 256 MB of the logits stored (head.hip).
 enum HeadForm { HEAD_FEW, HEAD_DIRECT, HEAD_TILED };
 constexpr int kFew = 64;
-constexpr int64_t kDirectScores = (int64_t)16 << 20;  // n times classes: 64 MB of scores
+// n times classes: 64 MB of scores (128 MB with their rows padded to 64, of 65 classes)
+constexpr int64_t kDirectScores = (int64_t)16 << 20;
 HeadForm head_form(const HeadArgs& a);
 size_t head_short_scratch(const HeadArgs& a, bool grad);
 hipError_t launch_head_short(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);
