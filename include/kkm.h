@@ -583,9 +583,10 @@ int kkm_head_loss(kkm_ctx *ctx, const kkm_head *head, const int32_t *ids, float 
  * rounded to the operands' 16 bits (fp32: three parts) before its products, of
  * others it stays in fp32.  Binary16's rounding is relative to each row's own
  * dloss; for dw it rounds a row's features too, to 2^-40 of the largest dloss
- * times feature of all rows.  Rows without a label or with dloss_i = 0 take no part: whatever they and their dloss
- * hold, their row of dh is zero.  A dloss that is infinite or NaN spoils its row
- * of dh and dw.  In a row whose target is left out G is zero there. */
+ * times feature of all rows.  Rows without a label or with dloss_i = 0 take no
+ * part: whatever they and their dloss hold, their row of dh is zero.  A dloss that
+ * is infinite or NaN spoils its row of dh, and dw.  In a row whose target is left
+ * out G is zero there. */
 int kkm_head_grad(kkm_ctx *ctx, const kkm_head *head, const int32_t *ids, const float *dloss, float *loss, float *lse,
                   void *dh, int64_t lddh, void *dw, int64_t lddw);
 
