@@ -141,9 +141,11 @@ __device__ inline float pair_key(const FewArgs& a, int64_t at, int& id, bool& ba
 // are bound by reading h: 60000 fp32 rows of 780, 10 classes, 59 us with G, 3.2
 // TB/s, the loss alone 37, 5.0 TB/s.  64 of them by the fp32 matrix instructions:
 // 20000 rows of 784 36 us, 56 TFLOP/s (a pass of 38.9 us is one of 42.5 if held to
-// three wavefronts a SIMD; the others may be).  dH in this launch as well, from G in LDS, read w again for every
-// 32 rows and was slower wherever it was timed: those cases with gradient 158 / 148
-// and 121 / 111, 200 rows of 64 and 20 classes 22.6 / 19.0.
+// three wavefronts a SIMD; the others may be).  dH
+// in this launch as well, from G in LDS, read w again for every 32 rows and was
+// slower in 45 of 47 cases: those two with gradient 158 / 148 and 121 / 111, 200 rows
+// of 64 and 20 classes 22.6 / 19.0, but 20000 bfloat16 rows of 2048, 64 classes 185 /
+// 196.
 template <typename XT, int CT>
 __global__ __launch_bounds__(256, CT == 4 && sizeof(XT) == 4 ? 1 : 3) void scores_few_classes_kernel(FewArgs a) {
   constexpr int NT = 2, S = CT * 16;
