@@ -612,10 +612,81 @@ int kkm_distill_loss(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teac
 int kkm_distill_grad(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teacher, const float *dloss, float *loss,
                      float *lse, void *dh, int64_t lddh, void *dw, int64_t lddw);
 
+/* An update along its orthogonalised momentum.  With X = u / (|u| + eps) (the
+ * root of the sum of squares), or its transpose where u has more rows than
+ * columns, every step is
+ *   A = X X^T,  X <- a X + (b A + c A^2) X
+ * with its own a, b, c: singular values s become a s + b s^3 + c s^5, singular
+ * vectors stay.  batch matrices of m x n, `stride` elements apart, each by itself.
+ *
+ * The products hold fp32's accuracy for every type: a short side of at most 64
+ * runs in 64 bits, others in two binary16 parts (22 bits) of each factor.  Steps
+ * that would let a singular value of at most 1 grow past 2^12 are refused.  A NaN or
+ * infinity spoils its matrix.  Scratch: 24 bytes an entry of matrices more than 64
+ * wide and high (of a batch, as many at a time as 1 GB holds). */
+#define KKM_MAX_STEPS 32
+typedef struct kkm_newton {
+  int32_t steps;      /* in [1, KKM_MAX_STEPS] */
+  const double *coef; /* host, 3 a step: a, b, c */
+  double eps;         /* > 0 */
+} kkm_newton;
+
+/* y = X after the steps, in the orientation of x.  y may be x (with its strides). */
+int kkm_orthogonalize(kkm_ctx *ctx, const kkm_newton *newton, int32_t type, int64_t batch, int64_t m, int64_t n,
+                      const void *x, int64_t ldx, int64_t stride_x, void *y, int64_t ldy, int64_t stride_y);
+
+/* v = momentum v + g;  u = g + momentum v (nesterov) or v;  w = keep w - rate X,
+ * X from u as above.  w and g of one type, v fp32, batch x m x n without gaps.
+ * keep: 1 - rate times the weights' decay, say; a factor for the matrix' shape
+ * goes into rate. */
+int kkm_orthogonal_step(kkm_ctx *ctx, const kkm_newton *newton, int32_t type, int64_t batch, int64_t m, int64_t n,
+                        void *w, int64_t ldw, int64_t stride_w, const void *g, int64_t ldg, int64_t stride_g, float *v,
+                        float momentum, int32_t nesterov, float rate, float keep);
+
+/* Answers from logits.  Row i of z (n x classes) with its lists gives
+ *   p(v) = z(i, v), of an id v that its `given` list names c > 0 times
+ *          (z > 0 ? z / repeat : z repeat) - (presence + c frequency),
+ *   u(v) = scale (p(v) + offset_v + bias(i, v)), each operation rounded to fp32,
+ * and -inf where the row's mask has no bit for v, or offset or bias is -inf,
+ * whatever z holds there.  Then
+ *   out = u rounded to z's type,  ids = the first v of the largest u,
+ *   lse = log sum_v exp u(v),  logp = u(ids) - lse.
+ * A row of which nothing is left has id -1, lse and logp -inf; one with a NaN left,
+ * or whose mask id is >= nmasks (out NaN too), id -1, lse and logp NaN.  An
+ * infinite largest u shares all probability with its equals. */
+#define KKM_MAX_GIVEN ((1 << 20) - 1)
+#define KKM_MAX_BIASES 1000
+typedef struct kkm_choice {
+  int32_t type; /* kkm_type of z and out */
+  int32_t classes;
+  int64_t n;
+  const void *z;
+  int64_t ldz;
+  float scale;          /* 1 / temperature; > 0 */
+  const float *offset;  /* fp32[classes] or NULL */
+  const int32_t *given; /* int32[n x ngiven]; ids outside [0, classes) are none */
+  int32_t ngiven;       /* 0: no lists */
+  float repeat;         /* > 0 */
+  float presence, frequency;
+  const int32_t *bias_ids; /* int32[n x nbias]; ids outside [0, classes) are none; of an id named twice the last counts */
+  const float *bias;       /* fp32[n x nbias] */
+  int32_t nbias;           /* 0: no lists */
+  const uint32_t *masks;   /* nmasks x words: bit v % 32 of word v / 32 allows v; or NULL */
+  int64_t words;           /* >= classes / 32 */
+  int32_t nmasks;
+  const int32_t *mask_ids; /* int32[n]; negative: no mask.  NULL: row i has mask i */
+} kkm_choice;
+
+/* out (n x classes, may be z with its stride), ids (int32[n]), logp and lse
+ * (fp32[n]); each may be NULL. */
+int kkm_choose(kkm_ctx *ctx, const kkm_choice *choice, void *out, int64_t ldo, int32_t *ids, float *logp, float *lse);
+
 /* The checks of these calls that need no context: KKM_OK or KKM_ERR_ARG (the
  * message from kkm_last_error(NULL)).  teacher may be NULL. */
 int kkm_check_norm_args(int32_t type, int64_t n, int32_t d, int64_t ldx, int32_t wtype, float eps);
 int kkm_check_head_args(const kkm_head *head, const kkm_teacher *teacher);
+int kkm_check_newton_args(const kkm_newton *newton, int32_t type, int64_t batch, int64_t m, int64_t n);
+int kkm_check_choice_args(const kkm_choice *choice);
 
 /* The stream of kkm_create. */
 int kkm_get_stream(kkm_ctx *ctx, void **out);

@@ -1,5 +1,6 @@
-// Host side of the model operators: the C ABI of layer norm, the class head
-// and its losses.  Argument checks run before any HIP call; nothing throws.
+// Host side of the model operators: the C ABI of layer norm, the class head and
+// its losses, orthogonalised updates and answers from logits.  Argument checks run
+// before any HIP call; nothing throws.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -14,6 +15,12 @@ namespace {
 const char* kTypes = "F32(0), F16(1) or BF16(2)";
 
 bool is_type(int32_t t) { return t == KKM_F32 || t == KKM_F16 || t == KKM_BF16; }
+
+int missing(kkm_ctx* c, const char* name) { return ctx_fail(c, KKM_ERR_ARG, "%s is NULL", name); }
+
+int done(kkm_ctx* c, hipError_t e, const char* what) {
+  return e == hipSuccess ? KKM_OK : ctx_fail(c, KKM_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
 
 int check_norm(kkm_ctx* c, int32_t type, int64_t n, int32_t d, int32_t wtype) {
   if (!is_type(type)) return ctx_fail(c, KKM_ERR_ARG, "type=%d is not %s", type, kTypes);
@@ -57,10 +64,73 @@ int check_teacher(kkm_ctx* c, const kkm_head* h, const kkm_teacher* t) {
   return KKM_OK;
 }
 
-int missing(kkm_ctx* c, const char* name) { return ctx_fail(c, KKM_ERR_ARG, "%s is NULL", name); }
+int check_newton(kkm_ctx* c, const kkm_newton* w, int32_t type, int64_t batch, int64_t m, int64_t n, NewtonSteps* out) {
+  if (!w) return missing(c, "newton");
+  if (!is_type(type)) return ctx_fail(c, KKM_ERR_ARG, "type=%d is not %s", type, kTypes);
+  if (batch < 0 || batch > KKM_MAX_ROWS)
+    return ctx_fail(c, KKM_ERR_ARG, "batch=%lld must be in [0, %d]", (long long)batch, KKM_MAX_ROWS);
+  if (m < 1 || m > KKM_MAX_FEATURES)
+    return ctx_fail(c, KKM_ERR_ARG, "m=%lld must be in [1, %d]", (long long)m, KKM_MAX_FEATURES);
+  if (n < 1 || n > KKM_MAX_FEATURES)
+    return ctx_fail(c, KKM_ERR_ARG, "n=%lld must be in [1, %d]", (long long)n, KKM_MAX_FEATURES);
+  if (w->steps < 1 || w->steps > KKM_MAX_STEPS)
+    return ctx_fail(c, KKM_ERR_ARG, "steps=%d must be in [1, %d]", w->steps, KKM_MAX_STEPS);
+  if (!w->coef) return missing(c, "coef");
+  if (!(w->eps > 0 && std::isfinite(w->eps)))
+    return ctx_fail(c, KKM_ERR_ARG, "eps=%g must be finite and > 0", w->eps);
+  out->steps = w->steps;
+  for (int i = 0; i < 3 * w->steps; ++i) {
+    if (!std::isfinite(w->coef[i])) return ctx_fail(c, KKM_ERR_ARG, "coef[%d]=%g must be finite", i, w->coef[i]);
+    out->coef[i] = w->coef[i];
+  }
+  if (!newton_in_range(*out))
+    return ctx_fail(c, KKM_ERR_ARG, "these %d steps let singular values grow past 2^12", w->steps);
+  return KKM_OK;
+}
 
-int done(kkm_ctx* c, hipError_t e, const char* what) {
-  return e == hipSuccess ? KKM_OK : ctx_fail(c, KKM_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+int check_apart(kkm_ctx* c, const char* name, int64_t batch, int64_t m, int64_t n, int64_t ld, int64_t stride) {
+  const int64_t least = (m - 1) * ld + n;
+  if (batch > 1 && (stride < least || stride > (int64_t)1 << 41))
+    return ctx_fail(c, KKM_ERR_ARG, "%s=%lld must be in [%lld, 2^41]", name, (long long)stride, (long long)least);
+  return KKM_OK;
+}
+
+int ortho_call(kkm_ctx* c, const char* what, OrthoArgs& a) {
+  void* ws = nullptr;
+  if (const size_t bytes = ortho_scratch(a))
+    if (int rc = ctx_workspace(c, bytes, &ws)) return rc;
+  return done(c, launch_ortho(a, ws, ctx_stream(c)), what);
+}
+
+int check_choice(kkm_ctx* c, const kkm_choice* q) {
+  if (!q) return missing(c, "choice");
+  if (!is_type(q->type)) return ctx_fail(c, KKM_ERR_ARG, "type=%d is not %s", q->type, kTypes);
+  if (q->n < 0 || q->n > KKM_MAX_ROWS)
+    return ctx_fail(c, KKM_ERR_ARG, "n=%lld must be in [0, %d]", (long long)q->n, KKM_MAX_ROWS);
+  if (q->classes < 1 || q->classes > KKM_MAX_ROWS)
+    return ctx_fail(c, KKM_ERR_ARG, "classes=%d must be in [1, %d]", q->classes, KKM_MAX_ROWS);
+  if (int rc = check_ld(c, "ldz", q->ldz, q->classes)) return rc;
+  if (!(q->scale > 0.f && std::isfinite(q->scale)))
+    return ctx_fail(c, KKM_ERR_ARG, "scale=%g must be finite and > 0", (double)q->scale);
+  if (q->ngiven < 0 || q->ngiven > KKM_MAX_GIVEN)
+    return ctx_fail(c, KKM_ERR_ARG, "ngiven=%d must be in [0, %d]", q->ngiven, KKM_MAX_GIVEN);
+  if (!(q->repeat > 0.f && std::isfinite(q->repeat)))
+    return ctx_fail(c, KKM_ERR_ARG, "repeat=%g must be finite and > 0", (double)q->repeat);
+  if (!std::isfinite(q->presence) || !std::isfinite(q->frequency))
+    return ctx_fail(c, KKM_ERR_ARG, "presence=%g and frequency=%g must be finite", (double)q->presence,
+                    (double)q->frequency);
+  if (q->nbias < 0 || q->nbias > KKM_MAX_BIASES)
+    return ctx_fail(c, KKM_ERR_ARG, "nbias=%d must be in [0, %d]", q->nbias, KKM_MAX_BIASES);
+  if (q->masks) {
+    if (q->words < (q->classes + 31) / 32)
+      return ctx_fail(c, KKM_ERR_ARG, "words=%lld must be at least %d", (long long)q->words, (q->classes + 31) / 32);
+    if (q->nmasks < 0) return ctx_fail(c, KKM_ERR_ARG, "nmasks=%d must not be negative", q->nmasks);
+    if (!q->mask_ids && q->nmasks < q->n)
+      return ctx_fail(c, KKM_ERR_ARG, "nmasks=%d must be at least n=%lld without mask_ids", q->nmasks, (long long)q->n);
+  } else if (q->mask_ids) {
+    return missing(c, "masks");
+  }
+  return KKM_OK;
 }
 
 // Both losses; ids alone stand for one pair per row.
@@ -128,6 +198,13 @@ int kkm_check_head_args(const kkm_head* head, const kkm_teacher* teacher) {
   if (int rc = check_head(nullptr, head)) return rc;
   return teacher ? check_teacher(nullptr, head, teacher) : KKM_OK;
 }
+
+int kkm_check_newton_args(const kkm_newton* newton, int32_t type, int64_t batch, int64_t m, int64_t n) {
+  NewtonSteps steps;
+  return check_newton(nullptr, newton, type, batch, m, n, &steps);
+}
+
+int kkm_check_choice_args(const kkm_choice* choice) { return check_choice(nullptr, choice); }
 
 int kkm_get_stream(kkm_ctx* c, void** out) {
   if (!c) return missing(nullptr, "ctx");
@@ -218,6 +295,107 @@ int kkm_distill_grad(kkm_ctx* c, const kkm_head* head, const kkm_teacher* teache
                      float* lse, void* dh, int64_t lddh, void* dw, int64_t lddw) {
   if (c && !teacher) return missing(c, "teacher");
   return head_call(c, "distillation gradient", head, nullptr, teacher, true, dloss, loss, lse, dh, lddh, dw, lddw);
+}
+
+int kkm_orthogonalize(kkm_ctx* c, const kkm_newton* newton, int32_t type, int64_t batch, int64_t m, int64_t n,
+                      const void* x, int64_t ldx, int64_t stride_x, void* y, int64_t ldy, int64_t stride_y) {
+  if (!c) return missing(nullptr, "ctx");
+  OrthoArgs a{};
+  if (int rc = check_newton(c, newton, type, batch, m, n, &a.newton)) return rc;
+  if (int rc = check_ld(c, "ldx", ldx, n)) return rc;
+  if (int rc = check_ld(c, "ldy", ldy, n)) return rc;
+  if (int rc = check_apart(c, "stride_x", batch, m, n, ldx, stride_x)) return rc;
+  if (int rc = check_apart(c, "stride_y", batch, m, n, ldy, stride_y)) return rc;
+  if (batch > 0 && !x) return missing(c, "x");
+  if (batch > 0 && !y) return missing(c, "y");
+  a.type = type;
+  a.batch = batch;
+  a.m = m;
+  a.n = n;
+  a.x = x;
+  a.ldx = ldx;
+  a.stride_x = stride_x;
+  a.y = y;
+  a.ldy = ldy;
+  a.stride_y = stride_y;
+  a.eps = newton->eps;
+  return ortho_call(c, "orthogonalising", a);
+}
+
+int kkm_orthogonal_step(kkm_ctx* c, const kkm_newton* newton, int32_t type, int64_t batch, int64_t m, int64_t n,
+                        void* w, int64_t ldw, int64_t stride_w, const void* g, int64_t ldg, int64_t stride_g, float* v,
+                        float momentum, int32_t nesterov, float rate, float keep) {
+  if (!c) return missing(nullptr, "ctx");
+  OrthoArgs a{};
+  if (int rc = check_newton(c, newton, type, batch, m, n, &a.newton)) return rc;
+  if (int rc = check_ld(c, "ldw", ldw, n)) return rc;
+  if (int rc = check_ld(c, "ldg", ldg, n)) return rc;
+  if (int rc = check_apart(c, "stride_w", batch, m, n, ldw, stride_w)) return rc;
+  if (int rc = check_apart(c, "stride_g", batch, m, n, ldg, stride_g)) return rc;
+  if (!std::isfinite(momentum) || !std::isfinite(rate) || !std::isfinite(keep))
+    return ctx_fail(c, KKM_ERR_ARG, "momentum=%g, rate=%g and keep=%g must be finite", (double)momentum, (double)rate,
+                    (double)keep);
+  if (batch > 0 && !w) return missing(c, "w");
+  if (batch > 0 && !g) return missing(c, "g");
+  if (batch > 0 && !v) return missing(c, "v");
+  a.type = type;
+  a.batch = batch;
+  a.m = m;
+  a.n = n;
+  a.x = g;
+  a.ldx = ldg;
+  a.stride_x = stride_g;
+  a.y = w;
+  a.ldy = ldw;
+  a.stride_y = stride_w;
+  a.v = v;
+  a.momentum = momentum;
+  a.nesterov = nesterov != 0;
+  a.rate = rate;
+  a.keep = keep;
+  a.eps = newton->eps;
+  return ortho_call(c, "orthogonal step", a);
+}
+
+int kkm_choose(kkm_ctx* c, const kkm_choice* q, void* out, int64_t ldo, int32_t* ids, float* logp, float* lse) {
+  if (!c) return missing(nullptr, "ctx");
+  if (int rc = check_choice(c, q)) return rc;
+  if (out)
+    if (int rc = check_ld(c, "ldo", ldo, q->classes)) return rc;
+  if (q->n > 0) {
+    if (!q->z) return missing(c, "z");
+    if (q->ngiven && !q->given) return missing(c, "given");
+    if (q->nbias && !q->bias_ids) return missing(c, "bias_ids");
+    if (q->nbias && !q->bias) return missing(c, "bias");
+  }
+  ChooseArgs a{};
+  a.type = q->type;
+  a.n = q->n;
+  a.classes = q->classes;
+  a.z = q->z;
+  a.ldz = q->ldz;
+  a.scale = q->scale;
+  a.offset = q->offset;
+  a.given = q->given;
+  a.ngiven = q->ngiven;
+  a.repeat = q->repeat;
+  a.presence = q->presence;
+  a.frequency = q->frequency;
+  a.bias_ids = q->bias_ids;
+  a.bias = q->bias;
+  a.nbias = q->nbias;
+  a.masks = q->masks;
+  a.words = q->words;
+  a.nmasks = q->nmasks;
+  a.mask_ids = q->mask_ids;
+  a.out = out;
+  a.ldo = ldo;
+  a.ids = ids;
+  a.logp = logp;
+  a.lse = lse;
+  if (const size_t bytes = choose_scratch(a))
+    if (int rc = ctx_workspace(c, bytes, &a.parts)) return rc;
+  return done(c, launch_choose(a, ctx_stream(c)), "choice");
 }
 
 }  // extern "C"

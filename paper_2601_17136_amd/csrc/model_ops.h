@@ -1,6 +1,7 @@
-// The operators of a model that learns from a clustering: layer norm, and a
-// class head with its losses (cross entropy with ids, distillation from a
-// teacher's top logits).  Declarations shared by their kernels and their C ABI.
+// The operators of a model that learns from a clustering: layer norm, a class
+// head with its losses (cross entropy with ids, distillation from a teacher's top
+// logits), a shared projection with adapters, orthogonalised updates, and answers
+// from logits.  Declarations shared by their kernels and their C ABI.
 #pragma once
 #include "kkm_internal.h"
 
@@ -66,5 +67,60 @@ hipError_t launch_head_short(const HeadArgs& a, bool grad, void* scratch, hipStr
 
 size_t head_scratch(const HeadArgs& a, bool grad);
 hipError_t launch_head(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);
+
+// Newton-Schulz steps: a, b, c of each.
+constexpr int kMaxSteps = 32;
+struct NewtonSteps {
+  double coef[3 * kMaxSteps];
+  int steps;
+};
+bool newton_in_range(const NewtonSteps& c);
+
+// Matrices m x n of a batch, orthogonalised: x into y, or (v not null) y moved
+// along x's momentum.
+struct OrthoArgs {
+  int type;
+  int64_t batch, m, n;
+  const void* x;
+  int64_t ldx, stride_x;
+  void* y;
+  int64_t ldy, stride_y;
+  float* v;  // batch x m x n
+  float momentum, rate, keep;
+  int nesterov;
+  double eps;
+  NewtonSteps newton;
+};
+size_t ortho_scratch(const OrthoArgs& a);
+hipError_t launch_ortho(const OrthoArgs& a, void* scratch, hipStream_t s);
+
+// Answers from logits.
+constexpr int kMaxGiven = 1 << 20, kMaxBiases = 1000;
+struct ChooseArgs {
+  int type;
+  int64_t n;
+  int classes;
+  const void* z;
+  int64_t ldz;
+  float scale;
+  const float* offset;     // per class; may be null
+  const int32_t* given;    // n x ngiven; negative: none
+  int ngiven;
+  float repeat, presence, frequency;
+  const int32_t* bias_ids;  // n x nbias; negative: none
+  const float* bias;
+  int nbias;
+  const uint32_t* masks;  // nmasks x words; may be null
+  int64_t words;
+  int nmasks;
+  const int32_t* mask_ids;  // per row; null: a row its own
+  void* out;                // may be null, as the others
+  int64_t ldo;
+  int32_t* ids;
+  float *logp, *lse;
+  void* parts;  // choose_scratch bytes
+};
+size_t choose_scratch(const ChooseArgs& a);
+hipError_t launch_choose(const ChooseArgs& a, hipStream_t s);
 
 }  // namespace kkm

@@ -1,0 +1,613 @@
+// An update orthogonalised by Newton-Schulz products.  With the short side as
+// rows, X = u / (|u| + eps) and per step
+//   A = X X^T,  X <- a X + (b A + c A^2) X,
+// which brings X's singular values s to a s + b s^3 + c s^5 and keeps its singular
+// vectors.  Two forms:
+//
+// flat (short side at most kFlat): every step is a polynomial of G = u u^T, so the
+//   steps run on the S x S matrix alone, in LDS, and one product Q u ends them.  A
+//   product of polynomials loses what iterated products of X keep (its small
+//   singular values' accuracy is that of their squares), so G, the steps and Q u
+//   are held in 64 bits, on the 64-bit matrix cores: reads of u remain the bound.
+//   |u|^2 is G's trace.
+// tiled: X and X^T as pairs of binary16 parts (pair_tile.h), three launches a
+//   step.  A and A^2 are symmetric, so only tiles on and above their diagonals are
+//   multiplied.  Two parts hold 22 bits at a fixed power of two: a host-side bound
+//   on the singular values after each step keeps every entry in range.  Measured
+//   against 64 bits their error is 0.4 to 0.9 of that of fp32 products.
+#include <algorithm>
+#include <cmath>
+
+#include "model_ops.h"
+#include "pair_tile.h"
+#include "vec_io.h"
+
+namespace kkm {
+
+namespace {
+
+constexpr int kFlat = 64;
+typedef double doublex4 __attribute__((ext_vector_type(4)));
+
+// What is orthogonalised, entry by entry: x itself, or the momentum's step.
+struct Source {
+  const void* x;  // x, or the gradient
+  int64_t ld, stride;
+  float* v;       // null: x itself
+  float momentum;
+  int nesterov;
+  int64_t m, n;
+};
+// v's new value is written where `update`, else v holds it already.
+template <typename T, bool UPDATE>
+__device__ inline float entry(const Source& q, int64_t b, int64_t i, int64_t j) {
+  const float g = (float)((const T*)q.x)[b * q.stride + i * q.ld + j];
+  if (!q.v) return g;
+  float* p = q.v + (b * q.m + i) * q.n + j;
+  float v = *p;
+  if (UPDATE) {
+    v = q.momentum * v + g;
+    *p = v;
+  }
+  return q.nesterov ? g + q.momentum * v : v;
+}
+
+// Where the result goes: y, or w = keep w - rate O.
+struct Target {
+  void* y;
+  int64_t ld, stride;
+  int update;
+  float rate, keep;
+};
+template <typename T>
+__device__ inline void put(const Target& t, int64_t b, int64_t i, int64_t j, float o) {
+  T* p = (T*)t.y + b * t.stride + i * t.ld + j;
+  *p = (T)(t.update ? t.keep * (float)*p - t.rate * o : o);
+}
+
+// ------------------------------------------------------------------ flat
+
+constexpr int kLong = 64, kLongLd = kLong + 4;  // long-side indices of a chunk; its padded rows in LDS
+
+// The chunk [k0, k0 + 64) of the long side into u[short][long], zero elsewhere.
+template <typename T, bool UPDATE, int SB>
+__device__ inline void load_chunk(const Source& q, int64_t b, int64_t k0, bool tall, float (*u)[kLongLd]) {
+  const int S = (int)(tall ? q.n : q.m);
+  const int64_t len = tall ? q.m : q.n;
+  for (int e = threadIdx.x; e < SB * 16 * kLong; e += 256) {
+    const int i = tall ? e % (SB * 16) : e / kLong, k = tall ? e / (SB * 16) : e % kLong;
+    u[i][k] = i < S && k0 + k < len ? (tall ? entry<T, UPDATE>(q, b, k0 + k, i) : entry<T, UPDATE>(q, b, i, k0 + k)) : 0.f;
+  }
+}
+
+// A slab of G: chunks [split * per, ..) of matrix blockIdx.y; the four wavefronts
+// take 16 of a chunk's 64 indices each.
+template <typename T, int SB>
+__global__ __launch_bounds__(256) void flat_gram_kernel(Source q, bool tall, int per, double* __restrict__ slabs) {
+  constexpr int S16 = SB * 16;
+  __shared__ union {
+    float u[S16][kLongLd];
+    double red[S16][S16];
+  } lds;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  const int64_t b = blockIdx.y, len = tall ? q.m : q.n;
+  doublex4 acc[SB][SB];
+#pragma unroll
+  for (int i = 0; i < SB; ++i)
+#pragma unroll
+    for (int j = 0; j < SB; ++j) acc[i][j] = doublex4{0, 0, 0, 0};
+  for (int c = 0; c < per; ++c) {
+    const int64_t k0 = ((int64_t)blockIdx.x * per + c) * kLong;
+    if (k0 >= len) break;
+    __syncthreads();
+    load_chunk<T, true, SB>(q, b, k0, tall, lds.u);
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      double f[SB];
+#pragma unroll
+      for (int i = 0; i < SB; ++i) f[i] = lds.u[i * 16 + l16][wave * 16 + s * 4 + g];
+#pragma unroll
+      for (int i = 0; i < SB; ++i)
+#pragma unroll
+        for (int j = i; j < SB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f64_16x16x4f64(f[i], f[j], acc[i][j], 0, 0, 0);
+    }
+  }
+  for (int o = 0; o < 4; ++o) {
+    __syncthreads();
+    if (wave == o)
+#pragma unroll
+      for (int i = 0; i < SB; ++i)
+#pragma unroll
+        for (int j = i; j < SB; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            double* p = &lds.red[i * 16 + g + 4 * r][j * 16 + l16];
+            *p = o ? *p + acc[i][j][r] : acc[i][j][r];
+          }
+  }
+  __syncthreads();
+  double* out = slabs + (b * gridDim.x + blockIdx.x) * (S16 * S16);
+  for (int e = threadIdx.x; e < S16 * S16; e += 256) {
+    const int i = e / S16, j = e % S16;
+    out[e] = i / 16 <= j / 16 ? lds.red[i][j] : lds.red[j][i];
+  }
+}
+
+// C = A B of symmetric S16 x S16 matrices in LDS, a wavefront's blocks at a time.
+template <int SB, int LD>
+__device__ inline void square_product(const double* A, const double* B, doublex4 (&acc)[(SB * SB + 3) / 4]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int t = 0; t < (SB * SB + 3) / 4; ++t) {
+    const int blk = t * 4 + wave;
+    acc[t] = doublex4{0, 0, 0, 0};
+    if (blk >= SB * SB) continue;
+    const double* pa = A + (blk / SB * 16 + l16) * LD + g;
+    const double* pb = B + (blk % SB * 16 + l16) * LD + g;
+#pragma unroll
+    for (int k = 0; k < SB * 16; k += 4) acc[t] = __builtin_amdgcn_mfma_f64_16x16x4f64(pa[k], pb[k], acc[t], 0, 0, 0);
+  }
+}
+template <int SB, int LD, class F>
+__device__ inline void each_entry(const doublex4 (&acc)[(SB * SB + 3) / 4], F f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int t = 0; t < (SB * SB + 3) / 4; ++t) {
+    const int blk = t * 4 + wave;
+    if (blk >= SB * SB) continue;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = blk / SB * 16 + g + 4 * r, j = blk % SB * 16 + l16;
+      f(i, j, i * LD + j, acc[t][r]);
+    }
+  }
+}
+
+// The steps on G alone: Q with X_last = Q u.
+template <int SB>
+__global__ __launch_bounds__(256) void flat_steps_kernel(const double* __restrict__ slabs, int count, NewtonSteps c,
+                                                         double eps, double* __restrict__ out) {
+  constexpr int S16 = SB * 16, LD = S16 + 2, N = (SB * SB + 3) / 4;
+  __shared__ double A[S16 * LD], P[S16 * LD], Q[S16 * LD];
+  const int64_t b = blockIdx.x;
+  for (int e = threadIdx.x; e < S16 * S16; e += 256) {
+    double s = 0;
+    for (int k = 0; k < count; ++k) s += slabs[(b * count + k) * (S16 * S16) + e];
+    A[e / S16 * LD + e % S16] = s;
+  }
+  __syncthreads();
+  double tr = 0;
+  for (int i = 0; i < S16; ++i) tr += A[i * LD + i];
+  const double inv = 1.0 / (sqrt(tr) + eps);
+  __syncthreads();
+  for (int e = threadIdx.x; e < S16 * S16; e += 256) A[e / S16 * LD + e % S16] *= inv * inv;
+  __syncthreads();
+  doublex4 acc[N];
+  for (int s = 0; s < c.steps; ++s) {
+    square_product<SB, LD>(A, A, acc);
+    const double ca = c.coef[3 * s], cb = c.coef[3 * s + 1], cc = c.coef[3 * s + 2];
+    each_entry<SB, LD>(acc, [&](int i, int j, int at, double v) {
+      P[at] = (i == j ? ca : 0.0) + cb * A[at] + cc * v;
+      if (s == 0) Q[at] = P[at];
+    });
+    __syncthreads();
+    if (s > 0) {
+      square_product<SB, LD>(Q, P, acc);
+      __syncthreads();
+      each_entry<SB, LD>(acc, [&](int, int, int at, double v) { Q[at] = v; });
+    }
+    if (s + 1 == c.steps) break;
+    for (int t = 0; t < 2; ++t) {
+      square_product<SB, LD>(A, P, acc);
+      __syncthreads();
+      each_entry<SB, LD>(acc, [&](int, int, int at, double v) { A[at] = v; });
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < S16 * S16; e += 256) out[b * (S16 * S16) + e] = Q[e / S16 * LD + e % S16] * inv;
+}
+
+// O = Q u, a chunk of the long side at a time; a wavefront has 16 of its indices.
+template <typename T, int SB>
+__global__ __launch_bounds__(256) void flat_apply_kernel(Source q, bool tall, const double* __restrict__ Qs, Target out) {
+  constexpr int S16 = SB * 16, LD = S16 + 2;
+  __shared__ float u[S16][kLongLd];
+  __shared__ double Q[S16 * LD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+  const int64_t b = blockIdx.y, len = tall ? q.m : q.n;
+  const int S = (int)(tall ? q.n : q.m);
+  for (int e = threadIdx.x; e < S16 * S16; e += 256) Q[e / S16 * LD + e % S16] = Qs[b * (S16 * S16) + e];
+  for (int64_t k0 = (int64_t)blockIdx.x * kLong; k0 < len; k0 += (int64_t)gridDim.x * kLong) {
+    __syncthreads();
+    load_chunk<T, false, SB>(q, b, k0, tall, u);
+    __syncthreads();
+    doublex4 acc[SB];
+#pragma unroll
+    for (int i = 0; i < SB; ++i) acc[i] = doublex4{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < S16; j += 4) {
+      const double f = u[j + g][wave * 16 + l16];
+#pragma unroll
+      for (int i = 0; i < SB; ++i)
+        acc[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(Q[(i * 16 + l16) * LD + j + g], f, acc[i], 0, 0, 0);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < SB; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) u[i * 16 + g + 4 * r][wave * 16 + l16] = (float)acc[i][r];
+    __syncthreads();
+    for (int e = threadIdx.x; e < S16 * kLong; e += 256) {
+      const int i = tall ? e % S16 : e / kLong, k = tall ? e / S16 : e % kLong;
+      if (i >= S || k0 + k >= len) continue;
+      if (tall)
+        put<T>(out, b, k0 + k, i, u[i][k]);
+      else
+        put<T>(out, b, i, k0 + k, u[i][k]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ tiled
+
+// Sums of squares of whole rows, a grid apart, in 64 bits; the momentum's new values.
+template <typename T>
+__global__ __launch_bounds__(256) void squares_kernel(Source q, double* __restrict__ part) {
+  __shared__ double red[4];
+  const int64_t b = blockIdx.y;
+  double s = 0;
+  for (int64_t i = blockIdx.x; i < q.m; i += gridDim.x)
+    for (int64_t j = threadIdx.x; j < q.n; j += 256) {
+      const double u = entry<T, true>(q, b, i, j);
+      s += u * u;
+    }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[b * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// Pairs of u / (|u| + eps), 2^exp times: `along`'s rows are u's, `across`'s its columns.
+template <typename T>
+__global__ __launch_bounds__(256) void pairs_kernel(Source q, const double* __restrict__ part, int count, double eps,
+                                                    float up, half_t* along, int64_t ld_along, half_t* across,
+                                                    int64_t ld_across) {
+  __shared__ float tile[64][65];
+  __shared__ double red[4];
+  const int64_t b = blockIdx.z, i0 = (int64_t)blockIdx.y * 64, j0 = (int64_t)blockIdx.x * 64;
+  double s = 0;
+  for (int k = threadIdx.x; k < count; k += 256) s += part[b * count + k];
+#pragma unroll
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  const double norm = sqrt((red[0] + red[1]) + (red[2] + red[3])) + eps;
+  for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+    const int64_t i = i0 + e / 64, j = j0 + e % 64;
+    tile[e / 64][e % 64] = i < q.m && j < q.n ? (float)((double)entry<T, false>(q, b, i, j) / norm) * up : 0.f;
+  }
+  __syncthreads();
+  along += b * q.m * ld_along;
+  across += b * q.n * ld_across;
+  for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+    const int64_t i = i0 + e / 64, j = j0 + e % 64;
+    if (i < q.m && j < ld_along / 2) {
+      half_t* p = along + i * ld_along + pair_at(j);
+      split_pair(tile[e / 64][e % 64], p[0], p[kPairBlock]);
+    }
+    const int64_t c = j0 + e / 64, r = i0 + e % 64;
+    if (c < q.n && r < ld_across / 2) {
+      half_t* p = across + c * ld_across + pair_at(r);
+      split_pair(tile[e % 64][e / 64], p[0], p[kPairBlock]);
+    }
+  }
+}
+
+// A tile's entries v = ca base + cm acc, base a pair matrix of the product's own
+// rows and columns (null: none).  Stored as pairs in the same order (`along`), in
+// the other (`across`), or as the result.
+struct TileArgs {
+  PairSide a, b;
+  int64_t stride_a, stride_b;  // of a matrix of the batch
+  int64_t M, N;
+  int nkb, mt, nt;
+  bool half;                   // symmetric: tiles on and above the diagonal
+  const half_t* base;
+  int64_t ld_base, stride_base;
+  float ca, cm;                // what base's and the sums' stored values are multiplied by
+  half_t *along, *across;
+  int64_t ld_along, ld_across, stride_along, stride_across;
+  Target out;
+};
+
+template <class S, bool LAST, typename OT>
+__global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q) {
+  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  const int64_t bt = blockIdx.y;
+  int mi, ni;
+  if (q.half) {  // tile t of the triangle, by columns: (i, j) with i <= j is t = j (j + 1) / 2 + i
+    const int t = blockIdx.x;
+    int j = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+    while ((j + 1) * (j + 2) / 2 <= t) ++j;
+    while (j * (j + 1) / 2 > t) --j;
+    mi = __builtin_amdgcn_readfirstlane(t - j * (j + 1) / 2);
+    ni = __builtin_amdgcn_readfirstlane(j);
+  } else {
+    tile_of(blockIdx.x, (unsigned)(q.mt * q.nt), q.mt, q.nt, mi, ni);
+  }
+  const int64_t r0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+  PairSide a = q.a, b = q.b;
+  a.p += bt * q.stride_a;
+  b.p += bt * q.stride_b;
+  floatx16 acc[S::WM][S::WN];
+  pair_product<S>(a, b, r0, n0, 0, q.nkb, lds, acc);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
+  const half_t* base = q.base ? q.base + bt * q.stride_base : nullptr;
+  half_t* along = q.along ? q.along + bt * q.stride_along : nullptr;
+  half_t* across = q.across ? q.across + bt * q.stride_across : nullptr;
+#pragma unroll
+  for (int bi = 0; bi < S::WM; ++bi) {
+    const int64_t b0 = r0 + (wm * S::WM + bi) * 32;
+    if (b0 >= q.M) continue;
+#pragma unroll
+    for (int bj = 0; bj < S::WN; ++bj) {
+      const int64_t c0 = n0 + (wn * S::WN + bj) * 32, col = c0 + l32;
+      if (c0 >= q.N) continue;
+      float v[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int64_t row = b0 + acc_row(r, h);
+        v[r] = acc[bi][bj][r] * q.cm;
+        const bool in = row < q.M && col < q.N;
+        if (base && in) {
+          const half_t* p = base + row * q.ld_base + pair_at(col);
+          v[r] += q.ca * ((float)p[0] + (float)p[kPairBlock]);
+        }
+        if (!in) v[r] = 0.f;
+        if (LAST) {
+          if (in) put<OT>(q.out, bt, row, col, v[r]);
+        } else if (row < q.M) {
+          half_t* p = along + row * q.ld_along + pair_at(col);
+          split_pair(v[r], p[0], p[kPairBlock]);
+        }
+      }
+      // (a tile on the diagonal is whole as it is)
+      if (!LAST && col < q.N && !(q.half && mi == ni))
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          typedef half_t half4 __attribute__((ext_vector_type(4)));
+          half4 hi, lo;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            half_t x, y;
+            split_pair(v[r + e], x, y);
+            hi[e] = x, lo[e] = y;
+          }
+          half_t* p = across + col * q.ld_across + pair_at(b0 + acc_row(r, h));
+          *(half4*)p = hi;
+          *(half4*)(p + kPairBlock) = lo;
+        }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t align(size_t v) { return (v + 255) / 256 * 256; }
+
+// The tiled form's layout for one group of matrices.
+struct TiledPlan {
+  int64_t S, len;     // short and long side
+  int64_t ldx, ldxt;  // of X (S rows) and X^T (len rows)
+  int64_t group;      // matrices at a time
+  int parts;
+  size_t x, xt, a, norm, total;  // bytes of one buffer each, and of all
+};
+constexpr size_t kGroupBytes = (size_t)1 << 30;
+TiledPlan tiled_plan(const OrthoArgs& a) {
+  TiledPlan p;
+  p.S = std::min(a.m, a.n);
+  p.len = std::max(a.m, a.n);
+  p.ldx = pair_ld(p.len);
+  p.ldxt = pair_ld(p.S);
+  p.parts = (int)std::min<int64_t>(a.m, 512);
+  const size_t one = (size_t)(2 * p.S * p.ldx + 2 * p.len * p.ldxt + 2 * p.S * p.ldxt) * sizeof(half_t);
+  p.group = std::max<int64_t>(1, std::min<int64_t>({a.batch, (int64_t)(kGroupBytes / one), 65535}));
+  p.x = align((size_t)p.group * p.S * p.ldx * sizeof(half_t));
+  p.xt = align((size_t)p.group * p.len * p.ldxt * sizeof(half_t));
+  p.a = align((size_t)p.group * p.S * p.ldxt * sizeof(half_t));
+  p.norm = align((size_t)p.group * p.parts * sizeof(double));
+  p.total = 2 * (p.x + p.xt + p.a) + p.norm;
+  return p;
+}
+
+int flat_splits(const OrthoArgs& a) {
+  const int64_t chunks = cdiv(std::max(a.m, a.n), kLong);
+  return (int)std::min<int64_t>({chunks, std::max<int64_t>(1, 512 / a.batch), 64});
+}
+int flat_side(const OrthoArgs& a) { return (int)cdiv(std::min(a.m, a.n), 16); }
+bool is_flat(const OrthoArgs& a) { return std::min(a.m, a.n) <= kFlat; }
+constexpr int64_t kBatchLaunch = 65535;
+
+Source source_of(const OrthoArgs& a, int64_t b0) {
+  const size_t size = elem_bytes(a.type);
+  return Source{(const char*)a.x + b0 * a.stride_x * size, a.ldx, a.stride_x, a.v ? a.v + b0 * a.m * a.n : nullptr,
+                a.momentum, a.nesterov, a.m, a.n};
+}
+Target target_of(const OrthoArgs& a, int64_t b0) {
+  return Target{(char*)a.y + b0 * a.stride_y * elem_bytes(a.type), a.ldy, a.stride_y, a.v != nullptr, a.rate, a.keep};
+}
+
+template <typename T, int SB>
+hipError_t launch_flat(const OrthoArgs& a, void* scratch, hipStream_t s) {
+  const int splits = flat_splits(a);
+  const bool tall = a.m > a.n;
+  const int64_t chunks = cdiv(std::max(a.m, a.n), kLong);
+  const int per = (int)cdiv(chunks, splits);
+  const int64_t group = std::min(a.batch, kBatchLaunch);
+  double* slabs = (double*)scratch;
+  double* Q = slabs + group * splits * (SB * SB * 256);
+  const unsigned across = (unsigned)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / std::min<int64_t>(a.batch, 2048)));
+  for (int64_t b0 = 0; b0 < a.batch; b0 += group) {
+    const unsigned nb = (unsigned)std::min(group, a.batch - b0);
+    flat_gram_kernel<T, SB><<<dim3(splits, nb), 256, 0, s>>>(source_of(a, b0), tall, per, slabs);
+    flat_steps_kernel<SB><<<nb, 256, 0, s>>>(slabs, splits, a.newton, a.eps, Q);
+    flat_apply_kernel<T, SB><<<dim3(across, nb), 256, 0, s>>>(source_of(a, b0), tall, Q, target_of(a, b0));
+  }
+  return hipGetLastError();
+}
+
+// The largest magnitude of a s + b s^3 + c s^5 over [0, top], with some room.
+double largest(double a, double b, double c, double top) {
+  double most = 0;
+  for (int i = 0; i <= 4096; ++i) {
+    const double s = top * i / 4096, q = s * s;
+    most = std::max(most, std::fabs(s * (a + q * (b + q * c))));
+  }
+  return most * 1.01 + 1e-6;
+}
+int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(top))); }
+
+template <typename T, class S>
+hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
+  const TiledPlan p = tiled_plan(a);
+  const bool tall = a.m > a.n;
+  char* at = (char*)scratch;
+  auto take = [&](size_t bytes) {
+    half_t* q = (half_t*)at;
+    at += bytes;
+    return q;
+  };
+  half_t *X[2], *XT[2];
+  for (int i = 0; i < 2; ++i) X[i] = take(p.x), XT[i] = take(p.xt);
+  half_t *A = take(p.a), *B = take(p.a);
+  double* norm = (double*)at;
+  const int64_t sx = p.S * p.ldx, sxt = p.len * p.ldxt, sa = p.S * p.ldxt;
+  const int mt = (int)cdiv(p.S, S::BM), nt = (int)cdiv(p.len, S::BN), half_tiles = mt * (mt + 1) / 2;
+  for (int64_t b0 = 0; b0 < a.batch; b0 += p.group) {
+    const unsigned nb = (unsigned)std::min(p.group, a.batch - b0);
+    const Source src = source_of(a, b0);
+    squares_kernel<T><<<dim3(p.parts, nb), 256, 0, s>>>(src, norm);
+    double top = 1.01;  // of X's singular values, and so of its entries
+    int ex = room_for(top);
+    half_t *along = tall ? XT[0] : X[0], *across = tall ? X[0] : XT[0];
+    pairs_kernel<T><<<dim3((unsigned)cdiv(a.n, 64), (unsigned)cdiv(a.m, 64), nb), 256, 0, s>>>(
+        src, norm, p.parts, a.eps, std::ldexp(1.f, ex), along, tall ? p.ldxt : p.ldx, across, tall ? p.ldx : p.ldxt);
+    for (int t = 0; t < a.newton.steps; ++t) {
+      const half_t *x = X[t & 1], *xt = XT[t & 1];
+      const double ca = a.newton.coef[3 * t], cb = a.newton.coef[3 * t + 1], cc = a.newton.coef[3 * t + 2];
+      // B's eigenvalues are b q + c q^2 at q = s^2
+      double most = 0;
+      for (int i = 0; i <= 4096; ++i) {
+        const double v = top * top * i / 4096;
+        most = std::max(most, std::fabs(v * (cb + v * cc)));
+      }
+      const int eb = room_for(most * 1.01 + 1e-6), ea = cc == 0 ? eb : room_for(top * top);
+      TileArgs g{};
+      g.a = g.b = {x, p.ldx, p.S};
+      g.stride_a = g.stride_b = sx;
+      g.M = g.N = p.S;
+      g.nkb = (int)(p.ldx / (2 * kPairBlock));
+      g.mt = g.nt = mt;
+      g.half = true;
+      g.cm = (float)std::ldexp(cc == 0 ? cb : 1.0, ea - 2 * ex);
+      g.along = g.across = cc == 0 ? B : A;
+      g.ld_along = g.ld_across = p.ldxt;
+      g.stride_along = g.stride_across = sa;
+      pair_kernel<S, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
+      if (cc != 0) {
+        g.a = g.b = {A, p.ldxt, p.S};
+        g.stride_a = g.stride_b = sa;
+        g.nkb = (int)(p.ldxt / (2 * kPairBlock));
+        g.base = A;
+        g.ld_base = p.ldxt;
+        g.stride_base = sa;
+        g.ca = (float)std::ldexp(cb, eb - ea);
+        g.cm = (float)std::ldexp(cc, eb - 2 * ea);
+        g.along = g.across = B;
+        pair_kernel<S, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
+      }
+      const bool last = t + 1 == a.newton.steps;
+      top = largest(ca, cb, cc, top);
+      const int en = last ? 0 : room_for(top);  // the result is stored as it is
+      TileArgs m{};
+      const PairSide sb = {B, p.ldxt, p.S}, sxs = {xt, p.ldxt, p.len};
+      const bool turned = last && tall;  // the result's rows are the long side
+      m.a = turned ? sxs : sb;
+      m.b = turned ? sb : sxs;
+      m.stride_a = turned ? sxt : sa;
+      m.stride_b = turned ? sa : sxt;
+      m.M = turned ? p.len : p.S;
+      m.N = turned ? p.S : p.len;
+      m.nkb = (int)(p.ldxt / (2 * kPairBlock));
+      m.mt = turned ? (int)cdiv(p.len, S::BM) : mt;
+      m.nt = turned ? (int)cdiv(p.S, S::BN) : nt;
+      m.base = turned ? xt : x;
+      m.ld_base = turned ? p.ldxt : p.ldx;
+      m.stride_base = turned ? sxt : sx;
+      m.ca = (float)std::ldexp(ca, en - ex);
+      m.cm = (float)std::ldexp(1.0, en - eb - ex);
+      const dim3 grid((unsigned)(m.mt * m.nt), nb);
+      if (last) {
+        m.out = target_of(a, b0);
+        pair_kernel<S, true, T><<<grid, S::threads, 0, s>>>(m);
+      } else {
+        m.along = X[(t + 1) & 1];
+        m.ld_along = p.ldx;
+        m.stride_along = sx;
+        m.across = XT[(t + 1) & 1];
+        m.ld_across = p.ldxt;
+        m.stride_across = sxt;
+        pair_kernel<S, false, float><<<grid, S::threads, 0, s>>>(m);
+      }
+      ex = en;
+    }
+  }
+  return hipGetLastError();
+}
+
+bool big_tiles(const OrthoArgs& a) { return cdiv(std::min(a.m, a.n), 256) * cdiv(std::max(a.m, a.n), 256) * a.batch >= 128; }
+
+template <typename T>
+hipError_t launch_typed(const OrthoArgs& a, void* scratch, hipStream_t s) {
+  if (!is_flat(a)) return big_tiles(a) ? launch_tiled<T, BigTile>(a, scratch, s) : launch_tiled<T, SmallTile>(a, scratch, s);
+  switch (flat_side(a)) {
+    case 1: return launch_flat<T, 1>(a, scratch, s);
+    case 2: return launch_flat<T, 2>(a, scratch, s);
+    case 3: return launch_flat<T, 3>(a, scratch, s);
+    default: return launch_flat<T, 4>(a, scratch, s);
+  }
+}
+
+}  // namespace
+
+// The bound on the singular values after every step that the tiled form's powers
+// of two rest on; false where it is not finite or past 2^12.
+bool newton_in_range(const NewtonSteps& c) {
+  double top = 1.01;
+  for (int t = 0; t < c.steps; ++t) {
+    top = largest(c.coef[3 * t], c.coef[3 * t + 1], c.coef[3 * t + 2], top);
+    if (!(top <= 4096)) return false;
+  }
+  return true;
+}
+
+size_t ortho_scratch(const OrthoArgs& a) {
+  if (a.batch == 0) return 0;
+  if (!is_flat(a)) return tiled_plan(a).total;
+  const int sb = flat_side(a);
+  return (size_t)std::min(a.batch, kBatchLaunch) * (flat_splits(a) + 1) * sb * sb * 256 * sizeof(double);
+}
+
+hipError_t launch_ortho(const OrthoArgs& a, void* scratch, hipStream_t s) {
+  if (a.batch == 0) return hipSuccess;
+  if (a.type == TYPE_F32) return launch_typed<float>(a, scratch, s);
+  return a.type == TYPE_F16 ? launch_typed<half_t>(a, scratch, s) : launch_typed<bf16_t>(a, scratch, s);
+}
+
+}  // namespace kkm

@@ -22,6 +22,9 @@ KKM_MODE_AUTO, KKM_MODE_RESIDENT, KKM_MODE_ONTHEFLY, KKM_MODE_PACKED = 0, 1, 2, 
 KKM_STORE_F32, KKM_STORE_F16 = 0, 1
 KKM_F32, KKM_F16, KKM_BF16 = 0, 1, 2
 KKM_MAX_TOP, KKM_MAX_FEATURES, KKM_MAX_ROWS = 256, 1 << 20, 1 << 21
+KKM_MAX_STEPS, KKM_MAX_GIVEN, KKM_MAX_BIASES = 32, (1 << 20) - 1, 1000
+# Steps that bring singular values from 0.01 .. 1 to 0.7 .. 1.2 in five, and steps that bring them to 1 in the end.
+KKM_QUINTIC, KKM_CUBIC = (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)
 STORAGES = {"f32": KKM_STORE_F32, "f16": KKM_STORE_F16}
 KKM_MAX_K = 1024
 KKM_PACKED_MAX_K = 64
@@ -72,9 +75,23 @@ class kkm_teacher(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class kkm_newton(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("coef", ctypes.POINTER(ctypes.c_double)), ("eps", ctypes.c_double)]
+
+
+class kkm_choice(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("classes", ctypes.c_int32), ("n", ctypes.c_int64), ("z", ctypes.c_void_p),
+                ("ldz", ctypes.c_int64), ("scale", ctypes.c_float), ("offset", ctypes.c_void_p),
+                ("given", ctypes.c_void_p), ("ngiven", ctypes.c_int32), ("repeat", ctypes.c_float),
+                ("presence", ctypes.c_float), ("frequency", ctypes.c_float), ("bias_ids", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("nbias", ctypes.c_int32), ("masks", ctypes.c_void_p),
+                ("words", ctypes.c_int64), ("nmasks", ctypes.c_int32), ("mask_ids", ctypes.c_void_p)]
+
+
 _lib = None
 _vp, _i32, _i64, _f64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
 _f32, _headp, _teacherp = ctypes.c_float, ctypes.POINTER(kkm_head), ctypes.POINTER(kkm_teacher)
+_newtonp, _choicep = ctypes.POINTER(kkm_newton), ctypes.POINTER(kkm_choice)
 _SIGS = {
     "kkm_abi_version": ([], _i32),
     "kkm_last_error": ([_vp], ctypes.c_char_p),
@@ -116,6 +133,12 @@ _SIGS = {
     "kkm_distill_grad": ([_vp, _headp, _teacherp, _vp, _vp, _vp, _vp, _i64, _vp, _i64], _i32),
     "kkm_check_norm_args": ([_i32, _i64, _i32, _i64, _i32, _f32], _i32),
     "kkm_check_head_args": ([_headp, _teacherp], _i32),
+    "kkm_orthogonalize": ([_vp, _newtonp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64], _i32),
+    "kkm_orthogonal_step": ([_vp, _newtonp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _f32, _i32,
+                             _f32, _f32], _i32),
+    "kkm_choose": ([_vp, _choicep, _vp, _i64, _vp, _vp, _vp], _i32),
+    "kkm_check_newton_args": ([_newtonp, _i32, _i64, _i64, _i64], _i32),
+    "kkm_check_choice_args": ([_choicep], _i32),
     "kkm_get_stream": ([_vp, ctypes.POINTER(_vp)], _i32),
 }
 
@@ -651,6 +674,118 @@ def kkm_distill_grad(ctx, h, w, top_ids, top_logits, dloss, loss, lse, dh=None, 
     with _ordered(ctx, h, w, offset, top_ids, top_logits, dloss, loss, lse, dh, dw):
         _check(lib().kkm_distill_grad(ctx, ctypes.byref(a), ctypes.byref(t), _dev_ptr(dloss, f32, "dloss", n),
                                       _dev_ptr(loss, f32, "loss", n), _dev_ptr(lse, f32, "lse", n), *g), ctx)
+
+
+def _matrices(t, name, dtype=None, shape=None):
+    """(address, row stride, matrix stride) of a device matrix, or of a batch of them, with contiguous rows."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name} must be a matrix or a batch of them, got {t.dim()} dimensions")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dim() == 2:
+        p, ld = _rows(t, name, dtype)
+        return p, ld, 0
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    batch, m, n = t.shape
+    stride, ld, step = t.stride()
+    if n > 1 and step != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    if m <= 1:
+        ld = n
+    if ld < n:
+        raise ValueError(f"{name}'s rows overlap (stride {ld}, width {n})")
+    if batch > 1 and stride < (m - 1) * ld + n:
+        raise ValueError(f"{name}'s matrices overlap (stride {stride})")
+    return t.data_ptr(), ld, stride
+
+
+def _newton_args(coef, eps):
+    flat = [float(v) for step in coef for v in step]
+    if len(flat) != 3 * len(coef):
+        raise ValueError("coef must hold three numbers a step")
+    return kkm_newton(len(coef), (ctypes.c_double * max(len(flat), 1))(*flat), float(eps))
+
+
+def _batch_shape(t):
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def kkm_orthogonalize(ctx, x, y, coef=(KKM_QUINTIC,) * 5, eps: float = 1e-7) -> None:
+    """Each matrix of x (m x n, or batch x m x n) divided by the root of its sum of
+    squares + eps and taken through Newton-Schulz steps, into y.  coef: (a, b, c)
+    of each step, X <- a X + (b A + c A A) X with A = X X^T.  y may be x."""
+    px, ldx, sx = _matrices(x, "x")
+    py, ldy, sy = _matrices(y, "y", x.dtype, x.shape)
+    w = _newton_args(coef, eps)
+    with _ordered(ctx, x, y):
+        _check(lib().kkm_orthogonalize(ctx, ctypes.byref(w), _type_code(x.dtype, "x"), *_batch_shape(x), px, ldx, sx,
+                                       py, ldy, sy), ctx)
+
+
+def kkm_orthogonal_step(ctx, w, g, v, rate: float, momentum: float = 0.95, nesterov: bool = True, keep: float = 1.0,
+                        coef=(KKM_QUINTIC,) * 5, eps: float = 1e-7) -> None:
+    """v = momentum v + g, u = g + momentum v (nesterov) or v, w = keep w - rate X with
+    X from u as in kkm_orthogonalize.  w and g (m x n, or batch x m x n) of one dtype,
+    v fp32 and contiguous."""
+    import torch
+    pw, ldw, sw = _matrices(w, "w")
+    pg, ldg, sg = _matrices(g, "g", w.dtype, w.shape)
+    a = _newton_args(coef, eps)
+    with _ordered(ctx, w, g, v):
+        _check(lib().kkm_orthogonal_step(ctx, ctypes.byref(a), _type_code(w.dtype, "w"), *_batch_shape(w), pw, ldw, sw,
+                                         pg, ldg, sg, _dev_ptr(v, torch.float32, "v", w.numel()), float(momentum),
+                                         int(nesterov), float(rate), float(keep)), ctx)
+
+
+def _list_width(t, n, name):
+    """Entries a row of a list matrix (0 of None)."""
+    if t is None:
+        return 0
+    if t.dim() != 2 or t.shape[0] != n:
+        raise ValueError(f"{name} must be a matrix of {n} rows, got shape {tuple(t.shape)}")
+    return t.shape[1]
+
+
+def kkm_choose(ctx, z, out=None, ids=None, logp=None, lse=None, scale: float = 1.0, offset=None, given=None,
+               repeat: float = 1.0, presence: float = 0.0, frequency: float = 0.0, bias_ids=None, bias=None, masks=None,
+               mask_ids=None) -> None:
+    """Answers from logits z (n x classes): penalties for the ids in given (int32, n x
+    any; negative: none), offset (fp32[classes]) and biases (bias of bias_ids, n x any)
+    added, scale, and the bit masks (int32, masks x words) that mask_ids (int32[n];
+    negative: none) names; into out (may be z), the first of the largest ids (int32[n]),
+    logp and lse (fp32[n]); each may be None."""
+    import torch
+    pz, ldz = _rows(z, "z")
+    n, classes = z.shape
+    pout, ldo = _rows(out, "out", z.dtype, z.shape) if out is not None else (None, 0)
+    i32, f32 = torch.int32, torch.float32
+    h, b = _list_width(given, n, "given"), _list_width(bias_ids, n, "bias_ids")
+    if b and bias is None:
+        raise ValueError("bias_ids need bias")
+    if masks is not None and masks.dim() != 2:
+        raise ValueError(f"masks must be a matrix, got {masks.dim()} dimensions")
+    a = kkm_choice(_type_code(z.dtype, "z"), classes, n, pz, ldz, float(scale),
+                   _dev_ptr(offset, f32, "offset", classes), _dev_ptr(given, i32, "given") if h else None, h,
+                   float(repeat), float(presence), float(frequency),
+                   _dev_ptr(bias_ids, i32, "bias_ids") if b else None,
+                   _dev_ptr(bias, f32, "bias", n * b) if b else None, b, _dev_ptr(masks, i32, "masks"),
+                   masks.shape[1] if masks is not None else 0, masks.shape[0] if masks is not None else 0,
+                   _dev_ptr(mask_ids, i32, "mask_ids", n))
+    with _ordered(ctx, z, out, ids, logp, lse, offset, given, bias_ids, bias, masks, mask_ids):
+        _check(lib().kkm_choose(ctx, ctypes.byref(a), pout, ldo, _dev_ptr(ids, i32, "ids", n),
+                                _dev_ptr(logp, f32, "logp", n), _dev_ptr(lse, f32, "lse", n)), ctx)
+
+
+def kkm_check_newton_args(newton: kkm_newton, type_: int, batch: int, m: int, n: int) -> int:
+    return lib().kkm_check_newton_args(ctypes.byref(newton), int(type_), int(batch), int(m), int(n))
+
+
+def kkm_check_choice_args(choice: kkm_choice) -> int:
+    return lib().kkm_check_choice_args(ctypes.byref(choice))
 
 
 def kkm_check_norm_args(type_: int, n: int, d: int, ldx: int, wtype: int, eps: float) -> int:

@@ -1,0 +1,169 @@
+"""Orthogonalised updates against the steps in 64 bits, at the shapes, types and strides where they can go wrong."""
+import pytest
+
+import learn_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+EPS = 1e-7
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU test on a machine without a GPU")
+    from paper_2601_17136_amd import kkm
+    c = kkm.kkm_create(kkm.current_stream_handle())
+    yield c
+    kkm.kkm_destroy(c)
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _stack(batch, m, n, dtype, pad, g, values=None):
+    t = torch.full((batch, m, n + pad), float("nan"), device="cuda", dtype=dtype)[:, :, pad // 2:pad // 2 + n]
+    t.copy_(torch.randn(batch, m, n, device="cuda", generator=g) if values is None else values)
+    return t
+
+
+def _norms(got, want):
+    return float((got.double().cpu() - want).norm())
+
+
+def _bound(u, coef, dtype):
+    """The 64-bit result and the bound of the kernel's error in the Frobenius norm."""
+    want, err = ref.newton(u, coef, EPS)
+    if min(u.shape) <= 64:  # 64 bits but for the result, rounded to fp32
+        err = ref.slope_of(coef) * 1e-12 + ref.U * float(want.norm())
+    return want, err + ref.UNIT[dtype] * float(want.norm()) + ref.STEP[dtype] * want.numel() ** 0.5
+
+
+SHAPES = [(1, 1, 1), (1, 1, 7), (1, 7, 1), (2, 3, 5), (3, 16, 16), (2, 17, 40), (1, 64, 64), (2, 64, 200), (1, 200, 33),
+          (1, 48, 900), (1, 901, 48), (2, 65, 65), (3, 66, 130), (2, 130, 66), (1, 128, 128), (2, 129, 257),
+          (1, 300, 301), (2, 257, 65), (1, 520, 700), (1, 1000, 65), (1, 32, 5000), (1, 5003, 64), (1, 777, 1001)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("batch,m,n", SHAPES)
+def test_orthogonalize(ctx, batch, m, n, dtype):
+    from paper_2601_17136_amd import kkm
+    t, g = DTYPES[dtype], _gen(m * 131 + n)
+    pad = (m + n) % 4
+    print(f"[gpu] orthogonalize {batch} x {m} x {n} {dtype} pad={pad}", flush=True)
+    x = _stack(batch, m, n, t, pad, g)
+    y = _stack(batch, m, n, t, 3 - pad, g)
+    coef = [kkm.KKM_QUINTIC] * 5
+    kkm.kkm_orthogonalize(ctx, x, y, eps=EPS)
+    for i in range(batch):
+        want, tol = _bound(x[i], coef, t)
+        off = _norms(y[i], want)
+        assert off <= tol, (i, off, tol)
+    # the same bits again, in place, and alone
+    z = x.clone()
+    kkm.kkm_orthogonalize(ctx, z, z, eps=EPS)
+    assert torch.equal(z, y)
+    if batch > 1 and min(m, n) > 64:
+        kkm.kkm_orthogonalize(ctx, x[1], z[1], eps=EPS)
+        assert torch.equal(z[1], y[1])
+
+
+@pytest.mark.parametrize("coef", ["cubic", "one", "mixed"])
+@pytest.mark.parametrize("m,n", [(5, 9), (40, 300), (70, 90), (200, 100)])
+def test_steps_of_each_kind(ctx, m, n, coef):
+    """Cubic steps (no A^2), a single step, and steps that differ."""
+    from paper_2601_17136_amd import kkm
+    steps = {"cubic": [kkm.KKM_CUBIC] * 30, "one": [(2.0, -1.5, 0.5)],
+             "mixed": [(3.0, -3.2, 1.2), kkm.KKM_CUBIC, (0.5, 0.25, 0.0), (-1.0, 0.5, -0.125)]}[coef]
+    x = torch.randn(m, n, device="cuda", generator=_gen(m))
+    y = torch.empty_like(x)
+    kkm.kkm_orthogonalize(ctx, x, y, coef=steps, eps=EPS)
+    want, tol = _bound(x, steps, torch.float32)
+    assert _norms(y, want) <= tol
+    if coef == "cubic":  # singular values become 1 (30 steps from at least 0.003: 1.5^15 of it, then quadratic)
+        s = torch.linalg.svdvals(y.double().cpu())
+        assert float((s - 1).abs().max()) < 1e-4
+
+
+def test_large_matrices(ctx):
+    """Tiles of 256 x 256, wide and tall."""
+    from paper_2601_17136_amd import kkm
+    for m, n in ((2050, 4100), (4100, 2050)):
+        x = torch.randn(m, n, device="cuda", generator=_gen(m)).bfloat16()
+        y = torch.empty(m, n, device="cuda", dtype=torch.bfloat16)
+        print(f"[gpu] orthogonalize {m} x {n}", flush=True)
+        kkm.kkm_orthogonalize(ctx, x, y, eps=EPS)
+        want, tol = _bound(x, [kkm.KKM_QUINTIC] * 5, torch.bfloat16)
+        assert _norms(y, want) <= tol
+
+
+def test_scales_zeros_and_nan(ctx):
+    """The scale of x is no matter, nor are entries whose squares pass fp32's range; zeros stay; a NaN spoils its own matrix."""
+    from paper_2601_17136_amd import kkm
+    for m, n in ((6, 50), (80, 70)):
+        x = torch.randn(5, m, n, device="cuda", generator=_gen(3))
+        x[1] = x[0] * 2.0 ** 80
+        x[2] = x[0] * 2.0 ** -60
+        x[3] = 0.0
+        x[4, m - 1, n - 1] = float("nan")
+        y = torch.empty_like(x)
+        kkm.kkm_orthogonalize(ctx, x, y, eps=1e-30)
+        assert torch.equal(y[1], y[0]) and not y[3].any() and torch.isnan(y[4]).any()
+        want, _ = ref.newton(x[0], [kkm.KKM_QUINTIC] * 5, 1e-30)
+        assert _norms(y[0], want) < 1e-4 * float(want.norm()) and _norms(y[2], want) < 1e-4 * float(want.norm())
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("batch,m,n", [(1, 1, 1), (3, 8, 100), (2, 100, 8), (1, 64, 64), (2, 65, 90), (1, 300, 200),
+                                       (1, 129, 640)])
+def test_step(ctx, batch, m, n, dtype, nesterov):
+    from paper_2601_17136_amd import kkm
+    t, g = DTYPES[dtype], _gen(m + 7 * n)
+    w, grad = _stack(batch, m, n, t, 1, g), _stack(batch, m, n, t, 2, g)
+    v = torch.randn(batch, m, n, device="cuda", generator=g)
+    w0, v0 = w.double().cpu(), v.double().cpu()
+    mu, rate, keep = 0.9, 0.25, 0.875
+    for k in range(2):
+        kkm.kkm_orthogonal_step(ctx, w, grad, v, rate, momentum=mu, nesterov=nesterov, keep=keep, eps=EPS)
+        gd = grad.double().cpu()
+        v1 = mu * v0 + gd
+        # mu is fp32's nearest; a product and a sum rounded
+        assert bool(((v.double().cpu() - v1).abs() <= 3 * ref.U * (mu * v0.abs() + gd.abs() + v1.abs())).all())
+        vk = v.double().cpu()
+        u = gd + mu * vk if nesterov else vk
+        du = 3 * ref.U * float((gd.abs() + vk.abs()).norm())  # u's entries, as v's
+        for i in range(batch):
+            want, tol = _bound(u[i], [kkm.KKM_QUINTIC] * 5, torch.float32)
+            tol += ref.slope_of([kkm.KKM_QUINTIC] * 5) * 2 * du / float(u[i].norm())
+            new = keep * w0[i] - rate * want
+            size = (keep * w0[i]).norm() + rate * want.norm()
+            bound = rate * tol + 3 * ref.U * float(size) + ref.UNIT[t] * float(new.norm()) + ref.STEP[t] * new.numel() ** 0.5
+            assert _norms(w[i], new) <= bound, (k, i)
+        w0, v0 = w.double().cpu(), vk
+
+
+def test_more_matrices_than_a_launch_takes(ctx):
+    from paper_2601_17136_amd import kkm
+    x = torch.randn(70001, 2, 3, device="cuda", generator=_gen(5))
+    y = torch.empty_like(x)
+    kkm.kkm_orthogonalize(ctx, x, y, eps=EPS)
+    for i in (0, 1, 65534, 65535, 65536, 70000):
+        want, tol = _bound(x[i], [kkm.KKM_QUINTIC] * 5, torch.float32)
+        assert _norms(y[i], want) <= tol
+    assert not torch.isnan(y).any()
+
+
+def test_groups_of_a_large_batch(ctx):
+    """Scratch holds a part of the batch at a time: 24 bytes an entry, 1 GB."""
+    from paper_2601_17136_amd import kkm
+    x = torch.randn(300, 400, 400, device="cuda", generator=_gen(6)).bfloat16()
+    y = torch.empty_like(x)
+    kkm.kkm_orthogonalize(ctx, x, y, eps=EPS)
+    one = torch.empty_like(x[0])
+    for i in (0, 137, 299):
+        want, tol = _bound(x[i], [kkm.KKM_QUINTIC] * 5, torch.bfloat16)
+        assert _norms(y[i], want) <= tol
