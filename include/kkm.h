@@ -612,6 +612,45 @@ int kkm_distill_loss(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teac
 int kkm_distill_grad(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teacher, const float *dloss, float *loss,
                      float *lse, void *dh, int64_t lddh, void *dw, int64_t lddw);
 
+/* A projection that all rows share, with a low-rank adapter for each row (of its
+ * source, or its request):
+ *   y_i = w x_i + f_g up_g (down_g x_i),  g = ids_i,
+ * n rows of x, d wide, into rows of y, m wide; w (m x d), `adapters` matrices down
+ * (rank x d) and up (m x rank), one after another without gaps, all of one type.
+ * factor (fp32[adapters], may be NULL: ones) holds f.  A row of negative id has no
+ * adapter; one whose id is >= adapters is NaN.  What an adapter holds reaches its own
+ * rows alone.  fp32 operands of large products are three bfloat16 parts, as the
+ * head's. */
+#define KKM_MAX_RANK 128
+#define KKM_MAX_ADAPTERS 1024
+typedef struct kkm_adapted {
+  int32_t type; /* kkm_type of x, w, down, up, y and the gradients */
+  int32_t d;
+  int64_t n, m;
+  const void *x;
+  int64_t ldx;
+  const void *w;
+  int64_t ldw;
+  int32_t adapters, rank;
+  const void *down, *up;
+  const int32_t *ids;
+  const float *factor;
+} kkm_adapted;
+
+/* Scratch: 12 bytes a row, 4 a row and rank (padded to 16, 32, 64 or 128); and copies
+ * of x and w where the product runs in tiles and they are fp32 (6 bytes an entry) or
+ * not aligned to 16 bytes (2). */
+int kkm_adapted_linear(kkm_ctx *ctx, const kkm_adapted *a, void *y, int64_t ldy);
+
+/* The gradient from dy (n x m); w, which the rows share, is held:
+ *   dx_i = w^T dy_i + down_g^T u_i with u_i = f_g up_g^T dy_i,
+ *   ddown_g = sum_{i: ids_i = g} u_i x_i^T,  dup_g = sum_{i: ids_i = g} f_g dy_i (down_g x_i)^T
+ * into dx (n x d), ddown and dup (as down and up); each may be NULL.  Adapters without
+ * rows have zeros, as all have where n = 0.  Rows of an id >= adapters have dx NaN and
+ * take no other part. */
+int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, int64_t lddy, void *dx, int64_t lddx,
+                            void *ddown, void *dup);
+
 /* An update along its orthogonalised momentum.  With X = u / (|u| + eps) (the
  * root of the sum of squares), or its transpose where u has more rows than
  * columns, every step is
@@ -685,6 +724,7 @@ int kkm_choose(kkm_ctx *ctx, const kkm_choice *choice, void *out, int64_t ldo, i
  * message from kkm_last_error(NULL)).  teacher may be NULL. */
 int kkm_check_norm_args(int32_t type, int64_t n, int32_t d, int64_t ldx, int32_t wtype, float eps);
 int kkm_check_head_args(const kkm_head *head, const kkm_teacher *teacher);
+int kkm_check_adapted_args(const kkm_adapted *a);
 int kkm_check_newton_args(const kkm_newton *newton, int32_t type, int64_t batch, int64_t m, int64_t n);
 int kkm_check_choice_args(const kkm_choice *choice);
 

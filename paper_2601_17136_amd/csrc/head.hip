@@ -73,17 +73,6 @@ __device__ inline int top_level(const unsigned* __restrict__ level) {
 
 // ------------------------------------------------------------------ operands
 
-template <typename E, int P>
-__device__ inline void split_planes(float x, E (&out)[P]) {
-  out[0] = (E)x;
-  if constexpr (P == 3) {
-    const bool fin = isfinite((float)out[0]);
-    const float r = fin ? x - (float)out[0] : 0.f;
-    out[1] = (E)r;
-    out[2] = (E)(r - (float)out[1]);
-  }
-}
-
 // A launch's work-items are a 32-bit count: a job of more than so many workgroups
 // of 256 goes over its items with what it has.
 constexpr int64_t kMaxBlocks = (int64_t)1 << 22;

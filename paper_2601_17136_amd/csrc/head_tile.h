@@ -15,6 +15,12 @@ struct Side {
   int64_t ld, plane;  // elements
   int64_t rows;
 };
+// Rows of a taken in another order, row i being row order[i] of memory; all of them lie
+// within 2 GB of p.
+struct InOrder {
+  const int32_t* order;
+};
+struct AsTheyAre {};
 
 // fp32 operands are three bfloat16 planes (hi, mid, lo: 24 bits, fp32's range),
 // and their product the six plane products above 2^-24 of it, small ones first.
@@ -32,6 +38,18 @@ __device__ inline floatx16 mfma16(f16x8 a, f16x8 b, floatx16 c) {
 }
 __device__ inline floatx16 mfma16(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// x as P parts of type E, each the rest of those before rounded.
+template <typename E, int P>
+__device__ inline void split_planes(float x, E (&out)[P]) {
+  out[0] = (E)x;
+  if constexpr (P == 3) {
+    const bool fin = isfinite((float)out[0]);
+    const float r = fin ? x - (float)out[0] : 0.f;
+    out[1] = (E)r;
+    out[2] = (E)(r - (float)out[1]);
+  }
 }
 
 constexpr int kChunkK = 64;  // contraction indices of a chunk, to which operands are padded
@@ -66,9 +84,9 @@ __device__ inline void wait_loads() { __builtin_amdgcn_s_waitcnt(7 << 4); }  // 
 // contraction indices past K read zero.  Chunk c + 1 is requested
 // while chunk c is multiplied; a step's operands are read from LDS while the
 // step before is multiplied, across the chunk's one barrier too.
-template <typename E, class S>
+template <typename E, class S, class Rows = AsTheyAre>
 __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, int64_t col0, int K, int nkc, int nseg,
-                                    int c0, int c1, char* lds, floatx16 (&acc)[S::WM][S::WN]) {
+                                    int c0, int c1, char* lds, floatx16 (&acc)[S::WM][S::WN], Rows rows = {}) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host pass knows no buffer resources)
   constexpr unsigned kBound = 0x7ffffff0u, kOut = 0x80000000u;
   constexpr int NS = kChunkK / 16, L = S::LA + S::LB;
@@ -81,7 +99,10 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
 #pragma unroll
   for (int j = 0; j < S::LA; ++j) {
     const int64_t r = row0 + (wave * S::LA + j) * S::group + lrow;
-    va[j] = (unsigned)((min(r, a.rows - 1) - row0) * a.ld * 2) + slot(j) * 16;
+    if constexpr (std::is_same<Rows, InOrder>::value)
+      va[j] = (unsigned)(rows.order[min(r, a.rows - 1)] * a.ld * 2) + slot(j) * 16;
+    else
+      va[j] = (unsigned)((min(r, a.rows - 1) - row0) * a.ld * 2) + slot(j) * 16;
   }
 #pragma unroll
   for (int j = 0; j < S::LB; ++j) {
@@ -107,7 +128,7 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
     char* st = lds + fst * S::stage_bytes;
     const int so = fk * S::row_bytes;
     if (j < S::LA) {
-      auto r = base(a, nseg > 1 ? seg_a(fs) : 0, row0);
+      auto r = base(a, nseg > 1 ? seg_a(fs) : 0, std::is_same<Rows, InOrder>::value ? 0 : row0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(st + (wave * S::LA + j) * 1024), 16,
                                                slot(j) * 8 < left ? va[j] : kOut, so, 0, 0);
     } else {

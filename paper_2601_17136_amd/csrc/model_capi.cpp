@@ -1,6 +1,6 @@
 // Host side of the model operators: the C ABI of layer norm, the class head and
-// its losses, orthogonalised updates and answers from logits.  Argument checks run
-// before any HIP call; nothing throws.
+// its losses, adapted projections, orthogonalised updates and answers from logits.
+// Argument checks run before any HIP call; nothing throws.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -62,6 +62,51 @@ int check_teacher(kkm_ctx* c, const kkm_head* h, const kkm_teacher* t) {
     return ctx_fail(c, KKM_ERR_ARG, "n=%lld times m=%d must be below 2^31", (long long)h->n, t->m);
   if (!std::isfinite(t->scale)) return ctx_fail(c, KKM_ERR_ARG, "teacher's scale=%g must be finite", (double)t->scale);
   return KKM_OK;
+}
+
+int check_adapted(kkm_ctx* c, const kkm_adapted* a) {
+  if (!a) return missing(c, "adapted");
+  if (!is_type(a->type)) return ctx_fail(c, KKM_ERR_ARG, "type=%d is not %s", a->type, kTypes);
+  if (a->d < 1 || a->d > KKM_MAX_FEATURES)
+    return ctx_fail(c, KKM_ERR_ARG, "d=%d must be in [1, %d]", a->d, KKM_MAX_FEATURES);
+  if (a->n < 0 || a->n > KKM_MAX_ROWS)
+    return ctx_fail(c, KKM_ERR_ARG, "n=%lld must be in [0, %d]", (long long)a->n, KKM_MAX_ROWS);
+  if (a->m < 1 || a->m > KKM_MAX_FEATURES)
+    return ctx_fail(c, KKM_ERR_ARG, "m=%lld must be in [1, %d]", (long long)a->m, KKM_MAX_FEATURES);
+  if (a->adapters < 1 || a->adapters > KKM_MAX_ADAPTERS)
+    return ctx_fail(c, KKM_ERR_ARG, "adapters=%d must be in [1, %d]", a->adapters, KKM_MAX_ADAPTERS);
+  if (a->rank < 1 || a->rank > KKM_MAX_RANK)
+    return ctx_fail(c, KKM_ERR_ARG, "rank=%d must be in [1, %d]", a->rank, KKM_MAX_RANK);
+  if (int rc = check_ld(c, "ldx", a->ldx, a->d)) return rc;
+  return check_ld(c, "ldw", a->ldw, a->d);
+}
+
+int adapted_call(kkm_ctx* c, const char* what, const kkm_adapted* q, bool grad, AdaptArgs& a) {
+  a.type = q->type;
+  a.n = q->n;
+  a.d = q->d;
+  a.m = (int)q->m;
+  a.x = q->x;
+  a.ldx = q->ldx;
+  a.w = q->w;
+  a.ldw = q->ldw;
+  a.adapters = q->adapters;
+  a.rank = q->rank;
+  a.down = q->down;
+  a.up = q->up;
+  a.ids = q->ids;
+  a.factor = q->factor;
+  if (a.n > 0) {
+    if (!a.x) return missing(c, "x");
+    if (!a.w) return missing(c, "w");
+    if (!a.down) return missing(c, "down");
+    if (!a.up) return missing(c, "up");
+    if (!a.ids) return missing(c, "ids");
+  }
+  void* ws = nullptr;
+  if (const size_t bytes = adapt_scratch(a, grad))
+    if (int rc = ctx_workspace(c, bytes, &ws)) return rc;
+  return done(c, launch_adapt(a, grad, ws, ctx_stream(c)), what);
 }
 
 int check_newton(kkm_ctx* c, const kkm_newton* w, int32_t type, int64_t batch, int64_t m, int64_t n, NewtonSteps* out) {
@@ -199,6 +244,8 @@ int kkm_check_head_args(const kkm_head* head, const kkm_teacher* teacher) {
   return teacher ? check_teacher(nullptr, head, teacher) : KKM_OK;
 }
 
+int kkm_check_adapted_args(const kkm_adapted* a) { return check_adapted(nullptr, a); }
+
 int kkm_check_newton_args(const kkm_newton* newton, int32_t type, int64_t batch, int64_t m, int64_t n) {
   NewtonSteps steps;
   return check_newton(nullptr, newton, type, batch, m, n, &steps);
@@ -295,6 +342,37 @@ int kkm_distill_grad(kkm_ctx* c, const kkm_head* head, const kkm_teacher* teache
                      float* lse, void* dh, int64_t lddh, void* dw, int64_t lddw) {
   if (c && !teacher) return missing(c, "teacher");
   return head_call(c, "distillation gradient", head, nullptr, teacher, true, dloss, loss, lse, dh, lddh, dw, lddw);
+}
+
+int kkm_adapted_linear(kkm_ctx* c, const kkm_adapted* q, void* y, int64_t ldy) {
+  if (!c) return missing(nullptr, "ctx");
+  if (int rc = check_adapted(c, q)) return rc;
+  if (int rc = check_ld(c, "ldy", ldy, q->m)) return rc;
+  if (q->n == 0) return KKM_OK;
+  if (!y) return missing(c, "y");
+  AdaptArgs a{};
+  a.y = y;
+  a.ldy = ldy;
+  return adapted_call(c, "adapted projection", q, false, a);
+}
+
+int kkm_adapted_linear_grad(kkm_ctx* c, const kkm_adapted* q, const void* dy, int64_t lddy, void* dx, int64_t lddx,
+                            void* ddown, void* dup) {
+  if (!c) return missing(nullptr, "ctx");
+  if (int rc = check_adapted(c, q)) return rc;
+  if (int rc = check_ld(c, "lddy", lddy, q->m)) return rc;
+  if (dx)
+    if (int rc = check_ld(c, "lddx", lddx, q->d)) return rc;
+  if (q->n > 0 && !dy) return missing(c, "dy");
+  if (!dx && !ddown && !dup) return KKM_OK;
+  AdaptArgs a{};
+  a.dy = dy;
+  a.lddy = lddy;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.ddown = ddown;
+  a.dup = dup;
+  return adapted_call(c, "adapted projection's gradient", q, true, a);
 }
 
 int kkm_orthogonalize(kkm_ctx* c, const kkm_newton* newton, int32_t type, int64_t batch, int64_t m, int64_t n,

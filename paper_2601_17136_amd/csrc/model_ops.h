@@ -68,6 +68,28 @@ hipError_t launch_head_short(const HeadArgs& a, bool grad, void* scratch, hipStr
 size_t head_scratch(const HeadArgs& a, bool grad);
 hipError_t launch_head(const HeadArgs& a, bool grad, void* scratch, hipStream_t s);
 
+// A shared projection with a low-rank adapter for each row, and its gradient.
+constexpr int kMaxRank = 128, kMaxAdapters = 1024;
+struct AdaptArgs {
+  int type;
+  int64_t n;
+  int d, m;
+  const void *x, *w;
+  int64_t ldx, ldw;
+  int adapters, rank;
+  const void *down, *up;  // adapters x rank x d, adapters x m x rank
+  const int32_t* ids;     // per row; negative: none
+  const float* factor;    // per adapter; null: 1
+  void* y;
+  int64_t ldy;
+  const void* dy;  // gradient only, as what follows
+  int64_t lddy;
+  void *dx, *ddown, *dup;  // each may be null
+  int64_t lddx;
+};
+size_t adapt_scratch(const AdaptArgs& a, bool grad);
+hipError_t launch_adapt(const AdaptArgs& a, bool grad, void* scratch, hipStream_t s);
+
 // Newton-Schulz steps: a, b, c of each.
 constexpr int kMaxSteps = 32;
 struct NewtonSteps {

@@ -22,6 +22,7 @@ KKM_MODE_AUTO, KKM_MODE_RESIDENT, KKM_MODE_ONTHEFLY, KKM_MODE_PACKED = 0, 1, 2, 
 KKM_STORE_F32, KKM_STORE_F16 = 0, 1
 KKM_F32, KKM_F16, KKM_BF16 = 0, 1, 2
 KKM_MAX_TOP, KKM_MAX_FEATURES, KKM_MAX_ROWS = 256, 1 << 20, 1 << 21
+KKM_MAX_RANK, KKM_MAX_ADAPTERS = 128, 1024
 KKM_MAX_STEPS, KKM_MAX_GIVEN, KKM_MAX_BIASES = 32, (1 << 20) - 1, 1000
 # Steps that bring singular values from 0.01 .. 1 to 0.7 .. 1.2 in five, and steps that bring them to 1 in the end.
 KKM_QUINTIC, KKM_CUBIC = (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)
@@ -75,6 +76,13 @@ class kkm_teacher(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class kkm_adapted(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("d", ctypes.c_int32), ("n", ctypes.c_int64), ("m", ctypes.c_int64),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("w", ctypes.c_void_p), ("ldw", ctypes.c_int64),
+                ("adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("down", ctypes.c_void_p),
+                ("up", ctypes.c_void_p), ("ids", ctypes.c_void_p), ("factor", ctypes.c_void_p)]
+
+
 class kkm_newton(ctypes.Structure):
     _fields_ = [("steps", ctypes.c_int32), ("coef", ctypes.POINTER(ctypes.c_double)), ("eps", ctypes.c_double)]
 
@@ -91,7 +99,7 @@ class kkm_choice(ctypes.Structure):
 _lib = None
 _vp, _i32, _i64, _f64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
 _f32, _headp, _teacherp = ctypes.c_float, ctypes.POINTER(kkm_head), ctypes.POINTER(kkm_teacher)
-_newtonp, _choicep = ctypes.POINTER(kkm_newton), ctypes.POINTER(kkm_choice)
+_adaptedp, _newtonp, _choicep = ctypes.POINTER(kkm_adapted), ctypes.POINTER(kkm_newton), ctypes.POINTER(kkm_choice)
 _SIGS = {
     "kkm_abi_version": ([], _i32),
     "kkm_last_error": ([_vp], ctypes.c_char_p),
@@ -133,10 +141,13 @@ _SIGS = {
     "kkm_distill_grad": ([_vp, _headp, _teacherp, _vp, _vp, _vp, _vp, _i64, _vp, _i64], _i32),
     "kkm_check_norm_args": ([_i32, _i64, _i32, _i64, _i32, _f32], _i32),
     "kkm_check_head_args": ([_headp, _teacherp], _i32),
+    "kkm_adapted_linear": ([_vp, _adaptedp, _vp, _i64], _i32),
+    "kkm_adapted_linear_grad": ([_vp, _adaptedp, _vp, _i64, _vp, _i64, _vp, _vp], _i32),
     "kkm_orthogonalize": ([_vp, _newtonp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64], _i32),
     "kkm_orthogonal_step": ([_vp, _newtonp, _i32, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _f32, _i32,
                              _f32, _f32], _i32),
     "kkm_choose": ([_vp, _choicep, _vp, _i64, _vp, _vp, _vp], _i32),
+    "kkm_check_adapted_args": ([_adaptedp], _i32),
     "kkm_check_newton_args": ([_newtonp, _i32, _i64, _i64, _i64], _i32),
     "kkm_check_choice_args": ([_choicep], _i32),
     "kkm_get_stream": ([_vp, ctypes.POINTER(_vp)], _i32),
@@ -676,6 +687,46 @@ def kkm_distill_grad(ctx, h, w, top_ids, top_logits, dloss, loss, lse, dh=None, 
                                       _dev_ptr(loss, f32, "loss", n), _dev_ptr(lse, f32, "lse", n), *g), ctx)
 
 
+def _adapted_args(x, w, down, up, ids, factor):
+    import torch
+    px, ldx = _rows(x, "x")
+    pw, ldw = _rows(w, "w", x.dtype)
+    n, d = x.shape
+    m = w.shape[0]
+    if w.shape[1] != d:
+        raise ValueError(f"w must be as wide as x ({d}), got {w.shape[1]}")
+    if down.dim() != 3 or down.shape[2] != d:
+        raise ValueError(f"down must have shape (adapters, rank, {d}), got {tuple(down.shape)}")
+    s, rank, _ = down.shape
+    if up.shape != (s, m, rank):
+        raise ValueError(f"up must have shape {(s, m, rank)}, got {tuple(up.shape)}")
+    return kkm_adapted(_type_code(x.dtype, "x"), d, n, m, px, ldx, pw, ldw, s, rank, _dev_ptr(down, x.dtype, "down"),
+                       _dev_ptr(up, x.dtype, "up"), _dev_ptr(ids, torch.int32, "ids", n),
+                       _dev_ptr(factor, torch.float32, "factor", s))
+
+
+def kkm_adapted_linear(ctx, x, w, down, up, ids, y, factor=None) -> None:
+    """y = x w^T, and for a row i of adapter g = ids[i] (int32[n]; negative: none)
+    factor[g] up[g] (down[g] x_i) added, into y (n x m).  down: adapters x rank x d,
+    up: adapters x m x rank, contiguous, of x's dtype; factor: fp32[adapters] or None."""
+    a = _adapted_args(x, w, down, up, ids, factor)
+    py, ldy = _rows(y, "y", x.dtype, (x.shape[0], w.shape[0]))
+    with _ordered(ctx, x, w, down, up, ids, y, factor):
+        _check(lib().kkm_adapted_linear(ctx, ctypes.byref(a), py, ldy), ctx)
+
+
+def kkm_adapted_linear_grad(ctx, x, w, down, up, ids, dy, dx=None, ddown=None, dup=None, factor=None) -> None:
+    """The gradient of kkm_adapted_linear from dy (n x m) by x, down and up, into dx,
+    ddown and dup (each may be None); w is held."""
+    a = _adapted_args(x, w, down, up, ids, factor)
+    pdy, lddy = _rows(dy, "dy", x.dtype, (x.shape[0], w.shape[0]))
+    pdx, lddx = _rows(dx, "dx", x.dtype, x.shape) if dx is not None else (None, 0)
+    with _ordered(ctx, x, w, down, up, ids, dy, dx, ddown, dup, factor):
+        _check(lib().kkm_adapted_linear_grad(ctx, ctypes.byref(a), pdy, lddy, pdx, lddx,
+                                             _dev_ptr(ddown, x.dtype, "ddown", down.numel()),
+                                             _dev_ptr(dup, x.dtype, "dup", up.numel())), ctx)
+
+
 def _matrices(t, name, dtype=None, shape=None):
     """(address, row stride, matrix stride) of a device matrix, or of a batch of them, with contiguous rows."""
     import torch
@@ -778,6 +829,10 @@ def kkm_choose(ctx, z, out=None, ids=None, logp=None, lse=None, scale: float = 1
     with _ordered(ctx, z, out, ids, logp, lse, offset, given, bias_ids, bias, masks, mask_ids):
         _check(lib().kkm_choose(ctx, ctypes.byref(a), pout, ldo, _dev_ptr(ids, i32, "ids", n),
                                 _dev_ptr(logp, f32, "logp", n), _dev_ptr(lse, f32, "lse", n)), ctx)
+
+
+def kkm_check_adapted_args(adapted: kkm_adapted) -> int:
+    return lib().kkm_check_adapted_args(ctypes.byref(adapted))
 
 
 def kkm_check_newton_args(newton: kkm_newton, type_: int, batch: int, m: int, n: int) -> int:

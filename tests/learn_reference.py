@@ -116,3 +116,56 @@ def slope_of(coef):
         slope *= float((a + 3 * b * s ** 2 + 5 * c * s ** 4).abs().max())
         top = max(float((a * s + b * s ** 3 + c * s ** 5).abs().max()), 1e-30) * (1 + 1e-6)
     return slope
+
+
+# ------------------------------------------------------------------ adapted projection
+
+def _sums(terms, dtype):
+    from model_reference import sum_error
+    return sum_error(terms, dtype)
+
+
+def adapted(x, w, down, up, ids, factor, dy):
+    """(y, dx, ddown, dup and a bound of each, entry by entry) in 64 bits, where the inputs are."""
+    dtype = x.dtype
+    x, w, down, up, dy = (v.double() for v in (x, w, down, up, dy))
+    n, d = x.shape
+    m = w.shape[0]
+    s, r, _ = down.shape
+    f = torch.ones(s, dtype=torch.float64, device=x.device) if factor is None else factor.double()
+    out = {"y": x @ w.t(), "dx": dy @ w, "ddown": torch.zeros_like(down), "dup": torch.zeros_like(up)}
+    tol = {"y": _sums(d, dtype) * (x.abs() @ w.abs().t()), "dx": _sums(m, dtype) * (dy.abs() @ w.abs()),
+           "ddown": torch.zeros_like(down), "dup": torch.zeros_like(up)}
+    for g in range(s):
+        i = torch.nonzero(ids == g)[:, 0]
+        if i.numel() == 0:
+            continue
+        # t and u: a sum of the width, times f; the second product r terms more; a gradient the rows' sum
+        t, u = f[g] * (x[i] @ down[g].t()), f[g] * (dy[i] @ up[g])
+        dt = f[g].abs() * (_sums(d, torch.float32) + 4 * U) * (x[i].abs() @ down[g].abs().t())
+        du = f[g].abs() * (_sums(m, torch.float32) + 4 * U) * (dy[i].abs() @ up[g].abs())
+        low, rows = (r + 8) * 2 * U, (i.numel() / 4 + 40) * 2 * U
+        out["y"][i] += t @ up[g].t()
+        tol["y"][i] += (dt + low * t.abs()) @ up[g].abs().t()
+        out["dx"][i] += u @ down[g]
+        tol["dx"][i] += (du + low * u.abs()) @ down[g].abs()
+        out["ddown"][g] = u.t() @ x[i]
+        tol["ddown"][g] = (du + rows * u.abs()).t() @ x[i].abs()
+        out["dup"][g] = dy[i].t() @ t
+        tol["dup"][g] = dy[i].abs().t() @ (dt + rows * t.abs())
+    bad = torch.nonzero(ids >= s)[:, 0]
+    out["y"][bad] = torch.nan
+    out["dx"][bad] = torch.nan
+    for k, v in out.items():
+        tol[k] += (UNIT[dtype] + 4 * U) * v.abs() + STEP[dtype]
+    return out, tol
+
+
+def check(name, got, want, tol):
+    got = got.double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), name
+    fine = ~torch.isnan(want)
+    off = (got - want).abs()[fine]
+    worst = float((off / tol[fine].clamp(min=1e-300)).max()) if off.numel() else 0.0
+    assert worst <= 1, (name, worst)
+    return worst

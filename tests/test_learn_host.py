@@ -27,6 +27,26 @@ def test_newton_argument_checks(coef, eps, args, ok):
     assert ok or kkm.kkm_last_error()
 
 
+def _adapted(**kw):
+    a = dict(type=kkm.KKM_BF16, d=8, n=10, m=4, x=None, ldx=8, w=None, ldw=8, adapters=3, rank=2, down=None, up=None,
+             ids=None, factor=None)
+    a.update(kw)
+    return kkm.kkm_adapted(*[a[f] for f, _ in kkm.kkm_adapted._fields_])
+
+
+@pytest.mark.parametrize("change,ok", [
+    ({}, True), ({"n": 0}, True), ({"ldx": 100}, True), ({"type": -1}, False), ({"d": 0}, False),
+    ({"d": kkm.KKM_MAX_FEATURES + 1}, False), ({"n": -1}, False), ({"n": kkm.KKM_MAX_ROWS + 1}, False), ({"m": 0}, False),
+    ({"m": kkm.KKM_MAX_FEATURES + 1}, False), ({"ldx": 7}, False), ({"ldw": 7}, False), ({"adapters": 0}, False),
+    ({"adapters": kkm.KKM_MAX_ADAPTERS}, True), ({"adapters": kkm.KKM_MAX_ADAPTERS + 1}, False), ({"rank": 0}, False),
+    ({"rank": kkm.KKM_MAX_RANK}, True), ({"rank": kkm.KKM_MAX_RANK + 1}, False),
+])
+def test_adapted_argument_checks(change, ok):
+    rc = kkm.kkm_check_adapted_args(_adapted(**change))
+    assert rc == (kkm.KKM_OK if ok else kkm.KKM_ERR_ARG)
+    assert ok or kkm.kkm_last_error()
+
+
 def _choice(**kw):
     a = dict(type=kkm.KKM_F32, classes=70, n=10, z=None, ldz=70, scale=1.0, offset=None, given=None, ngiven=0, repeat=1.0,
              presence=0.0, frequency=0.0, bias_ids=None, bias=None, nbias=0, masks=None, words=0, nmasks=0, mask_ids=None)
@@ -56,6 +76,8 @@ def test_limits_match_the_header():
     import os
     src = open(os.path.join(os.path.dirname(kkm.__file__), "..", "include", "kkm.h")).read()
     assert f"#define KKM_MAX_STEPS {kkm.KKM_MAX_STEPS}" in src and f"#define KKM_MAX_BIASES {kkm.KKM_MAX_BIASES}" in src
+    assert f"#define KKM_MAX_RANK {kkm.KKM_MAX_RANK}" in src
+    assert f"#define KKM_MAX_ADAPTERS {kkm.KKM_MAX_ADAPTERS}" in src
     assert "#define KKM_MAX_GIVEN ((1 << 20) - 1)" in src and kkm.KKM_MAX_GIVEN == (1 << 20) - 1
 
 
@@ -65,6 +87,10 @@ def test_null_context_is_rejected_without_a_gpu():
     assert L.kkm_orthogonal_step(None, ctypes.byref(w), 0, 1, 1, 1, None, 1, 1, None, 1, 1, None, 0.9, 1, 0.1,
                                  1.0) == kkm.KKM_ERR_ARG
     assert L.kkm_choose(None, ctypes.byref(q), None, 70, None, None, None) == kkm.KKM_ERR_ARG
+    a = _adapted()
+    assert L.kkm_adapted_linear(None, ctypes.byref(a), None, 4) == kkm.KKM_ERR_ARG
+    assert L.kkm_adapted_linear_grad(None, ctypes.byref(a), None, 4, None, 8, None, None) == kkm.KKM_ERR_ARG
+    assert L.kkm_check_adapted_args(None) == kkm.KKM_ERR_ARG
     assert L.kkm_check_newton_args(None, 0, 1, 1, 1) == kkm.KKM_ERR_ARG
     assert L.kkm_check_choice_args(None) == kkm.KKM_ERR_ARG
 
@@ -77,6 +103,8 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         kkm.kkm_orthogonal_step(None, x, x, x, 0.1)
     with pytest.raises(TypeError):
         kkm.kkm_choose(None, x)
+    with pytest.raises(TypeError):
+        kkm.kkm_adapted_linear(None, x, x, x[None], x[None], x[:, 0].int(), x)
     with pytest.raises(ValueError):
         kkm._newton_args([(1.0, 2.0)], 1e-7)
 
@@ -108,6 +136,24 @@ def test_calls_refuse_wrong_arguments():
         with pytest.raises(kkm.KKMError):
             kkm.kkm_orthogonal_step(c, y, x, v, float("nan"))
         assert not y.any() and not v.any()
+        p, w, down, up = torch.randn(6, 8, **f), torch.randn(5, 8, **f), torch.randn(3, 2, 8, **f), torch.randn(3, 5, 2, **f)
+        q, one = torch.zeros(6, 5, **f), torch.zeros(6, dtype=torch.int32, **f)
+        good = dict(x=p, w=w, down=down, up=up, ids=one, y=q)
+        for kw, exc in [(dict(w=w.half()), TypeError), (dict(w=w[:, :7]), ValueError), (dict(down=down[:, :, :7]), ValueError),
+                        (dict(down=down[0]), ValueError), (dict(down=down[:2]), ValueError), (dict(up=up[:, :4]), ValueError),
+                        (dict(up=up.half()), TypeError), (dict(down=down.transpose(0, 1).contiguous().transpose(0, 1)), ValueError),
+                        (dict(ids=one.long()), TypeError), (dict(ids=one[:5]), ValueError), (dict(y=q[:, :4]), ValueError),
+                        (dict(factor=torch.ones(2, **f)), ValueError), (dict(factor=torch.ones(3, **f).half()), TypeError),
+                        (dict(down=down[:, :0], up=up[:, :, :0]), kkm.KKMError)]:
+            with pytest.raises(exc):
+                kkm.kkm_adapted_linear(c, **{**good, **kw})
+        assert not q.any()
+        for kw, exc in [(dict(dx=p[:5]), ValueError), (dict(ddown=down[:2]), ValueError), (dict(dup=up.half()), TypeError),
+                        (dict(dy=q[:5]), ValueError)]:
+            with pytest.raises(exc):
+                kkm.kkm_adapted_linear_grad(c, **{"dy": q, **{k: v for k, v in good.items() if k != "y"}, **kw})
+        kkm.kkm_adapted_linear(c, **good)
+        assert q.any()
         z, ids = torch.randn(6, 40, **f), torch.zeros(6, dtype=torch.int32, **f)
         out, lists = torch.zeros(6, 40, **f), torch.zeros(6, 3, dtype=torch.int32, **f)
         for kw, exc in [(dict(out=out.half()), TypeError), (dict(out=out[:5]), ValueError), (dict(ids=ids.long()), TypeError),
