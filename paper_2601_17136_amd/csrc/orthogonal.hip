@@ -64,6 +64,27 @@ __device__ inline void put(const Target& t, int64_t b, int64_t i, int64_t j, flo
   T* p = (T*)t.y + b * t.stride + i * t.ld + j;
   *p = (T)(t.update ? t.keep * (float)*p - t.rate * o : o);
 }
+// `count` of 8 neighbouring entries of a row.
+template <typename T>
+__device__ inline void put(const Target& t, int64_t b, int64_t i, int64_t j, int count, const float (&o)[8]) {
+  T* p = (T*)t.y + b * t.stride + i * t.ld + j;
+  raw_n<8, T> v;
+  if (t.update) {
+    const raw_n<8, T> w = load_n<8>(p, 0, count);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (T)(t.keep * (float)w[k] - t.rate * o[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (T)o[k];
+  }
+  if (count == 8) {
+    *(any_n<8, T>*)p = v;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < count) p[k] = v[k];
+  }
+}
 
 // ------------------------------------------------------------------ flat
 
@@ -252,17 +273,43 @@ __global__ __launch_bounds__(256) void flat_apply_kernel(Source q, bool tall, co
 
 // ------------------------------------------------------------------ tiled
 
+// Eight entries of u, the row's from j on (zero past its end).
+template <typename T, bool UPDATE>
+__device__ inline void entries(const Source& q, int64_t b, int64_t i, int64_t j, float (&u)[8]) {
+  const int left = (int)min(q.n - j, (int64_t)8);
+  const raw_n<8, T> g = load_n<8>((const T*)q.x + b * q.stride + i * q.ld + j, 0, left);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) u[k] = (float)g[k];
+  if (!q.v) return;
+  float* p = q.v + (b * q.m + i) * q.n + j;
+  raw_n<8, float> v = load_n<8>(p, 0, left);
+  if (UPDATE) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = q.momentum * v[k] + u[k];
+    if (left == 8) {
+      *(any_n<8, float>*)p = v;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < left) p[k] = v[k];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) u[k] = q.nesterov ? u[k] + q.momentum * v[k] : v[k];
+}
+
 // Sums of squares of whole rows, a grid apart, in 64 bits; the momentum's new values.
 template <typename T>
 __global__ __launch_bounds__(256) void squares_kernel(Source q, double* __restrict__ part) {
   __shared__ double red[4];
-  const int64_t b = blockIdx.y;
+  const int64_t b = blockIdx.y, per = (q.n + 7) / 8;
   double s = 0;
-  for (int64_t i = blockIdx.x; i < q.m; i += gridDim.x)
-    for (int64_t j = threadIdx.x; j < q.n; j += 256) {
-      const double u = entry<T, true>(q, b, i, j);
-      s += u * u;
-    }
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < q.m * per; e += (int64_t)gridDim.x * 256) {
+    float u[8];
+    entries<T, true>(q, b, e / per, e % per * 8, u);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += (double)u[k] * (double)u[k];
+  }
 #pragma unroll
   for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -285,24 +332,41 @@ __global__ __launch_bounds__(256) void pairs_kernel(Source q, const double* __re
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
   const double norm = sqrt((red[0] + red[1]) + (red[2] + red[3])) + eps;
-  for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-    const int64_t i = i0 + e / 64, j = j0 + e % 64;
-    tile[e / 64][e % 64] = i < q.m && j < q.n ? (float)((double)entry<T, false>(q, b, i, j) / norm) * up : 0.f;
+  for (int e = threadIdx.x; e < 64 * 8; e += 256) {
+    const int lr = e / 8, lc = e % 8 * 8;
+    const int64_t i = i0 + lr, j = j0 + lc;
+    float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (i < q.m && j < q.n) entries<T, false>(q, b, i, j, u);
+    f16x8 hi, lo;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float v = j + k < q.n ? (float)((double)u[k] / norm) * up : 0.f;
+      tile[lr][lc + k] = v;
+      half_t x, y;
+      split_pair(v, x, y);
+      hi[k] = x, lo[k] = y;
+    }
+    if (i < q.m && j < ld_along / 2) {
+      half_t* p = along + (b * q.m + i) * ld_along + pair_at(j);
+      *(f16x8*)p = hi;
+      *(f16x8*)(p + kPairBlock) = lo;
+    }
   }
   __syncthreads();
-  along += b * q.m * ld_along;
-  across += b * q.n * ld_across;
-  for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-    const int64_t i = i0 + e / 64, j = j0 + e % 64;
-    if (i < q.m && j < ld_along / 2) {
-      half_t* p = along + i * ld_along + pair_at(j);
-      split_pair(tile[e / 64][e % 64], p[0], p[kPairBlock]);
+  for (int e = threadIdx.x; e < 64 * 8; e += 256) {
+    const int lc = e / 8, lr = e % 8 * 8;
+    const int64_t c = j0 + lc, r = i0 + lr;
+    if (c >= q.n || r >= ld_across / 2) continue;
+    f16x8 hi, lo;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      half_t x, y;
+      split_pair(tile[lr + k][lc], x, y);
+      hi[k] = x, lo[k] = y;
     }
-    const int64_t c = j0 + e / 64, r = i0 + e % 64;
-    if (c < q.n && r < ld_across / 2) {
-      half_t* p = across + c * ld_across + pair_at(r);
-      split_pair(tile[e % 64][e / 64], p[0], p[kPairBlock]);
-    }
+    half_t* p = across + (b * q.n + c) * ld_across + pair_at(r);
+    *(f16x8*)p = hi;
+    *(f16x8*)(p + kPairBlock) = lo;
   }
 }
 
@@ -323,9 +387,14 @@ struct TileArgs {
   Target out;
 };
 
-template <class S, bool LAST, typename OT>
+// The sums pass through LDS, 32 rows of each of the workgroup's GM at a time, so that
+// base is read and every result written 16 bytes a lane, whole 128-byte blocks in both
+// orders.
+template <class S, int NP, bool LAST, typename OT>
 __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q) {
-  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  constexpr int LD = S::BN + 4, ROWS = S::GM * 32;
+  constexpr int kBytes = S::lds_bytes > ROWS * LD * 4 ? S::lds_bytes : ROWS * LD * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[kBytes];
   const int64_t bt = blockIdx.y;
   int mi, ni;
   if (q.half) {  // tile t of the triangle, by columns: (i, j) with i <= j is t = j (j + 1) / 2 + i
@@ -343,53 +412,76 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
   a.p += bt * q.stride_a;
   b.p += bt * q.stride_b;
   floatx16 acc[S::WM][S::WN];
-  pair_product<S>(a, b, r0, n0, 0, q.nkb, lds, acc);
+  pair_product<S, NP>(a, b, r0, n0, 0, q.nkb, lds, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
   const half_t* base = q.base ? q.base + bt * q.stride_base : nullptr;
   half_t* along = q.along ? q.along + bt * q.stride_along : nullptr;
   half_t* across = q.across ? q.across + bt * q.stride_across : nullptr;
+  const bool whole = !(q.half && mi == ni);  // (a tile on the diagonal is whole as it is)
+  float* sums = (float*)lds;
 #pragma unroll
   for (int bi = 0; bi < S::WM; ++bi) {
-    const int64_t b0 = r0 + (wm * S::WM + bi) * 32;
-    if (b0 >= q.M) continue;
+    if (bi) __syncthreads();
 #pragma unroll
-    for (int bj = 0; bj < S::WN; ++bj) {
-      const int64_t c0 = n0 + (wn * S::WN + bj) * 32, col = c0 + l32;
-      if (c0 >= q.N) continue;
-      float v[16];
+    for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t row = b0 + acc_row(r, h);
-        v[r] = acc[bi][bj][r] * q.cm;
-        const bool in = row < q.M && col < q.N;
-        if (base && in) {
-          const half_t* p = base + row * q.ld_base + pair_at(col);
-          v[r] += q.ca * ((float)p[0] + (float)p[kPairBlock]);
+      for (int r = 0; r < 16; ++r)
+        sums[(wm * 32 + acc_row(r, h)) * LD + (wn * S::WN + bj) * 32 + l32] = acc[bi][bj][r];
+    __syncthreads();
+#pragma unroll
+    for (int e = threadIdx.x; e < ROWS * (S::BN / 8); e += S::threads) {
+      const int lr = e / (S::BN / 8), lc = e % (S::BN / 8) * 8;
+      const int64_t row = r0 + (lr / 32 * S::WM + bi) * 32 + lr % 32, col = n0 + lc;
+      float* p = sums + lr * LD + lc;
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = p[k] * q.cm;
+      const bool in = row < q.M && col < q.N;
+      if (base && in) {
+        const half_t* from = base + row * q.ld_base + pair_at(col);
+        const f16x8 hi = *(const f16x8*)from, lo = *(const f16x8*)(from + kPairBlock);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += q.ca * ((float)hi[k] + (float)lo[k]);
+      }
+      if constexpr (LAST) {
+        if (in) put<OT>(q.out, bt, row, col, (int)min(q.N - col, (int64_t)8), v);
+      } else {
+        f16x8 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (!(row < q.M && col + k < q.N)) v[k] = 0.f;
+          half_t x, y;
+          split_pair(v[k], x, y);
+          hi[k] = x, lo[k] = y;
+          p[k] = v[k];
         }
-        if (!in) v[r] = 0.f;
-        if (LAST) {
-          if (in) put<OT>(q.out, bt, row, col, v[r]);
-        } else if (row < q.M) {
-          half_t* p = along + row * q.ld_along + pair_at(col);
-          split_pair(v[r], p[0], p[kPairBlock]);
+        if (row < q.M && col < q.ld_along / 2) {
+          half_t* to = along + row * q.ld_along + pair_at(col);
+          *(f16x8*)to = hi;
+          *(f16x8*)(to + kPairBlock) = lo;
         }
       }
-      // (a tile on the diagonal is whole as it is)
-      if (!LAST && col < q.N && !(q.half && mi == ni))
+    }
+    if constexpr (!LAST) {
+      __syncthreads();
+      if (whole)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          typedef half_t half4 __attribute__((ext_vector_type(4)));
-          half4 hi, lo;
+        for (int e = threadIdx.x; e < S::BN * (ROWS / 8); e += S::threads) {
+          // four neighbouring lanes have 32 rows of a column
+          const int lc = e / 4 % S::BN, lr = (e / 4 / S::BN * 4 + e % 4) * 8;
+          const int64_t row = r0 + (lr / 32 * S::WM + bi) * 32 + lr % 32, col = n0 + lc;
+          if (col >= q.N || row >= q.ld_across / 2) continue;
+          f16x8 hi, lo;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int k = 0; k < 8; ++k) {
             half_t x, y;
-            split_pair(v[r + e], x, y);
-            hi[e] = x, lo[e] = y;
+            split_pair(sums[(lr + k) * LD + lc], x, y);
+            hi[k] = x, lo[k] = y;
           }
-          half_t* p = across + col * q.ld_across + pair_at(b0 + acc_row(r, h));
-          *(half4*)p = hi;
-          *(half4*)(p + kPairBlock) = lo;
+          half_t* to = across + col * q.ld_across + pair_at(row);
+          *(f16x8*)to = hi;
+          *(f16x8*)(to + kPairBlock) = lo;
         }
     }
   }
@@ -415,7 +507,7 @@ TiledPlan tiled_plan(const OrthoArgs& a) {
   p.len = std::max(a.m, a.n);
   p.ldx = pair_ld(p.len);
   p.ldxt = pair_ld(p.S);
-  p.parts = (int)std::min<int64_t>(a.m, 512);
+  p.parts = (int)std::min<int64_t>(cdiv(a.m * cdiv(a.n, 8), 256), 1024);
   const size_t one = (size_t)(2 * p.S * p.ldx + 2 * p.len * p.ldxt + 2 * p.S * p.ldxt) * sizeof(half_t);
   p.group = std::max<int64_t>(1, std::min<int64_t>({a.batch, (int64_t)(kGroupBytes / one), 65535}));
   p.x = align((size_t)p.group * p.S * p.ldx * sizeof(half_t));
@@ -473,6 +565,15 @@ double largest(double a, double b, double c, double top) {
 }
 int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(top))); }
 
+// Products of parts that a result of type T is worth.  A bfloat16 result is rounded
+// to 2^-9 of itself, 0.0017 in the 2-norm, so X enters its Gram matrix by hi alone (11
+// bits: 0.0003 to 0.0006 of the result) and, beside a X of both parts, its product
+// with B (0.0003 to 0.001 more), where all parts take 12 products of S x S x len, these 8.
+template <typename T>
+constexpr int kGramParts = std::is_same<T, bf16_t>::value ? 1 : 3;
+template <typename T>
+constexpr int kMoveParts = std::is_same<T, bf16_t>::value ? 2 : 3;
+
 template <typename T, class S>
 hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
   const TiledPlan p = tiled_plan(a);
@@ -519,7 +620,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       g.along = g.across = cc == 0 ? B : A;
       g.ld_along = g.ld_across = p.ldxt;
       g.stride_along = g.stride_across = sa;
-      pair_kernel<S, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
+      pair_kernel<S, kGramParts<T>, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
       if (cc != 0) {
         g.a = g.b = {A, p.ldxt, p.S};
         g.stride_a = g.stride_b = sa;
@@ -530,7 +631,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
         g.ca = (float)std::ldexp(cb, eb - ea);
         g.cm = (float)std::ldexp(cc, eb - 2 * ea);
         g.along = g.across = B;
-        pair_kernel<S, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
+        pair_kernel<S, 3, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
       }
       const bool last = t + 1 == a.newton.steps;
       top = largest(ca, cb, cc, top);
@@ -555,7 +656,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       const dim3 grid((unsigned)(m.mt * m.nt), nb);
       if (last) {
         m.out = target_of(a, b0);
-        pair_kernel<S, true, T><<<grid, S::threads, 0, s>>>(m);
+        pair_kernel<S, kMoveParts<T>, true, T><<<grid, S::threads, 0, s>>>(m);
       } else {
         m.along = X[(t + 1) & 1];
         m.ld_along = p.ldx;
@@ -563,7 +664,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
         m.across = XT[(t + 1) & 1];
         m.ld_across = p.ldxt;
         m.stride_across = sxt;
-        pair_kernel<S, false, float><<<grid, S::threads, 0, s>>>(m);
+        pair_kernel<S, kMoveParts<T>, false, float><<<grid, S::threads, 0, s>>>(m);
       }
       ex = en;
     }
@@ -571,11 +672,20 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
   return hipGetLastError();
 }
 
-bool big_tiles(const OrthoArgs& a) { return cdiv(std::min(a.m, a.n), 256) * cdiv(std::max(a.m, a.n), 256) * a.batch >= 128; }
+int64_t tiles_of(const OrthoArgs& a, int side) {
+  return cdiv(std::min(a.m, a.n), side) * cdiv(std::max(a.m, a.n), side) * a.batch;
+}
+using Pair256 = PairShape<BigTile, 2>;                  // 128 KB
+using Pair128 = PairShape<SmallTile, 3>;                // 96 KB
+using Pair64 = PairShape<TileShape<1, 1, 2, 2>, 4>;     // 64 KB
 
 template <typename T>
 hipError_t launch_typed(const OrthoArgs& a, void* scratch, hipStream_t s) {
-  if (!is_flat(a)) return big_tiles(a) ? launch_tiled<T, BigTile>(a, scratch, s) : launch_tiled<T, SmallTile>(a, scratch, s);
+  if (!is_flat(a)) {
+    if (tiles_of(a, 256) >= 128) return launch_tiled<T, Pair256>(a, scratch, s);
+    if (tiles_of(a, 128) >= 256) return launch_tiled<T, Pair128>(a, scratch, s);
+    return launch_tiled<T, Pair64>(a, scratch, s);
+  }
   switch (flat_side(a)) {
     case 1: return launch_flat<T, 1>(a, scratch, s);
     case 2: return launch_flat<T, 2>(a, scratch, s);

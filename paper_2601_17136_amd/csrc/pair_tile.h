@@ -25,16 +25,28 @@ __device__ inline void split_pair(float v, half_t& hi, half_t& lo) {
   lo = (half_t)(v - (float)hi);
 }
 
+// Tiles of pairs: a TileShape whose blocks lie in NST stages of LDS.
+template <class S_, int NST_>
+struct PairShape : S_ {
+  static constexpr int NST = NST_;
+  static constexpr int lds_bytes = S_::stage_bytes * NST_;
+  static constexpr int per_cu = lds_bytes <= 80 * 1024 ? 2 : 1;
+};
+
 // acc = the tile at rows row0 of a and col0 of b over blocks [c0, c1) of the
-// contraction.  Rows past an operand's end read its last one.  As tile_product: the
-// next block is requested while one is multiplied, a step's operands are read from
-// LDS during the step before, across the block's one barrier too.
-template <class S>
+// contraction.  NP products of parts: 3, or of a's both and b's hi (2), or of hi and
+// hi (1).  Rows past an operand's end read its last one.  Loads go straight to LDS,
+// NST - 1 blocks ahead; a step's operands are read from LDS during the step before,
+// across the block's one barrier too.
+template <class S, int NP>
 __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_t row0, int64_t col0, int c0, int c1,
                                     char* lds, floatx16 (&acc)[S::WM][S::WN]) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host pass knows no buffer resources)
   constexpr unsigned kBound = 0x7ffffff0u;
-  constexpr int L = S::LA + S::LB, F = S::WM + S::WN, per = S::WM * S::WN;
+  constexpr int L = S::LA + S::LB, F = S::WM + S::WN, per = S::WM * S::WN, NST = S::NST;
+  constexpr int M = NP * per, R = F + (NP > 1 ? S::WM : 0) + (NP > 2 ? S::WN : 0);  // products and reads of a step
+  constexpr int kAhead = (NST - 2) * L;  // loads that may be on their way when a block has to be there
+  static_assert(kAhead < 64, "what the counter holds");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
   const int lrow = lane / S::slots;
@@ -69,49 +81,55 @@ __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_
           rb, (lds_void*)(st + S::BM * S::row_bytes + (wave * S::LB + j - S::LA) * 1024), 16, vb[j - S::LA], so, 0, 0);
   };
   auto advance = [&]() {
-    fst ^= 1;
+    fst = fst + 1 == NST ? 0 : fst + 1;
     if (fc + 1 < c1) ++fc;
   };
-  f16x8 fa[2][2][S::WM], fb[2][2][S::WN];  // [set][part]
-  auto read = [&](int set, const char* st, int k, int i) {
-    const int part = i / F, o = i % F, sl = ((4 * part + 2 * k + h) ^ S::turn(l32)) * 16;
+  f16x8 fa[2][2][S::WM], fb[2][2][S::WN];  // [set][part: hi, lo]
+  auto read = [&](int set, const char* st, int k, int i) {  // hi of b and a, lo of a, lo of b
+    const int part = i >= F, o = i < F ? i : i - F < S::WM ? S::WN + i - F : i - F - S::WM;
+    const int sl = ((4 * part + 2 * k + h) ^ S::turn(l32)) * 16;
     if (o < S::WN)
       fb[set][part][o] = *(const f16x8*)(st + S::BM * S::row_bytes + ((wn * S::WN + o) * 32 + l32) * S::row_bytes + sl);
     else
       fa[set][part][o - S::WN] = *(const f16x8*)(st + ((wm * S::WM + o - S::WN) * 32 + l32) * S::row_bytes + sl);
   };
+  // Small products first: of b's lo, of a's lo, of hi and hi.
   auto multiply = [&](int k, const char* st, int kn) {
 #pragma unroll
-    for (int m = 0; m < 3 * per; ++m) {
-      const int p = m / per, bi = m % per / S::WN, bj = m % S::WN;
-      acc[bi][bj] = mfma16(fa[k][p == 0][bi], fb[k][p == 1][bj], acc[bi][bj]);
+    for (int m = 0; m < M; ++m) {
+      const int p = m / per + 3 - NP, bi = m % per / S::WN, bj = m % S::WN;
+      acc[bi][bj] = mfma16(fa[k][p == 1][bi], fb[k][p == 0][bj], acc[bi][bj]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = m * 2 * F / (3 * per); j < (m + 1) * 2 * F / (3 * per); ++j) read(k ^ 1, st, kn, j);
+      for (int j = m * R / M; j < (m + 1) * R / M; ++j) read(k ^ 1, st, kn, j);
       if (k == 0)
 #pragma unroll
-        for (int j = m * L / (3 * per); j < (m + 1) * L / (3 * per); ++j) issue(j);
+        for (int j = m * L / M; j < (m + 1) * L / M; ++j) issue(j);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto arrive = [&]() {
+  auto arrive = [&]() {  // this wavefront's part of the next block is in LDS; the barrier: everyone's
     __builtin_amdgcn_sched_barrier(0);
-    wait_loads();
+    __builtin_amdgcn_s_waitcnt((kAhead & 15) | (kAhead >> 4) << 14 | 7 << 4);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll
-  for (int j = 0; j < L; ++j) issue(j);
-  advance();
+  for (int st = 0; st < NST - 1; ++st) {
+#pragma unroll
+    for (int j = 0; j < L; ++j) issue(j);
+    advance();
+  }
   arrive();
 #pragma unroll
-  for (int i = 0; i < 2 * F; ++i) read(0, lds, 0, i);
+  for (int i = 0; i < R; ++i) read(0, lds, 0, i);
   int cst = 0;
   for (int c = c0; c < c1; ++c) {
+    // (the block fetched goes into the stage of block c - 1, which everyone has read)
     const char* st = lds + cst * S::stage_bytes;
-    cst ^= 1;
+    cst = cst + 1 == NST ? 0 : cst + 1;
     multiply(0, st, 1);
     arrive();
     multiply(1, lds + cst * S::stage_bytes, 0);

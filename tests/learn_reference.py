@@ -75,7 +75,7 @@ def choose(z, scale, offset=None, given=None, repeat=1.0, presence=0.0, frequenc
 
 # ------------------------------------------------------------------ orthogonalised updates
 
-def newton(u, coef, eps):
+def newton(u, coef, eps, dtype=torch.float32):
     """The steps in 64 bits, and a bound of the result's error in the Frobenius norm.
 
     A step x -> p(x) of the singular values carries an error of X on by at most the
@@ -83,7 +83,8 @@ def newton(u, coef, eps):
     differences and sums of p over those of s).  To it each step adds its own: two
     binary16 parts leave 2^-22 of an operand and the product without lo lo 2^-22 more,
     A, A^2 and B once each; fp32 sums of K terms on the matrix cores 2 U at each of
-    3 K / 16 instructions, of sizes that the norms' products bound."""
+    3 K / 16 instructions, of sizes that the norms' products bound.  A bfloat16 result's
+    Gram matrices and products with B take X by its hi part alone, 2^-11 of it off."""
     x = u.double().cpu()
     tall = x.shape[0] > x.shape[1]
     if tall:
@@ -97,11 +98,14 @@ def newton(u, coef, eps):
         A = x @ x.t()
         an, xn = float(A.norm()), float(x.norm())
         rel = lambda terms: 3 * 2.0 ** -22 + 2 * U * (3 * terms / 16 + 4)
-        dA = rel(K) * xn * xn
+        one = 2.0 ** -11 if dtype == torch.bfloat16 else 0.0
+        dA = (rel(K) + 2 * one) * xn * top
         B = b * A + c * (A @ A)
+        # (|X Y| <= |X| times Y's largest singular value)
         dB = (abs(b) + 2 * abs(c) * top ** 2) * dA + abs(c) * rel(S) * an * an + 2.0 ** -22 * (abs(b) * an + abs(c) * an * an)
         new = a * x + B @ x
-        local = dB * top + rel(S) * float(B.norm()) * xn + (2.0 ** -21) * (abs(a) * xn + float(new.norm()))
+        beta = float((b * s ** 2 + c * s ** 4).abs().max())  # the norm of B
+        local = dB * top + one * beta * xn + rel(S) * float(B.norm()) * xn + (2.0 ** -21) * (abs(a) * xn + float(new.norm()))
         err = slope * err + local
         top = max(float((a * s + b * s ** 3 + c * s ** 5).abs().max()), 1e-30) * (1 + 1e-6)
         x = new

@@ -34,9 +34,11 @@ def _norms(got, want):
     return float((got.double().cpu() - want).norm())
 
 
-def _bound(u, coef, dtype):
-    """The 64-bit result and the bound of the kernel's error in the Frobenius norm."""
-    want, err = ref.newton(u, coef, EPS)
+def _bound(u, coef, dtype, products=None):
+    """The 64-bit result and the bound of the kernel's error in the Frobenius norm: a result rounded to `dtype`, of
+    products for a result of type `products`."""
+    products = products or dtype
+    want, err = ref.newton(u, coef, EPS, products)
     if min(u.shape) <= 64:  # 64 bits but for the result, rounded to fp32
         err = ref.slope_of(coef) * 1e-12 + ref.U * float(want.norm())
     return want, err + ref.UNIT[dtype] * float(want.norm()) + ref.STEP[dtype] * want.numel() ** 0.5
@@ -137,7 +139,7 @@ def test_step(ctx, batch, m, n, dtype, nesterov):
         u = gd + mu * vk if nesterov else vk
         du = 3 * ref.U * float((gd.abs() + vk.abs()).norm())  # u's entries, as v's
         for i in range(batch):
-            want, tol = _bound(u[i], [kkm.KKM_QUINTIC] * 5, torch.float32)
+            want, tol = _bound(u[i], [kkm.KKM_QUINTIC] * 5, torch.float32, t)
             tol += ref.slope_of([kkm.KKM_QUINTIC] * 5) * 2 * du / float(u[i].norm())
             new = keep * w0[i] - rate * want
             size = (keep * w0[i]).norm() + rate * want.norm()
