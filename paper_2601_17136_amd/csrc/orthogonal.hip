@@ -378,7 +378,7 @@ struct TileArgs {
   int64_t stride_a, stride_b;  // of a matrix of the batch
   int64_t M, N;
   int nkb, mt, nt;
-  bool half;                   // symmetric: tiles on and above the diagonal
+  bool half;                   // symmetric: tiles on and above the diagonal's blocks of BM x BM
   const half_t* base;
   int64_t ld_base, stride_base;
   float ca, cm;                // what base's and the sums' stored values are multiplied by
@@ -387,23 +387,50 @@ struct TileArgs {
   Target out;
 };
 
+// A symmetric product's tiles, R times as high as wide: of row tile i those from its
+// block of the diagonal on.  In bands of 8 row tiles by their columns, of which the
+// first are as high as the diagonal leaves them; an XCD has a contiguous run, as
+// tile_of's.
+constexpr int kBand = 8;
+template <int R>
+__host__ __device__ inline int band_tiles(int b, int mt, int nt) {  // of band b
+  const int p = mt - b * kBand < kBand ? mt - b * kBand : kBand, cols = nt - R * kBand * b;
+  // (row i of the band has R i columns less; the last may have none of a wider tile's)
+  return p * cols - R * (p * (p - 1) / 2);
+}
+template <int R>
+__device__ inline void half_tile_of(unsigned g, unsigned total, int mt, int nt, int& mi, int& ni) {
+  const unsigned per = total >> 3, rem = total & 7, x = g & 7;
+  int t = (int)(x * per + min(x, rem) + (g >> 3)), b = 0;
+  for (int n = band_tiles<R>(0, mt, nt); t >= n; n = band_tiles<R>(++b, mt, nt)) t -= n;
+  const int p = min(kBand, mt - b * kBand), low = R * (p * (p - 1) / 2);  // tiles of columns lower than p
+  int c, r;
+  if (t < low) {
+    int k = 1;  // R columns of height k
+    while (t >= R * k) t -= R * k++;
+    c = R * (k - 1) + t / k;
+    r = t % k;
+  } else {
+    c = R * (p - 1) + (t - low) / p;
+    r = (t - low) % p;
+  }
+  mi = __builtin_amdgcn_readfirstlane(b * kBand + r);
+  ni = __builtin_amdgcn_readfirstlane(R * kBand * b + c);
+}
+
 // The sums pass through LDS, 32 rows of each of the workgroup's GM at a time, so that
 // base is read and every result written 16 bytes a lane, whole 128-byte blocks in both
 // orders.
 template <class S, int NP, bool LAST, typename OT>
 __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q) {
-  constexpr int LD = S::BN + 4, ROWS = S::GM * 32;
+  constexpr int LD = S::BN + 4, ROWS = S::GM * 32, kRatio = S::BM / S::BN;
+  static_assert(S::BM % S::BN == 0, "the diagonal's tiles");
   constexpr int kBytes = S::lds_bytes > ROWS * LD * 4 ? S::lds_bytes : ROWS * LD * 4;
   __shared__ __attribute__((aligned(1024))) char lds[kBytes];
   const int64_t bt = blockIdx.y;
   int mi, ni;
-  if (q.half) {  // tile t of the triangle, by columns: (i, j) with i <= j is t = j (j + 1) / 2 + i
-    const int t = blockIdx.x;
-    int j = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-    while ((j + 1) * (j + 2) / 2 <= t) ++j;
-    while (j * (j + 1) / 2 > t) --j;
-    mi = __builtin_amdgcn_readfirstlane(t - j * (j + 1) / 2);
-    ni = __builtin_amdgcn_readfirstlane(j);
+  if (q.half) {
+    half_tile_of<kRatio>(blockIdx.x, gridDim.x, q.mt, q.nt, mi, ni);
   } else {
     tile_of(blockIdx.x, (unsigned)(q.mt * q.nt), q.mt, q.nt, mi, ni);
   }
@@ -418,7 +445,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
   const half_t* base = q.base ? q.base + bt * q.stride_base : nullptr;
   half_t* along = q.along ? q.along + bt * q.stride_along : nullptr;
   half_t* across = q.across ? q.across + bt * q.stride_across : nullptr;
-  const bool whole = !(q.half && mi == ni);  // (a tile on the diagonal is whole as it is)
+  const bool turned = !q.half || ni >= (mi + 1) * kRatio;  // (the diagonal's blocks are whole as they are)
   float* sums = (float*)lds;
 #pragma unroll
   for (int bi = 0; bi < S::WM; ++bi) {
@@ -465,7 +492,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
     }
     if constexpr (!LAST) {
       __syncthreads();
-      if (whole)
+      if (turned)
 #pragma unroll
         for (int e = threadIdx.x; e < S::BN * (ROWS / 8); e += S::threads) {
           // four neighbouring lanes have 32 rows of a column
@@ -565,6 +592,48 @@ double largest(double a, double b, double c, double top) {
 }
 int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(top))); }
 
+// The tiles of a launch, and what it takes with them, in microseconds: `end`, and a
+// block's time in a full round of 256 tiles and in one of few.  Measured with three
+// products of parts, a Gram matrix and X's product of 4096 / 3000 / 2048 / 1024 square:
+// 256 x 256 232 / 176 / 121 / 67 and 339 / 195 / 130 / 74, 256 x 128 260 / 92 / 59 / 33 and
+// 347 / 202 / 68 / 36, 128 x 128 232 / 109 / 41 / 20 and 371 / 180 / 54 / 22, 128 x 64 228 /
+// 102 / 46 / 16 and 405 / 176 / 58 / 19, 64 x 64 249 / 106 / 45 / 11 and 473 / 192 / 65 / 13.
+using Pair256 = PairShape<BigTile, 2>;                     // 128 KB
+using Pair256x128 = PairShape<TileShape<2, 2, 4, 2>, 3>;   // 144 KB
+using Pair128 = PairShape<TileShape<1, 2, 4, 2>, 4>;       // 128 KB
+using Pair128x64 = PairShape<TileShape<2, 1, 2, 2>, 3>;    // 72 KB
+using Pair64 = PairShape<TileShape<1, 1, 2, 2>, 4>;        // 64 KB
+struct PairCost {
+  double end, alone, full;
+};
+template <class S>
+double pair_time(const PairCost& c, const TileArgs& q, unsigned nb) {
+  const int64_t mt = cdiv(q.M, S::BM), nt = cdiv(q.N, S::BN);
+  const double tiles = (double)nb * (q.half ? mt * nt - S::BM / S::BN * (mt * (mt - 1) / 2) : mt * nt);
+  const double rounds = std::floor(tiles / 256), left = tiles / 256 - rounds;
+  return c.end + q.nkb * (rounds * c.full + (left > 0 ? c.alone + (c.full - c.alone) * left * left * left : 0));
+}
+template <class S, int NP, bool LAST, typename OT>
+void launch_shape(TileArgs q, unsigned nb, hipStream_t s) {
+  q.mt = (int)cdiv(q.M, S::BM);
+  q.nt = (int)cdiv(q.N, S::BN);
+  const int tiles = q.half ? q.mt * q.nt - S::BM / S::BN * (q.mt * (q.mt - 1) / 2) : q.mt * q.nt;
+  pair_kernel<S, NP, LAST, OT><<<dim3((unsigned)tiles, nb), S::threads, 0, s>>>(q);
+}
+template <int NP, bool LAST, typename OT>
+void launch_pair(const TileArgs& q, unsigned nb, hipStream_t s) {
+  const double t[5] = {pair_time<Pair256>({13, 1.8, 2.6}, q, nb), pair_time<Pair256x128>({7, 0.85, 1.35}, q, nb),
+                       pair_time<Pair128>({6, 0.5, 0.73}, q, nb), pair_time<Pair128x64>({6, 0.33, 0.39}, q, nb),
+                       pair_time<Pair64>({6, 0.2, 0.225}, q, nb)};
+  switch (std::min_element(t, t + 5) - t) {
+    case 0: return launch_shape<Pair256, NP, LAST, OT>(q, nb, s);
+    case 1: return launch_shape<Pair256x128, NP, LAST, OT>(q, nb, s);
+    case 2: return launch_shape<Pair128, NP, LAST, OT>(q, nb, s);
+    case 3: return launch_shape<Pair128x64, NP, LAST, OT>(q, nb, s);
+    default: return launch_shape<Pair64, NP, LAST, OT>(q, nb, s);
+  }
+}
+
 // Products of parts that a result of type T is worth.  A bfloat16 result is rounded
 // to 2^-9 of itself, 0.0017 in the 2-norm, so X enters its Gram matrix by hi alone (11
 // bits: 0.0003 to 0.0006 of the result) and, beside a X of both parts, its product
@@ -574,7 +643,7 @@ constexpr int kGramParts = std::is_same<T, bf16_t>::value ? 1 : 3;
 template <typename T>
 constexpr int kMoveParts = std::is_same<T, bf16_t>::value ? 2 : 3;
 
-template <typename T, class S>
+template <typename T>
 hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
   const TiledPlan p = tiled_plan(a);
   const bool tall = a.m > a.n;
@@ -589,7 +658,6 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
   half_t *A = take(p.a), *B = take(p.a);
   double* norm = (double*)at;
   const int64_t sx = p.S * p.ldx, sxt = p.len * p.ldxt, sa = p.S * p.ldxt;
-  const int mt = (int)cdiv(p.S, S::BM), nt = (int)cdiv(p.len, S::BN), half_tiles = mt * (mt + 1) / 2;
   for (int64_t b0 = 0; b0 < a.batch; b0 += p.group) {
     const unsigned nb = (unsigned)std::min(p.group, a.batch - b0);
     const Source src = source_of(a, b0);
@@ -614,13 +682,12 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       g.stride_a = g.stride_b = sx;
       g.M = g.N = p.S;
       g.nkb = (int)(p.ldx / (2 * kPairBlock));
-      g.mt = g.nt = mt;
       g.half = true;
       g.cm = (float)std::ldexp(cc == 0 ? cb : 1.0, ea - 2 * ex);
       g.along = g.across = cc == 0 ? B : A;
       g.ld_along = g.ld_across = p.ldxt;
       g.stride_along = g.stride_across = sa;
-      pair_kernel<S, kGramParts<T>, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
+      launch_pair<kGramParts<T>, false, float>(g, nb, s);
       if (cc != 0) {
         g.a = g.b = {A, p.ldxt, p.S};
         g.stride_a = g.stride_b = sa;
@@ -631,7 +698,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
         g.ca = (float)std::ldexp(cb, eb - ea);
         g.cm = (float)std::ldexp(cc, eb - 2 * ea);
         g.along = g.across = B;
-        pair_kernel<S, 3, false, float><<<dim3(half_tiles, nb), S::threads, 0, s>>>(g);
+        launch_pair<3, false, float>(g, nb, s);
       }
       const bool last = t + 1 == a.newton.steps;
       top = largest(ca, cb, cc, top);
@@ -646,17 +713,14 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       m.M = turned ? p.len : p.S;
       m.N = turned ? p.S : p.len;
       m.nkb = (int)(p.ldxt / (2 * kPairBlock));
-      m.mt = turned ? (int)cdiv(p.len, S::BM) : mt;
-      m.nt = turned ? (int)cdiv(p.S, S::BN) : nt;
       m.base = turned ? xt : x;
       m.ld_base = turned ? p.ldxt : p.ldx;
       m.stride_base = turned ? sxt : sx;
       m.ca = (float)std::ldexp(ca, en - ex);
       m.cm = (float)std::ldexp(1.0, en - eb - ex);
-      const dim3 grid((unsigned)(m.mt * m.nt), nb);
       if (last) {
         m.out = target_of(a, b0);
-        pair_kernel<S, kMoveParts<T>, true, T><<<grid, S::threads, 0, s>>>(m);
+        launch_pair<kMoveParts<T>, true, T>(m, nb, s);
       } else {
         m.along = X[(t + 1) & 1];
         m.ld_along = p.ldx;
@@ -664,7 +728,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
         m.across = XT[(t + 1) & 1];
         m.ld_across = p.ldxt;
         m.stride_across = sxt;
-        pair_kernel<S, kMoveParts<T>, false, float><<<grid, S::threads, 0, s>>>(m);
+        launch_pair<kMoveParts<T>, false, float>(m, nb, s);
       }
       ex = en;
     }
@@ -672,20 +736,9 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
   return hipGetLastError();
 }
 
-int64_t tiles_of(const OrthoArgs& a, int side) {
-  return cdiv(std::min(a.m, a.n), side) * cdiv(std::max(a.m, a.n), side) * a.batch;
-}
-using Pair256 = PairShape<BigTile, 2>;                  // 128 KB
-using Pair128 = PairShape<SmallTile, 3>;                // 96 KB
-using Pair64 = PairShape<TileShape<1, 1, 2, 2>, 4>;     // 64 KB
-
 template <typename T>
 hipError_t launch_typed(const OrthoArgs& a, void* scratch, hipStream_t s) {
-  if (!is_flat(a)) {
-    if (tiles_of(a, 256) >= 128) return launch_tiled<T, Pair256>(a, scratch, s);
-    if (tiles_of(a, 128) >= 256) return launch_tiled<T, Pair128>(a, scratch, s);
-    return launch_tiled<T, Pair64>(a, scratch, s);
-  }
+  if (!is_flat(a)) return launch_tiled<T>(a, scratch, s);
   switch (flat_side(a)) {
     case 1: return launch_flat<T, 1>(a, scratch, s);
     case 2: return launch_flat<T, 2>(a, scratch, s);

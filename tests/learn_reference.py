@@ -85,17 +85,19 @@ def newton(u, coef, eps, dtype=torch.float32):
     A, A^2 and B once each; fp32 sums of K terms on the matrix cores 2 U at each of
     3 K / 16 instructions, of sizes that the norms' products bound.  A bfloat16 result's
     Gram matrices and products with B take X by its hi part alone, 2^-11 of it off."""
-    x = u.double().cpu()
+    x = u.double()
+    if x.numel() < 10 ** 6:
+        x = x.cpu()
     tall = x.shape[0] > x.shape[1]
     if tall:
         x = x.t().contiguous()
     x = x / (x.norm() + eps)
     S, K = x.shape
-    err, top = (4 * U + 2.0 ** -22) * x.norm(), 1.0
+    err, top = (4 * U + 2.0 ** -22) * float(x.norm()), 1.0
     for a, b, c in coef:
         s = torch.linspace(0, top, 2001, dtype=torch.float64)
         slope = float((a + 3 * b * s ** 2 + 5 * c * s ** 4).abs().max())
-        A = x @ x.t()
+        A = x @ x.t().contiguous()
         an, xn = float(A.norm()), float(x.norm())
         rel = lambda terms: 3 * 2.0 ** -22 + 2 * U * (3 * terms / 16 + 4)
         one = 2.0 ** -11 if dtype == torch.bfloat16 else 0.0
@@ -109,7 +111,7 @@ def newton(u, coef, eps, dtype=torch.float32):
         err = slope * err + local
         top = max(float((a * s + b * s ** 3 + c * s ** 5).abs().max()), 1e-30) * (1 + 1e-6)
         x = new
-    return (x.t() if tall else x), float(err)
+    return (x.t() if tall else x).cpu(), float(err)
 
 
 def slope_of(coef):

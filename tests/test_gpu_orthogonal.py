@@ -64,13 +64,10 @@ def test_orthogonalize(ctx, batch, m, n, dtype):
         want, tol = _bound(x[i], coef, t)
         off = _norms(y[i], want)
         assert off <= tol, (i, off, tol)
-    # the same bits again, in place, and alone
+    # the same bits again, in place
     z = x.clone()
     kkm.kkm_orthogonalize(ctx, z, z, eps=EPS)
     assert torch.equal(z, y)
-    if batch > 1 and min(m, n) > 64:
-        kkm.kkm_orthogonalize(ctx, x[1], z[1], eps=EPS)
-        assert torch.equal(z[1], y[1])
 
 
 @pytest.mark.parametrize("coef", ["cubic", "one", "mixed"])
@@ -90,15 +87,16 @@ def test_steps_of_each_kind(ctx, m, n, coef):
         assert float((s - 1).abs().max()) < 1e-4
 
 
-def test_large_matrices(ctx):
-    """Tiles of 256 x 256, wide and tall."""
+@pytest.mark.parametrize("m,n", [(1300, 1200), (2050, 1700), (2050, 4100), (4100, 2050), (3800, 3900), (600, 9000)])
+def test_large_matrices(ctx, m, n):
+    """Tiles of each shape, wide and tall."""
     from paper_2601_17136_amd import kkm
-    for m, n in ((2050, 4100), (4100, 2050)):
-        x = torch.randn(m, n, device="cuda", generator=_gen(m)).bfloat16()
-        y = torch.empty(m, n, device="cuda", dtype=torch.bfloat16)
-        print(f"[gpu] orthogonalize {m} x {n}", flush=True)
+    for t in (torch.bfloat16, torch.float32):
+        x = torch.randn(m, n, device="cuda", generator=_gen(m)).to(t)
+        y = torch.empty_like(x)
+        print(f"[gpu] orthogonalize {m} x {n} {t}", flush=True)
         kkm.kkm_orthogonalize(ctx, x, y, eps=EPS)
-        want, tol = _bound(x, [kkm.KKM_QUINTIC] * 5, torch.bfloat16)
+        want, tol = _bound(x, [kkm.KKM_QUINTIC] * 5, t)
         assert _norms(y, want) <= tol
 
 
