@@ -22,7 +22,7 @@
 #include <algorithm>
 
 #include "few_mma.h"
-#include "head_tile.h"
+#include "pair_tile.h"
 #include "model_ops.h"
 
 namespace kkm {
@@ -34,13 +34,13 @@ namespace {
 struct RowPlan {
   int32_t *order, *place, *bucket;  // row at a place, place of a row, bucket of a place
   int32_t *start;                   // adapters + 3: a bucket's first place
-  int32_t *tile, *piece;            // adapters + 1: its first tile of 16 rows, its first piece
+  int32_t *tile, *piece;            // adapters + 1: its first tile of `shrink`, its first piece
 };
 
 // One workgroup: each wavefront counts and then places a run of rows, 64 at a time.
 constexpr int kPlanWaves = 16;
 __global__ __launch_bounds__(kPlanWaves * 64) void plan_kernel(const int32_t* __restrict__ ids, int64_t n, int adapters,
-                                                               int bits, int piece, RowPlan q) {
+                                                               int bits, int tile, int piece, RowPlan q) {
   extern __shared__ int cnt[];  // [kPlanWaves][nb]
   __shared__ int sums[kPlanWaves][3];
   const int nb = adapters + 2, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -52,7 +52,18 @@ __global__ __launch_bounds__(kPlanWaves * 64) void plan_kernel(const int32_t* __
     return g < 0 ? adapters : g >= adapters ? adapters + 1 : g;
   };
   volatile int* own = cnt + wave * nb;
-  for (int64_t i = lo + lane; i < hi; i += 64) atomicAdd(cnt + wave * nb + bucket_of(i), 1);
+  constexpr int U = 8;  // runs of 64 rows whose ids are read at a time
+  int b8[U];
+  auto read = [&](int64_t i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) b8[u] = i0 + u * 64 + lane < hi ? bucket_of(i0 + u * 64 + lane) : -1;
+  };
+  for (int64_t i0 = lo; i0 < hi; i0 += 64 * U) {
+    read(i0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (b8[u] >= 0) atomicAdd(cnt + wave * nb + b8[u], 1);
+  }
   __syncthreads();
   // first places: by bucket, then by wavefront; tiles and pieces likewise
   int first = 0, tiles = 0, pieces = 0;  // of the buckets before this round's
@@ -61,7 +72,7 @@ __global__ __launch_bounds__(kPlanWaves * 64) void plan_kernel(const int32_t* __
     int total = 0;
     if (b < nb)
       for (int w = 0; w < kPlanWaves; ++w) total += cnt[w * nb + b];
-    int v[3] = {total, b < adapters ? (total + 15) / 16 : 0, b < adapters ? (total + piece - 1) / piece : 0};
+    int v[3] = {total, b < adapters ? (total + tile - 1) / tile : 0, b < adapters ? (total + piece - 1) / piece : 0};
     int s[3] = {v[0], v[1], v[2]};
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1)
@@ -97,25 +108,30 @@ __global__ __launch_bounds__(kPlanWaves * 64) void plan_kernel(const int32_t* __
     __syncthreads();
   }
   if (threadIdx.x == 0) q.start[nb] = first;
-  for (int64_t i0 = lo; i0 < hi; i0 += 64) {
-    const int64_t i = i0 + lane;
-    const bool here = i < hi;
-    const int b = here ? bucket_of(i) : 0;
-    unsigned long long same = __ballot(here);
-    for (int k = 0; k < bits; ++k) {
-      const unsigned long long set = __ballot(b >> k & 1);
-      same &= b >> k & 1 ? set : ~set;
-    }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    int at = 0;
-    if (here) at = own[b] + rank;
-    __builtin_amdgcn_wave_barrier();
-    if (here && rank == 0) own[b] = at + __popcll(same);
-    __builtin_amdgcn_wave_barrier();
-    if (here) {
-      q.order[at] = (int32_t)i;
-      q.place[i] = at;
-      q.bucket[at] = b;
+  for (int64_t i0 = lo; i0 < hi; i0 += 64 * U) {
+    read(i0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * 64 + lane;
+      if (i0 + u * 64 >= hi) break;
+      const int b = b8[u];
+      const bool here = b >= 0;
+      unsigned long long same = __ballot(here);
+      for (int k = 0; k < bits; ++k) {
+        const unsigned long long set = __ballot(b >> k & 1);
+        same &= b >> k & 1 ? set : ~set;
+      }
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      int at = 0;
+      if (here) at = own[b] + rank;
+      __builtin_amdgcn_wave_barrier();
+      if (here && rank == 0) own[b] = at + __popcll(same);
+      __builtin_amdgcn_wave_barrier();
+      if (here) {
+        q.order[at] = (int32_t)i;
+        q.place[i] = at;
+        q.bucket[at] = b;
+      }
     }
   }
 }
@@ -147,6 +163,7 @@ struct TurnJobs {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void turn_kernel(TurnJobs jobs) {
+  constexpr int VEC = kVec<T>, LANES = 64 / VEC, PASS = 256 / LANES;  // lanes of a row, rows of a pass
   __shared__ T tile[64][64 + 4 / sizeof(T)];
   const int64_t total = jobs.j[0].blocks + jobs.j[1].blocks + jobs.j[2].blocks;
   for (int64_t unit = blockIdx.x; unit < total; unit += gridDim.x) {
@@ -155,16 +172,31 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnJobs jobs) {
     while (k < 2 && g >= jobs.j[k].blocks) g -= jobs.j[k++].blocks;
     const TurnJob& j = jobs.j[k];
     const int64_t mat = g / j.per, b = g - mat * j.per, c0 = b % j.bx * 64, r0 = b / j.bx * 64;
-    const T* src = (const T*)j.src + mat * j.rows * j.ld;
+    const T* src = (const T*)j.src + mat * j.rows * j.ld + c0;
     T* dst = (T*)j.dst + mat * j.cols * j.ldd;
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-      const int64_t r = r0 + e / 64, c = c0 + e % 64;
-      if (r < j.rows && c < j.cols) tile[e / 64][e % 64] = src[r * j.ld + c];
+    const int wide = (int)min((int64_t)64, j.cols - c0), col = threadIdx.x % LANES * VEC;
+#pragma unroll
+    for (int o = 0; o < 64; o += PASS) {
+      const int r = o + threadIdx.x / LANES;
+      const bool use = r0 + r < j.rows;
+      const raw_vec<T> v = load_raw(src + (use ? r0 + r : 0) * j.ld, col, use ? wide : 0);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) tile[r][col + e] = v[e];
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-      const int64_t c = c0 + e / 64, r = r0 + e % 64;
-      if (c < j.cols && r < j.ldd) dst[c * j.ldd + r] = r < j.rows ? tile[e % 64][e / 64] : (T)0.f;
+    const int high = (int)min((int64_t)64, j.ldd - r0);  // (rows past the last are zero)
+#pragma unroll
+    for (int o = 0; o < 64; o += PASS) {
+      const int c = o + threadIdx.x / LANES, r = threadIdx.x % LANES * VEC;
+      if (c >= wide || r >= high) continue;
+      raw_vec<T> v;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] = tile[r + e][c];
+      T* to = dst + (c0 + c) * j.ldd + r0 + r;
+      if (r + VEC <= high)
+        *(any_vec<T>*)to = v;
+      else
+        for (int e = 0; e < high - r; ++e) to[e] = v[e];
     }
     __syncthreads();
   }
@@ -188,57 +220,99 @@ struct ShrinkJobs {
   RowPlan plan;
 };
 
-// 16 rows of an adapter by its rank; the four wavefronts take every fourth run of
-// steps of the width and join in LDS.
-template <typename T, int RB>
-__global__ __launch_bounds__(256) void shrink_kernel(ShrinkJobs q) {
-  constexpr int VEC = kVec<T>, KS = 4 * VEC, UN = RB > 4 ? 1 : RB > 2 ? 2 : 4, R = RB * 16;
-  __shared__ float zs[4][16][R + 1];
+// NT x 16 rows of an adapter by its rank; the WV wavefronts take runs of steps of the
+// width in turn and join in LDS.
+template <typename T, int RB, int NT, int WV>
+__global__ __launch_bounds__(WV * 64) void shrink_kernel(ShrinkJobs q) {
+  constexpr int VEC = kVec<T>, KS = 4 * VEC, UN = RB + NT > 4 ? 1 : RB + NT > 3 ? 2 : 4, R = RB * 16;
+  __shared__ float zs[WV][NT * 16][R + 1];
   const bool second = blockIdx.x >= q.j[0].blocks;
   const ShrinkJob& j = q.j[second];
   const int at = blockIdx.x - (second ? q.j[0].blocks : 0u);
   if (at >= q.plan.tile[q.adapters]) return;
   const int g = __builtin_amdgcn_readfirstlane(owner(q.plan.tile, q.adapters, at));
-  const int p0 = q.plan.start[g] + 16 * (at - q.plan.tile[g]), p1 = min(p0 + 16, q.plan.start[g + 1]);
+  const int p0 = q.plan.start[g] + NT * 16 * (at - q.plan.tile[g]), p1 = min(p0 + NT * 16, q.plan.start[g + 1]);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15,
             k4 = lane >> 4;
-  const T* pb = (const T*)j.x + (int64_t)q.plan.order[min(p0 + l16, p1 - 1)] * j.ldx;
-  const T* pa[RB];
+  const T *pb[NT], *pa[RB];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) pb[i] = (const T*)j.x + (int64_t)q.plan.order[min(p0 + i * 16 + l16, p1 - 1)] * j.ldx;
 #pragma unroll
   for (int i = 0; i < RB; ++i)
     pa[i] = (const T*)j.low + ((int64_t)g * q.rank + min(i * 16 + l16, q.rank - 1)) * j.lowld;
-  floatx4 acc[RB];
+  floatx4 acc[RB][NT];
 #pragma unroll
-  for (int i = 0; i < RB; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[i][n] = floatx4{0.f, 0.f, 0.f, 0.f};
   auto steps = [&](int s, auto whole) {
-    raw_vec<T> fa[UN][RB], fb[UN];
+    raw_vec<T> fa[UN][RB], fb[UN][NT];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int k = (s + u) * KS + k4 * VEC;
 #pragma unroll
+      for (int n = 0; n < NT; ++n) fb[u][n] = whole ? *(const any_vec<T>*)(pb[n] + k) : load_raw(pb[n], k, j.d);
+#pragma unroll
       for (int i = 0; i < RB; ++i) fa[u][i] = whole ? *(const any_vec<T>*)(pa[i] + k) : load_raw(pa[i], k, j.d);
-      fb[u] = whole ? *(const any_vec<T>*)(pb + k) : load_raw(pb, k, j.d);
     }
 #pragma unroll
     for (int u = 0; u < UN; ++u)
 #pragma unroll
-      for (int i = 0; i < RB; ++i) acc[i] = mfma_few(fa[u][i], fb[u], acc[i]);
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[i][n] = mfma_few(fa[u][i], fb[u][n], acc[i][n]);
   };
   const int full = j.d / KS;
   int s = wave * UN;
-  for (; s + UN <= full; s += 4 * UN) steps(s, std::true_type{});
-  for (; s * KS < j.d; s += 4 * UN) steps(s, std::false_type{});
+  for (; s + UN <= full; s += WV * UN) steps(s, std::true_type{});
+  for (; s * KS < j.d; s += WV * UN) steps(s, std::false_type{});
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) zs[wave][l16][i * 16 + 4 * k4 + r] = acc[i][r];
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) zs[wave][n * 16 + l16][i * 16 + 4 * k4 + r] = acc[i][n][r];
   __syncthreads();
   const float f = q.factor ? q.factor[g] : 1.f;
-  for (int e = threadIdx.x; e < 16 * R; e += 256) {
+  for (int e = threadIdx.x; e < NT * 16 * R; e += WV * 64) {
     const int row = e / R, c = e % R;
     if (p0 + row >= p1) continue;
-    const float v = (zs[0][row][c] + zs[1][row][c]) + (zs[2][row][c] + zs[3][row][c]);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WV; w += 4)
+      v += (zs[w][row][c] + zs[w + 1][row][c]) + (zs[w + 2][row][c] + zs[w + 3][row][c]);
     j.t[(int64_t)(p0 + row) * R + c] = c < q.rank ? v * f : 0.f;
+  }
+}
+
+// Few rows, in their own order (no plan): a workgroup a row, its wavefronts the
+// adapter's rows of the rank in turn.
+template <typename T>
+__global__ __launch_bounds__(1024) void shrink_rows_kernel(const T* __restrict__ x, int64_t ldx, int d,
+                                                           const T* __restrict__ down, int adapters, int rank, int R,
+                                                           const int32_t* __restrict__ ids,
+                                                           const float* __restrict__ factor, float* __restrict__ t) {
+  constexpr int VEC = kVec<T>;
+  const int64_t row = blockIdx.x;
+  const int g = ids[row], lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (g < 0 || g >= adapters) return;
+  const float f = factor ? factor[g] : 1.f;
+  const T* xr = x + row * ldx;
+  for (int r = wave; r < R; r += 16) {
+    float s = 0.f;
+    if (r < rank) {
+      const T* a = down + ((int64_t)g * rank + r) * d;
+#pragma unroll 4
+      for (int k = lane * VEC; k < d; k += 64 * VEC) {
+        float u[VEC], v[VEC];
+        load_part(xr, k, d, u);
+        load_part(a, k, d, v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s = fmaf(u[e], v[e], s);
+      }
+      s = wave_sum(s);
+    }
+    if (lane == 0) t[row * R + r] = s * f;
   }
 }
 
@@ -263,10 +337,10 @@ struct ProjectArgs {
 };
 
 // CT x 16 columns of y by NT x 16 rows, from the rows as they are.
-template <typename T, int CT, int NT>
-__global__ __launch_bounds__(256) void direct_kernel(ProjectArgs a) {
+template <typename T, int CT, int NT, int WV>
+__global__ __launch_bounds__(WV * 64) void direct_kernel(ProjectArgs a) {
   constexpr int VEC = kVec<T>, KS = 4 * VEC, UN = CT + NT > 4 ? 2 : 4;
-  __shared__ float zs[4][NT * 16][CT * 16 + 1];
+  __shared__ float zs[WV][NT * 16][CT * 16 + 1];
   const unsigned across = (unsigned)((a.m + CT * 16 - 1) / (CT * 16));
   const int64_t v0 = (int64_t)(blockIdx.x % across) * (CT * 16), t0 = (int64_t)(blockIdx.x / across) * (NT * 16);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15,
@@ -300,8 +374,8 @@ __global__ __launch_bounds__(256) void direct_kernel(ProjectArgs a) {
   };
   const int full = a.d / KS;
   int s = wave * UN;
-  for (; s + UN <= full; s += 4 * UN) steps(s, std::true_type{});
-  for (; s * KS < a.d; s += 4 * UN) steps(s, std::false_type{});
+  for (; s + UN <= full; s += WV * UN) steps(s, std::true_type{});
+  for (; s * KS < a.d; s += WV * UN) steps(s, std::false_type{});
 #pragma unroll
   for (int i = 0; i < CT; ++i)
 #pragma unroll
@@ -309,17 +383,19 @@ __global__ __launch_bounds__(256) void direct_kernel(ProjectArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) zs[wave][j * 16 + l16][i * 16 + 4 * k4 + r] = acc[i][j][r];
   __syncthreads();
-  for (int e = threadIdx.x; e < CT * NT * 256; e += 256) {
+  for (int e = threadIdx.x; e < CT * NT * 256; e += WV * 64) {
     const int c = e % (CT * 16), t = e / (CT * 16);
     const int64_t col = v0 + c, row = t0 + t;
     if (col >= a.m || row >= a.n) continue;
-    float v = (zs[0][t][c] + zs[1][t][c]) + (zs[2][t][c] + zs[3][t][c]);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WV; w += 4) v += (zs[w][t][c] + zs[w + 1][t][c]) + (zs[w + 2][t][c] + zs[w + 3][t][c]);
     const int g = a.ids[row];
     if (g >= a.adapters) {
       v = __builtin_nanf("");
     } else if (g >= 0) {
       const T* up = (const T*)a.up + ((int64_t)g * a.m + col) * a.uld;
-      const float* tr = a.t + (int64_t)a.plan.place[row] * a.R;
+      const float* tr = a.t + (a.plan.place ? a.plan.place[row] : row) * a.R;
       float s0 = 0.f;
       for (int k = 0; k < a.rank; k += VEC) {
         float b[VEC];
@@ -339,9 +415,11 @@ __global__ __launch_bounds__(256) void direct_kernel(ProjectArgs a) {
 struct TileProject {
   ProjectArgs a;
   Side x, w;
-  int K, nkc, nseg, mt, nt;
+  int K, nkc, mt, nt;
+  PairSide px, pw;       // fp32: pairs, each row at a power of two of its own
+  const int *ex, *ew;
 };
-template <typename T, typename E, class S, class Rows>
+template <typename T, class S, class Rows>
 __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProject q) {
   __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
   const ProjectArgs& a = q.a;
@@ -349,9 +427,13 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
   tile_of(blockIdx.x, (unsigned)(q.mt * q.nt), q.mt, q.nt, mi, ni);
   const int64_t r0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
   floatx16 acc[S::WM][S::WN];
-  Rows rows;
-  if constexpr (std::is_same<Rows, InOrder>::value) rows.order = a.plan.order;
-  tile_product<E, S, Rows>(q.x, q.w, r0, n0, q.K, q.nkc, q.nseg, 0, q.nkc * q.nseg, lds, acc, rows);
+  if constexpr (sizeof(T) == 4) {
+    pair_product<S, 3>(q.px, q.pw, r0, n0, 0, q.nkc, lds, acc);
+  } else {
+    Rows rows;
+    if constexpr (std::is_same<Rows, InOrder>::value) rows.order = a.plan.order;
+    tile_product<T, S, Rows>(q.x, q.w, r0, n0, q.K, q.nkc, 1, 0, q.nkc, lds, acc, rows);
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
 #pragma unroll
@@ -359,6 +441,17 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
     const int b0 = (int)r0 + (wm * S::WM + bi) * 32;
     if (b0 >= a.n) continue;
     const int b1 = (int)min((int64_t)b0 + 32, a.n);
+    if constexpr (sizeof(T) == 4) {
+      int ew[S::WN];
+#pragma unroll
+      for (int bj = 0; bj < S::WN; ++bj) ew[bj] = q.ew[min(n0 + (wn * S::WN + bj) * 32 + l32, (int64_t)a.m - 1)];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int ex = q.ex[min(b0 + acc_row(r, h), b1 - 1)];
+#pragma unroll
+        for (int bj = 0; bj < S::WN; ++bj) acc[bi][bj][r] = ldexpf(acc[bi][bj][r], -(ex + ew[bj]));
+      }
+    }
     for (int p = b0; p < b1;) {
       const int g = __builtin_amdgcn_readfirstlane(a.plan.bucket[p]);
       const int e = min(__builtin_amdgcn_readfirstlane(a.plan.start[g + 1]), b1);
@@ -414,39 +507,74 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
   }
 }
 
-// Copies for the tiles: rows kp wide (zero from d on) as P parts, in sorted order
-// where `order` is not null.
+// Copies for the tiles, in sorted order where `order` is not null: 16-bit rows kp wide,
+// zero from d on; fp32 rows as pairs, kp a whole number of blocks, each at the power of
+// two that brings its largest entry to 2^14 .. 2^15 (`exps`): 22 bits of an entry down to
+// 2^-17 of the row's largest, and 2^-40 of that below.  A row with an infinity or NaN is
+// taken as it is.
 struct CopyJob {
   const void* src;
   int64_t ld, rows;
   void* dst;
-  int64_t plane;
+  int* exps;
   const int32_t* order;
   unsigned blocks;
 };
 struct CopyJobs {
   CopyJob j[2];
 };
-template <typename T, typename E, int P>
+template <typename T>
 __global__ __launch_bounds__(256) void copy_kernel(CopyJobs jobs, int d, int kp) {
   const bool second = blockIdx.x >= jobs.j[0].blocks;
   const CopyJob& j = jobs.j[second];
-  const int64_t per = kp / 8, step = (int64_t)j.blocks * 256;
-  for (int64_t i = (int64_t)(blockIdx.x - (second ? jobs.j[0].blocks : 0u)) * 256 + threadIdx.x; i < j.rows * per;
-       i += step) {
-    const int64_t row = i / per;
-    const int c = (int)(i - row * per) * 8;
-    const raw_n<8, T> v = load_n<8>((const T*)j.src + (j.order ? j.order[row] : row) * j.ld, c, d);
-    frag<E> o[P];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      E pl[P];
-      split_planes<E, P>((float)v[e], pl);
-#pragma unroll
-      for (int p = 0; p < P; ++p) o[p][e] = pl[p];
+  const int64_t block = blockIdx.x - (second ? jobs.j[0].blocks : 0u);
+  if constexpr (sizeof(T) == 2) {
+    const int64_t per = kp / 8, step = (int64_t)j.blocks * 256;
+    for (int64_t i = block * 256 + threadIdx.x; i < j.rows * per; i += step) {
+      const int64_t row = i / per;
+      const int c = (int)(i - row * per) * 8;
+      *(raw_vec<T>*)((T*)j.dst + row * kp + c) = load_raw((const T*)j.src + (j.order ? j.order[row] : row) * j.ld, c, d);
     }
+  } else {  // a wavefront a row
+    const int lane = threadIdx.x & 63;
+    for (int64_t row = block * 4 + (threadIdx.x >> 6); row < j.rows; row += (int64_t)j.blocks * 4) {
+      const T* src = (const T*)j.src + (j.order ? j.order[row] : row) * j.ld;
+      float top = 0.f;
+      bool whole = true;
+#pragma unroll 4
+      for (int c = lane * 4; c < d; c += 256) {
+        float v[4];
+        load_part(src, c, d, v);
 #pragma unroll
-    for (int p = 0; p < P; ++p) *(frag<E>*)((E*)j.dst + p * j.plane + row * kp + c) = o[p];
+        for (int e = 0; e < 4; ++e) {
+          top = fmaxf(top, fabsf(v[e]));
+          whole &= fabsf(v[e]) < INFINITY;
+        }
+      }
+#pragma unroll
+      for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+      int e2 = 0;
+      if (top > 0.f && __all(whole)) {
+        (void)frexpf(top, &e2);
+        e2 = 15 - e2;
+      }
+      if (lane == 0) j.exps[row] = e2;
+      half_t* dst = (half_t*)j.dst + row * (2 * kp);
+#pragma unroll 2
+      for (int c = lane * 8; c < kp; c += 512) {
+        const raw_n<8, T> v = load_n<8>(src, c, d);
+        f16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          half_t x, y;
+          split_pair(ldexpf(v[e], e2), x, y);
+          hi[e] = x, lo[e] = y;
+        }
+        half_t* to = dst + pair_at(c);
+        *(f16x8*)to = hi;
+        *(f16x8*)(to + kPairBlock) = lo;
+      }
+    }
   }
 }
 
@@ -488,17 +616,37 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
   for (int e = 0; e < VEC; ++e)
 #pragma unroll
     for (int t = 0; t < CT; ++t) acc[e][t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  for (int p = p0 + wave * (4 * UN); p < p1; p += 16 * UN) {
-    raw_vec<T> x[UN];
-    float c[UN][CT];
+  // the next step's rows are on their way while one is multiplied, and the one's after that are being looked up
+  int row[UN];
+  raw_vec<T> x[UN], xn[UN];
+  float c[UN][CT], cn[UN][CT];
+  auto find = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) row[u] = q.plan.order[min(p + u * 4 + k4, p1 - 1)];
+  };
+  auto fetch = [&](int p) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int place = p + u * 4 + k4;
       const bool use = place < p1;
-      x[u] = load_raw((const T*)j.X + (int64_t)q.plan.order[use ? place : p0] * j.ldx, col, use ? j.d : 0);
+      xn[u] = load_raw((const T*)j.X + (int64_t)row[u] * j.ldx, col, use ? j.d : 0);
 #pragma unroll
-      for (int t = 0; t < CT; ++t) c[u][t] = use ? j.coef[(int64_t)place * q.R + s0 + t * 16 + l16] : 0.f;
+      for (int t = 0; t < CT; ++t) cn[u][t] = use ? j.coef[(int64_t)place * q.R + s0 + t * 16 + l16] : 0.f;
     }
+  };
+  int p = p0 + wave * (4 * UN);
+  find(p);
+  fetch(p);
+  find(p + 16 * UN);
+  for (; p < p1; p += 16 * UN) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      x[u] = xn[u];
+#pragma unroll
+      for (int t = 0; t < CT; ++t) c[u][t] = cn[u][t];
+    }
+    fetch(p + 16 * UN);
+    find(p + 32 * UN);
 #pragma unroll
     for (int u = 0; u < UN; ++u)
 #pragma unroll
@@ -534,23 +682,43 @@ struct JoinArgs {
   const int32_t* piece;
   void *ddown, *dup;  // each may be null
 };
+// A workgroup has 64 columns of 8 rows of an adapter's rank, its wavefronts every fourth piece.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
-  const int64_t nd = a.ddown ? (int64_t)a.adapters * a.rank * a.d : 0, nu = a.dup ? (int64_t)a.adapters * a.m : 0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < nd + nu; i += (int64_t)gridDim.x * 256) {
-    if (i < nd) {
-      const int64_t per = (int64_t)a.rank * a.d, g = i / per, e = i - g * per;
-      float s = 0.f;
-      for (int k = a.piece[g]; k < a.piece[g + 1]; ++k) s += a.down_slabs[k * per + e];
-      ((T*)a.ddown)[i] = (T)s;
-    } else {
-      const int64_t u = i - nd, g = u / a.m, c = u - g * a.m;
-      for (int r = 0; r < a.rank; ++r) {
-        float s = 0.f;
-        for (int k = a.piece[g]; k < a.piece[g + 1]; ++k) s += a.up_slabs[((int64_t)k * a.rank + r) * a.m + c];
-        ((T*)a.dup)[u * a.rank + r] = (T)s;
+  __shared__ float red[4][8][64 + 1];
+  const int rb = (a.rank + 7) / 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t per_d = a.ddown ? (int64_t)rb * ((a.d + 63) / 64) : 0, per_u = a.dup ? (int64_t)rb * ((a.m + 63) / 64) : 0;
+  for (int64_t unit = blockIdx.x; unit < a.adapters * (per_d + per_u); unit += gridDim.x) {
+    const bool up = unit >= a.adapters * per_d;
+    const int64_t i = up ? unit - a.adapters * per_d : unit, per = up ? per_u : per_d, g = i / per, b = i - g * per;
+    const int r0 = (int)(b % rb) * 8, width = up ? a.m : a.d;
+    const int64_t c = b / rb * 64 + lane;
+    const float* slabs = up ? a.up_slabs : a.down_slabs;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int k1 = a.piece[g + 1], rows = min(8, a.rank - r0);
+    if (c < width)
+#pragma unroll 2
+      for (int k = a.piece[g] + wave; k < k1; k += 4) {
+        const float* p = slabs + ((int64_t)k * a.rank + r0) * width + c;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (r < rows) s[r] += p[(int64_t)r * width];
       }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) red[wave][r][lane] = s[r];
+    __syncthreads();
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+      const int e = o * 256 + threadIdx.x, r = up ? e % 8 : e / 64, l = up ? e / 8 : e % 64;
+      const int64_t col = b / rb * 64 + l;
+      if (r >= rows || col >= width) continue;
+      const float v = (red[0][r][l] + red[1][r][l]) + (red[2][r][l] + red[3][r][l]);
+      if (up)
+        ((T*)a.dup)[(g * a.m + col) * a.rank + r0 + r] = (T)v;
+      else
+        ((T*)a.ddown)[(g * a.rank + r0 + r) * a.d + col] = (T)v;
     }
+    __syncthreads();
   }
 }
 
@@ -582,8 +750,8 @@ struct Layout {
 // A piece of an adapter's rows in `outer`: so many that the pieces fill the card
 // about twice over, 64 at least.
 int piece_of(const AdaptArgs& a) {
-  const int64_t across = cdiv(a.d, 64) + cdiv(a.m, 64);
-  const int64_t pieces = std::max<int64_t>(1, 4096 / across);
+  const int64_t w = 16 * 16 / (int64_t)elem_bytes(a.type), across = cdiv(a.d, w) + cdiv(a.m, w);
+  const int64_t pieces = std::max<int64_t>(1, 2048 / across);
   return (int)std::min<int64_t>(up_to(std::max<int64_t>(64, cdiv(a.n, pieces)), 16), 1 << 20);
 }
 int64_t most_pieces(const AdaptArgs& a) { return cdiv(a.n, piece_of(a)) + std::min<int64_t>(a.adapters, a.n); }
@@ -596,7 +764,7 @@ struct Way {
 Way way_of(int type, int64_t n, int d, int m, const void* x, int64_t ldx, const void* w, int64_t ldw, bool w_padded) {
   Way r{};
   r.tiled = n > 64 && m > 64 && (double)n * m * d > 2e9;
-  r.kp = (int)up_to(d, 8);
+  r.kp = (int)up_to(d, type == TYPE_F32 ? kPairBlock : 8);
   auto fits = [&](const void* p, int64_t ld) {
     return type != TYPE_F32 && d % 8 == 0 && ld % 8 == 0 && ld < (1 << 21) && (uintptr_t)p % 16 == 0;
   };
@@ -606,13 +774,17 @@ Way way_of(int type, int64_t n, int d, int m, const void* x, int64_t ldx, const 
   r.big = cdiv(n, 256) * cdiv(m, 256) >= 128;
   return r;
 }
-int planes(int type) { return type == TYPE_F32 ? 3 : 1; }
+// Rows of a tile of `shrink`: each reads its adapter's matrix once.
+int shrink_rows(const AdaptArgs& a) { return a.n >= 4096 && a.n >= 64 * (int64_t)a.adapters && a.rank <= 64 ? 32 : 16; }
+int64_t most_tiles(const AdaptArgs& a) { return cdiv(a.n, shrink_rows(a)) + std::min<int64_t>(a.adapters, a.n); }
+constexpr int kFewRows = 64;  // so many rows take no plan: t in their own order
 
 struct Scratch {
   RowPlan plan;
   float *t, *u;
   void *wt, *upt, *downt;  // turned
   void *xc, *wc;           // the tiles' copies
+  int *ex, *ew;
   float *down_slabs, *up_slabs;
   size_t bytes;
 };
@@ -629,9 +801,10 @@ Scratch scratch_of(const AdaptArgs& a, bool grad, void* p) {
   s.t = l.take<float>(a.n * R);
   auto copies = [&](const Way& w, int64_t rows) {
     if (!w.tiled) return;
-    const int64_t row = (int64_t)w.kp * planes(a.type) * 2;
+    const int64_t row = (int64_t)w.kp * size;
     if (w.copy_x) s.xc = l.take<char>(a.n * row);
     if (w.copy_w) s.wc = l.take<char>(rows * row);
+    if (a.type == TYPE_F32) s.ex = l.take<int>(a.n), s.ew = l.take<int>(rows);
   };
   if (!grad) {
     copies(way_of(a.type, a.n, a.d, a.m, a.x, a.ldx, a.w, a.ldw, false), a.m);
@@ -658,61 +831,82 @@ TurnJob turn_job(const void* src, int64_t count, int64_t ld, int64_t rows, int64
   return j;
 }
 
-template <typename T, typename E, int P, class S>
+template <typename T, class S>
 hipError_t launch_tiles(const ProjectArgs& a, const Way& w, const Scratch& sc, hipStream_t s) {
   CopyJobs jobs{};
-  auto job = [&](CopyJob& j, const void* src, int64_t ld, int64_t rows, void* dst, const int32_t* order) {
-    j = {src, ld, rows, dst, rows * w.kp, order, (unsigned)std::min<int64_t>(cdiv(rows * (w.kp / 8), 256), 8192)};
+  auto job = [&](CopyJob& j, const void* src, int64_t ld, int64_t rows, void* dst, int* exps, const int32_t* order) {
+    const int64_t units = sizeof(T) == 4 ? cdiv(rows, 4) : cdiv(rows * (w.kp / 8), 256);
+    j = {src, ld, rows, dst, exps, order, (unsigned)std::min<int64_t>(units, 8192)};
   };
-  if (w.copy_x) job(jobs.j[0], a.x, a.ldx, a.n, sc.xc, a.plan.order);
-  if (w.copy_w) job(jobs.j[1], a.w, a.ldw, a.m, sc.wc, nullptr);
-  if (const unsigned blocks = jobs.j[0].blocks + jobs.j[1].blocks)
-    copy_kernel<T, E, P><<<blocks, 256, 0, s>>>(jobs, a.d, w.kp);
+  if (w.copy_x) job(jobs.j[0], a.x, a.ldx, a.n, sc.xc, sc.ex, a.plan.order);
+  if (w.copy_w) job(jobs.j[1], a.w, a.ldw, a.m, sc.wc, sc.ew, nullptr);
+  if (const unsigned blocks = jobs.j[0].blocks + jobs.j[1].blocks) copy_kernel<T><<<blocks, 256, 0, s>>>(jobs, a.d, w.kp);
   TileProject q{};
   q.a = a;
-  q.x = w.copy_x ? Side{sc.xc, w.kp, a.n * w.kp, a.n} : Side{a.x, a.ldx, 0, a.n};
-  q.w = w.copy_w ? Side{sc.wc, w.kp, (int64_t)a.m * w.kp, a.m} : Side{a.w, a.ldw, 0, a.m};
   q.K = w.kp;
-  q.nkc = (int)cdiv(w.kp, kChunkK);
-  q.nseg = P == 3 ? kSegs : 1;
+  q.nkc = (int)cdiv(w.kp, sizeof(T) == 4 ? kPairBlock : kChunkK);
+  if constexpr (sizeof(T) == 4) {
+    q.px = {(const half_t*)sc.xc, 2 * w.kp, a.n};
+    q.pw = {(const half_t*)sc.wc, 2 * w.kp, a.m};
+    q.ex = sc.ex;
+    q.ew = sc.ew;
+  } else {
+    q.x = w.copy_x ? Side{sc.xc, w.kp, 0, a.n} : Side{a.x, a.ldx, 0, a.n};
+    q.w = w.copy_w ? Side{sc.wc, w.kp, 0, a.m} : Side{a.w, a.ldw, 0, a.m};
+  }
   q.mt = (int)cdiv(a.n, S::BM);
   q.nt = (int)cdiv(a.m, S::BN);
   const unsigned grid = (unsigned)(q.mt * q.nt);
-  if (w.gather)
-    project_kernel<T, E, S, InOrder><<<grid, S::threads, 0, s>>>(q);
+  if (sizeof(T) == 2 && w.gather)
+    project_kernel<T, S, InOrder><<<grid, S::threads, 0, s>>>(q);
   else
-    project_kernel<T, E, S, AsTheyAre><<<grid, S::threads, 0, s>>>(q);
-  return hipGetLastError();
-}
-
-template <typename T, typename E, int P>
-hipError_t launch_project(const ProjectArgs& a, const Way& w, const Scratch& sc, hipStream_t s) {
-  if (w.tiled)
-    return w.big ? launch_tiles<T, E, P, BigTile>(a, w, sc, s) : launch_tiles<T, E, P, SmallTile>(a, w, sc, s);
-  auto grid = [&](int ct, int nt) { return (unsigned)(cdiv(a.m, ct * 16) * cdiv(a.n, nt * 16)); };
-  if (a.n <= 16)
-    direct_kernel<T, 1, 1><<<grid(1, 1), 256, 0, s>>>(a);
-  else if (a.n <= 32)
-    direct_kernel<T, 1, 2><<<grid(1, 2), 256, 0, s>>>(a);
-  else if (a.n <= 64)
-    direct_kernel<T, 1, 4><<<grid(1, 4), 256, 0, s>>>(a);
-  else
-    direct_kernel<T, 4, 2><<<grid(4, 2), 256, 0, s>>>(a);
+    project_kernel<T, S, AsTheyAre><<<grid, S::threads, 0, s>>>(q);
   return hipGetLastError();
 }
 
 template <typename T>
-void launch_shrink(const AdaptArgs& a, const ShrinkJobs& q, hipStream_t s) {
+hipError_t launch_project(const ProjectArgs& a, const Way& w, const Scratch& sc, hipStream_t s) {
+  if (w.tiled) {
+    if constexpr (sizeof(T) == 4)
+      return w.big ? launch_tiles<T, PairShape<TileShape<2, 2, 4, 2>, 3>>(a, w, sc, s)
+                   : launch_tiles<T, PairShape<TileShape<1, 2, 4, 2>, 4>>(a, w, sc, s);
+    else
+      return w.big ? launch_tiles<T, BigTile>(a, w, sc, s) : launch_tiles<T, SmallTile>(a, w, sc, s);
+  }
+  auto grid = [&](int ct, int nt) { return (unsigned)(cdiv(a.m, ct * 16) * cdiv(a.n, nt * 16)); };
+  if (a.n <= 16)
+    direct_kernel<T, 1, 1, 8><<<grid(1, 1), 512, 0, s>>>(a);
+  else if (a.n <= 32)
+    direct_kernel<T, 1, 2, 8><<<grid(1, 2), 512, 0, s>>>(a);
+  else if (a.n <= 64)
+    direct_kernel<T, 1, 4, 8><<<grid(1, 4), 512, 0, s>>>(a);
+  else
+    direct_kernel<T, 4, 2, 4><<<grid(4, 2), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int RB>
+void launch_shrink_rank(const AdaptArgs& a, const ShrinkJobs& q, hipStream_t s) {
   const unsigned blocks = q.j[0].blocks + q.j[1].blocks;
+  if constexpr (RB <= 4)
+    if (shrink_rows(a) == 32) return (void)(shrink_kernel<T, RB, 2, 4><<<blocks, 256, 0, s>>>(q));
+  // (by the call's sizes alone: a gradient has the same bits whether or not others are asked for)
+  if (most_tiles(a) <= 256)  // few tiles: a workgroup's own time counts
+    shrink_kernel<T, RB, 1, RB == 8 ? 8 : 16><<<blocks, RB == 8 ? 512 : 1024, 0, s>>>(q);
+  else
+    shrink_kernel<T, RB, 1, 4><<<blocks, 256, 0, s>>>(q);
+}
+template <typename T>
+void launch_shrink(const AdaptArgs& a, const ShrinkJobs& q, hipStream_t s) {
   switch (rank_blocks(a.rank)) {
-    case 1: shrink_kernel<T, 1><<<blocks, 256, 0, s>>>(q); break;
-    case 2: shrink_kernel<T, 2><<<blocks, 256, 0, s>>>(q); break;
-    case 4: shrink_kernel<T, 4><<<blocks, 256, 0, s>>>(q); break;
-    default: shrink_kernel<T, 8><<<blocks, 256, 0, s>>>(q);
+    case 1: return launch_shrink_rank<T, 1>(a, q, s);
+    case 2: return launch_shrink_rank<T, 2>(a, q, s);
+    case 4: return launch_shrink_rank<T, 4>(a, q, s);
+    default: return launch_shrink_rank<T, 8>(a, q, s);
   }
 }
 
-template <typename T, typename E, int P>
+template <typename T>
 hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_t s) {
   const int RB = rank_blocks(a.rank), R = RB * 16;
   if (a.n == 0) {
@@ -724,12 +918,15 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
     return hipGetLastError();
   }
   const Scratch sc = scratch_of(a, grad, scratch);
-  int bits = 1;
-  while (1 << bits < a.adapters + 2) ++bits;
+  const bool few = !grad && a.n <= kFewRows;
   const int piece = piece_of(a);
-  plan_kernel<<<1, kPlanWaves * 64, kPlanWaves * (a.adapters + 2) * sizeof(int), s>>>(a.ids, a.n, a.adapters, bits, piece,
-                                                                                    sc.plan);
-  const unsigned tiles = (unsigned)(cdiv(a.n, 16) + std::min<int64_t>(a.adapters, a.n));
+  if (!few) {
+    int bits = 1;
+    while (1 << bits < a.adapters + 2) ++bits;
+    plan_kernel<<<1, kPlanWaves * 64, kPlanWaves * (a.adapters + 2) * sizeof(int), s>>>(
+        a.ids, a.n, a.adapters, bits, shrink_rows(a), piece, sc.plan);
+  }
+  const unsigned tiles = (unsigned)most_tiles(a);
   ShrinkJobs sh{};
   sh.adapters = a.adapters;
   sh.rank = a.rank;
@@ -746,13 +943,19 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   p.ids = a.ids;
   if (!grad) {
     sh.j[0] = of_x;
-    launch_shrink<T>(a, sh, s);
+    if (few) {
+      p.plan.place = nullptr;
+      shrink_rows_kernel<T><<<(unsigned)a.n, 1024, 0, s>>>((const T*)a.x, a.ldx, a.d, (const T*)a.down, a.adapters, a.rank,
+                                                           R, a.ids, a.factor, sc.t);
+    } else {
+      launch_shrink<T>(a, sh, s);
+    }
     p.x = a.x, p.ldx = a.ldx, p.d = a.d;
     p.w = a.w, p.ldw = a.ldw, p.m = a.m;
     p.up = a.up;
     p.t = sc.t;
     p.y = a.y, p.ldy = a.ldy;
-    return launch_project<T, E, P>(p, way_of(a.type, a.n, a.d, a.m, a.x, a.ldx, a.w, a.ldw, false), sc, s);
+    return launch_project<T>(p, way_of(a.type, a.n, a.d, a.m, a.x, a.ldx, a.w, a.ldw, false), sc, s);
   }
   TurnJobs turn{};
   const int64_t mp = up_to(a.m, 8);
@@ -774,7 +977,7 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
     p.up = sc.downt;
     p.t = sc.u;
     p.y = a.dx, p.ldy = a.lddx;
-    const hipError_t e = launch_project<T, E, P>(p, way_of(a.type, a.n, a.m, a.d, a.dy, a.lddy, sc.wt, mp, true), sc, s);
+    const hipError_t e = launch_project<T>(p, way_of(a.type, a.n, a.m, a.d, a.dy, a.lddy, sc.wt, mp, true), sc, s);
     if (e != hipSuccess) return e;
   }
   if (!a.ddown && !a.dup) return hipGetLastError();
@@ -796,8 +999,8 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   else
     outer_kernel<T, 4><<<grid, 256, 0, s>>>(o);
   const JoinArgs j = {sc.down_slabs, sc.up_slabs, a.adapters, a.rank, a.d, a.m, sc.plan.piece, a.ddown, a.dup};
-  const int64_t items = (a.ddown ? (int64_t)a.adapters * a.rank * a.d : 0) + (a.dup ? (int64_t)a.adapters * a.m : 0);
-  join_kernel<T><<<(unsigned)std::min<int64_t>(cdiv(items, 256), 65536), 256, 0, s>>>(j);
+  const int64_t units = a.adapters * cdiv(a.rank, 8) * ((a.ddown ? cdiv(a.d, 64) : 0) + (a.dup ? cdiv(a.m, 64) : 0));
+  join_kernel<T><<<(unsigned)std::min<int64_t>(units, 1 << 20), 256, 0, s>>>(j);
   return hipGetLastError();
 }
 
@@ -806,9 +1009,9 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
 size_t adapt_scratch(const AdaptArgs& a, bool grad) { return a.n ? scratch_of(a, grad, nullptr).bytes : 0; }
 
 hipError_t launch_adapt(const AdaptArgs& a, bool grad, void* scratch, hipStream_t s) {
-  if (a.type == TYPE_F32) return launch_typed<float, bf16_t, 3>(a, grad, scratch, s);
-  return a.type == TYPE_F16 ? launch_typed<half_t, half_t, 1>(a, grad, scratch, s)
-                            : launch_typed<bf16_t, bf16_t, 1>(a, grad, scratch, s);
+  if (a.type == TYPE_F32) return launch_typed<float>(a, grad, scratch, s);
+  return a.type == TYPE_F16 ? launch_typed<half_t>(a, grad, scratch, s)
+                            : launch_typed<bf16_t>(a, grad, scratch, s);
 }
 
 }  // namespace kkm
