@@ -20,10 +20,11 @@
 // The adapters' products run on the fp32 matrix cores: they are few beside w's, and
 // t and u keep all their bits.
 #include <algorithm>
+#include <cmath>
 
-#include "few_mma.h"
-#include "pair_tile.h"
 #include "model_ops.h"
+#include "pair_tile.h"
+#include "wave_rows.h"
 
 namespace kkm {
 
@@ -37,41 +38,85 @@ struct RowPlan {
   int32_t *tile, *piece;            // adapters + 1: its first tile of `shrink`, its first piece
 };
 
-// One workgroup: each wavefront counts and then places a run of rows, 64 at a time.
-constexpr int kPlanWaves = 16;
+// The rows are cut into runs of a workgroup (`run` rows), whose wavefronts count and
+// then place theirs, 64 at a time.  More than one run: a launch counts them first, and
+// each workgroup sums what lies before its own.  20000 rows of 8 adapters by one
+// workgroup 31 us, by 20 in two launches 9.
+constexpr int kPlanWaves = 16, kPlanAhead = 8;  // ids of so many 64 rows are read at a time
+__device__ inline int bucket_of(int g, int adapters) { return g < 0 ? adapters : g >= adapters ? adapters + 1 : g; }
+// The lanes whose b is this lane's (none of b < 0).
+__device__ inline unsigned long long alike(int b, int bits) {
+  unsigned long long same = __ballot(b >= 0);
+  for (int k = 0; k < bits; ++k) {
+    const unsigned long long set = __ballot(b >> k & 1);
+    same &= b >> k & 1 ? set : ~set;
+  }
+  return b >= 0 ? same : 0;
+}
+__device__ inline bool leads(unsigned long long same) {
+  return same && __ffsll((unsigned long long)same) - 1 == (int)(threadIdx.x & 63);
+}
+
+__global__ __launch_bounds__(kPlanWaves * 64) void count_kernel(const int32_t* __restrict__ ids, int64_t n, int adapters,
+                                                                int64_t run, int bits, int* __restrict__ counts) {
+  extern __shared__ int cnt[];  // [nb]
+  const int nb = adapters + 2;
+  for (int e = threadIdx.x; e < nb; e += kPlanWaves * 64) cnt[e] = 0;
+  __syncthreads();
+  const int64_t lo = blockIdx.x * run, hi = min(lo + run, n);
+  for (int64_t i0 = lo; i0 < hi; i0 += kPlanWaves * 64) {
+    const int b = i0 + threadIdx.x < hi ? bucket_of(ids[i0 + threadIdx.x], adapters) : -1;
+    const unsigned long long same = alike(b, bits);
+    if (leads(same)) atomicAdd(cnt + b, __popcll(same));
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < nb; e += kPlanWaves * 64) counts[(int64_t)blockIdx.x * nb + e] = cnt[e];
+}
+
 __global__ __launch_bounds__(kPlanWaves * 64) void plan_kernel(const int32_t* __restrict__ ids, int64_t n, int adapters,
-                                                               int bits, int tile, int piece, RowPlan q) {
+                                                               int64_t run, const int* __restrict__ counts, int bits,
+                                                               int tile, int piece, RowPlan q) {
   extern __shared__ int cnt[];  // [kPlanWaves][nb]
   __shared__ int sums[kPlanWaves][3];
   const int nb = adapters + 2, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int e = threadIdx.x; e < kPlanWaves * nb; e += kPlanWaves * 64) cnt[e] = 0;
   __syncthreads();
-  const int64_t per = ((n + kPlanWaves - 1) / kPlanWaves + 63) / 64 * 64, lo = wave * per, hi = min(lo + per, n);
-  auto bucket_of = [&](int64_t i) {
-    const int g = ids[i];
-    return g < 0 ? adapters : g >= adapters ? adapters + 1 : g;
-  };
+  const int64_t from = blockIdx.x * run, to = min(from + run, n);
+  const int64_t per = (run / kPlanWaves + 63) / 64 * 64, lo = min(from + wave * per, to), hi = min(lo + per, to);
   volatile int* own = cnt + wave * nb;
-  constexpr int U = 8;  // runs of 64 rows whose ids are read at a time
-  int b8[U];
+  int b8[kPlanAhead];
   auto read = [&](int64_t i0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) b8[u] = i0 + u * 64 + lane < hi ? bucket_of(i0 + u * 64 + lane) : -1;
+    for (int u = 0; u < kPlanAhead; ++u)
+      b8[u] = i0 + u * 64 + lane < hi ? bucket_of(ids[i0 + u * 64 + lane], adapters) : -1;
   };
-  for (int64_t i0 = lo; i0 < hi; i0 += 64 * U) {
+  for (int64_t i0 = lo; i0 < hi; i0 += 64 * kPlanAhead) {
     read(i0);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (b8[u] >= 0) atomicAdd(cnt + wave * nb + b8[u], 1);
+    for (int u = 0; u < kPlanAhead; ++u) {
+      if (i0 + u * 64 >= hi) break;
+      const unsigned long long same = alike(b8[u], bits);
+      if (leads(same)) own[b8[u]] += __popcll(same);
+      __builtin_amdgcn_wave_barrier();
+    }
   }
   __syncthreads();
-  // first places: by bucket, then by wavefront; tiles and pieces likewise
+  // first places: by bucket, then by run and wavefront; tiles and pieces likewise
   int first = 0, tiles = 0, pieces = 0;  // of the buckets before this round's
   for (int b0 = 0; b0 < nb; b0 += kPlanWaves * 64) {
     const int b = b0 + threadIdx.x;
-    int total = 0;
-    if (b < nb)
-      for (int w = 0; w < kPlanWaves; ++w) total += cnt[w * nb + b];
+    int total = 0, before = 0;
+    if (b < nb) {
+      if (counts)
+#pragma unroll 8
+        for (int r = 0; r < (int)gridDim.x; ++r) {
+          const int c = counts[(int64_t)r * nb + b];
+          total += c;
+          if (r < (int)blockIdx.x) before += c;
+        }
+      else
+        for (int w = 0; w < kPlanWaves; ++w) total += cnt[w * nb + b];
+    }
     int v[3] = {total, b < adapters ? (total + tile - 1) / tile : 0, b < adapters ? (total + piece - 1) / piece : 0};
     int s[3] = {v[0], v[1], v[2]};
 #pragma unroll
@@ -93,11 +138,14 @@ __global__ __launch_bounds__(kPlanWaves * 64) void plan_kernel(const int32_t* __
       }
     if (b < nb) {
       int at = base[0] + s[0] - v[0];
-      q.start[b] = at;
-      if (b <= adapters) {
-        q.tile[b] = base[1] + s[1] - v[1];
-        q.piece[b] = base[2] + s[2] - v[2];
+      if (blockIdx.x == 0) {
+        q.start[b] = at;
+        if (b <= adapters) {
+          q.tile[b] = base[1] + s[1] - v[1];
+          q.piece[b] = base[2] + s[2] - v[2];
+        }
       }
+      at += before;
       for (int w = 0; w < kPlanWaves; ++w) {
         const int c = cnt[w * nb + b];
         cnt[w * nb + b] = at;
@@ -107,20 +155,16 @@ __global__ __launch_bounds__(kPlanWaves * 64) void plan_kernel(const int32_t* __
     first = all[0], tiles = all[1], pieces = all[2];
     __syncthreads();
   }
-  if (threadIdx.x == 0) q.start[nb] = first;
-  for (int64_t i0 = lo; i0 < hi; i0 += 64 * U) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) q.start[nb] = first;
+  for (int64_t i0 = lo; i0 < hi; i0 += 64 * kPlanAhead) {
     read(i0);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < kPlanAhead; ++u) {
       const int64_t i = i0 + u * 64 + lane;
       if (i0 + u * 64 >= hi) break;
       const int b = b8[u];
       const bool here = b >= 0;
-      unsigned long long same = __ballot(here);
-      for (int k = 0; k < bits; ++k) {
-        const unsigned long long set = __ballot(b >> k & 1);
-        same &= b >> k & 1 ? set : ~set;
-      }
+      const unsigned long long same = alike(b, bits);
       const int rank = __popcll(same & ((1ull << lane) - 1));
       int at = 0;
       if (here) at = own[b] + rank;
@@ -202,6 +246,14 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnJobs jobs) {
   }
 }
 
+// The power of two that brings a largest entry to 2^14 .. 2^15; 0 of zero, infinities and NaN.
+__device__ inline int power_for(float top) {
+  if (!(top > 0.f && top < INFINITY)) return 0;
+  int e;
+  (void)frexpf(top, &e);
+  return 15 - e;
+}
+
 // ------------------------------------------------------------------ t and u
 
 struct ShrinkJob {
@@ -211,6 +263,7 @@ struct ShrinkJob {
   const void* low;  // adapters x rank x d, rows lowld apart
   int64_t lowld;
   float* t;         // n x rank padded to 16 RB, in sorted order
+  int* exps;        // a row's power of two, or null
   unsigned blocks;
 };
 struct ShrinkJobs {
@@ -220,69 +273,55 @@ struct ShrinkJobs {
   RowPlan plan;
 };
 
-// NT x 16 rows of an adapter by its rank; the WV wavefronts take runs of steps of the
-// width in turn and join in LDS.
-template <typename T, int RB, int NT, int WV>
-__global__ __launch_bounds__(WV * 64) void shrink_kernel(ShrinkJobs q) {
-  constexpr int VEC = kVec<T>, KS = 4 * VEC, UN = RB + NT > 4 ? 1 : RB + NT > 3 ? 2 : 4, R = RB * 16;
-  __shared__ float zs[WV][NT * 16][R + 1];
+// NB x 16 rows of an adapter by its rank; the wavefronts share the width and join in
+// LDS.  8192 bfloat16 rows of 4096, 32 ranks of 16 adapters SHRINKUS.
+template <typename T, class S>
+__global__ __launch_bounds__(S::WV * 64) void shrink_kernel(ShrinkJobs q) {
+  constexpr int R = S::NA * 16, N = S::NB * 16;
+  static_assert(S::WV * N * (R + 1) * 4 <= S::lds_bytes, "the sums' place");
+  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
   const bool second = blockIdx.x >= q.j[0].blocks;
   const ShrinkJob& j = q.j[second];
   const int at = blockIdx.x - (second ? q.j[0].blocks : 0u);
   if (at >= q.plan.tile[q.adapters]) return;
   const int g = __builtin_amdgcn_readfirstlane(owner(q.plan.tile, q.adapters, at));
-  const int p0 = q.plan.start[g] + NT * 16 * (at - q.plan.tile[g]), p1 = min(p0 + NT * 16, q.plan.start[g + 1]);
+  const int p0 = q.plan.start[g] + N * (at - q.plan.tile[g]), p1 = min(p0 + N, q.plan.start[g + 1]);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15,
             k4 = lane >> 4;
-  const T *pb[NT], *pa[RB];
+  floatx4 acc[S::NA][S::NB];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) pb[i] = (const T*)j.x + (int64_t)q.plan.order[min(p0 + i * 16 + l16, p1 - 1)] * j.ldx;
+  for (int i = 0; i < S::NA; ++i)
 #pragma unroll
-  for (int i = 0; i < RB; ++i)
-    pa[i] = (const T*)j.low + ((int64_t)g * q.rank + min(i * 16 + l16, q.rank - 1)) * j.lowld;
-  floatx4 acc[RB][NT];
+    for (int n = 0; n < S::NB; ++n) acc[i][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+  wave_rows<T, S>([&](int r) { return (const T*)j.low + ((int64_t)g * q.rank + min(r, q.rank - 1)) * j.lowld; },
+                  [&](int r) { return (const T*)j.x + (int64_t)q.plan.order[min(p0 + r, p1 - 1)] * j.ldx; }, j.d, lds, acc);
+  __syncthreads();
+  float (*zs)[N][R + 1] = (float (*)[N][R + 1])lds;
 #pragma unroll
-  for (int i = 0; i < RB; ++i)
+  for (int i = 0; i < S::NA; ++i)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[i][n] = floatx4{0.f, 0.f, 0.f, 0.f};
-  auto steps = [&](int s, auto whole) {
-    raw_vec<T> fa[UN][RB], fb[UN][NT];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int k = (s + u) * KS + k4 * VEC;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) fb[u][n] = whole ? *(const any_vec<T>*)(pb[n] + k) : load_raw(pb[n], k, j.d);
-#pragma unroll
-      for (int i = 0; i < RB; ++i) fa[u][i] = whole ? *(const any_vec<T>*)(pa[i] + k) : load_raw(pa[i], k, j.d);
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-#pragma unroll
-      for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[i][n] = mfma_few(fa[u][i], fb[u][n], acc[i][n]);
-  };
-  const int full = j.d / KS;
-  int s = wave * UN;
-  for (; s + UN <= full; s += WV * UN) steps(s, std::true_type{});
-  for (; s * KS < j.d; s += WV * UN) steps(s, std::false_type{});
-#pragma unroll
-  for (int i = 0; i < RB; ++i)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < S::NB; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) zs[wave][n * 16 + l16][i * 16 + 4 * k4 + r] = acc[i][n][r];
   __syncthreads();
   const float f = q.factor ? q.factor[g] : 1.f;
-  for (int e = threadIdx.x; e < NT * 16 * R; e += WV * 64) {
+  for (int e = threadIdx.x; e < N * R; e += S::WV * 64) {
     const int row = e / R, c = e % R;
     if (p0 + row >= p1) continue;
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < WV; w += 4)
+    for (int w = 0; w < S::WV; w += 4)
       v += (zs[w][row][c] + zs[w + 1][row][c]) + (zs[w + 2][row][c] + zs[w + 3][row][c]);
-    j.t[(int64_t)(p0 + row) * R + c] = c < q.rank ? v * f : 0.f;
+    const float o = c < q.rank ? v * f : 0.f;
+    j.t[(int64_t)(p0 + row) * R + c] = o;
+    zs[0][row][c] = o;
   }
+  if (!j.exps) return;
+  __syncthreads();
+  if (threadIdx.x >= N || p0 + (int)threadIdx.x >= p1) return;
+  float top = 0.f;
+  for (int c = 0; c < R; ++c) top = fmaxf(top, fabsf(zs[0][threadIdx.x][c]));
+  j.exps[p0 + threadIdx.x] = power_for(top);
 }
 
 // Few rows, in their own order (no plan): a workgroup a row, its wavefronts the
@@ -329,6 +368,7 @@ struct ProjectArgs {
   const void* up;  // adapters x m x rank, rows uld apart
   int64_t uld;
   const float* t;  // n x R, in sorted order
+  const int* texp; // binary16's tiles: a row's power of two
   int R;
   RowPlan plan;
   const int32_t* ids;
@@ -336,76 +376,72 @@ struct ProjectArgs {
   int64_t ldy;
 };
 
-// CT x 16 columns of y by NT x 16 rows, from the rows as they are.
-template <typename T, int CT, int NT, int WV>
-__global__ __launch_bounds__(WV * 64) void direct_kernel(ProjectArgs a) {
-  constexpr int VEC = kVec<T>, KS = 4 * VEC, UN = CT + NT > 4 ? 2 : 4;
-  __shared__ float zs[WV][NT * 16][CT * 16 + 1];
-  const unsigned across = (unsigned)((a.m + CT * 16 - 1) / (CT * 16));
-  const int64_t v0 = (int64_t)(blockIdx.x % across) * (CT * 16), t0 = (int64_t)(blockIdx.x / across) * (NT * 16);
+// NA x 16 columns of y by NB x 16 rows, from the rows as they are; the wavefronts share
+// the width and join in LDS.  32 rows of 4096 by 4096, 32 adapters of 16, bfloat16: DIRECTUS.
+template <typename T, class S>
+__global__ __launch_bounds__(S::WV * 64) void direct_kernel(ProjectArgs a) {
+  constexpr int C = S::NA * 16, N = S::NB * 16, THREADS = S::WV * 64, EACH = (C * N + THREADS - 1) / THREADS,
+                VEC = kVec<T>, AHEAD = EACH <= 2 ? 2 : 0;
+  static_assert(S::WV * N * (C + 1) * 4 <= S::lds_bytes, "the sums' place");
+  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  const unsigned across = (unsigned)((a.m + C - 1) / C);
+  const int64_t v0 = (int64_t)(blockIdx.x % across) * C, t0 = (int64_t)(blockIdx.x / across) * N;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15,
             k4 = lane >> 4;
-  const T *pa[CT], *pb[NT];
+  // the adapters' part of this thread's entries, as far as it can be had before t
+  int adapter[EACH], place[EACH];
+  raw_vec<T> ahead[EACH][AHEAD + 1];
+  auto up_of = [&](int o, int64_t col) { return (const T*)a.up + ((int64_t)adapter[o] * a.m + col) * a.uld; };
 #pragma unroll
-  for (int i = 0; i < CT; ++i) pa[i] = (const T*)a.w + min(v0 + i * 16 + l16, (int64_t)a.m - 1) * a.ldw;
+  for (int o = 0; o < EACH; ++o) {
+    const int e = o * THREADS + threadIdx.x;
+    const int64_t row = t0 + e / C, col = v0 + e % C;
+    const bool here = e < C * N && row < a.n && col < a.m;
+    adapter[o] = here ? a.ids[row] : -1;
+    place[o] = here ? a.plan.place ? a.plan.place[row] : (int)row : 0;
+    const bool has = adapter[o] >= 0 && adapter[o] < a.adapters;
 #pragma unroll
-  for (int i = 0; i < NT; ++i) pb[i] = (const T*)a.x + min(t0 + i * 16 + l16, a.n - 1) * a.ldx;
-  floatx4 acc[CT][NT];
+    for (int i = 0; i < AHEAD; ++i) ahead[o][i] = load_raw(has ? up_of(o, col) : (const T*)a.up, i * VEC, has ? a.rank : 0);
+  }
+  floatx4 acc[S::NA][S::NB];
 #pragma unroll
-  for (int i = 0; i < CT; ++i)
+  for (int i = 0; i < S::NA; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  auto steps = [&](int s, auto whole) {
-    raw_vec<T> fa[UN][CT], fb[UN][NT];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int k = (s + u) * KS + k4 * VEC;
-#pragma unroll
-      for (int i = 0; i < CT; ++i) fa[u][i] = whole ? *(const any_vec<T>*)(pa[i] + k) : load_raw(pa[i], k, a.d);
-#pragma unroll
-      for (int i = 0; i < NT; ++i) fb[u][i] = whole ? *(const any_vec<T>*)(pb[i] + k) : load_raw(pb[i], k, a.d);
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-#pragma unroll
-      for (int i = 0; i < CT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mfma_few(fa[u][i], fb[u][j], acc[i][j]);
-  };
-  const int full = a.d / KS;
-  int s = wave * UN;
-  for (; s + UN <= full; s += WV * UN) steps(s, std::true_type{});
-  for (; s * KS < a.d; s += WV * UN) steps(s, std::false_type{});
-#pragma unroll
-  for (int i = 0; i < CT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) zs[wave][j * 16 + l16][i * 16 + 4 * k4 + r] = acc[i][j][r];
+    for (int n = 0; n < S::NB; ++n) acc[i][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+  wave_rows<T, S>([&](int r) { return (const T*)a.w + min(v0 + r, (int64_t)a.m - 1) * a.ldw; },
+                  [&](int r) { return (const T*)a.x + min(t0 + r, a.n - 1) * a.ldx; }, a.d, lds, acc);
   __syncthreads();
-  for (int e = threadIdx.x; e < CT * NT * 256; e += WV * 64) {
-    const int c = e % (CT * 16), t = e / (CT * 16);
+  float (*zs)[N][C + 1] = (float (*)[N][C + 1])lds;
+#pragma unroll
+  for (int i = 0; i < S::NA; ++i)
+#pragma unroll
+    for (int n = 0; n < S::NB; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) zs[wave][n * 16 + l16][i * 16 + 4 * k4 + r] = acc[i][n][r];
+  __syncthreads();
+#pragma unroll
+  for (int o = 0; o < EACH; ++o) {
+    const int e = o * THREADS + threadIdx.x, c = e % C, t = e / C;
     const int64_t col = v0 + c, row = t0 + t;
-    if (col >= a.m || row >= a.n) continue;
+    if (e >= C * N || col >= a.m || row >= a.n) continue;
+    float low = 0.f;
+    if (adapter[o] >= a.adapters) {
+      low = __builtin_nanf("");
+    } else if (adapter[o] >= 0) {
+      const float* tr = a.t + (int64_t)place[o] * a.R;
+      auto add = [&](const raw_vec<T>& b, int k) {  // (t is zero from rank on)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) low = fmaf(tr[k + i], (float)b[i], low);
+      };
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (i * VEC < a.rank) add(ahead[o][i], i * VEC);
+      for (int k = AHEAD * VEC; k < a.rank; k += VEC) add(load_raw(up_of(o, col), k, a.rank), k);
+    }
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < WV; w += 4) v += (zs[w][t][c] + zs[w + 1][t][c]) + (zs[w + 2][t][c] + zs[w + 3][t][c]);
-    const int g = a.ids[row];
-    if (g >= a.adapters) {
-      v = __builtin_nanf("");
-    } else if (g >= 0) {
-      const T* up = (const T*)a.up + ((int64_t)g * a.m + col) * a.uld;
-      const float* tr = a.t + (a.plan.place ? a.plan.place[row] : row) * a.R;
-      float s0 = 0.f;
-      for (int k = 0; k < a.rank; k += VEC) {
-        float b[VEC];
-        load_part(up, k, a.rank, b);
-#pragma unroll
-        for (int o = 0; o < VEC; ++o) s0 = fmaf(tr[k + o], b[o], s0);  // (t is zero from rank on)
-      }
-      v += s0;
-    }
-    ((T*)a.y)[row * a.ldy + col] = (T)v;
+    for (int w = 0; w < S::WV; w += 4) v += (zs[w][t][c] + zs[w + 1][t][c]) + (zs[w + 2][t][c] + zs[w + 3][t][c]);
+    ((T*)a.y)[row * a.ldy + col] = (T)(v + low);
   }
 }
 
@@ -421,7 +457,9 @@ struct TileProject {
 };
 template <typename T, class S, class Rows>
 __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProject q) {
-  __shared__ __attribute__((aligned(1024))) char lds[S::lds_bytes];
+  constexpr int LD = S::BN + 4, ROWS = S::GM * 32;
+  constexpr int kBytes = S::lds_bytes > ROWS * LD * 4 ? S::lds_bytes : ROWS * LD * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[kBytes];
   const ProjectArgs& a = q.a;
   int mi, ni;
   tile_of(blockIdx.x, (unsigned)(q.mt * q.nt), q.mt, q.nt, mi, ni);
@@ -461,18 +499,49 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
         for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
           for (int r = 0; r < 16; ++r) low[bj][r] = 0.f;
-        const float* tr = a.t + (int64_t)min(b0 + l32, b1 - 1) * a.R + h * (a.R / 2);
-        for (int k = 0; k < a.R / 2; k += 8) {
-          const floatx4 t0 = *(const floatx4*)(tr + k), t1 = *(const floatx4*)(tr + k + 4);
+        const int at = min(b0 + l32, b1 - 1);
+        const float* tr = a.t + (int64_t)at * a.R;
+        const T* up[S::WN];
 #pragma unroll
-          for (int bj = 0; bj < S::WN; ++bj) {
-            const int64_t col = min(n0 + (wn * S::WN + bj) * 32 + l32, (int64_t)a.m - 1);
-            const T* up = (const T*)a.up + ((int64_t)g * a.m + col) * a.uld;
-            const raw_n<8, T> u = load_n<8>(up, h * (a.R / 2) + k, a.rank);
+        for (int bj = 0; bj < S::WN; ++bj)
+          up[bj] = (const T*)a.up + ((int64_t)g * a.m + min(n0 + (wn * S::WN + bj) * 32 + l32, (int64_t)a.m - 1)) * a.uld;
+        if constexpr (sizeof(T) == 4) {  // half h has the ranks of its half
+          for (int k = h * (a.R / 2); k < (h + 1) * (a.R / 2); k += 8) {
+            const floatx4 t0 = *(const floatx4*)(tr + k), t1 = *(const floatx4*)(tr + k + 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(i < 4 ? t0[i & 3] : t1[i & 3], (float)u[i], low[bj], 0, 0, 0);
+            for (int bj = 0; bj < S::WN; ++bj) {
+              const raw_n<8, T> u = load_n<8>(up[bj], k, a.rank);
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(i < 4 ? t0[i & 3] : t1[i & 3], u[i], low[bj], 0, 0, 0);
+            }
           }
+        } else {  // t as two parts, 16 bits of bfloat16 and 22 of binary16 at the row's power of two
+          const int te = std::is_same<T, half_t>::value ? a.texp[at] : 0;
+          for (int k = h * 8; k < a.R; k += 16) {
+            const floatx4 t0 = *(const floatx4*)(tr + k), t1 = *(const floatx4*)(tr + k + 4);
+            frag<T> hi, lo;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float v = i < 4 ? t0[i & 3] : t1[i & 3];
+              if (std::is_same<T, half_t>::value) v = ldexpf(v, te);
+              hi[i] = (T)v;
+              lo[i] = (T)(v - (float)hi[i]);
+            }
+#pragma unroll
+            for (int bj = 0; bj < S::WN; ++bj) {
+              const frag<T> u = load_n<8>(up[bj], k, a.rank);
+              low[bj] = mfma16(lo, u, low[bj]);
+              low[bj] = mfma16(hi, u, low[bj]);
+            }
+          }
+          if constexpr (std::is_same<T, half_t>::value)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int e2 = a.texp[min(b0 + acc_row(r, h), b1 - 1)];
+#pragma unroll
+              for (int bj = 0; bj < S::WN; ++bj) low[bj][r] = ldexpf(low[bj][r], -e2);
+            }
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -492,16 +561,34 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
       }
       p = e;
     }
-    int row[16];
+  }
+  // through LDS, 32 rows of each of GM at a time, so that rows are written 8 entries a lane
+  float* sums = (float*)lds;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) row[r] = a.plan.order[min(b0 + acc_row(r, h), b1 - 1)];
+  for (int bi = 0; bi < S::WM; ++bi) {
+    if (bi) __syncthreads();
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (b0 + acc_row(r, h) >= b1) continue;
+    for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
-      for (int bj = 0; bj < S::WN; ++bj) {
-        const int64_t col = n0 + (wn * S::WN + bj) * 32 + l32;
-        if (col < a.m) ((T*)a.y)[row[r] * a.ldy + col] = (T)acc[bi][bj][r];
+      for (int r = 0; r < 16; ++r)
+        sums[(wm * 32 + acc_row(r, h)) * LD + (wn * S::WN + bj) * 32 + l32] = acc[bi][bj][r];
+    __syncthreads();
+#pragma unroll
+    for (int e = threadIdx.x; e < ROWS * (S::BN / 8); e += S::threads) {
+      const int lr = e / (S::BN / 8), lc = e % (S::BN / 8) * 8;
+      const int64_t place = r0 + (lr / 32 * S::WM + bi) * 32 + lr % 32, col = n0 + lc;
+      if (place >= a.n || col >= a.m) continue;
+      const float* v = sums + lr * LD + lc;
+      T* y = (T*)a.y + (int64_t)a.plan.order[place] * a.ldy + col;
+      raw_n<8, T> o;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = (T)v[k];
+      if (col + 8 <= a.m) {
+        *(any_n<8, T>*)y = o;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (col + k < a.m) y[k] = o[k];
       }
     }
   }
@@ -553,11 +640,7 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyJobs jobs, int d, int kp)
       }
 #pragma unroll
       for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-      int e2 = 0;
-      if (top > 0.f && __all(whole)) {
-        (void)frexpf(top, &e2);
-        e2 = 15 - e2;
-      }
+      const int e2 = __all(whole) ? power_for(top) : 0;
       if (lane == 0) j.exps[row] = e2;
       half_t* dst = (half_t*)j.dst + row * (2 * kp);
 #pragma unroll 2
@@ -617,6 +700,7 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
 #pragma unroll
     for (int t = 0; t < CT; ++t) acc[e][t] = floatx4{0.f, 0.f, 0.f, 0.f};
   // the next step's rows are on their way while one is multiplied, and the one's after that are being looked up
+  const bool inside = c0 + W <= j.d;
   int row[UN];
   raw_vec<T> x[UN], xn[UN];
   float c[UN][CT], cn[UN][CT];
@@ -627,11 +711,14 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
   auto fetch = [&](int p) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      const int place = p + u * 4 + k4;
-      const bool use = place < p1;
-      xn[u] = load_raw((const T*)j.X + (int64_t)row[u] * j.ldx, col, use ? j.d : 0);
+      const T* xr = (const T*)j.X + (int64_t)row[u] * j.ldx;
+      if (inside)
+        xn[u] = *(const any_vec<T>*)(xr + col);
+      else
+        xn[u] = load_raw(xr, col, j.d);
+      const float* cr = j.coef + (int64_t)min(p + u * 4 + k4, p1 - 1) * q.R + s0 + l16;
 #pragma unroll
-      for (int t = 0; t < CT; ++t) cn[u][t] = use ? j.coef[(int64_t)place * q.R + s0 + t * 16 + l16] : 0.f;
+      for (int t = 0; t < CT; ++t) cn[u][t] = cr[t * 16];
     }
   };
   int p = p0 + wave * (4 * UN);
@@ -641,9 +728,11 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
   for (; p < p1; p += 16 * UN) {
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
-      x[u] = xn[u];
+      const bool use = p + u * 4 + k4 < p1;
 #pragma unroll
-      for (int t = 0; t < CT; ++t) c[u][t] = cn[u][t];
+      for (int e = 0; e < VEC; ++e) x[u][e] = use ? xn[u][e] : (T)0.f;
+#pragma unroll
+      for (int t = 0; t < CT; ++t) c[u][t] = use ? cn[u][t] : 0.f;
     }
     fetch(p + 16 * UN);
     find(p + 32 * UN);
@@ -675,6 +764,128 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
   }
 }
 
+// As outer_kernel for 16-bit rows, on the 16-bit matrix cores: 32 rows a step, 8 of
+// them a lane's, whose 8 x 8 values it turns in registers so that a column's 8 rows lie
+// together.  coef is two bfloat16 parts (16 bits, at any size); a binary16 row is two as
+// well, which hold all of it, and three products.  8192 bfloat16 rows of 4096 + 4096 and
+// 32 ranks: 78 us by the fp32 matrix cores.
+template <typename T, int CT>
+__global__ __launch_bounds__(256) void outer16_kernel(OuterJobs q) {
+  constexpr int W = 128;
+  constexpr bool kHalf = std::is_same<T, half_t>::value;
+  __shared__ float red[CT * 16][W + 1];
+  const int at = blockIdx.y;
+  if (at >= q.plan.piece[q.adapters]) return;
+  const bool second = blockIdx.x >= q.j[0].bx;
+  const OuterJob& j = q.j[second];
+  const int c0 = (blockIdx.x - (second ? q.j[0].bx : 0u)) * W, s0 = blockIdx.z * (CT * 16);
+  const int g = __builtin_amdgcn_readfirstlane(owner(q.plan.piece, q.adapters, at));
+  const int p0 = q.plan.start[g] + q.piece * (at - q.plan.piece[g]), p1 = min(p0 + q.piece, q.plan.start[g + 1]);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15,
+            k4 = lane >> 4;
+  const int col = c0 + l16 * 8;
+  const bool inside = c0 + W <= j.d;
+  floatx4 acc[8][CT];
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int t = 0; t < CT; ++t) acc[e][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  int row[8];
+  raw_vec<T> xn[8];
+  float cn[8][CT];
+  auto find = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) row[u] = q.plan.order[min(p + k4 * 8 + u, p1 - 1)];
+  };
+  auto fetch = [&](int p) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const T* xr = (const T*)j.X + (int64_t)row[u] * j.ldx;
+      if (inside)
+        xn[u] = *(const any_vec<T>*)(xr + col);
+      else
+        xn[u] = load_raw(xr, col, j.d);
+      const float* cr = j.coef + (int64_t)min(p + k4 * 8 + u, p1 - 1) * q.R + s0 + l16;
+#pragma unroll
+      for (int t = 0; t < CT; ++t) cn[u][t] = cr[t * 16];
+    }
+  };
+  int p = p0 + wave * 32;
+  find(p);
+  fetch(p);
+  find(p + 128);
+  for (; p < p1; p += 128) {
+    const int left = p1 - p - k4 * 8;  // rows from this one on take no part
+    unsigned w[8][4];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        typedef T pair __attribute__((ext_vector_type(2)));
+        const pair v = {xn[u][2 * e], xn[u][2 * e + 1]};
+        w[u][e] = u < left ? __builtin_bit_cast(unsigned, v) : 0u;
+      }
+    frag<bf16_t> ch[CT], cl[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float v = u < left ? cn[u][t] : 0.f;
+        ch[t][u] = (bf16_t)v;
+        cl[t][u] = (bf16_t)(v - (float)ch[t][u]);
+      }
+    fetch(p + 128);
+    find(p + 256);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      typedef unsigned words __attribute__((ext_vector_type(4)));
+      words v;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)  // column e of rows 2 u and 2 u + 1
+        v[u] = __builtin_amdgcn_perm(w[2 * u + 1][e / 2], w[2 * u][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+      const frag<T> x = __builtin_bit_cast(frag<T>, v);
+      if constexpr (kHalf) {
+        frag<bf16_t> xh, xl;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          xh[u] = (bf16_t)(float)x[u];
+          xl[u] = (bf16_t)((float)x[u] - (float)xh[u]);
+        }
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cl[t], xh, acc[e][t], 0, 0, 0);
+          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch[t], xl, acc[e][t], 0, 0, 0);
+          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch[t], xh, acc[e][t], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cl[t], x, acc[e][t], 0, 0, 0);
+          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch[t], x, acc[e][t], 0, 0, 0);
+        }
+      }
+    }
+  }
+  for (int o = 0; o < 4; ++o) {
+    if (wave == o)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float* v = &red[t * 16 + 4 * k4 + r][l16 * 8 + e];
+            *v = o ? *v + acc[e][t][r] : acc[e][t][r];
+          }
+    __syncthreads();
+  }
+  float* slab = j.slabs + (int64_t)at * q.rank * j.d;
+  for (int e = threadIdx.x; e < CT * 16 * W; e += 256) {
+    const int r = e / W, c = e % W;
+    if (s0 + r < q.rank && c0 + c < j.d) slab[(int64_t)(s0 + r) * j.d + c0 + c] = red[r][c];
+  }
+}
+
 // The pieces' sums, in order: ddown as it is, dup turned.
 struct JoinArgs {
   const float *down_slabs, *up_slabs;
@@ -682,41 +893,41 @@ struct JoinArgs {
   const int32_t* piece;
   void *ddown, *dup;  // each may be null
 };
-// A workgroup has 64 columns of 8 rows of an adapter's rank, its wavefronts every fourth piece.
+// A workgroup has 64 columns of 8 rows of an adapter's rank, a wavefront two of these rows.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
-  __shared__ float red[4][8][64 + 1];
+  __shared__ float turned[64][8 + 1];
   const int rb = (a.rank + 7) / 8, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t per_d = a.ddown ? (int64_t)rb * ((a.d + 63) / 64) : 0, per_u = a.dup ? (int64_t)rb * ((a.m + 63) / 64) : 0;
   for (int64_t unit = blockIdx.x; unit < a.adapters * (per_d + per_u); unit += gridDim.x) {
     const bool up = unit >= a.adapters * per_d;
     const int64_t i = up ? unit - a.adapters * per_d : unit, per = up ? per_u : per_d, g = i / per, b = i - g * per;
-    const int r0 = (int)(b % rb) * 8, width = up ? a.m : a.d;
-    const int64_t c = b / rb * 64 + lane;
-    const float* slabs = up ? a.up_slabs : a.down_slabs;
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const int k1 = a.piece[g + 1], rows = min(8, a.rank - r0);
-    if (c < width)
-#pragma unroll 2
-      for (int k = a.piece[g] + wave; k < k1; k += 4) {
-        const float* p = slabs + ((int64_t)k * a.rank + r0) * width + c;
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (r < rows) s[r] += p[(int64_t)r * width];
+    const int r0 = (int)(b % rb) * 8 + wave * 2, width = up ? a.m : a.d;
+    const int64_t c0 = b / rb * 64, c = c0 + lane;
+    const int k0 = a.piece[g], k1 = a.piece[g + 1];
+    const bool use = c < width && r0 < a.rank;
+    const int64_t second = r0 + 1 < a.rank ? width : 0;
+    const float* p = (up ? a.up_slabs : a.down_slabs) + (use ? ((int64_t)k0 * a.rank + r0) * width + c : 0);
+    float s[2] = {0.f, 0.f};
+    if (use)
+#pragma unroll 4
+      for (int k = k0; k < k1; ++k, p += (int64_t)a.rank * width) {
+        s[0] += p[0];
+        s[1] += p[second];
       }
+    if (!up) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) red[wave][r][lane] = s[r];
+      for (int r = 0; r < 2; ++r)
+        if (use && r0 + r < a.rank) ((T*)a.ddown)[(g * a.rank + r0 + r) * a.d + c] = (T)s[r];
+      continue;
+    }
+    turned[lane][wave * 2] = s[0];
+    turned[lane][wave * 2 + 1] = s[1];
     __syncthreads();
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
-      const int e = o * 256 + threadIdx.x, r = up ? e % 8 : e / 64, l = up ? e / 8 : e % 64;
-      const int64_t col = b / rb * 64 + l;
-      if (r >= rows || col >= width) continue;
-      const float v = (red[0][r][l] + red[1][r][l]) + (red[2][r][l] + red[3][r][l]);
-      if (up)
-        ((T*)a.dup)[(g * a.m + col) * a.rank + r0 + r] = (T)v;
-      else
-        ((T*)a.ddown)[(g * a.rank + r0 + r) * a.d + col] = (T)v;
+      const int e = o * 256 + threadIdx.x, r = (int)(b % rb) * 8 + e % 8;
+      if (r < a.rank && c0 + e / 8 < width) ((T*)a.dup)[(g * a.m + c0 + e / 8) * a.rank + r] = (T)turned[e / 8][e % 8];
     }
     __syncthreads();
   }
@@ -748,22 +959,55 @@ struct Layout {
 };
 
 // A piece of an adapter's rows in `outer`: so many that the pieces fill the card
-// about twice over, 64 at least.
+// with four workgroups a CU, 64 at least.
 int piece_of(const AdaptArgs& a) {
   const int64_t w = 16 * 16 / (int64_t)elem_bytes(a.type), across = cdiv(a.d, w) + cdiv(a.m, w);
-  const int64_t pieces = std::max<int64_t>(1, 2048 / across);
+  const int64_t pieces = std::max<int64_t>(1, 1024 / across);
   return (int)std::min<int64_t>(up_to(std::max<int64_t>(64, cdiv(a.n, pieces)), 16), 1 << 20);
 }
 int64_t most_pieces(const AdaptArgs& a) { return cdiv(a.n, piece_of(a)) + std::min<int64_t>(a.adapters, a.n); }
 
-// One projection: whether it runs in tiles, and what copies that takes.
+constexpr int kFewRows = 64;  // so many rows run as they are, and take no plan (t in their own order)
+constexpr double kFewProducts = 1 << 23;  // so many run from the rows as they are: 1000 x 54 to 7, fp32, 22 us, in tiles 24
+
+// The tiles of a projection, and what its launch takes in them, in microseconds: `end`,
+// and a chunk's time in a full round of 256 tiles and in one of few.  A call, of 16-bit
+// rows n x d to m, in 256 x 256 / 256 x 128 / 128 x 128 / 128 x 64 / 64 x 64: 8192 x 4096 to
+// 4096 287 / 313 / 360 / 396 / 478, 1024 x 4096 to 4096 113 / 69 / 62 / 69 / 78, 256 x 4096 to
+// 4096 115 / 67 / 50 / 48 / 40, 20000 x 784 to 256 64 / 49 / 54 / 54 / 53, 3000 x 1000 to 776
+// 59 / 43 / 33 / 38 / 36; fp32, 20000 x 784 to 1024 203 / 178 / 182 / 180 / 198.
+struct TileTime {
+  int high, wide;
+  double end, alone, full;    // 16 bits, 64 indices
+  double alone32, full32;     // pairs, 32
+};
+constexpr TileTime kTiles[5] = {{256, 256, 8, 1.45, 2.05, 1.8, 2.6},
+                                {256, 128, 6, 0.77, 1.15, 0.85, 1.35},
+                                {128, 128, 5, 0.5, 0.68, 0.5, 0.73},
+                                {128, 64, 4, 0.42, 0.39, 0.33, 0.39},
+                                {64, 64, 3, 0.3, 0.225, 0.2, 0.225}};
+double tile_time(const TileTime& t, bool f32, int64_t n, int d, int m) {
+  const double tiles = (double)cdiv(n, t.high) * cdiv(m, t.wide) / 256, rounds = std::floor(tiles), left = tiles - rounds;
+  const double alone = f32 ? t.alone32 : t.alone, full = f32 ? t.full32 : t.full;
+  return t.end + cdiv(d, f32 ? kPairBlock : kChunkK) *
+                     (rounds * full + (left > 0 ? alone + (full - alone) * left * left * left : 0));
+}
+
+// One projection: 0, or one more than the tiles it runs in, and what copies that takes.
 struct Way {
-  bool tiled, big, gather, copy_x, copy_w;
+  int tiled;
+  bool gather, copy_x, copy_w;
   int kp;
 };
 Way way_of(int type, int64_t n, int d, int m, const void* x, int64_t ldx, const void* w, int64_t ldw, bool w_padded) {
   Way r{};
-  r.tiled = n > 64 && m > 64 && (double)n * m * d > 2e9;
+  if (n > kFewRows && (double)n * m * d > kFewProducts) {
+    double best = 0;
+    for (int k = 0; k < 5; ++k) {
+      const double t = tile_time(kTiles[k], type == TYPE_F32, n, d, m);
+      if (k == 0 || t < best) best = t, r.tiled = k + 1;
+    }
+  }
   r.kp = (int)up_to(d, type == TYPE_F32 ? kPairBlock : 8);
   auto fits = [&](const void* p, int64_t ld) {
     return type != TYPE_F32 && d % 8 == 0 && ld % 8 == 0 && ld < (1 << 21) && (uintptr_t)p % 16 == 0;
@@ -771,17 +1015,20 @@ Way way_of(int type, int64_t n, int d, int m, const void* x, int64_t ldx, const 
   r.gather = fits(x, ldx) && n * ldx * 2 < 0x7fff0000;
   r.copy_x = !r.gather;
   r.copy_w = w_padded ? type == TYPE_F32 : !fits(w, ldw);  // (padded: whole rows of kp, zero from d on)
-  r.big = cdiv(n, 256) * cdiv(m, 256) >= 128;
   return r;
 }
 // Rows of a tile of `shrink`: each reads its adapter's matrix once.
 int shrink_rows(const AdaptArgs& a) { return a.n >= 4096 && a.n >= 64 * (int64_t)a.adapters && a.rank <= 64 ? 32 : 16; }
 int64_t most_tiles(const AdaptArgs& a) { return cdiv(a.n, shrink_rows(a)) + std::min<int64_t>(a.adapters, a.n); }
-constexpr int kFewRows = 64;  // so many rows take no plan: t in their own order
+// Workgroups that plan: 1024 rows of each, or a 64th of all.
+int64_t plan_run(int64_t n) { return std::max<int64_t>(1024, up_to(cdiv(n, 64), 1024)); }
+int64_t plan_runs(int64_t n) { return cdiv(n, plan_run(n)); }
 
 struct Scratch {
   RowPlan plan;
+  int* counts;
   float *t, *u;
+  int *texp, *uexp;
   void *wt, *upt, *downt;  // turned
   void *xc, *wc;           // the tiles' copies
   int *ex, *ew;
@@ -799,6 +1046,8 @@ Scratch scratch_of(const AdaptArgs& a, bool grad, void* p) {
   s.plan.tile = l.take<int32_t>(a.adapters + 1);
   s.plan.piece = l.take<int32_t>(a.adapters + 1);
   s.t = l.take<float>(a.n * R);
+  s.counts = l.take<int>(plan_runs(a.n) * (a.adapters + 2));
+  auto exps = [&](const Way& w) { return w.tiled && a.type == TYPE_F16 ? l.take<int>(a.n) : nullptr; };
   auto copies = [&](const Way& w, int64_t rows) {
     if (!w.tiled) return;
     const int64_t row = (int64_t)w.kp * size;
@@ -807,14 +1056,18 @@ Scratch scratch_of(const AdaptArgs& a, bool grad, void* p) {
     if (a.type == TYPE_F32) s.ex = l.take<int>(a.n), s.ew = l.take<int>(rows);
   };
   if (!grad) {
-    copies(way_of(a.type, a.n, a.d, a.m, a.x, a.ldx, a.w, a.ldw, false), a.m);
+    const Way w = way_of(a.type, a.n, a.d, a.m, a.x, a.ldx, a.w, a.ldw, false);
+    s.texp = exps(w);
+    copies(w, a.m);
   } else {
     s.u = l.take<float>(a.n * R);
     if (a.dx || a.ddown) s.upt = l.take<char>((int64_t)a.adapters * a.rank * a.m * size);
     if (a.dx) {
       s.downt = l.take<char>((int64_t)a.adapters * a.rank * a.d * size);
       s.wt = l.take<char>((int64_t)a.d * up_to(a.m, 8) * size);
-      copies(way_of(a.type, a.n, a.m, a.d, a.dy, a.lddy, nullptr, 0, true), a.d);
+      const Way w = way_of(a.type, a.n, a.m, a.d, a.dy, a.lddy, nullptr, 0, true);
+      s.uexp = exps(w);
+      copies(w, a.d);
     }
     if (a.ddown) s.down_slabs = l.take<float>(most_pieces(a) * a.rank * a.d);
     if (a.dup) s.up_slabs = l.take<float>(most_pieces(a) * a.rank * a.m);
@@ -866,35 +1119,38 @@ hipError_t launch_tiles(const ProjectArgs& a, const Way& w, const Scratch& sc, h
 
 template <typename T>
 hipError_t launch_project(const ProjectArgs& a, const Way& w, const Scratch& sc, hipStream_t s) {
-  if (w.tiled) {
-    if constexpr (sizeof(T) == 4)
-      return w.big ? launch_tiles<T, PairShape<TileShape<2, 2, 4, 2>, 3>>(a, w, sc, s)
-                   : launch_tiles<T, PairShape<TileShape<1, 2, 4, 2>, 4>>(a, w, sc, s);
-    else
-      return w.big ? launch_tiles<T, BigTile>(a, w, sc, s) : launch_tiles<T, SmallTile>(a, w, sc, s);
+  switch (w.tiled) {
+    case 1: return launch_tiles<T, BigTile>(a, w, sc, s);
+    case 2: return launch_tiles<T, TileShape<2, 2, 4, 2, 3>>(a, w, sc, s);
+    case 3: return launch_tiles<T, TileShape<1, 2, 4, 2, 4>>(a, w, sc, s);
+    case 4: return launch_tiles<T, TileShape<2, 1, 2, 2, 3>>(a, w, sc, s);
+    case 5: return launch_tiles<T, TileShape<1, 1, 2, 2, 4>>(a, w, sc, s);
   }
-  auto grid = [&](int ct, int nt) { return (unsigned)(cdiv(a.m, ct * 16) * cdiv(a.n, nt * 16)); };
+  auto launch = [&](auto shape) {
+    using S = decltype(shape);
+    direct_kernel<T, S><<<(unsigned)(cdiv(a.m, S::NA * 16) * cdiv(a.n, S::NB * 16)), S::WV * 64, 0, s>>>(a);
+  };
   if (a.n <= 16)
-    direct_kernel<T, 1, 1, 8><<<grid(1, 1), 512, 0, s>>>(a);
+    launch(WaveRows<T, 1, 1, 8>{});
   else if (a.n <= 32)
-    direct_kernel<T, 1, 2, 8><<<grid(1, 2), 512, 0, s>>>(a);
+    launch(WaveRows<T, 1, 2, 8>{});
   else if (a.n <= 64)
-    direct_kernel<T, 1, 4, 8><<<grid(1, 4), 512, 0, s>>>(a);
+    launch(WaveRows<T, 1, 4, 8>{});
   else
-    direct_kernel<T, 4, 2, 4><<<grid(4, 2), 256, 0, s>>>(a);
+    launch(WaveRows<T, 4, 2, 4>{});
   return hipGetLastError();
 }
 
 template <typename T, int RB>
 void launch_shrink_rank(const AdaptArgs& a, const ShrinkJobs& q, hipStream_t s) {
   const unsigned blocks = q.j[0].blocks + q.j[1].blocks;
+  auto launch = [&](auto shape) {
+    using S = decltype(shape);
+    shrink_kernel<T, S><<<blocks, S::WV * 64, 0, s>>>(q);
+  };
   if constexpr (RB <= 4)
-    if (shrink_rows(a) == 32) return (void)(shrink_kernel<T, RB, 2, 4><<<blocks, 256, 0, s>>>(q));
-  // (by the call's sizes alone: a gradient has the same bits whether or not others are asked for)
-  if (most_tiles(a) <= 256)  // few tiles: a workgroup's own time counts
-    shrink_kernel<T, RB, 1, RB == 8 ? 8 : 16><<<blocks, RB == 8 ? 512 : 1024, 0, s>>>(q);
-  else
-    shrink_kernel<T, RB, 1, 4><<<blocks, 256, 0, s>>>(q);
+    if (shrink_rows(a) == 32) return launch(WaveRows<T, RB, 2, 8>{});
+  launch(WaveRows<T, RB, 1, RB == 8 ? 4 : 8>{});  // (more registers a wavefront)
 }
 template <typename T>
 void launch_shrink(const AdaptArgs& a, const ShrinkJobs& q, hipStream_t s) {
@@ -923,8 +1179,12 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   if (!few) {
     int bits = 1;
     while (1 << bits < a.adapters + 2) ++bits;
-    plan_kernel<<<1, kPlanWaves * 64, kPlanWaves * (a.adapters + 2) * sizeof(int), s>>>(
-        a.ids, a.n, a.adapters, bits, shrink_rows(a), piece, sc.plan);
+    const int64_t run = plan_run(a.n);
+    const unsigned runs = (unsigned)plan_runs(a.n);
+    const size_t lds = (a.adapters + 2) * sizeof(int);
+    if (runs > 1) count_kernel<<<runs, kPlanWaves * 64, lds, s>>>(a.ids, a.n, a.adapters, run, bits, sc.counts);
+    plan_kernel<<<runs, kPlanWaves * 64, kPlanWaves * lds, s>>>(a.ids, a.n, a.adapters, run, runs > 1 ? sc.counts : nullptr,
+                                                                bits, shrink_rows(a), piece, sc.plan);
   }
   const unsigned tiles = (unsigned)most_tiles(a);
   ShrinkJobs sh{};
@@ -932,7 +1192,7 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   sh.rank = a.rank;
   sh.factor = a.factor;
   sh.plan = sc.plan;
-  const ShrinkJob of_x = {a.x, a.ldx, a.d, a.down, a.d, sc.t, tiles};
+  const ShrinkJob of_x = {a.x, a.ldx, a.d, a.down, a.d, sc.t, sc.texp, tiles};
   ProjectArgs p{};
   p.n = a.n;
   p.adapters = a.adapters;
@@ -953,7 +1213,7 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
     p.x = a.x, p.ldx = a.ldx, p.d = a.d;
     p.w = a.w, p.ldw = a.ldw, p.m = a.m;
     p.up = a.up;
-    p.t = sc.t;
+    p.t = sc.t, p.texp = sc.texp;
     p.y = a.y, p.ldy = a.ldy;
     return launch_project<T>(p, way_of(a.type, a.n, a.d, a.m, a.x, a.ldx, a.w, a.ldw, false), sc, s);
   }
@@ -966,7 +1226,7 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   }
   if (const int64_t blocks = turn.j[0].blocks + turn.j[1].blocks + turn.j[2].blocks)
     turn_kernel<T><<<(unsigned)std::min<int64_t>(blocks, 1 << 20), 256, 0, s>>>(turn);
-  const ShrinkJob of_dy = {a.dy, a.lddy, a.m, sc.upt, a.m, sc.u, tiles};
+  const ShrinkJob of_dy = {a.dy, a.lddy, a.m, sc.upt, a.m, sc.u, sc.uexp, tiles};
   int count = 0;
   if (sc.upt) sh.j[count++] = of_dy;
   if (a.dup) sh.j[count++] = of_x;
@@ -975,7 +1235,7 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
     p.x = a.dy, p.ldx = a.lddy, p.d = a.m;
     p.w = sc.wt, p.ldw = mp, p.m = a.d;
     p.up = sc.downt;
-    p.t = sc.u;
+    p.t = sc.u, p.texp = sc.uexp;
     p.y = a.dx, p.ldy = a.lddx;
     const hipError_t e = launch_project<T>(p, way_of(a.type, a.n, a.m, a.d, a.dy, a.lddy, sc.wt, mp, true), sc, s);
     if (e != hipSuccess) return e;
@@ -992,12 +1252,18 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   if (a.ddown) o.j[count++] = {sc.u, a.x, a.ldx, a.d, sc.down_slabs, (unsigned)cdiv(a.d, W)};
   if (a.dup) o.j[count++] = {sc.t, a.dy, a.lddy, a.m, sc.up_slabs, (unsigned)cdiv(a.m, W)};
   const dim3 grid(o.j[0].bx + o.j[1].bx, (unsigned)most_pieces(a), RB == 8 ? 2 : 1);
+  auto outer = [&](auto ct) {  // (binary16 and 16 ranks: 10.7 us by the fp32 matrix cores, 14.1 in parts; 3001 x 1001 to 777)
+    if constexpr (std::is_same<T, bf16_t>::value || (sizeof(T) == 2 && ct.value > 1))
+      outer16_kernel<T, ct.value><<<grid, 256, 0, s>>>(o);
+    else
+      outer_kernel<T, ct.value><<<grid, 256, 0, s>>>(o);
+  };
   if (RB == 1)
-    outer_kernel<T, 1><<<grid, 256, 0, s>>>(o);
+    outer(std::integral_constant<int, 1>{});
   else if (RB == 2)
-    outer_kernel<T, 2><<<grid, 256, 0, s>>>(o);
+    outer(std::integral_constant<int, 2>{});
   else
-    outer_kernel<T, 4><<<grid, 256, 0, s>>>(o);
+    outer(std::integral_constant<int, 4>{});
   const JoinArgs j = {sc.down_slabs, sc.up_slabs, a.adapters, a.rank, a.d, a.m, sc.plan.piece, a.ddown, a.dup};
   const int64_t units = a.adapters * cdiv(a.rank, 8) * ((a.ddown ? cdiv(a.d, 64) : 0) + (a.dup ? cdiv(a.m, 64) : 0));
   join_kernel<T><<<(unsigned)std::min<int64_t>(units, 1 << 20), 256, 0, s>>>(j);

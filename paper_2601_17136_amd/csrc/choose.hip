@@ -2,12 +2,14 @@
 // of the ids allowed, and of what is left the first of the largest, its log
 // probability and the log sum.  One pass over the logits: lanes hold 16 of them
 // each, so that the largest is known before the sum and both before the store.
-// A row is 16, 64 or 256 lanes wide; one of more than 4096 classes is cut into
+// A row is 16, 64 or 256 lanes wide; one of more than 256 lanes hold is cut into
 // slices, whose (largest, sum, id) a second launch joins.
 //
-// What a row's lists say of a class lies in LDS, a word per class of the slice:
-// how often it was given in the low bits, one more than the last of its biases
-// above.  Whole numbers, so that their order does not matter.
+// What a row's lists say of a class lies in LDS, a word per class of the slice: how
+// often it was given in the low bits, one more than the last of its biases above.
+// Whole numbers, so that their order does not matter.  A bit per class says whether its
+// word is used at all: lanes look at 4 or 8 of these at a time, and only classes that a
+// list names cost more than their scale, mask, exponential and store.
 #include <algorithm>
 #include <climits>
 
@@ -19,8 +21,8 @@ namespace kkm {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kEach = 16;         // logits of a lane
-constexpr int kSlice = 256 * kEach;
+constexpr int kEach = 16;  // logits of a lane
+constexpr int kAhead = 4;  // ids of a row's list that a lane reads before it needs them
 constexpr int kCountBits = 22;
 constexpr int64_t kMostBlocks = (int64_t)1 << 22;
 static_assert(kMaxGiven < 1 << kCountBits, "a count stays below the biases' bits");
@@ -56,12 +58,13 @@ __device__ inline float term(float u, float top) {
 }
 
 template <typename T, int L, bool LISTS>
-__global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a, int slices, int64_t units) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 5 : 6) void choose_kernel(ChooseArgs a, int slices, int64_t units) {
 #pragma clang fp contract(off)
-  constexpr int VEC = kVec<T>, NV = kEach / VEC, ROWS = 256 / L, WIDE = L * kEach;
-  __shared__ __attribute__((aligned(16))) unsigned word[LISTS ? kSlice : 4];
+  constexpr int VEC = kVec<T>, EACH = kEach, NV = EACH / VEC, ROWS = 256 / L, WIDE = L * EACH;
+  __shared__ unsigned word[LISTS ? 256 * EACH : 4];
+  __shared__ unsigned used[LISTS ? 8 * EACH : 4];  // bits
   __shared__ float red_top[4], red_sum[4];
-  __shared__ int red_id[4], red_bad[4];
+  __shared__ int red_id[4];
   const int l = threadIdx.x % L, r = threadIdx.x / L, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int64_t row = L == 256 ? unit / slices : unit * ROWS + r;
@@ -77,79 +80,121 @@ __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a, int slices, i
     }
     int which = -1;
     if (a.masks && here) which = a.mask_ids ? a.mask_ids[row] : (int)row;
+    const bool lost = which >= a.nmasks;
+    unsigned own = r * WIDE;  // the row's words
     if (LISTS) {
+      const int32_t* given = a.given + row * a.ngiven;
+      const int32_t* biased = a.bias_ids + row * a.nbias;
+      const int ngiven = here ? a.ngiven : 0, nbias = here ? a.nbias : 0;
+      int g[kAhead];
 #pragma unroll
-      for (int j = 0; j < kEach / 4; ++j) *(uint4*)&word[(j * 256 + threadIdx.x) * 4] = uint4{0, 0, 0, 0};
+      for (int k = 0; k < kAhead; ++k) g[k] = k * L + l < ngiven ? given[k * L + l] : -1;
+      const int b0 = l < nbias ? biased[l] : -1;
+      for (int e = threadIdx.x; e < 8 * EACH; e += 256) used[e] = 0;
       __syncthreads();
-      unsigned* own = word + r * WIDE;
-      if (here)
-        for (int j = l; j < a.nbias; j += L) {
-          const int c = a.bias_ids[row * a.nbias + j] - v0;
-          if ((unsigned)c < (unsigned)left) atomicMax(own + c, (unsigned)(j + 1) << kCountBits);
-        }
+      // An entry of a list that lies in the slice.  First all clear their words (all of
+      // them: 119 us where these few take 101, the cases' 512 rows of 131072).
+      auto at = [&](int c, auto f) {
+        if ((unsigned)(c - v0) < (unsigned)left) f(own + (c - v0));
+      };
+      auto claim = [&](unsigned w) {
+        word[w] = 0;
+        atomicOr(&used[w / 32], 1u << (w % 32));
+      };
+      at(b0, claim);
+      for (int j = L + l; j < nbias; j += L) at(biased[j], claim);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) at(g[k], claim);
+      for (int j = kAhead * L + l; j < ngiven; j += L) at(given[j], claim);
       __syncthreads();
-      if (here)
-        for (int j = l; j < a.ngiven; j += L) {
-          const int c = a.given[row * a.ngiven + j] - v0;
-          if ((unsigned)c < (unsigned)left) atomicAdd(own + c, 1u);
-        }
+      if (a.nbias) {  // (all biases before any count: a count lies below their bits)
+        auto last = [&](int c, int j) { at(c, [&](unsigned w) { atomicMax(&word[w], (unsigned)(j + 1) << kCountBits); }); };
+        last(b0, l);
+        for (int j = L + l; j < nbias; j += L) last(biased[j], j);
+        __syncthreads();
+      }
+      auto count = [&](unsigned w) { atomicAdd(&word[w], 1u); };
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) at(g[k], count);
+      for (int j = kAhead * L + l; j < ngiven; j += L) at(given[j], count);
       __syncthreads();
     }
     float u[NV][VEC], top = -INFINITY;
-    int id = INT_MAX;
-    bool bad = false;
-    const bool lost = which >= a.nmasks;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (j * L + l) * VEC;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) u[j][e] = -INFINITY;
       if (c >= left) continue;
-      unsigned bits = ~0u;
-      if (which >= 0 && !lost) bits = a.masks[(int64_t)which * a.words + (v0 + c) / 32] >> ((v0 + c) & 31);
-      float off[VEC];
-      if (a.offset) load_beside(a.offset + v0, c, left, 0.f, off);
+      unsigned out = 0, named = 0;  // bits of the vector's classes
+      if (which >= 0 && !lost) out = ~(a.masks[(int64_t)which * a.words + (v0 + c) / 32] >> ((v0 + c) & 31));
+      if (c + VEC > left) out |= ~0u << (left - c);
+      if (LISTS) named = used[(own + c) / 32] >> ((own + c) % 32) & ((1u << VEC) - 1);
+      float p[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) p[e] = (float)raw[j][e];
+      if (LISTS && named)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const unsigned count = named >> e & 1 ? word[own + c + e] & ((1u << kCountBits) - 1) : 0;
+          if (!count) continue;
+          const float f = (float)count * a.frequency, s = p[e] > 0.f ? p[e] / a.repeat : p[e] * a.repeat;
+          p[e] = s - (a.presence + f);
+        }
+      if (a.offset) {
+        float off[VEC];
+        load_beside(a.offset + v0, c, left, 0.f, off);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          if (off[e] == -INFINITY) out |= 1u << e;  // whatever its logit
+          p[e] = p[e] + off[e];
+        }
+      }
+      if (LISTS && named)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const unsigned at = named >> e & 1 ? word[own + c + e] >> kCountBits : 0;
+          if (!at) continue;
+          const float b = a.bias[row * a.nbias + at - 1];
+          if (b == -INFINITY) out |= 1u << e;
+          p[e] = p[e] + b;
+        }
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        float p = (float)raw[j][e];
-        float b = 0.f;
-        bool biased = false;
-        if (LISTS) {
-          const unsigned w = word[r * WIDE + c + e], count = w & ((1u << kCountBits) - 1), at = w >> kCountBits;
-          if (count) {
-            p = p > 0.f ? p / a.repeat : p * a.repeat;
-            const float f = (float)count * a.frequency;
-            p = p - (a.presence + f);
-          }
-          biased = at != 0;
-          if (biased) b = a.bias[row * a.nbias + at - 1];
-        }
-        if (a.offset) p = p + off[e];
-        if (biased) p = p + b;
-        p = p * a.scale;
-        if (lost) p = __builtin_nanf("");
-        // (out, whatever its logit)
-        if (!(bits >> e & 1) || c + e >= left || (a.offset && off[e] == -INFINITY) || b == -INFINITY) p = -INFINITY;
-        u[j][e] = p;
-        bad |= p != p;
-        if (p > top) top = p, id = v0 + c + e;
+        p[e] = p[e] * a.scale;
+        if (lost) p[e] = __builtin_nanf("");
+        u[j][e] = out >> e & 1 ? -INFINITY : p[e];
+        top = fmaxf(top, u[j][e]);  // (a NaN comes out in the sum)
       }
     }
-    near_top<L>(top, id);
-    if (L == 256) {
-      if (lane == 0) red_top[wave] = top, red_id[wave] = id;
-      __syncthreads();
-      top = red_top[0], id = red_id[0];
+    const float mine = top;
 #pragma unroll
-      for (int w = 1; w < 4; ++w)
-        if (red_top[w] > top || (red_top[w] == top && red_id[w] < id)) top = red_top[w], id = red_id[w];
+    for (int o = (L < 64 ? L : 64) / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (L == 256) {
+      if (lane == 0) red_top[wave] = top;
+      __syncthreads();
+      top = fmaxf(fmaxf(red_top[0], red_top[1]), fmaxf(red_top[2], red_top[3]));
     }
+    int id = INT_MAX;
+    if (mine == top && top > -INFINITY)
+#pragma unroll
+      for (int j = NV - 1; j >= 0; --j)
+#pragma unroll
+        for (int e = VEC - 1; e >= 0; --e)
+          if (u[j][e] == top) id = v0 + (j * L + l) * VEC + e;
     float sum = 0.f;
-    if (top > -INFINITY)
+    const float base = top == -INFINITY ? 0.f : top;
+    if (base < INFINITY) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum += term(u[j][e], top);
+        for (int e = 0; e < VEC; ++e) sum += __builtin_amdgcn_exp2f((u[j][e] - base) * kLog2e);
+    } else {  // its equals alone, and a NaN
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum += u[j][e] == base ? 1.f : u[j][e] != u[j][e] ? u[j][e] : 0.f;
+    }
     if (a.out && here) {
       T* out = (T*)a.out + row * a.ldo + v0;
 #pragma unroll
@@ -158,51 +203,53 @@ __global__ __launch_bounds__(256) void choose_kernel(ChooseArgs a, int slices, i
         if (c < left) store_part(out, c, left, u[j]);
       }
     }
-    int any = bad;
 #pragma unroll
     for (int o = (L < 64 ? L : 64) / 2; o; o >>= 1) {
       sum += __shfl_xor(sum, o, 64);
-      any |= __shfl_xor(any, o, 64);
+      id = min(id, __shfl_xor(id, o, 64));
     }
     if (L == 256) {
-      if (lane == 0) red_sum[wave] = sum, red_bad[wave] = any;
+      if (lane == 0) red_sum[wave] = sum, red_id[wave] = id;
       __syncthreads();
       sum = (red_sum[0] + red_sum[1]) + (red_sum[2] + red_sum[3]);
-      any = red_bad[0] | red_bad[1] | red_bad[2] | red_bad[3];
+      id = min(min(red_id[0], red_id[1]), min(red_id[2], red_id[3]));
     }
-    const Part part = {top, sum, id, any};
+    const Part part = {top, sum, id, sum != sum};
     if (l == 0 && here) {
       if (slices > 1)
         ((Part*)a.parts)[unit] = part;
       else
         finish(a, row, part);
     }
-    if (L == 256 || LISTS) __syncthreads();  // before the next unit's words and reductions
+    // before the next unit's words and reductions
+    if ((L == 256 || LISTS) && unit + gridDim.x < units) __syncthreads();
   }
 }
 
 // A row's slices, by a wavefront.
-__global__ __launch_bounds__(256) void join_kernel(ChooseArgs a, int slices) {
+__global__ __launch_bounds__(256) void join_kernel(ChooseArgs a, int parts) {
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= a.n) return;
-  const Part* p = (const Part*)a.parts + row * slices;
+  const Part* p = (const Part*)a.parts + row * parts;
   Part all = {-INFINITY, 0.f, INT_MAX, 0};
-  for (int s = lane; s < slices; s += 64) {
+  for (int s = lane; s < parts; s += 64) {
     const Part q = p[s];
     all.bad |= q.bad;
     if (q.top > all.top || (q.top == all.top && q.id < all.id)) all.top = q.top, all.id = q.id;
   }
   near_top<64>(all.top, all.id);
-  for (int s = lane; s < slices; s += 64)
-    if (p[s].sum > 0.f) all.sum += p[s].sum * term(p[s].top, all.top);
+  for (int s = lane; s < parts; s += 64)
+    if (p[s].sum > 0.f) all.sum += p[s].sum * term(p[s].top, all.top);  // (of NaN or nothing: no part)
   all.sum = wave_sum(all.sum);
 #pragma unroll
   for (int o = 32; o; o >>= 1) all.bad |= __shfl_xor(all.bad, o, 64);
   if (lane == 0) finish(a, row, all);
 }
 
-int slices_of(const ChooseArgs& a) { return a.classes > 64 * kEach ? (a.classes + kSlice - 1) / kSlice : 1; }
+int slices_of(const ChooseArgs& a) {
+  return a.classes > 64 * kEach ? (a.classes + 256 * kEach - 1) / (256 * kEach) : 1;
+}
 
 template <typename T, int L>
 void launch_rows(const ChooseArgs& a, int slices, hipStream_t s) {

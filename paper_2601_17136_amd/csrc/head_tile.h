@@ -54,14 +54,14 @@ __device__ inline void split_planes(float x, E (&out)[P]) {
 
 constexpr int kChunkK = 64;  // contraction indices of a chunk, to which operands are padded
 
-// A workgroup of GM x GN wavefronts, each WM x WN blocks of 32 x 32; two chunks
+// A workgroup of GM x GN wavefronts, each WM x WN blocks of 32 x 32; NST chunks
 // lie in LDS.
-template <int WM_, int WN_, int GM_, int GN_>
+template <int WM_, int WN_, int GM_, int GN_, int NST_ = 2>
 struct TileShape {
   static constexpr int WM = WM_, WN = WN_, GM = GM_, GN = GN_;
-  static constexpr int BM = WM * GM * 32, BN = WN * GN * 32, waves = GM * GN, threads = waves * 64;
+  static constexpr int NST = NST_, BM = WM * GM * 32, BN = WN * GN * 32, waves = GM * GN, threads = waves * 64;
   static constexpr int row_bytes = kChunkK * 2, slots = row_bytes / 16, group = 64 / slots;  // rows of a 1 KB load
-  static constexpr int stage_bytes = (BM + BN) * row_bytes, lds_bytes = stage_bytes * 2;
+  static constexpr int stage_bytes = (BM + BN) * row_bytes, lds_bytes = stage_bytes * NST;
   static constexpr int per_cu = lds_bytes <= 80 * 1024 ? 2 : 1;  // workgroups
   static constexpr int LA = BM / group / waves, LB = BN / group / waves;  // loads per wavefront and chunk
   static_assert(BM % (group * waves) == 0 && BN % (group * waves) == 0, "");
@@ -81,7 +81,7 @@ __device__ inline void wait_loads() { __builtin_amdgcn_s_waitcnt(7 << 4); }  // 
 // nseg x nkc (segment, chunk) pairs.  Loads go straight to LDS and permute
 // their source instead of their target, which is a wavefront's 1 KB in order.
 // Rows past the operand's end read its last one (what they give is not stored),
-// contraction indices past K read zero.  Chunk c + 1 is requested
+// contraction indices past K read zero.  Chunk c + NST - 1 is requested
 // while chunk c is multiplied; a step's operands are read from LDS while the
 // step before is multiplied, across the chunk's one barrier too.
 template <typename E, class S, class Rows = AsTheyAre>
@@ -89,8 +89,10 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
                                     int c0, int c1, char* lds, floatx16 (&acc)[S::WM][S::WN], Rows rows = {}) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host pass knows no buffer resources)
   constexpr unsigned kBound = 0x7ffffff0u, kOut = 0x80000000u;
-  constexpr int NS = kChunkK / 16, L = S::LA + S::LB;
-  constexpr int SP = NS / 2, LP = L / SP;  // a chunk's loads go out in its first SP steps
+  constexpr int NS = kChunkK / 16, L = S::LA + S::LB, NST = S::NST;
+  constexpr int SP = NS / 2;               // a chunk's loads go out in its first SP steps
+  constexpr int kAhead = (NST - 2) * L;    // loads that may be on their way when a chunk has to be there
+  static_assert(kAhead < 64, "what the counter holds");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
   const int lrow = lane / S::slots;
@@ -139,7 +141,7 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
     }
   };
   auto advance = [&]() {
-    fst ^= 1;
+    fst = fst + 1 == NST ? 0 : fst + 1;
     if (++fc < c1 && ++fk == nkc) {
       fk = 0;
       ++fs;
@@ -159,8 +161,7 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
   // the next step's operands (step kn of stage st) and the step's share of the
   // next chunk's loads.
   auto multiply = [&](int k, const char* st, int kn) {
-    constexpr int per = S::WM * S::WN, gap = per / LP;
-    static_assert(L % SP == 0 && per % LP == 0, "");
+    constexpr int per = S::WM * S::WN, all = SP * per;
 #pragma unroll
     for (int i = 0; i < per; ++i) {
       const int bi = i / S::WN, bj = i % S::WN;
@@ -168,21 +169,26 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = i * (S::WM + S::WN) / per; j < (i + 1) * (S::WM + S::WN) / per; ++j) read((k + 1) & 1, st, kn, j);
-      if (i % gap == 0 && k < SP) issue(k * LP + i / gap);
+      if (k < SP)
+#pragma unroll
+        for (int j = ((k * per + i) * L + all - 1) / all; j < ((k * per + i + 1) * L + all - 1) / all; ++j) issue(j);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   auto arrive = [&]() {  // this wavefront's part of the next chunk is in LDS; the barrier: everyone's
     __builtin_amdgcn_sched_barrier(0);
-    wait_loads();
+    __builtin_amdgcn_s_waitcnt((kAhead & 15) | (kAhead >> 4) << 14 | 7 << 4);  // (0: every load) and every LDS read
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
 #pragma unroll
-  for (int j = 0; j < L; ++j) issue(j);
-  advance();
+  for (int st = 0; st < NST - 1; ++st) {
+#pragma unroll
+    for (int j = 0; j < L; ++j) issue(j);
+    advance();
+  }
   arrive();
 #pragma unroll
   for (int i = 0; i < S::WM + S::WN; ++i) read(0, lds, 0, i);
@@ -190,7 +196,7 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
   for (int c = c0; c < c1; ++c) {
     // (the chunk fetched goes into the stage of chunk c - 1, which everyone has read)
     const char* st = lds + cst * S::stage_bytes;
-    cst ^= 1;
+    cst = cst + 1 == NST ? 0 : cst + 1;
 #pragma unroll
     for (int k = 0; k < NS - 1; ++k) multiply(k, st, k + 1);
     arrive();

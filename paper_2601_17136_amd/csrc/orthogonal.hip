@@ -581,13 +581,28 @@ hipError_t launch_flat(const OrthoArgs& a, void* scratch, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The largest magnitude of a s + b s^3 + c s^5 over [0, top], with some room.
+// The largest magnitude of a s + b s^3 + c s^5 over [0, top], with some room: at the end
+// or where the derivative, a + 3 b q + 5 c q^2 with q = s^2, is zero.
 double largest(double a, double b, double c, double top) {
-  double most = 0;
-  for (int i = 0; i <= 4096; ++i) {
-    const double s = top * i / 4096, q = s * s;
-    most = std::max(most, std::fabs(s * (a + q * (b + q * c))));
+  auto at = [&](double q) { return std::fabs(std::sqrt(q) * (a + q * (b + q * c))); };
+  double most = at(top * top);
+  double roots[2] = {-1, -1};
+  if (c != 0) {
+    const double d = 9 * b * b - 20 * a * c;
+    if (d >= 0)
+      for (int i = 0; i < 2; ++i) roots[i] = (-3 * b + (i ? 1 : -1) * std::sqrt(d)) / (10 * c);
+  } else if (b != 0) {
+    roots[0] = -a / (3 * b);
   }
+  for (double q : roots)
+    if (q > 0 && q < top * top) most = std::max(most, at(q));
+  return most * 1.01 + 1e-6;
+}
+// That of b q + c q^2 over [0, top^2]: of B's eigenvalues.
+double largest_even(double b, double c, double top) {
+  const double end = top * top, q = c != 0 ? -b / (2 * c) : -1;
+  double most = std::fabs(end * (b + end * c));
+  if (q > 0 && q < end) most = std::max(most, std::fabs(q * (b + q * c)));
   return most * 1.01 + 1e-6;
 }
 int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(top))); }
@@ -598,11 +613,11 @@ int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(to
 // 256 x 256 232 / 176 / 121 / 67 and 339 / 195 / 130 / 74, 256 x 128 260 / 92 / 59 / 33 and
 // 347 / 202 / 68 / 36, 128 x 128 232 / 109 / 41 / 20 and 371 / 180 / 54 / 22, 128 x 64 228 /
 // 102 / 46 / 16 and 405 / 176 / 58 / 19, 64 x 64 249 / 106 / 45 / 11 and 473 / 192 / 65 / 13.
-using Pair256 = PairShape<BigTile, 2>;                     // 128 KB
-using Pair256x128 = PairShape<TileShape<2, 2, 4, 2>, 3>;   // 144 KB
-using Pair128 = PairShape<TileShape<1, 2, 4, 2>, 4>;       // 128 KB
-using Pair128x64 = PairShape<TileShape<2, 1, 2, 2>, 3>;    // 72 KB
-using Pair64 = PairShape<TileShape<1, 1, 2, 2>, 4>;        // 64 KB
+using Pair256 = BigTile;                        // 128 KB
+using Pair256x128 = TileShape<2, 2, 4, 2, 3>;   // 144 KB
+using Pair128 = TileShape<1, 2, 4, 2, 4>;       // 128 KB
+using Pair128x64 = TileShape<2, 1, 2, 2, 3>;    // 72 KB
+using Pair64 = TileShape<1, 1, 2, 2, 4>;        // 64 KB
 struct PairCost {
   double end, alone, full;
 };
@@ -670,13 +685,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
     for (int t = 0; t < a.newton.steps; ++t) {
       const half_t *x = X[t & 1], *xt = XT[t & 1];
       const double ca = a.newton.coef[3 * t], cb = a.newton.coef[3 * t + 1], cc = a.newton.coef[3 * t + 2];
-      // B's eigenvalues are b q + c q^2 at q = s^2
-      double most = 0;
-      for (int i = 0; i <= 4096; ++i) {
-        const double v = top * top * i / 4096;
-        most = std::max(most, std::fabs(v * (cb + v * cc)));
-      }
-      const int eb = room_for(most * 1.01 + 1e-6), ea = cc == 0 ? eb : room_for(top * top);
+      const int eb = room_for(largest_even(cb, cc, top)), ea = cc == 0 ? eb : room_for(top * top);
       TileArgs g{};
       g.a = g.b = {x, p.ldx, p.S};
       g.stride_a = g.stride_b = sx;

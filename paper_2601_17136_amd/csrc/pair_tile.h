@@ -25,14 +25,6 @@ __device__ inline void split_pair(float v, half_t& hi, half_t& lo) {
   lo = (half_t)(v - (float)hi);
 }
 
-// Tiles of pairs: a TileShape whose blocks lie in NST stages of LDS.
-template <class S_, int NST_>
-struct PairShape : S_ {
-  static constexpr int NST = NST_;
-  static constexpr int lds_bytes = S_::stage_bytes * NST_;
-  static constexpr int per_cu = lds_bytes <= 80 * 1024 ? 2 : 1;
-};
-
 // acc = the tile at rows row0 of a and col0 of b over blocks [c0, c1) of the
 // contraction.  NP products of parts: 3, or of a's both and b's hi (2), or of hi and
 // hi (1).  Rows past an operand's end read its last one.  Loads go straight to LDS,
