@@ -1020,8 +1020,8 @@ Way way_of(int type, int64_t n, int d, int m, const void* x, int64_t ldx, const 
 // Rows of a tile of `shrink`: each reads its adapter's matrix once.
 int shrink_rows(const AdaptArgs& a) { return a.n >= 4096 && a.n >= 64 * (int64_t)a.adapters && a.rank <= 64 ? 32 : 16; }
 int64_t most_tiles(const AdaptArgs& a) { return cdiv(a.n, shrink_rows(a)) + std::min<int64_t>(a.adapters, a.n); }
-// Workgroups that plan: 1024 rows of each, or a 64th of all.
-int64_t plan_run(int64_t n) { return std::max<int64_t>(1024, up_to(cdiv(n, 64), 1024)); }
+// Rows of a workgroup that plans: all of few, else 1024, or a 64th of all.
+int64_t plan_run(int64_t n) { return n <= 2048 ? 2048 : std::max<int64_t>(1024, up_to(cdiv(n, 64), 1024)); }
 int64_t plan_runs(int64_t n) { return cdiv(n, plan_run(n)); }
 
 struct Scratch {

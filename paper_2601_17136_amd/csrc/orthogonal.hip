@@ -385,6 +385,10 @@ struct TileArgs {
   half_t *along, *across;
   int64_t ld_along, ld_across, stride_along, stride_across;
   Target out;
+  // The first `whole` tiles run whole; of the others' `splits` parts of the contraction
+  // each, the sums go to slabs, and a second launch joins and stores them.
+  int whole, splits;
+  float* slabs;
 };
 
 // A symmetric product's tiles, R times as high as wide: of row tile i those from its
@@ -421,7 +425,7 @@ __device__ inline void half_tile_of(unsigned g, unsigned total, int mt, int nt, 
 // The sums pass through LDS, 32 rows of each of the workgroup's GM at a time, so that
 // base is read and every result written 16 bytes a lane, whole 128-byte blocks in both
 // orders.
-template <class S, int NP, bool LAST, typename OT>
+template <class S, int NP, bool LAST, bool JOIN, typename OT>
 __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q) {
   constexpr int LD = S::BN + 4, ROWS = S::GM * 32, kRatio = S::BM / S::BN;
   static_assert(S::BM % S::BN == 0, "the diagonal's tiles");
@@ -429,17 +433,46 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
   __shared__ __attribute__((aligned(1024))) char lds[kBytes];
   const int64_t bt = blockIdx.y;
   int mi, ni;
-  if (q.half) {
-    half_tile_of<kRatio>(blockIdx.x, gridDim.x, q.mt, q.nt, mi, ni);
-  } else {
-    tile_of(blockIdx.x, (unsigned)(q.mt * q.nt), q.mt, q.nt, mi, ni);
-  }
+  const unsigned tiles = (unsigned)(q.half ? q.mt * q.nt - kRatio * (q.mt * (q.mt - 1) / 2) : q.mt * q.nt);
+  const int past = (int)blockIdx.x + (JOIN ? q.whole : 0) - q.whole;  // parts, or tiles, beyond the whole ones
+  const unsigned tile = past < 0 ? blockIdx.x : q.whole + (JOIN ? past : past / q.splits);
+  if (q.half)
+    half_tile_of<kRatio>(tile, tiles, q.mt, q.nt, mi, ni);
+  else
+    tile_of(tile, tiles, q.mt, q.nt, mi, ni);
   const int64_t r0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
-  PairSide a = q.a, b = q.b;
-  a.p += bt * q.stride_a;
-  b.p += bt * q.stride_b;
-  floatx16 acc[S::WM][S::WN];
-  pair_product<S, NP>(a, b, r0, n0, 0, q.nkb, lds, acc);
+  // (JOIN: a workgroup has one of WM times 32 GM rows of a tile)
+  constexpr int BI = JOIN ? 1 : S::WM;
+  const int bi0 = JOIN ? (int)blockIdx.z : 0;
+  floatx16 acc[BI][S::WN];
+  constexpr int64_t kTile = (int64_t)S::BM * S::BN;
+  // a thread's own sums, a workgroup apart
+  float* slab = q.slabs + (bt * ((int)tiles - q.whole) * q.splits + (JOIN ? past * q.splits : past)) * kTile + threadIdx.x;
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int bi = 0; bi < BI; ++bi)
+#pragma unroll
+      for (int bj = 0; bj < S::WN; ++bj)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          acc[bi][bj][r] = f(acc[bi][bj][r], (((bi0 + bi) * S::WN + bj) * 16 + r) * S::threads);
+  };
+  if constexpr (JOIN) {
+    each([&](float, int at) { return slab[at]; });
+#pragma unroll 2
+    for (int k = 1; k < q.splits; ++k)
+      each([&](float v, int at) { return v + slab[k * kTile + at]; });
+  } else {
+    PairSide a = q.a, b = q.b;
+    a.p += bt * q.stride_a;
+    b.p += bt * q.stride_b;
+    const int part = past < 0 ? 0 : past % q.splits, parts = past < 0 ? 1 : q.splits;
+    pair_product<S, NP>(a, b, r0, n0, q.nkb * part / parts, q.nkb * (part + 1) / parts, lds, acc);
+    if (past >= 0) {
+      each([&](float v, int at) { return slab[at] = v; });
+      return;
+    }
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
   const half_t* base = q.base ? q.base + bt * q.stride_base : nullptr;
@@ -448,13 +481,14 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
   const bool turned = !q.half || ni >= (mi + 1) * kRatio;  // (the diagonal's blocks are whole as they are)
   float* sums = (float*)lds;
 #pragma unroll
-  for (int bi = 0; bi < S::WM; ++bi) {
-    if (bi) __syncthreads();
+  for (int own = 0; own < BI; ++own) {
+    const int bi = bi0 + own;
+    if (own) __syncthreads();
 #pragma unroll
     for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        sums[(wm * 32 + acc_row(r, h)) * LD + (wn * S::WN + bj) * 32 + l32] = acc[bi][bj][r];
+        sums[(wm * 32 + acc_row(r, h)) * LD + (wn * S::WN + bj) * 32 + l32] = acc[own][bj][r];
     __syncthreads();
 #pragma unroll
     for (int e = threadIdx.x; e < ROWS * (S::BN / 8); e += S::threads) {
@@ -518,32 +552,6 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align(size_t v) { return (v + 255) / 256 * 256; }
-
-// The tiled form's layout for one group of matrices.
-struct TiledPlan {
-  int64_t S, len;     // short and long side
-  int64_t ldx, ldxt;  // of X (S rows) and X^T (len rows)
-  int64_t group;      // matrices at a time
-  int parts;
-  size_t x, xt, a, norm, total;  // bytes of one buffer each, and of all
-};
-constexpr size_t kGroupBytes = (size_t)1 << 30;
-TiledPlan tiled_plan(const OrthoArgs& a) {
-  TiledPlan p;
-  p.S = std::min(a.m, a.n);
-  p.len = std::max(a.m, a.n);
-  p.ldx = pair_ld(p.len);
-  p.ldxt = pair_ld(p.S);
-  p.parts = (int)std::min<int64_t>(cdiv(a.m * cdiv(a.n, 8), 256), 1024);
-  const size_t one = (size_t)(2 * p.S * p.ldx + 2 * p.len * p.ldxt + 2 * p.S * p.ldxt) * sizeof(half_t);
-  p.group = std::max<int64_t>(1, std::min<int64_t>({a.batch, (int64_t)(kGroupBytes / one), 65535}));
-  p.x = align((size_t)p.group * p.S * p.ldx * sizeof(half_t));
-  p.xt = align((size_t)p.group * p.len * p.ldxt * sizeof(half_t));
-  p.a = align((size_t)p.group * p.S * p.ldxt * sizeof(half_t));
-  p.norm = align((size_t)p.group * p.parts * sizeof(double));
-  p.total = 2 * (p.x + p.xt + p.a) + p.norm;
-  return p;
-}
 
 int flat_splits(const OrthoArgs& a) {
   const int64_t chunks = cdiv(std::max(a.m, a.n), kLong);
@@ -621,32 +629,101 @@ using Pair64 = TileShape<1, 1, 2, 2, 4>;        // 64 KB
 struct PairCost {
   double end, alone, full;
 };
+// How a launch runs: in which tiles, how many of them whole, and the parts of the
+// others (1: none), by what it takes.  The tiles past the last full round of 256 leave
+// most CUs idle for a round's time; in parts they take a share of it and a second
+// launch.  A Gram matrix of 4096 in 136 tiles of 256 x 256 232 us, in 256 of 256 x 128 and
+// 16 of 8 parts each 194 and 14.
+struct PairRun {
+  int shape, whole, splits;
+  int64_t slab;  // floats
+};
 template <class S>
-double pair_time(const PairCost& c, const TileArgs& q, unsigned nb) {
+void consider(int shape, const PairCost& c, const TileArgs& q, unsigned nb, double& best, PairRun& run) {
   const int64_t mt = cdiv(q.M, S::BM), nt = cdiv(q.N, S::BN);
-  const double tiles = (double)nb * (q.half ? mt * nt - S::BM / S::BN * (mt * (mt - 1) / 2) : mt * nt);
-  const double rounds = std::floor(tiles / 256), left = tiles / 256 - rounds;
-  return c.end + q.nkb * (rounds * c.full + (left > 0 ? c.alone + (c.full - c.alone) * left * left * left : 0));
+  const int64_t tiles = q.half ? mt * nt - S::BM / S::BN * (mt * (mt - 1) / 2) : mt * nt;
+  const double all = (double)nb * tiles / 256, rounds = std::floor(all), left = all - rounds;
+  auto take = [&](double t, int64_t whole, int splits) {
+    if (run.splits && t >= best) return;
+    best = t;
+    run = {shape, (int)whole, splits, splits > 1 ? (tiles - whole) * splits * nb * S::BM * S::BN : 0};
+  };
+  auto round = [&](double part) { return part > 0 ? c.alone + (c.full - c.alone) * part * part * part : 0; };
+  take(c.end + q.nkb * (rounds * c.full + round(left)), tiles, 1);
+  if (nb != 1 || rounds < 1 || left == 0) return;
+  const int64_t whole = (int64_t)rounds * 256;
+  for (int splits = 2; splits <= 8 && left * splits <= 1 && q.nkb / splits >= 4; ++splits)
+    take(c.end + q.nkb * (rounds * c.full + round(left * splits) / splits) + 10 + splits * (S::BM * S::BN * 4e-5 / S::WM),
+         whole, splits);
+}
+PairRun pair_run(const TileArgs& q, unsigned nb) {
+  PairRun run{};
+  double best = 0;
+  consider<Pair256>(0, {13, 1.8, 2.6}, q, nb, best, run);
+  consider<Pair256x128>(1, {7, 0.85, 1.35}, q, nb, best, run);
+  consider<Pair128>(2, {6, 0.5, 0.73}, q, nb, best, run);
+  consider<Pair128x64>(3, {6, 0.33, 0.39}, q, nb, best, run);
+  consider<Pair64>(4, {6, 0.2, 0.225}, q, nb, best, run);
+  return run;
 }
 template <class S, int NP, bool LAST, typename OT>
-void launch_shape(TileArgs q, unsigned nb, hipStream_t s) {
+void launch_shape(TileArgs q, const PairRun& run, unsigned nb, hipStream_t s) {
   q.mt = (int)cdiv(q.M, S::BM);
   q.nt = (int)cdiv(q.N, S::BN);
+  q.whole = run.whole;
+  q.splits = run.splits;
   const int tiles = q.half ? q.mt * q.nt - S::BM / S::BN * (q.mt * (q.mt - 1) / 2) : q.mt * q.nt;
-  pair_kernel<S, NP, LAST, OT><<<dim3((unsigned)tiles, nb), S::threads, 0, s>>>(q);
+  const unsigned blocks = (unsigned)(run.whole + (tiles - run.whole) * run.splits);
+  pair_kernel<S, NP, LAST, false, OT><<<dim3(blocks, nb), S::threads, 0, s>>>(q);
+  if (run.whole < tiles)
+    pair_kernel<S, NP, LAST, true, OT><<<dim3((unsigned)(tiles - run.whole), nb, S::WM), S::threads, 0, s>>>(q);
 }
 template <int NP, bool LAST, typename OT>
 void launch_pair(const TileArgs& q, unsigned nb, hipStream_t s) {
-  const double t[5] = {pair_time<Pair256>({13, 1.8, 2.6}, q, nb), pair_time<Pair256x128>({7, 0.85, 1.35}, q, nb),
-                       pair_time<Pair128>({6, 0.5, 0.73}, q, nb), pair_time<Pair128x64>({6, 0.33, 0.39}, q, nb),
-                       pair_time<Pair64>({6, 0.2, 0.225}, q, nb)};
-  switch (std::min_element(t, t + 5) - t) {
-    case 0: return launch_shape<Pair256, NP, LAST, OT>(q, nb, s);
-    case 1: return launch_shape<Pair256x128, NP, LAST, OT>(q, nb, s);
-    case 2: return launch_shape<Pair128, NP, LAST, OT>(q, nb, s);
-    case 3: return launch_shape<Pair128x64, NP, LAST, OT>(q, nb, s);
-    default: return launch_shape<Pair64, NP, LAST, OT>(q, nb, s);
+  const PairRun run = pair_run(q, nb);
+  switch (run.shape) {
+    case 0: return launch_shape<Pair256, NP, LAST, OT>(q, run, nb, s);
+    case 1: return launch_shape<Pair256x128, NP, LAST, OT>(q, run, nb, s);
+    case 2: return launch_shape<Pair128, NP, LAST, OT>(q, run, nb, s);
+    case 3: return launch_shape<Pair128x64, NP, LAST, OT>(q, run, nb, s);
+    default: return launch_shape<Pair64, NP, LAST, OT>(q, run, nb, s);
   }
+}
+
+// The tiled form's layout for one group of matrices.
+struct TiledPlan {
+  int64_t S, len;     // short and long side
+  int64_t ldx, ldxt;  // of X (S rows) and X^T (len rows)
+  int64_t group;      // matrices at a time
+  int parts;
+  size_t x, xt, a, norm, slabs, total;  // bytes of one buffer each, and of all
+};
+constexpr size_t kGroupBytes = (size_t)1 << 30;
+TiledPlan tiled_plan(const OrthoArgs& a) {
+  TiledPlan p;
+  p.S = std::min(a.m, a.n);
+  p.len = std::max(a.m, a.n);
+  p.ldx = pair_ld(p.len);
+  p.ldxt = pair_ld(p.S);
+  p.parts = (int)std::min<int64_t>(cdiv(a.m * cdiv(a.n, 8), 256), 1024);
+  const size_t one = (size_t)(2 * p.S * p.ldx + 2 * p.len * p.ldxt + 2 * p.S * p.ldxt) * sizeof(half_t);
+  p.group = std::max<int64_t>(1, std::min<int64_t>({a.batch, (int64_t)(kGroupBytes / one), 65535}));
+  p.x = align((size_t)p.group * p.S * p.ldx * sizeof(half_t));
+  p.xt = align((size_t)p.group * p.len * p.ldxt * sizeof(half_t));
+  p.a = align((size_t)p.group * p.S * p.ldxt * sizeof(half_t));
+  p.norm = align((size_t)p.group * p.parts * sizeof(double));
+  // the largest of the launches' slabs (only of a matrix by itself)
+  p.slabs = 0;
+  for (int k = 0; k < 4; ++k) {
+    TileArgs q{};
+    q.half = k < 2;
+    q.M = k == 3 ? p.len : p.S;
+    q.N = k == 2 ? p.len : p.S;
+    q.nkb = (int)((k == 0 ? p.ldx : p.ldxt) / (2 * kPairBlock));
+    p.slabs = std::max(p.slabs, align((size_t)pair_run(q, 1).slab * sizeof(float)));
+  }
+  p.total = 2 * (p.x + p.xt + p.a) + p.norm + p.slabs;
+  return p;
 }
 
 // Products of parts that a result of type T is worth.  A bfloat16 result is rounded
@@ -671,7 +748,8 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
   half_t *X[2], *XT[2];
   for (int i = 0; i < 2; ++i) X[i] = take(p.x), XT[i] = take(p.xt);
   half_t *A = take(p.a), *B = take(p.a);
-  double* norm = (double*)at;
+  double* norm = (double*)take(p.norm);
+  float* slabs = (float*)at;
   const int64_t sx = p.S * p.ldx, sxt = p.len * p.ldxt, sa = p.S * p.ldxt;
   for (int64_t b0 = 0; b0 < a.batch; b0 += p.group) {
     const unsigned nb = (unsigned)std::min(p.group, a.batch - b0);
@@ -687,6 +765,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       const double ca = a.newton.coef[3 * t], cb = a.newton.coef[3 * t + 1], cc = a.newton.coef[3 * t + 2];
       const int eb = room_for(largest_even(cb, cc, top)), ea = cc == 0 ? eb : room_for(top * top);
       TileArgs g{};
+      g.slabs = slabs;
       g.a = g.b = {x, p.ldx, p.S};
       g.stride_a = g.stride_b = sx;
       g.M = g.N = p.S;
@@ -713,6 +792,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       top = largest(ca, cb, cc, top);
       const int en = last ? 0 : room_for(top);  // the result is stored as it is
       TileArgs m{};
+      m.slabs = slabs;
       const PairSide sb = {B, p.ldxt, p.S}, sxs = {xt, p.ldxt, p.len};
       const bool turned = last && tall;  // the result's rows are the long side
       m.a = turned ? sxs : sb;
