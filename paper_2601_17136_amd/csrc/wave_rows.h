@@ -47,14 +47,19 @@ __device__ inline void wave_rows(RA row_a, RB row_b, int d, char* lds, floatx4 (
       for (int i = 0; i < L; ++i) reg[set][i] = load_raw(from[i], k, d);
     }
   };
-  auto to_lds = [&](int set) {
+  auto in_order = []() {  // of the wavefront's own LDS accesses, which the hardware keeps
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  auto to_lds = [&](int set) {
+    in_order();
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const int r = i * 8 + lane / 8;
       *(raw_vec<T>*)(own + r * 128 + ((lane & 7) ^ turn(r)) * 16) = reg[set][i];
     }
-    __builtin_amdgcn_wave_barrier();
+    in_order();
   };
   auto products = [&]() {
     raw_vec<T> fa[2][S::NA], fb[2][S::NB];

@@ -150,7 +150,10 @@ def adapted(x, w, down, up, ids, factor, dy):
         t, u = f[g] * (x[i] @ down[g].t()), f[g] * (dy[i] @ up[g])
         dt = f[g].abs() * (_sums(d, torch.float32) + 4 * U) * (x[i].abs() @ down[g].abs().t())
         du = f[g].abs() * (_sums(m, torch.float32) + 4 * U) * (dy[i].abs() @ up[g].abs())
-        low, rows = (r + 8) * 2 * U, (i.numel() / 4 + 40) * 2 * U
+        # (of 16-bit rows t and u are two parts of the rows' type, 16 or 22 bits, in y and dx, and two bfloat16 parts in
+        # the adapters' gradients)
+        low = (r + 8) * 2 * U + {torch.float32: 0.0, torch.float16: 2.0 ** -21, torch.bfloat16: 2.0 ** -16}[dtype]
+        rows = (i.numel() / 4 + 40) * 2 * U + (0.0 if dtype == torch.float32 else 2.0 ** -16)
         out["y"][i] += t @ up[g].t()
         tol["y"][i] += (dt + low * t.abs()) @ up[g].abs().t()
         out["dx"][i] += u @ down[g]

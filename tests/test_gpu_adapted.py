@@ -158,6 +158,34 @@ def test_rows_far_apart(ctx):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("s", [1, 1000])
+def test_two_million_rows(ctx, s):
+    """The largest n: the rows' order by many workgroups."""
+    from paper_2601_17136_amd import kkm
+    n, d, m, r = 1 << 21, 16, 24, 2
+    x, w, down, up, ids, f, dy = _case(n, d, m, s, r, "f16", 13)
+    y, ddown = torch.empty(n, m, device="cuda", dtype=torch.float16), torch.empty_like(down)
+    kkm.kkm_adapted_linear(ctx, x, w, down, up, ids, y, factor=f)
+    kkm.kkm_adapted_linear_grad(ctx, x, w, down, up, ids, dy, ddown=ddown, factor=f)
+    at = ids.clamp(min=0).long()
+    on = (ids >= 0).double()[:, None]
+    xd, wd = x.double(), w.double()
+    t = torch.stack([(xd * down[at, k].double()).sum(1) for k in range(r)], 1) * f[at].double()[:, None] * on
+    want, size = xd @ wd.t(), xd.abs() @ wd.abs().t()
+    for k in range(r):
+        want += t[:, k:k + 1] * up[at, :, k].double()
+        size += t[:, k:k + 1].abs() * up[at, :, k].double().abs()
+    off = (y.double() - want).abs()
+    assert bool((off <= want.abs() * (2.0 ** -11 + 4 * ref.U) + 64 * ref.U * size + 2.0 ** -20 * size + 2.0 ** -24).all())
+    u = torch.stack([(dy.double() * up[at, :, k].double()).sum(1) for k in range(r)], 1) * f[at].double()[:, None] * on
+    for k in range(r):
+        sums = torch.zeros(s, d, dtype=torch.float64, device="cuda").index_add_(0, at, u[:, k:k + 1] * xd)
+        sizes = torch.zeros(s, d, dtype=torch.float64, device="cuda").index_add_(0, at, (u[:, k:k + 1] * xd).abs())
+        rows = n / s / 4 + 2000
+        off = (ddown[:, k].double() - sums).abs()
+        assert bool((off <= sums.abs() * 2.0 ** -11 + (rows * 2 * ref.U + 2.0 ** -16) * sizes + 2.0 ** -24).all())
+
+
 def test_gradient_against_differences(ctx):
     """<dy, y(p + h q) - y(p - h q)> = 2 h <dp, q>, exact but for roundings: y is linear in each of x, down and up."""
     from paper_2601_17136_amd import kkm
