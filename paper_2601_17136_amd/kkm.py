@@ -182,6 +182,11 @@ def _dev_ptr(t, dtype, name, numel=None):
     """Raw device address of a contiguous CUDA/HIP tensor, with its checks."""
     if t is None:
         return None
+    try:  # (calls of a few microseconds are counted in these checks)
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (numel is None or t.numel() == numel):
+            return t.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(t, int):
         return t
     import torch
@@ -520,8 +525,7 @@ def _type_code(dtype, name):
 
 def _rows(t, name, dtype=None, shape=None):
     """(address, row stride in elements) of a device matrix whose rows are contiguous."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name} must be a device tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
@@ -729,8 +733,7 @@ def kkm_adapted_linear_grad(ctx, x, w, down, up, ids, dy, dx=None, ddown=None, d
 
 def _matrices(t, name, dtype=None, shape=None):
     """(address, row stride, matrix stride) of a device matrix, or of a batch of them, with contiguous rows."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not getattr(t, "is_cuda", False):
         raise TypeError(f"{name} must be a device tensor")
     if t.dim() not in (2, 3):
         raise ValueError(f"{name} must be a matrix or a batch of them, got {t.dim()} dimensions")

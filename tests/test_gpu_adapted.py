@@ -58,7 +58,7 @@ def _check(case, got):
 
 
 # rows, width, columns, adapters, rank
-DIRECT = [(1, 1, 1, 1, 1), (1, 784, 64, 8, 8), (5, 7, 3, 2, 1), (3, 100, 1000, 40, 17), (16, 33, 65, 5, 16), (17, 64, 16, 1, 5),
+DIRECT = [(1, 1, 1, 1, 1), (1, 784, 64, 8, 8), (1, 1001, 333, 3, 16), (1, 70, 40, 2, 17), (5, 7, 3, 2, 1), (3, 100, 1000, 40, 17), (16, 33, 65, 5, 16), (17, 64, 16, 1, 5),
           (31, 300, 130, 31, 33), (33, 54, 7, 2, 3), (64, 256, 300, 9, 64), (65, 65, 65, 3, 2), (100, 784, 10, 4, 8),
           (257, 48, 200, 1, 100), (1000, 130, 64, 7, 128), (3000, 16, 17, 20, 4), (700, 301, 129, 90, 12),
           (40, 2000, 2100, 3, 8), (2500, 40, 30, 1024, 2)]
@@ -130,6 +130,22 @@ def test_no_rows_and_no_factor(ctx):
     case = list(_case(90, 30, 20, 4, 5, "f32", 4))
     case[5] = None
     _check(case, _run(ctx, *case))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_row_of_each_id(ctx, dtype):
+    """A row by itself: of each adapter, of none, and of an id past the last, NaN in the other adapters."""
+    from paper_2601_17136_amd import kkm
+    x, w, down, up, _, f, dy = _case(1, 130, 50, 4, 7, dtype, 21)
+    for g in (-1, 0, 3, 4, 2 ** 31 - 1, -2 ** 31):
+        ids = torch.tensor([g], dtype=torch.int32, device="cuda")
+        d2, u2, f2 = (torch.full_like(t, NAN) for t in (down, up, f))
+        if 0 <= g < 4:
+            d2[g], u2[g], f2[g] = down[g], up[g], f[g]
+        y = torch.empty(1, 50, device="cuda", dtype=x.dtype)
+        kkm.kkm_adapted_linear(ctx, x, w, d2, u2, ids, y, factor=f2)
+        want, tol = ref.adapted(x, w, down, up, ids, f, dy)
+        ref.check("y", y, want["y"], tol["y"])
 
 
 def test_all_rows_without_an_adapter(ctx):
