@@ -67,8 +67,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 5 : 6) void choose_kernel(Cho
   __shared__ int red_id[4];
   const int l = threadIdx.x % L, r = threadIdx.x / L, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t row = L == 256 ? unit / slices : unit * ROWS + r;
-    const int slice = L == 256 ? (int)(unit - row * slices) : 0, v0 = slice * WIDE;
+    // (n times slices is below 2^31; in scalar registers)
+    const unsigned whole = L == 256 ? __builtin_amdgcn_readfirstlane((unsigned)unit / (unsigned)slices) : 0u;
+    const int64_t row = L == 256 ? whole : unit * ROWS + r;
+    const int slice = L == 256 ? __builtin_amdgcn_readfirstlane((unsigned)unit - whole * slices) : 0, v0 = slice * WIDE;
     const bool here = row < a.n;
     const int left = here ? min(a.classes - v0, WIDE) : 0;  // classes of the row's slice
     raw_vec<T> raw[NV];

@@ -194,6 +194,7 @@ __global__ __launch_bounds__(256) void flat_steps_kernel(const double* __restric
   const int64_t b = blockIdx.x;
   for (int e = threadIdx.x; e < S16 * S16; e += 256) {
     double s = 0;
+#pragma unroll 8
     for (int k = 0; k < count; ++k) s += slabs[(b * count + k) * (S16 * S16) + e];
     A[e / S16 * LD + e % S16] = s;
   }
