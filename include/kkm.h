@@ -619,8 +619,13 @@ int kkm_distill_grad(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teac
  * (rank x d) and up (m x rank), one after another without gaps, all of one type.
  * factor (fp32[adapters], may be NULL: ones) holds f.  A row of negative id has no
  * adapter; one whose id is >= adapters is NaN.  What an adapter holds reaches its own
- * rows alone.  fp32 operands of large products are three bfloat16 parts, as the
- * head's. */
+ * rows alone.
+ *
+ * More than 64 rows and 2^23 products (n m d) run in tiles.  There fp32 rows are two
+ * binary16 parts at a power of two of each row of x (dy) and of w: 22 bits of an entry
+ * down to 2^-17 of its row's largest, 2^-40 of that below; an infinite entry gives NaN.
+ * down x and up^T dy are fp32, and of 16-bit matrices two parts of 16 bits together (22
+ * of binary16) in their second products, two of 16 bits in the adapters' gradients. */
 #define KKM_MAX_RANK 128
 #define KKM_MAX_ADAPTERS 1024
 typedef struct kkm_adapted {
@@ -638,8 +643,8 @@ typedef struct kkm_adapted {
 } kkm_adapted;
 
 /* Scratch: 12 bytes a row, 4 a row and rank (padded to 16, 32, 64 or 128); and copies
- * of x and w where the product runs in tiles and they are fp32 (6 bytes an entry) or
- * not aligned to 16 bytes (2). */
+ * of x and w where the product runs in tiles and they are fp32 (4 bytes an entry), or
+ * not of whole 16 bytes or past 2 GB (2). */
 int kkm_adapted_linear(kkm_ctx *ctx, const kkm_adapted *a, void *y, int64_t ldy);
 
 /* The gradient from dy (n x m); w, which the rows share, is held:
@@ -647,7 +652,9 @@ int kkm_adapted_linear(kkm_ctx *ctx, const kkm_adapted *a, void *y, int64_t ldy)
  *   ddown_g = sum_{i: ids_i = g} u_i x_i^T,  dup_g = sum_{i: ids_i = g} f_g dy_i (down_g x_i)^T
  * into dx (n x d), ddown and dup (as down and up); each may be NULL.  Adapters without
  * rows have zeros, as all have where n = 0.  Rows of an id >= adapters have dx NaN and
- * take no other part. */
+ * take no other part.  Scratch beside that above: w, down and up turned, and 4 bytes for
+ * each entry of an adapter's gradients and piece of its rows (64 at least; all adapters
+ * together at most 1024 pieces and one of each). */
 int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, int64_t lddy, void *dx, int64_t lddx,
                             void *ddown, void *dup);
 
@@ -658,8 +665,10 @@ int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, 
  * with its own a, b, c: singular values s become a s + b s^3 + c s^5, singular
  * vectors stay.  batch matrices of m x n, `stride` elements apart, each by itself.
  *
- * The products hold fp32's accuracy for every type: a short side of at most 64
- * runs in 64 bits, others in two binary16 parts (22 bits) of each factor.  Steps
+ * A short side of at most 64 runs in 64 bits.  Others run in two binary16 parts (22
+ * bits) of each factor, which hold fp32's accuracy; for bfloat16 results X enters A and
+ * (b A + c A^2) X with one part (11 bits): 0.0003 to 0.0011 of the result in the 2-norm,
+ * beside the 0.0017 of its rounding.  Steps
  * that would let a singular value of at most 1 grow past 2^12 are refused.  A NaN or
  * infinity spoils its matrix.  Scratch: 24 bytes an entry of matrices more than 64
  * wide and high (of a batch, as many at a time as 1 GB holds). */

@@ -10,15 +10,15 @@
 //
 //   plan       order of the rows, where each adapter's begin
 //   turn       (gradient) w^T, up^T, down^T
-//   shrink     t, u: 16 rows of one adapter a workgroup
+//   shrink     t, u: 16 or 32 rows of one adapter a workgroup
 //   project    w's product with the adapters' part added before the one rounding:
-//              direct, from the rows as they are (at most 64 rows or columns, or
-//              little work), or in tiles of the sorted rows (head_tile.h)
+//              direct, from the rows as they are (at most 64 rows, or little work),
+//              or in tiles of the sorted rows (head_tile.h; fp32: pair_tile.h)
 //   outer      (gradient) the adapters' gradients of a piece of an adapter's rows
 //   join       their sums over the pieces
 //
-// The adapters' products run on the fp32 matrix cores: they are few beside w's, and
-// t and u keep all their bits.
+// t and u are used in fp32 or, beside 16-bit matrices, as two parts of 16 bits: their
+// products are few beside w's.  A row by itself takes one launch, at most 64 rows two.
 #include <algorithm>
 #include <cmath>
 
@@ -41,7 +41,7 @@ struct RowPlan {
 // The rows are cut into runs of a workgroup (`run` rows), whose wavefronts count and
 // then place theirs, 64 at a time.  More than one run: a launch counts them first, and
 // each workgroup sums what lies before its own.  20000 rows of 8 adapters by one
-// workgroup 31 us, by 20 in two launches 9.
+// workgroup 31 us, by 20 in two launches 5 and 8, of which most is the launches.
 constexpr int kPlanWaves = 16, kPlanAhead = 8;  // ids of so many 64 rows are read at a time
 __device__ inline int bucket_of(int g, int adapters) { return g < 0 ? adapters : g >= adapters ? adapters + 1 : g; }
 // The lanes whose b is this lane's (none of b < 0).
@@ -195,7 +195,8 @@ __device__ inline int owner(const int32_t* __restrict__ first, int count, int at
 
 // ------------------------------------------------------------------ turned copies
 
-// dst[c][r] = src[r][c] of `count` matrices, 64 x 64 at a time.
+// dst[c][r] = src[r][c] of `count` matrices, 64 x 64 at a time.  4096 x 4096 and 16
+// adapters of 32 ranks on both sides, bfloat16: 17 us, 5.1 TB/s read and written.
 struct TurnJob {
   const void* src;
   int64_t ld, rows, cols, ldd;
@@ -274,7 +275,9 @@ struct ShrinkJobs {
 };
 
 // NB x 16 rows of an adapter by its rank; the wavefronts share the width and join in
-// LDS.  8192 bfloat16 rows of 4096, 32 ranks of 16 adapters SHRINKUS.
+// LDS.  Bound by reading the rows: 8192 bfloat16 rows of 4096, 32 ranks of 16 adapters
+// 25 us, 2.6 TB/s, both sides of the gradient 41, 3.3 TB/s (45 a call on average with
+// lanes of 16 rows each).
 template <typename T, class S>
 __global__ __launch_bounds__(S::WV * 64) void shrink_kernel(ShrinkJobs q) {
   constexpr int R = S::NA * 16, N = S::NB * 16;
@@ -325,7 +328,7 @@ __global__ __launch_bounds__(S::WV * 64) void shrink_kernel(ShrinkJobs q) {
 }
 
 // Few rows, in their own order (no plan): a workgroup a row, its wavefronts the
-// adapter's rows of the rank in turn.
+// adapter's rows of the rank in turn.  32 rows of 4096, each its own 16 ranks: 6 us.
 template <typename T>
 __global__ __launch_bounds__(1024) void shrink_rows_kernel(const T* __restrict__ x, int64_t ldx, int d,
                                                            const T* __restrict__ down, int adapters, int rank, int R,
@@ -377,7 +380,8 @@ struct ProjectArgs {
 };
 
 // NA x 16 columns of y by NB x 16 rows, from the rows as they are; the wavefronts share
-// the width and join in LDS.  32 rows of 4096 by 4096, 32 adapters of 16, bfloat16: DIRECTUS.
+// the width and join in LDS.  Bound by reading w, and by the rows, which every workgroup
+// reads: 32 rows of 4096 by 4096, 32 adapters of 16, bfloat16: 10.5 us, 3.6 TB/s.
 template <typename T, class S>
 __global__ __launch_bounds__(S::WV * 64) void direct_kernel(ProjectArgs a) {
   constexpr int C = S::NA * 16, N = S::NB * 16, THREADS = S::WV * 64, EACH = (C * N + THREADS - 1) / THREADS,
@@ -492,7 +496,9 @@ __global__ __launch_bounds__(512) void one_row_kernel(ProjectArgs a, const T* __
 
 // A tile of the sorted rows; the adapters of each 32 rows one after another.  Their
 // products go into sums of their own, of which a row takes its adapter's: what
-// another adapter holds, were it NaN, does not reach it.
+// another adapter holds, were it NaN, does not reach it.  Bound by the matrix cores: 8192
+// bfloat16 rows of 4096 by 4096 with 32 ranks 247 to 264 us, 1.04 to 1.12 PFLOP/s; fp32,
+// 20000 of 784 by 1024 132 us, 243 TFLOP/s of fp32 products, 30 of it tiles' ends.
 struct TileProject {
   ProjectArgs a;
   Side x, w;
@@ -643,7 +649,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
 // zero from d on; fp32 rows as pairs, kp a whole number of blocks, each at the power of
 // two that brings its largest entry to 2^14 .. 2^15 (`exps`): 22 bits of an entry down to
 // 2^-17 of the row's largest, and 2^-40 of that below.  A row with an infinity or NaN is
-// taken as it is.
+// taken as it is.  20000 fp32 rows of 784 and 1024 of w 30 us, 4.4 TB/s.
 struct CopyJob {
   const void* src;
   int64_t ld, rows;
@@ -711,7 +717,8 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyJobs jobs, int d, int kp)
 // out[r][c] = sum over a piece of an adapter's rows of coef[place][r] X[row][c], to
 // the piece's slab: CT x 16 of the rank by 16 kVec columns a workgroup.  A step is 4
 // rows: a lane loads kVec columns of row lane / 16; the four wavefronts take every
-// fourth run of steps and join in LDS.
+// fourth run of steps and join in LDS.  20000 fp32 rows of 784 + 1024, 8 ranks 40 us, 3.6
+// TB/s.
 struct OuterJob {
   const float* coef;  // n x R, in sorted order
   const void* X;
@@ -813,7 +820,7 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
 // them a lane's, whose 8 x 8 values it turns in registers so that a column's 8 rows lie
 // together.  coef is two bfloat16 parts (16 bits, at any size); a binary16 row is two as
 // well, which hold all of it, and three products.  8192 bfloat16 rows of 4096 + 4096 and
-// 32 ranks: 78 us by the fp32 matrix cores.
+// 32 ranks: 44 us, 3.0 TB/s, where the fp32 matrix cores take 78.
 template <typename T, int CT>
 __global__ __launch_bounds__(256) void outer16_kernel(OuterJobs q) {
   constexpr int W = 128;
@@ -938,7 +945,8 @@ struct JoinArgs {
   const int32_t* piece;
   void *ddown, *dup;  // each may be null
 };
-// A workgroup has 64 columns of 8 rows of an adapter's rank, a wavefront two of these rows.
+// A workgroup has 64 columns of 8 rows of an adapter's rank, a wavefront two of these
+// rows.  33 MB of slabs 15 us.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
   __shared__ float turned[64][8 + 1];
@@ -1003,11 +1011,14 @@ struct Layout {
   }
 };
 
-// A piece of an adapter's rows in `outer`: so many that the pieces fill the card
-// with four workgroups a CU, 64 at least.
+// A piece of an adapter's rows in `outer`: 64 at least, and so many that the pieces of
+// all fill the card with two workgroups a CU, four of fp32.  The adapters' gradients in
+// microseconds with two / four / eight: bfloat16 8192 x 4096 to 4096, 16 adapters of 32
+// ranks 104 / 109 / 121, 4096 x 1000 to 1000, 60 of 16 60 / 70 / 71, binary16, 32 of 64 121 /
+// 156 / 157; fp32 20000 x 784 to 1024, 8 of 8 105 / 89 / 87.
 int piece_of(const AdaptArgs& a) {
   const int64_t w = 16 * 16 / (int64_t)elem_bytes(a.type), across = cdiv(a.d, w) + cdiv(a.m, w);
-  const int64_t pieces = std::max<int64_t>(1, 1024 / across);
+  const int64_t pieces = std::max<int64_t>(1, (a.type == TYPE_F32 ? 1024 : 512) / across);
   return (int)std::min<int64_t>(up_to(std::max<int64_t>(64, cdiv(a.n, pieces)), 16), 1 << 20);
 }
 int64_t most_pieces(const AdaptArgs& a) { return cdiv(a.n, piece_of(a)) + std::min<int64_t>(a.adapters, a.n); }
@@ -1062,7 +1073,9 @@ Way way_of(int type, int64_t n, int d, int m, const void* x, int64_t ldx, const 
   r.copy_w = w_padded ? type == TYPE_F32 : !fits(w, ldw);  // (padded: whole rows of kp, zero from d on)
   return r;
 }
-// Rows of a tile of `shrink`: each reads its adapter's matrix once.
+// Rows of a tile of `shrink`: each reads its adapter's matrix once.  A call with 16 / 32:
+// 8192 bfloat16 rows of 4096, 16 adapters of 32 ranks 298 / 293, 4096 binary16 of 1000, 32
+// of 64 59 / 51, 2048 bfloat16 of 4096, 4 of 16 48 / 51.
 int shrink_rows(const AdaptArgs& a) { return a.n >= 4096 && a.n >= 64 * (int64_t)a.adapters && a.rank <= 64 ? 32 : 16; }
 int64_t most_tiles(const AdaptArgs& a) { return cdiv(a.n, shrink_rows(a)) + std::min<int64_t>(a.adapters, a.n); }
 // Rows of a workgroup that plans: all of few, else 1024, or a 64th of all.
