@@ -140,8 +140,9 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
                                                16, slot(i) * 8 < left ? vb[i] : kOut, so, 0, 0);
     }
   };
+  auto next = [](int st) { return NST == 2 ? st ^ 1 : st + 1 == NST ? 0 : st + 1; };
   auto advance = [&]() {
-    fst = fst + 1 == NST ? 0 : fst + 1;
+    fst = next(fst);
     if (++fc < c1 && ++fk == nkc) {
       fk = 0;
       ++fs;
@@ -196,7 +197,7 @@ __device__ inline void tile_product(const Side& a, const Side& b, int64_t row0, 
   for (int c = c0; c < c1; ++c) {
     // (the chunk fetched goes into the stage of chunk c - 1, which everyone has read)
     const char* st = lds + cst * S::stage_bytes;
-    cst = cst + 1 == NST ? 0 : cst + 1;
+    cst = next(cst);
 #pragma unroll
     for (int k = 0; k < NS - 1; ++k) multiply(k, st, k + 1);
     arrive();

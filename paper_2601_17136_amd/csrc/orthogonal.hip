@@ -158,42 +158,92 @@ __global__ __launch_bounds__(256) void flat_gram_kernel(Source q, bool tall, int
   }
 }
 
-// C = A B of symmetric S16 x S16 matrices in LDS, a wavefront's blocks at a time.
-template <int SB, int LD>
-__device__ inline void square_product(const double* A, const double* B, doublex4 (&acc)[(SB * SB + 3) / 4]) {
+// C = A B of symmetric S16 x S16 matrices in LDS, of COUNT matrices A by one B, a
+// wavefront's blocks at a time.
+template <int SB, int COUNT>
+constexpr int kBlocks = (COUNT * SB * SB + 3) / 4;
+template <int SB, int LD, int COUNT>
+__device__ inline void square_products(const double* const (&A)[COUNT], const double* B,
+                                       doublex4 (&acc)[kBlocks<SB, COUNT>]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
 #pragma unroll
-  for (int t = 0; t < (SB * SB + 3) / 4; ++t) {
-    const int blk = t * 4 + wave;
+  for (int t = 0; t < kBlocks<SB, COUNT>; ++t) {
+    const int blk = t * 4 + wave, of = blk % (SB * SB);
     acc[t] = doublex4{0, 0, 0, 0};
-    if (blk >= SB * SB) continue;
-    const double* pa = A + (blk / SB * 16 + l16) * LD + g;
-    const double* pb = B + (blk % SB * 16 + l16) * LD + g;
+    if (blk >= COUNT * SB * SB) continue;
+    const double* pa = (COUNT > 1 && blk >= SB * SB ? A[COUNT - 1] : A[0]) + (of / SB * 16 + l16) * LD + g;
+    const double* pb = B + (of % SB * 16 + l16) * LD + g;
 #pragma unroll
     for (int k = 0; k < SB * 16; k += 4) acc[t] = __builtin_amdgcn_mfma_f64_16x16x4f64(pa[k], pb[k], acc[t], 0, 0, 0);
   }
 }
-template <int SB, int LD, class F>
-__device__ inline void each_entry(const doublex4 (&acc)[(SB * SB + 3) / 4], F f) {
+template <int SB, int LD, int COUNT, class F>
+__device__ inline void each_entry(const doublex4 (&acc)[kBlocks<SB, COUNT>], F f) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
 #pragma unroll
-  for (int t = 0; t < (SB * SB + 3) / 4; ++t) {
-    const int blk = t * 4 + wave;
-    if (blk >= SB * SB) continue;
+  for (int t = 0; t < kBlocks<SB, COUNT>; ++t) {
+    const int blk = t * 4 + wave, of = blk % (SB * SB);
+    if (blk >= COUNT * SB * SB) continue;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int i = blk / SB * 16 + g + 4 * r, j = blk % SB * 16 + l16;
-      f(i, j, i * LD + j, acc[t][r]);
+      const int i = of / SB * 16 + g + 4 * r, j = of % SB * 16 + l16;
+      f(blk / (SB * SB), i, j, i * LD + j, acc[t][r]);
     }
   }
 }
 
-// The steps on G alone: Q with X_last = Q u.  Bound by the chain of products in one
-// workgroup: five steps of 16 x 16 10 us, of 64 x 64 55.
+// The steps on A = G alone: Q with X_last = Q X, X = u inv, inv returned.  Q's product
+// and A's first are independent and run together (five steps of 16 x 16 in 9.1 us, one
+// after another 9.7).  Starts and ends with a barrier.
+template <int SB, int LD>
+__device__ inline double flat_steps(double* A, double* P, double* Q, const NewtonSteps& c, double eps) {
+  constexpr int S16 = SB * 16;
+  __syncthreads();
+  double tr = 0;
+#pragma unroll
+  for (int i = 0; i < S16; ++i) tr += A[i * LD + i];
+  const double inv = 1.0 / (sqrt(tr) + eps);
+  __syncthreads();
+  for (int e = threadIdx.x; e < S16 * S16; e += 256) A[e / S16 * LD + e % S16] *= inv * inv;
+  __syncthreads();
+  doublex4 one[kBlocks<SB, 1>], two[kBlocks<SB, 2>];
+  for (int s = 0; s < c.steps; ++s) {
+    const bool last = s + 1 == c.steps;
+    square_products<SB, LD, 1>({A}, A, one);
+    const double ca = c.coef[3 * s], cb = c.coef[3 * s + 1], cc = c.coef[3 * s + 2];
+    each_entry<SB, LD, 1>(one, [&](int, int i, int j, int at, double v) {
+      P[at] = (i == j ? ca : 0.0) + cb * A[at] + cc * v;
+      if (s == 0) Q[at] = P[at];
+    });
+    __syncthreads();
+    // Q <- Q P, A <- A P P
+    if (s > 0 && !last) {
+      square_products<SB, LD, 2>({Q, A}, P, two);
+      __syncthreads();
+      each_entry<SB, LD, 2>(two, [&](int which, int, int, int at, double v) { (which ? A : Q)[at] = v; });
+      __syncthreads();
+    } else if (s > 0 || !last) {
+      double* M = s > 0 ? Q : A;
+      square_products<SB, LD, 1>({M}, P, one);
+      __syncthreads();
+      each_entry<SB, LD, 1>(one, [&](int, int, int, int at, double v) { M[at] = v; });
+      __syncthreads();
+    }
+    if (last) break;
+    square_products<SB, LD, 1>({A}, P, one);
+    __syncthreads();
+    each_entry<SB, LD, 1>(one, [&](int, int, int, int at, double v) { A[at] = v; });
+    __syncthreads();
+  }
+  return inv;
+}
+
+// The steps by themselves, of a G in slabs.  Bound by the chain of products in one
+// workgroup: five steps of 16 x 16 9.1 us, of 64 x 64 47.
 template <int SB>
 __global__ __launch_bounds__(256) void flat_steps_kernel(const double* __restrict__ slabs, int count, NewtonSteps c,
                                                          double eps, double* __restrict__ out) {
-  constexpr int S16 = SB * 16, LD = S16 + 2, N = (SB * SB + 3) / 4;
+  constexpr int S16 = SB * 16, LD = S16 + 2;
   __shared__ double A[S16 * LD], P[S16 * LD], Q[S16 * LD];
   const int64_t b = blockIdx.x;
   for (int e = threadIdx.x; e < S16 * S16; e += 256) {
@@ -202,36 +252,7 @@ __global__ __launch_bounds__(256) void flat_steps_kernel(const double* __restric
     for (int k = 0; k < count; ++k) s += slabs[(b * count + k) * (S16 * S16) + e];
     A[e / S16 * LD + e % S16] = s;
   }
-  __syncthreads();
-  double tr = 0;
-  for (int i = 0; i < S16; ++i) tr += A[i * LD + i];
-  const double inv = 1.0 / (sqrt(tr) + eps);
-  __syncthreads();
-  for (int e = threadIdx.x; e < S16 * S16; e += 256) A[e / S16 * LD + e % S16] *= inv * inv;
-  __syncthreads();
-  doublex4 acc[N];
-  for (int s = 0; s < c.steps; ++s) {
-    square_product<SB, LD>(A, A, acc);
-    const double ca = c.coef[3 * s], cb = c.coef[3 * s + 1], cc = c.coef[3 * s + 2];
-    each_entry<SB, LD>(acc, [&](int i, int j, int at, double v) {
-      P[at] = (i == j ? ca : 0.0) + cb * A[at] + cc * v;
-      if (s == 0) Q[at] = P[at];
-    });
-    __syncthreads();
-    if (s > 0) {
-      square_product<SB, LD>(Q, P, acc);
-      __syncthreads();
-      each_entry<SB, LD>(acc, [&](int, int, int at, double v) { Q[at] = v; });
-    }
-    if (s + 1 == c.steps) break;
-    for (int t = 0; t < 2; ++t) {
-      square_product<SB, LD>(A, P, acc);
-      __syncthreads();
-      each_entry<SB, LD>(acc, [&](int, int, int at, double v) { A[at] = v; });
-      __syncthreads();
-    }
-  }
-  __syncthreads();
+  const double inv = flat_steps<SB, LD>(A, P, Q, c, eps);
   for (int e = threadIdx.x; e < S16 * S16; e += 256) out[b * (S16 * S16) + e] = Q[e / S16 * LD + e % S16] * inv;
 }
 

@@ -46,7 +46,7 @@ def _bound(u, coef, dtype, products=None):
 
 SHAPES = [(1, 1, 1), (1, 1, 7), (1, 7, 1), (2, 3, 5), (3, 16, 16), (2, 17, 40), (1, 64, 64), (2, 64, 200), (1, 200, 33),
           (1, 48, 900), (1, 901, 48), (2, 65, 65), (3, 66, 130), (2, 130, 66), (1, 128, 128), (2, 129, 257),
-          (1, 300, 301), (2, 257, 65), (1, 520, 700), (1, 1000, 65), (1, 32, 5000), (1, 5003, 64), (1, 777, 1001)]
+          (1, 300, 301), (2, 257, 65), (1, 520, 700), (1, 1000, 65), (1, 32, 5000), (1, 5003, 64), (2, 32, 761), (1, 1499, 16), (3, 9, 1540), (2, 766, 20), (1, 11, 1600), (1, 25, 800), (1, 777, 1001)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
