@@ -625,7 +625,8 @@ int kkm_distill_grad(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teac
  * binary16 parts at a power of two of each row of x (dy) and of w: 22 bits of an entry
  * down to 2^-17 of its row's largest, 2^-40 of that below; an infinite entry gives NaN.
  * down x and up^T dy are fp32, and of 16-bit matrices two parts of 16 bits together (22
- * of binary16) in their second products, two of 16 bits in the adapters' gradients. */
+ * of binary16) in their second products, two of 16 bits in the adapters' gradients: an
+ * infinite one gives NaN. */
 #define KKM_MAX_RANK 128
 #define KKM_MAX_ADAPTERS 1024
 typedef struct kkm_adapted {
@@ -671,7 +672,7 @@ int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, 
  * beside the 0.0017 of its rounding.  Steps
  * that would let a singular value of at most 1 grow past 2^12 are refused.  A NaN or
  * infinity spoils its matrix.  Scratch: 24 bytes an entry of matrices more than 64
- * wide and high (of a batch, as many at a time as 1 GB holds). */
+ * wide and high (of a batch, as many at a time as 1 GB holds); others at most 256 MB. */
 #define KKM_MAX_STEPS 32
 typedef struct kkm_newton {
   int32_t steps;      /* in [1, KKM_MAX_STEPS] */

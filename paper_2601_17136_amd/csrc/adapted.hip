@@ -354,7 +354,7 @@ __global__ __launch_bounds__(1024) void shrink_rows_kernel(const T* __restrict__
       }
       s = wave_sum(s);
     }
-    if (lane == 0) t[row * R + r] = s * f;
+    if (lane == 0) t[row * R + r] = r < rank ? s * f : 0.f;  // (zero from rank on, at any f)
   }
 }
 

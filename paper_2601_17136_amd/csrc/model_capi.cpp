@@ -140,6 +140,11 @@ int check_apart(kkm_ctx* c, const char* name, int64_t batch, int64_t m, int64_t 
   return KKM_OK;
 }
 
+// A result in its input's place lies as it does.
+int check_in_place(kkm_ctx* c, const char* what, bool same) {
+  return same ? KKM_OK : ctx_fail(c, KKM_ERR_ARG, "%s of another stride", what);
+}
+
 int ortho_call(kkm_ctx* c, const char* what, OrthoArgs& a) {
   void* ws = nullptr;
   if (const size_t bytes = ortho_scratch(a))
@@ -166,10 +171,10 @@ int check_choice(kkm_ctx* c, const kkm_choice* q) {
                     (double)q->frequency);
   if (q->nbias < 0 || q->nbias > KKM_MAX_BIASES)
     return ctx_fail(c, KKM_ERR_ARG, "nbias=%d must be in [0, %d]", q->nbias, KKM_MAX_BIASES);
+  if (q->nmasks < 0) return ctx_fail(c, KKM_ERR_ARG, "nmasks=%d must not be negative", q->nmasks);
   if (q->masks) {
     if (q->words < (q->classes + 31) / 32)
       return ctx_fail(c, KKM_ERR_ARG, "words=%lld must be at least %d", (long long)q->words, (q->classes + 31) / 32);
-    if (q->nmasks < 0) return ctx_fail(c, KKM_ERR_ARG, "nmasks=%d must not be negative", q->nmasks);
     if (!q->mask_ids && q->nmasks < q->n)
       return ctx_fail(c, KKM_ERR_ARG, "nmasks=%d must be at least n=%lld without mask_ids", q->nmasks, (long long)q->n);
   } else if (q->mask_ids) {
@@ -386,6 +391,8 @@ int kkm_orthogonalize(kkm_ctx* c, const kkm_newton* newton, int32_t type, int64_
   if (int rc = check_apart(c, "stride_y", batch, m, n, ldy, stride_y)) return rc;
   if (batch > 0 && !x) return missing(c, "x");
   if (batch > 0 && !y) return missing(c, "y");
+  if (batch > 0 && x == y)
+    if (int rc = check_in_place(c, "y is x", (m == 1 || ldx == ldy) && (batch <= 1 || stride_x == stride_y))) return rc;
   a.type = type;
   a.batch = batch;
   a.m = m;
@@ -445,6 +452,8 @@ int kkm_choose(kkm_ctx* c, const kkm_choice* q, void* out, int64_t ldo, int32_t*
     if (q->ngiven && !q->given) return missing(c, "given");
     if (q->nbias && !q->bias_ids) return missing(c, "bias_ids");
     if (q->nbias && !q->bias) return missing(c, "bias");
+    if (out == q->z)
+      if (int rc = check_in_place(c, "out is z", q->n == 1 || ldo == q->ldz)) return rc;
   }
   ChooseArgs a{};
   a.type = q->type;

@@ -202,7 +202,7 @@ __device__ inline double flat_steps(double* A, double* P, double* Q, const Newto
   double tr = 0;
 #pragma unroll
   for (int i = 0; i < S16; ++i) tr += A[i * LD + i];
-  const double inv = 1.0 / (sqrt(tr) + eps);
+  const double inv = 1.0 / fmax(sqrt(tr) + eps, 1e-100);  // (fp32's smallest is 1e-45: of a zero matrix and eps below)
   __syncthreads();
   for (int e = threadIdx.x; e < S16 * S16; e += 256) A[e / S16 * LD + e % S16] *= inv * inv;
   __syncthreads();
@@ -591,7 +591,13 @@ int flat_splits(const OrthoArgs& a) {
 }
 int flat_side(const OrthoArgs& a) { return (int)cdiv(std::min(a.m, a.n), 16); }
 bool is_flat(const OrthoArgs& a) { return std::min(a.m, a.n) <= kFlat; }
-constexpr int64_t kBatchLaunch = 65535;
+constexpr size_t kFlatBytes = (size_t)1 << 28;  // scratch of the matrices of a launch, about
+int64_t flat_bytes(const OrthoArgs& a) {
+  return (int64_t)(flat_splits(a) + 1) * flat_side(a) * flat_side(a) * 256 * (int64_t)sizeof(double);
+}
+int64_t flat_group(const OrthoArgs& a) {
+  return std::min<int64_t>({a.batch, 65535, std::max<int64_t>(1, (int64_t)kFlatBytes / flat_bytes(a))});
+}
 
 Source source_of(const OrthoArgs& a, int64_t b0) {
   const size_t size = elem_bytes(a.type);
@@ -608,7 +614,7 @@ hipError_t launch_flat(const OrthoArgs& a, void* scratch, hipStream_t s) {
   const bool tall = a.m > a.n;
   const int64_t chunks = cdiv(std::max(a.m, a.n), kLong);
   const int per = (int)cdiv(chunks, splits);
-  const int64_t group = std::min(a.batch, kBatchLaunch);
+  const int64_t group = flat_group(a);
   double* slabs = (double*)scratch;
   double* Q = slabs + group * splits * (SB * SB * 256);
   const unsigned across = (unsigned)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / std::min<int64_t>(a.batch, 2048)));
@@ -884,8 +890,7 @@ bool newton_in_range(const NewtonSteps& c) {
 size_t ortho_scratch(const OrthoArgs& a) {
   if (a.batch == 0) return 0;
   if (!is_flat(a)) return tiled_plan(a).total;
-  const int sb = flat_side(a);
-  return (size_t)std::min(a.batch, kBatchLaunch) * (flat_splits(a) + 1) * sb * sb * 256 * sizeof(double);
+  return (size_t)(flat_group(a) * flat_bytes(a));
 }
 
 hipError_t launch_ortho(const OrthoArgs& a, void* scratch, hipStream_t s) {

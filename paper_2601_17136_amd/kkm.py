@@ -820,6 +820,8 @@ def kkm_choose(ctx, z, out=None, ids=None, logp=None, lse=None, scale: float = 1
     h, b = _list_width(given, n, "given"), _list_width(bias_ids, n, "bias_ids")
     if b and bias is None:
         raise ValueError("bias_ids need bias")
+    if bias is not None and bias_ids is None:
+        raise ValueError("bias needs bias_ids")
     if masks is not None and masks.dim() != 2:
         raise ValueError(f"masks must be a matrix, got {masks.dim()} dimensions")
     a = kkm_choice(_type_code(z.dtype, "z"), classes, n, pz, ldz, float(scale),

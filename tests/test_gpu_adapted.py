@@ -224,3 +224,23 @@ def test_gradient_against_differences(ctx):
         # y of about 70 + 6 terms and the gradient of 120: each entry's roundings, by the sizes that enter
         room = 400 * ref.U * (size + float((got[name].double().abs() * q.double().abs()).sum()))
         assert abs(slope - want) <= room, (name, slope, want, room)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,r", [(1, 1), (1, 20), (9, 1), (9, 3), (90, 3)])
+def test_an_infinite_factor(ctx, n, r, dtype):
+    """Rows straight from memory: f down x is infinite, of one sign in all of the rank, and
+    so is the row's y; another adapter's rows are as they were."""
+    from paper_2601_17136_amd import kkm
+    d, m, dtype = 24, 10, DTYPES[dtype]
+    x = torch.ones(n, d, device="cuda", dtype=dtype)
+    w = torch.ones(m, d, device="cuda", dtype=dtype)
+    down, up = torch.ones(2, r, d, device="cuda", dtype=dtype), torch.ones(2, m, r, device="cuda", dtype=dtype)
+    up[:, 1::2] = -1
+    f = torch.tensor([float("inf"), 0.5], device="cuda")
+    ids = (torch.arange(n, device="cuda") % 2).to(torch.int32)
+    y = torch.zeros(n, m, device="cuda", dtype=dtype)
+    kkm.kkm_adapted_linear(ctx, x, w, down, up, ids, y, factor=f)
+    sign = up[0, :, 0].float()
+    want = torch.where(ids[:, None] == 0, sign * float("inf"), d + 0.5 * r * d * sign)
+    assert torch.equal(y.float(), want.expand(n, m))  # (small whole numbers and halves: exact in each type)

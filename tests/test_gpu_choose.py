@@ -178,3 +178,15 @@ def test_more_rows_than_a_launch_takes_at_once(ctx):
     kkm.kkm_choose(ctx, z, None, ids, None, lse)
     assert torch.equal(ids.long(), at)
     assert float((lse - torch.log(torch.tensor(V - 1 + 2.718281828459045))).abs().max()) < 1e-5
+
+
+def test_refusals_of_what_a_row_would_overwrite_or_lose(ctx):
+    from paper_2601_17136_amd import kkm
+    buf = torch.randn(400, device="cuda")
+    was = buf.clone()
+    z, out = buf.as_strided((6, 8), (8, 1)), buf.as_strided((6, 8), (9, 1))
+    with pytest.raises(kkm.KKMError):
+        kkm.kkm_choose(ctx, z, out=out)
+    with pytest.raises(ValueError):
+        kkm.kkm_choose(ctx, z, lse=torch.empty(6, device="cuda"), bias=torch.zeros(6, 2, device="cuda"))
+    assert torch.equal(buf, was)

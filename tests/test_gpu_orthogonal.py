@@ -46,7 +46,8 @@ def _bound(u, coef, dtype, products=None):
 
 SHAPES = [(1, 1, 1), (1, 1, 7), (1, 7, 1), (2, 3, 5), (3, 16, 16), (2, 17, 40), (1, 64, 64), (2, 64, 200), (1, 200, 33),
           (1, 48, 900), (1, 901, 48), (2, 65, 65), (3, 66, 130), (2, 130, 66), (1, 128, 128), (2, 129, 257),
-          (1, 300, 301), (2, 257, 65), (1, 520, 700), (1, 1000, 65), (1, 32, 5000), (1, 5003, 64), (2, 32, 761), (1, 1499, 16), (3, 9, 1540), (2, 766, 20), (1, 11, 1600), (1, 25, 800), (1, 777, 1001)]
+          (1, 300, 301), (2, 257, 65), (1, 520, 700), (1, 1000, 65), (1, 32, 5000), (1, 5003, 64), (2, 32, 761), (1, 1499, 16),
+          (3, 9, 1540), (2, 766, 20), (1, 11, 1600), (1, 25, 800), (1, 777, 1001)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -167,3 +168,48 @@ def test_groups_of_a_large_batch(ctx):
     for i in (0, 137, 299):
         want, tol = _bound(x[i], [kkm.KKM_QUINTIC] * 5, torch.bfloat16)
         assert _norms(y[i], want) <= tol
+
+
+@pytest.mark.parametrize("m,n", [(1, 1), (8, 100), (64, 64), (70, 90)])
+@pytest.mark.parametrize("eps", [1e-7, 1e-200, 5e-324])
+def test_zeros_beside_a_small_eps(ctx, m, n, eps):
+    from paper_2601_17136_amd import kkm
+    x = torch.zeros(2, m, n, device="cuda")
+    x[1, 0, 0] = 1e-45
+    y = torch.full_like(x, 7)
+    kkm.kkm_orthogonalize(ctx, x, y, coef=[(1.0, 0.0, 0.0)] * 2, eps=eps)
+    assert bool((y[0] == 0).all())
+    if eps < 1e-45:  # the second is one entry over itself; a few roundings of 2^-22
+        assert abs(float(y[1, 0, 0]) - 1) < 1e-6 and int((y[1] != 0).sum()) == 1
+
+
+def test_in_place_of_another_stride(ctx):
+    from paper_2601_17136_amd import kkm
+    buf = torch.randn(20 * 40, device="cuda")
+    was = buf.clone()
+    x, y = buf.as_strided((6, 8), (8, 1)), buf.as_strided((6, 8), (9, 1))
+    with pytest.raises(kkm.KKMError):
+        kkm.kkm_orthogonalize(ctx, x, y)
+    x, y = buf.as_strided((3, 6, 8), (48, 8, 1)), buf.as_strided((3, 6, 8), (60, 8, 1))
+    with pytest.raises(kkm.KKMError):
+        kkm.kkm_orthogonalize(ctx, x, y)
+    assert torch.equal(buf, was)
+    x, y = buf.as_strided((1, 8), (8, 1)), buf.as_strided((1, 8), (9, 1))  # (a row lies one way)
+    kkm.kkm_orthogonalize(ctx, x, y)
+
+
+def test_scratch_of_many_small_matrices():
+    from paper_2601_17136_amd import kkm
+    c = kkm.kkm_create(kkm.current_stream_handle())
+    x = torch.randn(9000, 64, 64, device="cuda")
+    y, one = torch.empty_like(x), torch.empty_like(x[0])
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    kkm.kkm_orthogonalize(c, x, y)
+    torch.cuda.synchronize()
+    assert free - torch.cuda.mem_get_info()[0] <= 300 << 20  # (256 MB, and the allocator's steps)
+    for i in (0, 4095, 4096, 8999):
+        kkm.kkm_orthogonalize(c, x[i], one)
+        # sums of 64 products in 64 bits, in one part here and in several there, then rounded to fp32 once
+        assert float((y[i] - one).abs().max()) <= 2 * 2.0 ** -24 * 1.3
+    kkm.kkm_destroy(c)

@@ -72,6 +72,11 @@ def test_choice_argument_checks(change, ok):
     assert ok or kkm.kkm_last_error()
 
 
+def test_masks_that_are_not_there_have_no_negative_count():
+    assert kkm.kkm_check_choice_args(_choice(nmasks=-5)) == kkm.KKM_ERR_ARG
+    assert kkm.kkm_check_choice_args(_choice(nmasks=7)) == kkm.KKM_OK
+
+
 def test_limits_match_the_header():
     import os
     src = open(os.path.join(os.path.dirname(kkm.__file__), "..", "include", "kkm.h")).read()
