@@ -497,8 +497,8 @@ __global__ __launch_bounds__(512) void one_row_kernel(ProjectArgs a, const T* __
 // A tile of the sorted rows; the adapters of each 32 rows one after another.  Their
 // products go into sums of their own, of which a row takes its adapter's: what
 // another adapter holds, were it NaN, does not reach it.  Bound by the matrix cores: 8192
-// bfloat16 rows of 4096 by 4096 with 32 ranks 247 to 264 us, 1.04 to 1.12 PFLOP/s; fp32,
-// 20000 of 784 by 1024 132 us, 243 TFLOP/s of fp32 products, 30 of it tiles' ends.
+// bfloat16 rows of 4096 by 4096 with 32 ranks 261 us, 1.06 PFLOP/s; fp32, 20000 of
+// 784 by 1024 133 us, 241 TFLOP/s of fp32 products, 30 of it tiles' ends.
 struct TileProject {
   ProjectArgs a;
   Side x, w;
@@ -515,6 +515,11 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
   int mi, ni;
   tile_of(blockIdx.x, (unsigned)(q.mt * q.nt), q.mt, q.nt, mi, ni);
   const int64_t r0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
+  int bucket[S::WM];  // of row lane % 32 of each 32
+#pragma unroll
+  for (int bi = 0; bi < S::WM; ++bi) bucket[bi] = a.plan.bucket[min(r0 + (wm * S::WM + bi) * 32 + l32, a.n - 1)];
   floatx16 acc[S::WM][S::WN];
   if constexpr (sizeof(T) == 4) {
     pair_product<S, 3>(q.px, q.pw, r0, n0, 0, q.nkc, lds, acc);
@@ -523,13 +528,49 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
     if constexpr (std::is_same<Rows, InOrder>::value) rows.order = a.plan.order;
     tile_product<T, S, Rows>(q.x, q.w, r0, n0, q.K, q.nkc, 1, 0, q.nkc, lds, acc, rows);
   }
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / S::GN, wn = wave % S::GN, l32 = lane & 31, h = lane >> 5;
 #pragma unroll
   for (int bi = 0; bi < S::WM; ++bi) {
     const int b0 = (int)r0 + (wm * S::WM + bi) * 32;
     if (b0 >= a.n) continue;
     const int b1 = (int)min((int64_t)b0 + 32, a.n);
+    // Runs of an adapter, in order, those without one and of none of them last.  As far as
+    // registers go t stays in them, and the next run's entries of up are on their way while
+    // one's are multiplied, both of the first HELD steps of 16 ranks.  A call of 2048
+    // bfloat16 rows of 4096 to 4096, 1024 adapters of 16 128 us, without 172; 512 rows, 512
+    // adapters of 64 160 and 189; 175 fp32 rows of 720 to 699, 48 of 18 40 and 46.  (Four
+    // steps held: 128, 146 and 41, but 183 where 181 for 20000 fp32 rows and 8 adapters.)
+    constexpr int HELD = S::WM * S::WN <= 2 ? 2 : S::WM * S::WN <= 4 ? 1 : 0;
+    const int at = min(b0 + l32, b1 - 1), steps = a.R / 16;
+    const float* tr = a.t + (int64_t)at * a.R;
+    const int te = std::is_same<T, half_t>::value ? a.texp[at] : 0;
+    // (of fp32 the halves of a wavefront have half of the ranks each)
+    auto rank0 = [&](int i) { return sizeof(T) == 4 ? h * (a.R / 2) + i * 8 : h * 8 + i * 16; };
+    // fp32, or two parts, 16 bits of bfloat16 and 22 of binary16 at the row's power of two
+    auto coefs = [&](int i, raw_n<8, T>& hi, raw_n<8, T>& lo) {
+      const floatx4 t0 = *(const floatx4*)(tr + rank0(i)), t1 = *(const floatx4*)(tr + rank0(i) + 4);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        float v = c < 4 ? t0[c & 3] : t1[c & 3];
+        if (std::is_same<T, half_t>::value) v = ldexpf(v, te);
+        hi[c] = (T)v;
+        if (sizeof(T) == 2) lo[c] = (T)(v - (float)hi[c]);
+      }
+    };
+    auto fetch = [&](int g, int i, raw_n<8, T> (&up)[S::WN]) {
+#pragma unroll
+      for (int bj = 0; bj < S::WN; ++bj) {
+        const int64_t col = min(n0 + (wn * S::WN + bj) * 32 + l32, (int64_t)a.m - 1);
+        up[bj] = load_n<8>((const T*)a.up + ((int64_t)g * a.m + col) * a.uld, rank0(i), a.rank);
+      }
+    };
+    raw_n<8, T> hi[HELD + 1], lo[HELD + 1], ahead[HELD + 1][S::WN];  // (the last: of the steps past these)
+    int g = __builtin_amdgcn_readlane(bucket[bi], 0);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i < steps && g < a.adapters) {
+        coefs(i, hi[i], lo[i]);
+        fetch(g, i, ahead[i]);
+      }
     if constexpr (sizeof(T) == 4) {
       int ew[S::WN];
 #pragma unroll
@@ -541,76 +582,61 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
         for (int bj = 0; bj < S::WN; ++bj) acc[bi][bj][r] = ldexpf(acc[bi][bj][r], -(ex + ew[bj]));
       }
     }
-    for (int p = b0; p < b1;) {
-      const int g = __builtin_amdgcn_readfirstlane(a.plan.bucket[p]);
-      const int e = min(__builtin_amdgcn_readfirstlane(a.plan.start[g + 1]), b1);
+    for (int p = 0; p < b1 - b0;) {
+      const int e = min(p + __popc((unsigned)__ballot(bucket[bi] == g)), b1 - b0);
+      const int then = e < b1 - b0 ? __builtin_amdgcn_readlane(bucket[bi], e) : a.adapters;
       if (g < a.adapters) {
         floatx16 low[S::WN];
 #pragma unroll
         for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
           for (int r = 0; r < 16; ++r) low[bj][r] = 0.f;
-        const int at = min(b0 + l32, b1 - 1);
-        const float* tr = a.t + (int64_t)at * a.R;
-        const T* up[S::WN];
+        auto products = [&](const raw_n<8, T>& hi, const raw_n<8, T>& lo, const raw_n<8, T> (&up)[S::WN]) {
 #pragma unroll
-        for (int bj = 0; bj < S::WN; ++bj)
-          up[bj] = (const T*)a.up + ((int64_t)g * a.m + min(n0 + (wn * S::WN + bj) * 32 + l32, (int64_t)a.m - 1)) * a.uld;
-        if constexpr (sizeof(T) == 4) {  // half h has the ranks of its half
-          for (int k = h * (a.R / 2); k < (h + 1) * (a.R / 2); k += 8) {
-            const floatx4 t0 = *(const floatx4*)(tr + k), t1 = *(const floatx4*)(tr + k + 4);
+          for (int bj = 0; bj < S::WN; ++bj)
+            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int bj = 0; bj < S::WN; ++bj) {
-              const raw_n<8, T> u = load_n<8>(up[bj], k, a.rank);
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(i < 4 ? t0[i & 3] : t1[i & 3], u[i], low[bj], 0, 0, 0);
+              for (int c = 0; c < 8; ++c) low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(hi[c], up[bj][c], low[bj], 0, 0, 0);
+            } else {
+              low[bj] = mfma16(lo, up[bj], low[bj]);
+              low[bj] = mfma16(hi, up[bj], low[bj]);
             }
+        };
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+          if (i < steps) {
+            products(hi[i], lo[i], ahead[i]);
+            if (then < a.adapters) fetch(then, i, ahead[i]);
           }
-        } else {  // t as two parts, 16 bits of bfloat16 and 22 of binary16 at the row's power of two
-          const int te = std::is_same<T, half_t>::value ? a.texp[at] : 0;
-          for (int k = h * 8; k < a.R; k += 16) {
-            const floatx4 t0 = *(const floatx4*)(tr + k), t1 = *(const floatx4*)(tr + k + 4);
-            frag<T> hi, lo;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              float v = i < 4 ? t0[i & 3] : t1[i & 3];
-              if (std::is_same<T, half_t>::value) v = ldexpf(v, te);
-              hi[i] = (T)v;
-              lo[i] = (T)(v - (float)hi[i]);
-            }
-#pragma unroll
-            for (int bj = 0; bj < S::WN; ++bj) {
-              const frag<T> u = load_n<8>(up[bj], k, a.rank);
-              low[bj] = mfma16(lo, u, low[bj]);
-              low[bj] = mfma16(hi, u, low[bj]);
-            }
-          }
-          if constexpr (std::is_same<T, half_t>::value)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int e2 = a.texp[min(b0 + acc_row(r, h), b1 - 1)];
-#pragma unroll
-              for (int bj = 0; bj < S::WN; ++bj) low[bj][r] = ldexpf(low[bj][r], -e2);
-            }
+        for (int i = HELD; i < steps; ++i) {
+          coefs(i, hi[HELD], lo[HELD]);
+          fetch(g, i, ahead[HELD]);
+          products(hi[HELD], lo[HELD], ahead[HELD]);
         }
+        if constexpr (std::is_same<T, half_t>::value)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int e2 = a.texp[min(b0 + acc_row(r, h), b1 - 1)];
+#pragma unroll
+            for (int bj = 0; bj < S::WN; ++bj) low[bj][r] = ldexpf(low[bj][r], -e2);
+          }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int place = b0 + acc_row(r, h);
-          if (place >= p && place < e)
+          const int row = acc_row(r, h);
+          if (row >= p && row < e)
 #pragma unroll
             for (int bj = 0; bj < S::WN; ++bj) acc[bi][bj][r] += low[bj][r];
         }
       } else if (g > a.adapters) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int place = b0 + acc_row(r, h);
-          if (place >= p && place < e)
+          const int row = acc_row(r, h);
+          if (row >= p && row < e)
 #pragma unroll
             for (int bj = 0; bj < S::WN; ++bj) acc[bi][bj][r] = __builtin_nanf("");
         }
       }
-      p = e;
+      p = e, g = then;
     }
   }
   // through LDS, 32 rows of each of GM at a time, so that rows are written 8 entries a lane
