@@ -675,7 +675,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
 // zero from d on; fp32 rows as pairs, kp a whole number of blocks, each at the power of
 // two that brings its largest entry to 2^14 .. 2^15 (`exps`): 22 bits of an entry down to
 // 2^-17 of the row's largest, and 2^-40 of that below.  A row with an infinity or NaN is
-// taken as it is.  20000 fp32 rows of 784 and 1024 of w 30 us, 4.4 TB/s.
+// taken as it is.  20000 fp32 rows of 784 and 1024 of w 32 us, 4.1 TB/s.
 struct CopyJob {
   const void* src;
   int64_t ld, rows;
@@ -846,7 +846,7 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
 // them a lane's, whose 8 x 8 values it turns in registers so that a column's 8 rows lie
 // together.  coef is two bfloat16 parts (16 bits, at any size); a binary16 row is two as
 // well, which hold all of it, and three products.  8192 bfloat16 rows of 4096 + 4096 and
-// 32 ranks: 44 us, 3.0 TB/s, where the fp32 matrix cores take 78.
+// 32 ranks: 39 us, 3.4 TB/s, where the fp32 matrix cores take 78.
 template <typename T, int CT>
 __global__ __launch_bounds__(256) void outer16_kernel(OuterJobs q) {
   constexpr int W = 128;
@@ -1340,7 +1340,7 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   if (a.ddown) o.j[count++] = {sc.u, a.x, a.ldx, a.d, sc.down_slabs, (unsigned)cdiv(a.d, W)};
   if (a.dup) o.j[count++] = {sc.t, a.dy, a.lddy, a.m, sc.up_slabs, (unsigned)cdiv(a.m, W)};
   const dim3 grid(o.j[0].bx + o.j[1].bx, (unsigned)most_pieces(a), RB == 8 ? 2 : 1);
-  auto outer = [&](auto ct) {  // (binary16 and 16 ranks: 10.7 us by the fp32 matrix cores, 14.1 in parts; 3001 x 1001 to 777)
+  auto outer = [&](auto ct) {  // (binary16 and 16 ranks: 13.4 us by the fp32 matrix cores, 14.3 in parts; 3001 x 1001 to 777)
     if constexpr (std::is_same<T, bf16_t>::value || (sizeof(T) == 2 && ct.value > 1))
       outer16_kernel<T, ct.value><<<grid, 256, 0, s>>>(o);
     else
