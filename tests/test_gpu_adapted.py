@@ -244,3 +244,21 @@ def test_an_infinite_factor(ctx, n, r, dtype):
     sign = up[0, :, 0].float()
     want = torch.where(ids[:, None] == 0, sign * float("inf"), d + 0.5 * r * d * sign)
     assert torch.equal(y.float(), want.expand(n, m))  # (small whole numbers and halves: exact in each type)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,m,s,r", [(200, 700, 130, 190, 64), (70, 900, 300, 66, 128), (130, 1000, 90, 130, 17),
+                                       (97, 1300, 70, 1000, 33), (600, 3000, 2000, 300, 48)])
+def test_many_adapters_in_a_tile(ctx, n, d, m, s, r, dtype):
+    """Runs of one to three rows in tiles, ranks of two to eight steps, rows without an adapter and of none of them."""
+    x, w, down, up, ids, f, dy = _case(n, d, m, s, r, dtype, n + m, drop=0.1)
+    ids[5], ids[n - 1] = s, s + 7
+    case = (x, w, down, up, ids, f, dy)
+    got = _run(ctx, *case)
+    lost = ids >= s
+    assert torch.isnan(got["y"][lost]).all() and torch.isnan(got["dx"][lost]).all()
+    want, tol = ref.adapted(*case)
+    for k in ("y", "dx"):
+        ref.check(k, got[k][~lost], want[k][~lost], tol[k][~lost])
+    for k in ("ddown", "dup"):
+        ref.check(k, got[k], want[k], tol[k])
