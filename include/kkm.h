@@ -624,9 +624,8 @@ int kkm_distill_grad(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teac
  * More than 64 rows and 2^23 products (n m d) run in tiles.  There fp32 rows are two
  * binary16 parts at a power of two of each row of x (dy) and of w: 22 bits of an entry
  * down to 2^-17 of its row's largest, 2^-40 of that below; an infinite entry gives NaN.
- * down x and up^T dy are fp32, and of 16-bit matrices two parts of 16 bits together (22
- * of binary16) in their second products, two of 16 bits in the adapters' gradients: an
- * infinite one gives NaN. */
+ * down x and up^T dy are fp32, in their second products and the adapters' gradients too
+ * (of 16-bit matrices as three parts, where an infinite one gives NaN). */
 #define KKM_MAX_RANK 128
 #define KKM_MAX_ADAPTERS 1024
 typedef struct kkm_adapted {

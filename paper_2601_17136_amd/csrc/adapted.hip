@@ -17,8 +17,9 @@
 //   outer      (gradient) the adapters' gradients of a piece of an adapter's rows
 //   join       their sums over the pieces
 //
-// t and u are used in fp32 or, beside 16-bit matrices, as two parts of 16 bits: their
-// products are few beside w's.  A row by itself takes one launch, at most 64 rows two.
+// t and u are used in fp32 or, beside 16-bit matrices, as three parts of 16 bits, all of
+// their 24 bits: their products are few beside w's.  A row by itself takes one launch, at
+// most 64 rows two.
 #include <algorithm>
 #include <cmath>
 
@@ -545,15 +546,19 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
     const int te = std::is_same<T, half_t>::value ? a.texp[at] : 0;
     // (of fp32 the halves of a wavefront have half of the ranks each)
     auto rank0 = [&](int i) { return sizeof(T) == 4 ? h * (a.R / 2) + i * 8 : h * 8 + i * 16; };
-    // fp32, or two parts, 16 bits of bfloat16 and 22 of binary16 at the row's power of two
-    auto coefs = [&](int i, raw_n<8, T>& hi, raw_n<8, T>& lo) {
+    // fp32, or three parts: 24 bits of bfloat16, and of binary16 at the row's power of two
+    constexpr int PARTS = sizeof(T) == 4 ? 1 : 3;
+    auto coefs = [&](int i, raw_n<8, T> (&part)[PARTS]) {
       const floatx4 t0 = *(const floatx4*)(tr + rank0(i)), t1 = *(const floatx4*)(tr + rank0(i) + 4);
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         float v = c < 4 ? t0[c & 3] : t1[c & 3];
         if (std::is_same<T, half_t>::value) v = ldexpf(v, te);
-        hi[c] = (T)v;
-        if (sizeof(T) == 2) lo[c] = (T)(v - (float)hi[c]);
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+          part[k][c] = (T)v;
+          v -= (float)part[k][c];
+        }
       }
     };
     auto fetch = [&](int g, int i, raw_n<8, T> (&up)[S::WN]) {
@@ -563,12 +568,12 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
         up[bj] = load_n<8>((const T*)a.up + ((int64_t)g * a.m + col) * a.uld, rank0(i), a.rank);
       }
     };
-    raw_n<8, T> hi[HELD + 1], lo[HELD + 1], ahead[HELD + 1][S::WN];  // (the last: of the steps past these)
+    raw_n<8, T> coef[HELD + 1][PARTS], ahead[HELD + 1][S::WN];  // (the last: of the steps past these)
     int g = __builtin_amdgcn_readlane(bucket[bi], 0);
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
       if (i < steps && g < a.adapters) {
-        coefs(i, hi[i], lo[i]);
+        coefs(i, coef[i]);
         fetch(g, i, ahead[i]);
       }
     if constexpr (sizeof(T) == 4) {
@@ -591,27 +596,28 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
         for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
           for (int r = 0; r < 16; ++r) low[bj][r] = 0.f;
-        auto products = [&](const raw_n<8, T>& hi, const raw_n<8, T>& lo, const raw_n<8, T> (&up)[S::WN]) {
+        auto products = [&](const raw_n<8, T> (&part)[PARTS], const raw_n<8, T> (&up)[S::WN]) {
 #pragma unroll
           for (int bj = 0; bj < S::WN; ++bj)
             if constexpr (sizeof(T) == 4) {
 #pragma unroll
-              for (int c = 0; c < 8; ++c) low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(hi[c], up[bj][c], low[bj], 0, 0, 0);
+              for (int c = 0; c < 8; ++c)
+                low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(part[0][c], up[bj][c], low[bj], 0, 0, 0);
             } else {
-              low[bj] = mfma16(lo, up[bj], low[bj]);
-              low[bj] = mfma16(hi, up[bj], low[bj]);
+#pragma unroll
+              for (int k = PARTS - 1; k >= 0; --k) low[bj] = mfma16(part[k], up[bj], low[bj]);  // small ones first
             }
         };
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
           if (i < steps) {
-            products(hi[i], lo[i], ahead[i]);
+            products(coef[i], ahead[i]);
             if (then < a.adapters) fetch(then, i, ahead[i]);
           }
         for (int i = HELD; i < steps; ++i) {
-          coefs(i, hi[HELD], lo[HELD]);
+          coefs(i, coef[HELD]);
           fetch(g, i, ahead[HELD]);
-          products(hi[HELD], lo[HELD], ahead[HELD]);
+          products(coef[HELD], ahead[HELD]);
         }
         if constexpr (std::is_same<T, half_t>::value)
 #pragma unroll
@@ -844,9 +850,10 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
 
 // As outer_kernel for 16-bit rows, on the 16-bit matrix cores: 32 rows a step, 8 of
 // them a lane's, whose 8 x 8 values it turns in registers so that a column's 8 rows lie
-// together.  coef is two bfloat16 parts (16 bits, at any size); a binary16 row is two as
-// well, which hold all of it, and three products.  8192 bfloat16 rows of 4096 + 4096 and
-// 32 ranks: 39 us, 3.4 TB/s, where the fp32 matrix cores take 78.
+// together.  coef is three bfloat16 parts, all of its 24 bits; a binary16 row is two, which
+// hold all of it, and five products (the sixth lies below the last bit kept).  8192
+// bfloat16 rows of 4096 + 4096 and 32 ranks: 39 us, 3.4 TB/s, where the fp32 matrix cores
+// take 78.
 template <typename T, int CT>
 __global__ __launch_bounds__(256) void outer16_kernel(OuterJobs q) {
   constexpr int W = 128;
@@ -903,14 +910,17 @@ __global__ __launch_bounds__(256) void outer16_kernel(OuterJobs q) {
         const pair v = {xn[u][2 * e], xn[u][2 * e + 1]};
         w[u][e] = u < left ? __builtin_bit_cast(unsigned, v) : 0u;
       }
-    frag<bf16_t> ch[CT], cl[CT];
+    frag<bf16_t> part[3][CT];
 #pragma unroll
     for (int t = 0; t < CT; ++t)
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const float v = u < left ? cn[u][t] : 0.f;
-        ch[t][u] = (bf16_t)v;
-        cl[t][u] = (bf16_t)(v - (float)ch[t][u]);
+        float v = u < left ? cn[u][t] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          part[k][t][u] = (bf16_t)v;
+          v -= (float)part[k][t][u];
+        }
       }
     fetch(p + 128);
     find(p + 256);
@@ -930,17 +940,18 @@ __global__ __launch_bounds__(256) void outer16_kernel(OuterJobs q) {
           xl[u] = (bf16_t)((float)x[u] - (float)xh[u]);
         }
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cl[t], xh, acc[e][t], 0, 0, 0);
-          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch[t], xl, acc[e][t], 0, 0, 0);
-          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch[t], xh, acc[e][t], 0, 0, 0);
-        }
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+          for (int k = 2; k >= 0; --k) {  // small ones first
+            acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[k][t], k == 2 ? xh : xl, acc[e][t], 0, 0, 0);
+            if (k < 2) acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[k][t], xh, acc[e][t], 0, 0, 0);
+          }
       } else {
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cl[t], x, acc[e][t], 0, 0, 0);
-          acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ch[t], x, acc[e][t], 0, 0, 0);
-        }
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+          for (int k = 2; k >= 0; --k)
+            acc[e][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(part[k][t], x, acc[e][t], 0, 0, 0);
       }
     }
   }
