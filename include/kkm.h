@@ -666,9 +666,7 @@ int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, 
  * vectors stay.  batch matrices of m x n, `stride` elements apart, each by itself.
  *
  * A short side of at most 64 runs in 64 bits.  Others run in two binary16 parts (22
- * bits) of each factor, which hold fp32's accuracy; for bfloat16 results X enters A and
- * (b A + c A^2) X with one part (11 bits): 0.0003 to 0.0011 of the result in the 2-norm,
- * beside the 0.0017 of its rounding.  Steps
+ * bits) of each factor, which hold fp32's accuracy, whatever the result's type.  Steps
  * that would let a singular value of at most 1 grow past 2^12 are refused.  A NaN or
  * infinity spoils its matrix.  Scratch: 24 bytes an entry of matrices more than 64
  * wide and high (of a batch, as many at a time as 1 GB holds); others at most 256 MB. */

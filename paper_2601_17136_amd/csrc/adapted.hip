@@ -523,7 +523,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
   for (int bi = 0; bi < S::WM; ++bi) bucket[bi] = a.plan.bucket[min(r0 + (wm * S::WM + bi) * 32 + l32, a.n - 1)];
   floatx16 acc[S::WM][S::WN];
   if constexpr (sizeof(T) == 4) {
-    pair_product<S, 3>(q.px, q.pw, r0, n0, 0, q.nkc, lds, acc);
+    pair_product<S>(q.px, q.pw, r0, n0, 0, q.nkc, lds, acc);
   } else {
     Rows rows;
     if constexpr (std::is_same<Rows, InOrder>::value) rows.order = a.plan.order;

@@ -457,7 +457,7 @@ __device__ inline void half_tile_of(unsigned g, unsigned total, int mt, int nt, 
 // The sums pass through LDS, 32 rows of each of the workgroup's GM at a time, so that
 // base is read and every result written 16 bytes a lane, whole 128-byte blocks in both
 // orders.
-template <class S, int NP, bool LAST, bool JOIN, typename OT>
+template <class S, bool LAST, bool JOIN, typename OT>
 __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q) {
   constexpr int LD = S::BN + 4, ROWS = S::GM * 32, kRatio = S::BM / S::BN;
   static_assert(S::BM % S::BN == 0, "the diagonal's tiles");
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
     a.p += bt * q.stride_a;
     b.p += bt * q.stride_b;
     const int part = past < 0 ? 0 : past % q.splits, parts = past < 0 ? 1 : q.splits;
-    pair_product<S, NP>(a, b, r0, n0, q.nkb * part / parts, q.nkb * (part + 1) / parts, lds, acc);
+    pair_product<S>(a, b, r0, n0, q.nkb * part / parts, q.nkb * (part + 1) / parts, lds, acc);
     if (past >= 0) {
       each([&](float v, int at) { return slab[at] = v; });
       return;
@@ -654,8 +654,8 @@ double largest_even(double b, double c, double top) {
 int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(top))); }
 
 // The tiles of a launch, and what it takes with them, in microseconds: `end`, and a
-// block's time in a full round of 256 tiles and in one of few.  Measured with three
-// products of parts, a Gram matrix and X's product of 4096 / 3000 / 2048 / 1024 square:
+// block's time in a full round of 256 tiles and in one of few.  Measured, a Gram matrix
+// and X's product of 4096 / 3000 / 2048 / 1024 square:
 // 256 x 256 232 / 176 / 121 / 67 and 339 / 195 / 130 / 74, 256 x 128 260 / 92 / 59 / 33 and
 // 347 / 202 / 68 / 36, 128 x 128 232 / 109 / 41 / 20 and 371 / 180 / 54 / 22, 128 x 64 228 /
 // 102 / 46 / 16 and 405 / 176 / 58 / 19, 64 x 64 249 / 106 / 45 / 11 and 473 / 192 / 65 / 13.
@@ -704,7 +704,7 @@ PairRun pair_run(const TileArgs& q, unsigned nb) {
   consider<Pair64>(4, {6, 0.2, 0.225}, q, nb, best, run);
   return run;
 }
-template <class S, int NP, bool LAST, typename OT>
+template <class S, bool LAST, typename OT>
 void launch_shape(TileArgs q, const PairRun& run, unsigned nb, hipStream_t s) {
   q.mt = (int)cdiv(q.M, S::BM);
   q.nt = (int)cdiv(q.N, S::BN);
@@ -712,19 +712,19 @@ void launch_shape(TileArgs q, const PairRun& run, unsigned nb, hipStream_t s) {
   q.splits = run.splits;
   const int tiles = q.half ? q.mt * q.nt - S::BM / S::BN * (q.mt * (q.mt - 1) / 2) : q.mt * q.nt;
   const unsigned blocks = (unsigned)(run.whole + (tiles - run.whole) * run.splits);
-  pair_kernel<S, NP, LAST, false, OT><<<dim3(blocks, nb), S::threads, 0, s>>>(q);
+  pair_kernel<S, LAST, false, OT><<<dim3(blocks, nb), S::threads, 0, s>>>(q);
   if (run.whole < tiles)
-    pair_kernel<S, NP, LAST, true, OT><<<dim3((unsigned)(tiles - run.whole), nb, S::WM), S::threads, 0, s>>>(q);
+    pair_kernel<S, LAST, true, OT><<<dim3((unsigned)(tiles - run.whole), nb, S::WM), S::threads, 0, s>>>(q);
 }
-template <int NP, bool LAST, typename OT>
+template <bool LAST, typename OT>
 void launch_pair(const TileArgs& q, unsigned nb, hipStream_t s) {
   const PairRun run = pair_run(q, nb);
   switch (run.shape) {
-    case 0: return launch_shape<Pair256, NP, LAST, OT>(q, run, nb, s);
-    case 1: return launch_shape<Pair256x128, NP, LAST, OT>(q, run, nb, s);
-    case 2: return launch_shape<Pair128, NP, LAST, OT>(q, run, nb, s);
-    case 3: return launch_shape<Pair128x64, NP, LAST, OT>(q, run, nb, s);
-    default: return launch_shape<Pair64, NP, LAST, OT>(q, run, nb, s);
+    case 0: return launch_shape<Pair256, LAST, OT>(q, run, nb, s);
+    case 1: return launch_shape<Pair256x128, LAST, OT>(q, run, nb, s);
+    case 2: return launch_shape<Pair128, LAST, OT>(q, run, nb, s);
+    case 3: return launch_shape<Pair128x64, LAST, OT>(q, run, nb, s);
+    default: return launch_shape<Pair64, LAST, OT>(q, run, nb, s);
   }
 }
 
@@ -763,15 +763,6 @@ TiledPlan tiled_plan(const OrthoArgs& a) {
   p.total = 2 * (p.x + p.xt + p.a) + p.norm + p.slabs;
   return p;
 }
-
-// Products of parts that a result of type T is worth.  A bfloat16 result is rounded
-// to 2^-9 of itself, 0.0017 in the 2-norm, so X enters its Gram matrix by hi alone (11
-// bits: 0.0003 to 0.0006 of the result) and, beside a X of both parts, its product
-// with B (0.0003 to 0.001 more), where all parts take 12 products of S x S x len, these 8.
-template <typename T>
-constexpr int kGramParts = std::is_same<T, bf16_t>::value ? 1 : 3;
-template <typename T>
-constexpr int kMoveParts = std::is_same<T, bf16_t>::value ? 2 : 3;
 
 template <typename T>
 hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
@@ -813,7 +804,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       g.along = g.across = cc == 0 ? B : A;
       g.ld_along = g.ld_across = p.ldxt;
       g.stride_along = g.stride_across = sa;
-      launch_pair<kGramParts<T>, false, float>(g, nb, s);
+      launch_pair<false, float>(g, nb, s);
       if (cc != 0) {
         g.a = g.b = {A, p.ldxt, p.S};
         g.stride_a = g.stride_b = sa;
@@ -824,7 +815,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
         g.ca = (float)std::ldexp(cb, eb - ea);
         g.cm = (float)std::ldexp(cc, eb - 2 * ea);
         g.along = g.across = B;
-        launch_pair<3, false, float>(g, nb, s);
+        launch_pair<false, float>(g, nb, s);
       }
       const bool last = t + 1 == a.newton.steps;
       top = largest(ca, cb, cc, top);
@@ -847,7 +838,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
       m.cm = (float)std::ldexp(1.0, en - eb - ex);
       if (last) {
         m.out = target_of(a, b0);
-        launch_pair<kMoveParts<T>, true, T>(m, nb, s);
+        launch_pair<true, T>(m, nb, s);
       } else {
         m.along = X[(t + 1) & 1];
         m.ld_along = p.ldx;
@@ -855,7 +846,7 @@ hipError_t launch_tiled(const OrthoArgs& a, void* scratch, hipStream_t s) {
         m.across = XT[(t + 1) & 1];
         m.ld_across = p.ldxt;
         m.stride_across = sxt;
-        launch_pair<kMoveParts<T>, false, float>(m, nb, s);
+        launch_pair<false, float>(m, nb, s);
       }
       ex = en;
     }

@@ -26,17 +26,16 @@ __device__ inline void split_pair(float v, half_t& hi, half_t& lo) {
 }
 
 // acc = the tile at rows row0 of a and col0 of b over blocks [c0, c1) of the
-// contraction.  NP products of parts: 3, or of a's both and b's hi (2), or of hi and
-// hi (1).  Rows past an operand's end read its last one.  Loads go straight to LDS,
-// NST - 1 blocks ahead; a step's operands are read from LDS during the step before,
-// across the block's one barrier too.
-template <class S, int NP>
+// contraction.  Rows past an operand's end read its last one.  Loads go straight to
+// LDS, NST - 1 blocks ahead; a step's operands are read from LDS during the step
+// before, across the block's one barrier too.
+template <class S>
 __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_t row0, int64_t col0, int c0, int c1,
                                     char* lds, floatx16 (&acc)[S::WM][S::WN]) {
 #ifdef __HIP_DEVICE_COMPILE__  // (the host pass knows no buffer resources)
   constexpr unsigned kBound = 0x7ffffff0u;
   constexpr int L = S::LA + S::LB, F = S::WM + S::WN, per = S::WM * S::WN, NST = S::NST;
-  constexpr int M = NP * per, R = F + (NP > 1 ? S::WM : 0) + (NP > 2 ? S::WN : 0);  // products and reads of a step
+  constexpr int M = 3 * per, R = 2 * F;  // products and reads of a step
   constexpr int kAhead = (NST - 2) * L;  // loads that may be on their way when a block has to be there
   static_assert(kAhead < 64, "what the counter holds");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -77,8 +76,8 @@ __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_
     if (fc + 1 < c1) ++fc;
   };
   f16x8 fa[2][2][S::WM], fb[2][2][S::WN];  // [set][part: hi, lo]
-  auto read = [&](int set, const char* st, int k, int i) {  // hi of b and a, lo of a, lo of b
-    const int part = i >= F, o = i < F ? i : i - F < S::WM ? S::WN + i - F : i - F - S::WM;
+  auto read = [&](int set, const char* st, int k, int i) {  // b and a, hi and then lo
+    const int part = i >= F, o = i - part * F;
     const int sl = ((4 * part + 2 * k + h) ^ S::turn(l32)) * 16;
     if (o < S::WN)
       fb[set][part][o] = *(const f16x8*)(st + S::BM * S::row_bytes + ((wn * S::WN + o) * 32 + l32) * S::row_bytes + sl);
@@ -89,7 +88,7 @@ __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_
   auto multiply = [&](int k, const char* st, int kn) {
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      const int p = m / per + 3 - NP, bi = m % per / S::WN, bj = m % S::WN;
+      const int p = m / per, bi = m % per / S::WN, bj = m % S::WN;
       acc[bi][bj] = mfma16(fa[k][p == 1][bi], fb[k][p == 0][bj], acc[bi][bj]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
