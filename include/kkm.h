@@ -623,7 +623,7 @@ int kkm_distill_grad(kkm_ctx *ctx, const kkm_head *head, const kkm_teacher *teac
  *
  * More than 64 rows and 2^23 products (n m d) run in tiles.  There fp32 rows are two
  * binary16 parts at a power of two of each row of x (dy) and of w: 22 bits of an entry
- * down to 2^-17 of its row's largest, 2^-40 of that below; an infinite entry gives NaN.
+ * down to 2^-28 of its row's largest, 2^-50 of that below; an infinite entry gives NaN.
  * down x and up^T dy are fp32, in their second products and the adapters' gradients too
  * (of 16-bit matrices as three parts, where an infinite one gives NaN). */
 #define KKM_MAX_RANK 128
@@ -666,7 +666,10 @@ int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, 
  * vectors stay.  batch matrices of m x n, `stride` elements apart, each by itself.
  *
  * A short side of at most 64 runs in 64 bits.  Others run in two binary16 parts (22
- * bits) of each factor, which hold fp32's accuracy, whatever the result's type.  Steps
+ * bits) of each factor, whatever the result's type: the error's norm is below that of
+ * fp32 products.  An entry is held to 2^-50 of the bound on the singular values, so rows
+ * or columns more than 2^-28 below the others' size, and a matrix whose norm is that far
+ * below eps, have fewer bits of their own.  Steps
  * that would let a singular value of at most 1 grow past 2^12 are refused.  A NaN or
  * infinity spoils its matrix.  Scratch: 24 bytes an entry of matrices more than 64
  * wide and high (of a batch, as many at a time as 1 GB holds); others at most 256 MB. */

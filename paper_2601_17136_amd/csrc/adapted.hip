@@ -680,7 +680,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
 // Copies for the tiles, in sorted order where `order` is not null: 16-bit rows kp wide,
 // zero from d on; fp32 rows as pairs, kp a whole number of blocks, each at the power of
 // two that brings its largest entry to 2^14 .. 2^15 (`exps`): 22 bits of an entry down to
-// 2^-17 of the row's largest, and 2^-40 of that below.  A row with an infinity or NaN is
+// 2^-28 of the row's largest, and 2^-50 of that below.  A row with an infinity or NaN is
 // taken as it is.  20000 fp32 rows of 784 and 1024 of w 32 us, 4.1 TB/s.
 struct CopyJob {
   const void* src;
@@ -1068,13 +1068,13 @@ constexpr double kFewProducts = 1 << 23;  // so many run from the rows as they a
 // rows n x d to m, in 256 x 256 / 256 x 128 / 128 x 128 / 128 x 64 / 64 x 64: 8192 x 4096 to
 // 4096 287 / 313 / 360 / 396 / 478, 1024 x 4096 to 4096 113 / 69 / 62 / 69 / 78, 256 x 4096 to
 // 4096 115 / 67 / 50 / 48 / 40, 20000 x 784 to 256 64 / 49 / 54 / 54 / 53, 3000 x 1000 to 776
-// 59 / 43 / 33 / 38 / 36; fp32, 20000 x 784 to 1024 203 / 178 / 182 / 180 / 198.
+// 59 / 43 / 33 / 38 / 36; fp32, 20000 x 784 to 1024 - / 178 / 182 / 180 / 198.
 struct TileTime {
   int high, wide;
   double end, alone, full;    // 16 bits, 64 indices
   double alone32, full32;     // pairs, 32
 };
-constexpr TileTime kTiles[5] = {{256, 256, 8, 1.45, 2.05, 1.8, 2.6},
+constexpr TileTime kTiles[5] = {{256, 256, 8, 1.45, 2.05, 0, 0},
                                 {256, 128, 6, 0.77, 1.15, 0.85, 1.35},
                                 {128, 128, 5, 0.5, 0.68, 0.5, 0.73},
                                 {128, 64, 4, 0.42, 0.39, 0.33, 0.39},
@@ -1096,9 +1096,9 @@ Way way_of(int type, int64_t n, int d, int m, const void* x, int64_t ldx, const 
   Way r{};
   if (n > kFewRows && (double)n * m * d > kFewProducts) {
     double best = 0;
-    for (int k = 0; k < 5; ++k) {
+    for (int k = type == TYPE_F32 ? 1 : 0; k < 5; ++k) {  // (a pair's two sums are too many for 256 x 256)
       const double t = tile_time(kTiles[k], type == TYPE_F32, n, d, m);
-      if (k == 0 || t < best) best = t, r.tiled = k + 1;
+      if (!r.tiled || t < best) best = t, r.tiled = k + 1;
     }
   }
   r.kp = (int)up_to(d, type == TYPE_F32 ? kPairBlock : 8);
@@ -1215,7 +1215,9 @@ hipError_t launch_tiles(const ProjectArgs& a, const Way& w, const Scratch& sc, h
 template <typename T>
 hipError_t launch_project(const ProjectArgs& a, const Way& w, const Scratch& sc, hipStream_t s) {
   switch (w.tiled) {
-    case 1: return launch_tiles<T, BigTile>(a, w, sc, s);
+    case 1:
+      if constexpr (sizeof(T) == 2) return launch_tiles<T, BigTile>(a, w, sc, s);
+      break;
     case 2: return launch_tiles<T, TileShape<2, 2, 4, 2, 3>>(a, w, sc, s);
     case 3: return launch_tiles<T, TileShape<1, 2, 4, 2, 4>>(a, w, sc, s);
     case 4: return launch_tiles<T, TileShape<2, 1, 2, 2, 3>>(a, w, sc, s);

@@ -13,7 +13,9 @@
 //   step.  A and A^2 are symmetric, so only tiles on and above their diagonals are
 //   multiplied.  Two parts hold 22 bits at a fixed power of two: a host-side bound
 //   on the singular values after each step keeps every entry in range.  Measured
-//   against 64 bits their error is 0.4 to 0.9 of that of fp32 products.
+//   against 64 bits their error is 0.4 to 0.9 of that of fp32 products; of rows or
+//   columns 1e-7 times the others it is 3 times, of 1e-9 times 300 times, since entries
+//   end at 2^-50 of that bound.
 //
 // Microseconds, flat / tiled, fp32: 64 x 64 69 / 68, 64 x 784 98 / 94, 8 of 48 x 784 68 / 99,
 // 64 x 4096 145 / 197, 33 x 50000 148 / 1585.
@@ -535,7 +537,7 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void pair_kernel(TileArgs q)
         const half_t* from = base + row * q.ld_base + pair_at(col);
         const f16x8 hi = *(const f16x8*)from, lo = *(const f16x8*)(from + kPairBlock);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] += q.ca * ((float)hi[k] + (float)lo[k]);
+        for (int k = 0; k < 8; ++k) v[k] += q.ca * join_pair(hi[k], lo[k]);
       }
       if constexpr (LAST) {
         if (in) put<OT>(q.out, bt, row, col, (int)min(q.N - col, (int64_t)8), v);
@@ -655,11 +657,9 @@ int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(to
 
 // The tiles of a launch, and what it takes with them, in microseconds: `end`, and a
 // block's time in a full round of 256 tiles and in one of few.  Measured, a Gram matrix
-// and X's product of 4096 / 3000 / 2048 / 1024 square:
-// 256 x 256 232 / 176 / 121 / 67 and 339 / 195 / 130 / 74, 256 x 128 260 / 92 / 59 / 33 and
+// and X's product of 4096 / 3000 / 2048 / 1024 square: 256 x 128 260 / 92 / 59 / 33 and
 // 347 / 202 / 68 / 36, 128 x 128 232 / 109 / 41 / 20 and 371 / 180 / 54 / 22, 128 x 64 228 /
 // 102 / 46 / 16 and 405 / 176 / 58 / 19, 64 x 64 249 / 106 / 45 / 11 and 473 / 192 / 65 / 13.
-using Pair256 = BigTile;                        // 128 KB
 using Pair256x128 = TileShape<2, 2, 4, 2, 3>;   // 144 KB
 using Pair128 = TileShape<1, 2, 4, 2, 4>;       // 128 KB
 using Pair128x64 = TileShape<2, 1, 2, 2, 3>;    // 72 KB
@@ -670,8 +670,8 @@ struct PairCost {
 // How a launch runs: in which tiles, how many of them whole, and the parts of the
 // others (1: none), by what it takes.  The tiles past the last full round of 256 leave
 // most CUs idle for a round's time; in parts they take a share of it and a second
-// launch.  A Gram matrix of 4096 in 136 tiles of 256 x 256 232 us, in 256 of 256 x 128 and
-// 16 of 8 parts each 194 and 14.
+// launch.  A Gram matrix of 4096 in 272 tiles of 256 x 128 260 us, in 256 and 16 of 8 parts
+// each 194 and 14.
 struct PairRun {
   int shape, whole, splits;
   int64_t slab;  // floats
@@ -697,11 +697,10 @@ void consider(int shape, const PairCost& c, const TileArgs& q, unsigned nb, doub
 PairRun pair_run(const TileArgs& q, unsigned nb) {
   PairRun run{};
   double best = 0;
-  consider<Pair256>(0, {13, 1.8, 2.6}, q, nb, best, run);
-  consider<Pair256x128>(1, {7, 0.85, 1.35}, q, nb, best, run);
-  consider<Pair128>(2, {6, 0.5, 0.73}, q, nb, best, run);
-  consider<Pair128x64>(3, {6, 0.33, 0.39}, q, nb, best, run);
-  consider<Pair64>(4, {6, 0.2, 0.225}, q, nb, best, run);
+  consider<Pair256x128>(0, {7, 0.85, 1.35}, q, nb, best, run);
+  consider<Pair128>(1, {6, 0.5, 0.73}, q, nb, best, run);
+  consider<Pair128x64>(2, {6, 0.33, 0.39}, q, nb, best, run);
+  consider<Pair64>(3, {6, 0.2, 0.225}, q, nb, best, run);
   return run;
 }
 template <class S, bool LAST, typename OT>
@@ -720,10 +719,9 @@ template <bool LAST, typename OT>
 void launch_pair(const TileArgs& q, unsigned nb, hipStream_t s) {
   const PairRun run = pair_run(q, nb);
   switch (run.shape) {
-    case 0: return launch_shape<Pair256, LAST, OT>(q, run, nb, s);
-    case 1: return launch_shape<Pair256x128, LAST, OT>(q, run, nb, s);
-    case 2: return launch_shape<Pair128, LAST, OT>(q, run, nb, s);
-    case 3: return launch_shape<Pair128x64, LAST, OT>(q, run, nb, s);
+    case 0: return launch_shape<Pair256x128, LAST, OT>(q, run, nb, s);
+    case 1: return launch_shape<Pair128, LAST, OT>(q, run, nb, s);
+    case 2: return launch_shape<Pair128x64, LAST, OT>(q, run, nb, s);
     default: return launch_shape<Pair64, LAST, OT>(q, run, nb, s);
   }
 }

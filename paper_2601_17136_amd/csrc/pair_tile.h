@@ -1,10 +1,13 @@
 // The matrix product of operands held as two binary16 parts, for the products of
 // an orthogonalised update: one workgroup's tile of A B^T.
 //
-// A value v is hi + lo, hi = v rounded to binary16 and lo the rest rounded again:
-// 22 bits, at a power of two chosen so that the largest entry stays in range.  A
-// product is lo hi + hi lo + hi hi (lo lo lies below the last bit kept) on the
-// 16-bit matrix cores, sums in fp32.
+// A value v is hi + 2^-11 lo, hi = v rounded to binary16 and lo 2^11 times the rest
+// rounded again, at a power of two chosen so that the largest entry stays in range:
+// 22 bits, as long as hi has its 11 (down to 2^-28 of a largest of 2^14), and 2^-50 of
+// the largest below.  (lo at hi's own power kept 22 bits down to 2^-17 only and 2^-39
+// below: binary16's smallest step.)  A product is hi hi + 2^-11 (lo hi + hi lo), lo lo
+// lying below the last bit kept, on the 16-bit matrix cores; the two sums are fp32, by
+// themselves, and joined once.
 #pragma once
 #include "head_tile.h"
 
@@ -20,10 +23,12 @@ struct PairSide {
 };
 inline int64_t pair_ld(int64_t k) { return (k + kPairBlock - 1) / kPairBlock * (2 * kPairBlock); }
 __device__ inline int64_t pair_at(int64_t col) { return col / kPairBlock * (2 * kPairBlock) + col % kPairBlock; }
+constexpr float kLoUp = 0x1p11f, kLoDown = 0x1p-11f;
 __device__ inline void split_pair(float v, half_t& hi, half_t& lo) {
   hi = (half_t)v;
-  lo = (half_t)(v - (float)hi);
+  lo = (half_t)((v - (float)hi) * kLoUp);
 }
+__device__ inline float join_pair(half_t hi, half_t lo) { return (float)hi + (float)lo * kLoDown; }
 
 // acc = the tile at rows row0 of a and col0 of b over blocks [c0, c1) of the
 // contraction.  Rows past an operand's end read its last one.  Loads go straight to
@@ -53,12 +58,13 @@ __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_
     const int64_t r = col0 + (wave * S::LB + j) * S::group + lrow;
     vb[j] = (unsigned)((min(r, b.rows - 1) - col0) * b.ld * 2) + slot(j) * 16;
   }
+  floatx16 low[S::WM][S::WN];  // lo hi + hi lo
 #pragma unroll
   for (int bi = 0; bi < S::WM; ++bi)
 #pragma unroll
     for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[bi][bj][r] = 0.f;
+      for (int r = 0; r < 16; ++r) acc[bi][bj][r] = low[bi][bj][r] = 0.f;
   const auto ra = __builtin_amdgcn_make_buffer_rsrc((void*)(a.p + row0 * a.ld), 0, kBound, 0x00027000);
   const auto rb = __builtin_amdgcn_make_buffer_rsrc((void*)(b.p + col0 * b.ld), 0, kBound, 0x00027000);
   int fc = c0, fst = 0;  // the block being fetched (past the last it is that one again), and its stage
@@ -84,12 +90,13 @@ __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_
     else
       fa[set][part][o - S::WN] = *(const f16x8*)(st + ((wm * S::WM + o - S::WN) * 32 + l32) * S::row_bytes + sl);
   };
-  // Small products first: of b's lo, of a's lo, of hi and hi.
+  // Products of b's lo, of a's lo, of hi and hi.
   auto multiply = [&](int k, const char* st, int kn) {
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       const int p = m / per, bi = m % per / S::WN, bj = m % S::WN;
-      acc[bi][bj] = mfma16(fa[k][p == 1][bi], fb[k][p == 0][bj], acc[bi][bj]);
+      floatx16& sum = p == 2 ? acc[bi][bj] : low[bi][bj];
+      sum = mfma16(fa[k][p == 1][bi], fb[k][p == 0][bj], sum);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = m * R / M; j < (m + 1) * R / M; ++j) read(k ^ 1, st, kn, j);
@@ -126,6 +133,12 @@ __device__ inline void pair_product(const PairSide& a, const PairSide& b, int64_
     multiply(1, lds + cst * S::stage_bytes, 0);
     advance();
   }
+#pragma unroll
+  for (int bi = 0; bi < S::WM; ++bi)
+#pragma unroll
+    for (int bj = 0; bj < S::WN; ++bj)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[bi][bj][r] = fmaf(low[bi][bj][r], kLoDown, acc[bi][bj][r]);
   wait_loads();
   __syncthreads();
 #endif
