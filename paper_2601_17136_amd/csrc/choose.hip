@@ -136,7 +136,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 5 : 6) void choose_kernel(Cho
       if (c >= left) continue;
       unsigned out = 0, named = 0;  // bits of the vector's classes
       if (which >= 0 && !lost) out = ~(a.masks[(int64_t)which * a.words + (v0 + c) / 32] >> ((v0 + c) & 31));
-      if (c + VEC > left) out |= ~0u << (left - c);
       if (LISTS) named = used[(own + c) / 32] >> ((own + c) % 32) & ((1u << VEC) - 1);
       float p[VEC];
 #pragma unroll
@@ -167,6 +166,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 5 : 6) void choose_kernel(Cho
           if (b == -INFINITY) out |= 1u << e;
           p[e] = p[e] + b;
         }
+      if (lost) out = 0;  // (NaN, what else is said of a class)
+      if (c + VEC > left) out |= ~0u << (left - c);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         p[e] = p[e] * a.scale;
