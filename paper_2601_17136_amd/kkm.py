@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -199,6 +200,16 @@ def _dev_ptr(t, dtype, name, numel=None):
     if numel is not None and t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements, got {t.numel()}")
     return t.data_ptr()
+
+
+def _shaped(t, dtype, name, shape):
+    """As _dev_ptr, of a tensor of this shape (dimensions of one aside) or of one dimension."""
+    p = _dev_ptr(t, dtype, name, math.prod(shape))
+    if t is None or isinstance(t, int) or t.shape == shape or t.dim() == 1:
+        return p
+    if [v for v in t.shape if v != 1] != [v for v in shape if v != 1]:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return p
 
 
 def current_stream_handle():
@@ -727,8 +738,8 @@ def kkm_adapted_linear_grad(ctx, x, w, down, up, ids, dy, dx=None, ddown=None, d
     pdx, lddx = _rows(dx, "dx", x.dtype, x.shape) if dx is not None else (None, 0)
     with _ordered(ctx, x, w, down, up, ids, dy, dx, ddown, dup, factor):
         _check(lib().kkm_adapted_linear_grad(ctx, ctypes.byref(a), pdy, lddy, pdx, lddx,
-                                             _dev_ptr(ddown, x.dtype, "ddown", down.numel()),
-                                             _dev_ptr(dup, x.dtype, "dup", up.numel())), ctx)
+                                             _shaped(ddown, x.dtype, "ddown", down.shape),
+                                             _shaped(dup, x.dtype, "dup", up.shape)), ctx)
 
 
 def _matrices(t, name, dtype=None, shape=None):
@@ -784,14 +795,14 @@ def kkm_orthogonal_step(ctx, w, g, v, rate: float, momentum: float = 0.95, neste
                         coef=(KKM_QUINTIC,) * 5, eps: float = 1e-7) -> None:
     """v = momentum v + g, u = g + momentum v (nesterov) or v, w = keep w - rate X with
     X from u as in kkm_orthogonalize.  w and g (m x n, or batch x m x n) of one dtype,
-    v fp32 and contiguous."""
+    v fp32, contiguous, of w's shape."""
     import torch
     pw, ldw, sw = _matrices(w, "w")
     pg, ldg, sg = _matrices(g, "g", w.dtype, w.shape)
     a = _newton_args(coef, eps)
     with _ordered(ctx, w, g, v):
         _check(lib().kkm_orthogonal_step(ctx, ctypes.byref(a), _type_code(w.dtype, "w"), *_batch_shape(w), pw, ldw, sw,
-                                         pg, ldg, sg, _dev_ptr(v, torch.float32, "v", w.numel()), float(momentum),
+                                         pg, ldg, sg, _shaped(v, torch.float32, "v", w.shape), float(momentum),
                                          int(nesterov), float(rate), float(keep)), ctx)
 
 
@@ -828,7 +839,7 @@ def kkm_choose(ctx, z, out=None, ids=None, logp=None, lse=None, scale: float = 1
                    _dev_ptr(offset, f32, "offset", classes), _dev_ptr(given, i32, "given") if h else None, h,
                    float(repeat), float(presence), float(frequency),
                    _dev_ptr(bias_ids, i32, "bias_ids") if b else None,
-                   _dev_ptr(bias, f32, "bias", n * b) if b else None, b, _dev_ptr(masks, i32, "masks"),
+                   _shaped(bias, f32, "bias", (n, b)) if b else None, b, _dev_ptr(masks, i32, "masks"),
                    masks.shape[1] if masks is not None else 0, masks.shape[0] if masks is not None else 0,
                    _dev_ptr(mask_ids, i32, "mask_ids", n))
     with _ordered(ctx, z, out, ids, logp, lse, offset, given, bias_ids, bias, masks, mask_ids):
