@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <initializer_list>
 
 #include "kkm.h"
 #include "model_ops.h"
@@ -143,6 +144,17 @@ int check_apart(kkm_ctx* c, const char* name, int64_t batch, int64_t m, int64_t 
 // A result in its input's place lies as it does.
 int check_in_place(kkm_ctx* c, const char* what, bool same) {
   return same ? KKM_OK : ctx_fail(c, KKM_ERR_ARG, "%s of another stride", what);
+}
+
+// A result lies apart from what is still read when it is written, and from other results.
+struct Named {
+  const char* name;
+  const void* p;
+};
+int check_own(kkm_ctx* c, const Named& out, std::initializer_list<Named> others) {
+  for (const Named& o : others)
+    if (out.p && out.p == o.p) return ctx_fail(c, KKM_ERR_ARG, "%s is %s", out.name, o.name);
+  return KKM_OK;
 }
 
 int ortho_call(kkm_ctx* c, const char* what, OrthoArgs& a) {
@@ -355,6 +367,7 @@ int kkm_adapted_linear(kkm_ctx* c, const kkm_adapted* q, void* y, int64_t ldy) {
   if (int rc = check_ld(c, "ldy", ldy, q->m)) return rc;
   if (q->n == 0) return KKM_OK;
   if (!y) return missing(c, "y");
+  if (int rc = check_own(c, {"y", y}, {{"x", q->x}, {"w", q->w}, {"down", q->down}, {"up", q->up}})) return rc;
   AdaptArgs a{};
   a.y = y;
   a.ldy = ldy;
@@ -370,6 +383,10 @@ int kkm_adapted_linear_grad(kkm_ctx* c, const kkm_adapted* q, const void* dy, in
     if (int rc = check_ld(c, "lddx", lddx, q->d)) return rc;
   if (q->n > 0 && !dy) return missing(c, "dy");
   if (!dx && !ddown && !dup) return KKM_OK;
+  for (const Named& out : {Named{"dx", dx}, Named{"ddown", ddown}, Named{"dup", dup}})
+    if (int rc = check_own(c, out, {{"x", q->x}, {"dy", dy}, {"w", q->w}, {"down", q->down}, {"up", q->up}})) return rc;
+  if (int rc = check_own(c, {"dx", dx}, {{"ddown", ddown}, {"dup", dup}})) return rc;
+  if (int rc = check_own(c, {"ddown", ddown}, {{"dup", dup}})) return rc;
   AdaptArgs a{};
   a.dy = dy;
   a.lddy = lddy;
@@ -423,6 +440,7 @@ int kkm_orthogonal_step(kkm_ctx* c, const kkm_newton* newton, int32_t type, int6
   if (batch > 0 && !w) return missing(c, "w");
   if (batch > 0 && !g) return missing(c, "g");
   if (batch > 0 && !v) return missing(c, "v");
+  if (int rc = check_own(c, {"v", v}, {{"w", w}, {"g", g}})) return rc;
   a.type = type;
   a.batch = batch;
   a.m = m;
