@@ -665,7 +665,9 @@ int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, 
  * with its own a, b, c: singular values s become a s + b s^3 + c s^5, singular
  * vectors stay.  batch matrices of m x n, `stride` elements apart, each by itself.
  *
- * A short side of at most 64 runs in 64 bits.  Others run in two binary16 parts (22
+ * A short side of at most 64 runs in 64 bits, also of a matrix that lacks rank; where the
+ * magnitudes of the a's (those above 1) multiply to more than 2^12 in stages, between which
+ * X takes 8 bytes of scratch an entry.  Others run in two binary16 parts (22
  * bits) of each factor, whatever the result's type: the error's norm is below that of
  * fp32 products.  An entry is held to 2^-50 of the bound on the singular values, so rows
  * or columns more than 2^-28 below the others' size, and a matrix whose norm is that far

@@ -8,7 +8,10 @@
 //   steps run on the S x S matrix alone, in LDS, and one product Q u ends them.  A
 //   product of polynomials loses what iterated products of X keep (its small
 //   singular values' accuracy is that of their squares), so G, the steps and Q u
-//   are held in 64 bits, on the 64-bit matrix cores.  |u|^2 is G's trace.
+//   are held in 64 bits, on the 64-bit matrix cores.  |u|^2 is G's trace.  What G's
+//   roundings leave where a singular value is zero, of either sign, a step multiplies
+//   by a^2 as well: after as many steps as multiply by 2^12 the X so far is stored, in
+//   64 bits, and the next ones begin with its own G (Stages).
 // tiled: X and X^T as pairs of binary16 parts (pair_tile.h), three launches a
 //   step.  A and A^2 are symmetric, so only tiles on and above their diagonals are
 //   multiplied.  Two parts hold 22 bits at a fixed power of two: a host-side bound
@@ -42,10 +45,14 @@ struct Source {
   int nesterov;
   int64_t m, n;
 };
+// What the flat form holds of an entry of type T.
+template <typename T>
+using flat_t = typename std::conditional<std::is_same<T, double>::value, double, float>::type;
 // v's new value is written where `update`, else v holds it already.
 template <typename T, bool UPDATE>
-__device__ inline float entry(const Source& q, int64_t b, int64_t i, int64_t j) {
-  const float g = (float)((const T*)q.x)[b * q.stride + i * q.ld + j];
+__device__ inline flat_t<T> entry(const Source& q, int64_t b, int64_t i, int64_t j) {
+  const flat_t<T> g = (flat_t<T>)((const T*)q.x)[b * q.stride + i * q.ld + j];
+  if constexpr (std::is_same<T, double>::value) return g;  // (an X between stages)
   if (!q.v) return g;
   float* p = q.v + (b * q.m + i) * q.n + j;
   float v = *p;
@@ -63,10 +70,13 @@ struct Target {
   int update;
   float rate, keep;
 };
-template <typename T>
-__device__ inline void put(const Target& t, int64_t b, int64_t i, int64_t j, float o) {
+template <typename T, typename O>
+__device__ inline void put(const Target& t, int64_t b, int64_t i, int64_t j, O o) {
   T* p = (T*)t.y + b * t.stride + i * t.ld + j;
-  *p = (T)(t.update ? t.keep * (float)*p - t.rate * o : o);
+  if constexpr (std::is_same<T, double>::value)
+    *p = o;
+  else
+    *p = (T)(t.update ? t.keep * (float)*p - t.rate * (float)o : (float)o);
 }
 // `count` of 8 neighbouring entries of a row.
 template <typename T>
@@ -95,13 +105,15 @@ __device__ inline void put(const Target& t, int64_t b, int64_t i, int64_t j, int
 constexpr int kLong = 64, kLongLd = kLong + 4;  // long-side indices of a chunk; its padded rows in LDS
 
 // The chunk [k0, k0 + 64) of the long side into u[short][long], zero elsewhere.
-template <typename T, bool UPDATE, int SB>
-__device__ inline void load_chunk(const Source& q, int64_t b, int64_t k0, bool tall, float (*u)[kLongLd]) {
+template <typename T, bool UPDATE, int SB, typename U>
+__device__ inline void load_chunk(const Source& q, int64_t b, int64_t k0, bool tall, U (*u)[kLongLd]) {
   const int S = (int)(tall ? q.n : q.m);
   const int64_t len = tall ? q.m : q.n;
   for (int e = threadIdx.x; e < SB * 16 * kLong; e += 256) {
     const int i = tall ? e % (SB * 16) : e / kLong, k = tall ? e / (SB * 16) : e % kLong;
-    u[i][k] = i < S && k0 + k < len ? (tall ? entry<T, UPDATE>(q, b, k0 + k, i) : entry<T, UPDATE>(q, b, i, k0 + k)) : 0.f;
+    U v = 0;
+    if (i < S && k0 + k < len) v = tall ? entry<T, UPDATE>(q, b, k0 + k, i) : entry<T, UPDATE>(q, b, i, k0 + k);
+    u[i][k] = v;
   }
 }
 
@@ -112,7 +124,7 @@ template <typename T, int SB>
 __global__ __launch_bounds__(256) void flat_gram_kernel(Source q, bool tall, int per, double* __restrict__ slabs) {
   constexpr int S16 = SB * 16;
   __shared__ union {
-    float u[S16][kLongLd];
+    flat_t<T> u[S16][kLongLd];
     double red[S16][S16];
   } lds;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
@@ -160,8 +172,10 @@ __global__ __launch_bounds__(256) void flat_gram_kernel(Source q, bool tall, int
   }
 }
 
-// C = A B of symmetric S16 x S16 matrices in LDS, of COUNT matrices A by one B, a
-// wavefront's blocks at a time.
+// C = A B of S16 x S16 matrices in LDS, of COUNT matrices A by one B, a wavefront's
+// blocks at a time.  (They are symmetric but for roundings.  Products with B's rows in
+// the place of its columns multiply what is not by up to 30 a step: 2e-10 off after six
+// steps where these are 1e-13.)
 template <int SB, int COUNT>
 constexpr int kBlocks = (COUNT * SB * SB + 3) / 4;
 template <int SB, int LD, int COUNT>
@@ -174,9 +188,10 @@ __device__ inline void square_products(const double* const (&A)[COUNT], const do
     acc[t] = doublex4{0, 0, 0, 0};
     if (blk >= COUNT * SB * SB) continue;
     const double* pa = (COUNT > 1 && blk >= SB * SB ? A[COUNT - 1] : A[0]) + (of / SB * 16 + l16) * LD + g;
-    const double* pb = B + (of % SB * 16 + l16) * LD + g;
+    const double* pb = B + g * LD + of % SB * 16 + l16;
 #pragma unroll
-    for (int k = 0; k < SB * 16; k += 4) acc[t] = __builtin_amdgcn_mfma_f64_16x16x4f64(pa[k], pb[k], acc[t], 0, 0, 0);
+    for (int k = 0; k < SB * 16; k += 4)
+      acc[t] = __builtin_amdgcn_mfma_f64_16x16x4f64(pa[k], pb[k * LD], acc[t], 0, 0, 0);
   }
 }
 template <int SB, int LD, int COUNT, class F>
@@ -194,59 +209,79 @@ __device__ inline void each_entry(const doublex4 (&acc)[kBlocks<SB, COUNT>], F f
   }
 }
 
-// The steps on A = G alone: Q with X_last = Q X, X = u inv, inv returned.  Q's product
-// and A's first are independent and run together (five steps of 16 x 16 in 9.1 us, one
-// after another 9.7).  Starts and ends with a barrier.
+// The steps [s0, s1) on A = G alone, each by a I + R with R = b A + c A^2: q and Q with
+// X_last = (q I + Q) X, X = u inv, inv returned (1 of an X between stages).  q stays
+// apart because Q alone has no part where a singular value is zero.  Q's product and A's
+// first are independent and run together (five steps of 16 x 16 in 9.1 us, one after
+// another 9.7).  Starts and ends with a barrier.
 template <int SB, int LD>
-__device__ inline double flat_steps(double* A, double* P, double* Q, const NewtonSteps& c, double eps) {
+__device__ inline double flat_steps(double* A, double* R, double* Q, const NewtonSteps& c, int s0, int s1, double eps,
+                                    double& q) {
   constexpr int S16 = SB * 16;
   __syncthreads();
-  double tr = 0;
+  double inv = 1;
+  if (s0 == 0) {
+    double tr = 0;
 #pragma unroll
-  for (int i = 0; i < S16; ++i) tr += A[i * LD + i];
-  const double inv = 1.0 / fmax(sqrt(tr) + eps, 1e-100);  // (fp32's smallest is 1e-45: of a zero matrix and eps below)
-  __syncthreads();
-  for (int e = threadIdx.x; e < S16 * S16; e += 256) A[e / S16 * LD + e % S16] *= inv * inv;
-  __syncthreads();
+    for (int i = 0; i < S16; ++i) tr += A[i * LD + i];
+    inv = 1.0 / fmax(sqrt(tr) + eps, 1e-100);  // (fp32's smallest is 1e-45: of a zero matrix and eps below)
+    __syncthreads();
+    for (int e = threadIdx.x; e < S16 * S16; e += 256) A[e / S16 * LD + e % S16] *= inv * inv;
+    __syncthreads();
+  }
   doublex4 one[kBlocks<SB, 1>], two[kBlocks<SB, 2>];
-  for (int s = 0; s < c.steps; ++s) {
-    const bool last = s + 1 == c.steps;
+  q = 1;
+  for (int s = s0; s < s1; ++s) {
+    const bool first = s == s0, last = s + 1 == s1;
     square_products<SB, LD, 1>({A}, A, one);
     const double ca = c.coef[3 * s], cb = c.coef[3 * s + 1], cc = c.coef[3 * s + 2];
-    each_entry<SB, LD, 1>(one, [&](int, int i, int j, int at, double v) {
-      P[at] = (i == j ? ca : 0.0) + cb * A[at] + cc * v;
-      if (s == 0) Q[at] = P[at];
+    each_entry<SB, LD, 1>(one, [&](int, int, int, int at, double v) {
+      R[at] = cb * A[at] + cc * v;
+      if (first) Q[at] = R[at];
     });
     __syncthreads();
-    // Q <- Q P, A <- A P P
-    if (s > 0 && !last) {
-      square_products<SB, LD, 2>({Q, A}, P, two);
+    // q I + Q <- (q I + Q) (a I + R), A <- A (a I + R)^2
+    auto onto_q = [&](int at, double v) { Q[at] = q * R[at] + (ca * Q[at] + v); };
+    auto onto_a = [&](int at, double v) { A[at] = ca * A[at] + v; };
+    if (!first && !last) {
+      square_products<SB, LD, 2>({Q, A}, R, two);
       __syncthreads();
-      each_entry<SB, LD, 2>(two, [&](int which, int, int, int at, double v) { (which ? A : Q)[at] = v; });
+      each_entry<SB, LD, 2>(two, [&](int which, int, int, int at, double v) {
+        if (which)
+          onto_a(at, v);
+        else
+          onto_q(at, v);
+      });
       __syncthreads();
-    } else if (s > 0 || !last) {
-      double* M = s > 0 ? Q : A;
-      square_products<SB, LD, 1>({M}, P, one);
+    } else if (!first || !last) {
+      square_products<SB, LD, 1>({first ? A : Q}, R, one);
       __syncthreads();
-      each_entry<SB, LD, 1>(one, [&](int, int, int, int at, double v) { M[at] = v; });
+      each_entry<SB, LD, 1>(one, [&](int, int, int, int at, double v) {
+        if (first)
+          onto_a(at, v);
+        else
+          onto_q(at, v);
+      });
       __syncthreads();
     }
+    q *= ca;
     if (last) break;
-    square_products<SB, LD, 1>({A}, P, one);
+    square_products<SB, LD, 1>({A}, R, one);
     __syncthreads();
-    each_entry<SB, LD, 1>(one, [&](int, int, int, int at, double v) { A[at] = v; });
+    each_entry<SB, LD, 1>(one, [&](int, int, int, int at, double v) { onto_a(at, v); });
     __syncthreads();
   }
   return inv;
 }
 
-// The steps by themselves, of a G in slabs.  Bound by the chain of products in one
-// workgroup: five steps of 16 x 16 9.1 us, of 64 x 64 47.
+// The steps of a stage by themselves, of a G in slabs: inv Q and inv q.  Bound by the
+// chain of products in one workgroup: five steps of 16 x 16 9.1 us, of 64 x 64 47.
 template <int SB>
 __global__ __launch_bounds__(256) void flat_steps_kernel(const double* __restrict__ slabs, int count, NewtonSteps c,
-                                                         double eps, double* __restrict__ out) {
+                                                         int s0, int s1, double eps, double* __restrict__ out,
+                                                         double* __restrict__ out_q) {
   constexpr int S16 = SB * 16, LD = S16 + 2;
-  __shared__ double A[S16 * LD], P[S16 * LD], Q[S16 * LD];
+  __shared__ double A[S16 * LD], R[S16 * LD], Q[S16 * LD];
   const int64_t b = blockIdx.x;
   for (int e = threadIdx.x; e < S16 * S16; e += 256) {
     double s = 0;
@@ -254,19 +289,25 @@ __global__ __launch_bounds__(256) void flat_steps_kernel(const double* __restric
     for (int k = 0; k < count; ++k) s += slabs[(b * count + k) * (S16 * S16) + e];
     A[e / S16 * LD + e % S16] = s;
   }
-  const double inv = flat_steps<SB, LD>(A, P, Q, c, eps);
+  double q;
+  const double inv = flat_steps<SB, LD>(A, R, Q, c, s0, s1, eps, q);
+  if (threadIdx.x == 0) out_q[b] = q * inv;
   for (int e = threadIdx.x; e < S16 * S16; e += 256) out[b * (S16 * S16) + e] = Q[e / S16 * LD + e % S16] * inv;
 }
 
-// O = Q u, a chunk of the long side at a time; a wavefront has 16 of its indices.
-template <typename T, int SB>
-__global__ __launch_bounds__(256) void flat_apply_kernel(Source q, bool tall, const double* __restrict__ Qs, Target out) {
+// O = q u + Q u, a chunk of the long side at a time; a wavefront has 16 of its indices.
+// (O may lie on u: a workgroup reads and writes its own chunks.)
+template <typename T, int SB, typename OT>
+__global__ __launch_bounds__(256) void flat_apply_kernel(Source q, bool tall, const double* __restrict__ Qs,
+                                                         const double* __restrict__ qs, Target out) {
   constexpr int S16 = SB * 16, LD = S16 + 2;
-  __shared__ float u[S16][kLongLd];
+  using U = typename std::conditional<std::is_same<OT, double>::value, double, flat_t<T>>::type;
+  __shared__ U u[S16][kLongLd];
   __shared__ double Q[S16 * LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
   const int64_t b = blockIdx.y, len = tall ? q.m : q.n;
   const int S = (int)(tall ? q.n : q.m);
+  const double whole = qs[b];
   for (int e = threadIdx.x; e < S16 * S16; e += 256) Q[e / S16 * LD + e % S16] = Qs[b * (S16 * S16) + e];
   for (int64_t k0 = (int64_t)blockIdx.x * kLong; k0 < len; k0 += (int64_t)gridDim.x * kLong) {
     __syncthreads();
@@ -286,15 +327,18 @@ __global__ __launch_bounds__(256) void flat_apply_kernel(Source q, bool tall, co
 #pragma unroll
     for (int i = 0; i < SB; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) u[i * 16 + g + 4 * r][wave * 16 + l16] = (float)acc[i][r];
+      for (int r = 0; r < 4; ++r) {
+        U& v = u[i * 16 + g + 4 * r][wave * 16 + l16];
+        v = (U)(whole * (double)v + acc[i][r]);
+      }
     __syncthreads();
     for (int e = threadIdx.x; e < S16 * kLong; e += 256) {
       const int i = tall ? e % S16 : e / kLong, k = tall ? e / S16 : e % kLong;
       if (i >= S || k0 + k >= len) continue;
       if (tall)
-        put<T>(out, b, k0 + k, i, u[i][k]);
+        put<OT>(out, b, k0 + k, i, u[i][k]);
       else
-        put<T>(out, b, i, k0 + k, u[i][k]);
+        put<OT>(out, b, i, k0 + k, u[i][k]);
     }
   }
 }
@@ -593,9 +637,23 @@ int flat_splits(const OrthoArgs& a) {
 }
 int flat_side(const OrthoArgs& a) { return (int)cdiv(std::min(a.m, a.n), 16); }
 bool is_flat(const OrthoArgs& a) { return std::min(a.m, a.n) <= kFlat; }
+// Stages of steps: as many together as let no zero singular value's rest grow past 2^12
+// times a rounding, and that X's own roundings, which q I and Q take from each other, past
+// 2^12 of theirs.  Duplicate rows and 32 steps of 3.4445: 1e-12 off; in one stage from
+// the 16th on by as much as the result.
+constexpr double kStageGrowth = 4096;
+int stage_end(const NewtonSteps& c, int s0) {
+  double grown = 1;
+  for (int s = s0; s < c.steps; ++s) {
+    grown *= std::max(1.0, std::fabs(c.coef[3 * s]));
+    if (s > s0 && grown > kStageGrowth) return s;
+  }
+  return c.steps;
+}
 constexpr size_t kFlatBytes = (size_t)1 << 28;  // scratch of the matrices of a launch, about
 int64_t flat_bytes(const OrthoArgs& a) {
-  return (int64_t)(flat_splits(a) + 1) * flat_side(a) * flat_side(a) * 256 * (int64_t)sizeof(double);
+  const int64_t kept = stage_end(a.newton, 0) < a.newton.steps ? a.m * a.n : 0;
+  return ((int64_t)(flat_splits(a) + 1) * flat_side(a) * flat_side(a) * 256 + 1 + kept) * (int64_t)sizeof(double);
 }
 int64_t flat_group(const OrthoArgs& a) {
   return std::min<int64_t>({a.batch, 65535, std::max<int64_t>(1, (int64_t)kFlatBytes / flat_bytes(a))});
@@ -619,12 +677,30 @@ hipError_t launch_flat(const OrthoArgs& a, void* scratch, hipStream_t s) {
   const int64_t group = flat_group(a);
   double* slabs = (double*)scratch;
   double* Q = slabs + group * splits * (SB * SB * 256);
+  double* q = Q + group * (SB * SB * 256);
+  double* kept = q + group;  // the X between stages
+  const Source between{kept, a.n, a.m * a.n, nullptr, 0.f, 0, a.m, a.n};
+  const Target keep{kept, a.n, a.m * a.n, 0, 0.f, 0.f};
   const unsigned across = (unsigned)std::min<int64_t>(chunks, std::max<int64_t>(1, 2048 / std::min<int64_t>(a.batch, 2048)));
   for (int64_t b0 = 0; b0 < a.batch; b0 += group) {
     const unsigned nb = (unsigned)std::min(group, a.batch - b0);
-    flat_gram_kernel<T, SB><<<dim3(splits, nb), 256, 0, s>>>(source_of(a, b0), tall, per, slabs);
-    flat_steps_kernel<SB><<<nb, 256, 0, s>>>(slabs, splits, a.newton, a.eps, Q);
-    flat_apply_kernel<T, SB><<<dim3(across, nb), 256, 0, s>>>(source_of(a, b0), tall, Q, target_of(a, b0));
+    for (int s0 = 0, s1; s0 < a.newton.steps; s0 = s1) {
+      s1 = stage_end(a.newton, s0);
+      const bool last = s1 == a.newton.steps;
+      auto stage = [&](auto from, const Source& src) {
+        using F = decltype(from);
+        flat_gram_kernel<F, SB><<<dim3(splits, nb), 256, 0, s>>>(src, tall, per, slabs);
+        flat_steps_kernel<SB><<<nb, 256, 0, s>>>(slabs, splits, a.newton, s0, s1, a.eps, Q, q);
+        if (last)
+          flat_apply_kernel<F, SB, T><<<dim3(across, nb), 256, 0, s>>>(src, tall, Q, q, target_of(a, b0));
+        else
+          flat_apply_kernel<F, SB, double><<<dim3(across, nb), 256, 0, s>>>(src, tall, Q, q, keep);
+      };
+      if (s0 == 0)
+        stage(T{}, source_of(a, b0));
+      else
+        stage(double{}, between);
+    }
   }
   return hipGetLastError();
 }
