@@ -642,9 +642,10 @@ typedef struct kkm_adapted {
   const float *factor;
 } kkm_adapted;
 
-/* Scratch: 12 bytes a row, 4 a row and rank (padded to 16, 32, 64 or 128); and copies
- * of x and w where the product runs in tiles and they are fp32 (4 bytes an entry), or
- * not of whole 16 bytes or past 2 GB (2). */
+/* Scratch: 16 bytes a row, 4 a row and rank (padded to 16, 32, 64 or 128), and 1 MB; and
+ * copies of x and w where the product runs in tiles and they are fp32 (4 bytes an entry,
+ * rows padded to 32, and 4 a row of each), or not of whole 16 bytes or past 2 GB (2, rows
+ * padded to 8). */
 int kkm_adapted_linear(kkm_ctx *ctx, const kkm_adapted *a, void *y, int64_t ldy);
 
 /* The gradient from dy (n x m); w, which the rows share, is held:
@@ -652,9 +653,10 @@ int kkm_adapted_linear(kkm_ctx *ctx, const kkm_adapted *a, void *y, int64_t ldy)
  *   ddown_g = sum_{i: ids_i = g} u_i x_i^T,  dup_g = sum_{i: ids_i = g} f_g dy_i (down_g x_i)^T
  * into dx (n x d), ddown and dup (as down and up); each may be NULL.  Adapters without
  * rows have zeros, as all have where n = 0.  Rows of an id >= adapters have dx NaN and
- * take no other part.  Scratch beside that above: w, down and up turned, and 4 bytes for
- * each entry of an adapter's gradients and piece of its rows (64 at least; all adapters
- * together at most 1024 pieces and one of each). */
+ * take no other part.  Scratch: 16 bytes a row, 8 a row and rank, and 1 MB; w (rows padded
+ * to 8), down and up turned; copies of dy and of w turned as those of x and w above; and 4
+ * bytes for each entry of an adapter's gradients and piece of its rows (64 at least; all
+ * adapters together at most 1024 pieces and one of each). */
 int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, int64_t lddy, void *dx, int64_t lddx,
                             void *ddown, void *dup);
 
@@ -668,13 +670,15 @@ int kkm_adapted_linear_grad(kkm_ctx *ctx, const kkm_adapted *a, const void *dy, 
  * A short side of at most 64 runs in 64 bits, also of a matrix that lacks rank; where the
  * magnitudes of the a's (those above 1) multiply to more than 2^12 in stages, between which
  * X takes 8 bytes of scratch an entry.  Others run in two binary16 parts (22
- * bits) of each factor, whatever the result's type: the error's norm is below that of
+ * bits) of each factor, whatever the result's type: the error's norm is about that of
  * fp32 products.  An entry is held to 2^-50 of the bound on the singular values, so rows
  * or columns more than 2^-28 below the others' size, and a matrix whose norm is that far
  * below eps, have fewer bits of their own.  Steps
  * that would let a singular value of at most 1 grow past 2^12 are refused.  A NaN or
- * infinity spoils its matrix.  Scratch: 24 bytes an entry of matrices more than 64
- * wide and high (of a batch, as many at a time as 1 GB holds); others at most 256 MB. */
+ * infinity spoils its matrix.  Scratch: of matrices more than 64 wide and high 24 bytes an
+ * entry, both sides rounded up to 32 (of a batch, as many matrices at a time as 1 GB
+ * holds, and one at least), up to 32 MB for a matrix by itself, and 1 MB; of others 256 MB
+ * at most, or what one of them takes: 3 MB and, in stages, 8 bytes an entry. */
 #define KKM_MAX_STEPS 32
 typedef struct kkm_newton {
   int32_t steps;      /* in [1, KKM_MAX_STEPS] */
@@ -723,13 +727,14 @@ typedef struct kkm_choice {
   const float *bias;       /* fp32[n x nbias] */
   int32_t nbias;           /* 0: no lists */
   const uint32_t *masks;   /* nmasks x words: bit v % 32 of word v / 32 allows v; or NULL */
-  int64_t words;           /* >= classes / 32 */
+  int64_t words;           /* >= (classes + 31) / 32 */
   int32_t nmasks;
   const int32_t *mask_ids; /* int32[n]; negative: no mask.  NULL: row i has mask i */
 } kkm_choice;
 
 /* out (n x classes, may be z with its stride), ids (int32[n]), logp and lse
- * (fp32[n]); each may be NULL. */
+ * (fp32[n]); each may be NULL.  Scratch: of more than 4096 classes 16 bytes for each
+ * 4096 of a row. */
 int kkm_choose(kkm_ctx *ctx, const kkm_choice *choice, void *out, int64_t ldo, int32_t *ids, float *logp, float *lse);
 
 /* The checks of these calls that need no context: KKM_OK or KKM_ERR_ARG (the
