@@ -769,9 +769,9 @@ def _matrices(t, name, dtype=None, shape=None):
 
 
 def _newton_args(coef, eps):
-    flat = [float(v) for step in coef for v in step]
-    if len(flat) != 3 * len(coef):
+    if any(len(step) != 3 for step in coef):
         raise ValueError("coef must hold three numbers a step")
+    flat = [float(v) for step in coef for v in step]
     return kkm_newton(len(coef), (ctypes.c_double * max(len(flat), 1))(*flat), float(eps))
 
 
