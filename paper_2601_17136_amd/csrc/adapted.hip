@@ -548,18 +548,22 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
     auto rank0 = [&](int i) { return sizeof(T) == 4 ? h * (a.R / 2) + i * 8 : h * 8 + i * 16; };
     // fp32, or three parts: 24 bits of bfloat16, and of binary16 at the row's power of two
     constexpr int PARTS = sizeof(T) == 4 ? 1 : 3;
-    auto coefs = [&](int i, raw_n<8, T> (&part)[PARTS]) {
+    auto coefs = [&](int i, float (&v)[8]) {
       const floatx4 t0 = *(const floatx4*)(tr + rank0(i)), t1 = *(const floatx4*)(tr + rank0(i) + 4);
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        float v = c < 4 ? t0[c & 3] : t1[c & 3];
-        if (std::is_same<T, half_t>::value) v = ldexpf(v, te);
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) {
-          part[k][c] = (T)v;
-          v -= (float)part[k][c];
-        }
+        v[c] = c < 4 ? t0[c & 3] : t1[c & 3];
+        if (std::is_same<T, half_t>::value) v[c] = ldexpf(v[c], te);
       }
+    };
+    auto next_part = [&](float (&v)[8]) {
+      raw_n<8, T> part;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        part[c] = (T)v[c];
+        v[c] -= (float)part[c];
+      }
+      return part;
     };
     auto fetch = [&](int g, int i, raw_n<8, T> (&up)[S::WN]) {
 #pragma unroll
@@ -568,12 +572,15 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
         up[bj] = load_n<8>((const T*)a.up + ((int64_t)g * a.m + col) * a.uld, rank0(i), a.rank);
       }
     };
-    raw_n<8, T> coef[HELD + 1][PARTS], ahead[HELD + 1][S::WN];  // (the last: of the steps past these)
+    raw_n<8, T> coef[HELD + 1][PARTS], ahead[HELD + 1][S::WN];  // (the last of ahead: of the steps past these)
     int g = __builtin_amdgcn_readlane(bucket[bi], 0);
 #pragma unroll
     for (int i = 0; i < HELD; ++i)
       if (i < steps && g < a.adapters) {
-        coefs(i, coef[i]);
+        float v[8];
+        coefs(i, v);
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) coef[i][k] = next_part(v);
         fetch(g, i, ahead[i]);
       }
     if constexpr (sizeof(T) == 4) {
@@ -596,28 +603,29 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
         for (int bj = 0; bj < S::WN; ++bj)
 #pragma unroll
           for (int r = 0; r < 16; ++r) low[bj][r] = 0.f;
-        auto products = [&](const raw_n<8, T> (&part)[PARTS], const raw_n<8, T> (&up)[S::WN]) {
+        auto products = [&](const raw_n<8, T>& part, const raw_n<8, T> (&up)[S::WN]) {
 #pragma unroll
           for (int bj = 0; bj < S::WN; ++bj)
             if constexpr (sizeof(T) == 4) {
 #pragma unroll
-              for (int c = 0; c < 8; ++c)
-                low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(part[0][c], up[bj][c], low[bj], 0, 0, 0);
+              for (int c = 0; c < 8; ++c) low[bj] = __builtin_amdgcn_mfma_f32_32x32x2f32(part[c], up[bj][c], low[bj], 0, 0, 0);
             } else {
-#pragma unroll
-              for (int k = PARTS - 1; k >= 0; --k) low[bj] = mfma16(part[k], up[bj], low[bj]);  // small ones first
+              low[bj] = mfma16(part, up[bj], low[bj]);
             }
         };
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
           if (i < steps) {
-            products(coef[i], ahead[i]);
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) products(coef[i][k], ahead[i]);
             if (then < a.adapters) fetch(then, i, ahead[i]);
           }
         for (int i = HELD; i < steps; ++i) {
-          coefs(i, coef[HELD]);
+          float v[8];
+          coefs(i, v);
           fetch(g, i, ahead[HELD]);
-          products(coef[HELD], ahead[HELD]);
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k) products(next_part(v), ahead[HELD]);  // (a part at a time: fewer registers)
         }
         if constexpr (std::is_same<T, half_t>::value)
 #pragma unroll
@@ -1205,10 +1213,12 @@ hipError_t launch_tiles(const ProjectArgs& a, const Way& w, const Scratch& sc, h
   q.mt = (int)cdiv(a.n, S::BM);
   q.nt = (int)cdiv(a.m, S::BN);
   const unsigned grid = (unsigned)(q.mt * q.nt);
-  if (sizeof(T) == 2 && w.gather)
-    project_kernel<T, S, InOrder><<<grid, S::threads, 0, s>>>(q);
-  else
-    project_kernel<T, S, AsTheyAre><<<grid, S::threads, 0, s>>>(q);
+  if constexpr (sizeof(T) == 2)
+    if (w.gather) {
+      project_kernel<T, S, InOrder><<<grid, S::threads, 0, s>>>(q);
+      return hipGetLastError();
+    }
+  project_kernel<T, S, AsTheyAre><<<grid, S::threads, 0, s>>>(q);
   return hipGetLastError();
 }
 

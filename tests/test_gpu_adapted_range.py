@@ -100,3 +100,18 @@ def test_infinities_and_nan_stay_in_their_rows(ctx, n, d, m, s, r):
     for k, got in _both(ctx, x, w, down, up, ids).items():
         assert torch.isnan(got[lost]).all()  # (an infinite entry has no parts)
         ref.check(k, got[~lost], want[~lost], tol[~lost])
+
+
+@pytest.mark.parametrize("n,d,m,s,r", SHAPES + [(2100, 4096, 1024, 2, 4)])
+def test_beside_fp32_products(ctx, n, d, m, s, r):
+    """No further from 64 bits than twice a library's fp32 product, which a product of one part each is not."""
+    x, w, down, up, ids = _case(n, d, m, s, r)
+    ids.fill_(-1)
+    want = x.double() @ w.double().t()
+    room = 2 * float(((x @ w.t()).double() - want).norm()) + 2 * U * float(want.norm())
+    one = x.half().double() @ w.half().double().t()
+    assert float((one - want).norm()) > 4 * room
+    for k, got in _both(ctx, x, w, down, up, ids).items():
+        off = float((got.double() - want).norm())
+        print(f"[gpu] {k} n={n} d={d} m={m}: {off / room:.2g} of the room", flush=True)
+        assert off <= room
