@@ -498,8 +498,8 @@ __global__ __launch_bounds__(512) void one_row_kernel(ProjectArgs a, const T* __
 // A tile of the sorted rows; the adapters of each 32 rows one after another.  Their
 // products go into sums of their own, of which a row takes its adapter's: what
 // another adapter holds, were it NaN, does not reach it.  Bound by the matrix cores: 8192
-// bfloat16 rows of 4096 by 4096 with 32 ranks 261 us, 1.06 PFLOP/s; fp32, 20000 of
-// 784 by 1024 133 us, 241 TFLOP/s of fp32 products, 30 of it tiles' ends.
+// bfloat16 rows of 4096 by 4096 with 32 ranks 256 us, 1.07 PFLOP/s; fp32, 20000 of
+// 784 by 1024 130 us, 247 TFLOP/s of fp32 products, 30 of it tiles' ends.
 struct TileProject {
   ProjectArgs a;
   Side x, w;
@@ -537,10 +537,10 @@ __global__ __launch_bounds__(S::threads, S::per_cu) void project_kernel(TileProj
     // Runs of an adapter, in order, those without one and of none of them last.  As far as
     // registers go t stays in them, and the next run's entries of up are on their way while
     // one's are multiplied, both of the first HELD steps of 16 ranks.  A call of 2048
-    // bfloat16 rows of 4096 to 4096, 1024 adapters of 16 128 us, without 172; 512 rows, 512
-    // adapters of 64 160 and 189; 175 fp32 rows of 720 to 699, 48 of 18 40 and 46.  (Four
-    // steps held: 128, 146 and 41, but 183 where 181 for 20000 fp32 rows and 8 adapters.)
-    constexpr int HELD = S::WM * S::WN <= 2 ? 2 : S::WM * S::WN <= 4 ? 1 : 0;
+    // bfloat16 rows of 4096 to 4096, 1024 adapters of 16 130 us, without 149; 512 rows, 512
+    // adapters of 64 150 and 181, with half as many steps held 173; 175 fp32 rows of 720 to
+    // 699, 48 of 18 40 and 46; 20000 fp32 rows of 784 to 1024, 8 of 8 170 each way.
+    constexpr int HELD = S::WM * S::WN <= 2 ? 4 : S::WM * S::WN <= 4 ? 2 : 0;
     const int at = min(b0 + l32, b1 - 1), steps = a.R / 16;
     const float* tr = a.t + (int64_t)at * a.R;
     const int te = std::is_same<T, half_t>::value ? a.texp[at] : 0;
@@ -860,7 +860,7 @@ __global__ __launch_bounds__(256) void outer_kernel(OuterJobs q) {
 // them a lane's, whose 8 x 8 values it turns in registers so that a column's 8 rows lie
 // together.  coef is three bfloat16 parts, all of its 24 bits; a binary16 row is two, which
 // hold all of it, and five products (the sixth lies below the last bit kept).  8192
-// bfloat16 rows of 4096 + 4096 and 32 ranks: 39 us, 3.4 TB/s, where the fp32 matrix cores
+// bfloat16 rows of 4096 + 4096 and 32 ranks: 41 us, 3.3 TB/s, where the fp32 matrix cores
 // take 78.
 template <typename T, int CT>
 __global__ __launch_bounds__(256) void outer16_kernel(OuterJobs q) {
@@ -1076,7 +1076,7 @@ constexpr double kFewProducts = 1 << 23;  // so many run from the rows as they a
 // rows n x d to m, in 256 x 256 / 256 x 128 / 128 x 128 / 128 x 64 / 64 x 64: 8192 x 4096 to
 // 4096 287 / 313 / 360 / 396 / 478, 1024 x 4096 to 4096 113 / 69 / 62 / 69 / 78, 256 x 4096 to
 // 4096 115 / 67 / 50 / 48 / 40, 20000 x 784 to 256 64 / 49 / 54 / 54 / 53, 3000 x 1000 to 776
-// 59 / 43 / 33 / 38 / 36; fp32, 20000 x 784 to 1024 - / 178 / 182 / 180 / 198.
+// 59 / 43 / 33 / 38 / 36; fp32, 20000 x 784 to 1024 - / 179 / 180 / 177 / 195.
 struct TileTime {
   int high, wide;
   double end, alone, full;    // 16 bits, 64 indices
@@ -1363,7 +1363,10 @@ hipError_t launch_typed(const AdaptArgs& a, bool grad, void* scratch, hipStream_
   if (a.ddown) o.j[count++] = {sc.u, a.x, a.ldx, a.d, sc.down_slabs, (unsigned)cdiv(a.d, W)};
   if (a.dup) o.j[count++] = {sc.t, a.dy, a.lddy, a.m, sc.up_slabs, (unsigned)cdiv(a.m, W)};
   const dim3 grid(o.j[0].bx + o.j[1].bx, (unsigned)most_pieces(a), RB == 8 ? 2 : 1);
-  auto outer = [&](auto ct) {  // (binary16 and 16 ranks: 13.4 us by the fp32 matrix cores, 14.3 in parts; 3001 x 1001 to 777)
+  // (binary16 of at most 16 ranks, both gradients by the fp32 matrix cores / in parts: 3001 x 1001 to 777, 5 adapters
+  // of 12 35 / 36 us, 4096 x 1000 to 1000, 60 of 16 49 / 57, 20000 x 784 to 1024, 8 of 8 72 / 71, 8192 x 4096 to 4096, 16
+  // of 16 81 / 77)
+  auto outer = [&](auto ct) {
     if constexpr (std::is_same<T, bf16_t>::value || (sizeof(T) == 2 && ct.value > 1))
       outer16_kernel<T, ct.value><<<grid, 256, 0, s>>>(o);
     else
