@@ -20,8 +20,8 @@
 //   columns 1e-7 times the others it is 3 times, of 1e-9 times 300 times, since entries
 //   end at 2^-50 of that bound.
 //
-// Microseconds, flat / tiled, fp32: 64 x 64 69 / 68, 64 x 784 98 / 94, 8 of 48 x 784 68 / 99,
-// 64 x 4096 145 / 197, 33 x 50000 148 / 1585.
+// Microseconds, flat / tiled, fp32: 64 x 64 73 / 68, 64 x 784 102 / 94, 8 of 48 x 784 70 / 99,
+// 64 x 4096 147 / 197, 33 x 50000 150 / 1579.
 #include <algorithm>
 #include <cmath>
 
@@ -212,8 +212,7 @@ __device__ inline void each_entry(const doublex4 (&acc)[kBlocks<SB, COUNT>], F f
 // The steps [s0, s1) on A = G alone, each by a I + R with R = b A + c A^2: q and Q with
 // X_last = (q I + Q) X, X = u inv, inv returned (1 of an X between stages).  q stays
 // apart because Q alone has no part where a singular value is zero.  Q's product and A's
-// first are independent and run together (five steps of 16 x 16 in 9.1 us, one after
-// another 9.7).  Starts and ends with a barrier.
+// first are independent and run together.  Starts and ends with a barrier.
 template <int SB, int LD>
 __device__ inline double flat_steps(double* A, double* R, double* Q, const NewtonSteps& c, int s0, int s1, double eps,
                                     double& q) {
@@ -275,7 +274,7 @@ __device__ inline double flat_steps(double* A, double* R, double* Q, const Newto
 }
 
 // The steps of a stage by themselves, of a G in slabs: inv Q and inv q.  Bound by the
-// chain of products in one workgroup: five steps of 16 x 16 9.1 us, of 64 x 64 47.
+// chain of products in one workgroup: five steps of 16 x 16 9.3 us, of 64 x 64 54.
 template <int SB>
 __global__ __launch_bounds__(256) void flat_steps_kernel(const double* __restrict__ slabs, int count, NewtonSteps c,
                                                          int s0, int s1, double eps, double* __restrict__ out,
@@ -391,7 +390,7 @@ __global__ __launch_bounds__(256) void squares_kernel(Source q, double* __restri
 }
 
 // Pairs of u / (|u| + eps), 2^exp times: `along`'s rows are u's, `across`'s its columns.
-// 4096 x 4096 bfloat16 47 us, 5.0 TB/s.
+// 4096 x 4096 bfloat16 50 us, 4.7 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void pairs_kernel(Source q, const double* __restrict__ part, int count, double eps,
                                                     float up, half_t* along, int64_t ld_along, half_t* across,
@@ -497,8 +496,8 @@ __device__ inline void half_tile_of(unsigned g, unsigned total, int mt, int nt, 
 }
 
 // Bound by the matrix cores where tiles fill the card (4096 square, three products of
-// parts: a square in 188 us, matrix cores busy 79 %; X's product 339, 1.22 PFLOP/s of
-// binary16 products), by a launch's own time where they do not: 1024 x 784 11 us a launch,
+// parts: a square in 186 us, matrix cores busy 78 %; X's product 345, 1.2 PFLOP/s of
+// binary16 products), by a launch's own time where they do not: 1024 x 784 11.5 us a launch,
 // of which its blocks take 5.
 // The sums pass through LDS, 32 rows of each of the workgroup's GM at a time, so that
 // base is read and every result written 16 bytes a lane, whole 128-byte blocks in both
@@ -733,9 +732,9 @@ int room_for(double top) { return 15 - std::max(-30, (int)std::ceil(std::log2(to
 
 // The tiles of a launch, and what it takes with them, in microseconds: `end`, and a
 // block's time in a full round of 256 tiles and in one of few.  Measured, a Gram matrix
-// and X's product of 4096 / 3000 / 2048 / 1024 square: 256 x 128 260 / 92 / 59 / 33 and
-// 347 / 202 / 68 / 36, 128 x 128 232 / 109 / 41 / 20 and 371 / 180 / 54 / 22, 128 x 64 228 /
-// 102 / 46 / 16 and 405 / 176 / 58 / 19, 64 x 64 249 / 106 / 45 / 11 and 473 / 192 / 65 / 13.
+// and X's product of 4096 / 3000 / 2048 / 1024 square: 256 x 128 288 / 98 / 66 / 35 and 345 /
+// 204 / 71 / 34, 128 x 128 269 / 114 / 39 / 22 and 395 / 182 / 52 / 21, 128 x 64 254 / 106 / 44 /
+// 18 and 415 / 177 / 56 / 17, 64 x 64 268 / 110 / 46 / 14 and 475 / 194 / 64 / 13.
 using Pair256x128 = TileShape<2, 2, 4, 2, 3>;   // 144 KB
 using Pair128 = TileShape<1, 2, 4, 2, 4>;       // 128 KB
 using Pair128x64 = TileShape<2, 1, 2, 2, 3>;    // 72 KB
@@ -746,8 +745,8 @@ struct PairCost {
 // How a launch runs: in which tiles, how many of them whole, and the parts of the
 // others (1: none), by what it takes.  The tiles past the last full round of 256 leave
 // most CUs idle for a round's time; in parts they take a share of it and a second
-// launch.  A Gram matrix of 4096 in 272 tiles of 256 x 128 260 us, in 256 and 16 of 8 parts
-// each 194 and 14.
+// launch.  A Gram matrix of 4096 in 272 tiles of 256 x 128 288 us, in 256 and 16 of 8 parts
+// each 182 and 12.
 struct PairRun {
   int shape, whole, splits;
   int64_t slab;  // floats
