@@ -48,7 +48,7 @@ def parts(u, coef, eps, count):
 def beyond(got, want):
     """The norm of what `got` is off by past half a step of its type."""
     _, e = torch.frexp(got.double())
-    half = torch.exp2((e - BITS[got.dtype] - 1).double())
+    half = torch.where(got == 0, 0.0, torch.exp2((e - BITS[got.dtype] - 1).double()))  # (a zero is not rounded to)
     if got.dtype == torch.float16:
         half = half.clamp(min=2.0 ** -25)
     return float(((got.double() - want).abs() - half).clamp(min=0.0).norm())
